@@ -221,14 +221,15 @@ def prepare(case, seed):
         if case["backward"]:
             st["do"] = normal(B, case["Sq"], case["heads"], d)
     if own:        # what a program keeps from call to call: outputs, tables, the plan of the key ranges, workspaces
-        from paper_2506_23858_b200 import binding as vb
-        from paper_2506_23858_b200.layer import RangeAttention, Rotary
         if case["kind"] == "rotary":
+            from paper_2506_23858_b200.layer import Rotary
             st["op"] = Rotary(_shape(case), st["pos"], st["freq"], st["axis"], layout=case["layout"], norm=case["norm"], mscale=m,
                               with_backward=case["backward"])
             out = (B, heads, S, d) if case["order"] == "block" else (B, S, heads, d)
             st["out"] = [torch.empty(out, dtype=dt, device="cuda") for _ in range(2)]
         else:
+            from paper_2506_23858_b200 import binding as vb
+            from paper_2506_23858_b200.layer import RangeAttention
             shape = vb.make_range_shape(B, case["heads"], case["kv_heads"], d, case["Sq"], case["Sk"], case["dtype"],
                                         mask_batch=st["ranges"].shape[0], softcap=case["cap"])
             st["op"] = RangeAttention(shape, st["ranges"], with_backward=case["backward"])
