@@ -323,6 +323,55 @@ int vmoba_full_attn(const vmoba_shape* shape, const void* q, const void* k, cons
                     int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * What video transformers do to q and k on their way into the layer: root-mean-square norm and rotary positions, in one pass over
+ * the tensors, together with the reordering of Eq. 1 if it is wanted (the paper's models do all three; it states no formula).
+ *   y  = x * w / sqrt(mean(x^2) + eps), the mean over a head (VMOBA_ROTARY_NORM_HEAD, w [head_dim]) or over all heads of a token
+ *        (VMOBA_ROTARY_NORM_ROW, w [heads * head_dim]); VMOBA_ROTARY_NORM_NONE: y = x
+ *   pair i of a head, i < pairs, is turned by the angle a = positions[token][axis[i]] * freq[i]:
+ *        out0 = mscale * (y0 cos a - y1 sin a),  out1 = mscale * (y1 cos a + y0 sin a)
+ *        VMOBA_ROTARY_HALF: channels i and i + pairs; VMOBA_ROTARY_INTERLEAVED: channels 2 i and 2 i + 1.
+ *        Channels from 2 * pairs on are y.
+ * Angles are formed and reduced in 64 bits (positions are any int32), everything else is fp32, rounded once.
+ */
+typedef enum { VMOBA_ROTARY_HALF = 0, VMOBA_ROTARY_INTERLEAVED = 1 } vmoba_rotary_layout;
+typedef enum { VMOBA_ROTARY_NORM_NONE = 0, VMOBA_ROTARY_NORM_HEAD = 1, VMOBA_ROTARY_NORM_ROW = 2 } vmoba_rotary_norm;
+typedef struct {
+  int32_t pairs;      /* rotated pairs per head, 0 .. head_dim / 2                                        */
+  int32_t axes;       /* positions per token, 1 .. 4 (frame, row, column, ...)                            */
+  int32_t layout;     /* vmoba_rotary_layout                                                              */
+  int32_t norm;       /* vmoba_rotary_norm                                                                */
+  int32_t pos_batch;  /* 1: all samples share the positions, B: [B, S, axes]                              */
+  float mscale;       /* factor on the sines and cosines (1 unless the context is stretched), > 0         */
+  float eps;          /* of the norm                                                                      */
+} vmoba_rotary_spec;
+
+/*
+ * Forward, n (1 .. 4) tensors of the shape in one launch.  The first `turned` of them are normed and rotated, the others only
+ * moved (v on its way into block order).  src: raster order through element strides {batch, token, head} (rows 16-byte aligned;
+ * strides of zero are fine).  dst: block-major if dst_strides_bsh_or_null is NULL, else raster order through its strides;
+ * in raster order dst[k] may be src[k] with the same strides.  weight_or_null[k]: fp32, 16-byte aligned; NULL: ones.
+ * positions int32 [pos_batch, S, axes], freq fp64 [pairs], axis int32 [pairs] (clamped into the axes there are), all on the
+ * device and unused where pairs is 0.  perm_or_null as for vmoba_partition.
+ */
+int vmoba_rotary(const vmoba_shape* shape, const vmoba_rotary_spec* spec, int32_t n, int32_t turned, const void* const* src,
+                 const int64_t (*src_strides_bsh)[3], void* const* dst, const int64_t (*dst_strides_bsh_or_null)[3],
+                 const float* const* weight_or_null, const int32_t* positions, const double* freq, const int32_t* axis,
+                 int32_t* perm_or_null, void* stream);
+
+/*
+ * Its gradients: dx[k] (raster order) from d_out[k] (raster order, or block-major if d_out_strides_bsh_or_null is NULL) and, with
+ * a norm, from the forward's x[k]; dweight_or_null[k] fp32, the sum over all tokens (and, norm per head, heads).  In raster order
+ * dx[k] may be d_out[k] with the same strides.  Without a norm x and ws may be NULL.  The results repeat bit for bit.
+ * ws: vmoba_rotary_workspace_bytes(shape, spec, n) bytes (0 for an invalid shape or spec).
+ */
+size_t vmoba_rotary_workspace_bytes(const vmoba_shape* shape, const vmoba_rotary_spec* spec, int32_t n);
+int vmoba_rotary_bwd(const vmoba_shape* shape, const vmoba_rotary_spec* spec, int32_t n, const void* const* d_out,
+                     const int64_t (*d_out_strides_bsh_or_null)[3], const void* const* x_or_null,
+                     const int64_t (*x_strides_bsh_or_null)[3], const float* const* weight_or_null, void* const* dx,
+                     const int64_t (*dx_strides_bsh)[3], float* const* dweight_or_null, const int32_t* positions,
+                     const double* freq, const int32_t* axis, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Diagnostics; not part of the method.  Registers a device buffer of 16 uint64 counters (NULL: clears the
  * registration) into which the tensor-core attention kernels launched afterwards ADD, per CTA, the clock
  * cycles that one representative thread of each warp role spent in each section of its loop; divide by the

@@ -23,6 +23,7 @@ EXPORTS = (
     "vmoba_block_scores_range", "vmoba_select", "vmoba_select_rule_apply", "vmoba_select_ranged", "vmoba_select_static", "vmoba_select_static_scratch_bytes", "vmoba_attn_fwd",
     "vmoba_attn_fwd_raster", "vmoba_attn_bwd", "vmoba_attn_bwd_raster",
     "vmoba_attn_bwd_raster_do", "vmoba_full_attn",
+    "vmoba_rotary", "vmoba_rotary_bwd", "vmoba_rotary_workspace_bytes",
     "vmoba_debug_wait_profile", "vmoba_debug_wait_timeout",
 )
 
@@ -31,6 +32,15 @@ class VmobaError(RuntimeError):
     def __init__(self, code, where):
         self.code = code
         super().__init__(f"{where}: status {code} ({status_string(code)})")
+
+
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_NORM_NONE, ROTARY_NORM_HEAD, ROTARY_NORM_ROW = 0, 1, 2
+
+
+class RotarySpec(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("pairs", "axes", "layout", "norm", "pos_batch")] + [
+        ("mscale", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
 class Shape(ctypes.Structure):
@@ -135,6 +145,13 @@ def lib():
     L.vmoba_debug_wait_profile.argtypes = [vp]
     L.vmoba_full_attn.restype = ctypes.c_int
     L.vmoba_full_attn.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    rs = ctypes.POINTER(RotarySpec)
+    L.vmoba_rotary_workspace_bytes.restype = sz
+    L.vmoba_rotary_workspace_bytes.argtypes = [sp, rs, i32]
+    L.vmoba_rotary.restype = ctypes.c_int
+    L.vmoba_rotary.argtypes = [sp, rs, i32, i32] + [vp] * 10
+    L.vmoba_rotary_bwd.restype = ctypes.c_int
+    L.vmoba_rotary_bwd.argtypes = [sp, rs, i32] + [vp] * 12 + [sz, vp]
     _lib = L
     return L
 
@@ -305,6 +322,39 @@ def vmoba_full_attn(shape, q, k, v, o, lse, do=None, dq=None, dk=None, dv=None, 
     _check(lib().vmoba_full_attn(ctypes.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(do),
                                  _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dev_status), p, n, _stream(stream)),
            "vmoba_full_attn")
+
+
+def rotary_workspace_bytes(shape, spec, n) -> int:
+    return int(lib().vmoba_rotary_workspace_bytes(ctypes.byref(shape), ctypes.byref(spec), n))
+
+
+def _pointers(tensors, n):
+    """Host array of n device pointers (None: null), or None for no list at all."""
+    return None if tensors is None else _MANY[n][1](*[None if t is None else t.data_ptr() for t in tensors])
+
+
+def _strides(triples, n):
+    return None if triples is None else _MANY[n][0](*[x for t in triples for x in t])
+
+
+def vmoba_rotary(shape, spec, turned, srcs, src_strides, dsts, dst_strides, weights, positions, freq, axis, perm=None,
+                 stream=None):
+    """Norm and rotation of the first `turned` of up to four tensors, the others moved; dst_strides None: into block order."""
+    n = len(srcs)
+    _check(lib().vmoba_rotary(ctypes.byref(shape), ctypes.byref(spec), n, turned, _pointers(srcs, n), _strides(src_strides, n),
+                              _pointers(dsts, n), _strides(dst_strides, n), _pointers(weights, n), _ptr(positions), _ptr(freq),
+                              _ptr(axis), _ptr(perm), _stream(stream)), "vmoba_rotary")
+
+
+def vmoba_rotary_bwd(shape, spec, d_outs, d_out_strides, xs, x_strides, weights, dxs, dx_strides, dweights, positions, freq, axis,
+                     ws=None, stream=None):
+    """Gradients of vmoba_rotary; d_out_strides None: the gradients that come in are block-major."""
+    n = len(d_outs)
+    p, size = _ws_args(ws)
+    _check(lib().vmoba_rotary_bwd(ctypes.byref(shape), ctypes.byref(spec), n, _pointers(d_outs, n), _strides(d_out_strides, n),
+                                  _pointers(xs, n), _strides(x_strides, n), _pointers(weights, n), _pointers(dxs, n),
+                                  _strides(dx_strides, n), _pointers(dweights, n), _ptr(positions), _ptr(freq), _ptr(axis), p, size,
+                                  _stream(stream)), "vmoba_rotary_bwd")
 
 
 def vmoba_debug_wait_timeout(dev_status, polls, out2=None, stream=None):

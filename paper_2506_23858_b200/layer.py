@@ -6,6 +6,9 @@ intermediate buffers so that tests can compare each stage with the oracle.
 """
 from __future__ import annotations
 
+import contextlib
+import math
+
 import torch
 
 from . import binding as vb
@@ -15,12 +18,143 @@ def torch_dtype(shape):
     return torch.bfloat16 if shape.dtype == vb.BF16 else torch.float32
 
 
+_HERE = contextlib.nullcontext()
+
+
+def _on(device):
+    """The context in which `device` is the current one (nothing to do where it is)."""
+    return _HERE if torch._C._cuda_getDevice() == device.index else torch.cuda.device(device)
+
+
+def _strides_bsh(x):
+    """Element strides (batch, token, head) of a [B, S, heads, d] tensor, as the kernels need them: those of dimensions of size
+    one, which address nothing, are taken for dense ones (torch leaves them at any value)."""
+    n, st = x.shape, list(x.stride()[:3])
+    for i, dense in ((2, n[3]), (1, n[2] * n[3]), (0, n[1] * n[2] * n[3])):
+        if n[i] == 1:
+            st[i] = dense
+    return tuple(st)
+
+
 def default_capacity(shape, tau: float, slack: float = 0.02) -> int:
     """Upper bound on the number of selected pairs: the threshold rule keeps at most ceil(tau*P)
     pairs per head (the kept fraction never exceeds tau, Section 4.1), plus exact ties."""
     P = shape.S * shape.n_blocks
     per_head = int(min(P, tau * P * (1.0 + slack) + 1024))
     return min(per_head * shape.B * shape.heads, 2 ** 31 - 1)
+
+
+def rotary_frequencies(pairs_per_axis, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained: int = 4096):
+    """What Rotary takes, as host tensors: fp64 frequency and int32 axis of every pair, and the factor on sines and cosines.
+
+    Axis a has pairs_per_axis[a] pairs; its pair i turns by theta^(-i / pairs) per position.  scaling, for contexts `factor`
+    times as long as the model was trained on: "linear" (positions interpolated), "base" (theta raised so that the slowest pair is
+    interpolated and the fastest kept), "parts" (pairs that make one turn or less over `trained` positions are interpolated,
+    those of 32 and more kept, a ramp in between; sines and cosines times 0.1 ln(factor) + 1)."""
+    if scaling not in ("none", "linear", "base", "parts"):
+        raise ValueError(f"rotary_frequencies: unknown scaling {scaling!r}")
+    if not factor >= 1.0 or not theta > 0.0 or any(n < 0 for n in pairs_per_axis):
+        raise ValueError("rotary_frequencies: factor >= 1, theta > 0 and no negative number of pairs required")
+    freq, axis = [], []
+    for a, n in enumerate(pairs_per_axis):
+        i = torch.arange(n, dtype=torch.float64)
+        base = theta * factor ** (n / max(1, n - 1)) if scaling == "base" else theta
+        f = base ** (-i / max(n, 1))
+        if scaling == "linear":
+            f = f / factor
+        elif scaling == "parts":
+            keep = ((trained * f / (2.0 * math.pi) - 1.0) / 31.0).clamp(0.0, 1.0)
+            f = f * keep + f / factor * (1.0 - keep)
+        freq.append(f)
+        axis.append(torch.full((n,), a, dtype=torch.int32))
+    return torch.cat(freq), torch.cat(axis), 0.1 * math.log(factor) + 1.0 if scaling == "parts" else 1.0
+
+
+class Rotary:
+    """Norm and rotary positions of q and k of one layer shape: holds the tables (and the backward's scratch).
+
+    positions: int32 [S, axes], or [B, S, axes] where samples differ (clips packed into one sequence restart theirs); freq fp64 and
+    axis int32 [pairs] on the device (rotary_frequencies); layout "interleaved" or "half"; norm "none", "head" or "row"."""
+
+    def __init__(self, shape, positions, freq, axis, layout="interleaved", norm="none", mscale=1.0, eps=1e-6, with_backward=False):
+        s = shape
+        if positions.dim() not in (2, 3) or positions.shape[-2] != s.S or (positions.dim() == 3 and positions.shape[0] not in (1, s.B)):
+            raise ValueError("Rotary: positions are [S, axes] or [B, S, axes]")
+        if positions.dtype != torch.int32 or freq.dtype != torch.float64 or axis.dtype != torch.int32 or freq.shape != axis.shape or freq.dim() != 1:
+            raise ValueError("Rotary: int32 positions, fp64 frequencies and as many int32 axes required")
+        if not (positions.is_cuda and positions.device == freq.device == axis.device):
+            raise ValueError("Rotary: positions, frequencies and axes have to be on one GPU")
+        self.shape, self.device = s, positions.device
+        self.positions, self.freq, self.axis = positions.contiguous(), freq.contiguous(), axis.contiguous()
+        self.spec = vb.RotarySpec(freq.numel(), positions.shape[-1], {"half": vb.ROTARY_HALF, "interleaved": vb.ROTARY_INTERLEAVED}[layout],
+                                  {"none": vb.ROTARY_NORM_NONE, "head": vb.ROTARY_NORM_HEAD, "row": vb.ROTARY_NORM_ROW}[norm],
+                                  s.B if positions.dim() == 3 and positions.shape[0] == s.B else 1, mscale, eps)
+        self.n_weights = {"none": 0, "head": s.head_dim, "row": s.heads * s.head_dim}[norm]
+        if vb.rotary_workspace_bytes(s, self.spec, 1) == 0:
+            raise ValueError("Rotary: shape, pairs (up to head_dim / 2), axes (1 to 4), mscale (> 0) or eps (>= 0) out of range")
+        self.ws = None
+        if with_backward:
+            self._scratch(2)
+
+    def _scratch(self, n):
+        need = vb.rotary_workspace_bytes(self.shape, self.spec, n)
+        if self.ws is None or self.ws.numel() < need:
+            self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+
+    def _raster(self, x, what):
+        s = self.shape
+        if tuple(x.shape) != (s.B, s.S, s.heads, s.head_dim) or x.dtype != torch_dtype(s) or x.device != self.device or x.stride(3) != 1:
+            raise ValueError(f"Rotary: {what} has to be [B, S, heads, head_dim] of the layer's type on {self.device}, head_dim contiguous")
+        return _strides_bsh(x)
+
+    def _block_major(self, x, what):
+        s = self.shape
+        if tuple(x.shape) != (s.B, s.heads, s.S, s.head_dim) or x.dtype != torch_dtype(s) or x.device != self.device or not x.is_contiguous():
+            raise ValueError(f"Rotary: {what} has to be [B, heads, S, head_dim] of the layer's type on {self.device}, contiguous")
+
+    def _weights(self, weights, n):
+        if weights is None or self.n_weights == 0:
+            return None
+        weights = list(weights) + [None] * (n - len(weights))
+        for w in weights:
+            if w is not None and (w.numel() != self.n_weights or w.dtype != torch.float32 or not w.is_contiguous() or w.device != self.device):
+                raise ValueError(f"Rotary: a weight has to be {self.n_weights} contiguous fp32 values on {self.device}")
+        return weights
+
+    def forward(self, xs, outs, weights=None, block_order=False, moved=(), moved_outs=(), perm=None, shape=None):
+        """Norms and rotates the raster-order tensors xs into outs: raster order, or block-major [B, heads, S, d] with block_order.
+        moved: tensors that only go along (v into block order).  shape: the layer's with another block shape."""
+        xs, outs = list(xs) + list(moved), list(outs) + list(moved_outs)
+        if len(xs) != len(outs) or not 1 <= len(xs) <= 4:
+            raise ValueError("Rotary: one to four tensors, and an output for each")
+        src = [self._raster(x, "an input") for x in xs]
+        dst = None if block_order else [self._raster(x, "an output") for x in outs]
+        if block_order:
+            for x in outs:
+                self._block_major(x, "an output in block order")
+        with _on(self.device):
+            vb.vmoba_rotary(shape or self.shape, self.spec, len(xs) - len(moved), xs, src, outs, dst, self._weights(weights, len(xs)),
+                            self.positions, self.freq, self.axis, perm)
+
+    def backward(self, d_outs, xs, dxs, weights=None, block_order=False):
+        """Gradients of forward(): dxs (raster order; may be d_outs) from d_outs (block-major with block_order) and the forward's
+        xs (unused without a norm).  Returns the weights' gradients, fp32, or None without a norm."""
+        n = len(d_outs)
+        if n != len(dxs) or not 1 <= n <= 4 or (self.n_weights and (xs is None or len(xs) != n)):
+            raise ValueError("Rotary: one to four gradients, as many results and, with a norm, as many inputs")
+        d_strides = None if block_order else [self._raster(x, "a gradient") for x in d_outs]
+        if block_order:
+            for x in d_outs:
+                self._block_major(x, "a gradient in block order")
+        dx_strides = [self._raster(x, "a result") for x in dxs]
+        x_strides = [self._raster(x, "an input") for x in xs] if self.n_weights else None
+        dw = [torch.empty(self.n_weights, dtype=torch.float32, device=self.device) for _ in range(n)] if self.n_weights else None
+        if self.n_weights:
+            self._scratch(n)
+        with _on(self.device):
+            vb.vmoba_rotary_bwd(self.shape, self.spec, d_outs, d_strides, xs if self.n_weights else None, x_strides,
+                                self._weights(weights, n), dxs, dx_strides, dw, self.positions, self.freq, self.axis, self.ws)
+        return dw
 
 
 class VmobaLayer:
@@ -165,14 +299,20 @@ class VmobaLayer:
                                  do_bm=self.do_bm if keep_do else None)
 
     # ---- whole layer --------------------------------------------------------------------
-    def forward(self, q, k, v, tau, o_out, fold_o=None):
+    def forward(self, q, k, v, tau, o_out, fold_o=None, rotary=None, weights=None):
         """q, k, v, o_out: [B, S, heads, d] raster-order tensors on the device.
+
+        rotary: a Rotary of the layer's shape that q and k go through on their way into block order (its weights: of q and of k).
 
         fold_o: let the forward kernels write o in raster order themselves (bf16, head_dim 128) instead of an inverse
         partition pass; off by default (measured on B200: the scattered 256-byte row writes cost the attention kernel
         more than the pass they save, at 12 heads as at 40).  o_out must then stay alive and unchanged until backward()."""
         # k last: the centroids, computed next, find the end of it in L2
-        self.partition_many((v, q, k), (self.v_bm, self.q_bm, self.k_bm), perm=self.perm)
+        if rotary is not None:
+            rotary.forward((k, q), (self.k_bm, self.q_bm), None if weights is None else (weights[1], weights[0]), block_order=True,
+                           moved=(v,), moved_outs=(self.v_bm,), perm=self.perm)
+        else:
+            self.partition_many((v, q, k), (self.v_bm, self.q_bm, self.k_bm), perm=self.perm)
         self.block_scores()
         self.select(tau)
         if fold_o:
@@ -181,8 +321,11 @@ class VmobaLayer:
         self.attn_fwd()
         self.partition(o_out, self.o_bm, inverse=True)
 
-    def backward(self, do, dq_out, dk_out, dv_out, fold_inverse=None, fold_do=False):
+    def backward(self, do, dq_out, dk_out, dv_out, fold_inverse=None, fold_do=False, rotary=None, qk=None, weights=None):
         """Gradients of the last forward(); do and the outputs are raster-order [B, S, heads, d].
+
+        rotary, weights: as given to forward(), with its (q, k) in qk where the Rotary has a norm; dq_out and dk_out are then the
+        gradients of those, and the weights' are returned.
 
         fold_inverse: let the backward kernels write dq, dk, dv in raster order themselves (bf16, head_dim 128,
         outputs with equal strides) instead of three inverse partition passes; default: whenever possible.
@@ -190,16 +333,19 @@ class VmobaLayer:
         for its own purpose, leaves a block-major copy."""
         if fold_inverse is None:
             fold_inverse = self.can_fold_inverse(dq_out, dk_out, dv_out)
-        if fold_inverse and fold_do:
-            self.attn_bwd_raster(do, dq_out, dk_out, dv_out)
-            return
         if fold_inverse:
-            self.attn_bwd_raster(do, dq_out, dk_out, dv_out, keep_do=True)
-            return
+            if fold_do:
+                self.attn_bwd_raster(do, dq_out, dk_out, dv_out)
+            else:
+                self.attn_bwd_raster(do, dq_out, dk_out, dv_out, keep_do=True)
+            return None if rotary is None else rotary.backward((dq_out, dk_out), qk, (dq_out, dk_out), weights)
         self.partition(do, self.do_bm)
         if self.o_raster is not None:      # the block-major backward reads o_bm, which the raster forward did not write
             self.partition(self.o_raster, self.o_bm)
         self.attn_bwd()
+        if rotary is not None:
+            self.partition(dv_out, self.dv_bm, inverse=True)
+            return rotary.backward((self.dq_bm, self.dk_bm), qk, (dq_out, dk_out), weights, block_order=True)
         self.partition_many((dq_out, dk_out, dv_out), (self.dq_bm, self.dk_bm, self.dv_bm), inverse=True)
 
     def check_status(self):
@@ -215,7 +361,6 @@ def dense_step_schedule(n_steps: int, dense_fraction: float = 0.25):
     """Which denoising steps of a sampling run use full attention: the paper's training-free setting runs the
     first 25 % of the steps dense and the rest through VMoBA (Section 4.1, implementation details).  Returns a list
     of n_steps booleans, True = dense; the number of dense steps is ceil(dense_fraction * n_steps)."""
-    import math
     if n_steps < 0 or not (0.0 <= dense_fraction <= 1.0):
         raise ValueError("n_steps >= 0 and 0 <= dense_fraction <= 1 required")
     n_dense = min(n_steps, int(math.ceil(dense_fraction * n_steps - 1e-9)))
@@ -236,8 +381,8 @@ class SteppedAttention:
         self._one_block = vb.Shape.from_buffer_copy(s)
         self._one_block.bT, self._one_block.bH, self._one_block.bW = s.T, s.H, s.W
 
-    def forward(self, step: int, q, k, v, o_out) -> str:
-        """Runs step `step`; returns which path ran ("dense" or "sparse")."""
+    def forward(self, step: int, q, k, v, o_out, rotary=None, weights=None) -> str:
+        """Runs step `step`; returns which path ran ("dense" or "sparse").  rotary, weights: as for VmobaLayer.forward()."""
         if self.schedule[step]:
             # the dense kernels take [B, heads, S, d].  The tokens stay in raster order: the running maximum that a row's
             # weights are rounded against, and with it the last bits of o, depends on the order of the keys.
@@ -247,7 +392,10 @@ class SteppedAttention:
             fresh = lambda x: torch.empty(x.shape, dtype=L.q_bm.dtype, device=L.device)
             q, k, v = (x if L.partitions(x) else fresh(x).copy_(x) for x in (q, k, v))
             qd, kd, vd, od = (torch.empty_like(L.q_bm) for _ in range(4))
-            vb.vmoba_partition_many(one, 0, (q, k, v), (qd, kd, vd), [L.raster_strides(x) for x in (q, k, v)])
+            if rotary is not None:
+                rotary.forward((q, k), (qd, kd), weights, block_order=True, moved=(v,), moved_outs=(vd,), shape=one)
+            else:
+                vb.vmoba_partition_many(one, 0, (q, k, v), (qd, kd, vd), [L.raster_strides(x) for x in (q, k, v)])
             vb.vmoba_full_attn(L.shape, qd, kd, vd, od, self._lse, dev_status=L.dev_status)
             # (an o_out whose elements share memory goes through copy_, which refuses it)
             shared = any(st == 0 and n > 1 for st, n in zip(o_out.stride(), o_out.shape))
@@ -256,7 +404,7 @@ class SteppedAttention:
             if o is not o_out:
                 o_out.copy_(o)
             return "dense"
-        self.layer.forward(q, k, v, self.tau, o_out)
+        self.layer.forward(q, k, v, self.tau, o_out, rotary=rotary, weights=weights)
         return "sparse"
 
 
