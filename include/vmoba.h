@@ -372,6 +372,54 @@ int vmoba_rotary_bwd(const vmoba_shape* shape, const vmoba_rotary_spec* spec, in
                      const double* freq, const int32_t* axis, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Attention in which every query sees one run of keys, beside vmoba_full_attn: clips of different lengths packed into one sequence
+ * (a query sees its own clip), frames that see the frames before them and a prefix, causal order, windows, padding (a query that sees
+ * nothing), and queries against a longer cache.  (The paper's layer has neither masks nor caches.)
+ *   t_ij = scale * q_i . k_j, or softcap * tanh(scale * q_i . k_j / softcap) if softcap > 0
+ *   o_i  = sum over j in [lo_i, hi_i) of exp(t_ij - lse_i) v_j,   lse_i = log of the sum of exp(t_ij)
+ * A query whose range holds no key gets o = 0, lse = -inf and zero gradients; what its q and d_o rows hold does not matter.  Keys
+ * and values behind the last key of all ranges are not used, whatever they hold; in between, a value that is not finite
+ * reaches every row of a tile of 128 query rows that loads it.
+ * kv_heads divides heads: query head h reads key head h / (heads / kv_heads), of which up to 64 share one.
+ * Tensors are addressed by element strides {batch, token, head}, head_dim contiguous, rows 16-byte aligned: q, o, d_o, dq
+ * [B, Sq, heads, head_dim], k, v, dk, dv [B, Sk, kv_heads, head_dim] in whatever order; strides of dimensions larger than one
+ * are at least head_dim.  lse [B, heads, Sq] fp32, contiguous.  bf16 with head_dim 128 runs on the tensor cores, everything else on the
+ * CUDA cores in fp32.
+ */
+typedef struct {
+  int32_t B, heads, kv_heads, head_dim; /* head_dim: 64 or 128                                              */
+  int32_t Sq, Sk;                       /* query and key tokens per sample                                  */
+  int32_t dtype;                        /* vmoba_dtype                                                      */
+  int32_t mask_batch;                   /* 1: all samples share the key ranges, B: each has its own         */
+  float softmax_scale;                  /* 0 => head_dim^-1/2                                               */
+  float softcap;                        /* 0: scores are not capped                                         */
+} vmoba_range_shape;
+
+/*
+ * The plan of a set of key ranges (int32 [mask_batch, Sq, 2], {lo, hi}, any values): clamped ranges, what every tile of
+ * queries and keys has to visit, and in which order.  Made once and used by any number of forward and backward calls of the
+ * same shape (dtype and head counts included), on any stream that is ordered behind it.  0 bytes: invalid shape.
+ */
+size_t vmoba_range_plan_bytes(const vmoba_range_shape* shape);
+int vmoba_range_plan(const vmoba_range_shape* shape, const int32_t* key_range, void* plan, size_t plan_bytes, void* stream);
+
+/* Scratch of a forward (backward = 0) or backward call; one buffer per stream that runs them at the same time. */
+size_t vmoba_range_workspace_bytes(const vmoba_range_shape* shape, int backward);
+
+/* o_resid_or_null (bf16 only, contiguous [B, Sq, heads, head_dim]): the rounding residual of o, kept for the backward as in
+ * vmoba_attn_fwd. */
+int vmoba_range_attn_fwd(const vmoba_range_shape* shape, const void* plan, const void* q, const int64_t q_strides[3], const void* k,
+                         const int64_t k_strides[3], const void* v, const int64_t v_strides[3], void* o, const int64_t o_strides[3],
+                         void* o_resid_or_null, float* lse, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
+
+/* The results repeat bit for bit; dk and dv of keys that no query sees are zero. */
+int vmoba_range_attn_bwd(const vmoba_range_shape* shape, const void* plan, const void* q, const int64_t q_strides[3], const void* k,
+                         const int64_t k_strides[3], const void* v, const int64_t v_strides[3], const void* o,
+                         const int64_t o_strides[3], const void* o_resid_or_null, const float* lse, const void* d_o,
+                         const int64_t do_strides[3], void* dq, const int64_t dq_strides[3], void* dk, const int64_t dk_strides[3],
+                         void* dv, const int64_t dv_strides[3], int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Diagnostics; not part of the method.  Registers a device buffer of 16 uint64 counters (NULL: clears the
  * registration) into which the tensor-core attention kernels launched afterwards ADD, per CTA, the clock
  * cycles that one representative thread of each warp role spent in each section of its loop; divide by the

@@ -24,6 +24,7 @@ EXPORTS = (
     "vmoba_attn_fwd_raster", "vmoba_attn_bwd", "vmoba_attn_bwd_raster",
     "vmoba_attn_bwd_raster_do", "vmoba_full_attn",
     "vmoba_rotary", "vmoba_rotary_bwd", "vmoba_rotary_workspace_bytes",
+    "vmoba_range_plan_bytes", "vmoba_range_plan", "vmoba_range_workspace_bytes", "vmoba_range_attn_fwd", "vmoba_range_attn_bwd",
     "vmoba_debug_wait_profile", "vmoba_debug_wait_timeout",
 )
 
@@ -41,6 +42,11 @@ ROTARY_NORM_NONE, ROTARY_NORM_HEAD, ROTARY_NORM_ROW = 0, 1, 2
 class RotarySpec(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("pairs", "axes", "layout", "norm", "pos_batch")] + [
         ("mscale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class RangeShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "heads", "kv_heads", "head_dim", "Sq", "Sk", "dtype", "mask_batch")] + [
+        ("softmax_scale", ctypes.c_float), ("softcap", ctypes.c_float)]
 
 
 class Shape(ctypes.Structure):
@@ -71,6 +77,11 @@ class Shape(ctypes.Structure):
 def make_shape(B, heads, head_dim, grid, block, dtype, softmax_scale=0.0) -> Shape:
     code = {"f32": F32, "bf16": BF16}[dtype] if isinstance(dtype, str) else int(dtype)
     return Shape(B, heads, head_dim, grid[0], grid[1], grid[2], block[0], block[1], block[2], code, softmax_scale)
+
+
+def make_range_shape(B, heads, kv_heads, head_dim, Sq, Sk, dtype, mask_batch=1, softmax_scale=0.0, softcap=0.0) -> RangeShape:
+    code = {"f32": F32, "bf16": BF16}[dtype] if isinstance(dtype, str) else int(dtype)
+    return RangeShape(B, heads, kv_heads, head_dim, Sq, Sk, code, mask_batch, softmax_scale, softcap)
 
 
 def shape_of(w) -> Shape:
@@ -152,6 +163,17 @@ def lib():
     L.vmoba_rotary.argtypes = [sp, rs, i32, i32] + [vp] * 10
     L.vmoba_rotary_bwd.restype = ctypes.c_int
     L.vmoba_rotary_bwd.argtypes = [sp, rs, i32] + [vp] * 12 + [sz, vp]
+    ap = ctypes.POINTER(RangeShape)
+    L.vmoba_range_plan_bytes.restype = sz
+    L.vmoba_range_plan_bytes.argtypes = [ap]
+    L.vmoba_range_workspace_bytes.restype = sz
+    L.vmoba_range_workspace_bytes.argtypes = [ap, ctypes.c_int]
+    L.vmoba_range_plan.restype = ctypes.c_int
+    L.vmoba_range_plan.argtypes = [ap, vp, vp, sz, vp]
+    L.vmoba_range_attn_fwd.restype = ctypes.c_int
+    L.vmoba_range_attn_fwd.argtypes = [ap, vp] + [vp, p64] * 4 + [vp, vp, vp, vp, sz, vp]
+    L.vmoba_range_attn_bwd.restype = ctypes.c_int
+    L.vmoba_range_attn_bwd.argtypes = [ap, vp] + [vp, p64] * 4 + [vp, vp] + [vp, p64] * 4 + [vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -355,6 +377,36 @@ def vmoba_rotary_bwd(shape, spec, d_outs, d_out_strides, xs, x_strides, weights,
                                   _pointers(xs, n), _strides(x_strides, n), _pointers(weights, n), _pointers(dxs, n),
                                   _strides(dx_strides, n), _pointers(dweights, n), _ptr(positions), _ptr(freq), _ptr(axis), p, size,
                                   _stream(stream)), "vmoba_rotary_bwd")
+
+
+def range_plan_bytes(shape) -> int:
+    return int(lib().vmoba_range_plan_bytes(ctypes.byref(shape)))
+
+
+def range_workspace_bytes(shape, backward: bool = False) -> int:
+    return int(lib().vmoba_range_workspace_bytes(ctypes.byref(shape), int(backward)))
+
+
+def vmoba_range_plan(shape, key_range, plan, stream=None):
+    p, n = _ws_args(plan)
+    _check(lib().vmoba_range_plan(ctypes.byref(shape), _ptr(key_range), p, n, _stream(stream)), "vmoba_range_plan")
+
+
+def vmoba_range_attn_fwd(shape, plan, q, qs, k, ks, v, vs, o, os_, o_resid, lse, dev_status, ws, stream=None):
+    """Tensors with their element strides (batch, token, head)."""
+    p, n = _ws_args(ws)
+    _check(lib().vmoba_range_attn_fwd(ctypes.byref(shape), _ptr(plan), _ptr(q), _I64x3(*qs), _ptr(k), _I64x3(*ks), _ptr(v), _I64x3(*vs),
+                                      _ptr(o), _I64x3(*os_), _ptr(o_resid), _ptr(lse), _ptr(dev_status), p, n, _stream(stream)),
+           "vmoba_range_attn_fwd")
+
+
+def vmoba_range_attn_bwd(shape, plan, q, qs, k, ks, v, vs, o, os_, o_resid, lse, d_o, dos, dq, dqs, dk, dks, dv, dvs, dev_status, ws,
+                         stream=None):
+    p, n = _ws_args(ws)
+    _check(lib().vmoba_range_attn_bwd(ctypes.byref(shape), _ptr(plan), _ptr(q), _I64x3(*qs), _ptr(k), _I64x3(*ks), _ptr(v), _I64x3(*vs),
+                                      _ptr(o), _I64x3(*os_), _ptr(o_resid), _ptr(lse), _ptr(d_o), _I64x3(*dos), _ptr(dq), _I64x3(*dqs),
+                                      _ptr(dk), _I64x3(*dks), _ptr(dv), _I64x3(*dvs), _ptr(dev_status), p, n, _stream(stream)),
+           "vmoba_range_attn_bwd")
 
 
 def vmoba_debug_wait_timeout(dev_status, polls, out2=None, stream=None):

@@ -1,0 +1,804 @@
+// Attention over key ranges: the plan, the CUDA-core kernels (fp32, and bf16 with head_dim 64), the joining of split key ranges,
+// and the entry points.
+//
+//   t = scale q.k, capped c tanh(t / c);  p = exp(t - lse) inside the range, else 0;  o = sum p v
+//   D = rowsum(dO * O);  dV = P^T dO;  dT = P (dO V^T - D) (1 - (t / c)^2);  dQ = scale dT K;  dK = scale dT^T Q
+//
+// A mask that is one run of keys per query needs two words per query, and what a tile of queries and a tile of keys have to do
+// with one another follows from four: smallest lo and largest hi (nothing outside is visited), largest lo and smallest hi (nothing
+// inside is masked).  Keys that no query of a unit sees are not read.
+#include "attn_range.cuh"
+
+#include "attn_simt.cuh"
+
+namespace vmoba {
+namespace range {
+
+using simt::dot_tiles;
+using simt::add_weighted;
+using simt::kLd;
+using simt::kLdP;
+using simt::kRows;
+using simt::kThreads;
+using simt::kTileFloats;
+
+// ------------------------------------------------------------------------------ plan
+// A warp per unit: clamps its tokens' ranges and takes the unit's four bounds.
+__global__ void __launch_bounds__(256)
+plan_units_kernel(const int2* __restrict__ in, Plan plan, RDims D) {
+  if (!grid_begin()) return;
+  const int lane = threadIdx.x & 31;
+  const long long n = (long long)D.Bm * D.nU;
+  for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < n; w += (long long)gridDim.x * 8) {
+    const long long bm = w / D.nU;
+    const int u = (int)(w - bm * D.nU), t0 = u * D.tpt, t1 = min(t0 + D.tpt, D.Sq);
+    int lo_min = INT32_MAX, hi_max = 0, lo_max = 0, hi_min = INT32_MAX;
+    for (int t = t0 + lane; t < t1; t += 32) {
+      int2 r = in[bm * D.Sq + t];
+      r.x = max(r.x, 0);
+      r.y = min(r.y, D.Sk);
+      if (r.x >= r.y) r = make_int2(0, 0);
+      plan.rows[bm * D.Sq + t] = r;
+      if (r.y > 0) { lo_min = min(lo_min, r.x); hi_max = max(hi_max, r.y); }
+      lo_max = max(lo_max, r.x);
+      hi_min = min(hi_min, r.y);
+    }
+    lo_min = __reduce_min_sync(0xffffffffu, lo_min);
+    hi_max = __reduce_max_sync(0xffffffffu, hi_max);
+    lo_max = __reduce_max_sync(0xffffffffu, lo_max);
+    hi_min = __reduce_min_sync(0xffffffffu, hi_min);
+    if (hi_max == 0) lo_min = 0;
+    if (lane == 0) plan.units[w] = make_int4(lo_min, hi_max, lo_max, hi_min);
+  }
+}
+
+// Keys that a forward item (one or two units from u0 on) visits.
+__device__ __forceinline__ int2 item_hull(const int4* units, int u0, int n) {
+  const int4 a = units[u0];
+  int2 h = make_int2(a.x, a.y);
+  if (n > 1) {
+    const int4 b = units[u0 + 1];
+    if (h.y <= h.x) h = make_int2(b.x, b.y);
+    else if (b.y > b.x) h = make_int2(min(h.x, b.x), max(h.y, b.y));
+  }
+  return h;
+}
+
+// The first Bm blocks put a sample's items in order (bins of equal width by the number of keys, the fullest first; inside a bin in any
+// order, which no result depends on), the others walk the key tiles, a warp each.
+constexpr int kBins = 1024;
+__global__ void __launch_bounds__(1024)
+plan_tiles_kernel(Plan plan, RDims D) {
+  if (!grid_begin()) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if ((int)blockIdx.x < D.Bm) {
+    __shared__ int bin[kBins];
+    const int per = D.tc ? 2 : 1;
+    const int4* units = plan.units + (long long)blockIdx.x * D.nU;
+    int* order = plan.order + (long long)blockIdx.x * D.nI;
+    auto bin_of = [&](int i) {
+      const int2 h = item_hull(units, i * per, min(per, D.nU - i * per));
+      return kBins - 1 - (int)((long long)max(h.y - h.x, 0) * (kBins - 1) / D.Sk);
+    };
+    bin[threadIdx.x] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < D.nI; i += 1024) atomicAdd(&bin[bin_of(i)], 1);
+    __syncthreads();
+    const int mine = bin[threadIdx.x];
+    int before = mine;
+    __shared__ int sums[32];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += x;
+    }
+    if (lane == 31) sums[warp] = before;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) before += sums[w];
+    bin[threadIdx.x] = before - mine;
+    __syncthreads();
+    for (int i = threadIdx.x; i < D.nI; i += 1024) order[atomicAdd(&bin[bin_of(i)], 1)] = i;
+    return;
+  }
+  const long long n = (long long)D.Bm * D.nK, warps = (long long)(gridDim.x - D.Bm) * 32;
+  for (long long w = (long long)(blockIdx.x - D.Bm) * 32 + warp; w < n; w += warps) {
+    const long long bm = w / D.nK;
+    const int t = (int)(w - bm * D.nK);
+    const int4* units = plan.units + bm * D.nU;
+    int first = INT32_MAX, last = -1, lo = INT32_MAX, hi = 0;
+    for (int u = lane; u < D.nU; u += 32) {
+      const int4 a = units[u];
+      if (!reaches(a, t, D.TR)) continue;
+      first = min(first, u);
+      last = max(last, u);
+      lo = min(lo, a.x);
+      hi = max(hi, a.y);
+    }
+    first = __reduce_min_sync(0xffffffffu, first);
+    last = __reduce_max_sync(0xffffffffu, last);
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (lane == 0)
+      plan.keys[w] = last < 0 ? make_int4(0, 0, 0, 0) : make_int4(first, last + 1, max(lo - t * D.TR, 0), min(hi - t * D.TR, D.TR));
+  }
+}
+
+// ------------------------------------------------------------------------------ CUDA-core kernels
+// Tiles of 64 rows x 64 keys as in attn_simt.cuh: a thread has rows 4 ty + i and keys tx + 16 j of a tile of scores.
+template <typename T, int DH>
+struct RowRegs {
+  static constexpr int V = DH / 4, N = kRows * V / kThreads;
+  float4 x[N];
+  template <typename RowOf>
+  __device__ __forceinline__ void fetch(RowOf row_of) {           // row_of(r): its first element, or null for zeros
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = threadIdx.x + n * kThreads, r = i / V, c4 = i % V;
+      const T* row = row_of(r);
+      x[n] = row ? load4(row + c4 * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  }
+  __device__ __forceinline__ void store(float* dst) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = threadIdx.x + n * kThreads, r = i / V, c4 = i % V;
+      *reinterpret_cast<float4*>(dst + r * kLd<DH> + c4 * 4) = x[n];
+    }
+  }
+};
+
+__device__ __forceinline__ float capped(float s, float scale, float cap) {
+  s *= scale;
+  return cap > 0.f ? cap * tanhf(s / cap) : s;
+}
+
+// A unit's rows: token and range of each, in shared memory.
+struct UnitRows { int tok[kRows]; int2 range[kRows]; };
+__device__ __forceinline__ void load_unit(UnitRows& s, const RDims& D, const Plan& plan, int b, int u) {
+  if (threadIdx.x < kRows) {
+    const int r = threadIdx.x, t = u * D.tpt + r / D.G;
+    const bool ok = r < D.tpt * D.G && t < D.Sq;
+    s.tok[r] = ok ? t : -1;
+    s.range[r] = ok ? plan.rows[(long long)mask_batch(D.Bm, b) * D.Sq + t] : make_int2(0, 0);
+  }
+}
+
+template <typename T, int DH>
+__global__ void __launch_bounds__(kThreads, 2)
+range_fwd_kernel(const RDims D, const Plan plan, const FwdArgs a) {
+  if (!grid_begin()) return;
+  extern __shared__ __align__(16) float simt_smem[];
+  float* Qs = simt_smem;
+  float* KVs = Qs + kTileFloats<DH>;
+  float* Ps = KVs + kTileFloats<DH>;
+  __shared__ UnitRows rows;
+  const int t = threadIdx.x, ty = t >> 4, tx = t & 15;
+  const long long n_items = (long long)D.B * D.Hk * D.nI * a.splits, all_rows = (long long)D.B * D.Hk * D.rows;
+  for (long long item = blockIdx.x; item < n_items; item += gridDim.x) {
+    const int split = (int)(item % a.splits);
+    const long long m = item / a.splits;
+    const int bhk = (int)(m / D.nI), b = bhk / D.Hk, hk = bhk - b * D.Hk;
+    const int u = plan.order[(long long)mask_batch(D.Bm, b) * D.nI + (m - (long long)bhk * D.nI)];
+    const int4 info = plan.units[(long long)mask_batch(D.Bm, b) * D.nU + u];
+    int first, last;
+    share((max(info.y - info.x, 0) + kRows - 1) / kRows, split, a.splits, first, last);
+    const int k_lo = info.x + first * kRows, k_hi = min(info.x + last * kRows, info.y);
+    __syncthreads();
+    load_unit(rows, D, plan, b, u);
+    __syncthreads();
+    const T* kb = reinterpret_cast<const T*>(a.k) + b * a.ks.b + hk * a.ks.h;
+    const T* vb = reinterpret_cast<const T*>(a.v) + b * a.vs.b + hk * a.vs.h;
+    const T* qb = reinterpret_cast<const T*>(a.q) + b * a.qs.b + (long long)hk * D.G * a.qs.h;
+    RowRegs<T, DH> next;
+    next.fetch([&](int r) { return rows.tok[r] < 0 ? nullptr : qb + rows.tok[r] * a.qs.t + (r % D.G) * a.qs.h; });
+    next.store(Qs);
+    float m_[4], l[4], acc[4][DH / 16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m_[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < DH / 16; ++c) acc[i][c] = 0.f;
+    }
+    const bool live = (ty & ~1) * 4 < D.tpt * D.G;    // (a warp has eight rows)
+    for (int t0 = k_lo; t0 < k_hi; t0 += kRows) {
+      const int nv = min(kRows, k_hi - t0);
+      next.fetch([&](int r) { return r < nv ? kb + (long long)(t0 + r) * a.ks.t : nullptr; });
+      __syncthreads();
+      next.store(KVs);
+      __syncthreads();
+      next.fetch([&](int r) { return r < nv ? vb + (long long)(t0 + r) * a.vs.t : nullptr; });
+      float corr[4];
+      if (live) {
+        float s[4][4];
+        dot_tiles<DH>(Qs, KVs, ty, tx, nv, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int2 rg = rows.range[4 * ty + i];
+          float mx = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int key = t0 + tx + 16 * j;
+            s[i][j] = key >= rg.x && key < rg.y && tx + 16 * j < nv ? capped(s[i][j], D.scale, D.cap) : -INFINITY;
+            mx = fmaxf(mx, s[i][j]);
+          }
+#pragma unroll
+          for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+          const float top = fmaxf(m_[i], mx), used = top == -INFINITY ? 0.f : top;
+          corr[i] = expf(m_[i] - used);
+          m_[i] = top;
+          l[i] *= corr[i];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float p = expf(s[i][j] - used);
+            l[i] += p;
+            Ps[(4 * ty + i) * kLdP + tx + 16 * j] = p;
+          }
+        }
+      }
+      __syncthreads();
+      next.store(KVs);
+      __syncthreads();
+      if (live) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < DH / 16; ++c) acc[i][c] *= corr[i];
+        add_weighted<DH>(Ps, KVs, ty, tx, kRows, acc);
+      }
+    }
+    if (!live) continue;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float total = l[i];
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      const int r = 4 * ty + i, tok = rows.tok[r];
+      if (tok < 0) continue;
+      const bool none = total == 0.f;                // (no key: everything is 0 and lse -inf; a NaN stays one)
+      const float inv = none ? 0.f : 1.0f / total, row_lse = none ? -INFINITY : m_[i] + logf(total);
+      const int g = r % D.G;
+      const long long packed = (long long)bhk * D.rows + (long long)tok * D.G + g, head = hk * D.G + g;
+#pragma unroll
+      for (int c = 0; c < DH / 64; ++c) {
+        const int col = 64 * c + 4 * tx;
+        const float4 x = make_float4(acc[i][4 * c] * inv, acc[i][4 * c + 1] * inv, acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv);
+        if (a.splits == 1) {
+          T* resid = a.resid ? reinterpret_cast<T*>(a.resid) + (((long long)b * D.Sq + tok) * D.Hq + head) * DH + col : nullptr;
+          store4_resid(reinterpret_cast<T*>(a.o) + b * a.os.b + tok * a.os.t + head * a.os.h + col, resid, x);
+        } else {
+          store4(a.part_o + (split * all_rows + packed) * DH + col, x);
+        }
+      }
+      if (tx == 0) {
+        if (a.splits == 1) a.lse[((long long)b * D.Hq + head) * D.Sq + tok] = row_lse;
+        else a.part_lse[split * all_rows + packed] = row_lse;
+      }
+    }
+  }
+}
+
+// Joins the splits of every row: a warp per row, in the order of the splits.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256)
+range_merge_kernel(const RDims D, const FwdArgs a) {
+  if (!grid_begin()) return;
+  constexpr int C = DH / 32;
+  const int lane = threadIdx.x & 31;
+  const long long all_rows = (long long)D.B * D.Hk * D.rows;
+  for (long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); row < all_rows; row += (long long)gridDim.x * 8) {
+    float mine = -INFINITY, mx = -INFINITY;
+    for (int s = lane; s < a.splits; s += 32) mx = fmaxf(mx, __ldg(a.part_lse + s * all_rows + row));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const float used = mx == -INFINITY ? 0.f : mx;
+    float total = 0.f, acc[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[c] = 0.f;
+    for (int s0 = 0; s0 < a.splits; s0 += 32) {
+      mine = s0 + lane < a.splits ? expf(__ldg(a.part_lse + (s0 + lane) * all_rows + row) - used) : 0.f;
+      const int n = min(32, a.splits - s0);
+#pragma unroll 4
+      for (int s = 0; s < n; ++s) {
+        const float w = __shfl_sync(0xffffffffu, mine, s);
+        const float* from = a.part_o + ((s0 + s) * all_rows + row) * DH + lane * C;
+        total += w;
+        if constexpr (C == 4) {
+          const float4 x = *reinterpret_cast<const float4*>(from);
+          acc[0] = fmaf(w, x.x, acc[0]); acc[1] = fmaf(w, x.y, acc[1]); acc[2] = fmaf(w, x.z, acc[2]); acc[3] = fmaf(w, x.w, acc[3]);
+        } else {
+          const float2 x = *reinterpret_cast<const float2*>(from);
+          acc[0] = fmaf(w, x.x, acc[0]); acc[1] = fmaf(w, x.y, acc[1]);
+        }
+      }
+    }
+    const bool none = total == 0.f;
+    const float inv = none ? 0.f : 1.0f / total;
+    const int bhk = (int)(row / D.rows), r = (int)(row - (long long)bhk * D.rows), tok = r / D.G, g = r - tok * D.G;
+    const int b = bhk / D.Hk, head = (bhk - b * D.Hk) * D.G + g;
+    T* o = reinterpret_cast<T*>(a.o) + b * a.os.b + tok * a.os.t + head * a.os.h + lane * C;
+    T* resid = a.resid ? reinterpret_cast<T*>(a.resid) + (((long long)b * D.Sq + tok) * D.Hq + head) * DH + lane * C : nullptr;
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[c] *= inv;
+    if constexpr (C == 4) {
+      store4_resid(o, resid, make_float4(acc[0], acc[1], acc[2], acc[3]));
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const T h = from_f32<T>(acc[c]);
+        o[c] = h;
+        if (resid) resid[c] = from_f32<T>(acc[c] - to_f32<T>(h));
+      }
+    }
+    if (lane == 0) a.lse[((long long)b * D.Hq + head) * D.Sq + tok] = none ? -INFINITY : mx + logf(total);
+  }
+}
+
+// D = rowsum(dO * O) per packed row, 0 where the row sees nothing (its dO is not read).  zero_words: counters cleared on the way.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256)
+range_rowdot_kernel(const RDims D, const Plan plan, const T* __restrict__ o, Strides os, const T* __restrict__ resid,
+                    const T* __restrict__ d_o, Strides dos, float* __restrict__ Dv, int* __restrict__ zero_words, long long n_words) {
+  if (!grid_begin()) return;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n_words; i += (long long)gridDim.x * blockDim.x)
+    zero_words[i] = 0;
+  constexpr int C = DH / 32, R = 4;            // channels per lane; rows of a warp whose loads are in flight together
+  const int lane = threadIdx.x & 31;
+  const long long all_rows = (long long)D.B * D.Hk * D.rows;
+  for (long long row0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * R; row0 < all_rows; row0 += (long long)gridDim.x * 8 * R) {
+    float x[R][C], y[R][C], z[R][C];
+#pragma unroll
+    for (int n = 0; n < R; ++n) {
+      const long long row = min(row0 + n, all_rows - 1);
+      const int bhk = (int)((unsigned)row / (unsigned)D.rows), r = (int)(row - (long long)bhk * D.rows), tok = r / D.G, g = r - tok * D.G;
+      const int b = bhk / D.Hk, head = (bhk - b * D.Hk) * D.G + g;
+      const bool some = __ldg(&plan.rows[(long long)mask_batch(D.Bm, b) * D.Sq + tok].y) > 0;
+#pragma unroll
+      for (int c = 0; c < C; ++c) x[n][c] = y[n][c] = z[n][c] = 0.f;
+      if (some) {
+        auto get = [&](const T* from, float (&to)[C]) {
+          if constexpr (C == 4) {
+            const float4 v = load4(from + lane * 4);
+            to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w;
+          } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c) to[c] = to_f32<T>(from[lane * C + c]);
+          }
+        };
+        get(o + b * os.b + tok * os.t + head * os.h, x[n]);
+        get(d_o + b * dos.b + tok * dos.t + head * dos.h, y[n]);
+        if (resid) get(resid + (((long long)b * D.Sq + tok) * D.Hq + head) * DH, z[n]);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < R; ++n) {
+      float s = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) s = fmaf(x[n][c] + z[n][c], y[n][c], s);
+#pragma unroll
+      for (int k = 16; k > 0; k >>= 1) s += __shfl_xor_sync(0xffffffffu, s, k);
+      if (lane == 0 && row0 + n < all_rows) Dv[row0 + n] = s;
+    }
+  }
+}
+
+// Scores of a tile as weights and slopes: p = exp(t - lse) inside the ranges, w = p (1 - (t / cap)^2).
+__device__ __forceinline__ void weigh(float s, bool in, float lse, const RDims& D, float& p, float& w) {
+  s *= D.scale;
+  float slope = 1.f;
+  if (D.cap > 0.f) {
+    const float u = tanhf(s / D.cap);
+    s = D.cap * u;
+    slope = 1.f - u * u;
+  }
+  p = in ? expf(s - lse) : 0.f;
+  w = in ? p * slope : 0.f;
+}
+
+// dK, dV: a CTA owns 64 keys of a key head and streams the units that reach into them, all query heads of the group.
+template <int DH> constexpr int kRangeBwdSmem = (4 * kTileFloats<DH> + kRows * kLdP) * 4;
+template <typename T, int DH>
+__global__ void __launch_bounds__(kThreads, DH == 64 ? 2 : 1)
+range_bwd_dkdv_kernel(const RDims D, const Plan plan, const BwdArgs a) {
+  if (!grid_begin()) return;
+  extern __shared__ __align__(16) float simt_smem[];
+  float* Ks = simt_smem;
+  float* Vs = Ks + kTileFloats<DH>;
+  float* Qs = Vs + kTileFloats<DH>;
+  float* dOs = Qs + kTileFloats<DH>;
+  float* Ps = dOs + kTileFloats<DH>;           // [key][query]: weights, then dT
+  __shared__ UnitRows rows;
+  __shared__ float s_lse[kRows], s_D[kRows];
+  const int t = threadIdx.x, ty = t >> 4, tx = t & 15;
+  const long long n_items = (long long)D.B * D.Hk * D.nK;
+  for (long long item = blockIdx.x; item < n_items; item += gridDim.x) {
+    const int bhk = (int)(item / D.nK), tile = (int)(item - (long long)bhk * D.nK), b = bhk / D.Hk, hk = bhk - b * D.Hk;
+    const int4 info = plan.keys[(long long)mask_batch(D.Bm, b) * D.nK + tile];
+    const int key0 = tile * kRows, keys = min(kRows, D.Sk - key0);
+    float dk_[4][DH / 16], dv_[4][DH / 16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < DH / 16; ++c) dk_[i][c] = dv_[i][c] = 0.f;
+    __syncthreads();
+    {
+      const T* kb = reinterpret_cast<const T*>(a.k) + b * a.ks.b + hk * a.ks.h;
+      const T* vb = reinterpret_cast<const T*>(a.v) + b * a.vs.b + hk * a.vs.h;
+      RowRegs<T, DH> x;
+      x.fetch([&](int r) { return r >= info.z && r < info.w ? kb + (long long)(key0 + r) * a.ks.t : nullptr; });
+      x.store(Ks);
+      x.fetch([&](int r) { return r >= info.z && r < info.w ? vb + (long long)(key0 + r) * a.vs.t : nullptr; });
+      x.store(Vs);
+    }
+    for (int u = info.x; u < info.y; ++u) {
+      if (!reaches(plan.units[(long long)mask_batch(D.Bm, b) * D.nU + u], tile, kRows)) continue;
+      __syncthreads();
+      load_unit(rows, D, plan, b, u);
+      __syncthreads();
+      if (t < kRows) {
+        const int tok = rows.tok[t];
+        const bool some = rows.range[t].y > 0;
+        s_lse[t] = some ? a.lse[((long long)b * D.Hq + hk * D.G + t % D.G) * D.Sq + tok] : INFINITY;
+        s_D[t] = some ? a.Dv[(long long)bhk * D.rows + (long long)tok * D.G + t % D.G] : 0.f;
+      }
+      {
+        const T* qb = reinterpret_cast<const T*>(a.q) + b * a.qs.b + (long long)hk * D.G * a.qs.h;
+        const T* ob = reinterpret_cast<const T*>(a.d_o) + b * a.dos.b + (long long)hk * D.G * a.dos.h;
+        RowRegs<T, DH> x;
+        x.fetch([&](int r) { return rows.range[r].y > 0 ? qb + rows.tok[r] * a.qs.t + (r % D.G) * a.qs.h : nullptr; });
+        x.store(Qs);
+        x.fetch([&](int r) { return rows.range[r].y > 0 ? ob + rows.tok[r] * a.dos.t + (r % D.G) * a.dos.h : nullptr; });
+        x.store(dOs);
+      }
+      __syncthreads();
+      float s[4][4], w[4][4];
+      dot_tiles<DH>(Ks, Qs, ty, tx, kRows, s);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = tx + 16 * j, key = key0 + 4 * ty + i;
+          const int2 rg = rows.range[r];
+          weigh(s[i][j], key >= rg.x && key < rg.y, s_lse[r], D, s[i][j], w[i][j]);
+          Ps[(4 * ty + i) * kLdP + r] = s[i][j];
+        }
+      __syncwarp();                            // (a warp reads its own eight rows)
+      add_weighted<DH>(Ps, dOs, ty, tx, kRows, dv_);
+      dot_tiles<DH>(Vs, dOs, ty, tx, kRows, s);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) Ps[(4 * ty + i) * kLdP + tx + 16 * j] = w[i][j] * (s[i][j] - s_D[tx + 16 * j]);
+      __syncwarp();
+      add_weighted<DH>(Ps, Qs, ty, tx, kRows, dk_);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (4 * ty + i >= keys) break;
+      T* dk = reinterpret_cast<T*>(a.dk) + b * a.dks.b + (long long)(key0 + 4 * ty + i) * a.dks.t + hk * a.dks.h;
+      T* dv = reinterpret_cast<T*>(a.dv) + b * a.dvs.b + (long long)(key0 + 4 * ty + i) * a.dvs.t + hk * a.dvs.h;
+#pragma unroll
+      for (int c = 0; c < DH / 64; ++c) {
+        const int col = 64 * c + 4 * tx;
+        store4(dk + col, make_float4(dk_[i][4 * c] * D.scale, dk_[i][4 * c + 1] * D.scale, dk_[i][4 * c + 2] * D.scale, dk_[i][4 * c + 3] * D.scale));
+        store4(dv + col, make_float4(dv_[i][4 * c], dv_[i][4 * c + 1], dv_[i][4 * c + 2], dv_[i][4 * c + 3]));
+      }
+    }
+  }
+}
+
+// dQ: a CTA takes a unit and works S and dP out again.
+template <typename T, int DH>
+__global__ void __launch_bounds__(kThreads, DH == 64 ? 2 : 1)
+range_bwd_dq_kernel(const RDims D, const Plan plan, const BwdArgs a, T* __restrict__ dq, const Strides dqs) {
+  if (!grid_begin()) return;
+  extern __shared__ __align__(16) float simt_smem[];
+  float* Qs = simt_smem;
+  float* dOs = Qs + kTileFloats<DH>;
+  float* Ks = dOs + kTileFloats<DH>;
+  float* Vs = Ks + kTileFloats<DH>;
+  float* Ps = Vs + kTileFloats<DH>;            // [query][key]: dT
+  __shared__ UnitRows rows;
+  const int t = threadIdx.x, ty = t >> 4, tx = t & 15;
+  const long long n_items = (long long)D.B * D.Hk * D.nU;
+  for (long long item = blockIdx.x; item < n_items; item += gridDim.x) {
+    const int bhk = (int)(item / D.nU), u = (int)(item - (long long)bhk * D.nU), b = bhk / D.Hk, hk = bhk - b * D.Hk;
+    const int4 info = plan.units[(long long)mask_batch(D.Bm, b) * D.nU + u];
+    __syncthreads();
+    load_unit(rows, D, plan, b, u);
+    __syncthreads();
+    {
+      const T* qb = reinterpret_cast<const T*>(a.q) + b * a.qs.b + (long long)hk * D.G * a.qs.h;
+      const T* ob = reinterpret_cast<const T*>(a.d_o) + b * a.dos.b + (long long)hk * D.G * a.dos.h;
+      RowRegs<T, DH> x;
+      x.fetch([&](int r) { return rows.range[r].y > 0 ? qb + rows.tok[r] * a.qs.t + (r % D.G) * a.qs.h : nullptr; });
+      x.store(Qs);
+      x.fetch([&](int r) { return rows.range[r].y > 0 ? ob + rows.tok[r] * a.dos.t + (r % D.G) * a.dos.h : nullptr; });
+      x.store(dOs);
+    }
+    float row_lse[4], row_D[4], acc[4][DH / 16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 4 * ty + i, tok = rows.tok[r];
+      const bool some = rows.range[r].y > 0;
+      row_lse[i] = some ? a.lse[((long long)b * D.Hq + hk * D.G + r % D.G) * D.Sq + tok] : INFINITY;
+      row_D[i] = some ? a.Dv[(long long)bhk * D.rows + (long long)tok * D.G + r % D.G] : 0.f;
+#pragma unroll
+      for (int c = 0; c < DH / 16; ++c) acc[i][c] = 0.f;
+    }
+    const T* kb = reinterpret_cast<const T*>(a.k) + b * a.ks.b + hk * a.ks.h;
+    const T* vb = reinterpret_cast<const T*>(a.v) + b * a.vs.b + hk * a.vs.h;
+    for (int t0 = info.x; t0 < info.y; t0 += kRows) {
+      const int nv = min(kRows, info.y - t0);
+      RowRegs<T, DH> x, y;
+      x.fetch([&](int r) { return r < nv ? kb + (long long)(t0 + r) * a.ks.t : nullptr; });
+      y.fetch([&](int r) { return r < nv ? vb + (long long)(t0 + r) * a.vs.t : nullptr; });
+      __syncthreads();
+      x.store(Ks);
+      y.store(Vs);
+      __syncthreads();
+      float p[4][4], s[4][4];
+      dot_tiles<DH>(Qs, Ks, ty, tx, kRows, p);
+      dot_tiles<DH>(dOs, Vs, ty, tx, kRows, s);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int2 rg = rows.range[4 * ty + i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int key = t0 + tx + 16 * j;
+          float w, none;
+          weigh(p[i][j], key >= rg.x && key < rg.y, row_lse[i], D, none, w);
+          Ps[(4 * ty + i) * kLdP + tx + 16 * j] = w * (s[i][j] - row_D[i]);
+        }
+      }
+      __syncwarp();                            // (a warp reads its own eight rows)
+      add_weighted<DH>(Ps, Ks, ty, tx, kRows, acc);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 4 * ty + i, tok = rows.tok[r];
+      if (tok < 0) continue;
+      T* row = dq + b * dqs.b + tok * dqs.t + (long long)(hk * D.G + r % D.G) * dqs.h + 4 * tx;
+#pragma unroll
+      for (int c = 0; c < DH / 64; ++c)
+        store4(row + 64 * c, make_float4(acc[i][4 * c] * D.scale, acc[i][4 * c + 1] * D.scale, acc[i][4 * c + 2] * D.scale, acc[i][4 * c + 3] * D.scale));
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------ host
+static int make_rdims(const vmoba_range_shape* s, RDims* o) {
+  if (!s) return VMOBA_ERR_ARG;
+  if (s->dtype != VMOBA_F32 && s->dtype != VMOBA_BF16) return VMOBA_ERR_ARG;
+  if (s->B <= 0 || s->heads <= 0 || s->kv_heads <= 0 || s->Sq <= 0 || s->Sk <= 0) return VMOBA_ERR_SHAPE;
+  if (s->head_dim != 64 && s->head_dim != 128) return VMOBA_ERR_SHAPE;
+  if (s->heads % s->kv_heads || s->heads / s->kv_heads > 64) return VMOBA_ERR_SHAPE;
+  if (s->mask_batch != 1 && s->mask_batch != s->B) return VMOBA_ERR_SHAPE;
+  if (!(s->softmax_scale >= 0.f) || s->softmax_scale > 1e30f || !(s->softcap >= 0.f) || s->softcap > 1e30f) return VMOBA_ERR_ARG;
+  if ((long long)s->B * s->heads > (1ll << 24) || (long long)s->B * s->heads * s->Sq > (1ll << 30) ||
+      (long long)s->B * s->kv_heads * s->Sk > (1ll << 30))
+    return VMOBA_ERR_SHAPE;
+  o->B = s->B; o->Hq = s->heads; o->Hk = s->kv_heads; o->G = s->heads / s->kv_heads; o->d = s->head_dim;
+  o->Sq = s->Sq; o->Sk = s->Sk; o->Bm = s->mask_batch; o->dtype = s->dtype;
+  o->es = s->dtype == VMOBA_BF16 ? 2 : 4;
+  o->scale = s->softmax_scale > 0.f ? s->softmax_scale : 1.0f / sqrtf((float)s->head_dim);
+  o->cap = s->softcap;
+  o->tc = false;
+  o->TR = o->tc ? 128 : 64;
+  o->tpt = o->TR / o->G;
+  o->rows = s->Sq * o->G;
+  o->nU = (s->Sq + o->tpt - 1) / o->tpt;
+  o->nK = (s->Sk + o->TR - 1) / o->TR;
+  o->nI = o->tc ? (o->nU + 1) / 2 : o->nU;
+  return VMOBA_OK;
+}
+
+static Plan carve_plan(const RDims& D, const void* mem, size_t* bytes) {
+  Carver c(const_cast<void*>(mem));
+  Plan p;
+  p.rows = c.take<int2>((size_t)D.Bm * D.Sq);
+  p.units = c.take<int4>((size_t)D.Bm * D.nU);
+  p.keys = c.take<int4>((size_t)D.Bm * D.nK);
+  p.order = c.take<int>((size_t)D.Bm * D.nI);
+  if (bytes) *bytes = c.total();
+  return p;
+}
+
+// How many pieces a key range is cut into: as many as shorten the longest queue of an SM.  A piece costs its rows a trip through memory
+// in fp32 (8 bytes per element and piece) and the last wave is paid in full.  The number of SMs is the design's, not the device's,
+// so that the workspace is a function of the shape alone.
+static int splits(const RDims& D) {
+  constexpr int kSms = 148;
+  const long long items = (long long)D.B * D.Hk * D.nI, tiles = D.nK;
+  if (items >= 4 * kSms || tiles < 8) return 1;
+  const double tile_us = D.tc ? 1.9 : 20.0, row_us = (double)D.B * D.Hk * D.rows * D.d * 8 / 6.0e6;
+  double best = 1e30;
+  int n = 1;
+  for (int s = 1; s <= 64 && s * 4 <= tiles; ++s) {
+    const long long waves = (items * s + kSms - 1) / kSms;
+    const double us = waves * ((double)tiles / s * tile_us + 4.0) + (s > 1 ? s * row_us + 4.0 : 0.0);
+    if (us < best * 0.98) { best = us; n = s; }
+  }
+  return n;
+}
+
+struct FwdWs { float *part_o, *part_lse; size_t bytes; Guards guards; };
+static FwdWs carve_fwd(const RDims& D, int n, void* ws) {
+  Carver c(ws);
+  FwdWs w = {};
+  const size_t rows = (size_t)D.B * D.Hk * D.rows;
+  if (n > 1) {
+    w.part_lse = c.take<float>(rows * n);
+    w.part_o = c.take<float>(rows * n * D.d);
+  }
+  w.bytes = std::max<size_t>(c.total(), 256);
+  w.guards = c.guards;
+  return w;
+}
+
+struct BwdWs { float* Dv; size_t bytes; Guards guards; };
+static BwdWs carve_bwd(const RDims& D, void* ws) {
+  Carver c(ws);
+  BwdWs w = {};
+  w.Dv = c.take<float>((size_t)D.B * D.Hk * D.rows);
+  w.bytes = c.total();
+  w.guards = c.guards;
+  return w;
+}
+
+// Element strides of a tensor [B, S, heads, d]; those of dimensions of size one address nothing and are taken for dense ones.
+static bool get_strides(const RDims& D, const int64_t s[3], int S, int heads, Strides* o) {
+  if (!s) return false;
+  const int per = 16 / D.es;
+  long long st[3] = {s[0], s[1], s[2]};
+  const int n[3] = {D.B, S, heads};
+  if (heads == 1) st[2] = D.d;
+  if (S == 1) st[1] = (long long)heads * D.d;
+  if (D.B == 1) st[0] = (long long)S * heads * D.d;
+  for (int i = 0; i < 3; ++i)
+    if (st[i] < 0 || st[i] % per || (n[i] > 1 && st[i] < D.d) || st[i] > (1ll << 38)) return false;
+  *o = {st[0], st[1], st[2]};
+  return true;
+}
+
+static int grid_for(long long items, int per_sm) {
+  return (int)std::max<long long>(1, std::min<long long>(items, (long long)sm_count() * per_sm));
+}
+
+// As for the CUDA-core kernels of the dense path: several of their CTAs share an SM, and long ones are not launched early.
+static bool early_simt(const RDims& D) { return (double)D.B * D.Hq * D.Sq * D.Sk * D.d <= (double)(1 << 25); }
+static bool early_rows(const RDims& D) { return (long long)D.B * D.Hq * D.Sq * D.d * D.es <= (16ll << 20); }
+
+template <typename T, int DH>
+static int forward(const RDims& D, const Plan& plan, FwdArgs a, cudaStream_t st) {
+  const long long items = (long long)D.B * D.Hk * D.nI * a.splits;
+  VMOBA_CUDA_OK(allow_smem(range_fwd_kernel<T, DH>, simt::kFwdSmem<DH>));
+  launch_kernel(early_simt(D), range_fwd_kernel<T, DH>, grid_for(items, 8), kThreads, simt::kFwdSmem<DH>, st, D, plan, a);
+  VMOBA_LAUNCH_OK(1);
+  if (a.splits > 1) {
+    launch_kernel(early_rows(D), range_merge_kernel<T, DH>, grid_for(((long long)D.B * D.Hk * D.rows + 7) / 8, 16), 256, 0, st, D, a);
+    VMOBA_LAUNCH_OK(1);
+  }
+  return VMOBA_OK;
+}
+
+template <typename T, int DH>
+static int backward(const RDims& D, const Plan& plan, const BwdArgs& a, const void* o, const Strides& os, const void* resid, float* Dv,
+                    void* dq, const Strides& dqs, cudaStream_t st) {
+  const long long all_rows = (long long)D.B * D.Hk * D.rows;
+  launch_kernel(early_rows(D), range_rowdot_kernel<T, DH>, grid_for((all_rows + 31) / 32, 16), 256, 0, st, D, plan, (const T*)o, os,
+                (const T*)resid, (const T*)a.d_o, a.dos, Dv, (int*)nullptr, 0ll);
+  VMOBA_CUDA_OK(allow_smem(range_bwd_dkdv_kernel<T, DH>, kRangeBwdSmem<DH>));
+  VMOBA_CUDA_OK(allow_smem(range_bwd_dq_kernel<T, DH>, kRangeBwdSmem<DH>));
+  launch_kernel(early_simt(D), range_bwd_dkdv_kernel<T, DH>, grid_for((long long)D.B * D.Hk * D.nK, 4), kThreads, kRangeBwdSmem<DH>, st, D, plan, a);
+  launch_kernel(early_simt(D), range_bwd_dq_kernel<T, DH>, grid_for((long long)D.B * D.Hk * D.nU, 4), kThreads, kRangeBwdSmem<DH>, st, D, plan, a,
+                (T*)dq, dqs);
+  VMOBA_LAUNCH_OK(3);
+  return VMOBA_OK;
+}
+
+#define VMOBA_RANGE_DISPATCH(rc, FN, ...)                                              \
+  do {                                                                                 \
+    if (D.dtype == VMOBA_BF16) {                                                       \
+      rc = D.d == 128 ? FN<__nv_bfloat16, 128>(__VA_ARGS__) : FN<__nv_bfloat16, 64>(__VA_ARGS__); \
+    } else {                                                                           \
+      rc = D.d == 128 ? FN<float, 128>(__VA_ARGS__) : FN<float, 64>(__VA_ARGS__);      \
+    }                                                                                  \
+  } while (0)
+
+}  // namespace range
+}  // namespace vmoba
+
+using namespace vmoba;
+using namespace vmoba::range;
+
+extern "C" size_t vmoba_range_plan_bytes(const vmoba_range_shape* shape) {
+  RDims D;
+  if (make_rdims(shape, &D)) return 0;
+  size_t bytes;
+  carve_plan(D, nullptr, &bytes);
+  return bytes;
+}
+
+extern "C" int vmoba_range_plan(const vmoba_range_shape* shape, const int32_t* key_range, void* plan, size_t plan_bytes,
+                                void* stream) {
+  RDims D;
+  if (int rc = make_rdims(shape, &D)) return rc;
+  if (!key_range || !plan || !aligned16(plan) || (reinterpret_cast<uintptr_t>(key_range) & 7u)) return VMOBA_ERR_ARG;
+  size_t need;
+  const Plan p = carve_plan(D, plan, &need);
+  if (plan_bytes < need) return VMOBA_ERR_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  launch_kernel(plan_units_kernel, grid_for(((long long)D.Bm * D.nU + 7) / 8, 8), 256, 0, st, reinterpret_cast<const int2*>(key_range), p, D);
+  const long long tile_blocks = std::min<long long>(((long long)D.Bm * D.nK + 31) / 32, 2ll * sm_count());
+  if (D.Bm > (1 << 20)) return VMOBA_ERR_SHAPE;
+  launch_kernel(plan_tiles_kernel, (unsigned)(D.Bm + tile_blocks), 1024, 0, st, p, D);
+  VMOBA_LAUNCH_OK(2);
+  return VMOBA_OK;
+}
+
+extern "C" size_t vmoba_range_workspace_bytes(const vmoba_range_shape* shape, int backward) {
+  RDims D;
+  if (make_rdims(shape, &D) || (backward != 0 && backward != 1)) return 0;
+  return backward ? carve_bwd(D, nullptr).bytes : carve_fwd(D, splits(D), nullptr).bytes;
+}
+
+extern "C" int vmoba_range_attn_fwd(const vmoba_range_shape* shape, const void* plan, const void* q, const int64_t q_strides[3],
+                                    const void* k, const int64_t k_strides[3], const void* v, const int64_t v_strides[3], void* o,
+                                    const int64_t o_strides[3], void* o_resid_or_null, float* lse, int32_t* dev_status, void* ws,
+                                    size_t ws_bytes, void* stream) {
+  RDims D;
+  if (int rc = make_rdims(shape, &D)) return rc;
+  if (!plan || !q || !k || !v || !o || !lse || !dev_status || !ws) return VMOBA_ERR_ARG;
+  if (!aligned16(plan) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(ws) || !aligned16(o_resid_or_null))
+    return VMOBA_ERR_ARG;
+  FwdArgs a = {};
+  if (!get_strides(D, q_strides, D.Sq, D.Hq, &a.qs) || !get_strides(D, k_strides, D.Sk, D.Hk, &a.ks) ||
+      !get_strides(D, v_strides, D.Sk, D.Hk, &a.vs) || !get_strides(D, o_strides, D.Sq, D.Hq, &a.os))
+    return VMOBA_ERR_ARG;
+  a.splits = splits(D);
+  FwdWs w = carve_fwd(D, a.splits, ws);
+  if (ws_bytes < w.bytes) return VMOBA_ERR_WORKSPACE;
+  a.q = q; a.k = k; a.v = v; a.o = o; a.resid = D.dtype == VMOBA_BF16 ? o_resid_or_null : nullptr; a.lse = lse;
+  a.part_o = w.part_o; a.part_lse = w.part_lse; a.status = dev_status;
+  const Plan p = carve_plan(D, plan, nullptr);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  VMOBA_GUARDS_ARM(w.guards, st);
+  int rc;
+  VMOBA_RANGE_DISPATCH(rc, forward, D, p, a, st);
+  VMOBA_GUARDS_CHECK(w.guards, dev_status, st);
+  return rc;
+}
+
+extern "C" int vmoba_range_attn_bwd(const vmoba_range_shape* shape, const void* plan, const void* q, const int64_t q_strides[3],
+                                    const void* k, const int64_t k_strides[3], const void* v, const int64_t v_strides[3], const void* o,
+                                    const int64_t o_strides[3], const void* o_resid_or_null, const float* lse, const void* d_o,
+                                    const int64_t do_strides[3], void* dq, const int64_t dq_strides[3], void* dk,
+                                    const int64_t dk_strides[3], void* dv, const int64_t dv_strides[3], int32_t* dev_status, void* ws,
+                                    size_t ws_bytes, void* stream) {
+  RDims D;
+  if (int rc = make_rdims(shape, &D)) return rc;
+  if (!plan || !q || !k || !v || !o || !lse || !d_o || !dq || !dk || !dv || !dev_status || !ws) return VMOBA_ERR_ARG;
+  if (!aligned16(plan) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(o_resid_or_null) ||
+      !aligned16(d_o) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(ws))
+    return VMOBA_ERR_ARG;
+  BwdArgs a = {};
+  Strides os, dqs;
+  if (!get_strides(D, q_strides, D.Sq, D.Hq, &a.qs) || !get_strides(D, k_strides, D.Sk, D.Hk, &a.ks) ||
+      !get_strides(D, v_strides, D.Sk, D.Hk, &a.vs) || !get_strides(D, o_strides, D.Sq, D.Hq, &os) ||
+      !get_strides(D, do_strides, D.Sq, D.Hq, &a.dos) || !get_strides(D, dq_strides, D.Sq, D.Hq, &dqs) ||
+      !get_strides(D, dk_strides, D.Sk, D.Hk, &a.dks) || !get_strides(D, dv_strides, D.Sk, D.Hk, &a.dvs))
+    return VMOBA_ERR_ARG;
+  BwdWs w = carve_bwd(D, ws);
+  if (ws_bytes < w.bytes) return VMOBA_ERR_WORKSPACE;
+  a.q = q; a.k = k; a.v = v; a.d_o = d_o; a.lse = lse; a.Dv = w.Dv; a.dk = dk; a.dv = dv; a.status = dev_status;
+  if (D.dtype != VMOBA_BF16) o_resid_or_null = nullptr;
+  const Plan p = carve_plan(D, plan, nullptr);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  VMOBA_GUARDS_ARM(w.guards, st);
+  int rc;
+  VMOBA_RANGE_DISPATCH(rc, backward, D, p, a, o, os, o_resid_or_null, w.Dv, dq, dqs, st);
+  VMOBA_GUARDS_CHECK(w.guards, dev_status, st);
+  return rc;
+}

@@ -1,0 +1,74 @@
+// Attention over key ranges: what its kernels share.
+//
+// Query i of a sample sees the keys [lo_i, hi_i).  The query heads of a group share a key head, so the rows that a kernel tiles are
+// packed: row r of (sample, key head) is token r / G and head r % G of the group (G = heads / kv_heads), and a unit is the rows of
+// tpt = TR / G whole tokens (TR = 128 rows on the tensor cores, 64 on the CUDA cores; less than TR rows where G does not divide it).
+//
+// The plan (device memory of the caller, made once per set of ranges):
+//   rows   int2 [Bm][Sq]   the ranges clamped into [0, Sk); (0, 0) where nothing is left
+//   units  int4 [Bm][nU]   of a unit's rows that see something: smallest lo, largest hi; of all its rows: largest lo, smallest hi
+//   keys   int4 [Bm][nK]   of a tile of TR keys: first and one past the last unit that reaches into it; first and one past the last
+//                          key (relative to the tile) that any unit's hull holds
+//   order  int  [Bm][nI]   the forward's items (two units on the tensor cores, else one), those with the most keys first
+#pragma once
+
+#include <algorithm>
+
+#include "common.cuh"
+
+namespace vmoba {
+namespace range {
+
+struct RDims {
+  int B, Hq, Hk, G, d, Sq, Sk, Bm, dtype, es;
+  float scale, cap;
+  bool tc;            // tensor-core path
+  int TR;             // rows of a unit at most, and keys of a tile
+  int tpt;            // tokens of a unit
+  int rows;           // rows of a (sample, key head): Sq * G
+  int nU, nK, nI;     // units, key tiles, forward items per (sample, key head)
+};
+
+struct Plan {
+  int2* rows;
+  int4* units;
+  int4* keys;
+  int* order;
+};
+
+struct Strides { long long b, t, h; };       // elements
+
+__device__ __forceinline__ int mask_batch(const int Bm, int b) { return Bm > 1 ? b : 0; }
+
+// Whether a unit with this record reaches into key tile t of TR keys.
+__device__ __forceinline__ bool reaches(const int4& u, int t, int TR) { return u.y > u.x && u.x < (t + 1) * TR && u.y > t * TR; }
+
+// The share of `split` of `n` splits of a range of `tiles` tiles: [first, last).
+__device__ __forceinline__ void share(int tiles, int split, int n, int& first, int& last) {
+  first = (int)((long long)tiles * split / n);
+  last = (int)((long long)tiles * (split + 1) / n);
+}
+
+// ---- tensor-core kernels (attn_range_fwd.cu, attn_range_bwd.cu)
+struct FwdArgs {
+  const void *q, *k, *v;
+  void *o, *resid;           // resid: contiguous [B, Sq, Hq, d] or null
+  float* lse;                // [B, Hq, Sq]
+  Strides qs, ks, vs, os;
+  int splits;
+  float *part_o, *part_lse;  // [split][B * Hk * rows][d], [split][B * Hk * rows]
+  int32_t* status;
+};
+struct BwdArgs {
+  const void *q, *k, *v, *d_o;
+  const float *lse, *Dv;     // Dv: [B * Hk * rows]
+  Strides qs, ks, vs, dos, dks, dvs;
+  void *dk, *dv;
+  float* dq_acc;             // [parts][B * Hk * rows][d]
+  int parts;
+  int* turns;
+  int32_t* status;
+};
+
+}  // namespace range
+}  // namespace vmoba

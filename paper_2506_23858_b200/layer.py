@@ -408,6 +408,109 @@ class SteppedAttention:
         return "sparse"
 
 
+def key_ranges(lens, n_tokens=None, n_queries=None, frame: int = 0, prefix: int = 0, window: int = 0, device="cuda"):
+    """The key ranges of RangeAttention, int32 [.., n_queries, 2].
+
+    lens, with n_tokens: the lengths of the clips packed one behind another into a sequence of n_tokens (what is left over is padding
+    and sees nothing); [1, n_tokens, 2].  lens, with n_queries: the filled length of each sample's cache, of which the queries are the
+    last n_queries tokens; [len(lens), n_queries, 2].
+    frame: a token sees up to the end of its own group of that many tokens, counted from its clip's start (1: causal; 0: its whole
+    clip); prefix: the first tokens of a clip that all of it sees nevertheless; window: of those keys only the last so many."""
+    lens = torch.as_tensor(lens, dtype=torch.int64, device=device)
+    if (n_tokens is None) == (n_queries is None) or lens.dim() != 1 or lens.numel() == 0 or min(frame, prefix, window) < 0 or bool((lens < 0).any()):
+        raise ValueError("key_ranges: lengths, and either n_tokens or n_queries, none of them negative, required")
+    if n_tokens is not None:
+        ends = lens.cumsum(0)
+        if int(ends[-1]) > n_tokens:
+            raise ValueError("key_ranges: the clips do not fit into the sequence")
+        at = torch.arange(n_tokens, device=device)[None]
+        clip = torch.searchsorted(ends, at, right=True)
+        some = clip < lens.numel()
+        clip = clip.clamp(max=lens.numel() - 1)
+        lo, hi = (ends - lens)[clip], ends[clip]
+    else:
+        at = (lens - n_queries)[:, None] + torch.arange(n_queries, device=device)
+        lo, hi, some = torch.zeros_like(at), lens[:, None].expand_as(at), at >= 0
+    if frame:
+        hi = torch.minimum(hi, lo + torch.maximum(((at - lo) // frame + 1) * frame, torch.full_like(at, prefix)))
+    if window:
+        lo = torch.maximum(lo, hi - window)
+    return torch.stack([torch.where(some, lo, 0), torch.where(some, hi, 0)], -1).to(torch.int32).contiguous()
+
+
+class RangeAttention:
+    """Attention over key ranges, forward and gradients: the plan of the ranges, scratch, lse and the rounding residual.
+
+    shape: binding.make_range_shape(); key_range: int32 [1 or B, Sq, 2] on the device (key_ranges).  Tensors are [B, S, heads, d], in
+    whatever order of their dimensions but the last.  An object serves one stream at a time."""
+
+    def __init__(self, shape, key_range, with_backward: bool = False):
+        s = self.shape = shape
+        self.device = key_range.device
+        if not key_range.is_cuda or vb.range_plan_bytes(s) == 0:
+            raise ValueError("RangeAttention: a valid shape and key ranges on a GPU required")
+        e = lambda n, dt=torch.uint8: torch.empty(n, dtype=dt, device=self.device)
+        self.plan = e(vb.range_plan_bytes(s))
+        self.lse = e((s.B, s.heads, s.Sq), torch.float32)
+        self.dev_status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.o_resid = e((s.B, s.Sq, s.heads, s.head_dim), torch.bfloat16) if with_backward and s.dtype == vb.BF16 else None
+        self.ws = e(max(vb.range_workspace_bytes(s), vb.range_workspace_bytes(s, True) if with_backward else 0))
+        self.with_backward = with_backward
+        self._kept = None
+        self.set_ranges(key_range)
+
+    def set_ranges(self, key_range):
+        """Takes other key ranges (a cache that has grown, another packing)."""
+        s = self.shape
+        if tuple(key_range.shape) != (s.mask_batch, s.Sq, 2) or key_range.dtype != torch.int32 or key_range.device != self.device:
+            raise ValueError("RangeAttention: key ranges are int32 [mask_batch, Sq, 2] on the plan's device")
+        with _on(self.device):
+            vb.vmoba_range_plan(s, key_range.contiguous(), self.plan)
+
+    def _tensor(self, x, S, heads, what, written=False):
+        """x as the kernels can address it (an input that they cannot is copied) and its strides."""
+        s = self.shape
+        if tuple(x.shape) != (s.B, S, heads, s.head_dim) or x.dtype != torch_dtype(s) or x.device != self.device:
+            raise ValueError(f"RangeAttention: {what} has to be [{s.B}, {S}, {heads}, {s.head_dim}] of the shape's type on {self.device}")
+        st, per = _strides_bsh(x), 16 // x.element_size()
+        if x.stride(3) == 1 and x.data_ptr() % 16 == 0 and all(i % per == 0 and i >= s.head_dim for i in st):
+            return x, st
+        if written:
+            raise ValueError(f"RangeAttention: {what} needs 16-byte rows on 16-byte boundaries that do not share memory")
+        x = torch.empty(x.shape, dtype=x.dtype, device=x.device).copy_(x)
+        return x, _strides_bsh(x)
+
+    def forward(self, q, k, v, o_out):
+        """o_out = attention of q over k and v; self.lse [B, heads, Sq].  With a backward to come q, k, v and o_out stay as they are."""
+        s = self.shape
+        q, qs = self._tensor(q, s.Sq, s.heads, "q")
+        k, ks = self._tensor(k, s.Sk, s.kv_heads, "k")
+        v, vs = self._tensor(v, s.Sk, s.kv_heads, "v")
+        _, os_ = self._tensor(o_out, s.Sq, s.heads, "o_out", True)
+        with _on(self.device):
+            vb.vmoba_range_attn_fwd(s, self.plan, q, qs, k, ks, v, vs, o_out, os_, self.o_resid, self.lse, self.dev_status, self.ws)
+        if self.with_backward:
+            self._kept = (q, qs, k, ks, v, vs, o_out, os_)
+
+    def backward(self, do, dq_out, dk_out, dv_out):
+        """Gradients of the last forward()."""
+        s = self.shape
+        if self._kept is None:
+            raise ValueError("RangeAttention: backward() follows a forward() of an object made with_backward")
+        do, dos = self._tensor(do, s.Sq, s.heads, "do")
+        _, dqs = self._tensor(dq_out, s.Sq, s.heads, "dq_out", True)
+        _, dks = self._tensor(dk_out, s.Sk, s.kv_heads, "dk_out", True)
+        _, dvs = self._tensor(dv_out, s.Sk, s.kv_heads, "dv_out", True)
+        with _on(self.device):
+            vb.vmoba_range_attn_bwd(s, self.plan, *self._kept, self.o_resid, self.lse, do, dos, dq_out, dqs, dk_out, dks, dv_out, dvs,
+                                    self.dev_status, self.ws)
+
+    def check_status(self):
+        code = int(self.dev_status.item())
+        if code != vb.OK:
+            raise vb.VmobaError(code, "device status")
+
+
 def lists_from_mask(mask_bh, capacity=None, device="cuda"):
     """Builds kb_ptr / q_idx / q_ptr / q_pairs on the host from a boolean mask [BH, S, Nb]
     (used by tests to feed the attention kernels a selection that did not come from

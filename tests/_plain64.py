@@ -63,8 +63,8 @@ def block_order(x, grid, block):
 
 # ------------------------------------------------------------------------------------------------ attention over key ranges
 def range_attention(q, k, v, ranges, cap=0.0, scale=None, do=None):
-    """q [B, Sq, h, d], k and v [B, Sk, hk, d], ranges [1 or B, Sq, 2].  dict of o, lse [B, h, Sq] and, with do, dq, dk, dv, and of the
-    magnitudes o_mag, dq_mag, dk_mag, dv_mag."""
+    """q [B, Sq, h, d], k and v [B, Sk, hk, d], ranges [1 or B, Sq, 2].  dict of o, lse [B, h, Sq] and, with do, dq, dk, dv, of the
+    magnitudes o_mag, dq_mag, dk_mag, dv_mag, and the largest |q| |k| scale."""
     q, k, v = q.double(), k.double(), v.double()
     B, Sq, h, d = q.shape
     Sk, hk = k.shape[1], k.shape[2]
@@ -85,14 +85,16 @@ def range_attention(q, k, v, ranges, cap=0.0, scale=None, do=None):
     lse = torch.logsumexp(t, -1)
     p = torch.where(seen, torch.exp(t - lse.clamp(min=-1e300)[..., None]), torch.zeros((), dtype=t.dtype))
     back = lambda x, n, heads: x.permute(0, 3, 1, 2, 4).reshape(B, n, heads, d)
-    out = {"o": back(p @ vh, Sq, h), "o_mag": back(p @ vh.abs(), Sq, h), "lse": lse.reshape(B, h, Sq)}
+    norms = qh.norm(dim=-1).amax() * kh.norm(dim=-1).amax() * scale
+    out = {"top": float(norms), "o": back(p @ vh, Sq, h), "o_mag": back(p @ vh.abs(), Sq, h), "lse": lse.reshape(B, h, Sq)}
     if do is not None:
         doh = do.double().view(B, Sq, hk, G, d).permute(0, 2, 3, 1, 4)
         doh = torch.where(torch.isfinite(doh), doh, torch.zeros((), dtype=doh.dtype))
         oh = p @ vh
         dp, D = doh @ vh.transpose(-1, -2), (doh * oh).sum(-1, keepdim=True)
         slope = 1.0 - u.square() if cap else torch.ones((), dtype=t.dtype)
-        ds, ds_mag = p * (dp - D) * slope, p * (doh.abs() @ vh.abs().transpose(-1, -2) + (doh * oh).abs().sum(-1, keepdim=True)) * slope
+        ds = p * (dp - D) * slope
+        ds_mag = p * (doh.abs() @ vh.abs().transpose(-1, -2) + (doh.abs() * (p @ vh.abs())).sum(-1, keepdim=True)) * slope
         shared = lambda x: x.sum(2, keepdim=True)
         backk = lambda x: x.permute(0, 3, 1, 2, 4).reshape(B, Sk, hk, d)
         out |= {"dq": back(ds @ kh * scale, Sq, h), "dq_mag": back(ds_mag @ kh.abs() * scale, Sq, h),
