@@ -584,7 +584,7 @@ static int make_rdims(const vmoba_range_shape* s, RDims* o) {
   o->es = s->dtype == VMOBA_BF16 ? 2 : 4;
   o->scale = s->softmax_scale > 0.f ? s->softmax_scale : 1.0f / sqrtf((float)s->head_dim);
   o->cap = s->softcap;
-  o->tc = false;
+  o->tc = o->dtype == VMOBA_BF16 && o->d == 128;
   o->TR = o->tc ? 128 : 64;
   o->tpt = o->TR / o->G;
   o->rows = s->Sq * o->G;
@@ -637,11 +637,15 @@ static FwdWs carve_fwd(const RDims& D, int n, void* ws) {
   return w;
 }
 
-struct BwdWs { float* Dv; size_t bytes; Guards guards; };
+struct BwdWs { float *Dv, *dq_acc; int* turns; size_t bytes; Guards guards; };
 static BwdWs carve_bwd(const RDims& D, void* ws) {
   Carver c(ws);
   BwdWs w = {};
   w.Dv = c.take<float>((size_t)D.B * D.Hk * D.rows);
+  if (D.tc) {
+    w.dq_acc = c.take<float>((size_t)D.B * D.Hk * D.rows * D.d * tc_range_bwd_parts(D));
+    w.turns = c.take<int>((size_t)tc_range_bwd_turns(D));
+  }
   w.bytes = c.total();
   w.guards = c.guards;
   return w;
@@ -672,10 +676,14 @@ static bool early_rows(const RDims& D) { return (long long)D.B * D.Hq * D.Sq * D
 
 template <typename T, int DH>
 static int forward(const RDims& D, const Plan& plan, FwdArgs a, cudaStream_t st) {
-  const long long items = (long long)D.B * D.Hk * D.nI * a.splits;
-  VMOBA_CUDA_OK(allow_smem(range_fwd_kernel<T, DH>, simt::kFwdSmem<DH>));
-  launch_kernel(early_simt(D), range_fwd_kernel<T, DH>, grid_for(items, 8), kThreads, simt::kFwdSmem<DH>, st, D, plan, a);
-  VMOBA_LAUNCH_OK(1);
+  if constexpr (sizeof(T) == 2 && DH == 128) {
+    if (int rc = tc_range_fwd(D, plan, a, st)) return rc;
+  } else {
+    const long long items = (long long)D.B * D.Hk * D.nI * a.splits;
+    VMOBA_CUDA_OK(allow_smem(range_fwd_kernel<T, DH>, simt::kFwdSmem<DH>));
+    launch_kernel(early_simt(D), range_fwd_kernel<T, DH>, grid_for(items, 8), kThreads, simt::kFwdSmem<DH>, st, D, plan, a);
+    VMOBA_LAUNCH_OK(1);
+  }
   if (a.splits > 1) {
     launch_kernel(early_rows(D), range_merge_kernel<T, DH>, grid_for(((long long)D.B * D.Hk * D.rows + 7) / 8, 16), 256, 0, st, D, a);
     VMOBA_LAUNCH_OK(1);
@@ -688,14 +696,19 @@ static int backward(const RDims& D, const Plan& plan, const BwdArgs& a, const vo
                     void* dq, const Strides& dqs, cudaStream_t st) {
   const long long all_rows = (long long)D.B * D.Hk * D.rows;
   launch_kernel(early_rows(D), range_rowdot_kernel<T, DH>, grid_for((all_rows + 31) / 32, 16), 256, 0, st, D, plan, (const T*)o, os,
-                (const T*)resid, (const T*)a.d_o, a.dos, Dv, (int*)nullptr, 0ll);
-  VMOBA_CUDA_OK(allow_smem(range_bwd_dkdv_kernel<T, DH>, kRangeBwdSmem<DH>));
-  VMOBA_CUDA_OK(allow_smem(range_bwd_dq_kernel<T, DH>, kRangeBwdSmem<DH>));
-  launch_kernel(early_simt(D), range_bwd_dkdv_kernel<T, DH>, grid_for((long long)D.B * D.Hk * D.nK, 4), kThreads, kRangeBwdSmem<DH>, st, D, plan, a);
-  launch_kernel(early_simt(D), range_bwd_dq_kernel<T, DH>, grid_for((long long)D.B * D.Hk * D.nU, 4), kThreads, kRangeBwdSmem<DH>, st, D, plan, a,
-                (T*)dq, dqs);
-  VMOBA_LAUNCH_OK(3);
-  return VMOBA_OK;
+                (const T*)resid, (const T*)a.d_o, a.dos, Dv, a.turns, a.turns ? tc_range_bwd_turns(D) : 0ll);
+  VMOBA_LAUNCH_OK(1);
+  if constexpr (sizeof(T) == 2 && DH == 128) {
+    return tc_range_bwd(D, plan, a, dq, dqs, early_rows(D), st);
+  } else {
+    VMOBA_CUDA_OK(allow_smem(range_bwd_dkdv_kernel<T, DH>, kRangeBwdSmem<DH>));
+    VMOBA_CUDA_OK(allow_smem(range_bwd_dq_kernel<T, DH>, kRangeBwdSmem<DH>));
+    launch_kernel(early_simt(D), range_bwd_dkdv_kernel<T, DH>, grid_for((long long)D.B * D.Hk * D.nK, 4), kThreads, kRangeBwdSmem<DH>, st, D, plan, a);
+    launch_kernel(early_simt(D), range_bwd_dq_kernel<T, DH>, grid_for((long long)D.B * D.Hk * D.nU, 4), kThreads, kRangeBwdSmem<DH>, st, D, plan, a,
+                  (T*)dq, dqs);
+    VMOBA_LAUNCH_OK(2);
+    return VMOBA_OK;
+  }
 }
 
 #define VMOBA_RANGE_DISPATCH(rc, FN, ...)                                              \
@@ -793,6 +806,8 @@ extern "C" int vmoba_range_attn_bwd(const vmoba_range_shape* shape, const void* 
   BwdWs w = carve_bwd(D, ws);
   if (ws_bytes < w.bytes) return VMOBA_ERR_WORKSPACE;
   a.q = q; a.k = k; a.v = v; a.d_o = d_o; a.lse = lse; a.Dv = w.Dv; a.dk = dk; a.dv = dv; a.status = dev_status;
+  a.dq_acc = w.dq_acc; a.turns = w.turns;
+  if (D.tc) a.parts = tc_range_bwd_parts(D);
   if (D.dtype != VMOBA_BF16) o_resid_or_null = nullptr;
   const Plan p = carve_plan(D, plan, nullptr);
   cudaStream_t st = static_cast<cudaStream_t>(stream);

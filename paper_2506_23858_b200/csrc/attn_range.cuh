@@ -14,6 +14,8 @@
 
 #include <algorithm>
 
+#include <cuda.h>
+
 #include "common.cuh"
 
 namespace vmoba {
@@ -69,6 +71,13 @@ struct BwdArgs {
   int* turns;
   int32_t* status;
 };
+
+bool make_tmap_keys(CUtensorMap* map, const void* base, const RDims& D, const Strides& s);       // attn_range_fwd.cu
+bool make_tmap_units(CUtensorMap* map, const void* base, const RDims& D, const Strides& s);
+int tc_range_fwd(const RDims& D, const Plan& plan, const FwdArgs& a, cudaStream_t st);
+int tc_range_bwd(const RDims& D, const Plan& plan, const BwdArgs& a, void* dq, const Strides& dqs, bool early, cudaStream_t st);
+int tc_range_bwd_parts(const RDims& D);              // accumulators of dq
+long long tc_range_bwd_turns(const RDims& D);        // words of `turns`, zero ahead of the kernel
 
 }  // namespace range
 }  // namespace vmoba

@@ -1,0 +1,571 @@
+// Tensor-core forward of attention over key ranges (bf16, head_dim 128).
+//
+// The wide forward of attn_tc_fwd.cu (two 128-row query tiles A and B that share every tile of K and V, one score buffer that they
+// use in turn, softmax threads that hold a whole row of 128 scores) with the items of a plan: an item is two units of packed rows against
+// the hull of their key ranges (or a share of it, where the range is split), in tiles of 128 keys from the hull's first key on.  A unit
+// takes part in the tiles that its own hull reaches; a score is compared with its row's range only in tiles where the unit's
+// bounds say that some row needs it.
+//
+// Every (item, unit) has at least one tile, masked as a whole if need be, and every tile at least one unit, so that no barrier skips a phase.
+//
+//   warp 0        TMA: K tiles into a ring of two stages, V tiles into one of three
+//   warps 1, 2    MMA issuers: Q K^T; P V (which first clears what a hull's last tile holds behind its last key: a weight of 0 times a
+//                 value that is not finite would not be 0)
+//   warps 4-11    softmax of unit A, of unit B: thread = row
+//   warps 12-15   Q tiles of the next item, o of the one before
+//
+// Capped scores: c tanh(x) = c - 2 c / (1 + exp(2 x)), with 2 x = 2 scale s / c; a weight is exp2(c' - m - 2 c' r) with r = 1 / (1 +
+// exp2(s k)), c' = c log2 e.  tanh is monotone, so the row's maximum is looked for among the uncapped scores.
+#include <algorithm>
+
+#include "attn_range.cuh"
+#include "sm100.cuh"
+
+namespace vmoba {
+namespace range {
+namespace tcf {
+
+using namespace sm100;
+
+constexpr int BM = 128, BN = 128, DH = 128;
+constexpr int KST = 2, VST = 3;
+constexpr int PANEL = BM * 128;      // bytes of one 64-column panel of a 128-row tile (16 KB)
+constexpr int TILE = 2 * PANEL;      // bytes of a [128 x 128] bf16 tile (32 KB)
+constexpr int THREADS = 512;         // warp groups {TMA, MMA, MMA, -}, A, B, loaders; registers 56, 200, 200, 56 (= 4 x 128)
+constexpr uint32_t TMEM_COLS = 512;
+constexpr uint32_t P_COL = 128, O_COL = 256;      // S at 0, P_X at 128 + 64 X, O_X at 256 + 128 X
+constexpr float RESCALE_LOG2 = 8.0f;
+constexpr float LOG2E = 1.4426950408889634f;
+
+struct Smem {
+  uint64_t k_full[KST], k_empty[KST], v_full[VST], v_empty[VST];
+  uint64_t s_full[2], p_ready[2];    // per unit: scores written (commit) / P written (128 arrivals)
+  uint64_t s_free;                   // the score buffer has been read (128 arrivals of whichever unit used it)
+  uint64_t o_done[2];                // per unit: P V of a key tile complete (commit)
+  uint64_t ep_ready[2];              // per unit: an item's normalisers are in ep_inv / ep_lse (128 softmax arrivals)
+  uint64_t o_free[2];                // per unit: epilogue has read them and the accumulator (128 arrivals)
+  uint64_t q_full, q_empty;          // Q tiles of an item landed / no longer needed (commit)
+  uint64_t drain[2];                 // (after a time-out only)
+  uint32_t tmem_base;
+  int abort_flag;
+  float ep_inv[2][BM], ep_lse[2][BM];   // 1 / sum of the rounded weights (0: the row saw nothing), natural-log lse
+};
+constexpr size_t SMEM_BYTES = (2 /*Q*/ + KST + VST) * TILE + sizeof(Smem) + 32;
+static_assert(SMEM_BYTES <= 232448, "range forward: shared memory");
+
+struct Params {
+  int B, Hk, G, Sq, Sk, Bm, tpt, nU, nI, splits, n_items;
+  const int2* rows;
+  const int4* units;
+  const int* order;
+  float scale_log2;      // scores -> exp2 domain: scale * log2 e, or capped: k = 2 scale log2 e / cap
+  float cap_log2;        // cap * log2 e
+  __nv_bfloat16 *o, *resid;
+  Strides os;
+  float* lse;
+  float *part_o, *part_lse;
+  int32_t* status;
+};
+
+struct Item {
+  int b, hk, u0, nx, split;
+  int k_begin, keys;               // first key of the item's tiles, keys in them (0: all masked)
+  int ntiles;
+  int tb[2], te[2];                // per unit: its tiles
+  int full_lo[2], full_hi[2];      // per unit: every row sees the keys between these
+};
+
+__device__ __forceinline__ Item decode_item(const Params& p, int item) {
+  Item it;
+  const int m = item / p.splits;
+  it.split = item - m * p.splits;
+  const int bhk = m / p.nI;
+  it.b = bhk / p.Hk;
+  it.hk = bhk - it.b * p.Hk;
+  const int bm = mask_batch(p.Bm, it.b);
+  it.u0 = 2 * __ldg(p.order + (long long)bm * p.nI + (m - bhk * p.nI));
+  it.nx = it.u0 + 1 < p.nU ? 2 : 1;
+  const int4* units = p.units + (long long)bm * p.nU + it.u0;
+  const int4 a = __ldg(units), c = it.nx == 2 ? __ldg(units + 1) : make_int4(0, 0, 0, 0);
+  int lo = a.x, hi = a.y;
+  if (c.y > c.x) {
+    lo = hi > lo ? min(lo, c.x) : c.x;
+    hi = max(hi, c.y);
+  }
+  const int all = (max(hi - lo, 0) + BN - 1) / BN;
+  int first, last;
+  share(all, it.split, p.splits, first, last);
+  it.k_begin = lo + first * BN;
+  it.keys = max(min(lo + last * BN, hi) - it.k_begin, 0);
+  if (it.keys == 0) it.k_begin = 0;
+  it.ntiles = max(last - first, 1);
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int4 u = x ? c : a;
+    const int from = u.x - it.k_begin, to = min(u.y - it.k_begin, it.keys);
+    it.tb[x] = max(from, 0) / BN;
+    it.te[x] = (max(to, 0) + BN - 1) / BN;
+    if (it.tb[x] >= it.te[x]) { it.tb[x] = 0; it.te[x] = 1; }
+    it.full_lo[x] = u.z;
+    it.full_hi[x] = u.w;
+  }
+  if (it.nx == 2) {                // no tile without a unit
+    if (it.tb[0] > 0 && it.tb[1] > 0) { if (it.tb[0] <= it.tb[1]) it.tb[0] = 0; else it.tb[1] = 0; }
+    if (it.te[0] < it.ntiles && it.te[1] < it.ntiles) { if (it.te[0] >= it.te[1]) it.te[0] = it.ntiles; else it.te[1] = it.ntiles; }
+    if (it.te[0] < it.tb[1]) it.te[0] = it.tb[1];
+    if (it.te[1] < it.tb[0]) it.te[1] = it.tb[0];
+  } else {
+    it.tb[0] = 0;
+    it.te[0] = it.ntiles;
+  }
+  return it;
+}
+// The same, known to be the same on all lanes of a warp (values from memory pass through a warp reduction).
+__device__ __forceinline__ Item uniform_item(const Params& p, int item) {
+  Item it = decode_item(p, item);
+  auto u = [](int v) { return __reduce_max_sync(0xffffffffu, v); };
+  it.nx = u(it.nx);
+  it.keys = u(it.keys);
+  it.ntiles = u(it.ntiles);
+#pragma unroll
+  for (int x = 0; x < 2; ++x) { it.tb[x] = u(it.tb[x]); it.te[x] = u(it.te[x]); }
+  return it;
+}
+// Keys of tile t that the matrix products take: whole steps of 16, one at least.
+__device__ __forceinline__ int key_steps(const Item& it, int t) { return (max(min(BN, it.keys - t * BN), 1) + 15) >> 4; }
+
+__device__ __forceinline__ constexpr uint32_t koff(int ks) { return (uint32_t)(((ks >> 2) * PANEL + (ks & 3) * 32) >> 4); }
+__device__ __forceinline__ constexpr uint32_t mnoff(int ks) { return (uint32_t)((ks * 2048) >> 4); }
+
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Weights of 32 scores; bf16 pairs (keys 2i, 2i+1 -> word i).  s0/s1 collect the exact weights, r0/r1 the rounded ones (the tensor core
+// multiplies the ROUNDED weights: o is normalised by their sum, so that the rounding perturbs the weights but never their total).
+// neg_m: minus the row's reference maximum; capped: c' minus it.
+template <bool CAP>
+__device__ __forceinline__ void exp_pack32(const uint32_t* sv, float scale, float cap2, float neg_m, bool masked, uint32_t (&pk)[16],
+                                           float& s0, float& s1, float& r0, float& r1) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float p0, p1;
+    const float x0 = __uint_as_float(sv[2 * i]), x1 = __uint_as_float(sv[2 * i + 1]);
+    if constexpr (CAP) {
+      mul2(p0, p1, x0, x1, scale, scale);
+      p0 = ex2(p0);
+      p1 = ex2(p1);
+      add2(p0, p1, p0, p1, 1.0f, 1.0f);
+      p0 = rcp(p0);
+      p1 = rcp(p1);
+      fma2(p0, p1, p0, p1, -cap2, -cap2, neg_m, neg_m);
+      p0 = ex2(p0);
+      p1 = ex2(p1);
+      if (masked) {                  // (uniform)
+        if (sv[2 * i] == 0xff800000u) p0 = 0.f;
+        if (sv[2 * i + 1] == 0xff800000u) p1 = 0.f;
+      }
+    } else {
+      fma2(p0, p1, x0, x1, scale, scale, neg_m, neg_m);
+      p0 = ex2(p0);
+      p1 = ex2(p1);
+    }
+    add2(s0, s1, s0, s1, p0, p1);
+    pk[i] = pack_bf16(p0, p1);
+    add_bf16_pair(r0, r1, pk[i]);
+  }
+}
+
+__device__ __forceinline__ void store8_resid(__nv_bfloat16* dst, __nv_bfloat16* rdst, const float (&v)[8]) {
+  uint32_t h[4], r[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    h[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
+    r[k] = pack_bf16(v[2 * k] - __uint_as_float(h[k] << 16), v[2 * k + 1] - __uint_as_float(h[k] & 0xffff0000u));
+  }
+  *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
+  if (rdst) *reinterpret_cast<uint4*>(rdst) = make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+template <bool CAP>
+__global__ void __launch_bounds__(THREADS, 1)
+attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                      const __grid_constant__ CUtensorMap tmQ, const Params p) {
+  if (!grid_begin()) return;
+  extern __shared__ uint8_t smem_raw[];
+  // the swizzled tiles need 1024-byte alignment and there is no room for alignment slack
+  if ((smem_u32(smem_raw) & 1023u) != 0) {
+    if (threadIdx.x == 0) set_status(p.status, VMOBA_ERR_CUDA);
+    return;
+  }
+  uint8_t* sQ = smem_raw;                  // [2 units][TILE]
+  uint8_t* sK = sQ + 2 * TILE;             // [KST][TILE]
+  uint8_t* sV = sK + KST * TILE;           // [VST][TILE]
+  Smem* sm = reinterpret_cast<Smem*>(sV + VST * TILE);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* abort_flag = &sm->abort_flag;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < KST; ++s) { mbar_init(&sm->k_full[s], 1); mbar_init(&sm->k_empty[s], 1); }
+    for (int s = 0; s < VST; ++s) { mbar_init(&sm->v_full[s], 1); mbar_init(&sm->v_empty[s], 1); }
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(&sm->s_full[x], 1); mbar_init(&sm->p_ready[x], 128);
+      mbar_init(&sm->o_done[x], 1); mbar_init(&sm->o_free[x], 128); mbar_init(&sm->ep_ready[x], 128);
+    }
+    mbar_init(&sm->s_free, 128);
+    mbar_init(&sm->q_full, 1); mbar_init(&sm->q_empty, 1);
+    mbar_init(&sm->drain[0], 1); mbar_init(&sm->drain[1], 1);
+    sm->abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tmap(&tmK);
+    prefetch_tmap(&tmV);
+    prefetch_tmap(&tmQ);
+  }
+  if (warp == 1) {
+    tmem_alloc(&sm->tmem_base, TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sm->tmem_base;
+  constexpr uint32_t IDESC_PV = make_idesc_bf16(BM, DH, false, true);
+
+  if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      uint32_t ks = 0, kp = 1, vs = 0, vp = 1;       // ring slots and the parities of their `empty` waits (the first pass at once)
+      for (int item = blockIdx.x; item < p.n_items; item += gridDim.x) {
+        const Item it = decode_item(p, item);
+        for (int t = 0; t < it.ntiles; ++t) {
+          const int y = it.k_begin + t * BN;
+          mbar_wait(&sm->k_empty[ks], kp, abort_flag, p.status);
+          mbar_expect_tx(&sm->k_full[ks], TILE);
+          tma_load_4d(sK + ks * TILE, &tmK, &sm->k_full[ks], 0, y, it.hk, it.b);
+          tma_load_4d(sK + ks * TILE + PANEL, &tmK, &sm->k_full[ks], 64, y, it.hk, it.b);
+          mbar_wait(&sm->v_empty[vs], vp, abort_flag, p.status);
+          mbar_expect_tx(&sm->v_full[vs], TILE);
+          tma_load_4d(sV + vs * TILE, &tmV, &sm->v_full[vs], 0, y, it.hk, it.b);
+          tma_load_4d(sV + vs * TILE + PANEL, &tmV, &sm->v_full[vs], 64, y, it.hk, it.b);
+          // drain: every issued load must have landed before the CTA may exit (only matters after a timeout)
+          if (*abort_flag) {
+            mbar_wait(&sm->k_full[ks], kp ^ 1, abort_flag, p.status);
+            mbar_wait(&sm->v_full[vs], vp ^ 1, abort_flag, p.status);
+          }
+          if (++ks == KST) { ks = 0; kp ^= 1; }
+          if (++vs == VST) { vs = 0; vp ^= 1; }
+        }
+      }
+    }
+  } else if (warp <= 2) {
+    // ------------------------------------------------------------------ MMA issuers: the whole warp walks the loop, one elected lane
+    // issues (warp-uniform control flow; see elect_one); the lanes look at an operation's barriers at once.
+    const bool leader = elect_one();
+    auto wait3 = [&](uint64_t* b0, uint32_t p0, uint64_t* b1, uint32_t p1, bool third, uint64_t* b2, uint32_t p2) {
+      const int which = lane & 3;
+      uint32_t bar = smem_u32(b0), par = p0;
+      if (which == 1) { bar = smem_u32(b1); par = p1; }
+      if (which == 2 && third) { bar = smem_u32(b2); par = p2; }
+      mbar_wait_lanes(bar, par, abort_flag, p.status);
+      __syncwarp();
+      tc_fence_after();
+    };
+    if (warp == 1) {
+      uint32_t uses = 0, n = 0, slot = 0, par = 0;      // uses of the score buffer, items, K ring position
+      const uint32_t lo_q = desc_lo(smem_u32(sQ), 16), lo_k = desc_lo(smem_u32(sK), 16);
+      for (int item = blockIdx.x; item < p.n_items; item += gridDim.x, ++n) {
+        const Item it = uniform_item(p, item);
+        bool first = true;
+        for (int t = 0; t < it.ntiles; ++t) {
+          const uint32_t idesc = make_idesc_bf16(BM, 16 * key_steps(it, t), false, false);
+          const uint32_t dk = lo_k + slot * (uint32_t)(TILE >> 4);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (x >= it.nx || t < it.tb[x] || t >= it.te[x]) continue;
+            // the score buffer has been read (its first use waits for a phase before the first: passes at once), the K tile
+            // is there, and the item's Q tiles
+            wait3(&sm->s_free, (uses + 1) & 1, &sm->k_full[slot], par, first, &sm->q_full, n & 1);
+            first = false;
+            ++uses;
+            const uint32_t dq = lo_q + x * (uint32_t)(TILE >> 4);
+#pragma unroll
+            for (int ks = 0; ks < DH / 16; ++ks)
+              if (leader) mma_ss_lo(tmem, dq + koff(ks), dk + koff(ks), idesc, ks > 0 ? 1u : 0u);
+            if (leader) mma_commit(&sm->s_full[x]);
+          }
+          if (leader) mma_commit(&sm->k_empty[slot]);
+          if (leader && t == it.ntiles - 1) mma_commit(&sm->q_empty);
+          if (++slot == KST) { slot = 0; par ^= 1; }
+        }
+      }
+    } else {
+      uint32_t tcnt[2] = {0, 0}, ecnt[2] = {0, 0}, slot = 0, par = 0;      // per unit: P V and items done; V ring position
+      const uint32_t lo_v = desc_lo(smem_u32(sV), PANEL);
+      for (int item = blockIdx.x; item < p.n_items; item += gridDim.x) {
+        const Item it = uniform_item(p, item);
+        for (int t = 0; t < it.ntiles; ++t) {
+          const int ksteps = key_steps(it, t);
+          int clear = t == it.ntiles - 1 ? max(it.keys - t * BN, 0) : BN;      // rows from here on are not the item's
+          const uint32_t mv = lo_v + slot * (uint32_t)(TILE >> 4);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (x >= it.nx || t < it.tb[x] || t >= it.te[x]) continue;
+            // P has been written, the V tile is there, the epilogue of the unit's previous item has read the accumulator
+            wait3(&sm->p_ready[x], tcnt[x] & 1, &sm->v_full[slot], par, t == it.tb[x], &sm->o_free[x], (ecnt[x] + 1) & 1);
+            tcnt[x] += 1;
+            if (clear < 16 * ksteps) {
+              for (int r = clear + (lane >> 4); r < 16 * ksteps; r += 2)
+                *reinterpret_cast<uint4*>(sV + slot * TILE + (lane >> 3 & 1) * PANEL + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+              fence_async_proxy();
+              __syncwarp();
+              clear = BN;
+            }
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+              if (leader && ks < ksteps)   // P of keys 16 ks .. 16 ks + 15 sits in columns 8 ks .. of the unit's P buffer
+                mma_ts_lo(tmem + O_COL + x * 128, tmem + P_COL + x * 64 + ks * 8, mv + mnoff(ks), IDESC_PV, (t > it.tb[x] || ks > 0) ? 1u : 0u);
+            if (leader) mma_commit(&sm->o_done[x]);
+          }
+          if (leader) mma_commit(&sm->v_empty[slot]);
+          if (++slot == VST) { slot = 0; par ^= 1; }
+        }
+        ecnt[0] += 1;
+        if (it.nx == 2) ecnt[1] += 1;
+      }
+    }
+    if (leader && *abort_flag) mma_drain(&sm->drain[warp - 1]);      // (nothing is under way when the CTA frees its TMEM)
+  } else if (warp >= 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    // ------------------------------------------------------------------ the Q tiles of item n, then o of item n - 1
+    const int lt = (warp - 12) * 32 + lane;   // 0..127: row of a unit
+    const int rows = p.tpt * p.G, rt = lt / p.G, rg = lt - rt * p.G;
+    uint32_t n = 0;
+    uint32_t tcs[2] = {0, 0}, eps[2] = {0, 0};        // per unit: P V and items done
+    const long long all_rows = (long long)p.B * p.Hk * p.Sq * p.G;
+    auto epilogue = [&](const Item& it) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        if (x >= it.nx) continue;
+        const uint32_t o_tmem = tmem + ((uint32_t)((warp & 3) * 32) << 16) + O_COL + x * 128;
+        const int tok = (it.u0 + x) * p.tpt + rt;
+        const bool row_ok = lt < rows && tok < p.Sq;
+        const long long head = (long long)it.hk * p.G + rg;
+        const long long packed = ((long long)it.b * p.Hk + it.hk) * p.Sq * p.G + (long long)tok * p.G + rg + it.split * all_rows;
+        tcs[x] += it.te[x] - it.tb[x];
+        mbar_wait(&sm->ep_ready[x], eps[x] & 1, abort_flag, p.status);
+        eps[x] += 1;
+        const float inv = sm->ep_inv[x][lt], row_lse = sm->ep_lse[x][lt];
+        mbar_wait(&sm->o_done[x], (tcs[x] - 1) & 1, abort_flag, p.status);
+        tc_fence_after();
+        __nv_bfloat16* o_row = p.o + it.b * p.os.b + tok * p.os.t + head * p.os.h;
+        __nv_bfloat16* r_row = p.resid ? p.resid + (((long long)it.b * p.Sq + tok) * p.Hk * p.G + head) * DH : nullptr;
+#pragma unroll 1
+        for (int c = 0; c < 8; ++c) {
+          uint32_t ov[16];
+          tmem_ld16(o_tmem + c * 16, ov);
+          tmem_ld_wait();
+          if (c == 7) {
+            tc_fence_before();
+            mbar_arrive(&sm->o_free[x]);
+          }
+          if (row_ok) {
+            const int col = 16 * c;
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = inv == 0.f ? 0.f : __uint_as_float(ov[i]) * inv;
+            if (p.splits == 1) {
+#pragma unroll
+              for (int i = 0; i < 16; i += 8)
+                store8_resid(o_row + col + i, r_row ? r_row + col + i : nullptr, *reinterpret_cast<const float(*)[8]>(&v[i]));
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; i += 4) store4(p.part_o + packed * DH + col + i, make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
+            }
+          }
+        }
+        if (row_ok) {
+          if (p.splits == 1) p.lse[((long long)it.b * p.Hk * p.G + head) * p.Sq + tok] = row_lse;
+          else p.part_lse[packed] = row_lse;
+        }
+      }
+    };
+    for (int item = blockIdx.x; item < p.n_items; item += gridDim.x, ++n) {
+      if (lt == 0) {
+        const Item it = decode_item(p, item);
+        if (n >= 1) mbar_wait(&sm->q_empty, (n - 1) & 1, abort_flag, p.status);
+        mbar_expect_tx(&sm->q_full, (uint32_t)(it.nx * rows * DH * 2));
+        for (int x = 0; x < it.nx; ++x) {
+          const int tok = (it.u0 + x) * p.tpt;
+          tma_load_5d(sQ + x * TILE, &tmQ, &sm->q_full, 0, 0, tok, it.hk, it.b);
+          tma_load_5d(sQ + x * TILE + PANEL, &tmQ, &sm->q_full, 64, 0, tok, it.hk, it.b);
+        }
+        if (*abort_flag) mbar_wait(&sm->q_full, n & 1, abort_flag, p.status);     // landed before the CTA may exit
+      }
+      __syncwarp();
+      if (n >= 1) epilogue(decode_item(p, item - (int)gridDim.x));      // (read again: two items do not fit the registers)
+    }
+    if (n >= 1) epilogue(decode_item(p, (int)blockIdx.x + (int)(n - 1) * (int)gridDim.x));
+  } else if (warp >= 4) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    // ------------------------------------------------------------------ softmax of one unit
+    const int x = (warp - 4) >> 2;                  // unit of this warp group
+    const int quad = warp & 3;                      // TMEM lane quarter this warp may access
+    const int r = quad * 32 + lane;                 // row of the unit
+    const int rt = r / p.G;
+    const bool is_row = r < p.tpt * p.G;
+    const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
+    const uint32_t s_tmem = tmem + lane_addr;
+    const uint32_t p_tmem = tmem + lane_addr + P_COL + x * 64;
+    const uint32_t o_tmem = tmem + lane_addr + O_COL + x * 128;
+    uint32_t tc = 0, items = 0;                      // key tiles and items done on this unit
+    for (int item = blockIdx.x; item < p.n_items; item += gridDim.x) {
+      const Item it = decode_item(p, item);
+      if (x >= it.nx) continue;
+      const int tok = (it.u0 + x) * p.tpt + rt;
+      int2 seen = make_int2(0, 0);
+      if (is_row && tok < p.Sq) seen = __ldg(p.rows + (long long)mask_batch(p.Bm, it.b) * p.Sq + tok);
+      // of the item's keys: [seen.x, seen.y)
+      seen.x = max(seen.x - it.k_begin, 0);
+      seen.y = min(seen.y - it.k_begin, it.keys);
+      const int tb = it.tb[x], te = it.te[x], full_lo = it.full_lo[x] - it.k_begin, full_hi = min(it.full_hi[x] - it.k_begin, it.keys);
+      float m_used = -INFINITY, l = 0.f, l_r = 0.f;   // l: exact sum (for LSE); l_r: sum of the bf16-rounded weights
+      for (int t = tb; t < te; ++t, ++tc) {
+        mbar_wait(&sm->s_full[x], tc & 1, abort_flag, p.status);
+        tc_fence_after();
+        const bool masked = full_lo > t * BN || full_hi < t * BN + BN;
+        const int valid = min(BN, it.keys - t * BN);
+        uint32_t sv[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(s_tmem + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(&sv[32 * c]));
+        tmem_ld_wait();
+        tc_fence_before();
+        mbar_arrive(&sm->s_free);                    // the other unit's Q K^T may have the buffer
+        if (masked) {                                // keys outside the row's range get score -inf
+          const int a = seen.x - t * BN, n = max(seen.y - t * BN - a, 0);
+#pragma unroll
+          for (int i = 0; i < BN; ++i)
+            if ((unsigned)(i - a) >= (unsigned)n) sv[i] = 0xff800000u;
+        }
+        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < BN; i += 8) {
+          mx0 = max3(mx0, __uint_as_float(sv[i]), __uint_as_float(sv[i + 1]));
+          mx1 = max3(mx1, __uint_as_float(sv[i + 2]), __uint_as_float(sv[i + 3]));
+          mx2 = max3(mx2, __uint_as_float(sv[i + 4]), __uint_as_float(sv[i + 5]));
+          mx3 = max3(mx3, __uint_as_float(sv[i + 6]), __uint_as_float(sv[i + 7]));
+        }
+        float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+        if (CAP) mx = mx == -INFINITY ? mx : fmaf(-2.0f * p.cap_log2, rcp(1.0f + ex2(mx * p.scale_log2)), p.cap_log2);
+        else mx *= p.scale_log2;                     // exp2 domain from here on (the scale is positive)
+        // lazy rescale: keep the old reference max unless the new one is more than 2^8 larger
+        float factor = 1.0f;
+        bool need = false;
+        if (t == tb) {
+          m_used = mx;
+        } else if (mx > m_used + RESCALE_LOG2) {
+          need = m_used > -INFINITY;                 // (else the row has seen nothing so far: its sums are 0)
+          factor = need ? ex2(m_used - mx) : 1.0f;
+          m_used = mx;
+        }
+        auto rescale_o = [&]() {                     // P V of the tile before is complete
+#pragma unroll 1
+          for (int c = 0; c < 8; ++c) {
+            uint32_t ov[16];
+            tmem_ld16(o_tmem + c * 16, ov);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * factor);
+            tmem_st16(o_tmem + c * 16, ov);
+          }
+        };
+        float s0 = 0.f, s1 = 0.f, r0 = 0.f, r1 = 0.f;
+        const float neg_m = (m_used == -INFINITY ? 0.f : -m_used) + (CAP ? p.cap_log2 : 0.f);
+        const float cap2 = 2.0f * p.cap_log2;
+        {
+          // the first half's weights stay in registers until P V of the tile before has read the P buffer
+          uint32_t pk[2][16];
+          exp_pack32<CAP>(sv, p.scale_log2, cap2, neg_m, masked, pk[0], s0, s1, r0, r1);
+          const uint32_t pv_done = mbar_test_wait(&sm->o_done[x], (tc + 1) & 1);      // (an early look, because the answer takes its time)
+          if (valid > 32) exp_pack32<CAP>(sv + 32, p.scale_log2, cap2, neg_m, masked, pk[1], s0, s1, r0, r1);
+          if (tc > 0) {                              // (of the item before, where t is its first)
+            if (!__all_sync(0xffffffffu, pv_done)) mbar_wait(&sm->o_done[x], (tc - 1) & 1, abort_flag, p.status);
+            tc_fence_after();
+            if (t > tb && __any_sync(0xffffffffu, need)) {
+              rescale_o();
+              l *= factor;
+              l_r *= factor;
+            }
+          }
+          tmem_st16(p_tmem, pk[0]);
+          tmem_st16(p_tmem + 16, pk[1]);             // (whatever it holds where valid <= 32: P V does not read it)
+        }
+#pragma unroll
+        for (int c = 2; c < 4; ++c) {
+          if (32 * c < valid) {                      // (uniform; P V takes the keys up to `valid` only)
+            uint32_t pk[16];
+            exp_pack32<CAP>(sv + 32 * c, p.scale_log2, cap2, neg_m, masked, pk, s0, s1, r0, r1);
+            tmem_st16(p_tmem + 16 * c, pk);
+          }
+        }
+        l += s0 + s1;
+        l_r += r0 + r1;
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&sm->p_ready[x]);
+      }
+      // ---- hand the row's normalisers to the epilogue warps, once they are through with the unit's previous item, and go on
+      if (items >= 1) mbar_wait(&sm->o_free[x], (items - 1) & 1, abort_flag, p.status);
+      sm->ep_inv[x][r] = l_r == 0.f ? 0.f : 1.0f / l_r;
+      sm->ep_lse[x][r] = l == 0.f ? -INFINITY : (m_used + log2f(l)) * 0.6931471805599453f;
+      mbar_arrive(&sm->ep_ready[x]);
+      ++items;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) tmem_dealloc(tmem, TMEM_COLS);
+}
+
+}  // namespace tcf
+
+// K or V: {head_dim, tokens, heads, samples}, a tile of 128 tokens; Q or dO: {head_dim, heads of a group, tokens, key heads, samples}, a
+// unit of packed rows.
+bool make_tmap_keys(CUtensorMap* map, const void* base, const RDims& D, const Strides& s) {
+  const uint64_t n[4] = {(uint64_t)D.d, (uint64_t)D.Sk, (uint64_t)D.Hk, (uint64_t)D.B};
+  const uint64_t st[4] = {1, (uint64_t)s.t, (uint64_t)s.h, (uint64_t)s.b};
+  const uint32_t box[4] = {64, 128, 1, 1};
+  return sm100::make_tmap_bf16_strided(map, base, 4, n, st, box);
+}
+bool make_tmap_units(CUtensorMap* map, const void* base, const RDims& D, const Strides& s) {
+  const uint64_t n[5] = {(uint64_t)D.d, (uint64_t)D.G, (uint64_t)D.Sq, (uint64_t)D.Hk, (uint64_t)D.B};
+  const uint64_t st[5] = {1, (uint64_t)s.h, (uint64_t)s.t, (uint64_t)s.h * D.G, (uint64_t)s.b};
+  const uint32_t box[5] = {64, (uint32_t)D.G, (uint32_t)D.tpt, 1, 1};
+  return sm100::make_tmap_bf16_strided(map, base, 5, n, st, box);
+}
+
+int tc_range_fwd(const RDims& D, const Plan& plan, const FwdArgs& a, cudaStream_t st) {
+  using namespace tcf;
+  const long long items = (long long)D.B * D.Hk * D.nI * a.splits;
+  if (items > (long long)INT32_MAX - 4096) return VMOBA_ERR_SHAPE;
+  Params p;
+  p.B = D.B; p.Hk = D.Hk; p.G = D.G; p.Sq = D.Sq; p.Sk = D.Sk; p.Bm = D.Bm; p.tpt = D.tpt; p.nU = D.nU; p.nI = D.nI;
+  p.splits = a.splits; p.n_items = (int)items;
+  p.rows = plan.rows; p.units = plan.units; p.order = plan.order;
+  p.scale_log2 = D.cap > 0.f ? 2.0f * D.scale * LOG2E / D.cap : D.scale * LOG2E;
+  p.cap_log2 = D.cap * LOG2E;
+  p.o = (__nv_bfloat16*)a.o; p.resid = (__nv_bfloat16*)a.resid; p.os = a.os; p.lse = a.lse;
+  p.part_o = a.part_o; p.part_lse = a.part_lse; p.status = a.status;
+  CUtensorMap tmK, tmV, tmQ;
+  if (!make_tmap_keys(&tmK, a.k, D, a.ks) || !make_tmap_keys(&tmV, a.v, D, a.vs) || !make_tmap_units(&tmQ, a.q, D, a.qs)) return VMOBA_ERR_CUDA;
+  auto kernel = D.cap > 0.f ? attn_range_fwd_kernel<true> : attn_range_fwd_kernel<false>;
+  VMOBA_CUDA_OK(allow_smem(kernel, (int)SMEM_BYTES));
+  launch_kernel(kernel, (unsigned)std::min<long long>(items, sm_count()), THREADS, SMEM_BYTES, st, tmK, tmV, tmQ, p);
+  VMOBA_LAUNCH_OK(1);
+  return VMOBA_OK;
+}
+
+}  // namespace range
+}  // namespace vmoba
