@@ -5,23 +5,39 @@
 // Backward: g = the gradient of out turned by -a (times m), then with s = w g:
 //   dx = r (s - x r^2 mean(s x)),   dw = sum over tokens (norm per head: and heads) of g x r.
 //
-// Bound by HBM: a row of a token (all heads) is read once and written once, forward; the gradient, x and dx, backward.  The
-// norm's two trips through a row are one through memory because the row stays in registers (up to eight 16-byte vectors per
-// thread; longer rows are read twice).  A row is taken by 1, 2, 4 or 8 warps.  The angles of a token are worked out once for all heads and
-// tensors of a CTA: product and reduction to (-pi, pi] in 64 bits, because a position of 10^6 times a frequency of one has no digit
-// behind the point left in 32.
+// Bound by HBM (a row of a token, all heads, is read once and written once, forward; the gradient, x and dx, backward) and, closely
+// behind, by instruction issue.  So: a row is taken by as few warps as hold it in six 16-byte vectors per thread, each warp or
+// group of warps on its own, token after token; a thread has the same channels of every head, so that its sines and cosines are
+// loaded once per token; angles are worked out once per token for all heads and tensors; layouts and vectors per thread are compiled in.
+// The norm's two trips through a row are one through memory: vectors come in by asynchronous copies into a ring of shared
+// memory that each thread has to itself, rows ahead of their use; rows longer than that are read twice.
+// An angle is formed and reduced in 64 bits, because a position of 10^6 times a frequency of one has no digit behind the point left in 32.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
+#include "sm100.cuh"
 
 namespace vmoba {
 namespace rotary {
 
+using sm100::fma2;
+using sm100::mul2;
+
 constexpr int kMaxTensors = 4;
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int NV = 8;                        // 16-byte vectors of a row per thread and trip
-constexpr int kMaxTok = 16;                  // tokens of a CTA at a time
+constexpr int kMaxWarps = 8;                 // of a CTA, and of a row
+constexpr int kMaxPairs = 64;
+
+// Quotients by a divisor known to the host, of numbers below 2^31.
+struct FastDiv {
+  unsigned m, s;
+  FastDiv() = default;
+  explicit FastDiv(unsigned d) : m(0), s(0) {
+    while ((1u << s) < d) ++s;
+    m = (unsigned)(((1ull << (31 + s)) + d - 1) / d);      // ceil(2^(31 + s) / d), below 2^32 for 2^(s - 1) < d <= 2^s
+  }
+  __device__ __forceinline__ int div(int n) const { return s ? (int)(__umulhi((unsigned)n, m) >> (s - 1)) : n; }
+};
 
 struct Tensor {
   const void* src;                           // forward: x; backward: the gradient of the output
@@ -33,30 +49,30 @@ struct Tensor {
 
 struct Params {
   int B, S, heads, d;
-  int T, H, W, bT, bH, bW, nH, nW;
+  int W, bT, bH, bW, sb;
+  FastDiv by_S, by_HW, by_W, by_bT, by_bH, by_bW;
+  int HW, nH, nW;
   int n, turned;                             // tensors; the first `turned` of them are normed and rotated, the others only moved
   int pairs, axes, layout, norm, pos_batch;
+  int full;                                  // every channel of a head belongs to a pair
   int src_bm, dst_bm;                        // src / dst is block-major (strides unused)
   float mscale, eps;
   const int* pos;
   const double* freq;
   const int* axis;
   int* perm;
-  int wpr;                                   // warps per row
-  int tok;                                   // tokens per CTA and trip
+  int wpr, groups;                           // warps per row, rows that a CTA has under way
   float* part;                               // backward: [tensor][CTA][weights] partial sums of dw
   Tensor t[kMaxTensors];
 };
 
-__host__ __device__ constexpr size_t ang_bytes(int tok, int pairs) { return ((size_t)tok * pairs * sizeof(float2) + 15) / 16 * 16; }
-
 // Block-major position of raster token r (the inverse of Eq. 1).
 __device__ __forceinline__ int block_pos(const Params& p, int r) {
-  const int hw = p.H * p.W, t = r / hw, r2 = r - t * hw, h = r2 / p.W, w = r2 - h * p.W;
-  const int jt = t / p.bT, jh = h / p.bH, jw = w / p.bW;
+  const int t = p.by_HW.div(r), r2 = r - t * p.HW, h = p.by_W.div(r2), w = r2 - h * p.W;
+  const int jt = p.by_bT.div(t), jh = p.by_bH.div(h), jw = p.by_bW.div(w);
   const int block = (jt * p.nH + jh) * p.nW + jw;
   const int slot = ((t - jt * p.bT) * p.bH + (h - jh * p.bH)) * p.bW + (w - jw * p.bW);
-  return block * (p.bT * p.bH * p.bW) + slot;
+  return block * p.sb + slot;
 }
 
 template <typename T>
@@ -86,83 +102,137 @@ struct Vec {
   }
 };
 
-// cos and sin (times mscale) of the angles of `count` tokens from flat token index first on, into ang[token][pair].
-__device__ __forceinline__ void angles(const Params& p, long long first, int count, float2* ang) {
-  constexpr double kTurn = 6.283185307179586476925, kTurnLow = 2.4492935982947064e-16;      // 2 pi and what its double lacks
-  for (int i = threadIdx.x; i < count * p.pairs; i += kThreads) {
-    const int t = i / p.pairs, pair = i - t * p.pairs;
-    const long long g = first + t;
-    const int b = (int)(g / p.S), s = (int)(g - (long long)b * p.S);
-    const int at = __ldg(p.pos + ((long long)(p.pos_batch > 1 ? b : 0) * p.S + s) * p.axes + min(max(__ldg(p.axis + pair), 0), p.axes - 1));
-    const double a = (double)at * __ldg(p.freq + pair), turns = rint(a * (1.0 / kTurn));
-    const float r = (float)fma(-turns, kTurnLow, fma(-turns, kTurn, a));
+// The layouts, as far as the kernels tell them apart: half with whole vectors as partners, and with any number of pairs.
+enum Layout { kInterleaved, kHalf, kHalfAny };
+
+// cos and sin (times mscale) of a token's angles, by the threads of a group: the angle in turns, less whole ones.
+struct alignas(16) Angles { float cs[kMaxPairs], sn[kMaxPairs]; };
+__device__ __forceinline__ void angles(const Params& p, int g, int l, int tpr, Angles* ang) {
+  const int at0 = p.pos_batch > 1 ? g : g - p.by_S.div(g) * p.S;
+#pragma unroll 1
+  for (int pair = l; pair < p.pairs; pair += tpr) {
+    const int at = __ldg(p.pos + (long long)at0 * p.axes + min(max(__ldg(p.axis + pair), 0), p.axes - 1));
+    const double turns = (double)at * __ldg(p.freq + pair) * 0.15915494309189533577;      // 1 / (2 pi)
     float sn, cs;
-    sincosf(r, &sn, &cs);
-    ang[i] = make_float2(cs * p.mscale, sn * p.mscale);
+    sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+    ang->cs[pair] = cs * p.mscale;
+    ang->sn[pair] = sn * p.mscale;
   }
 }
 
-// What a thread's vectors, all of the same channels c0 .. c0 + E - 1 of a head, are turned by: out[e] = y[e] cs[e] + partner[e] sn[e].
-template <int E>
+// A thread's ring: kDepth rows of its vectors.
+constexpr int kDepth = 2;
+__device__ __forceinline__ void copy16(uint4* to, const void* from, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(there ? 16u : 0u) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// What a thread's vectors, all of the same channels c0 .. c0 + E - 1 of a head, are turned by.  sign: -1 turns back.
+template <int E, Layout L>
 struct Turn {
-  float cs[E], sn[E];
+  float cs[L == kInterleaved ? E / 2 : E], sn[L == kInterleaved ? E / 2 : E];
   uint32_t mine;                             // bit e: channel c0 + e belongs to a pair
-  __device__ __forceinline__ void load(const Params& p, const float2* ang, int c0, float sign) {
+  __device__ __forceinline__ void load(const Params& p, const Angles& a, int c0, float sign) {
     mine = 0;
+    if constexpr (L == kInterleaved) {
+      if constexpr (E == 8) {
+        const float4 c = *reinterpret_cast<const float4*>(a.cs + c0 / 2), s = *reinterpret_cast<const float4*>(a.sn + c0 / 2);
+        cs[0] = c.x; cs[1] = c.y; cs[2] = c.z; cs[3] = c.w;
+        sn[0] = s.x * sign; sn[1] = s.y * sign; sn[2] = s.z * sign; sn[3] = s.w * sign;
+      } else {
+        const float2 c = *reinterpret_cast<const float2*>(a.cs + c0 / 2), s = *reinterpret_cast<const float2*>(a.sn + c0 / 2);
+        cs[0] = c.x; cs[1] = c.y;
+        sn[0] = s.x * sign; sn[1] = s.y * sign;
+      }
+      const int n = 2 * p.pairs - c0;
+      mine = n <= 0 ? 0u : n >= E ? (1u << E) - 1u : (1u << n) - 1u;
+    } else if constexpr (L == kHalf) {
+      const bool second = c0 >= p.pairs;
+      const int i = second ? c0 - p.pairs : c0;
+      if (c0 < 2 * p.pairs) mine = (1u << E) - 1u;
+      const float f = second ? sign : -sign;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = c0 + e;
-      const bool second = p.layout == VMOBA_ROTARY_HALF ? c >= p.pairs : (c & 1) != 0;
-      const int pair = p.layout == VMOBA_ROTARY_HALF ? (second ? c - p.pairs : c) : c >> 1;
-      cs[e] = 1.f; sn[e] = 0.f;
-      if (c < 2 * p.pairs) {
-        const float2 a = ang[pair];
-        cs[e] = a.x;
-        sn[e] = second ? sign * a.y : -sign * a.y;
-        mine |= 1u << e;
+      for (int e = 0; e < E; e += 4) {
+        const int at = c0 < 2 * p.pairs ? i + e : 0;
+        const float4 c = *reinterpret_cast<const float4*>(a.cs + at), s = *reinterpret_cast<const float4*>(a.sn + at);
+        cs[e] = c.x; cs[e + 1] = c.y; cs[e + 2] = c.z; cs[e + 3] = c.w;
+        sn[e] = s.x * f; sn[e + 1] = s.y * f; sn[e + 2] = s.z * f; sn[e + 3] = s.w * f;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int c = c0 + e;
+        const bool second = c >= p.pairs, ok = c < 2 * p.pairs;
+        const int i = ok ? (second ? c - p.pairs : c) : 0;
+        cs[e] = a.cs[i];
+        sn[e] = a.sn[i] * (second ? sign : -sign);
+        if (ok) mine |= 1u << e;
+      }
+    }
+  }
+  // buf (kHalfAny): 32 * E floats of the warp.  Called by whole warps.
+  __device__ __forceinline__ void apply(const Params& p, float (&y)[E], int c0, float* buf) const {
+    if constexpr (L == kInterleaved) {
+      auto turned = [&](bool all) {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+          const float y0 = y[2 * i], y1 = y[2 * i + 1];
+          if (all || (mine >> (2 * i) & 1)) {
+            y[2 * i] = fmaf(y0, cs[i], -y1 * sn[i]);
+            y[2 * i + 1] = fmaf(y1, cs[i], y0 * sn[i]);
+          }
+        }
+      };
+      if (p.full) turned(true);
+      else turned(false);
+    } else {
+      float o[E];
+      const int lane = threadIdx.x & 31;
+      if constexpr (L == kHalf) {            // the partners of a vector are a vector of another lane of the same head
+        const int by = p.pairs / E, from = (c0 < p.pairs ? lane + by : lane - by) & 31;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = __shfl_sync(0xffffffffu, y[e], from);
+      } else {
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < E; ++e) buf[lane * E + e] = y[e];
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = (mine >> e & 1) ? buf[lane * E + e + (c0 + e < p.pairs ? p.pairs : -p.pairs)] : 0.f;
+      }
+      if (p.full) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = fmaf(y[e], cs[e], o[e] * sn[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (mine >> e & 1) y[e] = fmaf(y[e], cs[e], o[e] * sn[e]);
       }
     }
   }
 };
 
-// The partner of each of a thread's channels.  Interleaved: its neighbour.  Half: `pairs` channels away in the same head, whose
-// vectors are in neighbouring lanes; by shuffles where whole vectors are partners (WHOLE), else through shared memory.
-// Called by whole warps.
-template <int E, bool WHOLE>
-__device__ __forceinline__ void partners(const Params& p, const float (&y)[E], float (&o)[E], int c0, uint32_t mine, float* buf) {
-  if (p.layout == VMOBA_ROTARY_INTERLEAVED) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = y[e ^ 1];
-  } else if constexpr (WHOLE) {
-    const int lane = threadIdx.x & 31, by = p.pairs / E;
-    const int from = c0 < p.pairs ? lane + by : lane - by;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = __shfl_sync(0xffffffffu, y[e], from & 31);
-  } else {
-    const int lane = threadIdx.x & 31;
-    __syncwarp();
-#pragma unroll
-    for (int e = 0; e < E; ++e) buf[lane * E + e] = y[e];
-    __syncwarp();
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = (mine >> e & 1) ? buf[lane * E + e + (c0 + e < p.pairs ? p.pairs : -p.pairs)] : 0.f;
-  }
+// The warps of a group meet (barrier 1 + group).
+__device__ __forceinline__ void meet(int group, int wpr) {
+  if (wpr == 1) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * wpr) : "memory");
 }
 
-// Sum over the threads of a row (all of the CTA call this); slot: two floats per warp.
-__device__ __forceinline__ float2 row_sum(float2 v, int wpr, float2* slot) {
+// Sum over the threads of a row.  slot: a pair of floats per warp of the group; the next call takes another one (a call that takes
+// this one again is two barriers away).
+__device__ __forceinline__ float2 row_sum(float2 v, int group, int wpr, float2* slot) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
     v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
   }
   if (wpr == 1) return v;
-  const int warp = threadIdx.x >> 5;
-  __syncthreads();                           // (the row before has been read)
-  if ((threadIdx.x & 31) == 0) slot[warp] = v;
-  __syncthreads();
+  if ((threadIdx.x & 31) == 0) slot[(threadIdx.x >> 5) - group * wpr] = v;
+  meet(group, wpr);
   float2 a = make_float2(0.f, 0.f);
-  for (int w = warp / wpr * wpr; w < (warp / wpr + 1) * wpr; ++w) { a.x += slot[w].x; a.y += slot[w].y; }
+  for (int w = 0; w < wpr; ++w) { a.x += slot[w].x; a.y += slot[w].y; }
   return a;
 }
 __device__ __forceinline__ float2 head_sum(float2 v, int lanes) {
@@ -182,267 +252,356 @@ __device__ __forceinline__ void weights(const float* w, float (&x)[E]) {
   }
 }
 
-// Where a row of a tensor begins and how far its heads lie apart, in elements.
-struct RowAt { long long base, head; };
-__device__ __forceinline__ RowAt row_at(const Params& p, bool bm, const long long (&s)[3], int b, int tok) {
-  if (bm) return {((long long)b * p.heads * p.S + block_pos(p, tok)) * p.d, (long long)p.S * p.d};
-  return {b * s[0] + tok * s[1], s[2]};
+// sum += a . b
+template <int E>
+__device__ __forceinline__ void dot(const float (&a)[E], const float (&b)[E], float& s0, float& s1) {
+#pragma unroll
+  for (int e = 0; e < E; e += 2) fma2(s0, s1, a[e], a[e + 1], b[e], b[e + 1], s0, s1);
+}
+template <int E>
+__device__ __forceinline__ void times(float (&a)[E], const float (&b)[E]) {
+#pragma unroll
+  for (int e = 0; e < E; e += 2) mul2(a[e], a[e + 1], a[e], a[e + 1], b[e], b[e + 1]);
+}
+template <int E>
+__device__ __forceinline__ void times(float (&a)[E], float b) {
+#pragma unroll
+  for (int e = 0; e < E; e += 2) mul2(a[e], a[e + 1], a[e], a[e + 1], b, b);
 }
 
 // ------------------------------------------------------------------------------ forward
-template <typename T, bool WHOLE>
-__global__ void __launch_bounds__(kThreads)
+// ONCE: the row fits the group's threads; else it is walked in trips, from global memory.
+template <typename T, Layout L, int NV, bool ONCE>
+__global__ void __launch_bounds__(32 * kMaxWarps, 3)
 rotary_fwd_kernel(const __grid_constant__ Params p) {
   if (!grid_begin()) return;
   constexpr int E = Vec<T>::E;
-  extern __shared__ __align__(16) uint8_t smem[];
-  float2* ang = reinterpret_cast<float2*>(smem);                                  // [tok][pairs]
-  __shared__ float2 slot[kWarps];
-  __shared__ float exchange[WHOLE ? 1 : kWarps * 32 * E];
-  const int warp = threadIdx.x >> 5;
-  float* buf = WHOLE ? exchange : exchange + warp * 32 * E;
-  const int V = p.d / E, nvec = p.heads * V, tpr = 32 * p.wpr, groups = kWarps / p.wpr;
-  const int group = warp / p.wpr, l = threadIdx.x - group * tpr, c0 = (l % V) * E;
-  const int vshift = 31 - __clz(V);
-  const long long tokens = (long long)p.B * p.S, first = (long long)blockIdx.x * p.tok;
-  const int count = (int)min((long long)p.tok, tokens - first);
-  angles(p, first, count, ang);
-  __syncthreads();
-  const int rows = count * p.n, trips = (rows + groups - 1) / groups;
-  for (int trip = 0; trip < trips; ++trip) {
-    const int row = trip * groups + group;
-    const bool ok = row < rows;
-    // tensors from the last to the first, a token's rows behind one another: what the caller reads next comes last
-    const int tk = ok ? row / p.n : 0, k = ok ? p.n - 1 - (row - tk * p.n) : 0;
-    const long long g = first + tk;
-    const int b = (int)(g / p.S), tok = (int)(g - (long long)b * p.S);
+  extern __shared__ __align__(16) uint4 ring[];                      // [kDepth][NV][threads]
+  __shared__ Angles ang[kMaxWarps][2];
+  __shared__ float2 slot[2][kMaxWarps];
+  __shared__ float exchange[L == kHalfAny ? kMaxWarps * 32 * E : 1];
+  const int warp = threadIdx.x >> 5, group = warp / p.wpr, tpr = 32 * p.wpr, l = threadIdx.x - group * tpr, threads = blockDim.x;
+  float* buf = L == kHalfAny ? exchange + warp * 32 * E : exchange;
+  uint4* mine = ring + threadIdx.x;
+  const int V = p.d / E, nvec = p.heads * V, c0 = (l % V) * E, vshift = 31 - __clz(V), head0 = l >> vshift, heads_per = tpr >> vshift;
+  const int per = NV * tpr;                  // vectors of a trip through a row
+  const int tokens = p.B * p.S, step = gridDim.x * p.groups;
+  // The row of (token, tensor): this thread's first vector.
+  auto src_row = [&](int g, int k) {
     const Tensor& t = p.t[k];
-    const RowAt from = row_at(p, false, t.ss, b, tok), to = row_at(p, p.dst_bm, t.ds, b, tok);
-    const T* src = reinterpret_cast<const T*>(t.src) + from.base + c0;
-    T* dst = reinterpret_cast<T*>(t.dst) + to.base + c0;
-    const bool turned = k < p.turned;
-    if (p.perm && ok && k == 0 && b == 0 && l == 0) p.perm[block_pos(p, tok)] = tok;
-    Turn<E> turn;
-    turn.load(p, ang + tk * p.pairs, turned ? c0 : p.d, 1.f);
-    uint4 raw[NV];
-    auto load = [&](int v0) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int v = v0 + l + i * tpr;
-        raw[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (ok && v < nvec) raw[i] = __ldcs(reinterpret_cast<const uint4*>(src + (long long)(v >> vshift) * from.head));
-      }
-    };
-    const int per = NV * tpr;                // vectors of a trip through the row
-    float r_row = 1.f;
-    if (p.norm == VMOBA_ROTARY_NORM_ROW) {
-      float2 sum = make_float2(0.f, 0.f);
-      for (int v0 = 0; v0 < nvec; v0 += per) {
-        load(v0);
+    const int b = p.by_S.div(g);
+    return reinterpret_cast<const T*>(t.src) + b * t.ss[0] + (long long)(g - b * p.S) * t.ss[1] + head0 * t.ss[2] + c0;
+  };
+  int g = blockIdx.x * p.groups + group;
+  if (g >= tokens) return;                   // (whole groups)
+  int ga = g, ka = p.n - 1;                  // the next row to ask for
+  uint4* in = mine;                          // and its place
+  auto ask = [&]() {
+    if (ONCE) {
+      if (ga < tokens) {
+        const T* at = src_row(ga, ka);
+        const long long apart = heads_per * p.t[ka].ss[2];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          float x[E];
-          Vec<T>::unpack(raw[i], x);
-#pragma unroll
-          for (int e = 0; e < E; ++e) sum.x = fmaf(x[e], x[e], sum.x);
+          const bool there = l + i * tpr < nvec;
+          copy16(in + i * threads, there ? at : reinterpret_cast<const T*>(p.t[ka].src), there);
+          at += apart;
         }
+        if (--ka < 0) { ka = p.n - 1; ga += step; }
       }
-      r_row = rsqrtf(row_sum(sum, p.wpr, slot).x / (float)(p.heads * p.d) + p.eps);
+      copies_commit();
+      in = in == mine ? mine + NV * threads : mine;      // (kDepth = 2)
     }
-    for (int v0 = 0; v0 < nvec; v0 += per) {
-      if (p.norm != VMOBA_ROTARY_NORM_ROW || nvec > per) load(v0);
+  };
+  ask();
+  ask();
+  angles(p, g, l, tpr, &ang[group][0]);
+  int turn_buf = 0, sum_buf = 0;
+  const uint4* row = mine;
+  for (; g < tokens; g += step, turn_buf ^= 1) {
+    meet(group, p.wpr);                      // (this token's angles)
+    Turn<E, L> turn;
+    turn.load(p, ang[group][turn_buf], c0, 1.f);
+    const int b = p.by_S.div(g), tok = g - b * p.S, bm = p.dst_bm || p.perm ? block_pos(p, tok) : 0;
+    if (p.perm && b == 0 && l == 0) p.perm[bm] = tok;
+    // tensors from the last to the first: what the caller reads next comes last
+#pragma unroll 1
+    for (int k = p.n - 1; k >= 0; --k) {
+      if (ONCE) copies_wait<kDepth - 1>();
+      const Tensor& t = p.t[k];
+      auto vec = [&](int v0, int i) {
+        if (ONCE) return row[i * threads];
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (v0 + l + i * tpr < nvec) x = __ldcg(reinterpret_cast<const uint4*>(src_row(g, k) + ((v0 >> vshift) + i * heads_per) * t.ss[2]));
+        return x;
+      };
+      const bool turned = k < p.turned;
+      const int norm = turned ? p.norm : VMOBA_ROTARY_NORM_NONE;
+      float r_row = 1.f;
+      if (norm == VMOBA_ROTARY_NORM_ROW) {
+        float s0 = 0.f, s1 = 0.f;
+        for (int v0 = 0; v0 < nvec; v0 += per) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int v = v0 + l + i * tpr;
-        if (v0 + (warp % p.wpr) * 32 + i * tpr >= nvec) break;      // (whole warps)
-        const bool there = ok && v < nvec;
-        float y[E];
-        Vec<T>::unpack(raw[i], y);
-        if (turned) {
-          if (p.norm != VMOBA_ROTARY_NORM_NONE) {
-            float r = r_row, w[E];
-            if (p.norm == VMOBA_ROTARY_NORM_HEAD) {
-              float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-              for (int e = 0; e < E; ++e) sum.x = fmaf(y[e], y[e], sum.x);
-              r = rsqrtf(head_sum(sum, V).x / (float)p.d + p.eps);
-              weights<E>(t.w ? t.w + c0 : nullptr, w);
-            } else {
-              weights<E>(t.w ? t.w + min(v, nvec - 1) * E : nullptr, w);
-            }
-#pragma unroll
-            for (int e = 0; e < E; ++e) y[e] = y[e] * r * w[e];
+          for (int i = 0; i < NV; ++i) {
+            float x[E];
+            Vec<T>::unpack(vec(v0, i), x);
+            dot<E>(x, x, s0, s1);
           }
-          if (p.pairs > 0) {
-            float o[E];
-            partners<E, WHOLE>(p, y, o, c0, turn.mine, buf);
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-              if (turn.mine >> e & 1) y[e] = fmaf(y[e], turn.cs[e], o[e] * turn.sn[e]);
-          }
+          if (ONCE) break;
         }
-        if (there) *reinterpret_cast<uint4*>(dst + (long long)(v >> vshift) * to.head) = Vec<T>::pack(y);
+        r_row = rsqrtf(row_sum(make_float2(s0 + s1, 0.f), group, p.wpr, slot[sum_buf] + group * p.wpr).x / (float)(p.heads * p.d) + p.eps);
+        sum_buf ^= 1;
       }
+      if (k == 0 && g + step < tokens) angles(p, g + step, l, tpr, &ang[group][turn_buf ^ 1]);
+      const long long to_head = p.dst_bm ? (long long)p.S * p.d : t.ds[2], to_next = heads_per * to_head;
+      T* dst = reinterpret_cast<T*>(t.dst) + (p.dst_bm ? ((long long)b * p.heads * p.S + bm) * p.d : b * t.ds[0] + tok * t.ds[1]) +
+               head0 * to_head + c0;
+      // the vectors of a trip, each through f
+      auto each = [&](auto f) {
+        for (int v0 = 0; v0 < nvec; v0 += per) {
+          const float* w = t.w ? t.w + (norm == VMOBA_ROTARY_NORM_ROW ? (v0 + l) * E : c0) : nullptr;
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            const bool there = v0 + l + i * tpr < nvec;
+            if (__any_sync(0xffffffffu, there)) {
+              float y[E];
+              Vec<T>::unpack(vec(v0, i), y);
+              f(y, there ? w : nullptr);
+              if (there) *reinterpret_cast<uint4*>(dst) = Vec<T>::pack(y);
+            }
+            dst += to_next;
+            if (w && norm == VMOBA_ROTARY_NORM_ROW) w += tpr * E;
+          }
+          if (ONCE) break;
+        }
+      };
+      if (!turned) {
+        each([&](float (&)[E], const float*) {});
+      } else if (norm == VMOBA_ROTARY_NORM_ROW) {
+        each([&](float (&y)[E], const float* w) {
+          float f[E];
+          weights<E>(w, f);
+          times<E>(y, r_row);
+          times<E>(y, f);
+          turn.apply(p, y, c0, buf);
+        });
+      } else if (norm == VMOBA_ROTARY_NORM_HEAD) {
+        each([&](float (&y)[E], const float* w) {
+          float f[E], s0 = 0.f, s1 = 0.f;
+          dot<E>(y, y, s0, s1);
+          weights<E>(w, f);
+          times<E>(y, rsqrtf(head_sum(make_float2(s0 + s1, 0.f), V).x / (float)p.d + p.eps));
+          times<E>(y, f);
+          turn.apply(p, y, c0, buf);
+        });
+      } else {
+        each([&](float (&y)[E], const float*) { turn.apply(p, y, c0, buf); });
+      }
+      row = row == mine ? mine + NV * threads : mine;
+      ask();                                 // (into the place of the row that has just been read)
     }
   }
 }
 
 // ------------------------------------------------------------------------------ backward
-// blockIdx.y: tensor.  A CTA walks its share of the tokens and keeps its part of dw: norm over the row, in shared memory, a copy for
-// each group of warps that takes a row (a thread owns its channels there); norm per head, in registers.  The parts are added up
-// in a fixed order by weight_sum_kernel: the results repeat bit for bit.
-template <typename T, bool WHOLE>
-__global__ void __launch_bounds__(kThreads)
+// blockIdx.y: tensor.  A thread has the same channels in every row that its group takes, and keeps their part of dw in registers (rows
+// longer than that: in shared memory).  The parts of a CTA's groups, and of the CTAs (weight_sum_kernel), are added up in a
+// fixed order: the results repeat bit for bit.
+template <typename T, Layout L, int NV, bool ONCE>
+__global__ void __launch_bounds__(32 * kMaxWarps, 2)
 rotary_bwd_kernel(const __grid_constant__ Params p) {
   if (!grid_begin()) return;
   constexpr int E = Vec<T>::E;
-  extern __shared__ __align__(16) uint8_t smem[];
-  float2* ang = reinterpret_cast<float2*>(smem);                                  // [tok][pairs]
-  float* acc_row = reinterpret_cast<float*>(smem + ang_bytes(p.tok, p.pairs));    // [group][heads * d]
-  __shared__ float2 slot[kWarps];
-  __shared__ float exchange[kWarps * 32 * E];
-  const int warp = threadIdx.x >> 5;
+  extern __shared__ __align__(16) uint4 ring[];                      // [kDepth][dy, x][NV][threads]; then, or instead, [group][heads * d]
+  float* acc_row = reinterpret_cast<float*>(ring);
+  __shared__ Angles ang[kMaxWarps][2];
+  __shared__ float2 slot[2][kMaxWarps];
+  __shared__ float exchange[kMaxWarps * 32 * E];
+  const int warp = threadIdx.x >> 5, group = warp / p.wpr, tpr = 32 * p.wpr, l = threadIdx.x - group * tpr, threads = blockDim.x;
   float* buf = exchange + warp * 32 * E;
-  const int V = p.d / E, nvec = p.heads * V, tpr = 32 * p.wpr, groups = kWarps / p.wpr;
-  const int group = warp / p.wpr, l = threadIdx.x - group * tpr, c0 = (l % V) * E;
-  const int vshift = 31 - __clz(V);
+  uint4* mine = ring + threadIdx.x;
+  const int V = p.d / E, nvec = p.heads * V, c0 = (l % V) * E, vshift = 31 - __clz(V), head0 = l >> vshift, heads_per = tpr >> vshift;
+  const int per = NV * tpr;
   const Tensor& t = p.t[blockIdx.y];
-  const long long tokens = (long long)p.B * p.S;
+  const int tokens = p.B * p.S, step = gridDim.x * p.groups;
   const bool by_row = p.norm == VMOBA_ROTARY_NORM_ROW, by_head = p.norm == VMOBA_ROTARY_NORM_HEAD, normed = by_row || by_head;
   const int row_ch = p.heads * p.d;
-  float acc[E];
+  const float inv_n = 1.0f / (float)(by_row ? row_ch : p.d);
+  float acc[NV][E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = 0.f;
-  if (by_row)
-    for (int i = threadIdx.x; i < groups * row_ch; i += kThreads) acc_row[i] = 0.f;
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[i][e] = 0.f;
   float* mine_acc = acc_row + (long long)group * row_ch;
-  for (long long first = (long long)blockIdx.x * p.tok; first < tokens; first += (long long)gridDim.x * p.tok) {
-    const int count = (int)min((long long)p.tok, tokens - first);
-    __syncthreads();
-    angles(p, first, count, ang);
-    __syncthreads();
-    const int trips = (count + groups - 1) / groups;
-    for (int trip = 0; trip < trips; ++trip) {
-      const int tk = trip * groups + group;
-      const bool ok = tk < count;
-      const long long g = first + (ok ? tk : 0);
-      const int b = (int)(g / p.S), tok = (int)(g - (long long)b * p.S);
-      const RowAt from = row_at(p, p.src_bm, t.ss, b, tok), at_x = row_at(p, false, t.xs, b, tok), to = row_at(p, false, t.ds, b, tok);
-      const T* src = reinterpret_cast<const T*>(t.src) + from.base + c0;
-      const T* xr = normed ? reinterpret_cast<const T*>(t.x) + at_x.base + c0 : nullptr;
-      T* dst = reinterpret_cast<T*>(t.dst) + to.base + c0;
-      Turn<E> turn;
-      turn.load(p, ang + (ok ? tk : 0) * p.pairs, c0, -1.f);
-      uint4 raw[NV], rawx[NV];
-      auto load = [&](int v0) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const int v = v0 + l + i * tpr;
-          raw[i] = rawx[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (ok && v < nvec) {
-            raw[i] = __ldcs(reinterpret_cast<const uint4*>(src + (long long)(v >> vshift) * from.head));
-            if (normed) rawx[i] = __ldcs(reinterpret_cast<const uint4*>(xr + (long long)(v >> vshift) * at_x.head));
-          }
-        }
-      };
-      auto turned_back = [&](const uint4& u, float (&y)[E]) {
-        Vec<T>::unpack(u, y);
-        if (p.pairs > 0) {
-          float o[E];
-          partners<E, WHOLE>(p, y, o, c0, turn.mine, buf);
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (turn.mine >> e & 1) y[e] = fmaf(y[e], turn.cs[e], o[e] * turn.sn[e]);
-        }
-      };
-      const int per = NV * tpr;
-      const float2 zero = make_float2(0.f, 0.f);
-      float2 sums = zero;                    // sum of squares of x, of x times its weighted gradient
-      if (by_row) {
-        for (int v0 = 0; v0 < nvec; v0 += per) {
-          load(v0);
+  if (by_row && !ONCE)
+    for (int i = l; i < row_ch; i += tpr) mine_acc[i] = 0.f;
+  const long long d_head = p.src_bm ? (long long)p.S * p.d : t.ss[2];
+  auto d_row = [&](int g) {
+    const int b = p.by_S.div(g), tok = g - b * p.S;
+    return reinterpret_cast<const T*>(t.src) + (p.src_bm ? ((long long)b * p.heads * p.S + block_pos(p, tok)) * p.d : b * t.ss[0] + tok * t.ss[1]) +
+           head0 * d_head + c0;
+  };
+  auto x_row = [&](int g) {
+    const int b = p.by_S.div(g), tok = g - b * p.S;
+    return reinterpret_cast<const T*>(t.x) + b * t.xs[0] + tok * t.xs[1] + head0 * t.xs[2] + c0;
+  };
+  int g = blockIdx.x * p.groups + group;
+  if (g < tokens) {                          // (whole groups; all threads meet again at the end)
+    int ga = g;
+    uint4* in = mine;
+    auto ask = [&]() {
+      if (ONCE) {
+        if (ga < tokens) {
+          const T *d = d_row(ga), *x = normed ? x_row(ga) : nullptr;
 #pragma unroll
           for (int i = 0; i < NV; ++i) {
-            if (v0 + (warp % p.wpr) * 32 + i * tpr >= nvec) break;
-            const int v = v0 + l + i * tpr;
-            float y[E], x[E], w[E];
-            turned_back(raw[i], y);
-            Vec<T>::unpack(rawx[i], x);
-            weights<E>(t.w ? t.w + min(v, nvec - 1) * E : nullptr, w);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-              sums.x = fmaf(x[e], x[e], sums.x);
-              sums.y = fmaf(x[e], y[e] * w[e], sums.y);
-            }
+            const bool there = l + i * tpr < nvec;
+            copy16(in + i * threads, there ? d : reinterpret_cast<const T*>(t.src), there);
+            if (normed) copy16(in + (NV + i) * threads, there ? x : reinterpret_cast<const T*>(t.x), there);
+            d += heads_per * d_head;
+            x += heads_per * t.xs[2];
           }
+          ga += step;
         }
-        sums = row_sum(sums, p.wpr, slot);
+        copies_commit();
+        in = in == mine ? mine + 2 * NV * threads : mine;      // (kDepth = 2)
       }
+    };
+    ask();
+    ask();
+    angles(p, g, l, tpr, &ang[group][0]);
+    int turn_buf = 0;
+    const uint4* row = mine;
+    for (; g < tokens; g += step, turn_buf ^= 1) {
+      meet(group, p.wpr);                    // (this token's angles)
+      Turn<E, L> turn;
+      turn.load(p, ang[group][turn_buf], c0, -1.f);
+      if (ONCE) copies_wait<kDepth - 1>();
+      auto vec_d = [&](int v0, int i) {
+        if (ONCE) return row[i * threads];
+        uint4 u = make_uint4(0u, 0u, 0u, 0u);
+        if (v0 + l + i * tpr < nvec) u = __ldcg(reinterpret_cast<const uint4*>(d_row(g) + ((v0 >> vshift) + i * heads_per) * d_head));
+        return u;
+      };
+      auto vec_x = [&](int v0, int i) {
+        if (ONCE) return row[(NV + i) * threads];
+        uint4 u = make_uint4(0u, 0u, 0u, 0u);
+        if (v0 + l + i * tpr < nvec) u = __ldcg(reinterpret_cast<const uint4*>(x_row(g) + ((v0 >> vshift) + i * heads_per) * t.xs[2]));
+        return u;
+      };
+      float r = 1.f, back = 0.f;             // 1 / rms; r^2 times the mean of x times its weighted gradient
+      auto scales = [&](const float2& s) {
+        r = rsqrtf(fmaf(s.x, inv_n, p.eps));
+        back = r * r * (s.y * inv_n);
+      };
+      if (by_row) {
+        float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
+        for (int v0 = 0; v0 < nvec; v0 += per) {
+          const float* w = t.w ? t.w + (v0 + l) * E : nullptr;
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            const bool there = v0 + l + i * tpr < nvec;
+            if (__any_sync(0xffffffffu, there)) {
+              float y[E], x[E], f[E];
+              Vec<T>::unpack(vec_d(v0, i), y);
+              turn.apply(p, y, c0, buf);
+              Vec<T>::unpack(vec_x(v0, i), x);
+              weights<E>(there ? w : nullptr, f);
+              dot<E>(x, x, s0, s1);
+              times<E>(y, f);
+              dot<E>(x, y, u0, u1);
+            }
+            if (w) w += tpr * E;
+          }
+          if (ONCE) break;
+        }
+        scales(row_sum(make_float2(s0 + s1, u0 + u1), group, p.wpr, slot[turn_buf] + group * p.wpr));
+      }
+      if (g + step < tokens) angles(p, g + step, l, tpr, &ang[group][turn_buf ^ 1]);
+      const int b = p.by_S.div(g), tok = g - b * p.S;
+      T* dst = reinterpret_cast<T*>(t.dst) + b * t.ds[0] + tok * t.ds[1] + head0 * t.ds[2] + c0;
       for (int v0 = 0; v0 < nvec; v0 += per) {
-        if (!by_row || nvec > per) load(v0);
+        const float* w = t.w ? t.w + (by_row ? (v0 + l) * E : c0) : nullptr;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          if (v0 + (warp % p.wpr) * 32 + i * tpr >= nvec) break;
-          const int v = v0 + l + i * tpr;
-          const bool there = ok && v < nvec;
-          float y[E];
-          turned_back(raw[i], y);
-          if (normed) {
-            float x[E], w[E];
-            Vec<T>::unpack(rawx[i], x);
-            weights<E>(!t.w ? nullptr : by_row ? t.w + min(v, nvec - 1) * E : t.w + c0, w);
-            float2 s = sums;
-            if (by_head) {
-              s = zero;
+          const bool there = v0 + l + i * tpr < nvec;
+          if (__any_sync(0xffffffffu, there)) {
+            float y[E];
+            Vec<T>::unpack(vec_d(v0, i), y);
+            turn.apply(p, y, c0, buf);
+            if (normed) {
+              float x[E], f[E];
+              Vec<T>::unpack(vec_x(v0, i), x);
+              weights<E>(there ? w : nullptr, f);
+              float yw[E];
 #pragma unroll
-              for (int e = 0; e < E; ++e) {
-                s.x = fmaf(x[e], x[e], s.x);
-                s.y = fmaf(x[e], y[e] * w[e], s.y);
+              for (int e = 0; e < E; e += 2) mul2(yw[e], yw[e + 1], y[e], y[e + 1], f[e], f[e + 1]);
+              if (by_head) {
+                float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
+                dot<E>(x, x, s0, s1);
+                dot<E>(x, yw, u0, u1);
+                scales(head_sum(make_float2(s0 + s1, u0 + u1), V));
               }
-              s = head_sum(s, V);
-            }
-            const float n = (float)(by_row ? row_ch : p.d), r = rsqrtf(s.x / n + p.eps), back = r * r * (s.y / n);
-            float dw[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-              dw[e] = y[e] * (x[e] * r);
-              y[e] = r * fmaf(-x[e], back, y[e] * w[e]);
-            }
-            if (by_head) {
-#pragma unroll
-              for (int e = 0; e < E; ++e) acc[e] += there ? dw[e] : 0.f;
-            } else if (there) {
-#pragma unroll
-              for (int e = 0; e < E; e += 4) {
-                float4* a = reinterpret_cast<float4*>(mine_acc + v * E + e);
-                float4 z = *a;
-                z.x += dw[e]; z.y += dw[e + 1]; z.z += dw[e + 2]; z.w += dw[e + 3];
-                *a = z;
+              for (int e = 0; e < E; e += 2) {
+                mul2(y[e], y[e + 1], y[e], y[e + 1], r, r);
+                if (by_row && !ONCE) {
+                  if (there) {
+                    float* a = mine_acc + (v0 + l + i * tpr) * E + e;
+                    a[0] = fmaf(y[e], x[e], a[0]);
+                    a[1] = fmaf(y[e + 1], x[e + 1], a[1]);
+                  }
+                } else {
+                  fma2(acc[i][e], acc[i][e + 1], y[e], y[e + 1], x[e], x[e + 1], acc[i][e], acc[i][e + 1]);      // (zeros beyond the row)
+                }
+                fma2(y[e], y[e + 1], x[e], x[e + 1], -back, -back, yw[e], yw[e + 1]);
+                mul2(y[e], y[e + 1], y[e], y[e + 1], r, r);
               }
             }
+            if (there) *reinterpret_cast<uint4*>(dst) = Vec<T>::pack(y);
           }
-          if (there) *reinterpret_cast<uint4*>(dst + (long long)(v >> vshift) * to.head) = Vec<T>::pack(y);
+          dst += heads_per * t.ds[2];
+          if (w && by_row) w += tpr * E;
         }
+        if (ONCE) break;
       }
+      row = row == mine ? mine + 2 * NV * threads : mine;
+      ask();
     }
   }
   if (!normed) return;
-  __syncthreads();
   const int n_w = by_row ? row_ch : p.d;
   float* out = p.part + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * n_w;
   if (by_row) {
-    for (int i = threadIdx.x; i < row_ch; i += kThreads) {
+    copies_wait<0>();
+    __syncthreads();                         // (the ring is free)
+    if (ONCE) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < E; e += 4)
+          if (l + i * tpr < nvec)
+            *reinterpret_cast<float4*>(mine_acc + (l + i * tpr) * E + e) = make_float4(acc[i][e], acc[i][e + 1], acc[i][e + 2], acc[i][e + 3]);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < row_ch; i += threads) {
       float a = 0.f;
-      for (int q = 0; q < groups; ++q) a += acc_row[(long long)q * row_ch + i];
+      for (int q = 0; q < p.groups; ++q) a += acc_row[(long long)q * row_ch + i];
       out[i] = a;
     }
   } else {
+    __syncthreads();                         // (the exchange buffers are free)
 #pragma unroll
-    for (int e = 0; e < E; ++e) exchange[threadIdx.x * E + e] = acc[e];
-    __syncthreads();
-    for (int c = threadIdx.x; c < p.d; c += kThreads) {      // threads c / E, c / E + V, ... hold channel c
+    for (int e = 0; e < E; ++e) {
       float a = 0.f;
-      for (int q = c / E; q < kThreads; q += V) a += exchange[q * E + c % E];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) a += acc[i][e];
+      exchange[threadIdx.x * E + e] = a;
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.d; c += threads) {               // threads c / E, c / E + V, ... hold channel c
+      float a = 0.f;
+      for (int q = c / E; q < threads; q += V) a += exchange[q * E + c % E];
       out[c] = a;
     }
   }
@@ -472,21 +631,24 @@ weight_sum_kernel(const float* __restrict__ part, int n_parts, int n_w, WeightOu
 }
 
 // ------------------------------------------------------------------------------ host
-static int bwd_ctas(const Dims& D, int tok) {
-  return (int)std::min<long long>(((long long)D.B * D.S + tok - 1) / tok, 2ll * sm_count());
-}
-static int tokens_per_cta(const Dims& D) {
-  // as many as share their angles without leaving SMs short of work
-  const long long per = (long long)D.B * D.S / ((long long)sm_count() * 8);
-  int tok = 1;
-  while (tok < kMaxTok && tok * 2 <= per) tok *= 2;
-  return tok;
-}
-static int warps_per_row(const Dims& D) {
+// How a row is laid over warps: up to six vectors per thread in the fewest idle lanes, of equals the fewest warps; CTAs of about eight
+// warps.  false: the row is longer than that (eight warps, trips of four vectors per thread).
+constexpr int kMaxNv = 6;
+static bool lay_out(const Dims& D, Params* p, int* nv) {
   const int nvec = D.heads * D.d * D.es / 16;
-  int w = 1;
-  while (w < kWarps && nvec > NV * 32 * w) w *= 2;
-  return w;
+  int best = INT32_MAX;
+  *nv = 4; p->wpr = kMaxWarps; p->groups = 1;
+  for (int w = 1; w <= kMaxWarps; ++w)
+    for (int v = 1; v <= kMaxNv; ++v) {
+      const int idle = w * 32 * v - nvec;
+      if (idle >= 0 && idle < best) { best = idle; *nv = v; p->wpr = w; p->groups = kMaxWarps / w; }
+    }
+  return best < INT32_MAX;
+}
+// CTAs of the backward (per tensor); at most kMaxParts parts of dw.
+constexpr int kMaxParts = 512;
+static int bwd_ctas(const Dims& D, const Params& p) {
+  return (int)std::min<long long>(((long long)D.B * D.S + p.groups - 1) / p.groups, std::min(kMaxParts, 2 * sm_count()));
 }
 
 static int check(const vmoba_shape* shape, const vmoba_rotary_spec* spec, Dims* D) {
@@ -513,36 +675,40 @@ static bool strides_ok(const Dims& D, const int64_t s[3], bool written) {
 
 static void fill(const Dims& D, const vmoba_rotary_spec* spec, Params* p) {
   p->B = D.B; p->S = D.S; p->heads = D.heads; p->d = D.d;
-  p->T = D.T; p->H = D.H; p->W = D.W; p->bT = D.bT; p->bH = D.bH; p->bW = D.bW; p->nH = D.nH; p->nW = D.nW;
+  p->W = D.W; p->bT = D.bT; p->bH = D.bH; p->bW = D.bW; p->sb = D.sb; p->HW = D.H * D.W; p->nH = D.nH; p->nW = D.nW;
+  p->by_S = FastDiv(D.S); p->by_HW = FastDiv(p->HW); p->by_W = FastDiv(D.W);
+  p->by_bT = FastDiv(D.bT); p->by_bH = FastDiv(D.bH); p->by_bW = FastDiv(D.bW);
   p->pairs = spec->pairs; p->axes = spec->axes; p->layout = spec->layout; p->norm = spec->norm; p->pos_batch = spec->pos_batch;
+  p->full = 2 * spec->pairs == D.d;
   p->mscale = spec->mscale; p->eps = spec->eps;
-  p->wpr = warps_per_row(D);
-  p->tok = tokens_per_cta(D);
 }
 
-static size_t bwd_smem(const Dims& D, const Params& p) {
-  return ang_bytes(p.tok, p.pairs) +
-         (p.norm == VMOBA_ROTARY_NORM_ROW ? (size_t)(kWarps / p.wpr) * D.heads * D.d * sizeof(float) : 0);
-}
-constexpr int kFwdSmem = kMaxTok * 64 * (int)sizeof(float2);
-
-template <typename T>
-static int launch_fwd(const Dims& D, const Params& p, cudaStream_t st) {
-  const bool whole = p.layout == VMOBA_ROTARY_INTERLEAVED || p.pairs % Vec<T>::E == 0;
-  const long long grid = ((long long)D.B * D.S + p.tok - 1) / p.tok;
-  auto kernel = whole ? rotary_fwd_kernel<T, true> : rotary_fwd_kernel<T, false>;
-  launch_kernel(early_rows(D), kernel, (unsigned)grid, kThreads, kFwdSmem, st, p);
+template <typename T, Layout L, int NV, bool ONCE>
+static int go_fwd(const Dims& D, const Params& p, cudaStream_t st) {
+  auto kernel = rotary_fwd_kernel<T, L, NV, ONCE>;
+  const int threads = 32 * p.wpr * p.groups;
+  const long long ctas = ((long long)D.B * D.S + p.groups - 1) / p.groups;
+  VMOBA_CUDA_OK(allow_smem(kernel, kDepth * NV * 32 * kMaxWarps * 16));
+  launch_kernel(early_rows(D), kernel, (unsigned)std::min<long long>(ctas, 3ll * sm_count()), threads,
+                ONCE ? (size_t)kDepth * NV * threads * 16 : 0, st, p);
   VMOBA_LAUNCH_OK(1);
   return VMOBA_OK;
 }
 
-template <typename T>
-static int launch_bwd(const Dims& D, const Params& p, const WeightOut& w, cudaStream_t st) {
-  const bool whole = p.layout == VMOBA_ROTARY_INTERLEAVED || p.pairs % Vec<T>::E == 0;
-  const int ctas = bwd_ctas(D, p.tok);
-  auto kernel = whole ? rotary_bwd_kernel<T, true> : rotary_bwd_kernel<T, false>;
-  VMOBA_CUDA_OK(allow_smem(kernel, 200 * 1024));
-  launch_kernel(early_rows(D), kernel, dim3(ctas, p.n), kThreads, bwd_smem(D, p), st, p);
+static size_t bwd_smem(const Dims& D, const Params& p, int nv, bool once) {
+  const size_t ring = once ? (size_t)2 * kDepth * nv * 32 * p.wpr * p.groups * 16 : 0;
+  return std::max(ring, p.norm == VMOBA_ROTARY_NORM_ROW ? (size_t)p.groups * D.heads * D.d * sizeof(float) : 0);
+}
+constexpr int kBwdSmemMost = 200 * 1024;
+
+template <typename T, Layout L, int NV, bool ONCE>
+static int go_bwd(const Dims& D, const Params& p, const WeightOut& w, cudaStream_t st) {
+  auto kernel = rotary_bwd_kernel<T, L, NV, ONCE>;
+  const int ctas = bwd_ctas(D, p);
+  const size_t smem = bwd_smem(D, p, NV, ONCE);
+  if (smem > (size_t)kBwdSmemMost) return VMOBA_ERR_NOT_IMPLEMENTED;
+  VMOBA_CUDA_OK(allow_smem(kernel, kBwdSmemMost));
+  launch_kernel(early_rows(D), kernel, dim3(ctas, p.n), 32 * p.wpr * p.groups, smem, st, p);
   VMOBA_LAUNCH_OK(1);
   if (p.norm != VMOBA_ROTARY_NORM_NONE) {
     const int n_w = p.norm == VMOBA_ROTARY_NORM_ROW ? D.heads * D.d : D.d;
@@ -550,6 +716,43 @@ static int launch_bwd(const Dims& D, const Params& p, const WeightOut& w, cudaSt
     VMOBA_LAUNCH_OK(1);
   }
   return VMOBA_OK;
+}
+
+// The compiled variant of a shape: go(layout, vectors per thread, whether the row fits).
+template <typename T, typename Go>
+static int dispatch(const Dims& D, Params& p, Go go) {
+  int nv;
+  const bool once = lay_out(D, &p, &nv);
+  auto with = [&](auto layout) {
+    constexpr Layout L = decltype(layout)::value;
+    auto pick = [&](auto n, auto o) { return go(layout, n, o); };
+    using std::integral_constant;
+    if (!once) return pick(integral_constant<int, 4>{}, std::false_type{});
+    if constexpr (L == kHalfAny) {           // (rare: one variant, with idle vectors)
+      return pick(integral_constant<int, kMaxNv>{}, std::true_type{});
+    } else {
+      switch (nv) {
+        case 1: return pick(integral_constant<int, 1>{}, std::true_type{});
+        case 2: return pick(integral_constant<int, 2>{}, std::true_type{});
+        case 3: return pick(integral_constant<int, 3>{}, std::true_type{});
+        case 4: return pick(integral_constant<int, 4>{}, std::true_type{});
+        case 5: return pick(integral_constant<int, 5>{}, std::true_type{});
+        default: return pick(integral_constant<int, 6>{}, std::true_type{});
+      }
+    }
+  };
+  if (p.layout == VMOBA_ROTARY_INTERLEAVED) return with(std::integral_constant<Layout, kInterleaved>{});
+  if (p.pairs % Vec<T>::E == 0) return with(std::integral_constant<Layout, kHalf>{});
+  return with(std::integral_constant<Layout, kHalfAny>{});
+}
+
+template <typename T>
+static int launch_fwd(const Dims& D, Params& p, cudaStream_t st) {
+  return dispatch<T>(D, p, [&](auto l, auto n, auto o) { return go_fwd<T, decltype(l)::value, decltype(n)::value, decltype(o)::value>(D, p, st); });
+}
+template <typename T>
+static int launch_bwd(const Dims& D, Params& p, const WeightOut& w, cudaStream_t st) {
+  return dispatch<T>(D, p, [&](auto l, auto n, auto o) { return go_bwd<T, decltype(l)::value, decltype(n)::value, decltype(o)::value>(D, p, w, st); });
 }
 
 }  // namespace rotary
@@ -562,8 +765,8 @@ extern "C" size_t vmoba_rotary_workspace_bytes(const vmoba_shape* shape, const v
   if (rotary::check(shape, spec, &D) || n < 1 || n > rotary::kMaxTensors) return 0;
   if (spec->norm == VMOBA_ROTARY_NORM_NONE) return 256;
   Carver c(nullptr);
-  // (for as many CTAs as any device of 256 SMs runs: the size is a function of the shape alone)
-  c.take<float>((size_t)n * std::min<long long>((long long)D.B * D.S, 512) * (spec->norm == VMOBA_ROTARY_NORM_ROW ? D.heads * D.d : D.d));
+  // (for as many parts as there can be: the size is a function of the shape alone)
+  c.take<float>((size_t)n * std::min<long long>((long long)D.B * D.S, rotary::kMaxParts) * (spec->norm == VMOBA_ROTARY_NORM_ROW ? D.heads * D.d : D.d));
   return c.total();
 }
 
@@ -630,7 +833,6 @@ extern "C" int vmoba_rotary_bwd(const vmoba_shape* shape, const vmoba_rotary_spe
     }
   }
   if (normed && ws_bytes < vmoba_rotary_workspace_bytes(shape, spec, n)) return VMOBA_ERR_WORKSPACE;
-  if (rotary::bwd_smem(D, p) > 200 * 1024) return VMOBA_ERR_NOT_IMPLEMENTED;
   p.part = static_cast<float*>(ws);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return D.dtype == VMOBA_BF16 ? rotary::launch_bwd<__nv_bfloat16>(D, p, w, st) : rotary::launch_bwd<float>(D, p, w, st);
