@@ -217,6 +217,12 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     prefetch_tmap(&tmK);
     prefetch_tmap(&tmV);
   }
+  // rows that a unit leaves over (the group's size does not divide 128): zeros, which no copy writes over
+  for (int i = threadIdx.x; i < (NQ + 1) * (QU - p.tpt * p.G) * 16; i += THREADS) {
+    const int r = p.tpt * p.G + i / ((NQ + 1) * 16), at = i % ((NQ + 1) * 16);
+    *reinterpret_cast<uint4*>(sQ + (at >> 4) * TILE + (at >> 3 & 1) * PANEL + r * 128 + (at & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  fence_async_proxy();
   if (warp == 1) {
     tmem_alloc(&sm->tmem_base, TMEM_COLS);
     tmem_relinquish();
@@ -359,7 +365,6 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     const int lt = threadIdx.x & 127, r0 = 4 * (warp & 3) + (lane >> 3), chunk = lane & 7;      // rows r0 + 16 k
     const int rt = lt / p.G, rg = lt - rt * p.G;
     const int2* rows = p.rows + (long long)mask_batch(p.Bm, it.b) * p.Sq;
-    const bool whole = p.tpt * p.G == QU;
     Walk walk(it);
     float sc = 0.f;
     auto fetch = [&]() {
@@ -381,10 +386,10 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
       (is_q ? sm->lse2[slot] : sm->negD[g & 1])[lt] = sc;
       const int tok0 = walk.u * p.tpt;
       uint8_t* tile = is_q ? sQ + slot * TILE : sO;
-      if (whole && walk.rec.w > 0) {
+      if (walk.rec.w > 0) {
         if (lt == 0) {
           const CUtensorMap* map = is_q ? &tmQ : &tmO;
-          mbar_expect_tx(full, TILE);
+          mbar_expect_tx(full, (uint32_t)(p.tpt * p.G * DH * 2));
           tma_load_5d(tile, map, full, 0, 0, tok0, it.hk, it.b);
           tma_load_5d(tile + PANEL, map, full, 64, 0, tok0, it.hk, it.b);
         } else {
@@ -557,8 +562,26 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
             tmem_st_16x128_x4(st_t + ROW16 + 16 * c, pk[1]);
           }
         };
-        if (masked) weights(true);
-        else weights(false);
+        // (the masked tiles' code out of the way: beside the other roles' it does not fit the instruction cache)
+        if constexpr (CAP) {
+          if (__builtin_expect(masked, 0)) weights(true);
+          else weights(false);
+        } else {
+          if (__builtin_expect(masked, 0)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t w = __shfl_sync(0xffffffffu, bounds, 4 * j + (lane & 3));
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {          // query e of the pair
+                const int lo = w >> (16 * e) & 0xff, n = (int)(w >> (16 * e + 8) & 0xff) - lo, at = key - lo;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)          // key + 8 k
+                  if ((unsigned)(at + 8 * k) >= (unsigned)n) pv[k >> 1][4 * j + 2 * (k & 1) + e] = 0xff800000u;
+              }
+            }
+          }
+          weights(false);
+        }
         // negD of this unit (dV needs the dO rows anyway; asked before dV can run, so that the barrier cannot be a phase ahead)
         wait(&sm->do_full, g & 1);
         tmem_st_wait();

@@ -9,13 +9,18 @@
 // Every (item, unit) has at least one tile, masked as a whole if need be, and every tile at least one unit, so that no barrier skips a phase.
 //
 //   warp 0        TMA: K tiles into a ring of two stages, V tiles into one of three
-//   warps 1, 2    MMA issuers: Q K^T; P V (which first clears what a hull's last tile holds behind its last key: a weight of 0 times a
-//                 value that is not finite would not be 0)
+//   warps 1, 2    MMA issuers: Q K^T; P V
+//   warp 3        clears what the V tile of an item's last keys holds behind them: a weight of 0 times a value that is not finite
+//                 would not be 0 (by the warp that issues P V, the clearing's code alone cost 8 % on tiles that need none)
 //   warps 4-11    softmax of unit A, of unit B: thread = row
 //   warps 12-15   Q tiles of the next item, o of the one before
 //
-// Capped scores: c tanh(x) = c - 2 c / (1 + exp(2 x)), with 2 x = 2 scale s / c; a weight is exp2(c' - m - 2 c' r) with r = 1 / (1 +
-// exp2(s k)), c' = c log2 e.  tanh is monotone, so the row's maximum is looked for among the uncapped scores.
+// Capped scores: c tanh(x), x = scale s / c.  By the exponential unit that is an exponential and a reciprocal more per score, and the
+// kernel is bound by that unit: a 33K clip by frames took 7.5 ms, 3.7 without the cap.  So tanh comes from the FMA pipe where a warp's
+// scores allow (32 keys at a time, |x| <= 3/4): an odd polynomial of five terms, fitted to tanh for the smallest largest error (by reweighted
+// least squares; 1.9e-7); larger scores take 1 - 2 / (1 + exp(2 x)).
+// And a cap bounds the weights: up to c log2 e = 96 (caps of 66) exp2 of a score, of no difference to a maximum, is a normal number, and so are
+// sums of 2^17 of them times values of up to 2^13.  So no maximum is looked for and nothing is rescaled.
 #include <algorithm>
 
 #include "attn_range.cuh"
@@ -39,6 +44,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 
 struct Smem {
   uint64_t k_full[KST], k_empty[KST], v_full[VST], v_empty[VST];
+  uint64_t v_tail[VST];              // the V tile of an item's last keys has landed (warp 3 clears its rest and completes v_full)
   uint64_t s_full[2], p_ready[2];    // per unit: scores written (commit) / P written (128 arrivals)
   uint64_t s_free;                   // the score buffer has been read (128 arrivals of whichever unit used it)
   uint64_t o_done[2];                // per unit: P V of a key tile complete (commit)
@@ -53,13 +59,21 @@ struct Smem {
 constexpr size_t SMEM_BYTES = (2 /*Q*/ + KST + VST) * TILE + sizeof(Smem) + 32;
 static_assert(SMEM_BYTES <= 232448, "range forward: shared memory");
 
+// Capped scores in the exp2 domain: c' tanh(a s), c' = cap * log2 e, a = scale / cap.
+struct Cap {
+  float c, twice_a_log2;         // c', 2 a log2 e
+  float most;                    // |s| up to this: by the polynomial (-1: none)
+  float p[5];                    // its coefficients of s, s^3, ...
+};
+
 struct Params {
   int B, Hk, G, Sq, Sk, Bm, tpt, nU, nI, splits, n_items;
+  FastDiv by_splits, by_nI, by_Hk, by_G;
   const int2* rows;
   const int4* units;
   const int* order;
-  float scale_log2;      // scores -> exp2 domain: scale * log2 e, or capped: k = 2 scale log2 e / cap
-  float cap_log2;        // cap * log2 e
+  float scale_log2;      // scores -> exp2 domain: scale * log2 e; 1 where they are capped first
+  Cap cap;
   __nv_bfloat16 *o, *resid;
   Strides os;
   float* lse;
@@ -77,10 +91,10 @@ struct Item {
 
 __device__ __forceinline__ Item decode_item(const Params& p, int item) {
   Item it;
-  const int m = item / p.splits;
+  const int m = p.by_splits.div(item);
   it.split = item - m * p.splits;
-  const int bhk = m / p.nI;
-  it.b = bhk / p.Hk;
+  const int bhk = p.by_nI.div(m);
+  it.b = p.by_Hk.div(bhk);
   it.hk = bhk - it.b * p.Hk;
   const int bm = mask_batch(p.Bm, it.b);
   it.u0 = 2 * __ldg(p.order + (long long)bm * p.nI + (m - bhk * p.nI));
@@ -93,8 +107,8 @@ __device__ __forceinline__ Item decode_item(const Params& p, int item) {
     hi = max(hi, c.y);
   }
   const int all = (max(hi - lo, 0) + BN - 1) / BN;
-  int first, last;
-  share(all, it.split, p.splits, first, last);
+  int first = 0, last = all;
+  if (p.splits > 1) share(all, it.split, p.splits, first, last);
   it.k_begin = lo + first * BN;
   it.keys = max(min(lo + last * BN, hi) - it.k_begin, 0);
   if (it.keys == 0) it.k_begin = 0;
@@ -134,6 +148,9 @@ __device__ __forceinline__ Item uniform_item(const Params& p, int item) {
 // Keys of tile t that the matrix products take: whole steps of 16, one at least.
 __device__ __forceinline__ int key_steps(const Item& it, int t) { return (max(min(BN, it.keys - t * BN), 1) + 15) >> 4; }
 
+// Whether the item's last tile ends inside a step of 16 keys.
+__device__ __forceinline__ bool has_tail(const Item& it) { return it.keys == 0 || (it.keys & 15) != 0; }
+
 __device__ __forceinline__ constexpr uint32_t koff(int ks) { return (uint32_t)(((ks >> 2) * PANEL + (ks & 3) * 32) >> 4); }
 __device__ __forceinline__ constexpr uint32_t mnoff(int ks) { return (uint32_t)((ks * 2048) >> 4); }
 
@@ -143,35 +160,74 @@ __device__ __forceinline__ float rcp(float x) {
   return y;
 }
 
-// Weights of 32 scores; bf16 pairs (keys 2i, 2i+1 -> word i).  s0/s1 collect the exact weights, r0/r1 the rounded ones (the tensor core
-// multiplies the ROUNDED weights: o is normalised by their sum, so that the rounding perturbs the weights but never their total).
-// neg_m: minus the row's reference maximum; capped: c' minus it.
-template <bool CAP>
-__device__ __forceinline__ void exp_pack32(const uint32_t* sv, float scale, float cap2, float neg_m, bool masked, uint32_t (&pk)[16],
-                                           float& s0, float& s1, float& r0, float& r1) {
+// c' tanh(a s) of 32 of a row's scores, in place.  Called by whole warps (which way is taken is the warp's choice).
+__device__ __forceinline__ void cap_pair(float& x0, float& x1, const Cap& cap) {
+  float z0, z1, r0 = cap.p[4], r1 = cap.p[4];
+  mul2(z0, z1, x0, x1, x0, x1);
+#pragma unroll
+  for (int k = 3; k >= 0; --k) fma2(r0, r1, r0, r1, z0, z1, cap.p[k], cap.p[k]);
+  mul2(x0, x1, r0, r1, x0, x1);
+}
+template <int N>
+__device__ __forceinline__ bool polynomial_does(const uint32_t* sv, const Cap& cap) {
+  float m0 = 0.f, m1 = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    m0 = max3(m0, fabsf(__uint_as_float(sv[i])), fabsf(__uint_as_float(sv[i + 1])));
+    m1 = max3(m1, fabsf(__uint_as_float(sv[i + 2])), fabsf(__uint_as_float(sv[i + 3])));
+  }
+  return __all_sync(0xffffffffu, fmaxf(m0, m1) <= cap.most);
+}
+__device__ __forceinline__ void cap32(uint32_t* sv, const Cap& cap) {
+  if (polynomial_does<32>(sv, cap)) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+      float x0 = __uint_as_float(sv[i]), x1 = __uint_as_float(sv[i + 1]);
+      cap_pair(x0, x1, cap);
+      sv[i] = __float_as_uint(x0);
+      sv[i + 1] = __float_as_uint(x1);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      sv[i] = __float_as_uint(fmaf(-2.0f * cap.c, rcp(1.0f + ex2(__uint_as_float(sv[i]) * cap.twice_a_log2)), cap.c));
+  }
+}
+// 32 scores from key i0 on of a row that sees n keys from key a on: those outside get -inf.
+__device__ __forceinline__ void mask32(uint32_t* sv, int i0, int a, int n) {
+  const int lo = min(max(a - i0, 0), 32), hi = min(max(a + n - i0, 0), 32);
+  const uint32_t w = (hi ? 0xffffffffu >> (32 - hi) : 0u) & (lo < 32 ? 0xffffffffu << lo : 0u);
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (!(w >> i & 1)) sv[i] = 0xff800000u;
+}
+
+// p = 2^(s * scale - m) for 32 scores; bf16 pairs (keys 2i, 2i+1 -> word i).  s0/s1 collect the exact weights, r0/r1 the rounded ones (the
+// tensor core multiplies the ROUNDED weights: o is normalised by their sum, so that the rounding perturbs the weights but never
+// their total).
+__device__ __forceinline__ void exp_pack32(const uint32_t* sv, float scale, float neg_m, uint32_t (&pk)[16], float& s0, float& s1, float& r0,
+                                           float& r1) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     float p0, p1;
-    const float x0 = __uint_as_float(sv[2 * i]), x1 = __uint_as_float(sv[2 * i + 1]);
-    if constexpr (CAP) {
-      mul2(p0, p1, x0, x1, scale, scale);
-      p0 = ex2(p0);
-      p1 = ex2(p1);
-      add2(p0, p1, p0, p1, 1.0f, 1.0f);
-      p0 = rcp(p0);
-      p1 = rcp(p1);
-      fma2(p0, p1, p0, p1, -cap2, -cap2, neg_m, neg_m);
-      p0 = ex2(p0);
-      p1 = ex2(p1);
-      if (masked) {                  // (uniform)
-        if (sv[2 * i] == 0xff800000u) p0 = 0.f;
-        if (sv[2 * i + 1] == 0xff800000u) p1 = 0.f;
-      }
-    } else {
-      fma2(p0, p1, x0, x1, scale, scale, neg_m, neg_m);
-      p0 = ex2(p0);
-      p1 = ex2(p1);
-    }
+    fma2(p0, p1, __uint_as_float(sv[2 * i]), __uint_as_float(sv[2 * i + 1]), scale, scale, neg_m, neg_m);
+    p0 = ex2(p0);
+    p1 = ex2(p1);
+    add2(s0, s1, s0, s1, p0, p1);
+    pk[i] = pack_bf16(p0, p1);
+    add_bf16_pair(r0, r1, pk[i]);
+  }
+}
+
+// The same of capped scores, by the polynomial (FAST), or of scores that have been capped already.
+template <bool FAST>
+__device__ __forceinline__ void exp_capped32(const uint32_t* sv, const Cap& cap, uint32_t (&pk)[16], float& s0, float& s1, float& r0, float& r1) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float p0 = __uint_as_float(sv[2 * i]), p1 = __uint_as_float(sv[2 * i + 1]);
+    if (FAST) cap_pair(p0, p1, cap);
+    p0 = ex2(p0);
+    p1 = ex2(p1);
     add2(s0, s1, s0, s1, p0, p1);
     pk[i] = pack_bf16(p0, p1);
     add_bf16_pair(r0, r1, pk[i]);
@@ -189,7 +245,11 @@ __device__ __forceinline__ void store8_resid(__nv_bfloat16* dst, __nv_bfloat16* 
   if (rdst) *reinterpret_cast<uint4*>(rdst) = make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-template <bool CAP>
+// What a kernel does with the scores: nothing, caps them and goes by the cap's bound, caps them and looks for the maximum as without.
+enum Mode { kPlain, kCapped, kCappedWide };
+constexpr float CAP_MOST = 96.0f;            // c log2 e
+
+template <Mode MODE>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                       const __grid_constant__ CUtensorMap tmQ, const Params p) {
@@ -209,7 +269,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < KST; ++s) { mbar_init(&sm->k_full[s], 1); mbar_init(&sm->k_empty[s], 1); }
-    for (int s = 0; s < VST; ++s) { mbar_init(&sm->v_full[s], 1); mbar_init(&sm->v_empty[s], 1); }
+    for (int s = 0; s < VST; ++s) { mbar_init(&sm->v_full[s], 1); mbar_init(&sm->v_empty[s], 1); mbar_init(&sm->v_tail[s], 1); }
     for (int x = 0; x < 2; ++x) {
       mbar_init(&sm->s_full[x], 1); mbar_init(&sm->p_ready[x], 128);
       mbar_init(&sm->o_done[x], 1); mbar_init(&sm->o_free[x], 128); mbar_init(&sm->ep_ready[x], 128);
@@ -223,6 +283,13 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     prefetch_tmap(&tmV);
     prefetch_tmap(&tmQ);
   }
+  // rows that a unit leaves over (the group's size does not divide 128): no copy writes them, and their scores have a say in the softmax
+  // warps' votes
+  for (int i = threadIdx.x; i < 2 * (BM - p.tpt * p.G) * 16; i += THREADS) {
+    const int r = p.tpt * p.G + (i >> 5), at = i & 31;
+    *reinterpret_cast<uint4*>(sQ + (at >> 4) * TILE + (at >> 3 & 1) * PANEL + r * 128 + (at & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  fence_async_proxy();
   if (warp == 1) {
     tmem_alloc(&sm->tmem_base, TMEM_COLS);
     tmem_relinquish();
@@ -247,12 +314,14 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
           tma_load_4d(sK + ks * TILE, &tmK, &sm->k_full[ks], 0, y, it.hk, it.b);
           tma_load_4d(sK + ks * TILE + PANEL, &tmK, &sm->k_full[ks], 64, y, it.hk, it.b);
           mbar_wait(&sm->v_empty[vs], vp, abort_flag, p.status);
-          mbar_expect_tx(&sm->v_full[vs], TILE);
-          tma_load_4d(sV + vs * TILE, &tmV, &sm->v_full[vs], 0, y, it.hk, it.b);
-          tma_load_4d(sV + vs * TILE + PANEL, &tmV, &sm->v_full[vs], 64, y, it.hk, it.b);
+          uint64_t* full = t == it.ntiles - 1 && has_tail(it) ? &sm->v_tail[vs] : &sm->v_full[vs];
+          mbar_expect_tx(full, TILE);
+          tma_load_4d(sV + vs * TILE, &tmV, full, 0, y, it.hk, it.b);
+          tma_load_4d(sV + vs * TILE + PANEL, &tmV, full, 64, y, it.hk, it.b);
           // drain: every issued load must have landed before the CTA may exit (only matters after a timeout)
           if (*abort_flag) {
             mbar_wait(&sm->k_full[ks], kp ^ 1, abort_flag, p.status);
+            mbar_wait(full, vp ^ 1, abort_flag, p.status);      // (of v_tail whatever phase: then v_full does not complete without it)
             mbar_wait(&sm->v_full[vs], vp ^ 1, abort_flag, p.status);
           }
           if (++ks == KST) { ks = 0; kp ^= 1; }
@@ -308,7 +377,6 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         const Item it = uniform_item(p, item);
         for (int t = 0; t < it.ntiles; ++t) {
           const int ksteps = key_steps(it, t);
-          int clear = t == it.ntiles - 1 ? max(it.keys - t * BN, 0) : BN;      // rows from here on are not the item's
           const uint32_t mv = lo_v + slot * (uint32_t)(TILE >> 4);
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
@@ -316,13 +384,6 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
             // P has been written, the V tile is there, the epilogue of the unit's previous item has read the accumulator
             wait3(&sm->p_ready[x], tcnt[x] & 1, &sm->v_full[slot], par, t == it.tb[x], &sm->o_free[x], (ecnt[x] + 1) & 1);
             tcnt[x] += 1;
-            if (clear < 16 * ksteps) {
-              for (int r = clear + (lane >> 4); r < 16 * ksteps; r += 2)
-                *reinterpret_cast<uint4*>(sV + slot * TILE + (lane >> 3 & 1) * PANEL + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-              fence_async_proxy();
-              __syncwarp();
-              clear = BN;
-            }
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks)
               if (leader && ks < ksteps)   // P of keys 16 ks .. 16 ks + 15 sits in columns 8 ks .. of the unit's P buffer
@@ -337,11 +398,28 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
       }
     }
     if (leader && *abort_flag) mma_drain(&sm->drain[warp - 1]);      // (nothing is under way when the CTA frees its TMEM)
+  } else if (warp == 3) {
+    // ------------------------------------------------------------------ V tiles that end inside a step of 16 keys
+    uint32_t tiles = 0, par = 0;             // tiles so far; bit s: parity of slot s
+    for (int item = blockIdx.x; item < p.n_items; item += gridDim.x) {
+      const Item it = decode_item(p, item);
+      tiles += it.ntiles;
+      if (!has_tail(it)) continue;
+      const uint32_t slot = (tiles - 1) % VST;
+      mbar_wait(&sm->v_tail[slot], par >> slot & 1, abort_flag, p.status);
+      par ^= 1u << slot;
+      const int t = it.ntiles - 1, from = max(it.keys - t * BN, 0);
+      for (int r = from + (lane >> 4); r < 16 * key_steps(it, t); r += 2)
+        *reinterpret_cast<uint4*>(sV + slot * TILE + (lane >> 3 & 1) * PANEL + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+      fence_async_proxy();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sm->v_full[slot]);
+    }
   } else if (warp >= 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     // ------------------------------------------------------------------ the Q tiles of item n, then o of item n - 1
     const int lt = (warp - 12) * 32 + lane;   // 0..127: row of a unit
-    const int rows = p.tpt * p.G, rt = lt / p.G, rg = lt - rt * p.G;
+    const int rows = p.tpt * p.G, rt = p.by_G.div(lt), rg = lt - rt * p.G;
     uint32_t n = 0;
     uint32_t tcs[2] = {0, 0}, eps[2] = {0, 0};        // per unit: P V and items done
     const long long all_rows = (long long)p.B * p.Hk * p.Sq * p.G;
@@ -372,17 +450,22 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
             mbar_arrive(&sm->o_free[x]);
           }
           if (row_ok) {
-            const int col = 16 * c;
-            float v[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = inv == 0.f ? 0.f : __uint_as_float(ov[i]) * inv;
             if (p.splits == 1) {
 #pragma unroll
-              for (int i = 0; i < 16; i += 8)
-                store8_resid(o_row + col + i, r_row ? r_row + col + i : nullptr, *reinterpret_cast<const float(*)[8]>(&v[i]));
-            } else {
+              for (int i = 0; i < 16; i += 8) {
+                float v[8];
 #pragma unroll
-              for (int i = 0; i < 16; i += 4) store4(p.part_o + packed * DH + col + i, make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
+                for (int k = 0; k < 8; ++k) v[k] = inv == 0.f ? 0.f : __uint_as_float(ov[i + k]) * inv;
+                store8_resid(o_row + i, r_row ? r_row + i : nullptr, v);
+              }
+              o_row += 16;
+              if (r_row) r_row += 16;
+            } else {
+              float* to = p.part_o + packed * DH + 16 * c;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) ov[i] = inv == 0.f ? 0u : __float_as_uint(__uint_as_float(ov[i]) * inv);
+#pragma unroll
+              for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4*>(to + i) = make_uint4(ov[i], ov[i + 1], ov[i + 2], ov[i + 3]);
             }
           }
         }
@@ -414,7 +497,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     const int x = (warp - 4) >> 2;                  // unit of this warp group
     const int quad = warp & 3;                      // TMEM lane quarter this warp may access
     const int r = quad * 32 + lane;                 // row of the unit
-    const int rt = r / p.G;
+    const int rt = p.by_G.div(r);
     const bool is_row = r < p.tpt * p.G;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
     const uint32_t s_tmem = tmem + lane_addr;
@@ -424,18 +507,21 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     for (int item = blockIdx.x; item < p.n_items; item += gridDim.x) {
       const Item it = decode_item(p, item);
       if (x >= it.nx) continue;
-      const int tok = (it.u0 + x) * p.tpt + rt;
-      int2 seen = make_int2(0, 0);
-      if (is_row && tok < p.Sq) seen = __ldg(p.rows + (long long)mask_batch(p.Bm, it.b) * p.Sq + tok);
-      // of the item's keys: [seen.x, seen.y)
-      seen.x = max(seen.x - it.k_begin, 0);
-      seen.y = min(seen.y - it.k_begin, it.keys);
-      const int tb = it.tb[x], te = it.te[x], full_lo = it.full_lo[x] - it.k_begin, full_hi = min(it.full_hi[x] - it.k_begin, it.keys);
-      float m_used = -INFINITY, l = 0.f, l_r = 0.f;   // l: exact sum (for LSE); l_r: sum of the bf16-rounded weights
+      const int tb = it.tb[x], te = it.te[x];
+      // tiles in [all_lo, all_hi) are seen by every row as a whole
+      const int all_lo = (max(it.full_lo[x] - it.k_begin, 0) + BN - 1) / BN, all_hi = max(min(it.full_hi[x] - it.k_begin, it.keys), 0) / BN;
+      // of tile t, this row's range: first key and number of keys
+      auto seen = [&](int t) {
+        const int tok = (it.u0 + x) * p.tpt + rt;
+        int2 r = make_int2(0, 0);
+        if (is_row && tok < p.Sq) r = __ldg(p.rows + (long long)mask_batch(p.Bm, it.b) * p.Sq + tok);
+        const int a = max(r.x - it.k_begin, 0) - t * BN;
+        return make_int2(a, max(min(r.y - it.k_begin, it.keys) - t * BN - a, 0));
+      };
+      float m_used = MODE == kCapped ? 0.f : -INFINITY, l = 0.f, l_r = 0.f;   // l: exact sum (for LSE); l_r: sum of the bf16-rounded weights
       for (int t = tb; t < te; ++t, ++tc) {
         mbar_wait(&sm->s_full[x], tc & 1, abort_flag, p.status);
         tc_fence_after();
-        const bool masked = full_lo > t * BN || full_hi < t * BN + BN;
         const int valid = min(BN, it.keys - t * BN);
         uint32_t sv[128];
 #pragma unroll
@@ -443,11 +529,56 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         tmem_ld_wait();
         tc_fence_before();
         mbar_arrive(&sm->s_free);                    // the other unit's Q K^T may have the buffer
-        if (masked) {                                // keys outside the row's range get score -inf
-          const int a = seen.x - t * BN, n = max(seen.y - t * BN - a, 0);
+        if constexpr (MODE == kCapped) {
+          // Tiles that every row sees as a whole, small scores: one run of instructions without a branch, in which the polynomial of some
+          // scores (FMA pipe) goes beside the exponentials of others.
+          const bool masked = t < all_lo || t >= all_hi;
+          float s0 = 0.f, s1 = 0.f, r0 = 0.f, r1 = 0.f;
+          auto p_free = [&]() {                              // P V of the tile before has read the P buffer
+            if (tc > 0) {
+              mbar_wait(&sm->o_done[x], (tc - 1) & 1, abort_flag, p.status);
+              tc_fence_after();
+            }
+          };
+          if (__builtin_expect(!masked && polynomial_does<128>(sv, p.cap), 1)) {
+            uint32_t pk[4][16];
+            exp_capped32<true>(sv, p.cap, pk[0], s0, s1, r0, r1);
+            exp_capped32<true>(sv + 32, p.cap, pk[1], s0, s1, r0, r1);
+            p_free();
+            tmem_st16(p_tmem, pk[0]);
+            tmem_st16(p_tmem + 16, pk[1]);
+            exp_capped32<true>(sv + 64, p.cap, pk[2], s0, s1, r0, r1);
+            tmem_st16(p_tmem + 32, pk[2]);
+            exp_capped32<true>(sv + 96, p.cap, pk[3], s0, s1, r0, r1);
+            tmem_st16(p_tmem + 48, pk[3]);
+          } else {
+            const int2 r = masked ? seen(t) : make_int2(0, BN);
+            p_free();
 #pragma unroll
-          for (int i = 0; i < BN; ++i)
-            if ((unsigned)(i - a) >= (unsigned)n) sv[i] = 0xff800000u;
+            for (int c = 0; c < 4; ++c) {
+              if (c > 0 && 32 * c >= valid) continue;        // (uniform; P V takes the keys up to `valid` only)
+              cap32(sv + 32 * c, p.cap);
+              if (masked) mask32(sv + 32 * c, 32 * c, r.x, r.y);
+              uint32_t pk[16];
+              exp_capped32<false>(sv + 32 * c, p.cap, pk, s0, s1, r0, r1);
+              tmem_st16(p_tmem + 16 * c, pk);
+            }
+          }
+          l += s0 + s1;
+          l_r += r0 + r1;
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive(&sm->p_ready[x]);
+          continue;
+        }
+        if (MODE == kCappedWide) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) cap32(sv + 32 * c, p.cap);
+        }
+        if (__builtin_expect(t < all_lo || t >= all_hi, 0)) {      // keys outside the row's range get score -inf
+          const int2 r = seen(t);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) mask32(sv + 32 * c, 32 * c, r.x, r.y);
         }
         float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
 #pragma unroll
@@ -457,9 +588,8 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
           mx2 = max3(mx2, __uint_as_float(sv[i + 4]), __uint_as_float(sv[i + 5]));
           mx3 = max3(mx3, __uint_as_float(sv[i + 6]), __uint_as_float(sv[i + 7]));
         }
-        float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
-        if (CAP) mx = mx == -INFINITY ? mx : fmaf(-2.0f * p.cap_log2, rcp(1.0f + ex2(mx * p.scale_log2)), p.cap_log2);
-        else mx *= p.scale_log2;                     // exp2 domain from here on (the scale is positive)
+        const float scale = MODE == kPlain ? p.scale_log2 : 1.0f;
+        const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * scale;      // exp2 domain from here on (the scale is positive)
         // lazy rescale: keep the old reference max unless the new one is more than 2^8 larger
         float factor = 1.0f;
         bool need = false;
@@ -482,14 +612,13 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
           }
         };
         float s0 = 0.f, s1 = 0.f, r0 = 0.f, r1 = 0.f;
-        const float neg_m = (m_used == -INFINITY ? 0.f : -m_used) + (CAP ? p.cap_log2 : 0.f);
-        const float cap2 = 2.0f * p.cap_log2;
+        const float neg_m = m_used == -INFINITY ? 0.f : -m_used;
         {
           // the first half's weights stay in registers until P V of the tile before has read the P buffer
           uint32_t pk[2][16];
-          exp_pack32<CAP>(sv, p.scale_log2, cap2, neg_m, masked, pk[0], s0, s1, r0, r1);
+          exp_pack32(sv, scale, neg_m, pk[0], s0, s1, r0, r1);
           const uint32_t pv_done = mbar_test_wait(&sm->o_done[x], (tc + 1) & 1);      // (an early look, because the answer takes its time)
-          if (valid > 32) exp_pack32<CAP>(sv + 32, p.scale_log2, cap2, neg_m, masked, pk[1], s0, s1, r0, r1);
+          if (valid > 32) exp_pack32(sv + 32, scale, neg_m, pk[1], s0, s1, r0, r1);
           if (tc > 0) {                              // (of the item before, where t is its first)
             if (!__all_sync(0xffffffffu, pv_done)) mbar_wait(&sm->o_done[x], (tc - 1) & 1, abort_flag, p.status);
             tc_fence_after();
@@ -506,7 +635,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         for (int c = 2; c < 4; ++c) {
           if (32 * c < valid) {                      // (uniform; P V takes the keys up to `valid` only)
             uint32_t pk[16];
-            exp_pack32<CAP>(sv + 32 * c, p.scale_log2, cap2, neg_m, masked, pk, s0, s1, r0, r1);
+            exp_pack32(sv + 32 * c, scale, neg_m, pk, s0, s1, r0, r1);
             tmem_st16(p_tmem + 16 * c, pk);
           }
         }
@@ -546,6 +675,21 @@ bool make_tmap_units(CUtensorMap* map, const void* base, const RDims& D, const S
   return sm100::make_tmap_bf16_strided(map, base, 5, n, st, box);
 }
 
+// The polynomial's coefficients with the factors of score and result folded in.  Where that leaves fp32's range (caps of more than some
+// hundred times the scale's usual) every score takes the long way.
+static tcf::Cap make_cap(const RDims& D) {
+  static const double k[5] = {0.9999972283, -0.3332307648, 0.1322609162, -0.04928044707, 0.01231883178};
+  tcf::Cap c = {};
+  if (!(D.cap > 0.f)) return c;
+  const double a = (double)D.scale / D.cap, top = (double)D.cap * 1.4426950408889634;
+  c.c = (float)top;
+  c.twice_a_log2 = (float)(2.0 * a * 1.4426950408889634);
+  c.most = a >= 2e-4 && a <= 1e3 && top <= 1e6 ? (float)(0.75 / a) : -1.f;
+  double f = top * a;
+  for (int i = 0; i < 5; ++i, f *= a * a) c.p[i] = (float)(k[i] * f);
+  return c;
+}
+
 int tc_range_fwd(const RDims& D, const Plan& plan, const FwdArgs& a, cudaStream_t st) {
   using namespace tcf;
   const long long items = (long long)D.B * D.Hk * D.nI * a.splits;
@@ -554,13 +698,16 @@ int tc_range_fwd(const RDims& D, const Plan& plan, const FwdArgs& a, cudaStream_
   p.B = D.B; p.Hk = D.Hk; p.G = D.G; p.Sq = D.Sq; p.Sk = D.Sk; p.Bm = D.Bm; p.tpt = D.tpt; p.nU = D.nU; p.nI = D.nI;
   p.splits = a.splits; p.n_items = (int)items;
   p.rows = plan.rows; p.units = plan.units; p.order = plan.order;
-  p.scale_log2 = D.cap > 0.f ? 2.0f * D.scale * LOG2E / D.cap : D.scale * LOG2E;
-  p.cap_log2 = D.cap * LOG2E;
+  p.by_splits = FastDiv(a.splits); p.by_nI = FastDiv(D.nI); p.by_Hk = FastDiv(D.Hk); p.by_G = FastDiv(D.G);
+  p.scale_log2 = D.scale * LOG2E;
+  p.cap = make_cap(D);
   p.o = (__nv_bfloat16*)a.o; p.resid = (__nv_bfloat16*)a.resid; p.os = a.os; p.lse = a.lse;
   p.part_o = a.part_o; p.part_lse = a.part_lse; p.status = a.status;
   CUtensorMap tmK, tmV, tmQ;
   if (!make_tmap_keys(&tmK, a.k, D, a.ks) || !make_tmap_keys(&tmV, a.v, D, a.vs) || !make_tmap_units(&tmQ, a.q, D, a.qs)) return VMOBA_ERR_CUDA;
-  auto kernel = D.cap > 0.f ? attn_range_fwd_kernel<true> : attn_range_fwd_kernel<false>;
+  auto kernel = !(D.cap > 0.f)           ? attn_range_fwd_kernel<kPlain>
+                : p.cap.c <= CAP_MOST ? attn_range_fwd_kernel<kCapped>
+                                      : attn_range_fwd_kernel<kCappedWide>;
   VMOBA_CUDA_OK(allow_smem(kernel, (int)SMEM_BYTES));
   launch_kernel(kernel, (unsigned)std::min<long long>(items, sm_count()), THREADS, SMEM_BYTES, st, tmK, tmV, tmQ, p);
   VMOBA_LAUNCH_OK(1);

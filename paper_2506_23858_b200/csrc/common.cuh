@@ -227,6 +227,19 @@ inline void launch_cluster(bool early, int cluster, void (*kernel)(P...), dim3 g
   cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
 }
 
+// Quotients by a divisor known to the host, of numbers below 2^31.
+struct FastDiv {
+  unsigned m, s;
+  FastDiv() = default;
+  explicit FastDiv(unsigned d) : m(0), s(0) {
+    while ((1u << s) < d) ++s;
+    m = (unsigned)(((1ull << (31 + s)) + d - 1) / d);      // ceil(2^(31 + s) / d), below 2^32 for 2^(s - 1) < d <= 2^s
+  }
+#ifdef __CUDACC__
+  __device__ __forceinline__ int div(int n) const { return s ? (int)(__umulhi((unsigned)n, m) >> (s - 1)) : n; }
+#endif
+};
+
 // One tensor of at most 16 MB: a pass over a few of them takes about ten microseconds, of which an early launch saves two.
 inline bool early_rows(const Dims& D) { return (long long)D.BH * D.S * D.d * D.es <= (16ll << 20); }
 

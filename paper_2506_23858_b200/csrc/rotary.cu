@@ -28,17 +28,6 @@ constexpr int kMaxTensors = 4;
 constexpr int kMaxWarps = 8;                 // of a CTA, and of a row
 constexpr int kMaxPairs = 64;
 
-// Quotients by a divisor known to the host, of numbers below 2^31.
-struct FastDiv {
-  unsigned m, s;
-  FastDiv() = default;
-  explicit FastDiv(unsigned d) : m(0), s(0) {
-    while ((1u << s) < d) ++s;
-    m = (unsigned)(((1ull << (31 + s)) + d - 1) / d);      // ceil(2^(31 + s) / d), below 2^32 for 2^(s - 1) < d <= 2^s
-  }
-  __device__ __forceinline__ int div(int n) const { return s ? (int)(__umulhi((unsigned)n, m) >> (s - 1)) : n; }
-};
-
 struct Tensor {
   const void* src;                           // forward: x; backward: the gradient of the output
   const void* x;                             // backward with a norm: x
