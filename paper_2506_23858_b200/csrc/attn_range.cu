@@ -105,7 +105,8 @@ plan_tiles_kernel(Plan plan, RDims D) {
     const long long bm = w / D.nK;
     const int t = (int)(w - bm * D.nK);
     const int4* units = plan.units + bm * D.nU;
-    int first = INT32_MAX, last = -1, lo = INT32_MAX, hi = 0;
+    int first = INT32_MAX, last = -1, lo = INT32_MAX, hi = 0, count = 0, whole = INT32_MAX, until = D.nU;
+    auto sees_all = [&](const int4& a) { return reaches(a, t, D.TR) && a.z <= t * D.TR && a.w >= (t + 1) * D.TR; };
     for (int u = lane; u < D.nU; u += 32) {
       const int4 a = units[u];
       if (!reaches(a, t, D.TR)) continue;
@@ -113,13 +114,23 @@ plan_tiles_kernel(Plan plan, RDims D) {
       last = max(last, u);
       lo = min(lo, a.x);
       hi = max(hi, a.y);
+      ++count;
+      if (sees_all(a)) whole = min(whole, u);
     }
+    whole = __reduce_min_sync(0xffffffffu, whole);
+    count = __reduce_add_sync(0xffffffffu, count);
+    if (whole < D.nU)
+      for (int u = whole + lane; u < D.nU; u += 32)
+        if (!sees_all(units[u])) { until = u; break; }
+    until = __reduce_min_sync(0xffffffffu, until);
     first = __reduce_min_sync(0xffffffffu, first);
     last = __reduce_max_sync(0xffffffffu, last);
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_max_sync(0xffffffffu, hi);
-    if (lane == 0)
+    if (lane == 0) {
+      plan.runs[w] = whole < D.nU ? make_int4(count, whole, until, 0) : make_int4(count, 0, 0, 0);
       plan.keys[w] = last < 0 ? make_int4(0, 0, 0, 0) : make_int4(first, last + 1, max(lo - t * D.TR, 0), min(hi - t * D.TR, D.TR));
+    }
   }
 }
 
@@ -333,51 +344,57 @@ range_merge_kernel(const RDims D, const FwdArgs a) {
   }
 }
 
-// D = rowsum(dO * O) per packed row, 0 where the row sees nothing (its dO is not read).  zero_words: counters cleared on the way.
+// D = rowsum(dO * O) per packed row, 0 where the row sees nothing (whatever its dO holds).  zero_words: counters cleared on the way.
+// A warp has four rows under way; nothing of a row's loads waits for another load (13,440 tokens x 12 heads: 51 us with the range looked at
+// first and quotients by division).
 template <typename T, int DH>
 __global__ void __launch_bounds__(256)
-range_rowdot_kernel(const RDims D, const Plan plan, const T* __restrict__ o, Strides os, const T* __restrict__ resid,
-                    const T* __restrict__ d_o, Strides dos, float* __restrict__ Dv, int* __restrict__ zero_words, long long n_words) {
+range_rowdot_kernel(const RDims D, const FastDiv by_rows, const FastDiv by_G, const FastDiv by_Hk, const Plan plan, const T* __restrict__ o,
+                    Strides os, const T* __restrict__ resid, const T* __restrict__ d_o, Strides dos, float* __restrict__ Dv,
+                    int* __restrict__ zero_words, long long n_words) {
   if (!grid_begin()) return;
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n_words; i += (long long)gridDim.x * blockDim.x)
     zero_words[i] = 0;
-  constexpr int C = DH / 32, R = 4;            // channels per lane; rows of a warp whose loads are in flight together
+  constexpr int C = DH / 32, R = 4;            // channels per lane; rows of a warp
   const int lane = threadIdx.x & 31;
-  const long long all_rows = (long long)D.B * D.Hk * D.rows;
-  for (long long row0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * R; row0 < all_rows; row0 += (long long)gridDim.x * 8 * R) {
+  const int all_rows = D.B * D.Hk * D.rows;    // (at most 2^30)
+  for (int row0 = (blockIdx.x * 8 + (threadIdx.x >> 5)) * R; row0 < all_rows; row0 += gridDim.x * 8 * R) {
     float x[R][C], y[R][C], z[R][C];
+    int seen[R];
 #pragma unroll
     for (int n = 0; n < R; ++n) {
-      const long long row = min(row0 + n, all_rows - 1);
-      const int bhk = (int)((unsigned)row / (unsigned)D.rows), r = (int)(row - (long long)bhk * D.rows), tok = r / D.G, g = r - tok * D.G;
-      const int b = bhk / D.Hk, head = (bhk - b * D.Hk) * D.G + g;
-      const bool some = __ldg(&plan.rows[(long long)mask_batch(D.Bm, b) * D.Sq + tok].y) > 0;
+      const int row = min(row0 + n, all_rows - 1), bhk = by_rows.div(row), r = row - bhk * D.rows, tok = by_G.div(r), g = r - tok * D.G;
+      const int b = by_Hk.div(bhk), head = (bhk - b * D.Hk) * D.G + g;
+      seen[n] = __ldg(&plan.rows[(long long)mask_batch(D.Bm, b) * D.Sq + tok].y);
+      auto get = [&](const T* from, float (&to)[C]) {
+        if constexpr (C == 4) {
+          const float4 v = load4(from + lane * 4);
+          to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w;
+        } else {
 #pragma unroll
-      for (int c = 0; c < C; ++c) x[n][c] = y[n][c] = z[n][c] = 0.f;
-      if (some) {
-        auto get = [&](const T* from, float (&to)[C]) {
-          if constexpr (C == 4) {
-            const float4 v = load4(from + lane * 4);
-            to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w;
-          } else {
+          for (int c = 0; c < C; ++c) to[c] = to_f32<T>(from[lane * C + c]);
+        }
+      };
+      get(o + b * os.b + tok * os.t + head * os.h, x[n]);
+      get(d_o + b * dos.b + tok * dos.t + head * dos.h, y[n]);
 #pragma unroll
-            for (int c = 0; c < C; ++c) to[c] = to_f32<T>(from[lane * C + c]);
-          }
-        };
-        get(o + b * os.b + tok * os.t + head * os.h, x[n]);
-        get(d_o + b * dos.b + tok * dos.t + head * dos.h, y[n]);
-        if (resid) get(resid + (((long long)b * D.Sq + tok) * D.Hq + head) * DH, z[n]);
-      }
+      for (int c = 0; c < C; ++c) z[n][c] = 0.f;
+      if (resid) get(resid + (((long long)b * D.Sq + tok) * D.Hq + head) * DH, z[n]);
     }
+    float s[R];
 #pragma unroll
     for (int n = 0; n < R; ++n) {
-      float s = 0.f;
+      s[n] = 0.f;
 #pragma unroll
-      for (int c = 0; c < C; ++c) s = fmaf(x[n][c] + z[n][c], y[n][c], s);
-#pragma unroll
-      for (int k = 16; k > 0; k >>= 1) s += __shfl_xor_sync(0xffffffffu, s, k);
-      if (lane == 0 && row0 + n < all_rows) Dv[row0 + n] = s;
+      for (int c = 0; c < C; ++c) s[n] = fmaf(x[n][c] + z[n][c], y[n][c], s[n]);
     }
+#pragma unroll
+    for (int k = 16; k > 0; k >>= 1)
+#pragma unroll
+      for (int n = 0; n < R; ++n) s[n] += __shfl_xor_sync(0xffffffffu, s[n], k);
+#pragma unroll
+    for (int n = 0; n < R; ++n)
+      if (lane == 0 && row0 + n < all_rows) Dv[row0 + n] = seen[n] > 0 ? s[n] : 0.f;
   }
 }
 
@@ -600,6 +617,7 @@ static Plan carve_plan(const RDims& D, const void* mem, size_t* bytes) {
   p.rows = c.take<int2>((size_t)D.Bm * D.Sq);
   p.units = c.take<int4>((size_t)D.Bm * D.nU);
   p.keys = c.take<int4>((size_t)D.Bm * D.nK);
+  p.runs = c.take<int4>((size_t)D.Bm * D.nK);
   p.order = c.take<int>((size_t)D.Bm * D.nI);
   if (bytes) *bytes = c.total();
   return p;
@@ -695,7 +713,8 @@ template <typename T, int DH>
 static int backward(const RDims& D, const Plan& plan, const BwdArgs& a, const void* o, const Strides& os, const void* resid, float* Dv,
                     void* dq, const Strides& dqs, cudaStream_t st) {
   const long long all_rows = (long long)D.B * D.Hk * D.rows;
-  launch_kernel(early_rows(D), range_rowdot_kernel<T, DH>, grid_for((all_rows + 31) / 32, 16), 256, 0, st, D, plan, (const T*)o, os,
+  launch_kernel(early_rows(D), range_rowdot_kernel<T, DH>, grid_for((all_rows + 31) / 32, 16), 256, 0, st, D, FastDiv(D.rows),
+                FastDiv(D.G), FastDiv(D.Hk), plan, (const T*)o, os,
                 (const T*)resid, (const T*)a.d_o, a.dos, Dv, a.turns, a.turns ? tc_range_bwd_turns(D) : 0ll);
   VMOBA_LAUNCH_OK(1);
   if constexpr (sizeof(T) == 2 && DH == 128) {

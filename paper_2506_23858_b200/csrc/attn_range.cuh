@@ -9,6 +9,7 @@
 //   units  int4 [Bm][nU]   of a unit's rows that see something: smallest lo, largest hi; of all its rows: largest lo, smallest hi
 //   keys   int4 [Bm][nK]   of a tile of TR keys: first and one past the last unit that reaches into it; first and one past the last
 //                          key (relative to the tile) that any unit's hull holds
+//   runs   int4 [Bm][nK]   how many units reach into it; a run [first, last) of units of which every row sees the whole tile
 //   order  int  [Bm][nI]   the forward's items (two units on the tensor cores, else one), those with the most keys first
 #pragma once
 
@@ -35,6 +36,7 @@ struct Plan {
   int2* rows;
   int4* units;
   int4* keys;
+  int4* runs;
   int* order;
 };
 
@@ -50,6 +52,15 @@ __device__ __forceinline__ void share(int tiles, int split, int n, int& first, i
   first = (int)((long long)tiles * split / n);
   last = (int)((long long)tiles * (split + 1) / n);
 }
+
+// Capped scores in the exp2 domain: c' tanh(a s), c' = cap * log2 e, a = scale / cap.
+struct Cap {
+  float c, twice_a_log2;         // c', 2 a log2 e
+  float most;                    // |s| up to this: by the polynomial (-1: none)
+  float p[5];                    // its coefficients of s, s^3, ...
+};
+
+Cap make_cap(const RDims& D);      // attn_range_fwd.cu
 
 // ---- tensor-core kernels (attn_range_fwd.cu, attn_range_bwd.cu)
 struct FwdArgs {

@@ -5,15 +5,20 @@
 // group among them, so that dK and dV of shared heads are sums inside the CTA and are written once.  Per unit, keys on the TMEM lanes:
 //     S^T = K Q^T;  P^T = exp2(c S^T - lse), capped exp2(c' tanh - lse), 0 outside the range;  dV += P^T dO
 //     dP^T = V dO^T;  dS^T = P^T (dP^T - D) (1 - tanh^2);  dK += dS^T Q;  dQ^T = K^T dS^T, added into an fp32 accumulator
-// The slope 1 - tanh^2 = 4 r (1 - r), r = 1 / (1 + exp(2 x)), is taken into the fp32 weights that the second step keeps, at no register.
+// The slope 1 - tanh^2 is taken into the fp32 weights that the second step keeps, at no register.  tanh comes from the forward's polynomial
+// where a warp's scores allow, else from r = 1 / (1 + exp(2 x)): slope 4 r (1 - r).
 //
 // dQ of a unit is added key tile after key tile, so that the backward repeats bit for bit: a counter per unit says how many of the
-// tiles of its hull (which are consecutive) have been added; the first one stores.  A tile waits for lower tickets only.  Up to four
+// tiles of its hull (which are consecutive) have been added; the first one stores.  A tile waits for lower tickets only.  Units go
+// from the last to the first: where hulls move forward with the queries (causal order, windows, clips) the lowest tile that a unit
+// waits for then starts with it, or all tiles come to it at the same time.  (From the first to the last, the tiles of a causal clip's later
+// frames waited for those of the first frame to get there: 13K tokens, two clips, 1.55 ms.)  Up to four
 // accumulators (tile n of a unit's hull adds to accumulator n mod 4) where they fit 128 MB, see the dense backward.
 //
 // Rows of a unit that see nothing are brought in as zeros (asynchronous copies instead of the TMA tile), keys that no query sees are
 // cleared in K: 0 times what they hold would not be 0 if it is not finite.
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_range.cuh"
 #include "sm100.cuh"
@@ -34,7 +39,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr int NQ = 3;                        // Q tiles in flight (one dO tile: see the dense backward)
 
 struct Smem {
-  uint64_t k_full, v_full;
+  uint64_t k_full, k_ready, v_full;                                // K landed / and cleared of keys that nobody sees; V landed
   uint64_t q_full[NQ], q_empty[NQ], do_full, do_empty;             // Q / dO rows of a unit (128 arrivals) / no longer needed (commit)
   uint64_t s_full, p_ready;                                        // S^T complete (commit) / P^T written (256 arrivals)
   uint64_t dp_full, ds_ready;                                      // dP^T complete (commit) / dS^T written (256 arrivals)
@@ -60,11 +65,14 @@ struct Params {
   int B, Hk, G, Sq, Sk, Bm, tpt, nU, nK;
   const int2* rows;
   const int4* units;
-  const int4* keys;
+  const int4 *keys, *runs;
+  FastDiv by_G, by_tpt, by_rows, by_Hk, by_parts;
   const __nv_bfloat16 *q, *d_o;
   Strides qs, dos;
   const float *lse, *Dv;
-  float scale, scale_log2, cap_log2;      // scores -> exp2 domain as in the forward
+  float scale, scale_log2;     // scale_log2: scores -> exp2 domain, not capped
+  Cap cap;
+  float cap_inv2;              // -1 / c'^2
   __nv_bfloat16 *dk, *dv;
   Strides dks, dvs;
   int dkv_32;                  // rows of dk and dv are 32-byte aligned: they go out with 32-byte stores
@@ -79,6 +87,7 @@ struct Params {
 struct Item {
   int bhk, b, hk, tile, key0, valid;
   int4 info;                   // first and one past the last unit, first and one past the last key that somebody sees
+  int4 run;                    // units that reach into the tile; [y, z): units that see all of it
   const int4* units;
 };
 __device__ __forceinline__ Item decode(const Params& p, int ticket) {
@@ -93,22 +102,24 @@ __device__ __forceinline__ Item decode(const Params& p, int ticket) {
   it.valid = min(BN, p.Sk - it.key0);
   const int bm = mask_batch(p.Bm, it.b);
   it.info = __ldg(p.keys + (long long)bm * p.nK + it.tile);
+  it.run = __ldg(p.runs + (long long)bm * p.nK + it.tile);
   it.units = p.units + (long long)bm * p.nU;
   return it;
 }
 
-// Walks the units of an item.
+// Walks the units of an item, from the last to the first.  Where they are consecutive, as they nearly always are, no record is read on
+// the way.
 struct Walk {
-  int u, last, tile;
+  int u, first, tile;
+  bool gaps;
   const int4* units;
-  int4 rec;
-  __device__ __forceinline__ explicit Walk(const Item& it) : u(it.info.x - 1), last(it.info.y), tile(it.tile), units(it.units) {}
+  __device__ __forceinline__ explicit Walk(const Item& it)
+      : u(it.info.y), first(it.info.x), tile(it.tile), gaps(it.run.x != it.info.y - it.info.x), units(it.units) {}
   __device__ __forceinline__ bool next() {
-    while (++u < last) {
-      rec = __ldg(units + u);
-      if (reaches(rec, tile, BN)) return true;
-    }
-    return false;
+    --u;
+    if (__builtin_expect(gaps, 0))
+      while (u >= first && !reaches(__ldg(units + u), tile, BN)) --u;
+    return u >= first;
   }
 };
 __device__ __forceinline__ int unit_rows(const Params& p, int u) { return min(p.tpt, p.Sq - u * p.tpt) * p.G; }
@@ -181,7 +192,8 @@ __device__ __forceinline__ void stmatrix_x4(uint32_t addr, uint32_t a, uint32_t 
                : "memory");
 }
 
-template <bool CAP>
+// MULTI: several accumulators (with p.parts read in the one kernel, the case of one is slower).
+template <bool CAP, bool MULTI>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                       const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmO, const Params p) {
@@ -203,7 +215,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
   auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, p.status); };
 
   if (threadIdx.x == 0) {
-    mbar_init(&sm->k_full, 1); mbar_init(&sm->v_full, 1);
+    mbar_init(&sm->k_full, 1); mbar_init(&sm->k_ready, 1); mbar_init(&sm->v_full, 1);
     for (int b = 0; b < NQ; ++b) { mbar_init(&sm->q_full[b], 128); mbar_init(&sm->q_empty[b], 1); }
     mbar_init(&sm->do_full, 128); mbar_init(&sm->do_empty, 1);
     mbar_init(&sm->s_full, 1); mbar_init(&sm->p_ready, 256);
@@ -212,7 +224,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     mbar_init(&sm->acc_done, 1); mbar_init(&sm->drain, 1);
     mbar_init(&sm->turn_ok, 1); mbar_init(&sm->rows_out, 256); mbar_init(&sm->rows_seen, 1);
     sm->abort_flag = 0;
-    sm->ticket = atomicAdd(p.turns + (long long)p.parts * p.B * p.Hk * p.nU, 1);
+    sm->ticket = atomicAdd(p.turns + (long long)(MULTI ? p.parts : 1) * p.B * p.Hk * p.nU, 1);
     fence_barrier_init();
     prefetch_tmap(&tmK);
     prefetch_tmap(&tmV);
@@ -239,15 +251,27 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if (warp == 0) {
       // ---------------------------------------------------------------- TMA: the K and V tiles
-      if (lane == 0 && some) {
-        mbar_expect_tx(&sm->k_full, TILE);
-        tma_load_4d(sK, &tmK, &sm->k_full, 0, it.key0, it.hk, it.b);
-        tma_load_4d(sK + PANEL, &tmK, &sm->k_full, 64, it.key0, it.hk, it.b);
-        mbar_expect_tx(&sm->v_full, TILE);
-        tma_load_4d(sV, &tmV, &sm->v_full, 0, it.key0, it.hk, it.b);
-        tma_load_4d(sV + PANEL, &tmV, &sm->v_full, 64, it.key0, it.hk, it.b);
-        wait(&sm->k_full, 0);        // landed before the CTA may exit, whatever the others do
-        wait(&sm->v_full, 0);
+      if (some) {
+        if (lane == 0) {
+          mbar_expect_tx(&sm->k_full, TILE);
+          tma_load_4d(sK, &tmK, &sm->k_full, 0, it.key0, it.hk, it.b);
+          tma_load_4d(sK + PANEL, &tmK, &sm->k_full, 64, it.key0, it.hk, it.b);
+          mbar_expect_tx(&sm->v_full, TILE);
+          tma_load_4d(sV, &tmV, &sm->v_full, 0, it.key0, it.hk, it.b);
+          tma_load_4d(sV + PANEL, &tmV, &sm->v_full, 64, it.key0, it.hk, it.b);
+        }
+        __syncwarp();
+        wait(&sm->k_full, 0);
+        __syncwarp();
+        if (it.info.z > 0 || it.info.w < BN) {             // keys that nobody sees
+          for (int r = lane >> 4; r < BN; r += 2)
+            if (r < it.info.z || r >= it.info.w)
+              *reinterpret_cast<uint4*>(sK + (lane >> 3 & 1) * PANEL + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          fence_async_proxy();
+          __syncwarp();
+        }
+        if (lane == 0) mbar_arrive(&sm->k_ready);
+        wait(&sm->v_full, 0);                              // landed before the CTA may exit, whatever the others do
       }
     } else if (warp == 1) {
       // ---------------------------------------------------------------- MMA issuer: the whole warp walks the loop, one elected lane
@@ -257,7 +281,8 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
       auto uniform = [](int v) { return __reduce_max_sync(0xffffffffu, v); };
       Walk walk(it);
       walk.u = uniform(walk.u);
-      walk.last = uniform(walk.last);
+      walk.first = uniform(walk.first);
+      walk.gaps = uniform(walk.gaps) != 0;
       // next unit's steps of 16 queries, or 0
       auto next = [&]() { return uniform(walk.next() ? (unit_rows(p, walk.u) + 15) >> 4 : 0); };
       uint32_t s_slot = 0, s_par = 0, k_slot = 0;      // Q ring: next unit's slot and parity for S^T, slot of the current dK
@@ -297,15 +322,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
       };
       int now = next();
       if (now) {
-        wwait(&sm->k_full, 0);
-        const int lo = uniform(it.info.z), hi = uniform(it.info.w);
-        if (lo > 0 || hi < BN) {             // keys that nobody sees
-          for (int r = lane >> 4; r < BN; r += 2)
-            if (r < lo || r >= hi)
-              *reinterpret_cast<uint4*>(sK + (lane >> 3 & 1) * PANEL + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-          fence_async_proxy();
-          __syncwarp();
-        }
+        wwait(&sm->k_ready, 0);
         int then = next();
         issue_s(now);
         wwait(&sm->v_full, 0);
@@ -343,8 +360,8 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
       // Warp 3 lets the writers go on only when warp 2 has noted the end of the unit before: no barrier gets a phase ahead.
       Walk walk(it);
       for (uint32_t i = 0; walk.next(); ++i) {
-        const int n = it.tile - walk.rec.x / BN, rank = n / p.parts;
-        int* turn = p.turns + ((long long)(n - rank * p.parts) * p.B * p.Hk + it.bhk) * p.nU + walk.u;
+        const int n = it.tile - __ldg(&it.units[walk.u].x) / BN, rank = MULTI ? p.by_parts.div(n) : n, part = MULTI ? n - rank * p.parts : 0;
+        int* turn = p.turns + ((long long)part * p.B * p.Hk + it.bhk) * p.nU + walk.u;
         if (warp == 3) {
           if (rank > 0) turn_wait(turn, rank, abort_flag, p.status);
           if (i > 0) wait(&sm->rows_seen, (i - 1) & 1);
@@ -363,11 +380,13 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     // something, else asynchronous 16-byte copies, eight threads per 128-byte half row, with zeros for the rows that do not.
     const bool is_q = warp < 8;
     const int lt = threadIdx.x & 127, r0 = 4 * (warp & 3) + (lane >> 3), chunk = lane & 7;      // rows r0 + 16 k
-    const int rt = lt / p.G, rg = lt - rt * p.G;
+    const int rt = p.by_G.div(lt), rg = lt - rt * p.G;
     const int2* rows = p.rows + (long long)mask_batch(p.Bm, it.b) * p.Sq;
     Walk walk(it);
     float sc = 0.f;
+    int least = 0;                             // smallest end of the unit's ranges (0: a row sees nothing)
     auto fetch = [&]() {
+      least = __ldg(&it.units[walk.u].w);
       const int tok = walk.u * p.tpt + rt;
       sc = is_q ? INFINITY : 0.f;                          // rows that see nothing: P = exp2(-inf) = 0
       if (lt < p.tpt * p.G && tok < p.Sq && __ldg(&rows[tok].y) > 0)
@@ -386,7 +405,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
       (is_q ? sm->lse2[slot] : sm->negD[g & 1])[lt] = sc;
       const int tok0 = walk.u * p.tpt;
       uint8_t* tile = is_q ? sQ + slot * TILE : sO;
-      if (walk.rec.w > 0) {
+      if (__builtin_expect(least > 0, 1)) {
         if (lt == 0) {
           const CUtensorMap* map = is_q ? &tmQ : &tmO;
           mbar_expect_tx(full, (uint32_t)(p.tpt * p.G * DH * 2));
@@ -403,11 +422,11 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         const Strides& s = is_q ? p.qs : p.dos;
         const __nv_bfloat16* base = (is_q ? p.q : p.d_o) + it.b * s.b + (long long)it.hk * p.G * s.h + chunk * 8;
         const uint32_t dst = smem_u32(tile) + r0 * 128 + ((chunk ^ (r0 & 7)) << 4);
-#pragma unroll 2
+#pragma unroll 1
         for (int k = 0; k < 8; ++k) {
-          const int r = r0 + 16 * k, tok = tok0 + r / p.G;
+          const int r = r0 + 16 * k, rk = p.by_G.div(r), tok = tok0 + rk;
           const bool ok = r < p.tpt * p.G && tok < p.Sq && __ldg(&rows[min(tok, p.Sq - 1)].y) > 0;
-          const __nv_bfloat16* row = ok ? base + tok * s.t + (r % p.G) * s.h : base;
+          const __nv_bfloat16* row = ok ? base + tok * s.t + (r - rk * p.G) * s.h : base;
           cp_async16(dst + k * 2048, row, ok ? 16u : 0u);
           cp_async16(dst + k * 2048 + PANEL, row + 64, ok ? 16u : 0u);
         }
@@ -431,8 +450,9 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     float* acc_head = p.dq_acc + quad * 32 + (lane & ~3) + (long long)it.bhk * p.Sq * p.G * DH;
     Walk walk(it);
     for (uint32_t g = 0; walk.next(); ++g) {
-      const int rows = unit_rows(p, walk.u), n = it.tile - walk.rec.x / BN;
-      float* acc = acc_head + ((long long)(n % p.parts) * all_rows + (long long)walk.u * p.tpt * p.G) * DH;
+      const int rows = unit_rows(p, walk.u), n = it.tile - __ldg(&it.units[walk.u].x) / BN;
+      float* acc = acc_head + (long long)walk.u * p.tpt * p.G * DH;
+      if constexpr (MULTI) acc += (long long)(n - p.by_parts.div(n) * p.parts) * all_rows * DH;
       wait(&sm->dq_full, g & 1);
       tc_fence_after();
       // everything out of TMEM first: the next dP^T waits for these columns
@@ -455,7 +475,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
           }
       };
       wait(&sm->turn_ok, g & 1);
-      if (n < p.parts)
+      if (n < (MULTI ? p.parts : 1))
         write_rows([](float* to, float a, float b, float c, float d) { *reinterpret_cast<float4*>(to) = make_float4(a, b, c, d); });
       else
         write_rows([](float* to, float a, float b, float c, float d) { red_add_v4(to, a, b, c, d); });
@@ -493,12 +513,13 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         const float2* lse2 = reinterpret_cast<const float2*>(sm->lse2[slot] + 64 * half) + (lane & 3);
         const float2* negD = reinterpret_cast<const float2*>(sm->negD[g & 1] + 64 * half) + (lane & 3);
         // Ranges relative to the tile, in bytes {lo, hi} of queries 2 lane and 2 lane + 1 of this half, if some query needs them.
-        const bool masked = walk.rec.z > it.key0 || walk.rec.w < it.key0 + BN;
-        uint32_t bounds = 0;
-        if (masked) {
+        const bool masked = walk.u < it.run.y || walk.u >= it.run.z;
+        uint32_t bounds = 0x80008000u;                 // (everything)
+        if (__builtin_expect(masked, 0)) {
+          bounds = 0;
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int rw = 64 * half + 2 * lane + e, tok = walk.u * p.tpt + rw / p.G;
+            const int rw = 64 * half + 2 * lane + e, tok = walk.u * p.tpt + p.by_G.div(rw);
             if (rw < p.tpt * p.G && tok < p.Sq) {
               const int2 s = __ldg(rows + tok);
               bounds |= (uint32_t)(min(max(s.x - it.key0, 0), BN) | min(max(s.y - it.key0, 0), BN) << 8) << (16 * e);
@@ -517,55 +538,78 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         tmem_ld_16x256_x8(st_t, pv[0]);
         tmem_ld_16x256_x8(st_t + ROW16, pv[1]);
         tmem_ld_wait();
-        // a pair of queries (of word w) and key + 8 k
-        auto weigh = [&](uint32_t& a, uint32_t& b, const float2& lse, uint32_t w, int k, bool mask) {
-          float x0, x1, s0 = 1.f, s1 = 1.f;
-          if constexpr (CAP) {
-            float e0, e1;
-            mul2(e0, e1, __uint_as_float(a), __uint_as_float(b), p.scale_log2, p.scale_log2);
-            e0 = rcp(1.0f + ex2(e0));
-            e1 = rcp(1.0f + ex2(e1));
-            s0 = 4.0f * fmaf(-e0, e0, e0);             // 1 - tanh^2
-            s1 = 4.0f * fmaf(-e1, e1, e1);
-            fma2(x0, x1, e0, e1, -2.0f * p.cap_log2, -2.0f * p.cap_log2, p.cap_log2 - lse.x, p.cap_log2 - lse.y);
+        // How a pair of scores becomes weights: plainly, capped by the polynomial, capped the long way.
+        enum How { kAsIs, kShort, kLong };
+        auto weigh = [&](auto how, uint32_t& a, uint32_t& b, const float2& lse) {
+          constexpr int H = decltype(how)::value;
+          float x0 = __uint_as_float(a), x1 = __uint_as_float(b), s0, s1;
+          if constexpr (H == kAsIs) {
+            fma2(x0, x1, x0, x1, p.scale_log2, p.scale_log2, -lse.x, -lse.y);
+          } else if constexpr (H == kShort) {
+            float z0, z1, r0 = p.cap.p[4], r1 = p.cap.p[4];
+            mul2(z0, z1, x0, x1, x0, x1);
+#pragma unroll
+            for (int k = 3; k >= 0; --k) fma2(r0, r1, r0, r1, z0, z1, p.cap.p[k], p.cap.p[k]);
+            mul2(x0, x1, r0, r1, x0, x1);
+            mul2(s0, s1, x0, x1, x0, x1);
+            fma2(s0, s1, s0, s1, p.cap_inv2, p.cap_inv2, 1.0f, 1.0f);
+            add2(x0, x1, x0, x1, -lse.x, -lse.y);
           } else {
-            fma2(x0, x1, __uint_as_float(a), __uint_as_float(b), p.scale_log2, p.scale_log2, -lse.x, -lse.y);
-          }
-          if (mask) {
-            const int at = key + 8 * k;
-            const int lo0 = w & 0xff, hi0 = w >> 8 & 0xff, lo1 = w >> 16 & 0xff, hi1 = w >> 24;
-            if (at < lo0 || at >= hi0) x0 = -INFINITY;
-            if (at < lo1 || at >= hi1) x1 = -INFINITY;
+            const float r0 = rcp(1.0f + ex2(x0 * p.cap.twice_a_log2)), r1 = rcp(1.0f + ex2(x1 * p.cap.twice_a_log2));
+            s0 = 4.0f * fmaf(-r0, r0, r0);
+            s1 = 4.0f * fmaf(-r1, r1, r1);
+            x0 = fmaf(r0, -2.0f * p.cap.c, p.cap.c - lse.x);
+            x1 = fmaf(r1, -2.0f * p.cap.c, p.cap.c - lse.y);
           }
           x0 = ex2(x0);
           x1 = ex2(x1);
           const uint32_t pair = pack_bf16(x0, x1);
-          if (CAP) mul2(x0, x1, x0, x1, s0, s1);
+          if constexpr (H != kAsIs) mul2(x0, x1, x0, x1, s0, s1);
           a = __float_as_uint(x0);
           b = __float_as_uint(x1);
           return pair;
         };
-        auto weights = [&](bool mask) {
+        // (words of the pairs; pairs that are not seen: zeros, by the bounds of their two queries)
+        auto weights = [&](auto how, auto mask) {
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             uint32_t pk[2][8];
 #pragma unroll
             for (int jj = 0; jj < 4; ++jj) {
               const int j = 4 * c + jj;
-              const uint32_t w = mask ? __shfl_sync(0xffffffffu, bounds, 4 * j + (lane & 3)) : 0u;
+              uint32_t w = 0;
+              if constexpr (decltype(mask)::value) w = __shfl_sync(0xffffffffu, bounds, 4 * j + (lane & 3));
 #pragma unroll
               for (int rh = 0; rh < 2; ++rh)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) pk[rh][2 * jj + e] = weigh(pv[rh][4 * j + 2 * e], pv[rh][4 * j + 2 * e + 1], l[j], w, 2 * rh + e, mask);
+                for (int e = 0; e < 2; ++e) {
+                  uint32_t &a = pv[rh][4 * j + 2 * e], &b = pv[rh][4 * j + 2 * e + 1];
+                  uint32_t pair = weigh(how, a, b, l[j]);
+                  if constexpr (decltype(mask)::value) {
+                    const int at = key + 16 * rh + 8 * e;
+                    if (at < (int)(w & 0xff) || at >= (int)(w >> 8 & 0xff)) { a = 0u; pair &= 0xffff0000u; }
+                    if (at < (int)(w >> 16 & 0xff) || at >= (int)(w >> 24)) { b = 0u; pair &= 0xffffu; }
+                  }
+                  pk[rh][2 * jj + e] = pair;
+                }
             }
             tmem_st_16x128_x4(st_t + 16 * c, pk[0]);
             tmem_st_16x128_x4(st_t + ROW16 + 16 * c, pk[1]);
           }
         };
-        // (the masked tiles' code out of the way: beside the other roles' it does not fit the instruction cache)
+        using std::integral_constant;
+        // (the rare cases' code out of the way: beside the other roles' it does not fit the instruction cache)
         if constexpr (CAP) {
-          if (__builtin_expect(masked, 0)) weights(true);
-          else weights(false);
+          float m0 = 0.f, m1 = 0.f;
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            m0 = max3(m0, fabsf(__uint_as_float(pv[0][i])), fabsf(__uint_as_float(pv[0][i + 1])));
+            m1 = max3(m1, fabsf(__uint_as_float(pv[1][i])), fabsf(__uint_as_float(pv[1][i + 1])));
+          }
+          if (__builtin_expect(!masked && __all_sync(0xffffffffu, fmaxf(m0, m1) <= p.cap.most), 1))
+            weights(integral_constant<int, kShort>{}, std::false_type{});
+          else
+            weights(integral_constant<int, kLong>{}, std::true_type{});
         } else {
           if (__builtin_expect(masked, 0)) {
 #pragma unroll
@@ -580,7 +624,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
               }
             }
           }
-          weights(false);
+          weights(integral_constant<int, kAsIs>{}, std::false_type{});
         }
         // negD of this unit (dV needs the dO rows anyway; asked before dV can run, so that the barrier cannot be a phase ahead)
         wait(&sm->do_full, g & 1);
@@ -671,32 +715,30 @@ range_cast_kernel(const Params p, __nv_bfloat16* __restrict__ dq, const Strides 
   // this lane's output columns 4 lane .. 4 lane + 3 sit at positions at, at + 4, at + 8, at + 12: one line of the row
   const int at = (lane & ~7) * 4 + 16 * (lane & 1) + ((lane & 7) >> 1);
   const int per = p.Sq * p.G;
-  const long long all_rows = (long long)p.B * p.Hk * per;
-  for (long long row0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * R; row0 < all_rows; row0 += (long long)gridDim.x * 8 * R) {
+  const int all_rows = p.B * p.Hk * per;       // (at most 2^30)
+  for (int row0 = (blockIdx.x * 8 + (threadIdx.x >> 5)) * R; row0 < all_rows; row0 += gridDim.x * 8 * R) {
     float4 v[R];
     long long to[R];
     int parts[R];
     int most = 0;
 #pragma unroll
     for (int n = 0; n < R; ++n) {
-      const long long row = min(row0 + n, all_rows - 1);
-      const int bhk = (int)((unsigned)row / (unsigned)per), r = (int)(row - (long long)bhk * per), tok = r / p.G, g = r - tok * p.G;
-      const int b = bhk / p.Hk, hk = bhk - b * p.Hk, bm = mask_batch(p.Bm, b);
+      const int row = min(row0 + n, all_rows - 1), bhk = p.by_rows.div(row), r = row - bhk * per, tok = p.by_G.div(r), g = r - tok * p.G;
+      const int b = p.by_Hk.div(bhk), hk = bhk - b * p.Hk, bm = mask_batch(p.Bm, b);
       to[n] = b * dqs.b + tok * dqs.t + (long long)(hk * p.G + g) * dqs.h + lane * 4;
-      const int4 u = __ldg(p.units + (long long)bm * p.nU + tok / p.tpt);
-      parts[n] = __ldg(&p.rows[(long long)bm * p.Sq + tok].y) > 0 ? min(p.parts, (u.y + BN - 1) / BN - u.x / BN) : 0;
+      const int4 u = __ldg(p.units + (long long)bm * p.nU + p.by_tpt.div(tok));
+      const int seen = __ldg(&p.rows[(long long)bm * p.Sq + tok].y);
+      const float* from = p.dq_acc + (long long)row * DH + at;      // (read ahead of the answer whether the row has any)
+      v[n] = make_float4(__ldg(from), __ldg(from + 4), __ldg(from + 8), __ldg(from + 12));
+      parts[n] = seen > 0 ? min(p.parts, (u.y + BN - 1) / BN - u.x / BN) : 0;
       most = max(most, parts[n]);
-      v[n] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (parts[n] > 0) {
-        const float* from = p.dq_acc + row * DH + at;
-        v[n] = make_float4(__ldg(from), __ldg(from + 4), __ldg(from + 8), __ldg(from + 12));
-      }
+      if (parts[n] == 0) v[n] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     for (int k = 1; k < most; ++k) {
 #pragma unroll
       for (int n = 0; n < R; ++n)
         if (k < parts[n]) {
-          const float* from = p.dq_acc + (k * all_rows + min(row0 + n, all_rows - 1)) * DH + at;
+          const float* from = p.dq_acc + ((long long)k * all_rows + min(row0 + n, all_rows - 1)) * DH + at;
           v[n].x += __ldg(from); v[n].y += __ldg(from + 4); v[n].z += __ldg(from + 8); v[n].w += __ldg(from + 12);
         }
     }
@@ -720,12 +762,14 @@ int tc_range_bwd(const RDims& D, const Plan& plan, const BwdArgs& a, void* dq, c
   if (items > (long long)INT32_MAX - 4096) return VMOBA_ERR_SHAPE;
   Params p;
   p.B = D.B; p.Hk = D.Hk; p.G = D.G; p.Sq = D.Sq; p.Sk = D.Sk; p.Bm = D.Bm; p.tpt = D.tpt; p.nU = D.nU; p.nK = D.nK;
-  p.rows = plan.rows; p.units = plan.units; p.keys = plan.keys;
+  p.rows = plan.rows; p.units = plan.units; p.keys = plan.keys; p.runs = plan.runs;
+  p.by_G = FastDiv(D.G); p.by_tpt = FastDiv(D.tpt); p.by_rows = FastDiv(D.rows); p.by_Hk = FastDiv(D.Hk); p.by_parts = FastDiv(a.parts);
   p.q = (const __nv_bfloat16*)a.q; p.d_o = (const __nv_bfloat16*)a.d_o; p.qs = a.qs; p.dos = a.dos;
   p.lse = a.lse; p.Dv = a.Dv;
   p.scale = D.scale;
-  p.scale_log2 = D.cap > 0.f ? 2.0f * D.scale * LOG2E / D.cap : D.scale * LOG2E;
-  p.cap_log2 = D.cap * LOG2E;
+  p.scale_log2 = D.scale * LOG2E;
+  p.cap = make_cap(D);
+  p.cap_inv2 = D.cap > 0.f ? -1.0f / (p.cap.c * p.cap.c) : 0.f;
   p.dk = (__nv_bfloat16*)a.dk; p.dv = (__nv_bfloat16*)a.dv; p.dks = a.dks; p.dvs = a.dvs;
   auto whole = [](const void* x, const Strides& s) {
     return reinterpret_cast<uintptr_t>(x) % 32 == 0 && s.b % 16 == 0 && s.t % 16 == 0 && s.h % 16 == 0;
@@ -739,7 +783,8 @@ int tc_range_bwd(const RDims& D, const Plan& plan, const BwdArgs& a, void* dq, c
   if (!make_tmap_keys(&tmK, a.k, D, a.ks) || !make_tmap_keys(&tmV, a.v, D, a.vs) || !make_tmap_units(&tmQ, a.q, D, a.qs) ||
       !make_tmap_units(&tmO, a.d_o, D, a.dos))
     return VMOBA_ERR_CUDA;
-  auto kernel = D.cap > 0.f ? attn_range_bwd_kernel<true> : attn_range_bwd_kernel<false>;
+  auto kernel = D.cap > 0.f ? (a.parts > 1 ? attn_range_bwd_kernel<true, true> : attn_range_bwd_kernel<true, false>)
+                            : (a.parts > 1 ? attn_range_bwd_kernel<false, true> : attn_range_bwd_kernel<false, false>);
   VMOBA_CUDA_OK(allow_smem(kernel, (int)SMEM_BYTES));
   launch_kernel(early, kernel, (unsigned)items, THREADS, SMEM_BYTES, st, tmK, tmV, tmQ, tmO, p);
   const long long all_rows = (long long)D.B * D.Hk * D.rows;

@@ -59,13 +59,6 @@ struct Smem {
 constexpr size_t SMEM_BYTES = (2 /*Q*/ + KST + VST) * TILE + sizeof(Smem) + 32;
 static_assert(SMEM_BYTES <= 232448, "range forward: shared memory");
 
-// Capped scores in the exp2 domain: c' tanh(a s), c' = cap * log2 e, a = scale / cap.
-struct Cap {
-  float c, twice_a_log2;         // c', 2 a log2 e
-  float most;                    // |s| up to this: by the polynomial (-1: none)
-  float p[5];                    // its coefficients of s, s^3, ...
-};
-
 struct Params {
   int B, Hk, G, Sq, Sk, Bm, tpt, nU, nI, splits, n_items;
   FastDiv by_splits, by_nI, by_Hk, by_G;
@@ -677,9 +670,9 @@ bool make_tmap_units(CUtensorMap* map, const void* base, const RDims& D, const S
 
 // The polynomial's coefficients with the factors of score and result folded in.  Where that leaves fp32's range (caps of more than some
 // hundred times the scale's usual) every score takes the long way.
-static tcf::Cap make_cap(const RDims& D) {
+Cap make_cap(const RDims& D) {
   static const double k[5] = {0.9999972283, -0.3332307648, 0.1322609162, -0.04928044707, 0.01231883178};
-  tcf::Cap c = {};
+  Cap c = {};
   if (!(D.cap > 0.f)) return c;
   const double a = (double)D.scale / D.cap, top = (double)D.cap * 1.4426950408889634;
   c.c = (float)top;
