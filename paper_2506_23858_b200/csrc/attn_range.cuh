@@ -58,6 +58,7 @@ struct Cap {
   float c, twice_a_log2;         // c', 2 a log2 e
   float most;                    // |s| up to this: by the polynomial (-1: none)
   float p[5];                    // its coefficients of s, s^3, ...
+  float q[4];                    // of one with a term less, off by 3.6e-6: enough where only weights are made that bf16 rounds (2^-9)
 };
 
 Cap make_cap(const RDims& D);      // attn_range_fwd.cu

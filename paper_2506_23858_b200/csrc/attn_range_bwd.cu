@@ -6,7 +6,7 @@
 //     S^T = K Q^T;  P^T = exp2(c S^T - lse), capped exp2(c' tanh - lse), 0 outside the range;  dV += P^T dO
 //     dP^T = V dO^T;  dS^T = P^T (dP^T - D) (1 - tanh^2);  dK += dS^T Q;  dQ^T = K^T dS^T, added into an fp32 accumulator
 // The slope 1 - tanh^2 is taken into the fp32 weights that the second step keeps, at no register.  tanh comes from the forward's polynomial
-// where a warp's scores allow, else from r = 1 / (1 + exp(2 x)): slope 4 r (1 - r).
+// where a warp's scores allow, else from 1 - 2 / (1 + exp(2 x)).
 //
 // dQ of a unit is added key tile after key tile, so that the backward repeats bit for bit: a counter per unit says how many of the
 // tiles of its hull (which are consecutive) have been added; the first one stores.  A tile waits for lower tickets only.  Units go
@@ -18,7 +18,6 @@
 // Rows of a unit that see nothing are brought in as zeros (asynchronous copies instead of the TMA tile), keys that no query sees are
 // cleared in K: 0 times what they hold would not be 0 if it is not finite.
 #include <algorithm>
-#include <type_traits>
 
 #include "attn_range.cuh"
 #include "sm100.cuh"
@@ -512,12 +511,24 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
       for (uint32_t g = 0; walk.next(); ++g) {
         const float2* lse2 = reinterpret_cast<const float2*>(sm->lse2[slot] + 64 * half) + (lane & 3);
         const float2* negD = reinterpret_cast<const float2*>(sm->negD[g & 1] + 64 * half) + (lane & 3);
-        // Ranges relative to the tile, in bytes {lo, hi} of queries 2 lane and 2 lane + 1 of this half, if some query needs them.
-        const bool masked = walk.u < it.run.y || walk.u >= it.run.z;
-        uint32_t bounds = 0x80008000u;                 // (everything)
+        // What the unit's queries see of the tile.  Mostly all of it, or all the same keys of it ([lo, hi): a clip's or a frame's end):
+        // then a thread masks by its four keys.  Else (apart) bounds: bytes {lo, hi} of queries 2 lane and 2 lane + 1 of this half.
+        // (Every unit of a clip that begins inside a tile is masked there, and the clip's other tiles add dQ behind that one: with
+        // bounds read and compared for each of them 13K tokens of two clips, capped, took 1406 us, so 1335.  The record brought by
+        // the loaders, through shared memory: 1345, and 5 % more where nothing is masked.)
+        const bool masked = walk.u < it.run.y || walk.u >= it.run.z, stale = CAP && unit_rows(p, walk.u) <= QU - 16;
+        bool apart = stale;
+        int lo = 0, hi = BN;
         if (__builtin_expect(masked, 0)) {
-          bounds = 0;
-#pragma unroll
+          const int4 u = __ldg(it.units + walk.u);
+          auto rel = [&](int v) { return min(max(v - it.key0, 0), BN); };
+          lo = rel(u.x);
+          hi = rel(u.w);
+          apart = apart || lo != rel(u.z) || hi != rel(u.y);
+        }
+        uint32_t bounds = 0;
+        if (__builtin_expect(apart, 0)) {
+#pragma unroll 1
           for (int e = 0; e < 2; ++e) {
             const int rw = 64 * half + 2 * lane + e, tok = walk.u * p.tpt + p.by_G.div(rw);
             if (rw < p.tpt * p.G && tok < p.Sq) {
@@ -538,93 +549,95 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         tmem_ld_16x256_x8(st_t, pv[0]);
         tmem_ld_16x256_x8(st_t + ROW16, pv[1]);
         tmem_ld_wait();
-        // How a pair of scores becomes weights: plainly, capped by the polynomial, capped the long way.
-        enum How { kAsIs, kShort, kLong };
-        auto weigh = [&](auto how, uint32_t& a, uint32_t& b, const float2& lse) {
-          constexpr int H = decltype(how)::value;
-          float x0 = __uint_as_float(a), x1 = __uint_as_float(b), s0, s1;
-          if constexpr (H == kAsIs) {
-            fma2(x0, x1, x0, x1, p.scale_log2, p.scale_log2, -lse.x, -lse.y);
-          } else if constexpr (H == kShort) {
-            float z0, z1, r0 = p.cap.p[4], r1 = p.cap.p[4];
-            mul2(z0, z1, x0, x1, x0, x1);
+        // scores outside their query's range get a value
+        auto mask = [&](uint32_t value) {
+          if (apart) {
 #pragma unroll
-            for (int k = 3; k >= 0; --k) fma2(r0, r1, r0, r1, z0, z1, p.cap.p[k], p.cap.p[k]);
-            mul2(x0, x1, r0, r1, x0, x1);
-            mul2(s0, s1, x0, x1, x0, x1);
-            fma2(s0, s1, s0, s1, p.cap_inv2, p.cap_inv2, 1.0f, 1.0f);
-            add2(x0, x1, x0, x1, -lse.x, -lse.y);
-          } else {
-            const float r0 = rcp(1.0f + ex2(x0 * p.cap.twice_a_log2)), r1 = rcp(1.0f + ex2(x1 * p.cap.twice_a_log2));
-            s0 = 4.0f * fmaf(-r0, r0, r0);
-            s1 = 4.0f * fmaf(-r1, r1, r1);
-            x0 = fmaf(r0, -2.0f * p.cap.c, p.cap.c - lse.x);
-            x1 = fmaf(r1, -2.0f * p.cap.c, p.cap.c - lse.y);
-          }
-          x0 = ex2(x0);
-          x1 = ex2(x1);
-          const uint32_t pair = pack_bf16(x0, x1);
-          if constexpr (H != kAsIs) mul2(x0, x1, x0, x1, s0, s1);
-          a = __float_as_uint(x0);
-          b = __float_as_uint(x1);
-          return pair;
-        };
-        // (words of the pairs; pairs that are not seen: zeros, by the bounds of their two queries)
-        auto weights = [&](auto how, auto mask) {
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t w = __shfl_sync(0xffffffffu, bounds, 4 * j + (lane & 3));
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            uint32_t pk[2][8];
+              for (int e = 0; e < 2; ++e) {          // query e of the pair
+                const int from = w >> (16 * e) & 0xff, n = (int)(w >> (16 * e + 8) & 0xff) - from, at = key - from;
 #pragma unroll
-            for (int jj = 0; jj < 4; ++jj) {
-              const int j = 4 * c + jj;
-              uint32_t w = 0;
-              if constexpr (decltype(mask)::value) w = __shfl_sync(0xffffffffu, bounds, 4 * j + (lane & 3));
-#pragma unroll
-              for (int rh = 0; rh < 2; ++rh)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                  uint32_t &a = pv[rh][4 * j + 2 * e], &b = pv[rh][4 * j + 2 * e + 1];
-                  uint32_t pair = weigh(how, a, b, l[j]);
-                  if constexpr (decltype(mask)::value) {
-                    const int at = key + 16 * rh + 8 * e;
-                    if (at < (int)(w & 0xff) || at >= (int)(w >> 8 & 0xff)) { a = 0u; pair &= 0xffff0000u; }
-                    if (at < (int)(w >> 16 & 0xff) || at >= (int)(w >> 24)) { b = 0u; pair &= 0xffffu; }
-                  }
-                  pk[rh][2 * jj + e] = pair;
-                }
+                for (int k = 0; k < 4; ++k)          // key + 8 k
+                  if ((unsigned)(at + 8 * k) >= (unsigned)n) pv[k >> 1][4 * j + 2 * (k & 1) + e] = value;
+              }
             }
-            tmem_st_16x128_x4(st_t + 16 * c, pk[0]);
-            tmem_st_16x128_x4(st_t + ROW16 + 16 * c, pk[1]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const bool out = key + 8 * k < lo || key + 8 * k >= hi;
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  if (out) pv[k >> 1][4 * j + 2 * (k & 1) + e] = value;
+            }
           }
         };
-        using std::integral_constant;
-        // (the rare cases' code out of the way: beside the other roles' it does not fit the instruction cache)
+        // (the rare cases' code is out of the way and short: beside the other roles' it does not fit the instruction cache)
         if constexpr (CAP) {
+          // scores -> c' tanh.  What no product has written (queries beyond the unit's) has no say in how the others are capped; -10^15: a weight
+          // of 0 and a finite slope
+          if (__builtin_expect(stale, 0)) mask(0u);
           float m0 = 0.f, m1 = 0.f;
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
             m0 = max3(m0, fabsf(__uint_as_float(pv[0][i])), fabsf(__uint_as_float(pv[0][i + 1])));
             m1 = max3(m1, fabsf(__uint_as_float(pv[1][i])), fabsf(__uint_as_float(pv[1][i + 1])));
           }
-          if (__builtin_expect(!masked && __all_sync(0xffffffffu, fmaxf(m0, m1) <= p.cap.most), 1))
-            weights(integral_constant<int, kShort>{}, std::false_type{});
-          else
-            weights(integral_constant<int, kLong>{}, std::true_type{});
-        } else {
-          if (__builtin_expect(masked, 0)) {
+          if (__builtin_expect(__all_sync(0xffffffffu, fmaxf(m0, m1) <= p.cap.most), 1)) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const uint32_t w = __shfl_sync(0xffffffffu, bounds, 4 * j + (lane & 3));
+            for (int rh = 0; rh < 2; ++rh)
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {          // query e of the pair
-                const int lo = w >> (16 * e) & 0xff, n = (int)(w >> (16 * e + 8) & 0xff) - lo, at = key - lo;
+              for (int i = 0; i < 32; i += 2) {
+                float x0 = __uint_as_float(pv[rh][i]), x1 = __uint_as_float(pv[rh][i + 1]), z0, z1, r0 = p.cap.q[3], r1 = p.cap.q[3];
+                mul2(z0, z1, x0, x1, x0, x1);
 #pragma unroll
-                for (int k = 0; k < 4; ++k)          // key + 8 k
-                  if ((unsigned)(at + 8 * k) >= (unsigned)n) pv[k >> 1][4 * j + 2 * (k & 1) + e] = 0xff800000u;
+                for (int k = 2; k >= 0; --k) fma2(r0, r1, r0, r1, z0, z1, p.cap.q[k], p.cap.q[k]);
+                mul2(x0, x1, r0, r1, x0, x1);
+                pv[rh][i] = __float_as_uint(x0);
+                pv[rh][i + 1] = __float_as_uint(x1);
               }
-            }
+          } else {
+#pragma unroll
+            for (int rh = 0; rh < 2; ++rh)
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                pv[rh][i] = __float_as_uint(fmaf(rcp(1.0f + ex2(__uint_as_float(pv[rh][i]) * p.cap.twice_a_log2)), -2.0f * p.cap.c, p.cap.c));
           }
-          weights(integral_constant<int, kAsIs>{}, std::false_type{});
+          if (__builtin_expect(masked || stale, 0)) mask(0xd8635fa9u);
+        } else {
+          if (__builtin_expect(masked, 0)) mask(0xff800000u);
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t pk[2][8];
+#pragma unroll
+          for (int jj = 0; jj < 4; ++jj) {
+            const int j = 4 * c + jj;
+#pragma unroll
+            for (int rh = 0; rh < 2; ++rh)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                float x0 = __uint_as_float(pv[rh][4 * j + 2 * e]), x1 = __uint_as_float(pv[rh][4 * j + 2 * e + 1]), s0, s1;
+                if constexpr (CAP) {                 // the slope 1 - (t / c')^2
+                  mul2(s0, s1, x0, x1, x0, x1);
+                  fma2(s0, s1, s0, s1, p.cap_inv2, p.cap_inv2, 1.0f, 1.0f);
+                  add2(x0, x1, x0, x1, -l[j].x, -l[j].y);
+                } else {
+                  fma2(x0, x1, x0, x1, p.scale_log2, p.scale_log2, -l[j].x, -l[j].y);
+                }
+                x0 = ex2(x0);
+                x1 = ex2(x1);
+                pk[rh][2 * jj + e] = pack_bf16(x0, x1);
+                if constexpr (CAP) mul2(x0, x1, x0, x1, s0, s1);
+                pv[rh][4 * j + 2 * e] = __float_as_uint(x0);
+                pv[rh][4 * j + 2 * e + 1] = __float_as_uint(x1);
+              }
+          }
+          tmem_st_16x128_x4(st_t + 16 * c, pk[0]);
+          tmem_st_16x128_x4(st_t + ROW16 + 16 * c, pk[1]);
         }
         // negD of this unit (dV needs the dO rows anyway; asked before dV can run, so that the barrier cannot be a phase ahead)
         wait(&sm->do_full, g & 1);

@@ -325,3 +325,21 @@ def test_norm_rotary_and_attention_on_packed_clips(dtype, d):
         check(got, dx, mag, 5e-6, "dx")
         check(gw, *wref, 1.3e-5, "dw")
     assert bool((o[:, 192:] == 0).all()) and bool((dv[:, 192:] == 0).all())
+
+
+@pytest.mark.parametrize("kind", [("bf16", 64), ("bf16", 128)], ids=lambda k: f"{k[0]}_{k[1]}")
+@pytest.mark.parametrize("i", [1, 4, 6, 10, 13])
+def test_results_do_not_depend_on_what_ran_before(i, kind):
+    """Between two runs others leave large scores and NaN in what registers, shared and tensor memory hold: units of fewer rows than a
+    tile, tiles of fewer keys and groups that do not divide one keep their bits (how a capped score is worked out is a warp's choice)."""
+    c = CASES[i]
+    dtype, d = kind
+    ranges, cap = c["r"](), 4.0
+    shape, op, host, dev, place = make(c["B"], c["Sq"], c["Sk"], c["h"], c["hk"], d, dtype, ranges, cap, c.get("layout", "raster"), seed=i)
+    full = torch.tensor([[[0, 640]] * 640], dtype=torch.int32)
+    others = [make(2, 640, 640, 80, 80, d, dtype, full, cap, seed=50 + k, gain=g) for k, g in enumerate((100.0, float("nan")))]
+    o, grads = run(op, dev, place, host)
+    for _, other, oh, odev, oplace in others:
+        run(other, odev, oplace, oh)
+        o2, grads2 = run(op, dev, place, host)
+        assert torch.equal(o2, o) and all(torch.equal(a, b) for a, b in zip(grads, grads2))
