@@ -64,8 +64,63 @@ __device__ __forceinline__ int2 item_hull(const int4* units, int u0, int n) {
   return h;
 }
 
+// Few items: their key ranges are cut into pieces of equally many tiles, as long as the SMs allow.  The length is the one of 32 (a whole
+// number of rounds over the SMs if every item were a multiple of it) with the smallest time of its last round; a piece costs a fixed time and
+// its rows' trip through memory, `fixed` tiles.  One block.
+constexpr int kSms = 148;                      // (of the design: plan and scratch are functions of the shape and the ranges alone)
+constexpr int kFewItems = 4 * kSms;
+__device__ __forceinline__ void plan_pieces(const Plan& plan, const RDims& D) {
+  __shared__ int tiles[kFewItems], sums[32], length, biggest;
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5, n = D.Bm * D.nI, per = D.tc ? 2 : 1;      // (n < kFewItems)
+  if (t == 0) biggest = 1;
+  __syncthreads();
+  int mine = 0;
+  if (t < n) {
+    const int bm = t / D.nI, u0 = (t - bm * D.nI) * per;
+    const int2 h = item_hull(plan.units + (long long)bm * D.nU, u0, min(per, D.nU - u0));
+    mine = max((h.y - h.x + D.TR - 1) / D.TR, 1);
+    tiles[t] = mine;
+    atomicMax(&biggest, mine);
+  }
+  const int total = __reduce_add_sync(0xffffffffu, mine);      // (of the warp)
+  if (lane == 0) sums[warp] = total;
+  __syncthreads();
+  if (warp == 0) {
+    const long long all = (long long)__reduce_add_sync(0xffffffffu, sums[lane]) * D.reps;
+    const float fixed = D.tc ? 1.5f + 2.0f * min(D.rows, 256) / 256.0f : 0.5f;
+    const int len = max(max((int)((all + (long long)kSms * (lane + 1) - 1) / ((long long)kSms * (lane + 1))), (biggest + D.smax - 1) / D.smax), 1);
+    long long pieces = 0;
+    for (int i = 0; i < n; ++i) pieces += (tiles[i] + len - 1) / len;
+    const float cost = (float)((pieces * D.reps + kSms - 1) / kSms) * ((float)len + fixed);
+    float best = cost;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) best = fminf(best, __shfl_xor_sync(0xffffffffu, best, o));
+    const int who = __ffs(__ballot_sync(0xffffffffu, cost == best)) - 1;
+    if (lane == who) length = len;
+  }
+  __syncthreads();
+  const int len = length, count = t < n ? (mine + len - 1) / len : 0;
+  int before = count;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, before, o);
+    if (lane >= o) before += x;
+  }
+  if (lane == 31) sums[warp] = before;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) before += sums[w];
+  if (t < n) {
+    plan.pieces[t] = count;
+    for (int k = 0; k < count; ++k) plan.work[before - count + k] = make_int4(t / D.nI, t % D.nI, k * len, k);
+  }
+  if (t == 1023) {
+    plan.head[0] = before;
+    plan.head[1] = len;
+  }
+}
+
 // The first Bm blocks put a sample's items in order (bins of equal width by the number of keys, the fullest first; inside a bin in any
-// order, which no result depends on), the others walk the key tiles, a warp each.
+// order, which no result depends on), the next one cuts few items into pieces, the others walk the key tiles, a warp each.
 constexpr int kBins = 1024;
 __global__ void __launch_bounds__(1024)
 plan_tiles_kernel(Plan plan, RDims D) {
@@ -100,8 +155,12 @@ plan_tiles_kernel(Plan plan, RDims D) {
     for (int i = threadIdx.x; i < D.nI; i += 1024) order[atomicAdd(&bin[bin_of(i)], 1)] = i;
     return;
   }
-  const long long n = (long long)D.Bm * D.nK, warps = (long long)(gridDim.x - D.Bm) * 32;
-  for (long long w = (long long)(blockIdx.x - D.Bm) * 32 + warp; w < n; w += warps) {
+  if ((int)blockIdx.x == D.Bm) {
+    if (D.smax > 1) plan_pieces(plan, D);
+    return;
+  }
+  const long long n = (long long)D.Bm * D.nK, warps = (long long)(gridDim.x - D.Bm - 1) * 32;
+  for (long long w = (long long)(blockIdx.x - D.Bm - 1) * 32 + warp; w < n; w += warps) {
     const long long bm = w / D.nK;
     const int t = (int)(w - bm * D.nK);
     const int4* units = plan.units + bm * D.nU;
@@ -184,16 +243,28 @@ range_fwd_kernel(const RDims D, const Plan plan, const FwdArgs a) {
   float* Ps = KVs + kTileFloats<DH>;
   __shared__ UnitRows rows;
   const int t = threadIdx.x, ty = t >> 4, tx = t & 15;
-  const long long n_items = (long long)D.B * D.Hk * D.nI * a.splits, all_rows = (long long)D.B * D.Hk * D.rows;
+  const bool cut = D.smax > 1;
+  const long long n_items = cut ? (long long)plan.head[0] * D.reps : (long long)D.B * D.Hk * D.nI, all_rows = (long long)D.B * D.Hk * D.rows;
   for (long long item = blockIdx.x; item < n_items; item += gridDim.x) {
-    const int split = (int)(item % a.splits);
-    const long long m = item / a.splits;
-    const int bhk = (int)(m / D.nI), b = bhk / D.Hk, hk = bhk - b * D.Hk;
-    const int u = plan.order[(long long)mask_batch(D.Bm, b) * D.nI + (m - (long long)bhk * D.nI)];
+    int b, hk, u, piece = 0, first = 0, last = INT32_MAX;
+    if (cut) {
+      const int4 w = plan.work[item / D.reps];
+      const int rep = (int)(item % D.reps);
+      b = D.Bm > 1 ? w.x : rep / D.Hk;
+      hk = D.Bm > 1 ? rep : rep % D.Hk;
+      u = w.y;
+      first = w.z;
+      last = first + plan.head[1];
+      piece = w.w;
+    } else {
+      const int bhk = (int)(item / D.nI);
+      b = bhk / D.Hk;
+      hk = bhk - b * D.Hk;
+      u = plan.order[(long long)mask_batch(D.Bm, b) * D.nI + (item - (long long)bhk * D.nI)];
+    }
+    const int bhk = b * D.Hk + hk;
     const int4 info = plan.units[(long long)mask_batch(D.Bm, b) * D.nU + u];
-    int first, last;
-    share((max(info.y - info.x, 0) + kRows - 1) / kRows, split, a.splits, first, last);
-    const int k_lo = info.x + first * kRows, k_hi = min(info.x + last * kRows, info.y);
+    const int k_lo = info.x + first * kRows, k_hi = (int)min((long long)info.x + (long long)last * kRows, (long long)info.y);
     __syncthreads();
     load_unit(rows, D, plan, b, u);
     __syncthreads();
@@ -273,59 +344,94 @@ range_fwd_kernel(const RDims D, const Plan plan, const FwdArgs a) {
       for (int c = 0; c < DH / 64; ++c) {
         const int col = 64 * c + 4 * tx;
         const float4 x = make_float4(acc[i][4 * c] * inv, acc[i][4 * c + 1] * inv, acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv);
-        if (a.splits == 1) {
+        if (!cut) {
           T* resid = a.resid ? reinterpret_cast<T*>(a.resid) + (((long long)b * D.Sq + tok) * D.Hq + head) * DH + col : nullptr;
           store4_resid(reinterpret_cast<T*>(a.o) + b * a.os.b + tok * a.os.t + head * a.os.h + col, resid, x);
         } else {
-          store4(a.part_o + (split * all_rows + packed) * DH + col, x);
+          store4(a.part_o + (piece * all_rows + packed) * DH + col, x);
         }
       }
       if (tx == 0) {
-        if (a.splits == 1) a.lse[((long long)b * D.Hq + head) * D.Sq + tok] = row_lse;
-        else a.part_lse[split * all_rows + packed] = row_lse;
+        if (!cut) a.lse[((long long)b * D.Hq + head) * D.Sq + tok] = row_lse;
+        else a.part_lse[piece * all_rows + packed] = row_lse;
       }
     }
   }
 }
 
-// Joins the splits of every row: a warp per row, in the order of the splits.
-template <typename T, int DH>
+// Joins the pieces of every row: W warps per row, warp w the pieces w, w + W, ...; the same order of sums in every call.  Bound by the
+// latency of loads where rows are few (48 of 64 pieces each: 20 us with a warp per row), else by the L2, which the pieces come from.
+template <typename T, int DH, int W>
 __global__ void __launch_bounds__(256)
-range_merge_kernel(const RDims D, const FwdArgs a) {
+range_merge_kernel(const RDims D, const FastDiv by_rows, const FastDiv by_G, const FastDiv by_Hk, const FastDiv by_item, const Plan plan,
+                   const FwdArgs a) {
   if (!grid_begin()) return;
-  constexpr int C = DH / 32;
-  const int lane = threadIdx.x & 31;
-  const long long all_rows = (long long)D.B * D.Hk * D.rows;
-  for (long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); row < all_rows; row += (long long)gridDim.x * 8) {
-    float mine = -INFINITY, mx = -INFINITY;
-    for (int s = lane; s < a.splits; s += 32) mx = fmaxf(mx, __ldg(a.part_lse + s * all_rows + row));
+  constexpr int C = DH / 32, AT_ONCE = 8;
+  __shared__ float part[W > 1 ? W : 1][W > 1 ? DH + 32 : 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % W;
+  const int all_rows = D.B * D.Hk * D.rows;    // (at most 2^30)
+  for (int row = blockIdx.x * (8 / W) + warp / W; row < all_rows; row += gridDim.x * (8 / W)) {
+    const int bhk = by_rows.div(row), r = row - bhk * D.rows, tok = by_G.div(r), g = r - tok * D.G;
+    const int b = by_Hk.div(bhk), head = (bhk - b * D.Hk) * D.G + g;
+    const int n_pieces = __ldg(plan.pieces + (long long)mask_batch(D.Bm, b) * D.nI + by_item.div(tok));
+    float lse[2], mx = -INFINITY;              // (n_pieces <= 64)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      lse[k] = lane + 32 * k < n_pieces ? __ldg(a.part_lse + (long long)(lane + 32 * k) * all_rows + row) : -INFINITY;
+      mx = fmaxf(mx, lse[k]);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     const float used = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) lse[k] = expf(lse[k] - used);
     float total = 0.f, acc[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) acc[c] = 0.f;
-    for (int s0 = 0; s0 < a.splits; s0 += 32) {
-      mine = s0 + lane < a.splits ? expf(__ldg(a.part_lse + (s0 + lane) * all_rows + row) - used) : 0.f;
-      const int n = min(32, a.splits - s0);
-#pragma unroll 4
-      for (int s = 0; s < n; ++s) {
-        const float w = __shfl_sync(0xffffffffu, mine, s);
-        const float* from = a.part_o + ((s0 + s) * all_rows + row) * DH + lane * C;
-        total += w;
+    for (int s0 = sub; s0 < n_pieces; s0 += W * AT_ONCE) {
+      float x[AT_ONCE][C];
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) {
+        const int s = s0 + k * W;
+        const float* from = a.part_o + ((long long)s * all_rows + row) * DH + lane * C;
         if constexpr (C == 4) {
-          const float4 x = *reinterpret_cast<const float4*>(from);
-          acc[0] = fmaf(w, x.x, acc[0]); acc[1] = fmaf(w, x.y, acc[1]); acc[2] = fmaf(w, x.z, acc[2]); acc[3] = fmaf(w, x.w, acc[3]);
+          const float4 v = s < n_pieces ? *reinterpret_cast<const float4*>(from) : make_float4(0.f, 0.f, 0.f, 0.f);
+          x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
         } else {
-          const float2 x = *reinterpret_cast<const float2*>(from);
-          acc[0] = fmaf(w, x.x, acc[0]); acc[1] = fmaf(w, x.y, acc[1]);
+          const float2 v = s < n_pieces ? *reinterpret_cast<const float2*>(from) : make_float2(0.f, 0.f);
+          x[k][0] = v.x; x[k][1] = v.y;
         }
+      }
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) {
+        const int s = s0 + k * W;
+        const float w0 = __shfl_sync(0xffffffffu, lse[0], s & 31), w1 = __shfl_sync(0xffffffffu, lse[1], s & 31);
+        const float w = s < n_pieces ? (s < 32 ? w0 : w1) : 0.f;
+        total += w;
+#pragma unroll
+        for (int c = 0; c < C; ++c) acc[c] = fmaf(w, x[k][c], acc[c]);
+      }
+    }
+    if constexpr (W > 1) {
+      static_assert(W == 8, "a block per row");
+      __syncthreads();                         // (the row before has been read)
+#pragma unroll
+      for (int c = 0; c < C; ++c) part[sub][lane * C + c] = acc[c];
+      if (lane == 0) part[sub][DH] = total;
+      __syncthreads();
+      if (sub > 0) continue;
+      total = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) acc[c] = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        total += part[w][DH];
+#pragma unroll
+        for (int c = 0; c < C; ++c) acc[c] += part[w][lane * C + c];
       }
     }
     const bool none = total == 0.f;
     const float inv = none ? 0.f : 1.0f / total;
-    const int bhk = (int)(row / D.rows), r = (int)(row - (long long)bhk * D.rows), tok = r / D.G, g = r - tok * D.G;
-    const int b = bhk / D.Hk, head = (bhk - b * D.Hk) * D.G + g;
     T* o = reinterpret_cast<T*>(a.o) + b * a.os.b + tok * a.os.t + head * a.os.h + lane * C;
     T* resid = a.resid ? reinterpret_cast<T*>(a.resid) + (((long long)b * D.Sq + tok) * D.Hq + head) * DH + lane * C : nullptr;
 #pragma unroll
@@ -411,119 +517,82 @@ __device__ __forceinline__ void weigh(float s, bool in, float lse, const RDims& 
   w = in ? p * slope : 0.f;
 }
 
-// dK, dV: a CTA owns 64 keys of a key head and streams the units that reach into them, all query heads of the group.
+// The gradients: one launch for dK / dV (an item is 64 keys of a key head, against the units that reach into them, all query heads of the
+// group) and dQ (an item is a unit, against the tiles of its hull, which works S and dP out again).  Where that leaves SMs without
+// an item, a cluster of C CTAs takes an item: each a C-th of what it streams, and their parts are added up through one another's shared
+// memory in the order of the CTAs.  (Two samples of 256 tokens, two heads of 64: 24 items, 86 us with two launches and a CTA each.)
 template <int DH> constexpr int kRangeBwdSmem = (4 * kTileFloats<DH> + kRows * kLdP) * 4;
+
+// acc (rows 4 ty + i of a tile) of all CTAs of the cluster, summed: row r goes to put(r, column, four sums).  part: a tile in shared memory
+// that nobody reads any more.
+template <int DH, typename Put>
+__device__ __forceinline__ void cluster_sum(int C, float (&acc)[4][DH / 16], float* part, int ty, int tx, Put put) {
+  if (C == 1) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < DH / 64; ++c)
+        put(4 * ty + i, 64 * c + 4 * tx, make_float4(acc[i][4 * c], acc[i][4 * c + 1], acc[i][4 * c + 2], acc[i][4 * c + 3]));
+    return;
+  }
+  cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int c = 0; c < DH / 64; ++c)
+      *reinterpret_cast<float4*>(part + (4 * ty + i) * kLd<DH> + 64 * c + 4 * tx) = make_float4(acc[i][4 * c], acc[i][4 * c + 1], acc[i][4 * c + 2], acc[i][4 * c + 3]);
+  cluster.sync();
+  constexpr int V = DH / 4;
+  for (int e = (int)cluster.block_rank() * kThreads + threadIdx.x; e < kRows * V; e += C * kThreads) {
+    const int r = e / V, col = e % V * 4;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int n = 0; n < C; ++n) {
+      const float4 x = *reinterpret_cast<const float4*>(cluster.map_shared_rank(part, n) + r * kLd<DH> + col);
+      a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+    }
+    put(r, col, a);
+  }
+  cluster.sync();                              // (nobody reads this CTA's part any more)
+}
+
 template <typename T, int DH>
-__global__ void __launch_bounds__(kThreads, DH == 64 ? 2 : 1)
-range_bwd_dkdv_kernel(const RDims D, const Plan plan, const BwdArgs a) {
-  if (!grid_begin()) return;
-  extern __shared__ __align__(16) float simt_smem[];
-  float* Ks = simt_smem;
+__device__ __forceinline__ void range_bwd_keys(const RDims& D, const Plan& plan, const BwdArgs& a, long long item, int rank, int C, float* smem, UnitRows& rows,
+                                               float* s_lse, float* s_D) {
+  float* Ks = smem;
   float* Vs = Ks + kTileFloats<DH>;
   float* Qs = Vs + kTileFloats<DH>;
   float* dOs = Qs + kTileFloats<DH>;
   float* Ps = dOs + kTileFloats<DH>;           // [key][query]: weights, then dT
-  __shared__ UnitRows rows;
-  __shared__ float s_lse[kRows], s_D[kRows];
   const int t = threadIdx.x, ty = t >> 4, tx = t & 15;
-  const long long n_items = (long long)D.B * D.Hk * D.nK;
-  for (long long item = blockIdx.x; item < n_items; item += gridDim.x) {
-    const int bhk = (int)(item / D.nK), tile = (int)(item - (long long)bhk * D.nK), b = bhk / D.Hk, hk = bhk - b * D.Hk;
-    const int4 info = plan.keys[(long long)mask_batch(D.Bm, b) * D.nK + tile];
-    const int key0 = tile * kRows, keys = min(kRows, D.Sk - key0);
-    float dk_[4][DH / 16], dv_[4][DH / 16];
+  const int bhk = (int)(item / D.nK), tile = (int)(item - (long long)bhk * D.nK), b = bhk / D.Hk, hk = bhk - b * D.Hk;
+  const int4 info = plan.keys[(long long)mask_batch(D.Bm, b) * D.nK + tile];
+  const int key0 = tile * kRows, keys = min(kRows, D.Sk - key0);
+  float dk_[4][DH / 16], dv_[4][DH / 16];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int c = 0; c < DH / 16; ++c) dk_[i][c] = dv_[i][c] = 0.f;
-    __syncthreads();
-    {
-      const T* kb = reinterpret_cast<const T*>(a.k) + b * a.ks.b + hk * a.ks.h;
-      const T* vb = reinterpret_cast<const T*>(a.v) + b * a.vs.b + hk * a.vs.h;
-      RowRegs<T, DH> x;
-      x.fetch([&](int r) { return r >= info.z && r < info.w ? kb + (long long)(key0 + r) * a.ks.t : nullptr; });
-      x.store(Ks);
-      x.fetch([&](int r) { return r >= info.z && r < info.w ? vb + (long long)(key0 + r) * a.vs.t : nullptr; });
-      x.store(Vs);
-    }
-    for (int u = info.x; u < info.y; ++u) {
-      if (!reaches(plan.units[(long long)mask_batch(D.Bm, b) * D.nU + u], tile, kRows)) continue;
-      __syncthreads();
-      load_unit(rows, D, plan, b, u);
-      __syncthreads();
-      if (t < kRows) {
-        const int tok = rows.tok[t];
-        const bool some = rows.range[t].y > 0;
-        s_lse[t] = some ? a.lse[((long long)b * D.Hq + hk * D.G + t % D.G) * D.Sq + tok] : INFINITY;
-        s_D[t] = some ? a.Dv[(long long)bhk * D.rows + (long long)tok * D.G + t % D.G] : 0.f;
-      }
-      {
-        const T* qb = reinterpret_cast<const T*>(a.q) + b * a.qs.b + (long long)hk * D.G * a.qs.h;
-        const T* ob = reinterpret_cast<const T*>(a.d_o) + b * a.dos.b + (long long)hk * D.G * a.dos.h;
-        RowRegs<T, DH> x;
-        x.fetch([&](int r) { return rows.range[r].y > 0 ? qb + rows.tok[r] * a.qs.t + (r % D.G) * a.qs.h : nullptr; });
-        x.store(Qs);
-        x.fetch([&](int r) { return rows.range[r].y > 0 ? ob + rows.tok[r] * a.dos.t + (r % D.G) * a.dos.h : nullptr; });
-        x.store(dOs);
-      }
-      __syncthreads();
-      float s[4][4], w[4][4];
-      dot_tiles<DH>(Ks, Qs, ty, tx, kRows, s);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = tx + 16 * j, key = key0 + 4 * ty + i;
-          const int2 rg = rows.range[r];
-          weigh(s[i][j], key >= rg.x && key < rg.y, s_lse[r], D, s[i][j], w[i][j]);
-          Ps[(4 * ty + i) * kLdP + r] = s[i][j];
-        }
-      __syncwarp();                            // (a warp reads its own eight rows)
-      add_weighted<DH>(Ps, dOs, ty, tx, kRows, dv_);
-      dot_tiles<DH>(Vs, dOs, ty, tx, kRows, s);
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) Ps[(4 * ty + i) * kLdP + tx + 16 * j] = w[i][j] * (s[i][j] - s_D[tx + 16 * j]);
-      __syncwarp();
-      add_weighted<DH>(Ps, Qs, ty, tx, kRows, dk_);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (4 * ty + i >= keys) break;
-      T* dk = reinterpret_cast<T*>(a.dk) + b * a.dks.b + (long long)(key0 + 4 * ty + i) * a.dks.t + hk * a.dks.h;
-      T* dv = reinterpret_cast<T*>(a.dv) + b * a.dvs.b + (long long)(key0 + 4 * ty + i) * a.dvs.t + hk * a.dvs.h;
-#pragma unroll
-      for (int c = 0; c < DH / 64; ++c) {
-        const int col = 64 * c + 4 * tx;
-        store4(dk + col, make_float4(dk_[i][4 * c] * D.scale, dk_[i][4 * c + 1] * D.scale, dk_[i][4 * c + 2] * D.scale, dk_[i][4 * c + 3] * D.scale));
-        store4(dv + col, make_float4(dv_[i][4 * c], dv_[i][4 * c + 1], dv_[i][4 * c + 2], dv_[i][4 * c + 3]));
-      }
-    }
+    for (int c = 0; c < DH / 16; ++c) dk_[i][c] = dv_[i][c] = 0.f;
+  __syncthreads();                             // (the item before is through with the shared memory)
+  {
+    const T* kb = reinterpret_cast<const T*>(a.k) + b * a.ks.b + hk * a.ks.h;
+    const T* vb = reinterpret_cast<const T*>(a.v) + b * a.vs.b + hk * a.vs.h;
+    RowRegs<T, DH> x;
+    x.fetch([&](int r) { return r >= info.z && r < info.w ? kb + (long long)(key0 + r) * a.ks.t : nullptr; });
+    x.store(Ks);
+    x.fetch([&](int r) { return r >= info.z && r < info.w ? vb + (long long)(key0 + r) * a.vs.t : nullptr; });
+    x.store(Vs);
   }
-}
-
-// dQ: a CTA takes a unit and works S and dP out again.
-template <typename T, int DH>
-__global__ void __launch_bounds__(kThreads, DH == 64 ? 2 : 1)
-range_bwd_dq_kernel(const RDims D, const Plan plan, const BwdArgs a, T* __restrict__ dq, const Strides dqs) {
-  if (!grid_begin()) return;
-  extern __shared__ __align__(16) float simt_smem[];
-  float* Qs = simt_smem;
-  float* dOs = Qs + kTileFloats<DH>;
-  float* Ks = dOs + kTileFloats<DH>;
-  float* Vs = Ks + kTileFloats<DH>;
-  float* Ps = Vs + kTileFloats<DH>;            // [query][key]: dT
-  __shared__ UnitRows rows;
-  const int t = threadIdx.x, ty = t >> 4, tx = t & 15;
-  const long long n_items = (long long)D.B * D.Hk * D.nU;
-  for (long long item = blockIdx.x; item < n_items; item += gridDim.x) {
-    const int bhk = (int)(item / D.nU), u = (int)(item - (long long)bhk * D.nU), b = bhk / D.Hk, hk = bhk - b * D.Hk;
-    const int4 info = plan.units[(long long)mask_batch(D.Bm, b) * D.nU + u];
+  for (int u = info.x + rank; u < info.y; u += C) {
+    if (!reaches(plan.units[(long long)mask_batch(D.Bm, b) * D.nU + u], tile, kRows)) continue;
     __syncthreads();
     load_unit(rows, D, plan, b, u);
     __syncthreads();
+    if (t < kRows) {
+      const int tok = rows.tok[t];
+      const bool some = rows.range[t].y > 0;
+      s_lse[t] = some ? a.lse[((long long)b * D.Hq + hk * D.G + t % D.G) * D.Sq + tok] : INFINITY;
+      s_D[t] = some ? a.Dv[(long long)bhk * D.rows + (long long)tok * D.G + t % D.G] : 0.f;
+    }
     {
       const T* qb = reinterpret_cast<const T*>(a.q) + b * a.qs.b + (long long)hk * D.G * a.qs.h;
       const T* ob = reinterpret_cast<const T*>(a.d_o) + b * a.dos.b + (long long)hk * D.G * a.dos.h;
@@ -533,54 +602,124 @@ range_bwd_dq_kernel(const RDims D, const Plan plan, const BwdArgs a, T* __restri
       x.fetch([&](int r) { return rows.range[r].y > 0 ? ob + rows.tok[r] * a.dos.t + (r % D.G) * a.dos.h : nullptr; });
       x.store(dOs);
     }
-    float row_lse[4], row_D[4], acc[4][DH / 16];
+    __syncthreads();
+    float s[4][4], w[4][4];
+    dot_tiles<DH>(Ks, Qs, ty, tx, kRows, s);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 4 * ty + i, tok = rows.tok[r];
-      const bool some = rows.range[r].y > 0;
-      row_lse[i] = some ? a.lse[((long long)b * D.Hq + hk * D.G + r % D.G) * D.Sq + tok] : INFINITY;
-      row_D[i] = some ? a.Dv[(long long)bhk * D.rows + (long long)tok * D.G + r % D.G] : 0.f;
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int c = 0; c < DH / 16; ++c) acc[i][c] = 0.f;
-    }
-    const T* kb = reinterpret_cast<const T*>(a.k) + b * a.ks.b + hk * a.ks.h;
-    const T* vb = reinterpret_cast<const T*>(a.v) + b * a.vs.b + hk * a.vs.h;
-    for (int t0 = info.x; t0 < info.y; t0 += kRows) {
-      const int nv = min(kRows, info.y - t0);
-      RowRegs<T, DH> x, y;
-      x.fetch([&](int r) { return r < nv ? kb + (long long)(t0 + r) * a.ks.t : nullptr; });
-      y.fetch([&](int r) { return r < nv ? vb + (long long)(t0 + r) * a.vs.t : nullptr; });
-      __syncthreads();
-      x.store(Ks);
-      y.store(Vs);
-      __syncthreads();
-      float p[4][4], s[4][4];
-      dot_tiles<DH>(Qs, Ks, ty, tx, kRows, p);
-      dot_tiles<DH>(dOs, Vs, ty, tx, kRows, s);
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int2 rg = rows.range[4 * ty + i];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int key = t0 + tx + 16 * j;
-          float w, none;
-          weigh(p[i][j], key >= rg.x && key < rg.y, row_lse[i], D, none, w);
-          Ps[(4 * ty + i) * kLdP + tx + 16 * j] = w * (s[i][j] - row_D[i]);
-        }
+      for (int j = 0; j < 4; ++j) {
+        const int r = tx + 16 * j, key = key0 + 4 * ty + i;
+        const int2 rg = rows.range[r];
+        weigh(s[i][j], key >= rg.x && key < rg.y, s_lse[r], D, s[i][j], w[i][j]);
+        Ps[(4 * ty + i) * kLdP + r] = s[i][j];
       }
-      __syncwarp();                            // (a warp reads its own eight rows)
-      add_weighted<DH>(Ps, Ks, ty, tx, kRows, acc);
-    }
+    __syncwarp();                              // (a warp reads its own eight rows)
+    add_weighted<DH>(Ps, dOs, ty, tx, kRows, dv_);
+    dot_tiles<DH>(Vs, dOs, ty, tx, kRows, s);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) Ps[(4 * ty + i) * kLdP + tx + 16 * j] = w[i][j] * (s[i][j] - s_D[tx + 16 * j]);
+    __syncwarp();
+    add_weighted<DH>(Ps, Qs, ty, tx, kRows, dk_);
+  }
+  __syncthreads();                             // (K and V have been read)
+  auto out = [&](void* to, const Strides& s, float scale) {
+    return [=](int r, int col, const float4& x) {
+      if (r < keys)
+        store4(reinterpret_cast<T*>(to) + b * s.b + (long long)(key0 + r) * s.t + hk * s.h + col, make_float4(x.x * scale, x.y * scale, x.z * scale, x.w * scale));
+    };
+  };
+  cluster_sum<DH>(C, dk_, Ks, ty, tx, out(a.dk, a.dks, D.scale));
+  cluster_sum<DH>(C, dv_, Vs, ty, tx, out(a.dv, a.dvs, 1.0f));
+}
+
+template <typename T, int DH>
+__device__ __forceinline__ void range_bwd_queries(const RDims& D, const Plan& plan, const BwdArgs& a, T* dq, const Strides& dqs, long long item, int rank,
+                                                  int C, float* smem, UnitRows& rows) {
+  float* Qs = smem;
+  float* dOs = Qs + kTileFloats<DH>;
+  float* Ks = dOs + kTileFloats<DH>;
+  float* Vs = Ks + kTileFloats<DH>;
+  float* Ps = Vs + kTileFloats<DH>;            // [query][key]: dT
+  const int t = threadIdx.x, ty = t >> 4, tx = t & 15;
+  const int bhk = (int)(item / D.nU), u = (int)(item - (long long)bhk * D.nU), b = bhk / D.Hk, hk = bhk - b * D.Hk;
+  const int4 info = plan.units[(long long)mask_batch(D.Bm, b) * D.nU + u];
+  __syncthreads();                             // (the item before is through with the shared memory)
+  load_unit(rows, D, plan, b, u);
+  __syncthreads();
+  {
+    const T* qb = reinterpret_cast<const T*>(a.q) + b * a.qs.b + (long long)hk * D.G * a.qs.h;
+    const T* ob = reinterpret_cast<const T*>(a.d_o) + b * a.dos.b + (long long)hk * D.G * a.dos.h;
+    RowRegs<T, DH> x;
+    x.fetch([&](int r) { return rows.range[r].y > 0 ? qb + rows.tok[r] * a.qs.t + (r % D.G) * a.qs.h : nullptr; });
+    x.store(Qs);
+    x.fetch([&](int r) { return rows.range[r].y > 0 ? ob + rows.tok[r] * a.dos.t + (r % D.G) * a.dos.h : nullptr; });
+    x.store(dOs);
+  }
+  float row_lse[4], row_D[4], acc[4][DH / 16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 4 * ty + i, tok = rows.tok[r];
+    const bool some = rows.range[r].y > 0;
+    row_lse[i] = some ? a.lse[((long long)b * D.Hq + hk * D.G + r % D.G) * D.Sq + tok] : INFINITY;
+    row_D[i] = some ? a.Dv[(long long)bhk * D.rows + (long long)tok * D.G + r % D.G] : 0.f;
+#pragma unroll
+    for (int c = 0; c < DH / 16; ++c) acc[i][c] = 0.f;
+  }
+  const T* kb = reinterpret_cast<const T*>(a.k) + b * a.ks.b + hk * a.ks.h;
+  const T* vb = reinterpret_cast<const T*>(a.v) + b * a.vs.b + hk * a.vs.h;
+  for (long long t0 = info.x + (long long)rank * kRows; t0 < info.y; t0 += (long long)C * kRows) {
+    const int nv = (int)min((long long)kRows, info.y - t0);
+    RowRegs<T, DH> x, y;
+    x.fetch([&](int r) { return r < nv ? kb + (t0 + r) * a.ks.t : nullptr; });
+    y.fetch([&](int r) { return r < nv ? vb + (t0 + r) * a.vs.t : nullptr; });
+    __syncthreads();
+    x.store(Ks);
+    y.store(Vs);
+    __syncthreads();
+    float p[4][4], s[4][4];
+    dot_tiles<DH>(Qs, Ks, ty, tx, kRows, p);
+    dot_tiles<DH>(dOs, Vs, ty, tx, kRows, s);
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r = 4 * ty + i, tok = rows.tok[r];
-      if (tok < 0) continue;
-      T* row = dq + b * dqs.b + tok * dqs.t + (long long)(hk * D.G + r % D.G) * dqs.h + 4 * tx;
+      const int2 rg = rows.range[4 * ty + i];
 #pragma unroll
-      for (int c = 0; c < DH / 64; ++c)
-        store4(row + 64 * c, make_float4(acc[i][4 * c] * D.scale, acc[i][4 * c + 1] * D.scale, acc[i][4 * c + 2] * D.scale, acc[i][4 * c + 3] * D.scale));
+      for (int j = 0; j < 4; ++j) {
+        const int key = (int)t0 + tx + 16 * j;
+        float w, none;
+        weigh(p[i][j], key >= rg.x && key < rg.y, row_lse[i], D, none, w);
+        Ps[(4 * ty + i) * kLdP + tx + 16 * j] = w * (s[i][j] - row_D[i]);
+      }
     }
+    __syncwarp();                              // (a warp reads its own eight rows)
+    add_weighted<DH>(Ps, Ks, ty, tx, kRows, acc);
+  }
+  __syncthreads();                             // (Q has been read)
+  cluster_sum<DH>(C, acc, Qs, ty, tx, [&](int r, int col, const float4& x) {
+    const int tok = rows.tok[r];
+    if (tok >= 0)
+      store4(dq + b * dqs.b + tok * dqs.t + (long long)(hk * D.G + r % D.G) * dqs.h + col,
+             make_float4(x.x * D.scale, x.y * D.scale, x.z * D.scale, x.w * D.scale));
+  });
+}
+
+// A grid of whole clusters of C CTAs.
+template <typename T, int DH>
+__global__ void __launch_bounds__(kThreads, DH == 64 ? 2 : 1)
+range_bwd_kernel(const RDims D, const Plan plan, const BwdArgs a, T* __restrict__ dq, const Strides dqs, const int C) {
+  if (!grid_begin()) return;
+  extern __shared__ __align__(16) float simt_smem[];
+  __shared__ UnitRows rows;
+  __shared__ float s_lse[kRows], s_D[kRows];
+  const long long n_keys = (long long)D.B * D.Hk * D.nK, n_items = n_keys + (long long)D.B * D.Hk * D.nU;
+  const int rank = blockIdx.x % C;
+  for (long long item = blockIdx.x / C; item < n_items; item += gridDim.x / C) {
+    if (item < n_keys) range_bwd_keys<T, DH>(D, plan, a, item, rank, C, simt_smem, rows, s_lse, s_D);
+    else range_bwd_queries<T, DH>(D, plan, a, dq, dqs, item - n_keys, rank, C, simt_smem, rows);
   }
 }
 
@@ -608,47 +747,41 @@ static int make_rdims(const vmoba_range_shape* s, RDims* o) {
   o->nU = (s->Sq + o->tpt - 1) / o->tpt;
   o->nK = (s->Sk + o->TR - 1) / o->TR;
   o->nI = o->tc ? (o->nU + 1) / 2 : o->nU;
+  // Fewer items than four for every SM: they are cut, where there is something to cut (a tile takes the tensor cores 2 us, the CUDA cores 4,
+  // joining the pieces 5 to 10: 256 keys in tiles of 64 took 20 us whole and 26 in pieces), eight pieces per SM at most on average and 64 of
+  // an item.
+  const long long items = (long long)s->B * s->kv_heads * o->nI;
+  o->smax = 1;
+  if (items < kFewItems && o->nK >= 8) o->smax = (int)std::min<long long>(std::min(64, o->nK), (8 * kSms + items - 1) / items);
+  o->reps = s->mask_batch == 1 ? s->B * s->kv_heads : s->kv_heads;
   return VMOBA_OK;
 }
 
 static Plan carve_plan(const RDims& D, const void* mem, size_t* bytes) {
   Carver c(const_cast<void*>(mem));
-  Plan p;
+  Plan p = {};
   p.rows = c.take<int2>((size_t)D.Bm * D.Sq);
   p.units = c.take<int4>((size_t)D.Bm * D.nU);
   p.keys = c.take<int4>((size_t)D.Bm * D.nK);
   p.runs = c.take<int4>((size_t)D.Bm * D.nK);
   p.order = c.take<int>((size_t)D.Bm * D.nI);
+  p.head = c.take<int>(2);
+  if (D.smax > 1) {
+    p.pieces = c.take<int>((size_t)D.Bm * D.nI);
+    p.work = c.take<int4>((size_t)D.Bm * D.nI * D.smax);
+  }
   if (bytes) *bytes = c.total();
   return p;
 }
 
-// How many pieces a key range is cut into: as many as shorten the longest queue of an SM.  A piece costs its rows a trip through memory
-// in fp32 (8 bytes per element and piece) and the last wave is paid in full.  The number of SMs is the design's, not the device's,
-// so that the workspace is a function of the shape alone.
-static int splits(const RDims& D) {
-  constexpr int kSms = 148;
-  const long long items = (long long)D.B * D.Hk * D.nI, tiles = D.nK;
-  if (items >= 4 * kSms || tiles < 8) return 1;
-  const double tile_us = D.tc ? 1.9 : 20.0, row_us = (double)D.B * D.Hk * D.rows * D.d * 8 / 6.0e6;
-  double best = 1e30;
-  int n = 1;
-  for (int s = 1; s <= 64 && s * 4 <= tiles; ++s) {
-    const long long waves = (items * s + kSms - 1) / kSms;
-    const double us = waves * ((double)tiles / s * tile_us + 4.0) + (s > 1 ? s * row_us + 4.0 : 0.0);
-    if (us < best * 0.98) { best = us; n = s; }
-  }
-  return n;
-}
-
 struct FwdWs { float *part_o, *part_lse; size_t bytes; Guards guards; };
-static FwdWs carve_fwd(const RDims& D, int n, void* ws) {
+static FwdWs carve_fwd(const RDims& D, void* ws) {
   Carver c(ws);
   FwdWs w = {};
   const size_t rows = (size_t)D.B * D.Hk * D.rows;
-  if (n > 1) {
-    w.part_lse = c.take<float>(rows * n);
-    w.part_o = c.take<float>(rows * n * D.d);
+  if (D.smax > 1) {
+    w.part_lse = c.take<float>(rows * D.smax);
+    w.part_o = c.take<float>(rows * D.smax * D.d);
   }
   w.bytes = std::max<size_t>(c.total(), 256);
   w.guards = c.guards;
@@ -697,13 +830,19 @@ static int forward(const RDims& D, const Plan& plan, FwdArgs a, cudaStream_t st)
   if constexpr (sizeof(T) == 2 && DH == 128) {
     if (int rc = tc_range_fwd(D, plan, a, st)) return rc;
   } else {
-    const long long items = (long long)D.B * D.Hk * D.nI * a.splits;
+    const long long items = (long long)D.B * D.Hk * D.nI * D.smax;
     VMOBA_CUDA_OK(allow_smem(range_fwd_kernel<T, DH>, simt::kFwdSmem<DH>));
     launch_kernel(early_simt(D), range_fwd_kernel<T, DH>, grid_for(items, 8), kThreads, simt::kFwdSmem<DH>, st, D, plan, a);
     VMOBA_LAUNCH_OK(1);
   }
-  if (a.splits > 1) {
-    launch_kernel(early_rows(D), range_merge_kernel<T, DH>, grid_for(((long long)D.B * D.Hk * D.rows + 7) / 8, 16), 256, 0, st, D, a);
+  if (D.smax > 1) {
+    const long long rows = (long long)D.B * D.Hk * D.rows;
+    const FastDiv by_rows(D.rows), by_G(D.G), by_Hk(D.Hk), by_item(D.tpt * (D.tc ? 2 : 1));
+    if (rows <= 8 * kSms)                      // (a block per row, all of them at once)
+      launch_kernel(early_rows(D), range_merge_kernel<T, DH, 8>, (int)rows, 256, 0, st, D, by_rows, by_G, by_Hk, by_item, plan, a);
+    else
+      launch_kernel(early_rows(D), range_merge_kernel<T, DH, 1>, grid_for((rows + 7) / 8, 16), 256, 0, st, D, by_rows, by_G, by_Hk, by_item,
+                    plan, a);
     VMOBA_LAUNCH_OK(1);
   }
   return VMOBA_OK;
@@ -720,12 +859,14 @@ static int backward(const RDims& D, const Plan& plan, const BwdArgs& a, const vo
   if constexpr (sizeof(T) == 2 && DH == 128) {
     return tc_range_bwd(D, plan, a, dq, dqs, early_rows(D), st);
   } else {
-    VMOBA_CUDA_OK(allow_smem(range_bwd_dkdv_kernel<T, DH>, kRangeBwdSmem<DH>));
-    VMOBA_CUDA_OK(allow_smem(range_bwd_dq_kernel<T, DH>, kRangeBwdSmem<DH>));
-    launch_kernel(early_simt(D), range_bwd_dkdv_kernel<T, DH>, grid_for((long long)D.B * D.Hk * D.nK, 4), kThreads, kRangeBwdSmem<DH>, st, D, plan, a);
-    launch_kernel(early_simt(D), range_bwd_dq_kernel<T, DH>, grid_for((long long)D.B * D.Hk * D.nU, 4), kThreads, kRangeBwdSmem<DH>, st, D, plan, a,
-                  (T*)dq, dqs);
-    VMOBA_LAUNCH_OK(2);
+    VMOBA_CUDA_OK(allow_smem(range_bwd_kernel<T, DH>, kRangeBwdSmem<DH>));
+    const long long items = (long long)D.B * D.Hk * (D.nK + D.nU), room = (long long)kSms * (DH == 64 ? 2 : 1);
+    int C = 1;
+    while (C < 8 && items * C * 2 <= room && std::max(D.nU, D.nK) >= 2 * C) C *= 2;
+    const int grid = C * (int)std::max<long long>(1, std::min<long long>(items, (long long)sm_count() * 4 / C));
+    if (C > 1) launch_cluster(early_simt(D), C, range_bwd_kernel<T, DH>, grid, kThreads, kRangeBwdSmem<DH>, st, D, plan, a, (T*)dq, dqs, C);
+    else launch_kernel(early_simt(D), range_bwd_kernel<T, DH>, grid, kThreads, kRangeBwdSmem<DH>, st, D, plan, a, (T*)dq, dqs, C);
+    VMOBA_LAUNCH_OK(1);
     return VMOBA_OK;
   }
 }
@@ -765,7 +906,7 @@ extern "C" int vmoba_range_plan(const vmoba_range_shape* shape, const int32_t* k
   launch_kernel(plan_units_kernel, grid_for(((long long)D.Bm * D.nU + 7) / 8, 8), 256, 0, st, reinterpret_cast<const int2*>(key_range), p, D);
   const long long tile_blocks = std::min<long long>(((long long)D.Bm * D.nK + 31) / 32, 2ll * sm_count());
   if (D.Bm > (1 << 20)) return VMOBA_ERR_SHAPE;
-  launch_kernel(plan_tiles_kernel, (unsigned)(D.Bm + tile_blocks), 1024, 0, st, p, D);
+  launch_kernel(plan_tiles_kernel, (unsigned)(D.Bm + 1 + tile_blocks), 1024, 0, st, p, D);
   VMOBA_LAUNCH_OK(2);
   return VMOBA_OK;
 }
@@ -773,7 +914,7 @@ extern "C" int vmoba_range_plan(const vmoba_range_shape* shape, const int32_t* k
 extern "C" size_t vmoba_range_workspace_bytes(const vmoba_range_shape* shape, int backward) {
   RDims D;
   if (make_rdims(shape, &D) || (backward != 0 && backward != 1)) return 0;
-  return backward ? carve_bwd(D, nullptr).bytes : carve_fwd(D, splits(D), nullptr).bytes;
+  return backward ? carve_bwd(D, nullptr).bytes : carve_fwd(D, nullptr).bytes;
 }
 
 extern "C" int vmoba_range_attn_fwd(const vmoba_range_shape* shape, const void* plan, const void* q, const int64_t q_strides[3],
@@ -789,8 +930,7 @@ extern "C" int vmoba_range_attn_fwd(const vmoba_range_shape* shape, const void* 
   if (!get_strides(D, q_strides, D.Sq, D.Hq, &a.qs) || !get_strides(D, k_strides, D.Sk, D.Hk, &a.ks) ||
       !get_strides(D, v_strides, D.Sk, D.Hk, &a.vs) || !get_strides(D, o_strides, D.Sq, D.Hq, &a.os))
     return VMOBA_ERR_ARG;
-  a.splits = splits(D);
-  FwdWs w = carve_fwd(D, a.splits, ws);
+  FwdWs w = carve_fwd(D, ws);
   if (ws_bytes < w.bytes) return VMOBA_ERR_WORKSPACE;
   a.q = q; a.k = k; a.v = v; a.o = o; a.resid = D.dtype == VMOBA_BF16 ? o_resid_or_null : nullptr; a.lse = lse;
   a.part_o = w.part_o; a.part_lse = w.part_lse; a.status = dev_status;

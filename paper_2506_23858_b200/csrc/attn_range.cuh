@@ -11,6 +11,10 @@
 //                          key (relative to the tile) that any unit's hull holds
 //   runs   int4 [Bm][nK]   how many units reach into it; a run [first, last) of units of which every row sees the whole tile
 //   order  int  [Bm][nI]   the forward's items (two units on the tensor cores, else one), those with the most keys first
+// and where there are so few items that their key ranges are cut into pieces (smax > 1):
+//   head   int  [2]        pieces of all items of all masks; tiles of keys in a piece
+//   pieces int  [Bm][nI]   pieces of an item
+//   work   int4 [...]      of a piece: mask, item, first tile, its number within the item
 #pragma once
 
 #include <algorithm>
@@ -30,6 +34,8 @@ struct RDims {
   int tpt;            // tokens of a unit
   int rows;           // rows of a (sample, key head): Sq * G
   int nU, nK, nI;     // units, key tiles, forward items per (sample, key head)
+  int smax;           // pieces that an item's key range is cut into at most (1: none is)
+  int reps;           // (sample, key head) pairs that share a mask's pieces
 };
 
 struct Plan {
@@ -38,6 +44,9 @@ struct Plan {
   int4* keys;
   int4* runs;
   int* order;
+  int* head;
+  int* pieces;
+  int4* work;
 };
 
 struct Strides { long long b, t, h; };       // elements
@@ -47,20 +56,14 @@ __device__ __forceinline__ int mask_batch(const int Bm, int b) { return Bm > 1 ?
 // Whether a unit with this record reaches into key tile t of TR keys.
 __device__ __forceinline__ bool reaches(const int4& u, int t, int TR) { return u.y > u.x && u.x < (t + 1) * TR && u.y > t * TR; }
 
-// The share of `split` of `n` splits of a range of `tiles` tiles: [first, last).
-__device__ __forceinline__ void share(int tiles, int split, int n, int& first, int& last) {
-  first = (int)((long long)tiles * split / n);
-  last = (int)((long long)tiles * (split + 1) / n);
-}
-
 // Capped scores in the exp2 domain: c' tanh(a s), c' = cap * log2 e, a = scale / cap.
 struct Cap {
-  float c, twice_a_log2;         // c', 2 a log2 e
-  float most;                    // |s| up to this: by the polynomial (-1: none)
+  float c, twice_log2;           // c'; 2 log2 e times the factor that pre does not take
+  float pre;                     // scores are multiplied by this first: 1 with a folded into all that follows, or a
+  float most;                    // |score| up to this: by the polynomial
   float p[5];                    // its coefficients of s, s^3, ...
-  float q[4];                    // of one with a term less, off by 3.6e-6: enough where only weights are made that bf16 rounds (2^-9)
+  float q[4];                    // of one with a term less, off by 3.6e-6 of c': enough where only weights are made that bf16 rounds (2^-9)
 };
-
 Cap make_cap(const RDims& D);      // attn_range_fwd.cu
 
 // ---- tensor-core kernels (attn_range_fwd.cu, attn_range_bwd.cu)
@@ -69,8 +72,7 @@ struct FwdArgs {
   void *o, *resid;           // resid: contiguous [B, Sq, Hq, d] or null
   float* lse;                // [B, Hq, Sq]
   Strides qs, ks, vs, os;
-  int splits;
-  float *part_o, *part_lse;  // [split][B * Hk * rows][d], [split][B * Hk * rows]
+  float *part_o, *part_lse;  // [piece][B * Hk * rows][d], [piece][B * Hk * rows]
   int32_t* status;
 };
 struct BwdArgs {

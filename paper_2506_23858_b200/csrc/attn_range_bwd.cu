@@ -599,12 +599,22 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
                 pv[rh][i] = __float_as_uint(x0);
                 pv[rh][i + 1] = __float_as_uint(x1);
               }
+          } else if (p.cap.pre != 1.0f) {            // (the vote above never finds for the polynomial then: score by score)
+#pragma unroll
+            for (int rh = 0; rh < 2; ++rh)
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float x = __uint_as_float(pv[rh][i]) * p.cap.pre, z = x * x;
+                const float near = x * fmaf(fmaf(fmaf(p.cap.q[3], z, p.cap.q[2]), z, p.cap.q[1]), z, p.cap.q[0]);
+                const float far = fmaf(rcp(1.0f + ex2(x * p.cap.twice_log2)), -2.0f * p.cap.c, p.cap.c);
+                pv[rh][i] = __float_as_uint(fabsf(x) <= 0.75f ? near : far);
+              }
           } else {
 #pragma unroll
             for (int rh = 0; rh < 2; ++rh)
 #pragma unroll
               for (int i = 0; i < 32; ++i)
-                pv[rh][i] = __float_as_uint(fmaf(rcp(1.0f + ex2(__uint_as_float(pv[rh][i]) * p.cap.twice_a_log2)), -2.0f * p.cap.c, p.cap.c));
+                pv[rh][i] = __float_as_uint(fmaf(rcp(1.0f + ex2(__uint_as_float(pv[rh][i]) * p.cap.twice_log2)), -2.0f * p.cap.c, p.cap.c));
           }
           if (__builtin_expect(masked || stale, 0)) mask(0xd8635fa9u);
         } else {
@@ -782,6 +792,7 @@ int tc_range_bwd(const RDims& D, const Plan& plan, const BwdArgs& a, void* dq, c
   p.scale = D.scale;
   p.scale_log2 = D.scale * LOG2E;
   p.cap = make_cap(D);
+  if (p.cap.pre != 1.0f) p.cap.most = -1.0f;
   p.cap_inv2 = D.cap > 0.f ? -1.0f / (p.cap.c * p.cap.c) : 0.f;
   p.dk = (__nv_bfloat16*)a.dk; p.dv = (__nv_bfloat16*)a.dv; p.dks = a.dks; p.dvs = a.dvs;
   auto whole = [](const void* x, const Strides& s) {

@@ -2,7 +2,7 @@
 //
 // The wide forward of attn_tc_fwd.cu (two 128-row query tiles A and B that share every tile of K and V, one score buffer that they
 // use in turn, softmax threads that hold a whole row of 128 scores) with the items of a plan: an item is two units of packed rows against
-// the hull of their key ranges (or a share of it, where the range is split), in tiles of 128 keys from the hull's first key on.  A unit
+// the hull of their key ranges (or a piece of it, where there are few items), in tiles of 128 keys from the hull's first key on.  A unit
 // takes part in the tiles that its own hull reaches; a score is compared with its row's range only in tiles where the unit's
 // bounds say that some row needs it.
 //
@@ -17,8 +17,8 @@
 //
 // Capped scores: c tanh(x), x = scale s / c.  By the exponential unit that is an exponential and a reciprocal more per score, and the
 // kernel is bound by that unit: a 33K clip by frames took 7.5 ms, 3.7 without the cap.  So tanh comes from the FMA pipe where a warp's
-// scores allow (32 keys at a time, |x| <= 3/4): an odd polynomial of five terms, fitted to tanh for the smallest largest error (by reweighted
-// least squares; 1.9e-7); larger scores take 1 - 2 / (1 + exp(2 x)).
+// scores allow (|x| <= 3/4): an odd polynomial of five terms, fitted to tanh for the smallest largest relative error (by reweighted least
+// squares; 5.7e-7); larger scores take 1 - 2 / (1 + exp(2 x)).
 // And a cap bounds the weights: up to c log2 e = 96 (caps of 66) exp2 of a score, of no difference to a maximum, is a normal number, and so are
 // sums of 2^17 of them times values of up to 2^13.  So no maximum is looked for and nothing is rescaled.
 #include <algorithm>
@@ -60,12 +60,14 @@ constexpr size_t SMEM_BYTES = (2 /*Q*/ + KST + VST) * TILE + sizeof(Smem) + 32;
 static_assert(SMEM_BYTES <= 232448, "range forward: shared memory");
 
 struct Params {
-  int B, Hk, G, Sq, Sk, Bm, tpt, nU, nI, splits, n_items;
+  int B, Hk, G, Sq, Sk, Bm, tpt, nU, nI, cut, reps, n_items;
   int group;             // key heads (of all samples) whose items are taken together
-  FastDiv by_splits, by_set, by_group, by_Hk, by_G;      // by_set: items of a group
+  FastDiv by_reps, by_set, by_group, by_Hk, by_G;      // by_set: items of a group
   const int2* rows;
   const int4* units;
   const int* order;
+  const int* head;
+  const int4* work;
   float scale_log2;      // scores -> exp2 domain: scale * log2 e; 1 where they are capped first
   Cap cap;
   __nv_bfloat16 *o, *resid;
@@ -76,7 +78,7 @@ struct Params {
 };
 
 struct Item {
-  int b, hk, u0, nx, split;
+  int b, hk, u0, nx, piece;
   int k_begin, keys;               // first key of the item's tiles, keys in them (0: all masked)
   int ntiles;
   int tb[2], te[2];                // per unit: its tiles
@@ -85,13 +87,25 @@ struct Item {
 
 __device__ __forceinline__ Item decode_item(const Params& p, int item) {
   Item it;
-  const int m = p.by_splits.div(item);
-  it.split = item - m * p.splits;
-  const int set = p.by_set.div(m), r = m - set * p.group * p.nI, rank = p.by_group.div(r), bhk = set * p.group + (r - rank * p.group);
-  it.b = p.by_Hk.div(bhk);
-  it.hk = bhk - it.b * p.Hk;
-  const int bm = mask_batch(p.Bm, it.b);
-  it.u0 = 2 * __ldg(p.order + (long long)bm * p.nI + rank);
+  int bm, first = 0, len = INT32_MAX;
+  it.piece = 0;
+  if (p.cut) {
+    const int entry = p.by_reps.div(item), rep = item - entry * p.reps;
+    const int4 w = __ldg(p.work + entry);
+    bm = w.x;
+    it.b = p.Bm > 1 ? w.x : p.by_Hk.div(rep);
+    it.hk = p.Bm > 1 ? rep : rep - it.b * p.Hk;
+    it.u0 = 2 * w.y;
+    first = w.z;
+    len = __ldg(p.head + 1);
+    it.piece = w.w;
+  } else {
+    const int set = p.by_set.div(item), r = item - set * p.group * p.nI, rank = p.by_group.div(r), bhk = set * p.group + (r - rank * p.group);
+    it.b = p.by_Hk.div(bhk);
+    it.hk = bhk - it.b * p.Hk;
+    bm = mask_batch(p.Bm, it.b);
+    it.u0 = 2 * __ldg(p.order + (long long)bm * p.nI + rank);
+  }
   it.nx = it.u0 + 1 < p.nU ? 2 : 1;
   const int4* units = p.units + (long long)bm * p.nU + it.u0;
   const int4 a = __ldg(units), c = it.nx == 2 ? __ldg(units + 1) : make_int4(0, 0, 0, 0);
@@ -100,13 +114,11 @@ __device__ __forceinline__ Item decode_item(const Params& p, int item) {
     lo = hi > lo ? min(lo, c.x) : c.x;
     hi = max(hi, c.y);
   }
-  const int all = (max(hi - lo, 0) + BN - 1) / BN;
-  int first = 0, last = all;
-  if (p.splits > 1) share(all, it.split, p.splits, first, last);
+  const int all = (max(hi - lo, 0) + BN - 1) / BN, tiles = max(min(len, all - first), 0);
   it.k_begin = lo + first * BN;
-  it.keys = max(min(lo + last * BN, hi) - it.k_begin, 0);
+  it.keys = max(min(tiles * BN, hi - it.k_begin), 0);
   if (it.keys == 0) it.k_begin = 0;
-  it.ntiles = max(last - first, 1);
+  it.ntiles = max(tiles, 1);
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const int4 u = x ? c : a;
@@ -190,7 +202,7 @@ __device__ __forceinline__ void cap32(uint32_t* sv, const Cap& cap) {
   } else {
 #pragma unroll
     for (int i = 0; i < 32; ++i)
-      sv[i] = __float_as_uint(fmaf(-2.0f * cap.c, rcp(1.0f + ex2(__uint_as_float(sv[i]) * cap.twice_a_log2)), cap.c));
+      sv[i] = __float_as_uint(fmaf(-2.0f * cap.c, rcp(1.0f + ex2(__uint_as_float(sv[i]) * cap.twice_log2)), cap.c));
   }
 }
 // 32 scores from key i0 on of a row that sees n keys from key a on: those outside get a value.
@@ -299,6 +311,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sm->tmem_base;
+  const int n_items = p.cut ? __ldg(p.head) * p.reps : p.n_items;
   constexpr uint32_t IDESC_PV = make_idesc_bf16(BM, DH, false, true);
 
   if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -306,7 +319,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     // ------------------------------------------------------------------ TMA producer
     if (lane == 0) {
       uint32_t ks = 0, kp = 1, vs = 0, vp = 1;       // ring slots and the parities of their `empty` waits (the first pass at once)
-      for (int round = 0, item; (item = item_at(round)) < p.n_items; ++round) {
+      for (int round = 0, item; (item = item_at(round)) < n_items; ++round) {
         const Item it = decode_item(p, item);
         for (int t = 0; t < it.ntiles; ++t) {
           const int y = it.k_begin + t * BN;
@@ -334,6 +347,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     // ------------------------------------------------------------------ MMA issuers: the whole warp walks the loop, one elected lane
     // issues (warp-uniform control flow; see elect_one); the lanes look at an operation's barriers at once.
     const bool leader = elect_one();
+    const int n_items_u = __reduce_max_sync(0xffffffffu, n_items);
     auto wait3 = [&](uint64_t* b0, uint32_t p0, uint64_t* b1, uint32_t p1, bool third, uint64_t* b2, uint32_t p2) {
       const int which = lane & 3;
       uint32_t bar = smem_u32(b0), par = p0;
@@ -346,7 +360,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     if (warp == 1) {
       uint32_t uses = 0, n = 0, slot = 0, par = 0;      // uses of the score buffer, items, K ring position
       const uint32_t lo_q = desc_lo(smem_u32(sQ), 16), lo_k = desc_lo(smem_u32(sK), 16);
-      for (int item; (item = item_at((int)n)) < p.n_items; ++n) {
+      for (int item; (item = item_at((int)n)) < n_items_u; ++n) {
         const Item it = uniform_item(p, item);
         bool first = true;
         for (int t = 0; t < it.ntiles; ++t) {
@@ -374,7 +388,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     } else {
       uint32_t tcnt[2] = {0, 0}, ecnt[2] = {0, 0}, slot = 0, par = 0;      // per unit: P V and items done; V ring position
       const uint32_t lo_v = desc_lo(smem_u32(sV), PANEL);
-      for (int round = 0, item; (item = item_at(round)) < p.n_items; ++round) {
+      for (int round = 0, item; (item = item_at(round)) < n_items_u; ++round) {
         const Item it = uniform_item(p, item);
         for (int t = 0; t < it.ntiles; ++t) {
           const int ksteps = key_steps(it, t);
@@ -402,7 +416,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
   } else if (warp == 3) {
     // ------------------------------------------------------------------ V tiles that end inside a step of 16 keys
     uint32_t tiles = 0, par = 0;             // tiles so far; bit s: parity of slot s
-    for (int round = 0, item; (item = item_at(round)) < p.n_items; ++round) {
+    for (int round = 0, item; (item = item_at(round)) < n_items; ++round) {
       const Item it = decode_item(p, item);
       tiles += it.ntiles;
       if (!has_tail(it)) continue;
@@ -432,7 +446,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         const int tok = (it.u0 + x) * p.tpt + rt;
         const bool row_ok = lt < rows && tok < p.Sq;
         const long long head = (long long)it.hk * p.G + rg;
-        const long long packed = ((long long)it.b * p.Hk + it.hk) * p.Sq * p.G + (long long)tok * p.G + rg + it.split * all_rows;
+        const long long packed = ((long long)it.b * p.Hk + it.hk) * p.Sq * p.G + (long long)tok * p.G + rg + it.piece * all_rows;
         tcs[x] += it.te[x] - it.tb[x];
         mbar_wait(&sm->ep_ready[x], eps[x] & 1, abort_flag, p.status);
         eps[x] += 1;
@@ -451,7 +465,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
             mbar_arrive(&sm->o_free[x]);
           }
           if (row_ok) {
-            if (p.splits == 1) {
+            if (!p.cut) {
 #pragma unroll
               for (int i = 0; i < 16; i += 8) {
                 float v[8];
@@ -471,12 +485,12 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
           }
         }
         if (row_ok) {
-          if (p.splits == 1) p.lse[((long long)it.b * p.Hk * p.G + head) * p.Sq + tok] = row_lse;
+          if (!p.cut) p.lse[((long long)it.b * p.Hk * p.G + head) * p.Sq + tok] = row_lse;
           else p.part_lse[packed] = row_lse;
         }
       }
     };
-    for (int item; (item = item_at((int)n)) < p.n_items; ++n) {
+    for (int item; (item = item_at((int)n)) < n_items; ++n) {
       if (lt == 0) {
         const Item it = decode_item(p, item);
         if (n >= 1) mbar_wait(&sm->q_empty, (n - 1) & 1, abort_flag, p.status);
@@ -505,7 +519,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
     const uint32_t p_tmem = tmem + lane_addr + P_COL + x * 64;
     const uint32_t o_tmem = tmem + lane_addr + O_COL + x * 128;
     uint32_t tc = 0, items = 0;                      // key tiles and items done on this unit
-    for (int round = 0, item; (item = item_at(round)) < p.n_items; ++round) {
+    for (int round = 0, item; (item = item_at(round)) < n_items; ++round) {
       const Item it = decode_item(p, item);
       if (x >= it.nx) continue;
       const int tb = it.tb[x], te = it.te[x];
@@ -578,6 +592,8 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
           const int2 r = masked ? seen(t) : make_int2(0, BN);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
+#pragma unroll
+            for (int i = 32 * c; i < 32 * c + 32; ++i) sv[i] = __float_as_uint(__uint_as_float(sv[i]) * p.cap.pre);
             if (masked) mask32(sv + 32 * c, 32 * c, r.x, r.y, 0u);
             cap32(sv + 32 * c, p.cap);
           }
@@ -682,17 +698,20 @@ bool make_tmap_units(CUtensorMap* map, const void* base, const RDims& D, const S
   return sm100::make_tmap_bf16_strided(map, base, 5, n, st, box);
 }
 
-// The polynomial's coefficients with the factors of score and result folded in.  Where that leaves fp32's range (caps of more than some
-// hundred times the scale's usual) every score takes the long way.
+// The polynomials' coefficients with the factors of score and result folded in.  Where the score's would leave fp32's range (caps of some
+// hundred times what is usual, scales far from it) scores are multiplied by it first.
 Cap make_cap(const RDims& D) {
-  static const double k[5] = {0.9999972283, -0.3332307648, 0.1322609162, -0.04928044707, 0.01231883178};
+  static const double k[5] = {0.9999994349, -0.333282515, 0.1325898302, -0.05005629744, 0.01292962787};
   static const double q[4] = {0.9999556007, -0.3322276355, 0.1257709159, -0.03377827421};
   Cap c = {};
   if (!(D.cap > 0.f)) return c;
-  const double a = (double)D.scale / D.cap, top = (double)D.cap * 1.4426950408889634;
+  double a = (double)D.scale / D.cap;
+  const double top = (double)D.cap * 1.4426950408889634;
   c.c = (float)top;
-  c.twice_a_log2 = (float)(2.0 * a * 1.4426950408889634);
-  c.most = a >= 2e-4 && a <= 1e3 && top <= 1e6 ? (float)(0.75 / a) : -1.f;
+  c.pre = 1.f;
+  if (!(a >= 2e-4 && a <= 1e3 && top <= 1e6)) { c.pre = (float)a; a = 1.0; }
+  c.twice_log2 = (float)(2.0 * a * 1.4426950408889634);
+  c.most = (float)(0.75 / a);
   double f = top * a;
   for (int i = 0; i < 5; ++i, f *= a * a) {
     c.p[i] = (float)(k[i] * f);
@@ -712,15 +731,15 @@ static int group_of_heads(const RDims& D) {
 
 int tc_range_fwd(const RDims& D, const Plan& plan, const FwdArgs& a, cudaStream_t st) {
   using namespace tcf;
-  const long long items = (long long)D.B * D.Hk * D.nI * a.splits;
+  const long long items = (long long)D.B * D.Hk * D.nI * D.smax;      // (at most)
   if (items > (long long)INT32_MAX - 4096) return VMOBA_ERR_SHAPE;
   Params p;
   p.B = D.B; p.Hk = D.Hk; p.G = D.G; p.Sq = D.Sq; p.Sk = D.Sk; p.Bm = D.Bm; p.tpt = D.tpt; p.nU = D.nU; p.nI = D.nI;
-  p.splits = a.splits; p.n_items = (int)items;
-  p.rows = plan.rows; p.units = plan.units; p.order = plan.order;
+  p.cut = D.smax > 1; p.reps = D.reps; p.n_items = (int)items;
+  p.rows = plan.rows; p.units = plan.units; p.order = plan.order; p.head = plan.head; p.work = plan.work;
   p.group = group_of_heads(D);
   p.by_set = FastDiv(p.group * D.nI); p.by_group = FastDiv(p.group);
-  p.by_splits = FastDiv(a.splits); p.by_Hk = FastDiv(D.Hk); p.by_G = FastDiv(D.G);
+  p.by_reps = FastDiv(D.reps); p.by_Hk = FastDiv(D.Hk); p.by_G = FastDiv(D.G);
   p.scale_log2 = D.scale * LOG2E;
   p.cap = make_cap(D);
   p.o = (__nv_bfloat16*)a.o; p.resid = (__nv_bfloat16*)a.resid; p.os = a.os; p.lse = a.lse;
@@ -728,7 +747,7 @@ int tc_range_fwd(const RDims& D, const Plan& plan, const FwdArgs& a, cudaStream_
   CUtensorMap tmK, tmV, tmQ;
   if (!make_tmap_keys(&tmK, a.k, D, a.ks) || !make_tmap_keys(&tmV, a.v, D, a.vs) || !make_tmap_units(&tmQ, a.q, D, a.qs)) return VMOBA_ERR_CUDA;
   auto kernel = !(D.cap > 0.f)           ? attn_range_fwd_kernel<kPlain>
-                : p.cap.c <= CAP_MOST ? attn_range_fwd_kernel<kCapped>
+                : p.cap.c <= CAP_MOST && p.cap.pre == 1.f ? attn_range_fwd_kernel<kCapped>
                                       : attn_range_fwd_kernel<kCappedWide>;
   VMOBA_CUDA_OK(allow_smem(kernel, (int)SMEM_BYTES));
   launch_kernel(kernel, (unsigned)std::min<long long>(items, sm_count()), THREADS, SMEM_BYTES, st, tmK, tmV, tmQ, p);

@@ -343,3 +343,18 @@ def test_results_do_not_depend_on_what_ran_before(i, kind):
         run(other, odev, oplace, oh)
         o2, grads2 = run(op, dev, place, host)
         assert torch.equal(o2, o) and all(torch.equal(a, b) for a, b in zip(grads, grads2))
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=lambda k: f"{k[0]}_{k[1]}")
+@pytest.mark.parametrize("cap,scale", [(100.0, 0.0), (700.0, 0.0), (1e6, 0.0), (0.5, 0.0), (30.0, 2.0), (30.0, 1e-6), (0.0, 1.5)])
+def test_caps_and_scales_far_from_the_usual(cap, scale, kind):
+    """Caps that nothing reaches and caps that everything exceeds, scales other than head_dim^-1/2."""
+    dtype, d = kind
+    ranges = key_ranges([100, 111], n_tokens=230, frame=1, device="cpu")
+    _, _, host, dev, place = make(2, 230, 230, 2, 1, d, dtype, ranges, seed=12)
+    shape = vb.make_range_shape(2, 2, 1, d, 230, 230, dtype, softmax_scale=scale, softcap=cap)
+    op = RangeAttention(shape, ranges.cuda(), with_backward=True)
+    ref = P.range_attention(*host[:3], ranges, cap, scale=scale or None, do=host[3])
+    o, grads = run(op, dev, place, host)
+    # (the error of a capped score by the exponential is 3e-7 of the cap where the cap is reached; where it is not, of the score)
+    check_all(ref, dtype, d, min(cap, ref["top"]), o, op.lse, grads)
