@@ -5,12 +5,12 @@
 // Backward: g = the gradient of out turned by -a (times m), then with s = w g:
 //   dx = r (s - x r^2 mean(s x)),   dw = sum over tokens (norm per head: and heads) of g x r.
 //
-// Bound by HBM (a row of a token, all heads, is read once and written once, forward; the gradient, x and dx, backward) and, closely
-// behind, by instruction issue.  So: a row is taken by as few warps as hold it in six 16-byte vectors per thread, each warp or
-// group of warps on its own, token after token; a thread has the same channels of every head, so that its sines and cosines are
-// loaded once per token; angles are worked out once per token for all heads and tensors; layouts and vectors per thread are compiled in.
-// The norm's two trips through a row are one through memory: vectors come in by asynchronous copies into a ring of shared
-// memory that each thread has to itself, rows ahead of their use; rows longer than that are read twice.
+// Bound by HBM (a row of a token, all heads, is read once and written once, forward; the gradient, x and dx, backward), if the
+// instructions are few enough.  So: a row is taken by as few warps as hold it in a few 16-byte vectors per thread, each warp or group of
+// warps on its own, token after token, and stays in registers between the norm's two trips through it, while the next row is on its
+// way; a thread has the same channels of every head, so that its sines and cosines are loaded once per token; angles are
+// worked out once per token for all heads and tensors; the norm's weights lie in shared memory in the order of the registers; even and
+// odd channels are apart, so that pairs turn by packed instructions.  Rows longer than that are read twice.
 // An angle is formed and reduced in 64 bits, because a position of 10^6 times a frequency of one has no digit behind the point left in 32.
 #include <algorithm>
 #include <type_traits>
@@ -25,7 +25,8 @@ using sm100::fma2;
 using sm100::mul2;
 
 constexpr int kMaxTensors = 4;
-constexpr int kMaxWarps = 8;                 // of a CTA, and of a row
+constexpr int kMaxWarps = 8;                 // of a row, and of a CTA
+constexpr int kBwdWarps = 12;                // of the backward's CTAs, one per SM: 168 registers per thread
 constexpr int kMaxPairs = 64;
 
 struct Tensor {
@@ -34,7 +35,16 @@ struct Tensor {
   void* dst;
   const float* w;                            // norm weights or null (ones)
   long long ss[3], xs[3], ds[3];             // element strides {batch, token, head} of src, x and dst
+  unsigned ss1, xs1, ds1;                    // bytes from token to token where samples follow one another at that distance too, else 0
 };
+
+// The row of token g = (b, tok) of a tensor whose first row, from the thread's first channel on, is at `base`.
+template <typename T>
+__device__ __forceinline__ T* row_of(T* base, const long long (&s)[3], unsigned bytes, int g, int b, int tok) {
+  using Byte = typename std::conditional<std::is_const<T>::value, const char, char>::type;
+  if (bytes) return reinterpret_cast<T*>(reinterpret_cast<Byte*>(base) + (unsigned long long)(unsigned)g * bytes);
+  return base + b * s[0] + tok * s[1];
+}
 
 struct Params {
   int B, S, heads, d;
@@ -96,33 +106,81 @@ enum Layout { kInterleaved, kHalf, kHalfAny };
 
 // cos and sin (times mscale) of a token's angles, by the threads of a group: the angle in turns, less whole ones.
 struct alignas(16) Angles { float cs[kMaxPairs], sn[kMaxPairs]; };
-__device__ __forceinline__ void angles(const Params& p, int g, int l, int tpr, Angles* ang) {
-  const int at0 = p.pos_batch > 1 ? g : g - p.by_S.div(g) * p.S;
-#pragma unroll 1
-  for (int pair = l; pair < p.pairs; pair += tpr) {
-    const int at = __ldg(p.pos + (long long)at0 * p.axes + min(max(__ldg(p.axis + pair), 0), p.axes - 1));
-    const double turns = (double)at * __ldg(p.freq + pair) * 0.15915494309189533577;      // 1 / (2 pi)
-    float sn, cs;
-    sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
-    ang->cs[pair] = cs * p.mscale;
-    ang->sn[pair] = sn * p.mscale;
+// The pairs' frequencies in turns and axes, in shared memory, and the positions that a thread's pairs l, l + tpr (there are at most 64, and 32
+// threads at least) take them at.
+struct Frequencies { double f[kMaxPairs]; int axis[kMaxPairs]; };
+__device__ __forceinline__ void stage_frequencies(const Params& p, Frequencies* to) {
+  for (int i = threadIdx.x; i < p.pairs; i += blockDim.x) {
+    to->f[i] = __ldg(p.freq + i) * 0.15915494309189533577;      // 1 / (2 pi)
+    to->axis[i] = min(max(__ldg(p.axis + i), 0), p.axes - 1);
   }
 }
+struct Positions {
+  int at[2];
+  __device__ __forceinline__ void load(const Params& p, const Frequencies& f, int g, int l, int tpr) {
+    const int at0 = p.pos_batch > 1 ? g : g - p.by_S.div(g) * p.S;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (l + j * tpr < p.pairs) at[j] = __ldg(p.pos + (long long)at0 * p.axes + f.axis[l + j * tpr]);
+  }
+  __device__ __forceinline__ void angles(const Params& p, const Frequencies& f, int l, int tpr, Angles* ang) const {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int i = l + j * tpr;
+      if (i >= p.pairs) continue;
+      const double turns = (double)at[j] * f.f[i];
+      float sn, cs;
+      sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+      ang->cs[i] = cs * p.mscale;
+      ang->sn[i] = sn * p.mscale;
+    }
+  }
+};
 
-// A thread's ring: kDepth rows of its vectors.
-constexpr int kDepth = 2;
-__device__ __forceinline__ void copy16(uint4* to, const void* from, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(there ? 16u : 0u) : "memory");
+// The channel, of a vector's, that a thread holds in place e: even ones ahead of odd ones where those are a pair.
+template <int E, Layout L>
+__device__ __forceinline__ constexpr int channel(int e) { return L != kInterleaved ? e : e < E / 2 ? 2 * e : 2 * e - E + 1; }
+
+template <typename T, Layout L>
+struct Row {
+  static constexpr int E = Vec<T>::E;
+  static __device__ __forceinline__ void unpack(const uint4& u, float (&x)[E]) {
+    float y[E];
+    Vec<T>::unpack(u, y);
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = y[channel<E, L>(e)];
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[E]) {
+    float y[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[channel<E, L>(e)] = x[e];
+    return Vec<T>::pack(y);
+  }
+};
+
+// sum += a . b
+template <int E>
+__device__ __forceinline__ void dot(const float (&a)[E], const float (&b)[E], float& s0, float& s1) {
+#pragma unroll
+  for (int e = 0; e < E; e += 2) fma2(s0, s1, a[e], a[e + 1], b[e], b[e + 1], s0, s1);
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <int E>
+__device__ __forceinline__ void times(float (&a)[E], const float (&b)[E]) {
+#pragma unroll
+  for (int e = 0; e < E; e += 2) mul2(a[e], a[e + 1], a[e], a[e + 1], b[e], b[e + 1]);
+}
+template <int E>
+__device__ __forceinline__ void times(float (&a)[E], float b) {
+#pragma unroll
+  for (int e = 0; e < E; e += 2) mul2(a[e], a[e + 1], a[e], a[e + 1], b, b);
+}
 
 // What a thread's vectors, all of the same channels c0 .. c0 + E - 1 of a head, are turned by.  sign: -1 turns back.
 template <int E, Layout L>
 struct Turn {
-  float cs[L == kInterleaved ? E / 2 : E], sn[L == kInterleaved ? E / 2 : E];
-  uint32_t mine;                             // bit e: channel c0 + e belongs to a pair
+  static constexpr int N = L == kInterleaved ? E / 2 : E;
+  float cs[N], sn[N];
+  uint32_t mine;                             // bit e: the channel in place e belongs to a pair
   __device__ __forceinline__ void load(const Params& p, const Angles& a, int c0, float sign) {
     mine = 0;
     if constexpr (L == kInterleaved) {
@@ -135,8 +193,10 @@ struct Turn {
         cs[0] = c.x; cs[1] = c.y;
         sn[0] = s.x * sign; sn[1] = s.y * sign;
       }
-      const int n = 2 * p.pairs - c0;
-      mine = n <= 0 ? 0u : n >= E ? (1u << E) - 1u : (1u << n) - 1u;
+      if (!p.full) {
+        const int n = min(max(p.pairs - c0 / 2, 0), N);
+        mine = ((1u << n) - 1u) * ((1u << N) + 1u);
+      }
     } else if constexpr (L == kHalf) {
       const bool second = c0 >= p.pairs;
       const int i = second ? c0 - p.pairs : c0;
@@ -161,22 +221,32 @@ struct Turn {
       }
     }
   }
-  // buf (kHalfAny): 32 * E floats of the warp.  Called by whole warps.
-  __device__ __forceinline__ void apply(const Params& p, float (&y)[E], int c0, float* buf) const {
+  // Turns a vector and multiplies it by r.  buf (kHalfAny): 32 * E floats of the warp.  Called by whole warps.
+  __device__ __forceinline__ void apply(const Params& p, float (&y)[E], float r, int c0, float* buf) const {
     if constexpr (L == kInterleaved) {
-      auto turned = [&](bool all) {
+      if (p.full) {
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) {
-          const float y0 = y[2 * i], y1 = y[2 * i + 1];
-          if (all || (mine >> (2 * i) & 1)) {
-            y[2 * i] = fmaf(y0, cs[i], -y1 * sn[i]);
-            y[2 * i + 1] = fmaf(y1, cs[i], y0 * sn[i]);
+        for (int i = 0; i < N; i += 2) {     // (r times sine and cosine: the same of every vector of a row)
+          const float c0 = cs[i] * r, c1 = cs[i + 1] * r, s0 = sn[i] * r, s1 = sn[i + 1] * r;
+          float t0, t1, u0, u1;
+          mul2(t0, t1, y[N + i], y[N + i + 1], -s0, -s1);
+          mul2(u0, u1, y[i], y[i + 1], s0, s1);
+          fma2(y[i], y[i + 1], y[i], y[i + 1], c0, c1, t0, t1);
+          fma2(y[N + i], y[N + i + 1], y[N + i], y[N + i + 1], c0, c1, u0, u1);
+        }
+      } else {
+        times<E>(y, r);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float y0 = y[i], y1 = y[N + i];
+          if (mine >> i & 1) {
+            y[i] = fmaf(y0, cs[i], -y1 * sn[i]);
+            y[N + i] = fmaf(y1, cs[i], y0 * sn[i]);
           }
         }
-      };
-      if (p.full) turned(true);
-      else turned(false);
+      }
     } else {
+      times<E>(y, r);
       float o[E];
       const int lane = threadIdx.x & 31;
       if constexpr (L == kHalf) {            // the partners of a vector are a vector of another lane of the same head
@@ -193,7 +263,10 @@ struct Turn {
       }
       if (p.full) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = fmaf(y[e], cs[e], o[e] * sn[e]);
+        for (int e = 0; e < E; e += 2) {
+          mul2(o[e], o[e + 1], o[e], o[e + 1], sn[e], sn[e + 1]);
+          fma2(y[e], y[e + 1], y[e], y[e + 1], cs[e], cs[e + 1], o[e], o[e + 1]);
+        }
       } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -209,13 +282,14 @@ __device__ __forceinline__ void meet(int group, int wpr) {
   else asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * wpr) : "memory");
 }
 
-// Sum over the threads of a row.  slot: a pair of floats per warp of the group; the next call takes another one (a call that takes
-// this one again is two barriers away).
+// Sums over the threads of a row, of one value or two.  slot: a pair of floats per warp of the group; the next call takes another one (a
+// call that takes this one again is two barriers away).
+template <bool TWO>
 __device__ __forceinline__ float2 row_sum(float2 v, int group, int wpr, float2* slot) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+    if (TWO) v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
   }
   if (wpr == 1) return v;
   if ((threadIdx.x & 31) == 0) slot[(threadIdx.x >> 5) - group * wpr] = v;
@@ -224,170 +298,270 @@ __device__ __forceinline__ float2 row_sum(float2 v, int group, int wpr, float2* 
   for (int w = 0; w < wpr; ++w) { a.x += slot[w].x; a.y += slot[w].y; }
   return a;
 }
-__device__ __forceinline__ float2 head_sum(float2 v, int lanes) {
-  for (int o = lanes >> 1; o > 0; o >>= 1) {
-    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-  }
-  return v;
+// Sums over the lanes of a head, of N vectors.
+template <int N>
+__device__ __forceinline__ void head_sums(float (&v)[N], int lanes) {
+#pragma unroll 1
+  for (int o = lanes >> 1; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
 }
 
+// The norm's weights in shared memory, in the order of a thread's registers: of `tensors` tensors, planes of four of a vector's E weights,
+// `count` vectors each, of which `there` exist.  Ones where there are none.
+template <int E, Layout L>
+__device__ __forceinline__ void stage_weights(float4* to, const Tensor* t, int tensors, int count, int there) {
+  constexpr int P = E / 4;
+  for (int i = threadIdx.x; i < tensors * P * count; i += blockDim.x) {
+    const int v = i % count, plane = i / count % P, k = i / (count * P);
+    const float* w = t[k].w && v < there ? t[k].w + v * E : nullptr;
+    float f[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int low = channel<E, L>(e), high = channel<E, L>(E - 4 + e);
+      f[e] = w ? __ldg(w + (plane ? high : low)) : 1.f;
+    }
+    to[i] = make_float4(f[0], f[1], f[2], f[3]);
+  }
+}
 template <int E>
-__device__ __forceinline__ void weights(const float* w, float (&x)[E]) {
+__device__ __forceinline__ void staged_weights(const float4* from, int count, float (&f)[E]) {
 #pragma unroll
   for (int e = 0; e < E; e += 4) {
-    const float4 v = w ? __ldg(reinterpret_cast<const float4*>(w + e)) : make_float4(1.f, 1.f, 1.f, 1.f);
-    x[e] = v.x; x[e + 1] = v.y; x[e + 2] = v.z; x[e + 3] = v.w;
+    const float4 v = from[e / 4 * count];
+    f[e] = v.x; f[e + 1] = v.y; f[e + 2] = v.z; f[e + 3] = v.w;
   }
 }
-
-// sum += a . b
-template <int E>
-__device__ __forceinline__ void dot(const float (&a)[E], const float (&b)[E], float& s0, float& s1) {
+template <int E, Layout L>
+__device__ __forceinline__ void weights(const float* w, float (&f)[E]) {      // (from global memory)
 #pragma unroll
-  for (int e = 0; e < E; e += 2) fma2(s0, s1, a[e], a[e + 1], b[e], b[e + 1], s0, s1);
-}
-template <int E>
-__device__ __forceinline__ void times(float (&a)[E], const float (&b)[E]) {
-#pragma unroll
-  for (int e = 0; e < E; e += 2) mul2(a[e], a[e + 1], a[e], a[e + 1], b[e], b[e + 1]);
-}
-template <int E>
-__device__ __forceinline__ void times(float (&a)[E], float b) {
-#pragma unroll
-  for (int e = 0; e < E; e += 2) mul2(a[e], a[e + 1], a[e], a[e + 1], b, b);
+  for (int e = 0; e < E; ++e) f[e] = w ? __ldg(w + channel<E, L>(e)) : 1.f;
 }
 
 // ------------------------------------------------------------------------------ forward
-// ONCE: the row fits the group's threads; else it is walked in trips, from global memory.
-template <typename T, Layout L, int NV, bool ONCE>
-__global__ void __launch_bounds__(32 * kMaxWarps, 3)
+// A thread's place in a row: the vectors l, l + tpr, ... of all heads, the same channels of each.
+struct Place {
+  int group, l, tpr, V, nvec, c0, vshift, head0, heads_per;
+  __device__ __forceinline__ Place(const Params& p, int E) {
+    group = (int)(threadIdx.x >> 5) / p.wpr;
+    tpr = 32 * p.wpr;
+    l = threadIdx.x - group * tpr;
+    V = p.d / E;
+    nvec = p.heads * V;
+    c0 = (l % V) * E;
+    vshift = 31 - __clz(V);
+    head0 = l >> vshift;
+    heads_per = tpr >> vshift;
+  }
+};
+
+// Rows that a group's threads hold in NV vectors each: 128 registers for six of them and the next row's, 16 warps per SM.
+// q, k, v of 32,760 tokens x 12 heads of 128 into block order, 402 MB: 73 us (with a ring of asynchronous copies in shared memory, 883 instructions
+// per row instead of 411: 90); of 75,600 tokens x 40 heads, 3.1 GB: 549 us.
+template <typename T, Layout L, int NV>
+__global__ void __launch_bounds__(32 * kMaxWarps, 2)
 rotary_fwd_kernel(const __grid_constant__ Params p) {
   if (!grid_begin()) return;
   constexpr int E = Vec<T>::E;
-  extern __shared__ __align__(16) uint4 ring[];                      // [kDepth][NV][threads]
+  extern __shared__ __align__(16) float4 w_all[];
+  __shared__ Frequencies freq;
   __shared__ Angles ang[kMaxWarps][2];
   __shared__ float2 slot[2][kMaxWarps];
   __shared__ float exchange[L == kHalfAny ? kMaxWarps * 32 * E : 1];
-  const int warp = threadIdx.x >> 5, group = warp / p.wpr, tpr = 32 * p.wpr, l = threadIdx.x - group * tpr, threads = blockDim.x;
-  float* buf = L == kHalfAny ? exchange + warp * 32 * E : exchange;
-  uint4* mine = ring + threadIdx.x;
-  const int V = p.d / E, nvec = p.heads * V, c0 = (l % V) * E, vshift = 31 - __clz(V), head0 = l >> vshift, heads_per = tpr >> vshift;
-  const int per = NV * tpr;                  // vectors of a trip through a row
+  const Place at(p, E);
+  const int l = at.l, tpr = at.tpr, group = at.group, c0 = at.c0;
+  float* buf = L == kHalfAny ? exchange + (threadIdx.x >> 5) * 32 * E : exchange;
+  const bool by_row = p.norm == VMOBA_ROTARY_NORM_ROW;
+  const int n_w = by_row ? NV * tpr : at.V;
+  stage_frequencies(p, &freq);
+  if (p.norm != VMOBA_ROTARY_NORM_NONE) stage_weights<E, L>(w_all, p.t, p.turned, n_w, by_row ? at.nvec : at.V);
+  __syncthreads();
+  const float inv_n = 1.0f / (float)(by_row ? p.heads * p.d : p.d);
+  const int have = l < at.nvec ? (at.nvec - l + tpr - 1) / tpr : 0;      // vectors of this thread
   const int tokens = p.B * p.S, step = gridDim.x * p.groups;
-  // The row of (token, tensor): this thread's first vector.
-  auto src_row = [&](int g, int k) {
-    const Tensor& t = p.t[k];
-    const int b = p.by_S.div(g);
-    return reinterpret_cast<const T*>(t.src) + b * t.ss[0] + (long long)(g - b * p.S) * t.ss[1] + head0 * t.ss[2] + c0;
-  };
   int g = blockIdx.x * p.groups + group;
   if (g >= tokens) return;                   // (whole groups)
-  int ga = g, ka = p.n - 1;                  // the next row to ask for
-  uint4* in = mine;                          // and its place
-  auto ask = [&]() {
-    if (ONCE) {
-      if (ga < tokens) {
-        const T* at = src_row(ga, ka);
-        const long long apart = heads_per * p.t[ka].ss[2];
+  uint4 next[NV];                            // the next row (those that the thread does not have stay zero)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const bool there = l + i * tpr < nvec;
-          copy16(in + i * threads, there ? at : reinterpret_cast<const T*>(p.t[ka].src), there);
-          at += apart;
-        }
-        if (--ka < 0) { ka = p.n - 1; ga += step; }
-      }
-      copies_commit();
-      in = in == mine ? mine + NV * threads : mine;      // (kDepth = 2)
+  for (int i = 0; i < NV; ++i) next[i] = make_uint4(0u, 0u, 0u, 0u);
+  auto fetch = [&](int g, int k) {
+    if (g >= tokens) return;
+    const Tensor& t = p.t[k];
+    const int b = p.by_S.div(g);
+    const T* from = row_of(reinterpret_cast<const T*>(t.src) + at.head0 * t.ss[2] + c0, t.ss, t.ss1, g, b, g - b * p.S);
+    const long long apart = at.heads_per * t.ss[2];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (i < have) next[i] = __ldcs(reinterpret_cast<const uint4*>(from));
+      from += apart;
     }
   };
-  ask();
-  ask();
-  angles(p, g, l, tpr, &ang[group][0]);
+  fetch(g, p.n - 1);
+  Positions positions;
+  positions.load(p, freq, g, l, tpr);
+  positions.angles(p, freq, l, tpr, &ang[group][0]);
   int turn_buf = 0, sum_buf = 0;
-  const uint4* row = mine;
   for (; g < tokens; g += step, turn_buf ^= 1) {
     meet(group, p.wpr);                      // (this token's angles)
     Turn<E, L> turn;
     turn.load(p, ang[group][turn_buf], c0, 1.f);
+    if (g + step < tokens) positions.load(p, freq, g + step, l, tpr);
     const int b = p.by_S.div(g), tok = g - b * p.S, bm = p.dst_bm || p.perm ? block_pos(p, tok) : 0;
     if (p.perm && b == 0 && l == 0) p.perm[bm] = tok;
     // tensors from the last to the first: what the caller reads next comes last
 #pragma unroll 1
     for (int k = p.n - 1; k >= 0; --k) {
-      if (ONCE) copies_wait<kDepth - 1>();
       const Tensor& t = p.t[k];
-      auto vec = [&](int v0, int i) {
-        if (ONCE) return row[i * threads];
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (v0 + l + i * tpr < nvec) x = __ldcg(reinterpret_cast<const uint4*>(src_row(g, k) + ((v0 >> vshift) + i * heads_per) * t.ss[2]));
-        return x;
+      const long long to_head = p.dst_bm ? (long long)p.S * p.d : t.ds[2], to_next = at.heads_per * to_head;
+      T* dst = reinterpret_cast<T*>(t.dst) + at.head0 * to_head + c0;
+      dst = p.dst_bm ? dst + (unsigned long long)(unsigned)(b * p.heads * p.S + bm) * (unsigned)p.d : row_of(dst, t.ds, t.ds1, g, b, tok);
+      const int gn = k > 0 ? g : g + step, kn = k > 0 ? k - 1 : p.n - 1;
+      if (k >= p.turned) {                   // only moved
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          if (i < have) *reinterpret_cast<uint4*>(dst) = next[i];
+          dst += to_next;
+        }
+        fetch(gn, kn);
+        continue;
+      }
+      float y[NV][E];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) Row<T, L>::unpack(next[i], y[i]);
+      fetch(gn, kn);
+      auto put = [&](int i) {
+        if (i < have) *reinterpret_cast<uint4*>(dst) = Row<T, L>::pack(y[i]);
+        dst += to_next;
+      };
+      if (by_row) {
+        float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) dot<E>(y[i], y[i], s0, s1);
+        const float r = rsqrtf(fmaf(row_sum<false>(make_float2(s0 + s1, 0.f), group, p.wpr, slot[sum_buf] + group * p.wpr).x, inv_n, p.eps));
+        sum_buf ^= 1;
+        const float4* w = w_all + k * (E / 4) * n_w + l;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          float f[E];
+          staged_weights<E>(w + i * tpr, n_w, f);
+          times<E>(y[i], f);
+          turn.apply(p, y[i], r, c0, buf);
+          put(i);
+        }
+      } else if (p.norm == VMOBA_ROTARY_NORM_HEAD) {
+        float f[E], sums[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          float s0 = 0.f, s1 = 0.f;
+          dot<E>(y[i], y[i], s0, s1);
+          sums[i] = s0 + s1;
+        }
+        head_sums<NV>(sums, at.V);
+        staged_weights<E>(w_all + k * (E / 4) * n_w + c0 / E, n_w, f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          times<E>(y[i], rsqrtf(fmaf(sums[i], inv_n, p.eps)));
+          times<E>(y[i], f);
+          turn.apply(p, y[i], 1.f, c0, buf);
+          put(i);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          turn.apply(p, y[i], 1.f, c0, buf);
+          put(i);
+        }
+      }
+    }
+    if (g + step < tokens) positions.angles(p, freq, l, tpr, &ang[group][turn_buf ^ 1]);
+  }
+}
+
+// Longer rows: a CTA each, in trips of four vectors per thread, read once for the norm and once more for the result.
+constexpr int kTrip = 4;
+template <typename T, Layout L>
+__global__ void __launch_bounds__(32 * kMaxWarps)
+rotary_fwd_long_kernel(const __grid_constant__ Params p) {
+  if (!grid_begin()) return;
+  constexpr int E = Vec<T>::E;
+  __shared__ Frequencies freq;
+  __shared__ Angles ang[2];
+  __shared__ float2 slot[2][kMaxWarps];
+  __shared__ float exchange[L == kHalfAny ? kMaxWarps * 32 * E : 1];
+  const Place at(p, E);
+  const int l = at.l, tpr = at.tpr, c0 = at.c0;
+  float* buf = L == kHalfAny ? exchange + (threadIdx.x >> 5) * 32 * E : exchange;
+  const bool by_row = p.norm == VMOBA_ROTARY_NORM_ROW;
+  Positions positions;
+  stage_frequencies(p, &freq);
+  __syncthreads();
+  int turn_buf = 0, sum_buf = 0;
+  for (int g = blockIdx.x; g < p.B * p.S; g += gridDim.x, turn_buf ^= 1) {
+    positions.load(p, freq, g, l, tpr);
+    positions.angles(p, freq, l, tpr, &ang[turn_buf]);
+    meet(0, p.wpr);
+    Turn<E, L> turn;
+    turn.load(p, ang[turn_buf], c0, 1.f);
+    const int b = p.by_S.div(g), tok = g - b * p.S, bm = p.dst_bm || p.perm ? block_pos(p, tok) : 0;
+    if (p.perm && b == 0 && l == 0) p.perm[bm] = tok;
+#pragma unroll 1
+    for (int k = p.n - 1; k >= 0; --k) {
+      const Tensor& t = p.t[k];
+      const T* src = row_of(reinterpret_cast<const T*>(t.src) + at.head0 * t.ss[2] + c0, t.ss, t.ss1, g, b, tok);
+      const long long to_head = p.dst_bm ? (long long)p.S * p.d : t.ds[2];
+      T* dst = reinterpret_cast<T*>(t.dst) + at.head0 * to_head + c0;
+      dst = p.dst_bm ? dst + (unsigned long long)(unsigned)(b * p.heads * p.S + bm) * (unsigned)p.d : row_of(dst, t.ds, t.ds1, g, b, tok);
+      uint4 u[kTrip];
+      auto fetch = [&](int v0) {
+#pragma unroll
+        for (int i = 0; i < kTrip; ++i) {
+          u[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (v0 + l + i * tpr < at.nvec) u[i] = __ldcg(reinterpret_cast<const uint4*>(src + ((v0 >> at.vshift) + i * at.heads_per) * t.ss[2]));
+        }
       };
       const bool turned = k < p.turned;
-      const int norm = turned ? p.norm : VMOBA_ROTARY_NORM_NONE;
-      float r_row = 1.f;
-      if (norm == VMOBA_ROTARY_NORM_ROW) {
+      float r = 1.f;
+      if (turned && by_row) {
         float s0 = 0.f, s1 = 0.f;
-        for (int v0 = 0; v0 < nvec; v0 += per) {
+        for (int v0 = 0; v0 < at.nvec; v0 += kTrip * tpr) {
+          fetch(v0);
 #pragma unroll
-          for (int i = 0; i < NV; ++i) {
+          for (int i = 0; i < kTrip; ++i) {
             float x[E];
-            Vec<T>::unpack(vec(v0, i), x);
+            Vec<T>::unpack(u[i], x);
             dot<E>(x, x, s0, s1);
           }
-          if (ONCE) break;
         }
-        r_row = rsqrtf(row_sum(make_float2(s0 + s1, 0.f), group, p.wpr, slot[sum_buf] + group * p.wpr).x / (float)(p.heads * p.d) + p.eps);
+        r = rsqrtf(row_sum<false>(make_float2(s0 + s1, 0.f), 0, p.wpr, slot[sum_buf]).x / (float)(p.heads * p.d) + p.eps);
         sum_buf ^= 1;
       }
-      if (k == 0 && g + step < tokens) angles(p, g + step, l, tpr, &ang[group][turn_buf ^ 1]);
-      const long long to_head = p.dst_bm ? (long long)p.S * p.d : t.ds[2], to_next = heads_per * to_head;
-      T* dst = reinterpret_cast<T*>(t.dst) + (p.dst_bm ? ((long long)b * p.heads * p.S + bm) * p.d : b * t.ds[0] + tok * t.ds[1]) +
-               head0 * to_head + c0;
-      // the vectors of a trip, each through f
-      auto each = [&](auto f) {
-        for (int v0 = 0; v0 < nvec; v0 += per) {
-          const float* w = t.w ? t.w + (norm == VMOBA_ROTARY_NORM_ROW ? (v0 + l) * E : c0) : nullptr;
+      for (int v0 = 0; v0 < at.nvec; v0 += kTrip * tpr) {
+        fetch(v0);
 #pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            const bool there = v0 + l + i * tpr < nvec;
-            if (__any_sync(0xffffffffu, there)) {
-              float y[E];
-              Vec<T>::unpack(vec(v0, i), y);
-              f(y, there ? w : nullptr);
-              if (there) *reinterpret_cast<uint4*>(dst) = Vec<T>::pack(y);
+        for (int i = 0; i < kTrip; ++i) {
+          const int v = v0 + l + i * tpr;
+          const bool there = v < at.nvec;
+          float y[E];
+          Row<T, L>::unpack(u[i], y);
+          if (turned) {
+            if (p.norm != VMOBA_ROTARY_NORM_NONE) {
+              float f[E];
+              weights<E, L>(t.w && there ? t.w + (by_row ? v * E : c0) : nullptr, f);
+              if (!by_row) {
+                float s[1], s1 = 0.f;
+                s[0] = 0.f;
+                dot<E>(y, y, s[0], s1);
+                s[0] += s1;
+                head_sums<1>(s, at.V);
+                times<E>(y, rsqrtf(s[0] / (float)p.d + p.eps));
+              }
+              times<E>(y, f);
             }
-            dst += to_next;
-            if (w && norm == VMOBA_ROTARY_NORM_ROW) w += tpr * E;
+            turn.apply(p, y, r, c0, buf);
           }
-          if (ONCE) break;
+          if (there) *reinterpret_cast<uint4*>(dst + ((v0 >> at.vshift) + i * at.heads_per) * to_head) = Row<T, L>::pack(y);
         }
-      };
-      if (!turned) {
-        each([&](float (&)[E], const float*) {});
-      } else if (norm == VMOBA_ROTARY_NORM_ROW) {
-        each([&](float (&y)[E], const float* w) {
-          float f[E];
-          weights<E>(w, f);
-          times<E>(y, r_row);
-          times<E>(y, f);
-          turn.apply(p, y, c0, buf);
-        });
-      } else if (norm == VMOBA_ROTARY_NORM_HEAD) {
-        each([&](float (&y)[E], const float* w) {
-          float f[E], s0 = 0.f, s1 = 0.f;
-          dot<E>(y, y, s0, s1);
-          weights<E>(w, f);
-          times<E>(y, rsqrtf(head_sum(make_float2(s0 + s1, 0.f), V).x / (float)p.d + p.eps));
-          times<E>(y, f);
-          turn.apply(p, y, c0, buf);
-        });
-      } else {
-        each([&](float (&y)[E], const float*) { turn.apply(p, y, c0, buf); });
       }
-      row = row == mine ? mine + NV * threads : mine;
-      ask();                                 // (into the place of the row that has just been read)
     }
   }
 }
@@ -396,203 +570,322 @@ rotary_fwd_kernel(const __grid_constant__ Params p) {
 // blockIdx.y: tensor.  A thread has the same channels in every row that its group takes, and keeps their part of dw in registers (rows
 // longer than that: in shared memory).  The parts of a CTA's groups, and of the CTAs (weight_sum_kernel), are added up in a
 // fixed order: the results repeat bit for bit.
-template <typename T, Layout L, int NV, bool ONCE>
-__global__ void __launch_bounds__(32 * kMaxWarps, 2)
+struct Gradients {                           // a tensor's rows, from a thread's first head on
+  const Params& p;
+  const Tensor& t;
+  const Place& at;
+  long long d_head;
+  __device__ __forceinline__ Gradients(const Params& p, const Tensor& t, const Place& at)
+      : p(p), t(t), at(at), d_head(p.src_bm ? (long long)p.S * p.d : t.ss[2]) {}
+  template <typename T>
+  __device__ __forceinline__ const T* d(int g, int b, int tok) const {
+    const T* from = reinterpret_cast<const T*>(t.src) + at.head0 * d_head + at.c0;
+    if (p.src_bm) return from + (unsigned long long)(unsigned)(b * p.heads * p.S + block_pos(p, tok)) * (unsigned)p.d;
+    return row_of(from, t.ss, t.ss1, g, b, tok);
+  }
+  template <typename T>
+  __device__ __forceinline__ const T* x(int g, int b, int tok) const {
+    return row_of(reinterpret_cast<const T*>(t.x) + at.head0 * t.xs[2] + at.c0, t.xs, t.xs1, g, b, tok);
+  }
+  template <typename T>
+  __device__ __forceinline__ T* dx(int g, int b, int tok) const {
+    return row_of(reinterpret_cast<T*>(t.dst) + at.head0 * t.ds[2] + at.c0, t.ds, t.ds1, g, b, tok);
+  }
+};
+// g -> dx, given x r: f g r - (x r) back, back = r^2 mean(x f g);  acc += g x r.
+template <int E>
+__device__ __forceinline__ void finish(float (&g)[E], const float (&xr)[E], const float (&f)[E], float r, float back, float (&acc)[E]) {
+#pragma unroll
+  for (int e = 0; e < E; e += 2) {
+    fma2(acc[e], acc[e + 1], g[e], g[e + 1], xr[e], xr[e + 1], acc[e], acc[e + 1]);
+    mul2(g[e], g[e + 1], g[e], g[e + 1], f[e], f[e + 1]);
+    mul2(g[e], g[e + 1], g[e], g[e + 1], r, r);
+    fma2(g[e], g[e + 1], xr[e], xr[e + 1], -back, -back, g[e], g[e + 1]);
+  }
+}
+// x . x and x . (g f)
+template <int E>
+__device__ __forceinline__ void sums_of(const float (&x)[E], const float (&g)[E], const float (&f)[E], float (&s)[4]) {
+  dot<E>(x, x, s[0], s[1]);
+#pragma unroll
+  for (int e = 0; e < E; e += 2) {
+    float a, b;
+    mul2(a, b, g[e], g[e + 1], f[e], f[e + 1]);
+    fma2(s[2], s[3], x[e], x[e + 1], a, b, s[2], s[3]);
+  }
+}
+
+// Keeps the compiler from carrying what it has made of u.
+__device__ __forceinline__ void opaque(uint4& u) { asm volatile("" : "+r"(u.x), "+r"(u.y), "+r"(u.z), "+r"(u.w)); }
+
+// Rows that a group's threads hold in NV vectors each: three of the gradient, x and dw, and the next row's two, in 168 registers, 12 warps per SM.
+// q, k of 32,760 tokens x 12 heads of 128, norm per row, 604 MB: 131 us (128 registers and 16 warps: 156, the reloads of 40 registers per row).
+template <typename T, Layout L, int NV>
+__global__ void __launch_bounds__(32 * kBwdWarps, 1)
 rotary_bwd_kernel(const __grid_constant__ Params p) {
   if (!grid_begin()) return;
   constexpr int E = Vec<T>::E;
-  extern __shared__ __align__(16) uint4 ring[];                      // [kDepth][dy, x][NV][threads]; then, or instead, [group][heads * d]
-  float* acc_row = reinterpret_cast<float*>(ring);
-  __shared__ Angles ang[kMaxWarps][2];
-  __shared__ float2 slot[2][kMaxWarps];
-  __shared__ float exchange[kMaxWarps * 32 * E];
-  const int warp = threadIdx.x >> 5, group = warp / p.wpr, tpr = 32 * p.wpr, l = threadIdx.x - group * tpr, threads = blockDim.x;
-  float* buf = exchange + warp * 32 * E;
-  uint4* mine = ring + threadIdx.x;
-  const int V = p.d / E, nvec = p.heads * V, c0 = (l % V) * E, vshift = 31 - __clz(V), head0 = l >> vshift, heads_per = tpr >> vshift;
-  const int per = NV * tpr;
+  extern __shared__ __align__(16) float4 w_all[];                    // the weights; at the end [group][heads * d] sums
+  __shared__ Frequencies freq;
+  __shared__ Angles ang[kBwdWarps][2];
+  __shared__ float2 slot[2][kBwdWarps];
+  __shared__ float exchange[kBwdWarps * 32 * E];
+  const Place at(p, E);
+  const int l = at.l, tpr = at.tpr, group = at.group, c0 = at.c0;
+  float* buf = exchange + (threadIdx.x >> 5) * 32 * E;
   const Tensor& t = p.t[blockIdx.y];
-  const int tokens = p.B * p.S, step = gridDim.x * p.groups;
-  const bool by_row = p.norm == VMOBA_ROTARY_NORM_ROW, by_head = p.norm == VMOBA_ROTARY_NORM_HEAD, normed = by_row || by_head;
-  const int row_ch = p.heads * p.d;
+  const bool by_row = p.norm == VMOBA_ROTARY_NORM_ROW, normed = p.norm != VMOBA_ROTARY_NORM_NONE;
+  const int row_ch = p.heads * p.d, n_w = by_row ? NV * tpr : at.V;
   const float inv_n = 1.0f / (float)(by_row ? row_ch : p.d);
-  float acc[NV][E];
+  const float4* w_mine = w_all + (by_row ? l : c0 / E);
+  stage_frequencies(p, &freq);
+  if (normed) stage_weights<E, L>(w_all, &t, 1, n_w, by_row ? at.nvec : at.V);
+  __syncthreads();
+  float acc[NV][E];                          // (norm per head: all in acc[0])
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[i][e] = 0.f;
-  float* mine_acc = acc_row + (long long)group * row_ch;
-  if (by_row && !ONCE)
-    for (int i = l; i < row_ch; i += tpr) mine_acc[i] = 0.f;
-  const long long d_head = p.src_bm ? (long long)p.S * p.d : t.ss[2];
-  auto d_row = [&](int g) {
-    const int b = p.by_S.div(g), tok = g - b * p.S;
-    return reinterpret_cast<const T*>(t.src) + (p.src_bm ? ((long long)b * p.heads * p.S + block_pos(p, tok)) * p.d : b * t.ss[0] + tok * t.ss[1]) +
-           head0 * d_head + c0;
-  };
-  auto x_row = [&](int g) {
-    const int b = p.by_S.div(g), tok = g - b * p.S;
-    return reinterpret_cast<const T*>(t.x) + b * t.xs[0] + tok * t.xs[1] + head0 * t.xs[2] + c0;
-  };
+  const Gradients rows(p, t, at);
+  const int have = l < at.nvec ? (at.nvec - l + tpr - 1) / tpr : 0;
+  const int tokens = p.B * p.S, step = gridDim.x * p.groups;
   int g = blockIdx.x * p.groups + group;
   if (g < tokens) {                          // (whole groups; all threads meet again at the end)
-    int ga = g;
-    uint4* in = mine;
-    auto ask = [&]() {
-      if (ONCE) {
-        if (ga < tokens) {
-          const T *d = d_row(ga), *x = normed ? x_row(ga) : nullptr;
+    uint4 next_d[NV], next_x[NV];
 #pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            const bool there = l + i * tpr < nvec;
-            copy16(in + i * threads, there ? d : reinterpret_cast<const T*>(t.src), there);
-            if (normed) copy16(in + (NV + i) * threads, there ? x : reinterpret_cast<const T*>(t.x), there);
-            d += heads_per * d_head;
-            x += heads_per * t.xs[2];
-          }
-          ga += step;
+    for (int i = 0; i < NV; ++i) next_d[i] = next_x[i] = make_uint4(0u, 0u, 0u, 0u);
+    auto fetch = [&](int g) {
+      const int b = p.by_S.div(g), tok = g - b * p.S;
+      const T* d = rows.d<T>(g, b, tok);
+      const long long d_apart = at.heads_per * rows.d_head, x_apart = at.heads_per * t.xs[2];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (i < have) next_d[i] = __ldcs(reinterpret_cast<const uint4*>(d));
+        d += d_apart;
+      }
+      if (normed) {
+        const T* x = rows.x<T>(g, b, tok);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          if (i < have) next_x[i] = __ldcs(reinterpret_cast<const uint4*>(x));
+          x += x_apart;
         }
-        copies_commit();
-        in = in == mine ? mine + 2 * NV * threads : mine;      // (kDepth = 2)
       }
     };
-    ask();
-    ask();
-    angles(p, g, l, tpr, &ang[group][0]);
+    fetch(g);
+    Positions positions;
+    positions.load(p, freq, g, l, tpr);
+    positions.angles(p, freq, l, tpr, &ang[group][0]);
     int turn_buf = 0;
-    const uint4* row = mine;
     for (; g < tokens; g += step, turn_buf ^= 1) {
       meet(group, p.wpr);                    // (this token's angles)
       Turn<E, L> turn;
       turn.load(p, ang[group][turn_buf], c0, -1.f);
-      if (ONCE) copies_wait<kDepth - 1>();
-      auto vec_d = [&](int v0, int i) {
-        if (ONCE) return row[i * threads];
-        uint4 u = make_uint4(0u, 0u, 0u, 0u);
-        if (v0 + l + i * tpr < nvec) u = __ldcg(reinterpret_cast<const uint4*>(d_row(g) + ((v0 >> vshift) + i * heads_per) * d_head));
-        return u;
-      };
-      auto vec_x = [&](int v0, int i) {
-        if (ONCE) return row[(NV + i) * threads];
-        uint4 u = make_uint4(0u, 0u, 0u, 0u);
-        if (v0 + l + i * tpr < nvec) u = __ldcg(reinterpret_cast<const uint4*>(x_row(g) + ((v0 >> vshift) + i * heads_per) * t.xs[2]));
-        return u;
-      };
-      float r = 1.f, back = 0.f;             // 1 / rms; r^2 times the mean of x times its weighted gradient
-      auto scales = [&](const float2& s) {
-        r = rsqrtf(fmaf(s.x, inv_n, p.eps));
-        back = r * r * (s.y * inv_n);
+      const bool more = g + step < tokens;
+      if (more) positions.load(p, freq, g + step, l, tpr);
+      const int b = p.by_S.div(g), tok = g - b * p.S;
+      const long long apart = at.heads_per * t.ds[2];
+      T* dst = rows.dx<T>(g, b, tok);
+      float y[NV][E];
+      uint4 x_raw[NV];                       // (unpacked twice: 24 registers less)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        Row<T, L>::unpack(next_d[i], y[i]);
+        x_raw[i] = next_x[i];
+      }
+      if (more) fetch(g + step);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) turn.apply(p, y[i], 1.f, c0, buf);
+      float r, back;                         // 1 / rms; r^2 times the mean of x times its weighted gradient
+      auto scales = [&](float xx, float xg) {
+        r = rsqrtf(fmaf(xx, inv_n, p.eps));
+        back = r * r * (xg * inv_n);
       };
       if (by_row) {
-        float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
-        for (int v0 = 0; v0 < nvec; v0 += per) {
-          const float* w = t.w ? t.w + (v0 + l) * E : nullptr;
-#pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            const bool there = v0 + l + i * tpr < nvec;
-            if (__any_sync(0xffffffffu, there)) {
-              float y[E], x[E], f[E];
-              Vec<T>::unpack(vec_d(v0, i), y);
-              turn.apply(p, y, c0, buf);
-              Vec<T>::unpack(vec_x(v0, i), x);
-              weights<E>(there ? w : nullptr, f);
-              dot<E>(x, x, s0, s1);
-              times<E>(y, f);
-              dot<E>(x, y, u0, u1);
-            }
-            if (w) w += tpr * E;
-          }
-          if (ONCE) break;
-        }
-        scales(row_sum(make_float2(s0 + s1, u0 + u1), group, p.wpr, slot[turn_buf] + group * p.wpr));
-      }
-      if (g + step < tokens) angles(p, g + step, l, tpr, &ang[group][turn_buf ^ 1]);
-      const int b = p.by_S.div(g), tok = g - b * p.S;
-      T* dst = reinterpret_cast<T*>(t.dst) + b * t.ds[0] + tok * t.ds[1] + head0 * t.ds[2] + c0;
-      for (int v0 = 0; v0 < nvec; v0 += per) {
-        const float* w = t.w ? t.w + (by_row ? (v0 + l) * E : c0) : nullptr;
+        float s[4] = {0.f, 0.f, 0.f, 0.f}, f[E];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          const bool there = v0 + l + i * tpr < nvec;
-          if (__any_sync(0xffffffffu, there)) {
-            float y[E];
-            Vec<T>::unpack(vec_d(v0, i), y);
-            turn.apply(p, y, c0, buf);
-            if (normed) {
-              float x[E], f[E];
-              Vec<T>::unpack(vec_x(v0, i), x);
-              weights<E>(there ? w : nullptr, f);
-              float yw[E];
-#pragma unroll
-              for (int e = 0; e < E; e += 2) mul2(yw[e], yw[e + 1], y[e], y[e + 1], f[e], f[e + 1]);
-              if (by_head) {
-                float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
-                dot<E>(x, x, s0, s1);
-                dot<E>(x, yw, u0, u1);
-                scales(head_sum(make_float2(s0 + s1, u0 + u1), V));
-              }
-#pragma unroll
-              for (int e = 0; e < E; e += 2) {
-                mul2(y[e], y[e + 1], y[e], y[e + 1], r, r);
-                if (by_row && !ONCE) {
-                  if (there) {
-                    float* a = mine_acc + (v0 + l + i * tpr) * E + e;
-                    a[0] = fmaf(y[e], x[e], a[0]);
-                    a[1] = fmaf(y[e + 1], x[e + 1], a[1]);
-                  }
-                } else {
-                  fma2(acc[i][e], acc[i][e + 1], y[e], y[e + 1], x[e], x[e + 1], acc[i][e], acc[i][e + 1]);      // (zeros beyond the row)
-                }
-                fma2(y[e], y[e + 1], x[e], x[e + 1], -back, -back, yw[e], yw[e + 1]);
-                mul2(y[e], y[e + 1], y[e], y[e + 1], r, r);
-              }
-            }
-            if (there) *reinterpret_cast<uint4*>(dst) = Vec<T>::pack(y);
-          }
-          dst += heads_per * t.ds[2];
-          if (w && by_row) w += tpr * E;
+          float x[E];
+          staged_weights<E>(w_mine + i * tpr, n_w, f);
+          Row<T, L>::unpack(x_raw[i], x);
+          sums_of<E>(x, y[i], f, s);
         }
-        if (ONCE) break;
+        const float2 total = row_sum<true>(make_float2(s[0] + s[1], s[2] + s[3]), group, p.wpr, slot[turn_buf] + group * p.wpr);
+        scales(total.x, total.y);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          float x[E];
+          opaque(x_raw[i]);
+          staged_weights<E>(w_mine + i * tpr, n_w, f);
+          Row<T, L>::unpack(x_raw[i], x);
+          times<E>(x, r);
+          finish<E>(y[i], x, f, r, back, acc[i]);
+        }
+      } else if (normed) {
+        float sums[2 * NV], f[E];
+        staged_weights<E>(w_mine, n_w, f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          float s[4] = {0.f, 0.f, 0.f, 0.f};
+          float x[E];
+          Row<T, L>::unpack(x_raw[i], x);
+          sums_of<E>(x, y[i], f, s);
+          sums[2 * i] = s[0] + s[1];
+          sums[2 * i + 1] = s[2] + s[3];
+        }
+        head_sums<2 * NV>(sums, at.V);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          scales(sums[2 * i], sums[2 * i + 1]);
+          float x[E];
+          opaque(x_raw[i]);
+          Row<T, L>::unpack(x_raw[i], x);
+          times<E>(x, r);
+          finish<E>(y[i], x, f, r, back, acc[0]);      // (zeros beyond the row)
+        }
       }
-      row = row == mine ? mine + 2 * NV * threads : mine;
-      ask();
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (i < have) *reinterpret_cast<uint4*>(dst) = Row<T, L>::pack(y[i]);
+        dst += apart;
+      }
+      if (more) positions.angles(p, freq, l, tpr, &ang[group][turn_buf ^ 1]);
     }
   }
   if (!normed) return;
-  const int n_w = by_row ? row_ch : p.d;
-  float* out = p.part + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * n_w;
-  if (by_row) {
-    copies_wait<0>();
-    __syncthreads();                         // (the ring is free)
-    if (ONCE) {
+  float* out = p.part + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * (by_row ? row_ch : p.d);
+  float* sums = by_row ? reinterpret_cast<float*>(w_all) : exchange;
+  __syncthreads();                           // (the weights and the exchange buffers are free)
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < E; e += 4)
-          if (l + i * tpr < nvec)
-            *reinterpret_cast<float4*>(mine_acc + (l + i * tpr) * E + e) = make_float4(acc[i][e], acc[i][e + 1], acc[i][e + 2], acc[i][e + 3]);
+    for (int e = 0; e < E; ++e) {
+      if (by_row) {
+        if (i < have) sums[group * row_ch + (l + i * tpr) * E + channel<E, L>(e)] = acc[i][e];
+      } else if (i == 0) {
+        sums[threadIdx.x * E + channel<E, L>(e)] = acc[0][e];
+      }
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < row_ch; i += threads) {
+  __syncthreads();
+  if (by_row) {
+    for (int i = threadIdx.x; i < row_ch; i += blockDim.x) {
       float a = 0.f;
-      for (int q = 0; q < p.groups; ++q) a += acc_row[(long long)q * row_ch + i];
+      for (int q = 0; q < p.groups; ++q) a += sums[q * row_ch + i];
       out[i] = a;
     }
   } else {
-    __syncthreads();                         // (the exchange buffers are free)
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
+    for (int c = threadIdx.x; c < p.d; c += blockDim.x) {            // threads c / E, c / E + V, ... hold channel c
       float a = 0.f;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) a += acc[i][e];
-      exchange[threadIdx.x * E + e] = a;
-    }
-    __syncthreads();
-    for (int c = threadIdx.x; c < p.d; c += threads) {               // threads c / E, c / E + V, ... hold channel c
-      float a = 0.f;
-      for (int q = c / E; q < threads; q += V) a += exchange[q * E + c % E];
+      for (int q = c / E; q < (int)blockDim.x; q += at.V) a += sums[q * E + c % E];
       out[c] = a;
     }
+  }
+}
+
+// Longer rows: a CTA each, read twice where the norm is theirs.
+template <typename T, Layout L>
+__global__ void __launch_bounds__(32 * kMaxWarps)
+rotary_bwd_long_kernel(const __grid_constant__ Params p) {
+  if (!grid_begin()) return;
+  constexpr int E = Vec<T>::E;
+  extern __shared__ __align__(16) float sums[];                      // [heads * d] (norm per row)
+  __shared__ Frequencies freq;
+  __shared__ Angles ang[2];
+  __shared__ float2 slot[2][kMaxWarps];
+  __shared__ float exchange[kMaxWarps * 32 * E];
+  const Place at(p, E);
+  const int l = at.l, tpr = at.tpr, c0 = at.c0;
+  float* buf = exchange + (threadIdx.x >> 5) * 32 * E;
+  const Tensor& t = p.t[blockIdx.y];
+  const bool by_row = p.norm == VMOBA_ROTARY_NORM_ROW, normed = p.norm != VMOBA_ROTARY_NORM_NONE;
+  const int row_ch = p.heads * p.d;
+  const float inv_n = 1.0f / (float)(by_row ? row_ch : p.d);
+  const Gradients rows(p, t, at);
+  float acc[E];                              // (norm per head)
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+  if (by_row)
+    for (int i = l; i < row_ch; i += tpr) sums[i] = 0.f;
+  Positions positions;
+  stage_frequencies(p, &freq);
+  __syncthreads();
+  int turn_buf = 0;
+  for (int g = blockIdx.x; g < p.B * p.S; g += gridDim.x, turn_buf ^= 1) {
+    positions.load(p, freq, g, l, tpr);
+    positions.angles(p, freq, l, tpr, &ang[turn_buf]);
+    meet(0, p.wpr);
+    Turn<E, L> turn;
+    turn.load(p, ang[turn_buf], c0, -1.f);
+    const int b = p.by_S.div(g), tok = g - b * p.S;
+    const T *d = rows.d<T>(g, b, tok), *xs = normed ? rows.x<T>(g, b, tok) : nullptr;
+    T* dst = rows.dx<T>(g, b, tok);
+    // the vectors of the row: the gradient turned back, x and the weights
+    auto each = [&](auto f) {
+      for (int v0 = 0; v0 < at.nvec; v0 += tpr) {
+        const int v = v0 + l, head = v0 >> at.vshift;
+        const bool there = v < at.nvec;
+        uint4 u = make_uint4(0u, 0u, 0u, 0u);
+        float y[E], x[E], w[E];
+        if (there) u = __ldcg(reinterpret_cast<const uint4*>(d + head * rows.d_head));
+        Row<T, L>::unpack(u, y);
+        turn.apply(p, y, 1.f, c0, buf);
+        if (normed) {
+          u = make_uint4(0u, 0u, 0u, 0u);
+          if (there) u = __ldcg(reinterpret_cast<const uint4*>(xs + head * t.xs[2]));
+          Row<T, L>::unpack(u, x);
+          weights<E, L>(t.w && there ? t.w + (by_row ? v * E : c0) : nullptr, w);
+        }
+        f(v, head, there, y, x, w);
+      }
+    };
+    float r = 1.f, back = 0.f;
+    auto scales = [&](float xx, float xg) {
+      r = rsqrtf(fmaf(xx, inv_n, p.eps));
+      back = r * r * (xg * inv_n);
+    };
+    if (by_row) {
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      each([&](int, int, bool, float (&y)[E], float (&x)[E], float (&w)[E]) { sums_of<E>(x, y, w, s); });
+      const float2 total = row_sum<true>(make_float2(s[0] + s[1], s[2] + s[3]), 0, p.wpr, slot[turn_buf]);
+      scales(total.x, total.y);
+    }
+    each([&](int v, int head, bool there, float (&y)[E], float (&x)[E], float (&w)[E]) {
+      if (normed) {
+        if (!by_row) {
+          float s[4] = {0.f, 0.f, 0.f, 0.f};
+          sums_of<E>(x, y, w, s);
+          float two[2] = {s[0] + s[1], s[2] + s[3]};
+          head_sums<2>(two, at.V);
+          scales(two[0], two[1]);
+        }
+        times<E>(x, r);
+        float part[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) part[e] = by_row ? (there ? sums[v * E + channel<E, L>(e)] : 0.f) : acc[e];
+        finish<E>(y, x, w, r, back, part);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          if (!by_row) acc[e] = part[e];
+          else if (there) sums[v * E + channel<E, L>(e)] = part[e];
+        }
+      }
+      if (there) *reinterpret_cast<uint4*>(dst + head * t.ds[2]) = Row<T, L>::pack(y);
+    });
+  }
+  if (!normed) return;
+  float* out = p.part + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * (by_row ? row_ch : p.d);
+  __syncthreads();
+  if (by_row) {
+    for (int i = l; i < row_ch; i += tpr) out[i] = sums[i];
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) exchange[threadIdx.x * E + channel<E, L>(e)] = acc[e];
+  __syncthreads();
+  for (int c = threadIdx.x; c < p.d; c += blockDim.x) {
+    float a = 0.f;
+    for (int q = c / E; q < (int)blockDim.x; q += at.V) a += exchange[q * E + c % E];
+    out[c] = a;
   }
 }
 
@@ -620,24 +913,32 @@ weight_sum_kernel(const float* __restrict__ part, int n_parts, int n_w, WeightOu
 }
 
 // ------------------------------------------------------------------------------ host
-// How a row is laid over warps: up to six vectors per thread in the fewest idle lanes, of equals the fewest warps; CTAs of about eight
-// warps.  false: the row is longer than that (eight warps, trips of four vectors per thread).
-constexpr int kMaxNv = 6;
-static bool lay_out(const Dims& D, Params* p, int* nv) {
+// How a row is laid over warps: up to `most` vectors per thread in the fewest idle lanes, of equals the fewest warps (40 heads of 128: 549 us with
+// four warps of five vectors, 618 with five of four); CTAs of about `warps` warps.  false: the row is longer than that, or its
+// `tensors` weights are more than two CTAs of an SM have room for.
+constexpr int kFwdVectors = 6, kBwdVectors = 3;
+constexpr int kSmemMost = 96 * 1024;
+static bool lay_out(const Dims& D, int most, int warps, int tensors, Params* p, int* nv) {
   const int nvec = D.heads * D.d * D.es / 16;
   int best = INT32_MAX;
-  *nv = 4; p->wpr = kMaxWarps; p->groups = 1;
+  *nv = 0;
   for (int w = 1; w <= kMaxWarps; ++w)
-    for (int v = 1; v <= kMaxNv; ++v) {
+    for (int v = 1; v <= most; ++v) {
       const int idle = w * 32 * v - nvec;
-      if (idle >= 0 && idle < best) { best = idle; *nv = v; p->wpr = w; p->groups = kMaxWarps / w; }
+      if (idle >= 0 && idle < best) { best = idle; *nv = v; p->wpr = w; p->groups = warps / w; }
     }
-  return best < INT32_MAX;
+  if (best < INT32_MAX &&
+      (p->norm != VMOBA_ROTARY_NORM_ROW || (size_t)tensors * 32 * p->wpr * most * (16 / D.es) * sizeof(float) <= kSmemMost))
+    return true;
+  p->wpr = kMaxWarps; p->groups = 1;
+  return false;
 }
+// CTAs that the SMs hold at once, `warps` of them each.
+static long long resident(const Params& p, int warps) { return (long long)sm_count() * (warps / (p.wpr * p.groups)); }
 // CTAs of the backward (per tensor); at most kMaxParts parts of dw.
 constexpr int kMaxParts = 512;
 static int bwd_ctas(const Dims& D, const Params& p) {
-  return (int)std::min<long long>(((long long)D.B * D.S + p.groups - 1) / p.groups, std::min(kMaxParts, 2 * sm_count()));
+  return (int)std::min({((long long)D.B * D.S + p.groups - 1) / p.groups, (long long)kMaxParts, std::max(resident(p, kBwdWarps) / p.n, 1ll)});
 }
 
 static int check(const vmoba_shape* shape, const vmoba_rotary_spec* spec, Dims* D) {
@@ -662,6 +963,11 @@ static bool strides_ok(const Dims& D, const int64_t s[3], bool written) {
   return true;
 }
 
+static unsigned token_bytes(const Dims& D, const long long s[3]) {
+  const long long bytes = s[1] * D.es;
+  return (D.B == 1 || s[0] == s[1] * D.S) && bytes <= 0xffffffffll ? (unsigned)bytes : 0u;
+}
+
 static void fill(const Dims& D, const vmoba_rotary_spec* spec, Params* p) {
   p->B = D.B; p->S = D.S; p->heads = D.heads; p->d = D.d;
   p->W = D.W; p->bT = D.bT; p->bH = D.bH; p->bW = D.bW; p->sb = D.sb; p->HW = D.H * D.W; p->nH = D.nH; p->nW = D.nW;
@@ -672,63 +978,72 @@ static void fill(const Dims& D, const vmoba_rotary_spec* spec, Params* p) {
   p->mscale = spec->mscale; p->eps = spec->eps;
 }
 
-template <typename T, Layout L, int NV, bool ONCE>
+// Shared memory of the staged weights: whole vectors for all threads of a row, or one head's.
+static size_t weight_bytes(const Dims& D, const Params& p, int nv, int tensors) {
+  if (p.norm == VMOBA_ROTARY_NORM_NONE) return 0;
+  return (size_t)tensors * (p.norm == VMOBA_ROTARY_NORM_ROW ? 32 * p.wpr * nv * (16 / D.es) : D.d) * sizeof(float);
+}
+
+// NV: vectors per thread; 0: the kernels for longer rows.
+template <typename T, Layout L, int NV>
 static int go_fwd(const Dims& D, const Params& p, cudaStream_t st) {
-  auto kernel = rotary_fwd_kernel<T, L, NV, ONCE>;
   const int threads = 32 * p.wpr * p.groups;
-  const long long ctas = ((long long)D.B * D.S + p.groups - 1) / p.groups;
-  VMOBA_CUDA_OK(allow_smem(kernel, kDepth * NV * 32 * kMaxWarps * 16));
-  launch_kernel(early_rows(D), kernel, (unsigned)std::min<long long>(ctas, 3ll * sm_count()), threads,
-                ONCE ? (size_t)kDepth * NV * threads * 16 : 0, st, p);
+  const long long rows = ((long long)D.B * D.S + p.groups - 1) / p.groups;
+  const unsigned ctas = (unsigned)std::min(rows, resident(p, 2 * kMaxWarps));
+  if constexpr (NV == 0) {
+    launch_kernel(early_rows(D), rotary_fwd_long_kernel<T, L>, ctas, threads, 0, st, p);
+  } else {
+    auto kernel = rotary_fwd_kernel<T, L, NV>;
+    VMOBA_CUDA_OK(allow_smem(kernel, kSmemMost));
+    launch_kernel(early_rows(D), kernel, ctas, threads, weight_bytes(D, p, NV, p.turned), st, p);
+  }
   VMOBA_LAUNCH_OK(1);
   return VMOBA_OK;
 }
 
-static size_t bwd_smem(const Dims& D, const Params& p, int nv, bool once) {
-  const size_t ring = once ? (size_t)2 * kDepth * nv * 32 * p.wpr * p.groups * 16 : 0;
-  return std::max(ring, p.norm == VMOBA_ROTARY_NORM_ROW ? (size_t)p.groups * D.heads * D.d * sizeof(float) : 0);
-}
-constexpr int kBwdSmemMost = 200 * 1024;
+constexpr int kLongSmemMost = 200 * 1024;
 
-template <typename T, Layout L, int NV, bool ONCE>
+template <typename T, Layout L, int NV>
 static int go_bwd(const Dims& D, const Params& p, const WeightOut& w, cudaStream_t st) {
-  auto kernel = rotary_bwd_kernel<T, L, NV, ONCE>;
-  const int ctas = bwd_ctas(D, p);
-  const size_t smem = bwd_smem(D, p, NV, ONCE);
-  if (smem > (size_t)kBwdSmemMost) return VMOBA_ERR_NOT_IMPLEMENTED;
-  VMOBA_CUDA_OK(allow_smem(kernel, kBwdSmemMost));
-  launch_kernel(early_rows(D), kernel, dim3(ctas, p.n), 32 * p.wpr * p.groups, smem, st, p);
+  const int ctas = bwd_ctas(D, p), threads = 32 * p.wpr * p.groups;
+  const int n_w = p.norm == VMOBA_ROTARY_NORM_ROW ? D.heads * D.d : D.d;
+  const size_t sums = p.norm == VMOBA_ROTARY_NORM_ROW ? (size_t)p.groups * n_w * sizeof(float) : 0;
+  if constexpr (NV == 0) {
+    auto kernel = rotary_bwd_long_kernel<T, L>;
+    if (sums > (size_t)kLongSmemMost) return VMOBA_ERR_NOT_IMPLEMENTED;
+    VMOBA_CUDA_OK(allow_smem(kernel, kLongSmemMost));
+    launch_kernel(early_rows(D), kernel, dim3(ctas, p.n), threads, sums, st, p);
+  } else {
+    auto kernel = rotary_bwd_kernel<T, L, NV>;
+    VMOBA_CUDA_OK(allow_smem(kernel, kSmemMost));
+    launch_kernel(early_rows(D), kernel, dim3(ctas, p.n), threads, std::max(sums, weight_bytes(D, p, NV, 1)), st, p);
+  }
   VMOBA_LAUNCH_OK(1);
   if (p.norm != VMOBA_ROTARY_NORM_NONE) {
-    const int n_w = p.norm == VMOBA_ROTARY_NORM_ROW ? D.heads * D.d : D.d;
     launch_kernel(weight_sum_kernel, dim3((n_w + 31) / 32, p.n), 1024, 0, st, p.part, ctas, n_w, w);
     VMOBA_LAUNCH_OK(1);
   }
   return VMOBA_OK;
 }
 
-// The compiled variant of a shape: go(layout, vectors per thread, whether the row fits).
-template <typename T, typename Go>
-static int dispatch(const Dims& D, Params& p, Go go) {
+// The compiled variant of a shape: go(layout, vectors per thread).
+template <typename T, int MOST, typename Go>
+static int dispatch(const Dims& D, Params& p, int tensors, Go go) {
   int nv;
-  const bool once = lay_out(D, &p, &nv);
+  const bool once = lay_out(D, MOST, MOST == kFwdVectors ? kMaxWarps : kBwdWarps, tensors, &p, &nv);
   auto with = [&](auto layout) {
-    constexpr Layout L = decltype(layout)::value;
-    auto pick = [&](auto n, auto o) { return go(layout, n, o); };
     using std::integral_constant;
-    if (!once) return pick(integral_constant<int, 4>{}, std::false_type{});
-    if constexpr (L == kHalfAny) {           // (rare: one variant, with idle vectors)
-      return pick(integral_constant<int, kMaxNv>{}, std::true_type{});
-    } else {
-      switch (nv) {
-        case 1: return pick(integral_constant<int, 1>{}, std::true_type{});
-        case 2: return pick(integral_constant<int, 2>{}, std::true_type{});
-        case 3: return pick(integral_constant<int, 3>{}, std::true_type{});
-        case 4: return pick(integral_constant<int, 4>{}, std::true_type{});
-        case 5: return pick(integral_constant<int, 5>{}, std::true_type{});
-        default: return pick(integral_constant<int, 6>{}, std::true_type{});
+    if (!once) return go(layout, integral_constant<int, 0>{});
+    if constexpr (decltype(layout)::value != kHalfAny) {      // (rare: one variant, with idle vectors)
+      if (nv == 1) return go(layout, integral_constant<int, 1>{});
+      if (nv == 2) return go(layout, integral_constant<int, 2>{});
+      if constexpr (MOST > 3) {
+        if (nv == 3) return go(layout, integral_constant<int, 3>{});
+        if (nv == 4) return go(layout, integral_constant<int, 4>{});
+        if (nv == 5) return go(layout, integral_constant<int, 5>{});
       }
     }
+    return go(layout, integral_constant<int, MOST>{});
   };
   if (p.layout == VMOBA_ROTARY_INTERLEAVED) return with(std::integral_constant<Layout, kInterleaved>{});
   if (p.pairs % Vec<T>::E == 0) return with(std::integral_constant<Layout, kHalf>{});
@@ -737,11 +1052,11 @@ static int dispatch(const Dims& D, Params& p, Go go) {
 
 template <typename T>
 static int launch_fwd(const Dims& D, Params& p, cudaStream_t st) {
-  return dispatch<T>(D, p, [&](auto l, auto n, auto o) { return go_fwd<T, decltype(l)::value, decltype(n)::value, decltype(o)::value>(D, p, st); });
+  return dispatch<T, kFwdVectors>(D, p, p.turned, [&](auto l, auto n) { return go_fwd<T, decltype(l)::value, decltype(n)::value>(D, p, st); });
 }
 template <typename T>
 static int launch_bwd(const Dims& D, Params& p, const WeightOut& w, cudaStream_t st) {
-  return dispatch<T>(D, p, [&](auto l, auto n, auto o) { return go_bwd<T, decltype(l)::value, decltype(n)::value, decltype(o)::value>(D, p, w, st); });
+  return dispatch<T, kBwdVectors>(D, p, 1, [&](auto l, auto n) { return go_bwd<T, decltype(l)::value, decltype(n)::value>(D, p, w, st); });
 }
 
 }  // namespace rotary
@@ -781,6 +1096,8 @@ extern "C" int vmoba_rotary(const vmoba_shape* shape, const vmoba_rotary_spec* s
     t.w = spec->norm != VMOBA_ROTARY_NORM_NONE && weight_or_null && k < turned ? weight_or_null[k] : nullptr;
     if (!aligned16(t.w)) return VMOBA_ERR_ARG;
     for (int i = 0; i < 3; ++i) { t.ss[i] = src_strides_bsh[k][i]; t.ds[i] = p.dst_bm ? 0 : dst_strides_bsh_or_null[k][i]; }
+    t.ss1 = rotary::token_bytes(D, t.ss);
+    t.ds1 = rotary::token_bytes(D, t.ds);
   }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return D.dtype == VMOBA_BF16 ? rotary::launch_fwd<__nv_bfloat16>(D, p, st) : rotary::launch_fwd<float>(D, p, st);
@@ -812,10 +1129,13 @@ extern "C" int vmoba_rotary_bwd(const vmoba_shape* shape, const vmoba_rotary_spe
       t.ss[i] = p.src_bm ? 0 : d_out_strides_bsh_or_null[k][i];
       t.ds[i] = dx_strides_bsh[k][i];
     }
+    t.ss1 = rotary::token_bytes(D, t.ss);
+    t.ds1 = rotary::token_bytes(D, t.ds);
     if (normed) {
       if (!x_or_null[k] || !aligned16(x_or_null[k]) || !rotary::strides_ok(D, x_strides_bsh_or_null[k], false)) return VMOBA_ERR_ARG;
       t.x = x_or_null[k];
       for (int i = 0; i < 3; ++i) t.xs[i] = x_strides_bsh_or_null[k][i];
+      t.xs1 = rotary::token_bytes(D, t.xs);
       t.w = weight_or_null ? weight_or_null[k] : nullptr;
       if (!aligned16(t.w)) return VMOBA_ERR_ARG;
       w.dw[k] = dweight_or_null ? dweight_or_null[k] : nullptr;

@@ -54,6 +54,11 @@ CASES = [
     dict(B=1, heads=3, d=128, grid=(5, 30, 40), block=(5, 6, 8), dtype="bf16", pairs=(0,), norm="head", layout="half"),
     dict(B=1, heads=2, d=64, grid=(1, 9, 9), block=(1, 3, 9), dtype="f32", pairs=(32,), norm="none", layout="interleaved", big=True),
     dict(B=1, heads=4, d=64, grid=(1, 9, 9), block=(1, 3, 9), dtype="f32", pairs=(1, 1, 1, 1), norm="row", layout="half", weight=False),
+    # rows too long for the registers of a thread: of the backward, of both
+    dict(B=2, heads=60, d=128, grid=(1, 2, 9), block=(1, 2, 3), dtype="bf16", pairs=(22, 21, 21), norm="row", layout="interleaved"),
+    dict(B=1, heads=101, d=128, grid=(1, 5, 3), block=(1, 5, 3), dtype="bf16", pairs=(20, 21), norm="row", layout="interleaved"),
+    dict(B=2, heads=100, d=128, grid=(1, 2, 9), block=(1, 2, 3), dtype="bf16", pairs=(13,), norm="head", layout="half", batch_pos=True),
+    dict(B=1, heads=130, d=128, grid=(2, 3, 3), block=(1, 3, 3), dtype="bf16", pairs=(64,), norm="none", layout="half"),
 ]
 
 
@@ -191,3 +196,28 @@ def test_captured_and_on_another_stream():
         graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(out + dx + dw, want))
+
+
+@pytest.mark.parametrize("norm", ["none", "head", "row"])
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+def test_what_is_not_finite_stays_where_it_is(layout, norm):
+    """Channels that no pair holds pass through whatever stands beside them; a row (norm per head: a head) that holds no such value keeps its
+    bits."""
+    shape, op, x, dy, w, *_ = case(1, 3, 64, (1, 4, 4), (1, 4, 4), "bf16", (10,), norm, layout, seed=8)
+    xs, ws = [t.cuda() for t in x], [None if t is None else t.cuda() for t in w]
+    outs = [torch.empty_like(t) for t in xs]
+    op.forward(xs, outs, ws)
+    bad = [t.clone() for t in xs]
+    bad[0][0, 5, 1, 40] = float("inf")
+    bad[0][0, 9, 2, 41] = float("nan")
+    got = [torch.empty_like(t) for t in xs]
+    op.forward(bad, got, ws)
+    same = torch.ones_like(outs[0], dtype=torch.bool)
+    if norm == "none":
+        same[0, 5, 1, 40] = same[0, 9, 2, 41] = False
+        assert got[0][0, 5, 1, 40] == float("inf") and got[0][0, 9, 2, 41].isnan()
+    elif norm == "head":
+        same[0, 5, 1] = same[0, 9, 2] = False
+    else:
+        same[0, 5] = same[0, 9] = False
+    assert torch.equal(got[0][same], outs[0][same]) and torch.equal(got[1], outs[1])
