@@ -84,7 +84,9 @@ class Rotary:
             raise ValueError("Rotary: int32 positions, fp64 frequencies and as many int32 axes required")
         if not (positions.is_cuda and positions.device == freq.device == axis.device):
             raise ValueError("Rotary: positions, frequencies and axes have to be on one GPU")
-        self.shape, self.device = s, positions.device
+        self.shape, self.device, self.dtype = s, positions.device, torch_dtype(s)
+        self._size = torch.Size((s.B, s.S, s.heads, s.head_dim))
+        self._dense = (s.S * s.heads * s.head_dim, s.heads * s.head_dim, s.head_dim)
         self.positions, self.freq, self.axis = positions.contiguous(), freq.contiguous(), axis.contiguous()
         self.spec = vb.RotarySpec(freq.numel(), positions.shape[-1], {"half": vb.ROTARY_HALF, "interleaved": vb.ROTARY_INTERLEAVED}[layout],
                                   {"none": vb.ROTARY_NORM_NONE, "head": vb.ROTARY_NORM_HEAD, "row": vb.ROTARY_NORM_ROW}[norm],
@@ -102,20 +104,22 @@ class Rotary:
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
 
     def _raster(self, x, what):
-        s = self.shape
-        if tuple(x.shape) != (s.B, s.S, s.heads, s.head_dim) or x.dtype != torch_dtype(s) or x.device != self.device or x.stride(3) != 1:
-            raise ValueError(f"Rotary: {what} has to be [B, S, heads, head_dim] of the layer's type on {self.device}, head_dim contiguous")
-        return _strides_bsh(x)
+        if x.shape == self._size and x.dtype is self.dtype and x.device == self.device:
+            if x.is_contiguous():          # (a size of one may have any stride)
+                return self._dense
+            if x.stride(3) == 1:
+                return _strides_bsh(x)
+        raise ValueError(f"Rotary: {what} has to be [B, S, heads, head_dim] of the layer's type on {self.device}, head_dim contiguous")
 
     def _block_major(self, x, what):
         s = self.shape
-        if tuple(x.shape) != (s.B, s.heads, s.S, s.head_dim) or x.dtype != torch_dtype(s) or x.device != self.device or not x.is_contiguous():
+        if x.shape != (s.B, s.heads, s.S, s.head_dim) or x.dtype is not self.dtype or x.device != self.device or not x.is_contiguous():
             raise ValueError(f"Rotary: {what} has to be [B, heads, S, head_dim] of the layer's type on {self.device}, contiguous")
 
     def _weights(self, weights, n):
         if weights is None or self.n_weights == 0:
             return None
-        weights = list(weights) + [None] * (n - len(weights))
+        weights = [*weights, *[None] * (n - len(weights))]
         for w in weights:
             if w is not None and (w.numel() != self.n_weights or w.dtype != torch.float32 or not w.is_contiguous() or w.device != self.device):
                 raise ValueError(f"Rotary: a weight has to be {self.n_weights} contiguous fp32 values on {self.device}")
@@ -470,8 +474,10 @@ class RangeAttention:
     def _tensor(self, x, S, heads, what, written=False):
         """x as the kernels can address it (an input that they cannot is copied) and its strides."""
         s = self.shape
-        if tuple(x.shape) != (s.B, S, heads, s.head_dim) or x.dtype != torch_dtype(s) or x.device != self.device:
+        if x.shape != (s.B, S, heads, s.head_dim) or x.dtype is not torch_dtype(s) or x.device != self.device:
             raise ValueError(f"RangeAttention: {what} has to be [{s.B}, {S}, {heads}, {s.head_dim}] of the shape's type on {self.device}")
+        if x.is_contiguous() and x.data_ptr() % 16 == 0:
+            return x, (S * heads * s.head_dim, heads * s.head_dim, s.head_dim)
         st, per = _strides_bsh(x), 16 // x.element_size()
         if x.stride(3) == 1 and x.data_ptr() % 16 == 0 and all(i % per == 0 and i >= s.head_dim for i in st):
             return x, st
