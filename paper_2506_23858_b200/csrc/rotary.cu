@@ -221,7 +221,8 @@ struct Turn {
       }
     }
   }
-  // Turns a vector and multiplies it by r.  buf (kHalfAny): 32 * E floats of the warp.  Called by whole warps.
+  // Turns a vector and multiplies it by r (SCALED: not known to be 1).  buf (kHalfAny): 32 * E floats of the warp.  Called by whole warps.
+  template <bool SCALED>
   __device__ __forceinline__ void apply(const Params& p, float (&y)[E], float r, int c0, float* buf) const {
     if constexpr (L == kInterleaved) {
       if (p.full) {
@@ -235,7 +236,7 @@ struct Turn {
           fma2(y[N + i], y[N + i + 1], y[N + i], y[N + i + 1], c0, c1, u0, u1);
         }
       } else {
-        times<E>(y, r);
+        if (SCALED) times<E>(y, r);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const float y0 = y[i], y1 = y[N + i];
@@ -246,7 +247,7 @@ struct Turn {
         }
       }
     } else {
-      times<E>(y, r);
+      if (SCALED) times<E>(y, r);
       float o[E];
       const int lane = threadIdx.x & 31;
       if constexpr (L == kHalf) {            // the partners of a vector are a vector of another lane of the same head
@@ -445,7 +446,7 @@ rotary_fwd_kernel(const __grid_constant__ Params p) {
           float f[E];
           staged_weights<E>(w + i * tpr, n_w, f);
           times<E>(y[i], f);
-          turn.apply(p, y[i], r, c0, buf);
+          turn.template apply<true>(p, y[i], r, c0, buf);
           put(i);
         }
       } else if (p.norm == VMOBA_ROTARY_NORM_HEAD) {
@@ -462,13 +463,13 @@ rotary_fwd_kernel(const __grid_constant__ Params p) {
         for (int i = 0; i < NV; ++i) {
           times<E>(y[i], rsqrtf(fmaf(sums[i], inv_n, p.eps)));
           times<E>(y[i], f);
-          turn.apply(p, y[i], 1.f, c0, buf);
+          turn.template apply<false>(p, y[i], 1.f, c0, buf);
           put(i);
         }
       } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          turn.apply(p, y[i], 1.f, c0, buf);
+          turn.template apply<false>(p, y[i], 1.f, c0, buf);
           put(i);
         }
       }
@@ -557,7 +558,7 @@ rotary_fwd_long_kernel(const __grid_constant__ Params p) {
               }
               times<E>(y, f);
             }
-            turn.apply(p, y, r, c0, buf);
+            turn.template apply<true>(p, y, r, c0, buf);
           }
           if (there) *reinterpret_cast<uint4*>(dst + ((v0 >> at.vshift) + i * at.heads_per) * to_head) = Row<T, L>::pack(y);
         }
@@ -695,7 +696,7 @@ rotary_bwd_kernel(const __grid_constant__ Params p) {
       }
       if (more) fetch(g + step);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) turn.apply(p, y[i], 1.f, c0, buf);
+      for (int i = 0; i < NV; ++i) turn.template apply<false>(p, y[i], 1.f, c0, buf);
       float r, back;                         // 1 / rms; r^2 times the mean of x times its weighted gradient
       auto scales = [&](float xx, float xg) {
         r = rsqrtf(fmaf(xx, inv_n, p.eps));
@@ -828,7 +829,7 @@ rotary_bwd_long_kernel(const __grid_constant__ Params p) {
         float y[E], x[E], w[E];
         if (there) u = __ldcg(reinterpret_cast<const uint4*>(d + head * rows.d_head));
         Row<T, L>::unpack(u, y);
-        turn.apply(p, y, 1.f, c0, buf);
+        turn.template apply<false>(p, y, 1.f, c0, buf);
         if (normed) {
           u = make_uint4(0u, 0u, 0u, 0u);
           if (there) u = __ldcg(reinterpret_cast<const uint4*>(xs + head * t.xs[2]));

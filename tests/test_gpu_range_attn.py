@@ -358,3 +358,53 @@ def test_caps_and_scales_far_from_the_usual(cap, scale, kind):
     o, grads = run(op, dev, place, host)
     # (the error of a capped score by the exponential is 3e-7 of the cap where the cap is reached; where it is not, of the score)
     check_all(ref, dtype, d, min(cap, ref["top"]), o, op.lse, grads)
+
+
+@pytest.mark.parametrize("dtype,d", [("f32", 64), ("bf16", 128)])
+def test_offsets_beyond_32_bits(dtype, d):
+    """A cache whose last token lies more than 2^31 elements behind its first; gradients of the same layout."""
+    Sq, Sk, apart = 3, 2200, 2 ** 20
+    ranges = torch.tensor([[[0, 2200], [2100, 2200], [1, 2199]]], dtype=torch.int32)
+    g = torch.Generator().manual_seed(3)
+    mk = lambda S, n: torch.randn((1, S, n, d), generator=g).to(DT[dtype])
+    q, k, v, do = mk(Sq, 2), mk(Sk, 1), mk(Sk, 1), mk(Sq, 2)
+    big = torch.empty(Sk * apart, dtype=DT[dtype], device="cuda")
+    k_far, v_far, dk, dv = [big.as_strided((1, Sk, 1, d), (Sk * apart, apart, d, 1), i * d) for i in range(4)]
+    k_far.copy_(k)
+    v_far.copy_(v)
+    op = RangeAttention(vb.make_range_shape(1, 2, 1, d, Sq, Sk, dtype), ranges.cuda(), with_backward=True)
+    o, dq = torch.empty_like(q, device="cuda"), torch.empty_like(q, device="cuda")
+    op.forward(q.cuda(), k_far, v_far, o)
+    op.backward(do.cuda(), dq, dk, dv)
+    op.check_status()
+    ref = P.range_attention(q, k, v, ranges, 0.0, do=do)
+    check_all(ref, dtype, d, 0.0, o, op.lse, [dq, dk, dv])
+    del big, k_far, v_far, dk, dv
+
+
+@pytest.mark.parametrize("kind", [("f32", 64), ("bf16", 128)], ids=lambda k: f"{k[0]}_{k[1]}")
+@pytest.mark.parametrize("B,Sq,shared", [(3, 1, True), (3, 1, False), (1, 300, True), (3, 700, False)])
+def test_a_captured_call_takes_new_ranges_of_a_growing_cache(B, Sq, shared, kind):
+    """The pieces that a long cache is cut into follow from the ranges: one captured forward, replayed as the cache grows from nothing to its
+    whole length, with samples that differ, against the statement; what lies behind a sequence does not matter."""
+    dtype, d = kind
+    Sk = 1500
+    g = torch.Generator().manual_seed(21)
+    mk = lambda S, n: torch.randn((B, S, n, d), generator=g).to(DT[dtype])
+    q, k, v = mk(Sq, 2), mk(Sk, 1), mk(Sk, 1)
+    dev = [x.cuda() for x in (q, k, v)]
+    of = lambda n: key_ranges([n] if shared else [n, n // 3, max(n - 1, 0)], n_queries=Sq, device="cpu")
+    op = RangeAttention(vb.make_range_shape(B, 2, 1, d, Sq, Sk, dtype, mask_batch=of(1).shape[0]), of(Sk).cuda())
+    o = torch.empty_like(dev[0])
+    op.forward(*dev, o)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        op.forward(*dev, o)
+    for n in (0, 1, 129, 1024, Sk):
+        op.set_ranges(of(n).cuda())
+        o.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_all(P.range_attention(q, k, v, of(n), 0.0), dtype, d, 0.0, o, op.lse)
+    op.check_status()

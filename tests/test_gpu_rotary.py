@@ -221,3 +221,21 @@ def test_what_is_not_finite_stays_where_it_is(layout, norm):
     else:
         same[0, 5] = same[0, 9] = False
     assert torch.equal(got[0][same], outs[0][same]) and torch.equal(got[1], outs[1])
+
+
+@pytest.mark.parametrize("B,S,token,sample", [(1, 2200, 2 ** 20, 0), (2, 5, 2 ** 28, 2 ** 31)])
+def test_offsets_beyond_32_bits(B, S, token, sample):
+    """The last token more than 2^31 elements behind the first; samples that do not follow one another at the tokens' distance."""
+    shape, op, x, dy, w, pos, f, axis, m = case(B, 2, 64, (1, 1, S), (1, 1, S), "bf16", (32,), "row", "half", seed=2)
+    big = torch.empty((B - 1) * sample + S * token, dtype=torch.bfloat16, device="cuda")
+    far = [big.as_strided((B, S, 2, 64), (sample or S * token, token, 64, 1), 128 * i) for i in range(4)]
+    for a, b in zip(far, x):
+        a.copy_(b)
+    ws = [t.cuda() for t in w]
+    op.forward(far[:2], far[2:], ws)
+    got = [torch.empty((B, S, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    op.backward([t.cuda() for t in dy], far[:2], got, ws)
+    for k in range(2):
+        check(far[2 + k], *P.norm_rotate(x[k], w[k], pos, f, axis, "half", "row", m), 5e-6, f"far {k}")
+        (dx, mag), _ = P.norm_rotate_grad(dy[k], x[k], w[k], pos, f, axis, "half", "row", m)
+        check(got[k], dx, mag, 5e-6, f"dx {k}")
