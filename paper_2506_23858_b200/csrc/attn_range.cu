@@ -99,23 +99,29 @@ __device__ __forceinline__ void plan_pieces(const Plan& plan, const RDims& D) {
     if (lane == who) length = len;
   }
   __syncthreads();
-  const int len = length, count = t < n ? (mine + len - 1) / len : 0;
-  int before = count;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, before, o);
-    if (lane >= o) before += x;
-  }
-  if (lane == 31) sums[warp] = before;
-  __syncthreads();
-  for (int w = 0; w < warp; ++w) before += sums[w];
+  // The order: the first pieces of all items, the second ones, ...: what runs at the same time reads the same keys (a frame of 1,560 tokens
+  // against 33K, 12 heads of a cache larger than the L2, item after item: 329 us, so 309).
+  const int len = length;
   if (t < n) {
-    plan.pieces[t] = count;
-    for (int k = 0; k < count; ++k) plan.work[before - count + k] = make_int4(t / D.nI, t % D.nI, k * len, k);
+    tiles[t] = (mine + len - 1) / len;
+    plan.pieces[t] = tiles[t];
   }
-  if (t == 1023) {
-    plan.head[0] = before;
-    plan.head[1] = len;
+  __syncthreads();
+  for (int k = warp; k < D.smax; k += 32) {    // (an item has at most smax pieces)
+    int before = 0;
+    for (int i = lane; i < n; i += 32) before += min(tiles[i], k);
+    before = __reduce_add_sync(0xffffffffu, before);
+    for (int i0 = 0; i0 < n; i0 += 32) {
+      const int i = i0 + lane;
+      const bool has = i < n && tiles[i] > k;
+      const uint32_t all = __ballot_sync(0xffffffffu, has);
+      if (has) plan.work[before + __popc(all & ((1u << lane) - 1u))] = make_int4(i / D.nI, i % D.nI, k * len, k);
+      before += __popc(all);
+    }
+    if (k == D.smax - 1 && lane == 0) {
+      plan.head[0] = before;
+      plan.head[1] = len;
+    }
   }
 }
 
