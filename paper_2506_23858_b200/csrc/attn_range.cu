@@ -100,7 +100,7 @@ __device__ __forceinline__ void plan_pieces(const Plan& plan, const RDims& D) {
   }
   __syncthreads();
   // The order: the first pieces of all items, the second ones, ...: what runs at the same time reads the same keys (a frame of 1,560 tokens
-  // against 33K, 12 heads of a cache larger than the L2, item after item: 329 us, so 309).
+  // against 31,200, 12 heads, a cache larger than the L2: 329 us item after item, so 309).
   const int len = length;
   if (t < n) {
     tiles[t] = (mine + len - 1) / len;
@@ -526,7 +526,7 @@ __device__ __forceinline__ void weigh(float s, bool in, float lse, const RDims& 
 // The gradients: one launch for dK / dV (an item is 64 keys of a key head, against the units that reach into them, all query heads of the
 // group) and dQ (an item is a unit, against the tiles of its hull, which works S and dP out again).  Where that leaves SMs without
 // an item, a cluster of C CTAs takes an item: each a C-th of what it streams, and their parts are added up through one another's shared
-// memory in the order of the CTAs.  (Two samples of 256 tokens, two heads of 64: 24 items, 86 us with two launches and a CTA each.)
+// memory in the order of the CTAs.  (Two samples of 256 tokens, two heads of 64: 24 items, 80 us with two launches and a CTA each, so 32.)
 template <int DH> constexpr int kRangeBwdSmem = (4 * kTileFloats<DH> + kRows * kLdP) * 4;
 
 // acc (rows 4 ty + i of a tile) of all CTAs of the cluster, summed: row r goes to put(r, column, four sums).  part: a tile in shared memory

@@ -6,6 +6,11 @@
 // takes part in the tiles that its own hull reaches; a score is compared with its row's range only in tiles where the unit's
 // bounds say that some row needs it.
 //
+// Bound by the exponentials of two tiles and the one score buffer, as the dense forward is; the weights are rounded to bf16 (2^-8) for P V, and o
+// is normalised by the sum of the rounded ones.  12 heads: 32,760 tokens by frames 3.1 ms (1110 TFLOP/s of the visible pairs), capped 3.5 to 3.8
+// (power-capped); 13,440 tokens, eight clips packed, 257 us (985); a frame of 1,560 tokens against 31,200 keys 309 us (970), its
+// pieces joined through memory; a token of each of four samples against 8K to 76K keys, four key heads, 362 MB, 74 us (4.9 TB/s).
+//
 // Every (item, unit) has at least one tile, masked as a whole if need be, and every tile at least one unit, so that no barrier skips a phase.
 //
 //   warp 0        TMA: K tiles into a ring of two stages, V tiles into one of three
