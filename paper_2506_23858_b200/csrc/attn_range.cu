@@ -239,9 +239,13 @@ __device__ __forceinline__ void load_unit(UnitRows& s, const RDims& D, const Pla
   }
 }
 
+// Forward: an item (64 packed rows, or a piece of their keys) per CTA and turn, one pass with the running maximum and sum.  Bound by the FMA
+// pipe; with few items by the chain of tiles.  Then a cluster of C CTAs takes an item, every C-th tile each, and their parts are joined through one
+// another's shared memory, in the order of the CTAs.  (Two samples of 256 tokens, two heads of 64 on one key head, fp32: 16 items, 20.5 us with a CTA
+// each, 15 with four.)
 template <typename T, int DH>
 __global__ void __launch_bounds__(kThreads, 2)
-range_fwd_kernel(const RDims D, const Plan plan, const FwdArgs a) {
+range_fwd_kernel(const RDims D, const Plan plan, const FwdArgs a, const int C) {
   if (!grid_begin()) return;
   extern __shared__ __align__(16) float simt_smem[];
   float* Qs = simt_smem;
@@ -251,7 +255,8 @@ range_fwd_kernel(const RDims D, const Plan plan, const FwdArgs a) {
   const int t = threadIdx.x, ty = t >> 4, tx = t & 15;
   const bool cut = D.smax > 1;
   const long long n_items = cut ? (long long)plan.head[0] * D.reps : (long long)D.B * D.Hk * D.nI, all_rows = (long long)D.B * D.Hk * D.rows;
-  for (long long item = blockIdx.x; item < n_items; item += gridDim.x) {
+  const int rank = blockIdx.x % C;
+  for (long long item = blockIdx.x / C; item < n_items; item += gridDim.x / C) {
     int b, hk, u, piece = 0, first = 0, last = INT32_MAX;
     if (cut) {
       const int4 w = plan.work[item / D.reps];
@@ -288,13 +293,13 @@ range_fwd_kernel(const RDims D, const Plan plan, const FwdArgs a) {
       for (int c = 0; c < DH / 16; ++c) acc[i][c] = 0.f;
     }
     const bool live = (ty & ~1) * 4 < D.tpt * D.G;    // (a warp has eight rows)
-    for (int t0 = k_lo; t0 < k_hi; t0 += kRows) {
-      const int nv = min(kRows, k_hi - t0);
-      next.fetch([&](int r) { return r < nv ? kb + (long long)(t0 + r) * a.ks.t : nullptr; });
+    for (long long t0 = k_lo + (long long)rank * kRows; t0 < k_hi; t0 += (long long)C * kRows) {
+      const int nv = (int)min((long long)kRows, k_hi - t0);
+      next.fetch([&](int r) { return r < nv ? kb + (t0 + r) * a.ks.t : nullptr; });
       __syncthreads();
       next.store(KVs);
       __syncthreads();
-      next.fetch([&](int r) { return r < nv ? vb + (long long)(t0 + r) * a.vs.t : nullptr; });
+      next.fetch([&](int r) { return r < nv ? vb + (t0 + r) * a.vs.t : nullptr; });
       float corr[4];
       if (live) {
         float s[4][4];
@@ -305,7 +310,7 @@ range_fwd_kernel(const RDims D, const Plan plan, const FwdArgs a) {
           float mx = -INFINITY;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int key = t0 + tx + 16 * j;
+            const int key = (int)t0 + tx + 16 * j;
             s[i][j] = key >= rg.x && key < rg.y && tx + 16 * j < nv ? capped(s[i][j], D.scale, D.cap) : -INFINITY;
             mx = fmaxf(mx, s[i][j]);
           }
@@ -334,34 +339,65 @@ range_fwd_kernel(const RDims D, const Plan plan, const FwdArgs a) {
         add_weighted<DH>(Ps, KVs, ty, tx, kRows, acc);
       }
     }
-    if (!live) continue;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float total = l[i];
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-      const int r = 4 * ty + i, tok = rows.tok[r];
-      if (tok < 0) continue;
+    // four channels of a row: the sum of its weights times values, the maximum and the sum of the weights
+    auto put = [&](int r, int col, const float4& sum, float m, float total) {
+      const int tok = rows.tok[r], g = r % D.G;
+      if (tok < 0) return;
       const bool none = total == 0.f;                // (no key: everything is 0 and lse -inf; a NaN stays one)
-      const float inv = none ? 0.f : 1.0f / total, row_lse = none ? -INFINITY : m_[i] + logf(total);
-      const int g = r % D.G;
+      const float inv = none ? 0.f : 1.0f / total, row_lse = none ? -INFINITY : m + logf(total);
       const long long packed = (long long)bhk * D.rows + (long long)tok * D.G + g, head = hk * D.G + g;
-#pragma unroll
-      for (int c = 0; c < DH / 64; ++c) {
-        const int col = 64 * c + 4 * tx;
-        const float4 x = make_float4(acc[i][4 * c] * inv, acc[i][4 * c + 1] * inv, acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv);
-        if (!cut) {
-          T* resid = a.resid ? reinterpret_cast<T*>(a.resid) + (((long long)b * D.Sq + tok) * D.Hq + head) * DH + col : nullptr;
-          store4_resid(reinterpret_cast<T*>(a.o) + b * a.os.b + tok * a.os.t + head * a.os.h + col, resid, x);
-        } else {
-          store4(a.part_o + (piece * all_rows + packed) * DH + col, x);
-        }
+      const float4 x = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+      if (!cut) {
+        T* resid = a.resid ? reinterpret_cast<T*>(a.resid) + (((long long)b * D.Sq + tok) * D.Hq + head) * DH + col : nullptr;
+        store4_resid(reinterpret_cast<T*>(a.o) + b * a.os.b + tok * a.os.t + head * a.os.h + col, resid, x);
+      } else {
+        store4(a.part_o + (piece * all_rows + packed) * DH + col, x);
       }
-      if (tx == 0) {
+      if (col == 0) {
         if (!cut) a.lse[((long long)b * D.Hq + head) * D.Sq + tok] = row_lse;
         else a.part_lse[piece * all_rows + packed] = row_lse;
       }
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+    if (C == 1) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < DH / 64; ++c)
+          put(4 * ty + i, 64 * c + 4 * tx, make_float4(acc[i][4 * c], acc[i][4 * c + 1], acc[i][4 * c + 2], acc[i][4 * c + 3]), m_[i], l[i]);
+      continue;
     }
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    __syncthreads();                                 // (values and weights have been read)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 4 * ty + i;
+#pragma unroll
+      for (int c = 0; c < DH / 64; ++c)
+        *reinterpret_cast<float4*>(KVs + r * kLd<DH> + 64 * c + 4 * tx) = make_float4(acc[i][4 * c], acc[i][4 * c + 1], acc[i][4 * c + 2], acc[i][4 * c + 3]);
+      if (tx == 0) { Ps[r] = m_[i]; Ps[kRows + r] = l[i]; }
+    }
+    cluster.sync();
+    constexpr int V = DH / 4;
+    for (int e = rank * kThreads + t; e < kRows * V; e += C * kThreads) {
+      const int r = e / V, col = e % V * 4;
+      float top = -INFINITY, total = 0.f;
+      for (int n = 0; n < C; ++n) top = fmaxf(top, cluster.map_shared_rank(Ps, n)[r]);
+      const float used = top == -INFINITY ? 0.f : top;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int n = 0; n < C; ++n) {
+        const float* stats = cluster.map_shared_rank(Ps, n);
+        const float w = expf(stats[r] - used);
+        const float4 x = *reinterpret_cast<const float4*>(cluster.map_shared_rank(KVs, n) + r * kLd<DH> + col);
+        total = fmaf(w, stats[kRows + r], total);
+        sum.x = fmaf(w, x.x, sum.x); sum.y = fmaf(w, x.y, sum.y); sum.z = fmaf(w, x.z, sum.z); sum.w = fmaf(w, x.w, sum.w);
+      }
+      put(r, col, sum, top, total);
+    }
+    cluster.sync();                                  // (nobody reads this CTA's part any more)
   }
 }
 
@@ -754,11 +790,13 @@ static int make_rdims(const vmoba_range_shape* s, RDims* o) {
   o->nK = (s->Sk + o->TR - 1) / o->TR;
   o->nI = o->tc ? (o->nU + 1) / 2 : o->nU;
   // Fewer items than four for every SM: they are cut, where there is something to cut (a tile takes the tensor cores 2 us, the CUDA cores 4,
-  // joining the pieces 5 to 10: 256 keys in tiles of 64 took 20 us whole and 26 in pieces), eight pieces per SM at most on average and 64 of
-  // an item.
+  // joining the pieces 5 to 10), eight pieces per SM at most on average and 64 of an item.  On the CUDA cores clusters do the same without
+  // that, where eight CTAs for each item fill the SMs and there are up to eight tiles for every SM (fp32, heads of 64, 900 tokens x 2 heads: 45 us
+  // in pieces, 29 by clusters; one token x 2 heads against 900 keys: 14 and 18; 1,200 queries x 4 heads of 128 against 1,900 keys: 196 and 288).
   const long long items = (long long)s->B * s->kv_heads * o->nI;
+  const bool clusters = !o->tc && 8 * items >= kSms && items * o->nK <= 8 * kSms;
   o->smax = 1;
-  if (items < kFewItems && o->nK >= 8) o->smax = (int)std::min<long long>(std::min(64, o->nK), (8 * kSms + items - 1) / items);
+  if (items < kFewItems && o->nK >= 8 && !clusters) o->smax = (int)std::min<long long>(std::min(64, o->nK), (8 * kSms + items - 1) / items);
   o->reps = s->mask_batch == 1 ? s->B * s->kv_heads : s->kv_heads;
   return VMOBA_OK;
 }
@@ -838,7 +876,13 @@ static int forward(const RDims& D, const Plan& plan, FwdArgs a, cudaStream_t st)
   } else {
     const long long items = (long long)D.B * D.Hk * D.nI * D.smax;
     VMOBA_CUDA_OK(allow_smem(range_fwd_kernel<T, DH>, simt::kFwdSmem<DH>));
-    launch_kernel(early_simt(D), range_fwd_kernel<T, DH>, grid_for(items, 8), kThreads, simt::kFwdSmem<DH>, st, D, plan, a);
+    int C = 1;
+    if (D.smax == 1)
+      while (C < 8 && items * C * 2 <= 2 * kSms && D.nK >= 2 * C) C *= 2;
+    if (C > 1)
+      launch_cluster(early_simt(D), C, range_fwd_kernel<T, DH>, (int)items * C, kThreads, simt::kFwdSmem<DH>, st, D, plan, a, C);
+    else
+      launch_kernel(early_simt(D), range_fwd_kernel<T, DH>, grid_for(items, 8), kThreads, simt::kFwdSmem<DH>, st, D, plan, a, C);
     VMOBA_LAUNCH_OK(1);
   }
   if (D.smax > 1) {
