@@ -914,20 +914,21 @@ weight_sum_kernel(const float* __restrict__ part, int n_parts, int n_w, WeightOu
 }
 
 // ------------------------------------------------------------------------------ host
-// How a row is laid over warps: up to `most` vectors per thread in the fewest idle lanes, of equals the fewest warps (40 heads of 128: 549 us with
-// four warps of five vectors, 618 with five of four); CTAs of about `warps` warps.  false: the row is longer than that, or its
-// `tensors` weights are more than two CTAs of an SM have room for.
+// How a row is laid over warps, up to `most` vectors per thread: with the most rows that a CTA of `warps` warps has under way, of equals in the
+// fewest idle lanes (40 heads of 128: 549 us with four warps of five vectors, 618 with five of four; backward of 26 heads, norm per head, 54,543
+// tokens: 923 us with seven warps of two vectors, the fewest idle lanes, 564 with five of three).  false: the row is longer than that, or
+// its `tensors` weights are more than two CTAs of an SM have room for.
 constexpr int kFwdVectors = 6, kBwdVectors = 3;
 constexpr int kSmemMost = 96 * 1024;
 static bool lay_out(const Dims& D, int most, int warps, int tensors, Params* p, int* nv) {
   const int nvec = D.heads * D.d * D.es / 16;
   int best = INT32_MAX;
-  *nv = 0;
-  for (int w = 1; w <= kMaxWarps; ++w)
-    for (int v = 1; v <= most; ++v) {
-      const int idle = w * 32 * v - nvec;
-      if (idle >= 0 && idle < best) { best = idle; *nv = v; p->wpr = w; p->groups = warps / w; }
-    }
+  *nv = 0; p->groups = 0;
+  for (int w = 1; w <= kMaxWarps; ++w) {
+    const int v = (nvec + 32 * w - 1) / (32 * w), idle = w * 32 * v - nvec;
+    if (v > most || warps / w < p->groups || (warps / w == p->groups && idle >= best)) continue;
+    best = idle; *nv = v; p->wpr = w; p->groups = warps / w;
+  }
   if (best < INT32_MAX &&
       (p->norm != VMOBA_ROTARY_NORM_ROW || (size_t)tensors * 32 * p->wpr * most * (16 / D.es) * sizeof(float) <= kSmemMost))
     return true;
