@@ -911,8 +911,11 @@ static int backward(const RDims& D, const Plan& plan, const BwdArgs& a, const vo
   } else {
     VMOBA_CUDA_OK(allow_smem(range_bwd_kernel<T, DH>, kRangeBwdSmem<DH>));
     const long long items = (long long)D.B * D.Hk * (D.nK + D.nU), room = (long long)kSms * (DH == 64 ? 2 : 1);
+    // The items that stream the most decide; of the others, which are short then, more come one after another.  (Room for all items at once
+    // instead: 500 tokens x 2, eight heads of 64 on one key head, bf16, 469 us, so 158; 600 tokens, four of 128 on one, fp32, 363 and 124.)
+    const long long longest = (long long)D.B * D.Hk * std::min(D.nK, D.nU);
     int C = 1;
-    while (C < 8 && items * C * 2 <= room && std::max(D.nU, D.nK) >= 2 * C) C *= 2;
+    while (C < 8 && longest * C * 2 <= room && std::max(D.nU, D.nK) >= 2 * C) C *= 2;
     const int grid = C * (int)std::max<long long>(1, std::min<long long>(items, (long long)sm_count() * 4 / C));
     if (C > 1) launch_cluster(early_simt(D), C, range_bwd_kernel<T, DH>, grid, kThreads, kRangeBwdSmem<DH>, st, D, plan, a, (T*)dq, dqs, C);
     else launch_kernel(early_simt(D), range_bwd_kernel<T, DH>, grid, kThreads, kRangeBwdSmem<DH>, st, D, plan, a, (T*)dq, dqs, C);
