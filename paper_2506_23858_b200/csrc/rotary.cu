@@ -738,11 +738,12 @@ rotary_bwd_kernel(const __grid_constant__ Params p) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           scales(sums[2 * i], sums[2 * i + 1]);
+          if (i >= have) r = back = 0.f;     // (beyond the row: without an eps r is infinite there, and dw is a sum over all vectors)
           float x[E];
           opaque(x_raw[i]);
           Row<T, L>::unpack(x_raw[i], x);
           times<E>(x, r);
-          finish<E>(y[i], x, f, r, back, acc[0]);      // (zeros beyond the row)
+          finish<E>(y[i], x, f, r, back, acc[0]);
         }
       }
 #pragma unroll
@@ -858,6 +859,7 @@ rotary_bwd_long_kernel(const __grid_constant__ Params p) {
           float two[2] = {s[0] + s[1], s[2] + s[3]};
           head_sums<2>(two, at.V);
           scales(two[0], two[1]);
+          if (!there) r = back = 0.f;        // (as above)
         }
         times<E>(x, r);
         float part[E];
