@@ -460,14 +460,14 @@ class RangeAttention:
         self.o_resid = e((s.B, s.Sq, s.heads, s.head_dim), torch.bfloat16) if with_backward and s.dtype == vb.BF16 else None
         self.ws = e(max(vb.range_workspace_bytes(s), vb.range_workspace_bytes(s, True) if with_backward else 0))
         self.with_backward = with_backward
-        self._kept = None
         self.set_ranges(key_range)
 
     def set_ranges(self, key_range):
-        """Takes other key ranges (a cache that has grown, another packing)."""
+        """Takes other key ranges (a cache that has grown, another packing).  backward() then needs another forward()."""
         s = self.shape
         if tuple(key_range.shape) != (s.mask_batch, s.Sq, 2) or key_range.dtype != torch.int32 or key_range.device != self.device:
             raise ValueError("RangeAttention: key ranges are int32 [mask_batch, Sq, 2] on the plan's device")
+        self._kept = None          # (the last forward's lse and o belong to the ranges it ran under)
         with _on(self.device):
             vb.vmoba_range_plan(s, key_range.contiguous(), self.plan)
 
@@ -502,7 +502,7 @@ class RangeAttention:
         """Gradients of the last forward()."""
         s = self.shape
         if self._kept is None:
-            raise ValueError("RangeAttention: backward() follows a forward() of an object made with_backward")
+            raise ValueError("RangeAttention: backward() follows a forward() under the same ranges, of an object made with_backward")
         do, dos = self._tensor(do, s.Sq, s.heads, "do")
         _, dqs = self._tensor(dq_out, s.Sq, s.heads, "dq_out", True)
         _, dks = self._tensor(dk_out, s.Sk, s.kv_heads, "dk_out", True)
