@@ -71,7 +71,7 @@ def rotary_frequencies(pairs_per_axis, theta: float = 10000.0, scaling: str = "n
 
 
 class Rotary:
-    """Norm and rotary positions of q and k of one layer shape: holds the tables (and the backward's scratch).
+    """Norm and rotary positions of q and k of layers of one shape, in whatever blocks: holds the tables (and the backward's scratch).
 
     positions: int32 [S, axes], or [B, S, axes] where samples differ (clips packed into one sequence restart theirs); freq fp64 and
     axis int32 [pairs] on the device (rotary_frequencies); layout "interleaved" or "half"; norm "none", "head" or "row"."""
@@ -125,25 +125,35 @@ class Rotary:
                 raise ValueError(f"Rotary: a weight has to be {self.n_weights} contiguous fp32 values on {self.device}")
         return weights
 
+    def _blocks(self, shape):
+        """The shape whose blocks block order means: this object's, or another of the same sizes (positions know no blocks)."""
+        if shape is None:
+            return self.shape
+        if any(getattr(shape, n) != getattr(self.shape, n) for n in ("B", "S", "heads", "head_dim", "dtype")):
+            raise ValueError("Rotary: a layer's shape has to have the samples, tokens, heads, head_dim and type of the Rotary's")
+        return shape
+
     def forward(self, xs, outs, weights=None, block_order=False, moved=(), moved_outs=(), perm=None, shape=None):
         """Norms and rotates the raster-order tensors xs into outs: raster order, or block-major [B, heads, S, d] with block_order.
-        moved: tensors that only go along (v into block order).  shape: the layer's with another block shape."""
+        moved: tensors that only go along (v into block order).  shape: one of the same sizes in other blocks."""
         xs, outs = list(xs) + list(moved), list(outs) + list(moved_outs)
         if len(xs) != len(outs) or not 1 <= len(xs) <= 4:
             raise ValueError("Rotary: one to four tensors, and an output for each")
+        shape = self._blocks(shape)
         src = [self._raster(x, "an input") for x in xs]
         dst = None if block_order else [self._raster(x, "an output") for x in outs]
         if block_order:
             for x in outs:
                 self._block_major(x, "an output in block order")
         with _on(self.device):
-            vb.vmoba_rotary(shape or self.shape, self.spec, len(xs) - len(moved), xs, src, outs, dst, self._weights(weights, len(xs)),
+            vb.vmoba_rotary(shape, self.spec, len(xs) - len(moved), xs, src, outs, dst, self._weights(weights, len(xs)),
                             self.positions, self.freq, self.axis, perm)
 
-    def backward(self, d_outs, xs, dxs, weights=None, block_order=False):
+    def backward(self, d_outs, xs, dxs, weights=None, block_order=False, shape=None):
         """Gradients of forward(): dxs (raster order; may be d_outs) from d_outs (block-major with block_order) and the forward's
-        xs (unused without a norm).  Returns the weights' gradients, fp32, or None without a norm."""
+        xs (unused without a norm); shape as given to that.  Returns the weights' gradients, fp32, or None without a norm."""
         n = len(d_outs)
+        shape = self._blocks(shape)
         if n != len(dxs) or not 1 <= n <= 4 or (self.n_weights and (xs is None or len(xs) != n)):
             raise ValueError("Rotary: one to four gradients, as many results and, with a norm, as many inputs")
         d_strides = None if block_order else [self._raster(x, "a gradient") for x in d_outs]
@@ -156,7 +166,7 @@ class Rotary:
         if self.n_weights:
             self._scratch(n)
         with _on(self.device):
-            vb.vmoba_rotary_bwd(self.shape, self.spec, d_outs, d_strides, xs if self.n_weights else None, x_strides,
+            vb.vmoba_rotary_bwd(shape, self.spec, d_outs, d_strides, xs if self.n_weights else None, x_strides,
                                 self._weights(weights, n), dxs, dx_strides, dw, self.positions, self.freq, self.axis, self.ws)
         return dw
 
@@ -306,7 +316,8 @@ class VmobaLayer:
     def forward(self, q, k, v, tau, o_out, fold_o=None, rotary=None, weights=None):
         """q, k, v, o_out: [B, S, heads, d] raster-order tensors on the device.
 
-        rotary: a Rotary of the layer's shape that q and k go through on their way into block order (its weights: of q and of k).
+        rotary: a Rotary of the layer's sizes, whatever its blocks, that q and k go through on their way into block order (its weights:
+        of q and of k).
 
         fold_o: let the forward kernels write o in raster order themselves (bf16, head_dim 128) instead of an inverse
         partition pass; off by default (measured on B200: the scattered 256-byte row writes cost the attention kernel
@@ -314,7 +325,7 @@ class VmobaLayer:
         # k last: the centroids, computed next, find the end of it in L2
         if rotary is not None:
             rotary.forward((k, q), (self.k_bm, self.q_bm), None if weights is None else (weights[1], weights[0]), block_order=True,
-                           moved=(v,), moved_outs=(self.v_bm,), perm=self.perm)
+                           moved=(v,), moved_outs=(self.v_bm,), perm=self.perm, shape=self.shape)
         else:
             self.partition_many((v, q, k), (self.v_bm, self.q_bm, self.k_bm), perm=self.perm)
         self.block_scores()
@@ -349,7 +360,7 @@ class VmobaLayer:
         self.attn_bwd()
         if rotary is not None:
             self.partition(dv_out, self.dv_bm, inverse=True)
-            return rotary.backward((self.dq_bm, self.dk_bm), qk, (dq_out, dk_out), weights, block_order=True)
+            return rotary.backward((self.dq_bm, self.dk_bm), qk, (dq_out, dk_out), weights, block_order=True, shape=self.shape)
         self.partition_many((dq_out, dk_out, dv_out), (self.dq_bm, self.dk_bm, self.dv_bm), inverse=True)
 
     def check_status(self):
