@@ -71,10 +71,12 @@ def rotary_frequencies(pairs_per_axis, theta: float = 10000.0, scaling: str = "n
 
 
 class Rotary:
-    """Norm and rotary positions of q and k of layers of one shape, in whatever blocks: holds the tables (and the backward's scratch).
+    """Norm and rotary positions of q and k of layers of one shape, in whatever blocks: holds the tables, which nothing writes, so that
+    any number of layers, streams and captured graphs can use one at the same time.
 
     positions: int32 [S, axes], or [B, S, axes] where samples differ (clips packed into one sequence restart theirs); freq fp64 and
-    axis int32 [pairs] on the device (rotary_frequencies); layout "interleaved" or "half"; norm "none", "head" or "row"."""
+    axis int32 [pairs] on the device (rotary_frequencies); layout "interleaved" or "half"; norm "none", "head" or "row".  with_backward is taken as
+    by the other classes; nothing is held for it, since a backward's scratch is the call's own."""
 
     def __init__(self, shape, positions, freq, axis, layout="interleaved", norm="none", mscale=1.0, eps=1e-6, with_backward=False):
         s = shape
@@ -94,14 +96,8 @@ class Rotary:
         self.n_weights = {"none": 0, "head": s.head_dim, "row": s.heads * s.head_dim}[norm]
         if vb.rotary_workspace_bytes(s, self.spec, 1) == 0:
             raise ValueError("Rotary: shape, pairs (up to head_dim / 2), axes (1 to 4), mscale (> 0) or eps (>= 0) out of range")
-        self.ws = None
-        if with_backward:
-            self._scratch(2)
-
-    def _scratch(self, n):
-        need = vb.rotary_workspace_bytes(self.shape, self.spec, n)
-        if self.ws is None or self.ws.numel() < need:
-            self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        # bytes of a backward's scratch by the number of tensors
+        self._scratch = {n: vb.rotary_workspace_bytes(s, self.spec, n) for n in range(1, 5)} if self.n_weights else {}
 
     def _raster(self, x, what):
         if x.shape == self._size and x.dtype is self.dtype and x.device == self.device:
@@ -163,11 +159,10 @@ class Rotary:
         dx_strides = [self._raster(x, "a result") for x in dxs]
         x_strides = [self._raster(x, "an input") for x in xs] if self.n_weights else None
         dw = [torch.empty(self.n_weights, dtype=torch.float32, device=self.device) for _ in range(n)] if self.n_weights else None
-        if self.n_weights:
-            self._scratch(n)
+        ws = torch.empty(self._scratch[n], dtype=torch.uint8, device=self.device) if self.n_weights else None
         with _on(self.device):
             vb.vmoba_rotary_bwd(shape, self.spec, d_outs, d_strides, xs if self.n_weights else None, x_strides,
-                                self._weights(weights, n), dxs, dx_strides, dw, self.positions, self.freq, self.axis, self.ws)
+                                self._weights(weights, n), dxs, dx_strides, dw, self.positions, self.freq, self.axis, ws)
         return dw
 
 
