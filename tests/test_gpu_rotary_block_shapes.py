@@ -67,3 +67,18 @@ def test_a_shape_of_other_sizes_is_refused():
             with pytest.raises(ValueError):
                 layer.forward(y, y, y, 0.4, torch.empty_like(y), rotary=rot)
     assert vb.kernel_launches() == before and bool((out == 2).all())
+
+
+def test_a_permutation_table_that_does_not_hold_the_tokens_is_refused():
+    rot = _rotary(3, 64, "f32", GRID, (1, 8, 8), "row")
+    x, out = torch.randn((1, 256, 3, 64), device="cuda"), torch.empty((1, 3, 256, 64), device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    before = vb.kernel_launches()
+    for bad in (torch.empty(255, **i32), torch.empty(256, dtype=torch.int64, device="cuda"), torch.empty(512, **i32)[::2],
+                torch.empty(256, dtype=torch.int32), torch.empty((1, 256), **i32)):
+        with pytest.raises(ValueError):
+            rot.forward((x,), (out,), block_order=True, perm=bad)
+    assert vb.kernel_launches() == before
+    perm = torch.full((256,), -1, **i32)
+    rot.forward((x,), (torch.empty_like(x),), perm=perm)                 # (raster order: the table alone)
+    assert torch.equal(perm.sort().values, torch.arange(256, **i32))
