@@ -141,7 +141,7 @@ class Rotary:
         if block_order:
             for x in outs:
                 self._block_major(x, "an output in block order")
-        if perm is not None and (perm.shape != (self.shape.S,) or perm.dtype != torch.int32 or not perm.is_contiguous() or perm.device != self.device):
+        if perm is not None and (perm.numel() < self.shape.S or perm.dtype != torch.int32 or not perm.is_contiguous() or perm.device != self.device):
             raise ValueError(f"Rotary: perm has to be {self.shape.S} contiguous int32 values on {self.device}")
         with _on(self.device):
             vb.vmoba_rotary(shape, self.spec, len(xs) - len(moved), xs, src, outs, dst, self._weights(weights, len(xs)),

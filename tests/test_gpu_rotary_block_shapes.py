@@ -75,10 +75,12 @@ def test_a_permutation_table_that_does_not_hold_the_tokens_is_refused():
     i32 = dict(dtype=torch.int32, device="cuda")
     before = vb.kernel_launches()
     for bad in (torch.empty(255, **i32), torch.empty(256, dtype=torch.int64, device="cuda"), torch.empty(512, **i32)[::2],
-                torch.empty(256, dtype=torch.int32), torch.empty((1, 256), **i32)):
+                torch.empty(256, dtype=torch.int32)):
         with pytest.raises(ValueError):
             rot.forward((x,), (out,), block_order=True, perm=bad)
     assert vb.kernel_launches() == before
-    perm = torch.full((256,), -1, **i32)
-    rot.forward((x,), (torch.empty_like(x),), perm=perm)                 # (raster order: the table alone)
-    assert torch.equal(perm.sort().values, torch.arange(256, **i32))
+    for shape in ((256,), (1, 256), (300,)):
+        perm = torch.full(shape, -1, **i32)
+        rot.forward((x,), (torch.empty_like(x),), perm=perm)             # (raster order: the table alone)
+        perm = perm.flatten()
+        assert torch.equal(perm[:256].sort().values, torch.arange(256, **i32)) and bool((perm[256:] == -1).all())
