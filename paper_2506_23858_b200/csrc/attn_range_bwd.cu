@@ -77,6 +77,7 @@ struct Params {
   float scale, scale_log2;     // scale_log2: scores -> exp2 domain, not capped
   Cap cap;
   float cap_inv2;              // -1 / c'^2
+  float cap_masked;            // stands for a capped score outside its query's range: a weight of 0 and a finite slope
   __nv_bfloat16 *dk, *dv;
   Strides dks, dvs;
   int dkv_32;                  // rows of dk and dv are 32-byte aligned: they go out with 32-byte stores
@@ -582,8 +583,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         };
         // (the rare cases' code is out of the way and short: beside the other roles' it does not fit the instruction cache)
         if constexpr (CAP) {
-          // scores -> c' tanh.  What no product has written (queries beyond the unit's) has no say in how the others are capped; -10^15: a weight
-          // of 0 and a finite slope
+          // scores -> c' tanh.  What no product has written (queries beyond the unit's) has no say in how the others are capped
           if (__builtin_expect(stale, 0)) mask(0u);
           float m0 = 0.f, m1 = 0.f;
 #pragma unroll
@@ -621,7 +621,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
               for (int i = 0; i < 32; ++i)
                 pv[rh][i] = __float_as_uint(fmaf(rcp(1.0f + ex2(__uint_as_float(pv[rh][i]) * p.cap.twice_log2)), -2.0f * p.cap.c, p.cap.c));
           }
-          if (__builtin_expect(masked || stale, 0)) mask(0xd8635fa9u);
+          if (__builtin_expect(masked || stale, 0)) mask(__float_as_uint(p.cap_masked));
         } else {
           if (__builtin_expect(masked, 0)) mask(0xff800000u);
         }
@@ -798,7 +798,10 @@ int tc_range_bwd(const RDims& D, const Plan& plan, const BwdArgs& a, void* dq, c
   p.scale_log2 = D.scale * LOG2E;
   p.cap = make_cap(D);
   if (p.cap.pre != 1.0f) p.cap.most = -1.0f;
-  p.cap_inv2 = D.cap > 0.f ? -1.0f / (p.cap.c * p.cap.c) : 0.f;
+  // lse2 is -c' at least, so that -2 c' - 256 is a weight of 0, and its slope 1 - (2 + 256 / c')^2.  Beyond caps of 10^18, where squares leave fp32's
+  // range, slopes are 1, which they are to 2^-24 where scores stay below 10^14.
+  p.cap_inv2 = D.cap > 0.f && p.cap.c <= 1e18f ? -1.0f / (p.cap.c * p.cap.c) : 0.f;
+  p.cap_masked = -fminf(2.0f * p.cap.c + 256.0f, 4e18f);
   p.dk = (__nv_bfloat16*)a.dk; p.dv = (__nv_bfloat16*)a.dv; p.dks = a.dks; p.dvs = a.dvs;
   auto whole = [](const void* x, const Strides& s) {
     return reinterpret_cast<uintptr_t>(x) % 32 == 0 && s.b % 16 == 0 && s.t % 16 == 0 && s.h % 16 == 0;

@@ -704,14 +704,15 @@ bool make_tmap_units(CUtensorMap* map, const void* base, const RDims& D, const S
 }
 
 // The polynomials' coefficients with the factors of score and result folded in.  Where the score's would leave fp32's range (caps of some
-// hundred times what is usual, scales far from it) scores are multiplied by it first.
+// hundred times what is usual, scales far from it) scores are multiplied by it first.  Scores of less than 10^-9 change no
+// weight: tanh is taken of scale s / cap whatever the cap, and multiplied by 10^-9 at least, so that c'^2 is a number of fp32's.
 Cap make_cap(const RDims& D) {
   static const double k[5] = {0.9999994349, -0.333282515, 0.1325898302, -0.05005629744, 0.01292962787};
   static const double q[4] = {0.9999556007, -0.3322276355, 0.1257709159, -0.03377827421};
   Cap c = {};
   if (!(D.cap > 0.f)) return c;
-  double a = (double)D.scale / D.cap;
-  const double top = (double)D.cap * 1.4426950408889634;
+  double a = std::min((double)D.scale / D.cap, 1e30);
+  const double top = std::max((double)D.cap, 1e-9) * 1.4426950408889634;
   c.c = (float)top;
   c.pre = 1.f;
   if (!(a >= 2e-4 && a <= 1e3 && top <= 1e6)) { c.pre = (float)a; a = 1.0; }
