@@ -62,7 +62,6 @@ struct Cap {
   float pre;                     // scores are multiplied by this first: 1 with a folded into all that follows, or a
   float most;                    // |score| up to this: by the polynomial
   float p[5];                    // its coefficients of s, s^3, ...
-  float q[4];                    // of one with a term less, off by 3.6e-6 of c': enough where only weights are made that bf16 rounds (2^-8)
 };
 Cap make_cap(const RDims& D);      // attn_range_fwd.cu
 

@@ -7,8 +7,9 @@
 //     dP^T = V dO^T;  dS^T = P^T (dP^T - D) (1 - tanh^2);  dK += dS^T Q;  dQ^T = K^T dS^T, added into an fp32 accumulator
 // P and dS are rounded to bf16 (2^-8 each, once) for the products that the tensor cores do with them; in fp32 halves they would be twice
 // the products, and dQ, dK and dV are rounded to the same type after that.  All sums, D and the weights under dS are fp32.
-// The slope 1 - tanh^2 is taken into the fp32 weights that the second step keeps, at no register.  tanh comes from a polynomial like the
-// forward's, a term shorter, where a warp's scores allow, else from 1 - 2 / (1 + exp(2 x)).
+// The slope 1 - tanh^2 is taken into the fp32 weights that the second step keeps, at no register.  tanh comes from the forward's polynomial
+// where a warp's scores allow, else from 1 - 2 / (1 + exp(2 x)): the same error in the weights and in the lse that they are divided by, so that
+// it leaves their sum at one.  (With a term less, off by 4.4e-5 of a score, weights of scores of 300 were 1.3 % off, all to the same side.)
 //
 // Bound by the exponentials, the turns of dQ and the tensor cores' waits for both, as the dense backward is.  13,440 tokens x 12 heads: eight
 // clips packed, 633 GFLOP, 866 us (730 TFLOP/s); two clips by frames, key heads shared by three, 1.03 ms (735), capped 1.32 ms (575).
@@ -596,10 +597,10 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
             for (int rh = 0; rh < 2; ++rh)
 #pragma unroll
               for (int i = 0; i < 32; i += 2) {
-                float x0 = __uint_as_float(pv[rh][i]), x1 = __uint_as_float(pv[rh][i + 1]), z0, z1, r0 = p.cap.q[3], r1 = p.cap.q[3];
+                float x0 = __uint_as_float(pv[rh][i]), x1 = __uint_as_float(pv[rh][i + 1]), z0, z1, r0 = p.cap.p[4], r1 = p.cap.p[4];
                 mul2(z0, z1, x0, x1, x0, x1);
 #pragma unroll
-                for (int k = 2; k >= 0; --k) fma2(r0, r1, r0, r1, z0, z1, p.cap.q[k], p.cap.q[k]);
+                for (int k = 3; k >= 0; --k) fma2(r0, r1, r0, r1, z0, z1, p.cap.p[k], p.cap.p[k]);
                 mul2(x0, x1, r0, r1, x0, x1);
                 pv[rh][i] = __float_as_uint(x0);
                 pv[rh][i + 1] = __float_as_uint(x1);
@@ -610,7 +611,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
 #pragma unroll
               for (int i = 0; i < 32; ++i) {
                 const float x = __uint_as_float(pv[rh][i]) * p.cap.pre, z = x * x;
-                const float near = x * fmaf(fmaf(fmaf(p.cap.q[3], z, p.cap.q[2]), z, p.cap.q[1]), z, p.cap.q[0]);
+                const float near = x * fmaf(fmaf(fmaf(fmaf(p.cap.p[4], z, p.cap.p[3]), z, p.cap.p[2]), z, p.cap.p[1]), z, p.cap.p[0]);
                 const float far = fmaf(rcp(1.0f + ex2(x * p.cap.twice_log2)), -2.0f * p.cap.c, p.cap.c);
                 pv[rh][i] = __float_as_uint(fabsf(x) <= 0.75f ? near : far);
               }

@@ -703,12 +703,11 @@ bool make_tmap_units(CUtensorMap* map, const void* base, const RDims& D, const S
   return sm100::make_tmap_bf16_strided(map, base, 5, n, st, box);
 }
 
-// The polynomials' coefficients with the factors of score and result folded in.  Where the score's would leave fp32's range (caps of some
+// The polynomial's coefficients with the factors of score and result folded in.  Where the score's would leave fp32's range (caps of some
 // hundred times what is usual, scales far from it) scores are multiplied by it first.  Scores of less than 10^-9 change no
 // weight: tanh is taken of scale s / cap whatever the cap, and multiplied by 10^-9 at least, so that c'^2 is a number of fp32's.
 Cap make_cap(const RDims& D) {
   static const double k[5] = {0.9999994349, -0.333282515, 0.1325898302, -0.05005629744, 0.01292962787};
-  static const double q[4] = {0.9999556007, -0.3322276355, 0.1257709159, -0.03377827421};
   Cap c = {};
   if (!(D.cap > 0.f)) return c;
   double a = std::min((double)D.scale / D.cap, 1e30);
@@ -719,10 +718,7 @@ Cap make_cap(const RDims& D) {
   c.twice_log2 = (float)(2.0 * a * 1.4426950408889634);
   c.most = (float)(0.75 / a);
   double f = top * a;
-  for (int i = 0; i < 5; ++i, f *= a * a) {
-    c.p[i] = (float)(k[i] * f);
-    if (i < 4) c.q[i] = (float)(q[i] * f);
-  }
+  for (int i = 0; i < 5; ++i, f *= a * a) c.p[i] = (float)(k[i] * f);
   return c;
 }
 
