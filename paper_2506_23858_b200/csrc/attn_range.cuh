@@ -63,6 +63,7 @@ struct Cap {
   float most;                    // |score| up to this: by the polynomial
   float p[5];                    // its coefficients of s, s^3, ...
 };
+constexpr float CAP_MOST = 96.0f;    // c' up to this: weights need no maximum
 Cap make_cap(const RDims& D);      // attn_range_fwd.cu
 
 // ---- tensor-core kernels (attn_range_fwd.cu, attn_range_bwd.cu)

@@ -77,6 +77,7 @@ struct Params {
   const float *lse, *Dv;
   float scale, scale_log2;     // scale_log2: scores -> exp2 domain, not capped
   Cap cap;
+  float cap_apart;             // |score| up to this: by the polynomial, whatever the others of the warp are; 0: as the warp's vote says
   float cap_inv2;              // -1 / c'^2
   float cap_masked;            // stands for a capped score outside its query's range: a weight of 0 and a finite slope
   __nv_bfloat16 *dk, *dv;
@@ -605,7 +606,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
                 pv[rh][i] = __float_as_uint(x0);
                 pv[rh][i + 1] = __float_as_uint(x1);
               }
-          } else if (p.cap.pre != 1.0f) {            // (the vote above never finds for the polynomial then: score by score)
+          } else if (p.cap_apart > 0.0f) {           // (larger caps: score by score, as in the forward)
 #pragma unroll
             for (int rh = 0; rh < 2; ++rh)
 #pragma unroll
@@ -613,7 +614,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
                 const float x = __uint_as_float(pv[rh][i]) * p.cap.pre, z = x * x;
                 const float near = x * fmaf(fmaf(fmaf(fmaf(p.cap.p[4], z, p.cap.p[3]), z, p.cap.p[2]), z, p.cap.p[1]), z, p.cap.p[0]);
                 const float far = fmaf(rcp(1.0f + ex2(x * p.cap.twice_log2)), -2.0f * p.cap.c, p.cap.c);
-                pv[rh][i] = __float_as_uint(fabsf(x) <= 0.75f ? near : far);
+                pv[rh][i] = __float_as_uint(fabsf(x) <= p.cap_apart ? near : far);
               }
           } else {
 #pragma unroll
@@ -798,7 +799,8 @@ int tc_range_bwd(const RDims& D, const Plan& plan, const BwdArgs& a, void* dq, c
   p.scale = D.scale;
   p.scale_log2 = D.scale * LOG2E;
   p.cap = make_cap(D);
-  if (p.cap.pre != 1.0f) p.cap.most = -1.0f;
+  p.cap_apart = p.cap.pre != 1.0f || p.cap.c > CAP_MOST ? p.cap.most : 0.f;
+  if (p.cap.pre != 1.0f) p.cap.most = -1.0f;      // (the vote never finds for the polynomial: its scores have not been multiplied)
   // lse2 is -c' at least, so that -2 c' - 256 is a weight of 0, and its slope 1 - (2 + 256 / c')^2.  Beyond caps of 10^18, where squares leave fp32's
   // range, slopes are 1, which they are to 2^-24 where scores stay below 10^14.
   p.cap_inv2 = D.cap > 0.f && p.cap.c <= 1e18f ? -1.0f / (p.cap.c * p.cap.c) : 0.f;

@@ -195,6 +195,9 @@ __device__ __forceinline__ bool polynomial_does(const uint32_t* sv, const Cap& c
   }
   return __all_sync(0xffffffffu, fmaxf(m0, m1) <= cap.most);
 }
+// APART: caps that may be large.  1 - 2 / (1 + exp(2 x)) is off by 1.6e-7 of the cap, and the scores of a warp's other rows need not be of its size:
+// those that the polynomial does keep it.
+template <bool APART>
 __device__ __forceinline__ void cap32(uint32_t* sv, const Cap& cap) {
   if (polynomial_does<32>(sv, cap)) {
 #pragma unroll
@@ -206,8 +209,18 @@ __device__ __forceinline__ void cap32(uint32_t* sv, const Cap& cap) {
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      sv[i] = __float_as_uint(fmaf(-2.0f * cap.c, rcp(1.0f + ex2(__uint_as_float(sv[i]) * cap.twice_log2)), cap.c));
+    for (int i = 0; i < 32; ++i) {
+      const float x = __uint_as_float(sv[i]), far = fmaf(-2.0f * cap.c, rcp(1.0f + ex2(x * cap.twice_log2)), cap.c);
+      if (APART && fabsf(x) <= cap.most) {
+        const float z = x * x;
+        float r = cap.p[4];
+#pragma unroll
+        for (int k = 3; k >= 0; --k) r = fmaf(r, z, cap.p[k]);
+        sv[i] = __float_as_uint(r * x);
+      } else {
+        sv[i] = __float_as_uint(far);
+      }
+    }
   }
 }
 // 32 scores from key i0 on of a row that sees n keys from key a on: those outside get a value.
@@ -265,7 +278,6 @@ __device__ __forceinline__ void store8_resid(__nv_bfloat16* dst, __nv_bfloat16* 
 
 // What a kernel does with the scores: nothing, caps them and goes by the cap's bound, caps them and looks for the maximum as without.
 enum Mode { kPlain, kCapped, kCappedWide };
-constexpr float CAP_MOST = 96.0f;            // c log2 e
 
 template <Mode MODE>
 __global__ void __launch_bounds__(THREADS, 1)
@@ -578,7 +590,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
             for (int c = 0; c < 4; ++c) {
               if (c > 0 && 32 * c >= valid) continue;        // (uniform; P V takes the keys up to `valid` only)
               if (masked) mask32(sv + 32 * c, 32 * c, r.x, r.y, 0u);      // (what nobody sees has no say in how the others are capped)
-              cap32(sv + 32 * c, p.cap);
+              cap32<false>(sv + 32 * c, p.cap);
               if (masked) mask32(sv + 32 * c, 32 * c, r.x, r.y, MINUS_INF);
               uint32_t pk[16];
               exp_capped32<false>(sv + 32 * c, p.cap, pk, s0, s1, r0, r1);
@@ -600,7 +612,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
 #pragma unroll
             for (int i = 32 * c; i < 32 * c + 32; ++i) sv[i] = __float_as_uint(__uint_as_float(sv[i]) * p.cap.pre);
             if (masked) mask32(sv + 32 * c, 32 * c, r.x, r.y, 0u);
-            cap32(sv + 32 * c, p.cap);
+            cap32<true>(sv + 32 * c, p.cap);
           }
         }
         if (__builtin_expect(t < all_lo || t >= all_hi, 0)) {      // keys outside the row's range get score -inf

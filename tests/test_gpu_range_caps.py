@@ -44,3 +44,37 @@ def test_scores_of_hundreds_under_larger_caps(cap, kind):
     assert 280 < ref["top"] < 340
     o, grads = run(op, dev, lambda x: x.cuda(), host)
     check_all(ref, dtype, d, min(cap, ref["top"]), o, op.lse, grads)
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=lambda k: f"{k[0]}_{k[1]}")
+@pytest.mark.parametrize("cap,scale", [(1e6, 0.0), (1e5, 100.0), (2e3, 1.0)])
+def test_rows_that_reach_a_large_cap_leave_the_others_exact(cap, scale, kind):
+    """One query in twenty has scores of the size of the cap; those of the others are of the size of one, and so is what may be wrong with them.
+    (The large ones get no gradient, so that dk and dv are sums over the others.)"""
+    dtype, d = kind
+    S = 260
+    s = scale or d ** -0.5
+    g = torch.Generator().manual_seed(17)
+    mk = lambda n: torch.randn((1, S, n, d), generator=g)
+    q, k, v, do = mk(2) / (s * math.sqrt(d)) / 64, mk(1) * 64, mk(1), mk(2)
+    large = torch.arange(S) % 20 == 3
+    big = q.clone()
+    big[:, large] *= cap
+    q[:, large] = 0
+    do[:, large] = 0
+    q, big, k, v, do = (x.to(DT[dtype]) for x in (q, big, k, v, do))
+    ranges = key_ranges([S], n_tokens=S, device="cpu")
+    ref = P.range_attention(q, k, v, ranges, cap, scale=scale or None, do=do)
+    far = P.range_attention(big, k, v, ranges, cap, scale=scale or None)
+    assert ref["top"] < 40 and float(far["lse"][..., large].max()) > 0.8 * cap
+    op = RangeAttention(vb.make_range_shape(1, 2, 1, d, S, S, dtype, softmax_scale=scale, softcap=cap), ranges.cuda(), with_backward=True)
+    dev = [x.cuda() for x in (big, k, v, do)]
+    o, grads = run(op, dev, lambda x: x.cuda(), (big, k, v, do))
+    lse = op.lse.cpu()
+    assert bool(((lse - far["lse"])[..., large].abs() <= 1e-5 * cap).all())
+    # the rows of the large ones as the statement without them has them: what is compared is the others
+    o, dq, lse = o.cpu(), grads[0].cpu(), lse
+    o[:, large] = ref["o"][:, large].to(o.dtype)
+    dq[:, large] = ref["dq"][:, large].to(o.dtype)
+    lse[..., large] = ref["lse"][..., large].float()
+    check_all(ref, dtype, d, ref["top"], o, lse, [dq, grads[1], grads[2]])
