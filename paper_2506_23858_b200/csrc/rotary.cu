@@ -784,13 +784,14 @@ rotary_bwd_kernel(const __grid_constant__ Params p) {
   }
 }
 
-// Longer rows: a CTA each, read twice where the norm is theirs.
-template <typename T, Layout L>
+// Longer rows: a CTA each, read twice where the norm is theirs.  STAGED: the sums of dw (norm per row) lie in shared memory; else they grow where they
+// end up, in the workspace (a channel's sum is one thread's).
+template <typename T, Layout L, bool STAGED>
 __global__ void __launch_bounds__(32 * kMaxWarps)
 rotary_bwd_long_kernel(const __grid_constant__ Params p) {
   if (!grid_begin()) return;
   constexpr int E = Vec<T>::E;
-  extern __shared__ __align__(16) float sums[];                      // [heads * d] (norm per row)
+  extern __shared__ __align__(16) float staged[];                    // [heads * d] (norm per row)
   __shared__ Frequencies freq;
   __shared__ Angles ang[2];
   __shared__ float2 slot[2][kMaxWarps];
@@ -803,6 +804,8 @@ rotary_bwd_long_kernel(const __grid_constant__ Params p) {
   const int row_ch = p.heads * p.d;
   const float inv_n = 1.0f / (float)(by_row ? row_ch : p.d);
   const Gradients rows(p, t, at);
+  float* out = normed ? p.part + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * (by_row ? row_ch : p.d) : nullptr;
+  float* sums = STAGED ? staged : out;
   float acc[E];                              // (norm per head)
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
@@ -876,10 +879,10 @@ rotary_bwd_long_kernel(const __grid_constant__ Params p) {
     });
   }
   if (!normed) return;
-  float* out = p.part + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * (by_row ? row_ch : p.d);
   __syncthreads();
   if (by_row) {
-    for (int i = l; i < row_ch; i += tpr) out[i] = sums[i];
+    if (STAGED)
+      for (int i = l; i < row_ch; i += tpr) out[i] = sums[i];
     return;
   }
 #pragma unroll
@@ -1013,10 +1016,13 @@ static int go_bwd(const Dims& D, const Params& p, const WeightOut& w, cudaStream
   const int n_w = p.norm == VMOBA_ROTARY_NORM_ROW ? D.heads * D.d : D.d;
   const size_t sums = p.norm == VMOBA_ROTARY_NORM_ROW ? (size_t)p.groups * n_w * sizeof(float) : 0;
   if constexpr (NV == 0) {
-    auto kernel = rotary_bwd_long_kernel<T, L>;
-    if (sums > (size_t)kLongSmemMost) return VMOBA_ERR_NOT_IMPLEMENTED;
-    VMOBA_CUDA_OK(allow_smem(kernel, kLongSmemMost));
-    launch_kernel(early_rows(D), kernel, dim3(ctas, p.n), threads, sums, st, p);
+    if (sums <= (size_t)kLongSmemMost) {
+      auto kernel = rotary_bwd_long_kernel<T, L, true>;
+      VMOBA_CUDA_OK(allow_smem(kernel, kLongSmemMost));
+      launch_kernel(early_rows(D), kernel, dim3(ctas, p.n), threads, sums, st, p);
+    } else {
+      launch_kernel(early_rows(D), rotary_bwd_long_kernel<T, L, false>, dim3(ctas, p.n), threads, 0, st, p);
+    }
   } else {
     auto kernel = rotary_bwd_kernel<T, L, NV>;
     VMOBA_CUDA_OK(allow_smem(kernel, kSmemMost));
