@@ -332,6 +332,7 @@ int vmoba_full_attn(const vmoba_shape* shape, const void* q, const void* k, cons
  *        VMOBA_ROTARY_HALF: channels i and i + pairs; VMOBA_ROTARY_INTERLEAVED: channels 2 i and 2 i + 1.
  *        Channels from 2 * pairs on are y.
  * Angles are formed and reduced in 64 bits (positions are any int32), everything else is fp32, rounded once.
+ * A row (heads * head_dim elements) has less than 2^31 bytes.
  */
 typedef enum { VMOBA_ROTARY_HALF = 0, VMOBA_ROTARY_INTERLEAVED = 1 } vmoba_rotary_layout;
 typedef enum { VMOBA_ROTARY_NORM_NONE = 0, VMOBA_ROTARY_NORM_HEAD = 1, VMOBA_ROTARY_NORM_ROW = 2 } vmoba_rotary_norm;

@@ -951,6 +951,7 @@ static int bwd_ctas(const Dims& D, const Params& p) {
 static int check(const vmoba_shape* shape, const vmoba_rotary_spec* spec, Dims* D) {
   if (!spec) return VMOBA_ERR_ARG;
   if (int rc = make_dims(shape, D)) return rc;
+  if ((long long)D->heads * D->d * D->es > INT32_MAX) return VMOBA_ERR_SHAPE;      // (a row's vectors are counted in 32 bits)
   if (spec->pairs < 0 || spec->pairs > D->d / 2) return VMOBA_ERR_SHAPE;
   if (spec->axes < 1 || spec->axes > 4) return VMOBA_ERR_SHAPE;
   if (spec->pos_batch != 1 && spec->pos_batch != D->B) return VMOBA_ERR_SHAPE;
