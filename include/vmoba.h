@@ -391,7 +391,7 @@ typedef struct {
   int32_t B, heads, kv_heads, head_dim; /* head_dim: 64 or 128                                              */
   int32_t Sq, Sk;                       /* query and key tokens per sample                                  */
   int32_t dtype;                        /* vmoba_dtype                                                      */
-  int32_t mask_batch;                   /* 1: all samples share the key ranges, B: each has its own         */
+  int32_t mask_batch;                   /* 1: all samples share the key ranges, B (up to 2^20): each has its own */
   float softmax_scale;                  /* 0 => head_dim^-1/2                                               */
   float softcap;                        /* 0: scores are not capped                                         */
 } vmoba_range_shape;

@@ -772,7 +772,7 @@ static int make_rdims(const vmoba_range_shape* s, RDims* o) {
   if (s->B <= 0 || s->heads <= 0 || s->kv_heads <= 0 || s->Sq <= 0 || s->Sk <= 0) return VMOBA_ERR_SHAPE;
   if (s->head_dim != 64 && s->head_dim != 128) return VMOBA_ERR_SHAPE;
   if (s->heads % s->kv_heads || s->heads / s->kv_heads > 64) return VMOBA_ERR_SHAPE;
-  if (s->mask_batch != 1 && s->mask_batch != s->B) return VMOBA_ERR_SHAPE;
+  if ((s->mask_batch != 1 && s->mask_batch != s->B) || s->mask_batch > 1 << 20) return VMOBA_ERR_SHAPE;      // (blocks of the plan)
   if (!(s->softmax_scale >= 0.f) || s->softmax_scale > 1e30f || !(s->softcap >= 0.f) || s->softcap > 1e30f) return VMOBA_ERR_ARG;
   if ((long long)s->B * s->heads > (1ll << 24) || (long long)s->B * s->heads * s->Sq > (1ll << 30) ||
       (long long)s->B * s->kv_heads * s->Sk > (1ll << 30))
@@ -958,7 +958,6 @@ extern "C" int vmoba_range_plan(const vmoba_range_shape* shape, const int32_t* k
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   launch_kernel(plan_units_kernel, grid_for(((long long)D.Bm * D.nU + 7) / 8, 8), 256, 0, st, reinterpret_cast<const int2*>(key_range), p, D);
   const long long tile_blocks = std::min<long long>(((long long)D.Bm * D.nK + 31) / 32, 2ll * sm_count());
-  if (D.Bm > (1 << 20)) return VMOBA_ERR_SHAPE;
   launch_kernel(plan_tiles_kernel, (unsigned)(D.Bm + 1 + tile_blocks), 1024, 0, st, p, D);
   VMOBA_LAUNCH_OK(2);
   return VMOBA_OK;
