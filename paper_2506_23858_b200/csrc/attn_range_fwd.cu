@@ -24,8 +24,9 @@
 // kernel is bound by that unit: a 33K clip by frames took 7.5 ms, 3.7 without the cap.  So tanh comes from the FMA pipe where a warp's
 // scores allow (|x| <= 3/4): an odd polynomial of five terms, fitted to tanh for the smallest largest relative error (by reweighted least
 // squares; 5.7e-7); larger scores take 1 - 2 / (1 + exp(2 x)).
-// And a cap bounds the weights: up to c log2 e = 96 (caps of 66) exp2 of a score, of no difference to a maximum, is a normal number, and so are
-// sums of 2^17 of them times values of up to 2^13.  So no maximum is looked for and nothing is rescaled.
+// And a cap bounds the weights: up to c' = c log2 e = 96 (caps of 66) exp2 of a score is a normal number, of no difference to the row's maximum but to one
+// number for all rows: 0, or c' - 80 where that is more.  Weights of up to 2^80 leave room for sums of 2^17 of them times values of up to 2^29; they are
+// 2^-112 at least.  So no maximum is looked for and nothing is rescaled.
 #include <algorithm>
 
 #include "attn_range.cuh"
@@ -177,13 +178,13 @@ __device__ __forceinline__ float rcp(float x) {
   return y;
 }
 
-// c' tanh(a s) of 32 of a row's scores, in place.  Called by whole warps (which way is taken is the warp's choice).
+// c' tanh(a s), less the shift, of 32 of a row's scores, in place.  Called by whole warps (which way is taken is the warp's choice).
 __device__ __forceinline__ void cap_pair(float& x0, float& x1, const Cap& cap) {
   float z0, z1, r0 = cap.p[4], r1 = cap.p[4];
   mul2(z0, z1, x0, x1, x0, x1);
 #pragma unroll
   for (int k = 3; k >= 0; --k) fma2(r0, r1, r0, r1, z0, z1, cap.p[k], cap.p[k]);
-  mul2(x0, x1, r0, r1, x0, x1);
+  fma2(x0, x1, r0, r1, x0, x1, -cap.shift, -cap.shift);
 }
 template <int N>
 __device__ __forceinline__ bool polynomial_does(const uint32_t* sv, const Cap& cap) {
@@ -210,13 +211,13 @@ __device__ __forceinline__ void cap32(uint32_t* sv, const Cap& cap) {
   } else {
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-      const float x = __uint_as_float(sv[i]), far = fmaf(-2.0f * cap.c, rcp(1.0f + ex2(x * cap.twice_log2)), cap.c);
+      const float x = __uint_as_float(sv[i]), far = fmaf(-2.0f * cap.c, rcp(1.0f + ex2(x * cap.twice_log2)), cap.c - cap.shift);
       if (APART && fabsf(x) <= cap.most) {
         const float z = x * x;
         float r = cap.p[4];
 #pragma unroll
         for (int k = 3; k >= 0; --k) r = fmaf(r, z, cap.p[k]);
-        sv[i] = __float_as_uint(r * x);
+        sv[i] = __float_as_uint(fmaf(r, x, -cap.shift));
       } else {
         sv[i] = __float_as_uint(far);
       }
@@ -550,7 +551,7 @@ attn_range_fwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         const int a = max(r.x - it.k_begin, 0) - t * BN;
         return make_int2(a, max(min(r.y - it.k_begin, it.keys) - t * BN - a, 0));
       };
-      float m_used = MODE == kCapped ? 0.f : -INFINITY, l = 0.f, l_r = 0.f;   // l: exact sum (for LSE); l_r: sum of the bf16-rounded weights
+      float m_used = MODE == kCapped ? p.cap.shift : -INFINITY, l = 0.f, l_r = 0.f;   // l: exact sum (for LSE); l_r: sum of the bf16-rounded weights
       for (int t = tb; t < te; ++t, ++tc) {
         mbar_wait(&sm->s_full[x], tc & 1, abort_flag, p.status);
         tc_fence_after();
@@ -729,6 +730,7 @@ Cap make_cap(const RDims& D) {
   if (!(a >= 2e-4 && a <= 1e3 && top <= 1e6)) { c.pre = (float)a; a = 1.0; }
   c.twice_log2 = (float)(2.0 * a * 1.4426950408889634);
   c.most = (float)(0.75 / a);
+  c.shift = c.pre == 1.f && c.c <= CAP_MOST ? std::max(c.c - 80.0f, 0.0f) : 0.f;
   double f = top * a;
   for (int i = 0; i < 5; ++i, f *= a * a) c.p[i] = (float)(k[i] * f);
   return c;

@@ -8,7 +8,7 @@ import torch
 from paper_2506_23858_b200 import binding as vb
 from paper_2506_23858_b200.layer import RangeAttention, key_ranges
 from tests import _plain64 as P
-from tests.test_gpu_range_attn import DT, KINDS, check_all, make, run
+from tests.test_gpu_range_attn import DT, KINDS, check, check_all, make, run
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +78,27 @@ def test_rows_that_reach_a_large_cap_leave_the_others_exact(cap, scale, kind):
     dq[:, large] = ref["dq"][:, large].to(o.dtype)
     lse[..., large] = ref["lse"][..., large].float()
     check_all(ref, dtype, d, ref["top"], o, lse, [dq, grads[1], grads[2]])
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=lambda k: f"{k[0]}_{k[1]}")
+@pytest.mark.parametrize("cap", [44.0, 50.0, 55.0, 58.0, 66.0])
+@pytest.mark.parametrize("sign,size", [(1, 1e8), (-1, 1e-6)])
+def test_all_scores_at_the_cap_and_large_or_small_values(sign, size, cap, kind):
+    """Every score of a row at the cap's one end, so that no weight is small against the others: sums of thousands of them times values of
+    10^8 are in fp32's range whatever stands for the row's maximum."""
+    dtype, d = kind
+    Sq, Sk = 70, 4100
+    ranges = key_ranges([Sk], n_queries=Sq, device="cpu")
+    g = torch.Generator().manual_seed(23)
+    mk = lambda S, n: torch.randn((1, S, n, d), generator=g)
+    u = torch.randn(d, generator=g)
+    u *= math.sqrt(8.0 * cap * math.sqrt(d)) / u.norm()
+    host = [(sign * u + 0.05 * mk(Sq, 2)).to(DT[dtype]), (u + 0.05 * mk(Sk, 1)).to(DT[dtype]),
+            (size * (1 + 0.1 * mk(Sk, 1))).to(DT[dtype]), (mk(Sq, 2) / size).to(DT[dtype])]
+    ref = P.range_attention(*host[:3], ranges, cap, do=host[3])
+    op = RangeAttention(vb.make_range_shape(1, 2, 1, d, Sq, Sk, dtype, softcap=cap), ranges.cuda(), with_backward=True)
+    o, grads = run(op, [x.cuda() for x in host], lambda x: x.cuda(), host)
+    assert all(bool(torch.isfinite(x).all()) for x in [o, op.lse] + grads)
+    check_all(ref, dtype, d, cap, o, op.lse)
+    # (slopes are 0 to 2^-21 here, and so is what dq and dk are relative to dv's magnitudes: what they are is the slopes' rounding)
+    check(grads[2], ref["dv"], ref["dv_mag"], 4 * (4 * math.sqrt(d) * 2.0 ** -24 * ref["top"] + 3e-7 * cap + 2e-5) + (2.0 ** -8 if dtype == "bf16" else 0), "dv")
