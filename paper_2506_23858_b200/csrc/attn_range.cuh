@@ -61,7 +61,7 @@ struct Cap {
   float c, twice_log2;           // c'; 2 log2 e times the factor that pre does not take
   float pre;                     // scores are multiplied by this first: 1 with a folded into all that follows, or a
   float most;                    // |score| up to this: by the polynomial
-  float p[5];                    // its coefficients of s, s^3, ...
+  float p[5], u[5];              // its coefficients of s, s^3, ...; of tanh alone
   float shift;                   // what stands for the rows' maximum where none is looked for (forward); else 0
 };
 constexpr float CAP_MOST = 96.0f;    // c' up to this: weights need no maximum

@@ -3,11 +3,11 @@
 //
 // A CTA takes one tile of 128 keys of a key head (by ticket) and streams the units of packed query rows that reach into it, all heads of the
 // group among them, so that dK and dV of shared heads are sums inside the CTA and are written once.  Per unit, keys on the TMEM lanes:
-//     S^T = K Q^T;  P^T = exp2(c S^T - lse), capped exp2(c' tanh - lse), 0 outside the range;  dV += P^T dO
-//     dP^T = V dO^T;  dS^T = P^T (dP^T - D) (1 - tanh^2);  dK += dS^T Q;  dQ^T = K^T dS^T, added into an fp32 accumulator
+//     S^T = K Q^T;  P^T = exp2(c S^T - lse), capped exp2(c' u - lse), u = tanh, 0 outside the range;  dV += P^T dO
+//     dP^T = V dO^T;  dS^T = P^T (dP^T - D) (1 - u^2);  dK += dS^T Q;  dQ^T = K^T dS^T, added into an fp32 accumulator
 // P and dS are rounded to bf16 (2^-8 each, once) for the products that the tensor cores do with them; in fp32 halves they would be twice
 // the products, and dQ, dK and dV are rounded to the same type after that.  All sums, D and the weights under dS are fp32.
-// The slope 1 - tanh^2 is taken into the fp32 weights that the second step keeps, at no register.  tanh comes from the forward's polynomial
+// The slope 1 - u^2 is taken into the fp32 weights that the second step keeps, at no register.  tanh comes from the forward's polynomial
 // where a warp's scores allow, else from 1 - 2 / (1 + exp(2 x)): the same error in the weights and in the lse that they are divided by, so that
 // it leaves their sum at one.  (With a term less, off by 4.4e-5 of a score, weights of scores of 300 were 1.3 % off, all to the same side.)
 //
@@ -75,11 +75,11 @@ struct Params {
   const __nv_bfloat16 *q, *d_o;
   Strides qs, dos;
   const float *lse, *Dv;
-  float scale, scale_log2;     // scale_log2: scores -> exp2 domain, not capped
+  float scale;
+  float to_exp2;               // scores, or tanh of capped ones, -> exp2 domain: scale * log2 e, or c'
   Cap cap;
   float cap_apart;             // |score| up to this: by the polynomial, whatever the others of the warp are; 0: as the warp's vote says
-  float cap_inv2;              // -1 / c'^2
-  float cap_masked;            // stands for a capped score outside its query's range: a weight of 0 and a finite slope
+  float cap_masked;            // stands for tanh of a score outside its query's range: a weight of 0 and a finite slope
   __nv_bfloat16 *dk, *dv;
   Strides dks, dvs;
   int dkv_32;                  // rows of dk and dv are 32-byte aligned: they go out with 32-byte stores
@@ -585,7 +585,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         };
         // (the rare cases' code is out of the way and short: beside the other roles' it does not fit the instruction cache)
         if constexpr (CAP) {
-          // scores -> c' tanh.  What no product has written (queries beyond the unit's) has no say in how the others are capped
+          // scores -> tanh (1 exactly where it is 1 to fp32, so that the slope is 0).  What no product has written (queries beyond the unit's) has no say in how the others are capped
           if (__builtin_expect(stale, 0)) mask(0u);
           float m0 = 0.f, m1 = 0.f;
 #pragma unroll
@@ -598,10 +598,10 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
             for (int rh = 0; rh < 2; ++rh)
 #pragma unroll
               for (int i = 0; i < 32; i += 2) {
-                float x0 = __uint_as_float(pv[rh][i]), x1 = __uint_as_float(pv[rh][i + 1]), z0, z1, r0 = p.cap.p[4], r1 = p.cap.p[4];
+                float x0 = __uint_as_float(pv[rh][i]), x1 = __uint_as_float(pv[rh][i + 1]), z0, z1, r0 = p.cap.u[4], r1 = p.cap.u[4];
                 mul2(z0, z1, x0, x1, x0, x1);
 #pragma unroll
-                for (int k = 3; k >= 0; --k) fma2(r0, r1, r0, r1, z0, z1, p.cap.p[k], p.cap.p[k]);
+                for (int k = 3; k >= 0; --k) fma2(r0, r1, r0, r1, z0, z1, p.cap.u[k], p.cap.u[k]);
                 mul2(x0, x1, r0, r1, x0, x1);
                 pv[rh][i] = __float_as_uint(x0);
                 pv[rh][i + 1] = __float_as_uint(x1);
@@ -612,8 +612,8 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
 #pragma unroll
               for (int i = 0; i < 32; ++i) {
                 const float x = __uint_as_float(pv[rh][i]) * p.cap.pre, z = x * x;
-                const float near = x * fmaf(fmaf(fmaf(fmaf(p.cap.p[4], z, p.cap.p[3]), z, p.cap.p[2]), z, p.cap.p[1]), z, p.cap.p[0]);
-                const float far = fmaf(rcp(1.0f + ex2(x * p.cap.twice_log2)), -2.0f * p.cap.c, p.cap.c);
+                const float near = x * fmaf(fmaf(fmaf(fmaf(p.cap.u[4], z, p.cap.u[3]), z, p.cap.u[2]), z, p.cap.u[1]), z, p.cap.u[0]);
+                const float far = fmaf(rcp(1.0f + ex2(x * p.cap.twice_log2)), -2.0f, 1.0f);
                 pv[rh][i] = __float_as_uint(fabsf(x) <= p.cap_apart ? near : far);
               }
           } else {
@@ -621,7 +621,7 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
             for (int rh = 0; rh < 2; ++rh)
 #pragma unroll
               for (int i = 0; i < 32; ++i)
-                pv[rh][i] = __float_as_uint(fmaf(rcp(1.0f + ex2(__uint_as_float(pv[rh][i]) * p.cap.twice_log2)), -2.0f * p.cap.c, p.cap.c));
+                pv[rh][i] = __float_as_uint(fmaf(rcp(1.0f + ex2(__uint_as_float(pv[rh][i]) * p.cap.twice_log2)), -2.0f, 1.0f));
           }
           if (__builtin_expect(masked || stale, 0)) mask(__float_as_uint(p.cap_masked));
         } else {
@@ -638,13 +638,11 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
                 float x0 = __uint_as_float(pv[rh][4 * j + 2 * e]), x1 = __uint_as_float(pv[rh][4 * j + 2 * e + 1]), s0, s1;
-                if constexpr (CAP) {                 // the slope 1 - (t / c')^2
+                if constexpr (CAP) {                 // the slope
                   mul2(s0, s1, x0, x1, x0, x1);
-                  fma2(s0, s1, s0, s1, p.cap_inv2, p.cap_inv2, 1.0f, 1.0f);
-                  add2(x0, x1, x0, x1, -l[j].x, -l[j].y);
-                } else {
-                  fma2(x0, x1, x0, x1, p.scale_log2, p.scale_log2, -l[j].x, -l[j].y);
+                  fma2(s0, s1, s0, s1, -1.0f, -1.0f, 1.0f, 1.0f);
                 }
+                fma2(x0, x1, x0, x1, p.to_exp2, p.to_exp2, -l[j].x, -l[j].y);
                 x0 = ex2(x0);
                 x1 = ex2(x1);
                 pk[rh][2 * jj + e] = pack_bf16(x0, x1);
@@ -797,14 +795,12 @@ int tc_range_bwd(const RDims& D, const Plan& plan, const BwdArgs& a, void* dq, c
   p.q = (const __nv_bfloat16*)a.q; p.d_o = (const __nv_bfloat16*)a.d_o; p.qs = a.qs; p.dos = a.dos;
   p.lse = a.lse; p.Dv = a.Dv;
   p.scale = D.scale;
-  p.scale_log2 = D.scale * LOG2E;
   p.cap = make_cap(D);
+  p.to_exp2 = D.cap > 0.f ? p.cap.c : D.scale * LOG2E;
   p.cap_apart = p.cap.pre != 1.0f || p.cap.c > CAP_MOST ? p.cap.most : 0.f;
   if (p.cap.pre != 1.0f) p.cap.most = -1.0f;      // (the vote never finds for the polynomial: its scores have not been multiplied)
-  // lse2 is -c' at least, so that -2 c' - 256 is a weight of 0, and its slope 1 - (2 + 256 / c')^2.  Beyond caps of 10^18, where squares leave fp32's
-  // range, slopes are 1, which they are to 2^-24 where scores stay below 10^14.
-  p.cap_inv2 = D.cap > 0.f && p.cap.c <= 1e18f ? -1.0f / (p.cap.c * p.cap.c) : 0.f;
-  p.cap_masked = -fminf(2.0f * p.cap.c + 256.0f, 4e18f);
+  // lse2 is -c' at least, so that -2 c' - 256 is a weight of 0, and its slope 1 - (2 + 256 / c')^2, of c' = 10^-9 at least
+  p.cap_masked = D.cap > 0.f ? -2.0f - 256.0f / p.cap.c : 0.f;
   p.dk = (__nv_bfloat16*)a.dk; p.dv = (__nv_bfloat16*)a.dv; p.dks = a.dks; p.dvs = a.dvs;
   auto whole = [](const void* x, const Strides& s) {
     return reinterpret_cast<uintptr_t>(x) % 32 == 0 && s.b % 16 == 0 && s.t % 16 == 0 && s.h % 16 == 0;

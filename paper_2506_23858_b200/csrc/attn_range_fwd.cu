@@ -718,7 +718,7 @@ bool make_tmap_units(CUtensorMap* map, const void* base, const RDims& D, const S
 
 // The polynomial's coefficients with the factors of score and result folded in.  Where the score's would leave fp32's range (caps of some
 // hundred times what is usual, scales far from it) scores are multiplied by it first.  Scores of less than 10^-9 change no
-// weight: tanh is taken of scale s / cap whatever the cap, and multiplied by 10^-9 at least, so that c'^2 is a number of fp32's.
+// weight: tanh is taken of scale s / cap whatever the cap, and multiplied by 10^-9 at least, so that 1 / c' is a number of fp32's.
 Cap make_cap(const RDims& D) {
   static const double k[5] = {0.9999994349, -0.333282515, 0.1325898302, -0.05005629744, 0.01292962787};
   Cap c = {};
@@ -731,8 +731,11 @@ Cap make_cap(const RDims& D) {
   c.twice_log2 = (float)(2.0 * a * 1.4426950408889634);
   c.most = (float)(0.75 / a);
   c.shift = c.pre == 1.f && c.c <= CAP_MOST ? std::max(c.c - 80.0f, 0.0f) : 0.f;
-  double f = top * a;
-  for (int i = 0; i < 5; ++i, f *= a * a) c.p[i] = (float)(k[i] * f);
+  double f = a;
+  for (int i = 0; i < 5; ++i, f *= a * a) {
+    c.p[i] = (float)(k[i] * top * f);
+    c.u[i] = (float)(k[i] * f);
+  }
   return c;
 }
 

@@ -102,3 +102,25 @@ def test_all_scores_at_the_cap_and_large_or_small_values(sign, size, cap, kind):
     check_all(ref, dtype, d, cap, o, op.lse)
     # (slopes are 0 to 2^-21 here, and so is what dq and dk are relative to dv's magnitudes: what they are is the slopes' rounding)
     check(grads[2], ref["dv"], ref["dv_mag"], 4 * (4 * math.sqrt(d) * 2.0 ** -24 * ref["top"] + 3e-7 * cap + 2e-5) + (2.0 ** -8 if dtype == "bf16" else 0), "dv")
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=lambda k: f"{k[0]}_{k[1]}")
+@pytest.mark.parametrize("cap", [0.3, 5.0, 27.0, 300.0])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_far_beyond_the_cap_have_no_gradient(sign, cap, kind):
+    """From 9 caps on tanh is 1 to half a step of fp32 (2 exp(-18) < 2^-25) and its slope 0; dq and dk are sums of what it multiplies."""
+    dtype, d = kind
+    ranges = key_ranges([130, 90], n_tokens=230, frame=1, device="cpu")
+    g = torch.Generator().manual_seed(24)
+    mk = lambda n: torch.randn((1, 230, n, d), generator=g)
+    u = torch.randn(d, generator=g)
+    u *= math.sqrt(20.0 * cap * math.sqrt(d)) / u.norm()
+    s = 0.05 * u.norm() / math.sqrt(d)
+    host = [(sign * u + s * mk(2)).to(DT[dtype]), (u + s * mk(1)).to(DT[dtype]), mk(1).to(DT[dtype]), mk(2).to(DT[dtype])]
+    ref = P.range_attention(*host[:3], ranges, cap, do=host[3])
+    op = RangeAttention(vb.make_range_shape(1, 2, 1, d, 230, 230, dtype, softcap=cap), ranges.cuda(), with_backward=True)
+    o, grads = run(op, [x.cuda() for x in host], lambda x: x.cuda(), host)
+    assert float(ref["dq"].abs().max()) < 1e-9 and float(ref["dk"].abs().max()) < 1e-9
+    assert bool((grads[0] == 0).all()) and bool((grads[1] == 0).all())
+    check_all(ref, dtype, d, cap, o, op.lse)
+    check(grads[2], ref["dv"], ref["dv_mag"], 4 * (4 * math.sqrt(d) * 2.0 ** -24 * ref["top"] + 3e-7 * cap + 2e-5) + (2.0 ** -8 if dtype == "bf16" else 0), "dv")
