@@ -475,9 +475,12 @@ class RangeAttention:
         s = self.shape
         if tuple(key_range.shape) != (s.mask_batch, s.Sq, 2) or key_range.dtype != torch.int32 or key_range.device != self.device:
             raise ValueError("RangeAttention: key ranges are int32 [mask_batch, Sq, 2] on the plan's device")
+        key_range = key_range.contiguous()
+        if key_range.data_ptr() % 8:
+            key_range = key_range.clone()                # (a pair is read as one word)
         self._kept = None          # (the last forward's lse and o belong to the ranges it ran under)
         with _on(self.device):
-            vb.vmoba_range_plan(s, key_range.contiguous(), self.plan)
+            vb.vmoba_range_plan(s, key_range, self.plan)
 
     def _tensor(self, x, S, heads, what, written=False):
         """x as the kernels can address it (an input that they cannot is copied) and its strides."""
