@@ -380,7 +380,7 @@ int vmoba_rotary_bwd(const vmoba_shape* shape, const vmoba_rotary_spec* spec, in
  *   o_i  = sum over j in [lo_i, hi_i) of exp(t_ij - lse_i) v_j,   lse_i = log of the sum of exp(t_ij)
  * A query whose range holds no key gets o = 0, lse = -inf and zero gradients; what its q and d_o rows hold does not matter.  Keys
  * and values behind the last key of all ranges are not used, whatever they hold; in between, a value that is not finite
- * reaches every row of a tile of 128 query rows that loads it.
+ * reaches every row of a tile of 128 query rows that loads it (and a key that is not finite the dq of those).
  * kv_heads divides heads: query head h reads key head h / (heads / kv_heads), of which up to 64 share one.
  * Tensors are addressed by element strides {batch, token, head}, head_dim contiguous, rows 16-byte aligned: q, o, d_o, dq
  * [B, Sq, heads, head_dim], k, v, dk, dv [B, Sk, kv_heads, head_dim] in whatever order; strides of dimensions larger than one
@@ -393,7 +393,7 @@ typedef struct {
   int32_t dtype;                        /* vmoba_dtype                                                      */
   int32_t mask_batch;                   /* 1: all samples share the key ranges, B (up to 2^20): each has its own */
   float softmax_scale;                  /* 0 => head_dim^-1/2                                               */
-  float softcap;                        /* 0: scores are not capped                                         */
+  float softcap;                        /* 0: scores are not capped; any cap up to 10^30, time goes by how near scores come to it */
 } vmoba_range_shape;
 
 /*

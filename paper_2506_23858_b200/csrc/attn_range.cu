@@ -100,7 +100,7 @@ __device__ __forceinline__ void plan_pieces(const Plan& plan, const RDims& D) {
   }
   __syncthreads();
   // The order: the first pieces of all items, the second ones, ...: what runs at the same time reads the same keys (a frame of 1,560 tokens
-  // against 31,200, 12 heads, a cache larger than the L2: 329 us item after item, so 309).
+  // against 31,200, 12 heads, a cache larger than the L2, the same call again and again: 329 us item after item, so 309).
   const int len = length;
   if (t < n) {
     tiles[t] = (mine + len - 1) / len;
@@ -912,7 +912,8 @@ static int backward(const RDims& D, const Plan& plan, const BwdArgs& a, const vo
     VMOBA_CUDA_OK(allow_smem(range_bwd_kernel<T, DH>, kRangeBwdSmem<DH>));
     const long long items = (long long)D.B * D.Hk * (D.nK + D.nU), room = (long long)kSms * (DH == 64 ? 2 : 1);
     // The items that stream the most decide; of the others, which are short then, more come one after another.  (Room for all items at once
-    // instead: 500 tokens x 2, eight heads of 64 on one key head, bf16, 469 us, so 158; 600 tokens, four of 128 on one, fp32, 363 and 124.)
+    // instead: 500 tokens x 2, eight heads of 64 on one key head, bf16, 469 us, so 158; 600 tokens, four of 128 on one, fp32, 363 and 124; but
+    // 100 queries x 2 heads of 64 against 1,500 keys, fp32, 81 and 91.)
     const long long longest = (long long)D.B * D.Hk * std::min(D.nK, D.nU);
     int C = 1;
     while (C < 8 && longest * C * 2 <= room && std::max(D.nU, D.nK) >= 2 * C) C *= 2;

@@ -12,7 +12,8 @@
 // it leaves their sum at one.  (With a term less, off by 4.4e-5 of a score, weights of scores of 300 were 1.3 % off, all to the same side.)
 //
 // Bound by the exponentials, the turns of dQ and the tensor cores' waits for both, as the dense backward is.  13,440 tokens x 12 heads: eight
-// clips packed, 633 GFLOP, 866 us (730 TFLOP/s); two clips by frames, key heads shared by three, 1.03 ms (735), capped 1.32 ms (575).
+// clips packed, 633 GFLOP, 866 us (730 TFLOP/s); two clips by frames, key heads shared by three, 1.04 ms (730), capped 1.26 ms (600), and 1.59 where
+// scores have the cap's size.
 //
 // dQ of a unit is added key tile after key tile, so that the backward repeats bit for bit: a counter per unit says how many of the
 // tiles of its hull (which are consecutive) have been added; the first one stores.  A tile waits for lower tickets only.  Units go

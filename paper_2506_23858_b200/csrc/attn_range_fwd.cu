@@ -7,9 +7,9 @@
 // bounds say that some row needs it.
 //
 // Bound by the exponentials of two tiles and the one score buffer, as the dense forward is; the weights are rounded to bf16 (2^-8) for P V, and o
-// is normalised by the sum of the rounded ones.  12 heads: 32,760 tokens by frames 3.1 ms (1110 TFLOP/s of the visible pairs), capped 3.5 to 3.8
-// (power-capped); 13,440 tokens, eight clips packed, 257 us (985); a frame of 1,560 tokens against 31,200 keys 309 us (970), its
-// pieces joined through memory; a token of each of four samples against 8K to 76K keys, four key heads, 362 MB, 74 us (4.9 TB/s).
+// is normalised by the sum of the rounded ones.  12 heads: 32,760 tokens by frames 2.85 ms (1210 TFLOP/s of the visible pairs), capped 3.5, and
+// 4.1 in call after call on other inputs (power-capped); 13,440 tokens, eight clips packed, 257 us (985); a frame of 1,560 tokens against 31,200
+// keys 315 us where the same call is repeated, 357 on other inputs each time, its pieces joined through memory; a token of each of four samples against 8K to 76K keys, four key heads, 362 MB, 74 us (4.9 TB/s).
 //
 // Every (item, unit) has at least one tile, masked as a whole if need be, and every tile at least one unit, so that no barrier skips a phase.
 //
@@ -23,7 +23,8 @@
 // Capped scores: c tanh(x), x = scale s / c.  By the exponential unit that is an exponential and a reciprocal more per score, and the
 // kernel is bound by that unit: a 33K clip by frames took 7.5 ms, 3.7 without the cap.  So tanh comes from the FMA pipe where a warp's
 // scores allow (|x| <= 3/4): an odd polynomial of five terms, fitted to tanh for the smallest largest relative error (by reweighted least
-// squares; 5.7e-7); larger scores take 1 - 2 / (1 + exp(2 x)).
+// squares; 5.7e-7); larger scores take 1 - 2 / (1 + exp(2 x)).  So the time goes by the scores: the 33K clip, scores of a standard deviation of a tenth of
+// the cap 3.5 ms, of half the cap and of the whole 6.8, where nearly every warp has one that is larger.
 // And a cap bounds the weights: up to c' = c log2 e = 96 (caps of 66) exp2 of a score is a normal number, of no difference to the row's maximum but to one
 // number for all rows: 0, or c' - 80 where that is more.  Weights of up to 2^80 leave room for sums of 2^17 of them times values of up to 2^29; they are
 // 2^-112 at least.  So no maximum is looked for and nothing is rescaled.
@@ -740,7 +741,8 @@ Cap make_cap(const RDims& D) {
 }
 
 // The more heads together, the evener the CTAs' shares; their keys and values have to stay in the L2 (126 MB).  33K clip by frames, capped: 4 of 12
-// heads (67 MB) 3.71 ms, 6 (101 MB) 3.52, all (201 MB) 3.59.
+// heads (67 MB) 3.71 ms, 6 (101 MB) 3.52, all (201 MB) 3.59.  Groups are equal ones: a prime number of heads that do not fit together goes head by
+// head (causal, 1,600 tokens: 131 heads 168 us, 132 heads, two groups, 143).
 static int group_of_heads(const RDims& D) {
   const long long all = (long long)D.B * D.Hk, one = (long long)D.Sk * D.d * 4;      // K and V of a head, bytes
   long long g = std::max<long long>(1, std::min<long long>(all, (101ll << 20) / one));

@@ -357,8 +357,8 @@ struct Place {
 };
 
 // Rows that a group's threads hold in NV vectors each: 128 registers for six of them and the next row's, 16 warps per SM.
-// q, k, v of 32,760 tokens x 12 heads of 128 into block order, 402 MB: 73 us (with a ring of asynchronous copies in shared memory, 883 instructions
-// per row instead of 411: 90); of 75,600 tokens x 40 heads, 3.1 GB: 549 us.
+// q, k of 32,760 tokens x 12 heads of 128 into block order, 402 MB: 73 us, 600 warp instructions per row in 54 % of the issue slots (with a ring of
+// asynchronous copies in shared memory, which every row is read from twice: 90); of 75,600 tokens x 40 heads, 3.1 GB: 556 us.
 template <typename T, Layout L, int NV>
 __global__ void __launch_bounds__(32 * kMaxWarps, 2)
 rotary_fwd_kernel(const __grid_constant__ Params p) {
