@@ -586,7 +586,8 @@ attn_range_bwd_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_cons
         };
         // (the rare cases' code is out of the way and short: beside the other roles' it does not fit the instruction cache)
         if constexpr (CAP) {
-          // scores -> tanh (1 exactly where it is 1 to fp32, so that the slope is 0).  What no product has written (queries beyond the unit's) has no say in how the others are capped
+          // scores -> tanh (1 exactly where it is 1 to fp32, so that the slope is 0).  What no product has written (queries beyond the unit's)
+          // has no say in how the others are capped
           if (__builtin_expect(stale, 0)) mask(0u);
           float m0 = 0.f, m1 = 0.f;
 #pragma unroll

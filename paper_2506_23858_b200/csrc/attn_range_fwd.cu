@@ -9,7 +9,8 @@
 // Bound by the exponentials of two tiles and the one score buffer, as the dense forward is; the weights are rounded to bf16 (2^-8) for P V, and o
 // is normalised by the sum of the rounded ones.  12 heads: 32,760 tokens by frames 2.85 ms (1210 TFLOP/s of the visible pairs), capped 3.5, and
 // 4.1 in call after call on other inputs (power-capped); 13,440 tokens, eight clips packed, 257 us (985); a frame of 1,560 tokens against 31,200
-// keys 315 us where the same call is repeated, 357 on other inputs each time, its pieces joined through memory; a token of each of four samples against 8K to 76K keys, four key heads, 362 MB, 74 us (4.9 TB/s).
+// keys 315 us where the same call is repeated, 357 on other inputs each time, its pieces joined through memory; a token of each of four
+// samples against 8K to 76K keys, four key heads, 362 MB, 76 us (4.8 TB/s).
 //
 // Every (item, unit) has at least one tile, masked as a whole if need be, and every tile at least one unit, so that no barrier skips a phase.
 //
