@@ -421,6 +421,117 @@ int vmoba_range_attn_bwd(const vmoba_range_shape* shape, const void* plan, const
                          void* dv, const int64_t dv_strides[3], int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * What stands around the attention layer in a transformer block, for training and for serving.
+ *
+ * Linear layers: out = residual + gate * act(x W^T + bias), every part but the product optional; gated: W has 2 * out rows, and
+ * act(x Wg^T + bias_g) * (x Wu^T + bias_u) takes the place of act(..), Wg the first half.  VMOBA_ACT_GELU is the tanh form,
+ * u (1 + tanh(sqrt(2 / pi) (u + 0.044715 u^3))) / 2; VMOBA_ACT_SILU u / (1 + exp(-u)).
+ *   x        raster order [B, S, in] through element strides {batch, token}, or (heads > 0) block-major [B, heads, S, in / heads],
+ *            contiguous: the o of an attention layer.  Token p of it is then token perm_or_null[p] (int32 [S], as vmoba_partition
+ *            leaves it; NULL: p) of every other tensor.  A place outside [0, S) leaves its row out.
+ *   weight   [out or 2 * out, in], contiguous; bias [out or 2 * out]; both of the layer's type
+ *   gate     fp32 [B, groups, out] through element strides {batch, group} (zero: shared), one row for gate_tokens consecutive tokens, the last
+ *            group as many as are left; gate_tokens 0: one row per sample
+ *   residual, out   [B, S, out] through element strides {batch, token}; out may be the residual, with the same strides
+ *   kept     contiguous [B, S, out or 2 * out] in the order of x, the layer's type: x W^T + bias, for the backward pass
+ * in and out are multiples of 8; rows lie on 16-byte boundaries; strides of dimensions larger than one are at least a row.
+ * bf16 runs on the tensor cores, fp32 on the CUDA cores; sums are fp32, rounded once per tensor written.
+ */
+typedef enum { VMOBA_ACT_NONE = 0, VMOBA_ACT_GELU = 1, VMOBA_ACT_SILU = 2 } vmoba_activation;
+typedef struct {
+  int32_t B, S;         /* samples, tokens per sample: B * S <= 2^30                                       */
+  int32_t in, out;      /* channels, up to 2^20                                                            */
+  int32_t dtype;        /* vmoba_dtype                                                                     */
+  int32_t activation;   /* vmoba_activation                                                                */
+  int32_t gated;        /* 1: the activation of one half of the product times the other                    */
+  int32_t heads;        /* 0: x in raster order; else block-major, with heads of 64 or 128 channels        */
+  int32_t gate_tokens;  /* tokens that share a row of the gate; 0: all of a sample                         */
+} vmoba_linear_shape;
+
+/* Scratch of a forward (backward = 0) or backward call, one buffer per call under way; 0 bytes: invalid shape. */
+size_t vmoba_linear_workspace_bytes(const vmoba_linear_shape* shape, int backward);
+int vmoba_linear(const vmoba_linear_shape* shape, const void* x, const int64_t x_strides[2], const void* weight, const void* bias_or_null,
+                 const float* gate_or_null, const int64_t gate_strides[2], const void* residual_or_null, const int64_t residual_strides[2],
+                 void* out, const int64_t out_strides[2], void* kept_or_null, const int32_t* perm_or_null, int32_t* dev_status, void* ws,
+                 size_t ws_bytes, void* stream);
+
+/*
+ * Its gradients (the residual's is d_out itself): dx in the order of x, dweight and dbias of the layer's type, dgate fp32
+ * [B, groups, out], contiguous; NULL where one is not wanted.  kept as the forward left it: needed with an activation, gated, and for dgate.
+ * du, the gradient of the product, is rounded to the layer's type ahead of dx and dweight; dbias and dgate are sums of unrounded
+ * values.  The results repeat bit for bit.
+ */
+int vmoba_linear_bwd(const vmoba_linear_shape* shape, const void* d_out, const int64_t d_out_strides[2], const void* x,
+                     const int64_t x_strides[2], const void* weight, const void* kept_or_null, const float* gate_or_null,
+                     const int64_t gate_strides[2], void* dx_or_null, const int64_t dx_strides[2], void* dweight_or_null,
+                     void* dbias_or_null, float* dgate_or_null, const int32_t* perm_or_null, int32_t* dev_status, void* ws,
+                     size_t ws_bytes, void* stream);
+
+/*
+ * A feed-forward block: out = residual + gate * (h W_down^T + b_down), h = act(x W_up^T + b_up), gated as above; tensors as for
+ * vmoba_linear, in raster order.  shape: in = channels, out = hidden channels (of h), heads 0.  h is rounded to the block's type.
+ * kept_up [B, S, hidden or 2 * hidden] and kept_down [B, S, channels], both or none: the products ahead of activation and gate.
+ */
+size_t vmoba_ffn_workspace_bytes(const vmoba_linear_shape* shape, int backward);
+int vmoba_ffn(const vmoba_linear_shape* shape, const void* x, const int64_t x_strides[2], const void* w_up, const void* b_up_or_null,
+              const void* w_down, const void* b_down_or_null, const float* gate_or_null, const int64_t gate_strides[2],
+              const void* residual_or_null, const int64_t residual_strides[2], void* out, const int64_t out_strides[2],
+              void* kept_up_or_null, void* kept_down_or_null, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
+
+/* Its gradients; what is not wanted may be NULL.  kept_down is read for dgate alone.  The gradient of h is rounded to the block's type
+ * once (between the two products it stands between), and db_up is the sum of what follows from it. */
+int vmoba_ffn_bwd(const vmoba_linear_shape* shape, const void* d_out, const int64_t d_out_strides[2], const void* x,
+                  const int64_t x_strides[2], const void* w_up, const void* w_down, const void* kept_up, const void* kept_down_or_null,
+                  const float* gate_or_null, const int64_t gate_strides[2], void* dx_or_null, const int64_t dx_strides[2],
+                  void* dw_up_or_null, void* db_up_or_null, void* dw_down_or_null, void* db_down_or_null, float* dgate_or_null,
+                  int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * What stands between two branches of a block: the gated residual of the one, the norm and modulation ahead of the next.
+ *   z   = y or its norm (post_norm), times post_weight          h   = x + gate * z     (no y: h = x)
+ *   out = (norm(h) * weight + bias) * (1 + scale) + shift
+ *   norm: VMOBA_NORM_RMS   v / sqrt(mean(v^2) + eps),  VMOBA_NORM_LAYER   (v - mean) / sqrt(var + eps), over the channels of a token
+ * x and h [B, S, C] of stream_dtype, y and out of dtype (fp32 of them next to a bf16 stream is VMOBA_ERR_NOT_IMPLEMENTED), through element strides {batch, token};
+ * h may be x, with the same strides.  gate, scale, shift fp32 [B, groups, C] through element strides {batch, group} (zero: shared), one row for
+ * mod_tokens consecutive tokens (0: one per sample); weight, bias, post_weight fp32 [C].  Everything but x is optional; one of h and
+ * out is there.  C is a multiple of 8, up to 8192.  Arithmetic is fp32; the norm is taken of h before it is rounded.
+ */
+typedef enum { VMOBA_NORM_NONE = 0, VMOBA_NORM_RMS = 1, VMOBA_NORM_LAYER = 2 } vmoba_norm;
+typedef struct {
+  int32_t B, S, C;       /* samples, tokens per sample (B * S <= 2^30), channels                            */
+  int32_t dtype, stream_dtype;
+  int32_t norm;          /* VMOBA_NORM_RMS or VMOBA_NORM_LAYER                                              */
+  int32_t post_norm;     /* of y, any of the three                                                          */
+  int32_t mod_tokens;    /* tokens that share a row of gate, scale and shift; 0: all of a sample            */
+  float eps;             /* of both norms                                                                   */
+} vmoba_norm_shape;
+/* The rows of gate, scale and shift: pointers (NULL: none) and their element strides {batch, group}. */
+typedef struct {
+  const float *gate, *scale, *shift;
+  int64_t gate_strides[2], scale_strides[2], shift_strides[2];
+  const float *weight, *bias, *post_weight;
+} vmoba_norm_params;
+
+int vmoba_block_norm(const vmoba_norm_shape* shape, const vmoba_norm_params* params, const void* x, const int64_t x_strides[2],
+                     const void* y_or_null, const int64_t y_strides[2], void* h_or_null, const int64_t h_strides[2], void* out_or_null,
+                     const int64_t out_strides[2], void* stream);
+
+/*
+ * Its gradients, from h as the forward left it (rounded; without y that is x), y, d_out and what else arrives at h (d_h, NULL: nothing):
+ * dx (that of x and of h, stream_dtype; may be d_h, with the same strides), dy (may be d_out), and in fp32, contiguous, those of the params that
+ * are there: dgate, dscale, dshift [B, groups, C], dweight, dbias, dpost_weight [C].  A gradient whose pointer is NULL is left out.
+ * The results repeat bit for bit.
+ */
+typedef struct {
+  float *gate, *scale, *shift, *weight, *bias, *post_weight;
+} vmoba_norm_grads;
+size_t vmoba_block_norm_workspace_bytes(const vmoba_norm_shape* shape);      /* of a backward call; 0: invalid shape */
+int vmoba_block_norm_bwd(const vmoba_norm_shape* shape, const vmoba_norm_params* params, const void* d_out, const int64_t d_out_strides[2],
+                         const void* h, const int64_t h_strides[2], const void* d_h_or_null, const int64_t d_h_strides[2],
+                         const void* y_or_null, const int64_t y_strides[2], void* dx, const int64_t dx_strides[2], void* dy_or_null,
+                         const int64_t dy_strides[2], const vmoba_norm_grads* grads, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Diagnostics; not part of the method.  Registers a device buffer of 16 uint64 counters (NULL: clears the
  * registration) into which the tensor-core attention kernels launched afterwards ADD, per CTA, the clock
  * cycles that one representative thread of each warp role spent in each section of its loop; divide by the

@@ -25,6 +25,8 @@ EXPORTS = (
     "vmoba_attn_bwd_raster_do", "vmoba_full_attn",
     "vmoba_rotary", "vmoba_rotary_bwd", "vmoba_rotary_workspace_bytes",
     "vmoba_range_plan_bytes", "vmoba_range_plan", "vmoba_range_workspace_bytes", "vmoba_range_attn_fwd", "vmoba_range_attn_bwd",
+    "vmoba_linear_workspace_bytes", "vmoba_linear", "vmoba_linear_bwd", "vmoba_ffn_workspace_bytes", "vmoba_ffn", "vmoba_ffn_bwd",
+    "vmoba_block_norm_workspace_bytes", "vmoba_block_norm", "vmoba_block_norm_bwd",
     "vmoba_debug_wait_profile", "vmoba_debug_wait_timeout",
 )
 
@@ -47,6 +49,46 @@ class RotarySpec(ctypes.Structure):
 class RangeShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "heads", "kv_heads", "head_dim", "Sq", "Sk", "dtype", "mask_batch")] + [
         ("softmax_scale", ctypes.c_float), ("softcap", ctypes.c_float)]
+
+
+ACT_NONE, ACT_GELU, ACT_SILU = 0, 1, 2
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+_ACTS = {"none": ACT_NONE, "gelu": ACT_GELU, "silu": ACT_SILU}
+_NORMS = {"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
+_DTYPES = {"f32": F32, "bf16": BF16}
+
+
+class LinearShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "S", "n_in", "n_out", "dtype", "activation", "gated", "heads", "gate_tokens")]
+
+    @property
+    def wide(self):
+        """Rows of the weight."""
+        return self.n_out * (2 if self.gated else 1)
+
+    @property
+    def groups(self):
+        """Rows of the gate, per sample."""
+        return -(-self.S // self.gate_tokens) if self.gate_tokens else 1
+
+
+class NormShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "S", "C", "dtype", "stream_dtype", "norm", "post_norm", "mod_tokens")] + [
+        ("eps", ctypes.c_float)]
+
+    @property
+    def groups(self):
+        """Rows of gate, scale and shift, per sample."""
+        return -(-self.S // self.mod_tokens) if self.mod_tokens else 1
+
+
+class NormParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("gate", "scale", "shift")] + [
+        (n + "_strides", ctypes.c_int64 * 2) for n in ("gate", "scale", "shift")] + [(n, ctypes.c_void_p) for n in ("weight", "bias", "post_weight")]
+
+
+class NormGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("gate", "scale", "shift", "weight", "bias", "post_weight")]
 
 
 class Shape(ctypes.Structure):
@@ -82,6 +124,18 @@ def make_shape(B, heads, head_dim, grid, block, dtype, softmax_scale=0.0) -> Sha
 def make_range_shape(B, heads, kv_heads, head_dim, Sq, Sk, dtype, mask_batch=1, softmax_scale=0.0, softcap=0.0) -> RangeShape:
     code = {"f32": F32, "bf16": BF16}[dtype] if isinstance(dtype, str) else int(dtype)
     return RangeShape(B, heads, kv_heads, head_dim, Sq, Sk, code, mask_batch, softmax_scale, softcap)
+
+
+def make_linear_shape(B, S, n_in, n_out, dtype, activation="none", gated=False, heads=0, gate_tokens=0) -> LinearShape:
+    return LinearShape(B, S, n_in, n_out, _DTYPES[dtype] if isinstance(dtype, str) else int(dtype),
+                       _ACTS[activation] if isinstance(activation, str) else int(activation), int(gated), heads, gate_tokens)
+
+
+def make_norm_shape(B, S, channels, dtype, stream_dtype=None, norm="layer", post_norm="none", mod_tokens=0, eps=1e-6) -> NormShape:
+    """stream_dtype: of the residual stream (default: dtype)."""
+    code = lambda table, x: table[x] if isinstance(x, str) else int(x)
+    return NormShape(B, S, channels, code(_DTYPES, dtype), code(_DTYPES, dtype if stream_dtype is None else stream_dtype), code(_NORMS, norm),
+                     code(_NORMS, post_norm), mod_tokens, eps)
 
 
 def shape_of(w) -> Shape:
@@ -174,6 +228,24 @@ def lib():
     L.vmoba_range_attn_fwd.argtypes = [ap, vp] + [vp, p64] * 4 + [vp, vp, vp, vp, sz, vp]
     L.vmoba_range_attn_bwd.restype = ctypes.c_int
     L.vmoba_range_attn_bwd.argtypes = [ap, vp] + [vp, p64] * 4 + [vp, vp] + [vp, p64] * 4 + [vp, vp, sz, vp]
+    ls, ns, np_, ng = (ctypes.POINTER(t) for t in (LinearShape, NormShape, NormParams, NormGrads))
+    for name in ("vmoba_linear_workspace_bytes", "vmoba_ffn_workspace_bytes"):
+        getattr(L, name).restype = sz
+        getattr(L, name).argtypes = [ls, ctypes.c_int]
+    L.vmoba_linear.restype = ctypes.c_int
+    L.vmoba_linear.argtypes = [ls, vp, p64, vp, vp, vp, p64, vp, p64, vp, p64, vp, vp, vp, vp, sz, vp]
+    L.vmoba_linear_bwd.restype = ctypes.c_int
+    L.vmoba_linear_bwd.argtypes = [ls, vp, p64, vp, p64, vp, vp, vp, p64, vp, p64, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.vmoba_ffn.restype = ctypes.c_int
+    L.vmoba_ffn.argtypes = [ls, vp, p64, vp, vp, vp, vp, vp, p64, vp, p64, vp, p64, vp, vp, vp, vp, sz, vp]
+    L.vmoba_ffn_bwd.restype = ctypes.c_int
+    L.vmoba_ffn_bwd.argtypes = [ls, vp, p64, vp, p64, vp, vp, vp, vp, vp, p64, vp, p64] + [vp] * 7 + [sz, vp]
+    L.vmoba_block_norm_workspace_bytes.restype = sz
+    L.vmoba_block_norm_workspace_bytes.argtypes = [ns]
+    L.vmoba_block_norm.restype = ctypes.c_int
+    L.vmoba_block_norm.argtypes = [ns, np_] + [vp, p64] * 4 + [vp]
+    L.vmoba_block_norm_bwd.restype = ctypes.c_int
+    L.vmoba_block_norm_bwd.argtypes = [ns, np_] + [vp, p64] * 6 + [ng, vp, sz, vp]
     _lib = L
     return L
 
@@ -407,6 +479,75 @@ def vmoba_range_attn_bwd(shape, plan, q, qs, k, ks, v, vs, o, os_, o_resid, lse,
                                       _ptr(o), _I64x3(*os_), _ptr(o_resid), _ptr(lse), _ptr(d_o), _I64x3(*dos), _ptr(dq), _I64x3(*dqs),
                                       _ptr(dk), _I64x3(*dks), _ptr(dv), _I64x3(*dvs), _ptr(dev_status), p, n, _stream(stream)),
            "vmoba_range_attn_bwd")
+
+
+_I64x2 = ctypes.c_int64 * 2
+
+
+def _pair(st):
+    return None if st is None else _I64x2(*st)
+
+
+def linear_workspace_bytes(shape, backward: bool = False) -> int:
+    return int(lib().vmoba_linear_workspace_bytes(ctypes.byref(shape), int(backward)))
+
+
+def ffn_workspace_bytes(shape, backward: bool = False) -> int:
+    return int(lib().vmoba_ffn_workspace_bytes(ctypes.byref(shape), int(backward)))
+
+
+def vmoba_linear(shape, x, xs, weight, bias, gate, gs, residual, rs, out, os_, kept, perm, dev_status, ws, stream=None):
+    """Tensors with their element strides (batch, token), the gate's (batch, group)."""
+    p, n = _ws_args(ws)
+    _check(lib().vmoba_linear(ctypes.byref(shape), _ptr(x), _pair(xs), _ptr(weight), _ptr(bias), _ptr(gate), _pair(gs), _ptr(residual), _pair(rs),
+                              _ptr(out), _pair(os_), _ptr(kept), _ptr(perm), _ptr(dev_status), p, n, _stream(stream)), "vmoba_linear")
+
+
+def vmoba_linear_bwd(shape, d_out, dos, x, xs, weight, kept, gate, gs, dx, dxs, dweight, dbias, dgate, perm, dev_status, ws, stream=None):
+    p, n = _ws_args(ws)
+    _check(lib().vmoba_linear_bwd(ctypes.byref(shape), _ptr(d_out), _pair(dos), _ptr(x), _pair(xs), _ptr(weight), _ptr(kept), _ptr(gate), _pair(gs),
+                                  _ptr(dx), _pair(dxs), _ptr(dweight), _ptr(dbias), _ptr(dgate), _ptr(perm), _ptr(dev_status), p, n,
+                                  _stream(stream)), "vmoba_linear_bwd")
+
+
+def vmoba_ffn(shape, x, xs, w_up, b_up, w_down, b_down, gate, gs, residual, rs, out, os_, kept_up, kept_down, dev_status, ws, stream=None):
+    p, n = _ws_args(ws)
+    _check(lib().vmoba_ffn(ctypes.byref(shape), _ptr(x), _pair(xs), _ptr(w_up), _ptr(b_up), _ptr(w_down), _ptr(b_down), _ptr(gate), _pair(gs),
+                           _ptr(residual), _pair(rs), _ptr(out), _pair(os_), _ptr(kept_up), _ptr(kept_down), _ptr(dev_status), p, n,
+                           _stream(stream)), "vmoba_ffn")
+
+
+def vmoba_ffn_bwd(shape, d_out, dos, x, xs, w_up, w_down, kept_up, kept_down, gate, gs, dx, dxs, dw_up, db_up, dw_down, db_down, dgate,
+                  dev_status, ws, stream=None):
+    p, n = _ws_args(ws)
+    _check(lib().vmoba_ffn_bwd(ctypes.byref(shape), _ptr(d_out), _pair(dos), _ptr(x), _pair(xs), _ptr(w_up), _ptr(w_down), _ptr(kept_up),
+                               _ptr(kept_down), _ptr(gate), _pair(gs), _ptr(dx), _pair(dxs), _ptr(dw_up), _ptr(db_up), _ptr(dw_down),
+                               _ptr(db_down), _ptr(dgate), _ptr(dev_status), p, n, _stream(stream)), "vmoba_ffn_bwd")
+
+
+def block_norm_workspace_bytes(shape) -> int:
+    return int(lib().vmoba_block_norm_workspace_bytes(ctypes.byref(shape)))
+
+
+def norm_params(gate=None, gate_strides=(0, 0), scale=None, scale_strides=(0, 0), shift=None, shift_strides=(0, 0), weight=None, bias=None,
+                post_weight=None) -> NormParams:
+    return NormParams(_ptr(gate), _ptr(scale), _ptr(shift), _I64x2(*gate_strides), _I64x2(*scale_strides), _I64x2(*shift_strides), _ptr(weight),
+                      _ptr(bias), _ptr(post_weight))
+
+
+def vmoba_block_norm(shape, params, x, xs, y, ys, h, hs, out, os_, stream=None):
+    """params: norm_params(); tensors with their element strides (batch, token)."""
+    _check(lib().vmoba_block_norm(ctypes.byref(shape), ctypes.byref(params), _ptr(x), _pair(xs), _ptr(y), _pair(ys), _ptr(h), _pair(hs), _ptr(out),
+                                  _pair(os_), _stream(stream)), "vmoba_block_norm")
+
+
+def vmoba_block_norm_bwd(shape, params, d_out, dos, h, hs, d_h, dhs, y, ys, dx, dxs, dy, dys, grads, ws, stream=None):
+    """grads: a dict of fp32 tensors by the params' names; what is not in it is left out."""
+    p, n = _ws_args(ws)
+    g = NormGrads(**{k: _ptr(t) for k, t in grads.items()})
+    _check(lib().vmoba_block_norm_bwd(ctypes.byref(shape), ctypes.byref(params), _ptr(d_out), _pair(dos), _ptr(h), _pair(hs), _ptr(d_h), _pair(dhs),
+                                      _ptr(y), _pair(ys), _ptr(dx), _pair(dxs), _ptr(dy), _pair(dys), ctypes.byref(g), p, n, _stream(stream)),
+           "vmoba_block_norm_bwd")
 
 
 def vmoba_debug_wait_timeout(dev_status, polls, out2=None, stream=None):

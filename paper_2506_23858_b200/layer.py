@@ -168,6 +168,253 @@ class Rotary:
         return dw
 
 
+_F32, _BF16 = torch.float32, torch.bfloat16
+
+
+class _Rows:
+    """What Linear, FeedForward and BlockNorm share: checks of tensors [B, S, channels] and of rows of gates."""
+
+    def _rows(self, x, channels, dtype, what, written=False):
+        """x as the kernels can address it (an input that they cannot is copied) and its strides (batch, token)."""
+        s = self.shape
+        if x.shape != (s.B, s.S, channels) or x.dtype is not dtype or x.device != self.device:
+            raise ValueError(f"{type(self).__name__}: {what} has to be {dtype} [{s.B}, {s.S}, {channels}] on {self.device}")
+        if x.is_contiguous() and x.data_ptr() % 16 == 0:
+            return x, (s.S * channels, channels)
+        st, per = x.stride(), 16 // x.element_size()
+        if x.stride(2) == 1 and x.data_ptr() % 16 == 0 and all(n == 1 or (i % per == 0 and channels <= i < 2 ** 38) for n, i in zip(x.shape[:2], st)):
+            return x, st[:2]
+        if written:
+            raise ValueError(f"{type(self).__name__}: {what} needs 16-byte rows on 16-byte boundaries that do not share memory")
+        x = torch.empty(x.shape, dtype=dtype, device=x.device).copy_(x)
+        return x, (s.S * channels, channels)
+
+    def _groups(self, g, channels, what):
+        """Rows of a gate, scale or shift [B (or 1), groups, channels] and their strides (batch, group)."""
+        if g is None:
+            return None, (0, 0)
+        s = self.shape
+        if g.dim() != 3 or g.shape[0] not in (1, s.B) or g.shape[1:] != (s.groups, channels) or g.dtype is not _F32 or g.device != self.device:
+            raise ValueError(f"{type(self).__name__}: {what} has to be fp32 [{s.B} or 1, {s.groups}, {channels}] on {self.device}")
+        st = [0 if n == 1 else i for n, i in zip(g.shape[:2], g.stride())]
+        if g.stride(2) != 1 or g.data_ptr() % 16 or any(i % 4 or (i != 0 and not channels <= i < 2 ** 38) for i in st):
+            g = torch.empty(g.shape, dtype=_F32, device=g.device).copy_(g)
+            st = [0 if n == 1 else i for n, i in zip(g.shape[:2], g.stride())]
+        return g, st
+
+    def _dense(self, x, shape, dtype, what):
+        """A contiguous tensor of this shape; one that begins elsewhere than on 16 bytes is copied."""
+        if x is None:
+            return None
+        if tuple(x.shape) != tuple(shape) or x.dtype is not dtype or x.device != self.device or not x.is_contiguous():
+            raise ValueError(f"{type(self).__name__}: {what} has to be {dtype} {list(shape)} on {self.device}, contiguous")
+        return x if x.data_ptr() % 16 == 0 else torch.empty_like(x).copy_(x)
+
+    def _written(self, x, shape, dtype, what):
+        if x is not None and self._dense(x, shape, dtype, what) is not x:
+            raise ValueError(f"{type(self).__name__}: {what} has to begin on a 16-byte boundary")
+        return x
+
+    def _new(self, shape, dtype, wanted=True):
+        return torch.empty(shape, dtype=dtype, device=self.device) if wanted else None
+
+    def check_status(self):
+        code = int(self.dev_status.item())
+        if code != vb.OK:
+            raise vb.VmobaError(code, "device status")
+
+
+def _cuda_device(device, what):
+    d = torch.device(device)
+    if d.type != "cuda":
+        raise ValueError(f"{what}: a GPU required")
+    return torch.device("cuda", torch.cuda.current_device() if d.index is None else d.index)
+
+
+class Linear(_Rows):
+    """A linear layer with what follows it in a transformer block: out = residual + gate * act(x W^T + bias); gated: W is [2 n_out, n_in], and
+    act(first half of the product) * second half takes the place of act(..).
+
+    shape: binding.make_linear_shape().  x is [B, S, n_in], or with heads the block-major [B, heads, S, n_in / heads] that an attention layer
+    leaves, perm then being the raster token of its every position (VmobaLayer.perm).  The object holds no tensors of a call (but a word for
+    the device's status), so that any number of streams and captured graphs can use it at the same time."""
+
+    def __init__(self, shape, device="cuda"):
+        self.shape, self.device = shape, _cuda_device(device, "Linear")
+        self._ws = vb.linear_workspace_bytes(shape)
+        if self._ws == 0:
+            raise ValueError("Linear: channels are multiples of 8, heads of 64 or 128 channels; shape out of range")
+        self._ws_bwd = vb.linear_workspace_bytes(shape, True)
+        self.dtype = torch_dtype(shape)
+        self.dev_status = torch.zeros(1, dtype=torch.int32, device=self.device)
+
+    def _input(self, x, what, written=False):
+        s = self.shape
+        if not s.heads:
+            return self._rows(x, s.n_in, self.dtype, what, written)
+        return (self._written if written else self._dense)(x, (s.B, s.heads, s.S, s.n_in // s.heads), self.dtype, what), None
+
+    def _perm(self, perm):
+        if perm is not None and (not self.shape.heads or perm.dtype != torch.int32 or perm.numel() != self.shape.S or not perm.is_contiguous()
+                                 or perm.device != self.device):
+            raise ValueError(f"Linear: perm goes with heads, and is {self.shape.S} contiguous int32 values on {self.device}")
+        return perm
+
+    def forward(self, x, weight, out, bias=None, gate=None, residual=None, perm=None, kept=None):
+        """Writes out [B, S, n_out], which may be the residual.  kept [B, S, n_out or 2 n_out]: receives x W^T + bias, in the order of x, for
+        backward()."""
+        s, dt = self.shape, self.dtype
+        x, xs = self._input(x, "x")
+        weight = self._dense(weight, (s.wide, s.n_in), dt, "weight")
+        bias = self._dense(bias, (s.wide,), dt, "bias")
+        gate, gs = self._groups(gate, s.n_out, "gate")
+        residual, rs = (None, None) if residual is None else self._rows(residual, s.n_out, dt, "residual")
+        out, os_ = self._rows(out, s.n_out, dt, "out", True)
+        kept = self._written(kept, (s.B, s.S, s.wide), dt, "kept")
+        with _on(self.device):
+            vb.vmoba_linear(s, x, xs, weight, bias, gate, gs, residual, rs, out, os_, kept, self._perm(perm), self.dev_status,
+                            self._new(self._ws, torch.uint8))
+
+    def backward(self, d_out, x, weight, dx_out, kept=None, gate=None, perm=None, with_weight=True, with_bias=False):
+        """Gradients of forward(), whose residual's is d_out: writes dx_out (the order of x; None: not wanted), returns those of weight, bias
+        and gate (fp32 [B, groups, n_out]), None for what is not wanted or not there.  kept as forward() left it; without an activation, gated product
+        or gate it may be None."""
+        s, dt = self.shape, self.dtype
+        d_out, dos = self._rows(d_out, s.n_out, dt, "d_out")
+        x, xs = self._input(x, "x")
+        weight = self._dense(weight, (s.wide, s.n_in), dt, "weight")
+        kept = self._dense(kept, (s.B, s.S, s.wide), dt, "kept")
+        gate, gs = self._groups(gate, s.n_out, "gate")
+        if kept is None and (s.activation != vb.ACT_NONE or s.gated or gate is not None):
+            raise ValueError("Linear: this layer's backward() needs what forward() left in kept")
+        dx_out, dxs = (None, None) if dx_out is None else self._input(dx_out, "dx_out", True)
+        dw, db = self._new((s.wide, s.n_in), dt, with_weight), self._new((s.wide,), dt, with_bias)
+        dg = self._new((s.B, s.groups, s.n_out), _F32, gate is not None)
+        with _on(self.device):
+            vb.vmoba_linear_bwd(s, d_out, dos, x, xs, weight, kept, gate, gs, dx_out, dxs, dw, db, dg, self._perm(perm), self.dev_status,
+                                self._new(self._ws_bwd, torch.uint8))
+        return dw, db, dg
+
+
+class FeedForward(_Rows):
+    """A feed-forward block: out = residual + gate * (h W_down^T + b_down), h = act(x W_up^T + b_up); gated: W_up is [2 hidden, channels], and
+    h = act(first half of the product) * second half.  Holds no tensors of a call (but a word for the device's status)."""
+
+    def __init__(self, B, S, channels, hidden, dtype="bf16", activation="gelu", gated=False, gate_tokens=0, device="cuda"):
+        self.shape, self.device = vb.make_linear_shape(B, S, channels, hidden, dtype, activation, gated, 0, gate_tokens), _cuda_device(device, "FeedForward")
+        self._ws = vb.ffn_workspace_bytes(self.shape)
+        if self._ws == 0:
+            raise ValueError("FeedForward: channels are multiples of 8; shape out of range")
+        self._ws_bwd = vb.ffn_workspace_bytes(self.shape, True)
+        self.dtype = torch_dtype(self.shape)
+        self.dev_status = torch.zeros(1, dtype=torch.int32, device=self.device)
+
+    def keep(self):
+        """Tensors for forward() to leave in what backward() needs: the products ahead of the activation and of the gate."""
+        s = self.shape
+        return self._new((s.B, s.S, s.wide), self.dtype), self._new((s.B, s.S, s.n_in), self.dtype)
+
+    def _weights(self, w_up, w_down):
+        s = self.shape
+        return (self._dense(w_up, (s.wide, s.n_in), self.dtype, "w_up"), self._dense(w_down, (s.n_in, s.n_out), self.dtype, "w_down"))
+
+    def forward(self, x, w_up, w_down, out, b_up=None, b_down=None, gate=None, residual=None, kept=None):
+        """Writes out [B, S, channels], which may be the residual.  kept: keep(), filled for backward()."""
+        s, dt = self.shape, self.dtype
+        x, xs = self._rows(x, s.n_in, dt, "x")
+        w_up, w_down = self._weights(w_up, w_down)
+        b_up, b_down = self._dense(b_up, (s.wide,), dt, "b_up"), self._dense(b_down, (s.n_in,), dt, "b_down")
+        gate, gs = self._groups(gate, s.n_in, "gate")
+        residual, rs = (None, None) if residual is None else self._rows(residual, s.n_in, dt, "residual")
+        out, os_ = self._rows(out, s.n_in, dt, "out", True)
+        up, down = (None, None) if kept is None else kept
+        up, down = self._written(up, (s.B, s.S, s.wide), dt, "kept"), self._written(down, (s.B, s.S, s.n_in), dt, "kept")
+        with _on(self.device):
+            vb.vmoba_ffn(s, x, xs, w_up, b_up, w_down, b_down, gate, gs, residual, rs, out, os_, up, down, self.dev_status,
+                         self._new(self._ws, torch.uint8))
+
+    def backward(self, d_out, x, w_up, w_down, kept, dx_out, gate=None, with_weights=True, with_bias=False):
+        """Gradients of forward(), whose residual's is d_out: writes dx_out (None: not wanted), returns those of w_up, w_down, b_up, b_down and
+        gate (fp32 [B, groups, channels]), None for what is not wanted or not there.  kept: as forward() left it; without a gate the
+        second of the two may be None."""
+        s, dt = self.shape, self.dtype
+        d_out, dos = self._rows(d_out, s.n_in, dt, "d_out")
+        x, xs = self._rows(x, s.n_in, dt, "x")
+        w_up, w_down = self._weights(w_up, w_down)
+        up, down = self._dense(kept[0], (s.B, s.S, s.wide), dt, "kept"), self._dense(kept[1], (s.B, s.S, s.n_in), dt, "kept")
+        gate, gs = self._groups(gate, s.n_in, "gate")
+        if up is None or (gate is not None and down is None):
+            raise ValueError("FeedForward: backward() needs what forward() left in kept")
+        dx_out, dxs = (None, None) if dx_out is None else self._rows(dx_out, s.n_in, dt, "dx_out", True)
+        dwu, dwd = self._new((s.wide, s.n_in), dt, with_weights), self._new((s.n_in, s.n_out), dt, with_weights)
+        dbu, dbd = self._new((s.wide,), dt, with_bias), self._new((s.n_in,), dt, with_bias)
+        dg = self._new((s.B, s.groups, s.n_in), _F32, gate is not None)
+        with _on(self.device):
+            vb.vmoba_ffn_bwd(s, d_out, dos, x, xs, w_up, w_down, up, down, gate, gs, dx_out, dxs, dwu, dbu, dwd, dbd, dg, self.dev_status,
+                             self._new(self._ws_bwd, torch.uint8))
+        return dwu, dwd, dbu, dbd, dg
+
+
+class BlockNorm(_Rows):
+    """What stands between two branches of a transformer block: h = x + gate * post(y), out = (norm(h) * weight + bias) * (1 + scale) + shift.
+
+    shape: binding.make_norm_shape().  x, y, h and out are [B, S, channels], x and h of the stream's type; gate, scale and shift fp32
+    [B or 1, groups, channels], one row for mod_tokens tokens; weight, bias and post_weight fp32 [channels]; everything but x may be
+    left out.  Holds no tensors, so that any number of streams and captured graphs can use one at the same time."""
+
+    def __init__(self, shape, device="cuda"):
+        self.shape, self.device = shape, _cuda_device(device, "BlockNorm")
+        self._ws = vb.block_norm_workspace_bytes(shape)
+        if self._ws == 0:
+            raise ValueError("BlockNorm: channels are multiples of 8 up to 8192, fp32 branches go with fp32 streams; shape out of range")
+        self.dtype = torch_dtype(shape)
+        self.stream_dtype = _BF16 if shape.stream_dtype == vb.BF16 else _F32
+
+    def _params(self, gate, scale, shift, weight, bias, post_weight):
+        C = self.shape.C
+        (gate, gs), (scale, ss), (shift, hs) = (self._groups(g, C, n) for g, n in ((gate, "gate"), (scale, "scale"), (shift, "shift")))
+        weight, bias, post_weight = (self._dense(v, (C,), _F32, n) for v, n in ((weight, "weight"), (bias, "bias"), (post_weight, "post_weight")))
+        held = (gate, scale, shift, weight, bias, post_weight)      # (copies live until the launch)
+        return vb.norm_params(gate, gs, scale, ss, shift, hs, weight, bias, post_weight), held
+
+    def _opt(self, x, dtype, what, written=False):
+        return (None, None) if x is None else self._rows(x, self.shape.C, dtype, what, written)
+
+    def forward(self, x, out=None, y=None, h_out=None, gate=None, scale=None, shift=None, weight=None, bias=None, post_weight=None):
+        """Writes out and h_out (either may be None; h_out may be x)."""
+        params, held = self._params(gate, scale, shift, weight, bias, post_weight)
+        x, xs = self._rows(x, self.shape.C, self.stream_dtype, "x")
+        y, ys = self._opt(y, self.dtype, "y")
+        h_out, hs = self._opt(h_out, self.stream_dtype, "h_out", True)
+        out, os_ = self._opt(out, self.dtype, "out", True)
+        if out is None and h_out is None:
+            raise ValueError("BlockNorm: out or h_out required")
+        with _on(self.device):
+            vb.vmoba_block_norm(self.shape, params, x, xs, y, ys, h_out, hs, out, os_)
+
+    def backward(self, d_out, h, dx_out, d_h=None, y=None, dy_out=None, gate=None, scale=None, shift=None, weight=None, bias=None,
+                 post_weight=None):
+        """Gradients of forward() from its h (x, where there was no y): writes dx_out (that of x; may be d_h, what else arrives at h) and
+        dy_out; returns a dict of dgate, dscale, dshift (fp32 [B, groups, channels]), dweight, dbias and dpost_weight (fp32 [channels]), None
+        where the parameter is not there."""
+        s, C = self.shape, self.shape.C
+        params, held = self._params(gate, scale, shift, weight, bias, post_weight)
+        if y is None and (dy_out is not None or gate is not None or post_weight is not None):
+            raise ValueError("BlockNorm: dy_out, gate and post_weight go with y")
+        d_out, dos = self._rows(d_out, C, self.dtype, "d_out")
+        h, hs = self._rows(h, C, self.stream_dtype, "h")
+        d_h, dhs = self._opt(d_h, self.stream_dtype, "d_h")
+        y, ys = self._opt(y, self.dtype, "y")
+        dx_out, dxs = self._rows(dx_out, C, self.stream_dtype, "dx_out", True)
+        dy_out, dys = self._opt(dy_out, self.dtype, "dy_out", True)
+        there = {"gate": gate, "scale": scale, "shift": shift, "weight": weight, "bias": bias, "post_weight": post_weight}
+        grads = {n: self._new((s.B, s.groups, C) if n in ("gate", "scale", "shift") else (C,), _F32) for n, t in there.items() if t is not None}
+        with _on(self.device):
+            vb.vmoba_block_norm_bwd(s, params, d_out, dos, h, hs, d_h, dhs, y, ys, dx_out, dxs, dy_out, dys, grads,
+                                    self._new(self._ws, torch.uint8))
+        return {"d" + n: grads.get(n) for n in there}
+
+
 class VmobaLayer:
     """Owns the device buffers of one layer shape and runs the stages on the current stream."""
 
