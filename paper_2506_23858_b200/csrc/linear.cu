@@ -220,8 +220,8 @@ int sum_chunks(const float* part, int cols, int groups, int per, void* out, bool
   return VMOBA_OK;
 }
 
-size_t product_scratch(const Product& p) { return 0; }
-int run_product(const Product& p, float* scratch, cudaStream_t st) { return simt_product(p, scratch, st); }
+size_t product_scratch(const Product& p) { return p.bf16 ? tc_scratch(p) : 0; }
+int run_product(const Product& p, float* scratch, cudaStream_t st) { return p.bf16 ? tc_product(p, scratch, st) : simt_product(p, st); }
 
 namespace {
 

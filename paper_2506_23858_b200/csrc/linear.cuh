@@ -62,7 +62,7 @@ size_t product_scratch(const Product& p);
 int run_product(const Product& p, float* scratch, cudaStream_t st);
 
 // fp32 (linear_simt.cu) and bf16 (linear_tc.cu).
-int simt_product(const Product& p, float* scratch, cudaStream_t st);
+int simt_product(const Product& p, cudaStream_t st);
 size_t tc_scratch(const Product& p);
 int tc_product(const Product& p, float* scratch, cudaStream_t st);
 

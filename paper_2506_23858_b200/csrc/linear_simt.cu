@@ -138,14 +138,14 @@ int by_form(const Product& p, const Args& a, cudaStream_t st) {
 
 }  // namespace
 
-int simt_product(const Product& p, float*, cudaStream_t st) {
+int simt_product(const Product& p, cudaStream_t st) {
   Args a;
   a.a = p.a; a.b = p.b; a.e = p.e; a.M = p.M; a.N = p.N;
   a.a_S = FastDiv((unsigned)p.a.S); a.a_inner = FastDiv((unsigned)p.a.inner);
   a.b_S = FastDiv((unsigned)p.b.S); a.b_inner = FastDiv((unsigned)p.b.inner);
   a.a_rows = p.a.B * p.a.S; a.b_rows = p.b.B * p.b.S;
   a.K = p.form == kColsCols ? a.a_rows : p.a.cols;
-  return p.bf16 ? by_form<__nv_bfloat16>(p, a, st) : by_form<float>(p, a, st);
+  return by_form<float>(p, a, st);
 }
 
 }  // namespace linear
