@@ -529,7 +529,8 @@ size_t vmoba_block_norm_workspace_bytes(const vmoba_norm_shape* shape);      /* 
 int vmoba_block_norm_bwd(const vmoba_norm_shape* shape, const vmoba_norm_params* params, const void* d_out, const int64_t d_out_strides[2],
                          const void* h, const int64_t h_strides[2], const void* d_h_or_null, const int64_t d_h_strides[2],
                          const void* y_or_null, const int64_t y_strides[2], void* dx, const int64_t dx_strides[2], void* dy_or_null,
-                         const int64_t dy_strides[2], const vmoba_norm_grads* grads, void* ws, size_t ws_bytes, void* stream);
+                         const int64_t dy_strides[2], const vmoba_norm_grads* grads, int32_t* dev_status, void* ws, size_t ws_bytes,
+                         void* stream);
 
 /*
  * Diagnostics; not part of the method.  Registers a device buffer of 16 uint64 counters (NULL: clears the

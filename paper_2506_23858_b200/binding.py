@@ -245,7 +245,7 @@ def lib():
     L.vmoba_block_norm.restype = ctypes.c_int
     L.vmoba_block_norm.argtypes = [ns, np_] + [vp, p64] * 4 + [vp]
     L.vmoba_block_norm_bwd.restype = ctypes.c_int
-    L.vmoba_block_norm_bwd.argtypes = [ns, np_] + [vp, p64] * 6 + [ng, vp, sz, vp]
+    L.vmoba_block_norm_bwd.argtypes = [ns, np_] + [vp, p64] * 6 + [ng, vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -541,12 +541,13 @@ def vmoba_block_norm(shape, params, x, xs, y, ys, h, hs, out, os_, stream=None):
                                   _pair(os_), _stream(stream)), "vmoba_block_norm")
 
 
-def vmoba_block_norm_bwd(shape, params, d_out, dos, h, hs, d_h, dhs, y, ys, dx, dxs, dy, dys, grads, ws, stream=None):
+def vmoba_block_norm_bwd(shape, params, d_out, dos, h, hs, d_h, dhs, y, ys, dx, dxs, dy, dys, grads, dev_status, ws, stream=None):
     """grads: a dict of fp32 tensors by the params' names; what is not in it is left out."""
     p, n = _ws_args(ws)
     g = NormGrads(**{k: _ptr(t) for k, t in grads.items()})
     _check(lib().vmoba_block_norm_bwd(ctypes.byref(shape), ctypes.byref(params), _ptr(d_out), _pair(dos), _ptr(h), _pair(hs), _ptr(d_h), _pair(dhs),
-                                      _ptr(y), _pair(ys), _ptr(dx), _pair(dxs), _ptr(dy), _pair(dys), ctypes.byref(g), p, n, _stream(stream)),
+                                      _ptr(y), _pair(ys), _ptr(dx), _pair(dxs), _ptr(dy), _pair(dys), ctypes.byref(g), _ptr(dev_status), p, n,
+                                      _stream(stream)),
            "vmoba_block_norm_bwd")
 
 

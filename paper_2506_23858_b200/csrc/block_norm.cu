@@ -4,10 +4,12 @@
 //   dh = d_h + r (dm w - n mean(dm w n) [- mean(dm w)]),   dz = gate * dh,   dy = dz, or through the post norm in the same way
 //   with, per group of tokens that share a row of scale, shift and gate,   A = sum d_out n,   D = sum d_out,   E = sum dh post(y):
 //   dscale = w A + b D,  dshift = D,  dgate = wp E,   dw = sum over groups (1 + scale) A,  db = sum (1 + scale) D,  dwp = sum gate E.
-// Bound by HBM: forward x and y in, h and out out; backward d_out, d_h, h and y in, dx and dy out.  So a row stays in registers between the
-// norms' trips through it.  Forward, a row is taken by as few warps as hold it in six 8-channel pieces per thread, each group of warps on
-// its own.  Backward, a thread keeps its channels over all rows of its CTA's chunk of a group, so that A, D and E add up in registers; the chunks' sums are
-// added by a second kernel in a fixed order.  Variances are taken about the mean, in a second trip.
+// Bound by HBM: forward x and y in, h and out out; backward d_out, d_h, h and y in, dx and dy out.  So a row stays on the SM between the norms'
+// trips through it.  Forward, a row is taken by as few warps as hold it in three 8-channel pieces per thread, in registers, each group of warps on its
+// own.  Backward, a thread keeps its channels over all rows of its CTA's chunk of a group, so that A, D and E add up in registers and scale and
+// gate are loaded once; the rows come through a ring in shared memory, a bulk copy per tensor, so that the sums over a row (two meetings of the
+// CTA, three with a post norm) wait for no memory.  The chunks' sums are added by a second kernel in a fixed order.
+// Variances are taken about the mean of a warp's channels, and the warps' means and variances put together.
 #include <algorithm>
 
 #include "linear.cuh"
@@ -19,7 +21,7 @@ using linear::load_vec;
 using linear::store_vec;
 
 constexpr int kMostChannels = 8192;
-constexpr int kFwdPieces = 6, kFwdWarps = 8;
+constexpr int kFwdPieces = 3, kFwdWarps = 8;
 
 struct Rows {
   const void* p;
@@ -37,7 +39,9 @@ struct Params {
   const float *weight, *bias, *post_weight;
   int wpr, groups;                           // forward: warps per row, rows that a CTA has under way
   int cpg, chunk;                            // backward: chunks per group, rows of a chunk
+  int batch, stage_dh;                       // rows of a batch; whether d_h goes through the ring
   float* part;                               // [chunk][3][C]
+  int32_t* status;
 };
 
 template <typename T>
@@ -45,39 +49,122 @@ __device__ __forceinline__ T* row_of(const Rows& r, int b, int t) {
   return static_cast<T*>(const_cast<void*>(r.p)) + b * r.sb + t * r.st;
 }
 
-// Sums over the threads of a row, of two values.  slot: a pair per warp of the row; a call that takes the same one again has another
-// call between (whose barrier no warp passes before it has read this one's).
-__device__ __forceinline__ float2 row_sum(float a, float b, int warp, int warps, int barrier, float2* slot) {
+__device__ __forceinline__ float warp_sum(float a) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+  return a;
+}
+__device__ __forceinline__ float2 warp_sum(float2 a) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    a += __shfl_xor_sync(0xffffffffu, a, o);
-    b += __shfl_xor_sync(0xffffffffu, b, o);
+    a.x += __shfl_xor_sync(0xffffffffu, a.x, o);
+    a.y += __shfl_xor_sync(0xffffffffu, a.y, o);
   }
-  if (warps == 1) return make_float2(a, b);
-  if ((threadIdx.x & 31) == 0) slot[warp] = make_float2(a, b);
-  asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
-  float2 s = make_float2(0.f, 0.f);
-  for (int w = 0; w < warps; ++w) { s.x += slot[w].x; s.y += slot[w].y; }
-  return s;
+  return a;
 }
+__device__ __forceinline__ void meet(int barrier, int warps) {
+  asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
+}
+
+// Eight channels at a time, in pairs: d = a b + c with a number or another piece for b and c.
+struct Same { float v; __device__ __forceinline__ float operator[](int) const { return v; } };
+template <typename B, typename C>
+__device__ __forceinline__ void fma8(float (&d)[8], const float (&a)[8], const B& b, const C& c) {
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) sm100::fma2(d[k], d[k + 1], a[k], a[k + 1], b[k], b[k + 1], c[k], c[k + 1]);
+}
+template <typename B>
+__device__ __forceinline__ void mul8(float (&d)[8], const float (&a)[8], const B& b) {
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) sm100::mul2(d[k], d[k + 1], a[k], a[k + 1], b[k], b[k + 1]);
+}
+template <typename B>
+__device__ __forceinline__ void add8(float (&d)[8], const float (&a)[8], const B& b) {
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) sm100::add2(d[k], d[k + 1], a[k], a[k + 1], b[k], b[k + 1]);
+}
+// s += a . b, and s += sum of a, in two halves
+__device__ __forceinline__ void dot8(float2& s, const float (&a)[8], const float (&b)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) sm100::fma2(s.x, s.y, a[k], a[k + 1], b[k], b[k + 1], s.x, s.y);
+}
+__device__ __forceinline__ void sum8(float2& s, const float (&a)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) sm100::add2(s.x, s.y, s.x, s.y, a[k], a[k + 1]);
+}
+
+// Mean (0 for a root-mean-square norm) and 1 / sqrt(variance + eps) of a row, from those of its warps' channels.
+struct Stat { float mean, factor; };
+// What a warp has to say of its channels: their sum and the sum of squares about their mean (about 0: root mean square); n of them.
+template <int P>
+__device__ __forceinline__ float2 warp_stat(int kind, const float (&v)[P][8], const bool (&mine)[P], float n) {
+  float s = 0.f, q = 0.f;
+  if (kind == VMOBA_NORM_LAYER) {
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += v[i][k];            // (0 where there are no channels)
+    s = warp_sum(s);
+  }
+  const float mean = n > 0.f ? __fdividef(s, n) : 0.f;
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+    if (mine[i])
+#pragma unroll
+      for (int k = 0; k < 8; ++k) { const float d = v[i][k] - mean; q = fmaf(d, d, q); }
+  return make_float2(s, warp_sum(q));
+}
+// n_of: the number of channels of a warp.
+template <typename N>
+__device__ __forceinline__ Stat put_together(int kind, const float2* slot, int warps, N n_of, float inv_c, float eps) {
+  float s = 0.f, q = 0.f;
+  for (int w = 0; w < warps; ++w) { const float2 a = slot[w]; s += a.x; q += a.y; }
+  const float mean = s * inv_c;
+  if (kind == VMOBA_NORM_LAYER && warps > 1)
+    for (int w = 0; w < warps; ++w) {
+      const float n = n_of(w);
+      if (n > 0.f) { const float d = __fdividef(slot[w].x, n) - mean; q = fmaf(n * d, d, q); }
+    }
+  return {kind == VMOBA_NORM_LAYER ? mean : 0.f, 1.f / sqrtf(q * inv_c + eps)};
+}
+
+// CTAs of the forward on an SM, by the registers of P pieces per thread.
+__host__ __device__ constexpr int fwd_ctas(int P) { return P == 1 ? 4 : P <= 3 ? 3 : 2; }
 
 // TS: the stream's type, T: the branch's.  P: pieces per thread.
 template <typename TS, typename T, int P>
-__global__ void __launch_bounds__(32 * kFwdWarps) norm_fwd_kernel(Params p) {
+__global__ void __launch_bounds__(32 * kFwdWarps, fwd_ctas(P)) norm_fwd_kernel(Params p) {
   if (!grid_begin()) return;
-  __shared__ float2 s_slots[2][4][kFwdWarps];
+  __shared__ float2 s_slots[2][2][kFwdWarps];
   const int group = (threadIdx.x >> 5) / p.wpr, warp = (threadIdx.x >> 5) - group * p.wpr, tpr = 32 * p.wpr;
   const int l = threadIdx.x - group * tpr;
-  int turn = 0;                              // (a row may have a single sum: the next one's goes elsewhere)
-  auto sum = [&](float a, float b, int slot) { return row_sum(a, b, warp, p.wpr, 1 + group, &s_slots[turn][slot][group * p.wpr]); };
+  bool mine[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) mine[i] = 8 * (l + i * tpr) < p.C;
+  // pieces of warp w: 32 of every run of tpr, as far as there are any
+  auto n_of = [&](int w) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < P; ++i) n += min(max(p.pieces - 32 * w - i * tpr, 0), 32);
+    return 8.f * (float)n;
+  };
+  const float n_mine = n_of(warp);
+  int turn = 0;                              // (a row may have a single meeting: the next one's numbers go elsewhere)
+  auto stat = [&](int kind, const float (&v)[P][8], int which) {
+    const float2 a = warp_stat<P>(kind, v, mine, n_mine);
+    if (p.wpr == 1) return put_together(kind, &a, 1, n_of, p.mean, p.eps);
+    float2* slot = &s_slots[turn][which][group * p.wpr];
+    if ((threadIdx.x & 31) == 0) slot[warp] = a;
+    meet(1 + group, p.wpr);
+    return put_together(kind, slot, p.wpr, n_of, p.mean, p.eps);
+  };
   for (int r = blockIdx.x * p.groups + group; r < p.rows; r += gridDim.x * p.groups, turn ^= 1) {
     const int b = p.by_S.div(r), t = r - b * p.S, g = p.by_gt.div(t);
     float h[P][8];
     const TS* x_row = row_of<const TS>(p.x, b, t);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int c = 8 * (l + i * tpr);
-      if (c < p.C) load_vec<8>(x_row + c, h[i]);
+      if (mine[i]) load_vec<8>(x_row + 8 * (l + i * tpr), h[i]);
       else
 #pragma unroll
         for (int k = 0; k < 8; ++k) h[i][k] = 0.f;
@@ -87,39 +174,24 @@ __global__ void __launch_bounds__(32 * kFwdWarps) norm_fwd_kernel(Params p) {
       float y[P][8];
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        const int c = 8 * (l + i * tpr);
-        if (c < p.C) load_vec<8>(y_row + c, y[i]);
+        if (mine[i]) load_vec<8>(y_row + 8 * (l + i * tpr), y[i]);
         else
 #pragma unroll
           for (int k = 0; k < 8; ++k) y[i][k] = 0.f;
       }
-      float mean = 0.f, factor = 1.f;
-      if (p.post == VMOBA_NORM_LAYER) {
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < P; ++i)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) s += y[i][k];
-        mean = sum(s, 0.f, 0).x * p.mean;
-      }
       if (p.post != VMOBA_NORM_NONE) {
-        float s = 0.f;
+        const Stat s = stat(p.post, y, 0);
 #pragma unroll
         for (int i = 0; i < P; ++i)
-          if (8 * (l + i * tpr) < p.C)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) { y[i][k] -= mean; s = fmaf(y[i][k], y[i][k], s); }
-        factor = 1.f / sqrtf(sum(s, 0.f, 1).x * p.mean + p.eps);
+          for (int k = 0; k < 8; ++k) y[i][k] = (y[i][k] - s.mean) * s.factor;
       }
       const float* gate = p.gate ? p.gate + b * p.gate_s[0] + g * p.gate_s[1] : nullptr;
-      TS* h_row = p.h.p ? row_of<TS>(p.h, b, t) : nullptr;
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         const int c = 8 * (l + i * tpr);
-        if (c >= p.C) continue;
+        if (!mine[i]) continue;
         float f[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) y[i][k] *= factor;
         if (p.post_weight) {
           load_vec<8>(p.post_weight + c, f);
 #pragma unroll
@@ -133,41 +205,26 @@ __global__ void __launch_bounds__(32 * kFwdWarps) norm_fwd_kernel(Params p) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) h[i][k] += y[i][k];
         }
-        if (h_row) store_vec<8>(h_row + c, h[i]);
       }
-    } else if (p.h.p) {
+    }
+    if (p.h.p) {
       TS* h_row = row_of<TS>(p.h, b, t);
 #pragma unroll
       for (int i = 0; i < P; ++i)
-        if (8 * (l + i * tpr) < p.C) store_vec<8>(h_row + 8 * (l + i * tpr), h[i]);
+        if (mine[i]) store_vec<8>(h_row + 8 * (l + i * tpr), h[i]);
     }
     if (!p.out.p) continue;
-    float mean = 0.f;
-    if (p.norm == VMOBA_NORM_LAYER) {
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < P; ++i)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s += h[i][k];
-      mean = sum(s, 0.f, 2).x * p.mean;
-    }
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < P; ++i)
-      if (8 * (l + i * tpr) < p.C)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) { h[i][k] -= mean; s = fmaf(h[i][k], h[i][k], s); }
-    const float factor = 1.f / sqrtf(sum(s, 0.f, 3).x * p.mean + p.eps);
+    const Stat s = stat(p.norm, h, 1);
     const float* scale = p.scale ? p.scale + b * p.scale_s[0] + g * p.scale_s[1] : nullptr;
     const float* shift = p.shift ? p.shift + b * p.shift_s[0] + g * p.shift_s[1] : nullptr;
     T* out_row = row_of<T>(p.out, b, t);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const int c = 8 * (l + i * tpr);
-      if (c >= p.C) continue;
+      if (!mine[i]) continue;
       float f[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) h[i][k] *= factor;
+      for (int k = 0; k < 8; ++k) h[i][k] = (h[i][k] - s.mean) * s.factor;
       if (p.weight) {
         load_vec<8>(p.weight + c, f);
 #pragma unroll
@@ -193,129 +250,265 @@ __global__ void __launch_bounds__(32 * kFwdWarps) norm_fwd_kernel(Params p) {
   }
 }
 
-// A CTA takes the rows of one chunk one after another; thread l the pieces l, l + blockDim.x ..
-template <typename TS, typename T, int P>
-__global__ void __launch_bounds__(P == 1 ? 256 : 512) norm_bwd_kernel(Params p) {
+// Backward.  A CTA takes the rows of one chunk, a few at a time (a batch; the next one is on its way into the other half of the ring), a thread the
+// same channels of all of them.  What a row's sums need of a thread's channels goes to shared memory, a warp adds up each row, and the
+// threads go on with the sums: no lane adds up with another but in those warps.  (All warps adding up every row across their lanes: 3,400
+// instructions a row of 1,536 channels, 347 us for 32,760 of them; a warp going through a whole row for its sums: 2,290 and 206 us.)
+__host__ __device__ constexpr int batch_rows(int P) { return P == 1 ? 4 : 2; }
+struct alignas(16) RowSums { float mean, factor, along, level, y_mean, y_factor, y_along, y_level; };
+
+template <typename TS, typename T, int P, bool POST>
+__global__ void __launch_bounds__(P == 1 ? 256 : 512, P == 1 ? 2 : 1) norm_bwd_kernel(Params p) {
   if (!grid_begin()) return;
-  __shared__ float2 s_slots[4][16];
-  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, l = threadIdx.x, tpr = blockDim.x;
-  auto sum = [&](float a, float b, int slot) { return row_sum(a, b, warp, warps, 0, s_slots[slot]); };
+  constexpr int NB = batch_rows(P);
+  extern __shared__ __align__(128) char s_rows[];
+  __shared__ RowSums s_sums[NB];
+  __shared__ uint64_t s_full[2];
+  __shared__ int s_abort;
+  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31, l = threadIdx.x, tpr = blockDim.x;
   const int gi = blockIdx.x / p.cpg, j = blockIdx.x - gi * p.cpg, b = gi / p.G, g = gi - b * p.G;
   const int t0 = g * p.gt + j * p.chunk, t1 = min(min(t0 + p.chunk, (g + 1) * p.gt), p.S);
-  float A[P][8] = {}, D[P][8] = {}, E[P][8] = {};
+  const bool dh_here = p.stage_dh != 0, layer = p.norm == VMOBA_NORM_LAYER, y_layer = POST && p.post == VMOBA_NORM_LAYER;
+  // bytes of a row of the stream's and of the branch's type; places in a slot: h, d_out, y, d_h; behind the ring the threads' parts of sums
+  const uint32_t bs = (uint32_t)p.C * sizeof(TS), bt = (uint32_t)p.C * sizeof(T);
+  const uint32_t at_d = bs, at_y = at_d + bt, at_dh = at_y + (p.y.p ? bt : 0u);
+  const uint32_t bytes = at_dh + (dh_here ? bs : 0u), stride = (bytes + 127u) & ~127u;
+  float2* const s_part = reinterpret_cast<float2*>(s_rows + 2 * p.batch * stride);      // [row][thread], and again for y
+  float2* const s_part_y = s_part + p.batch * tpr;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) sm100::mbar_init(&s_full[i], 1);
+    s_abort = 0;
+    sm100::fence_barrier_init();
+  }
+  __syncthreads();
+  auto ask = [&](int k) {                    // (one thread) for batch k
+    const int first = t0 + k * p.batch, n = min(p.batch, t1 - first);
+    if (n <= 0) return;
+    uint64_t* bar = &s_full[k & 1];
+    sm100::mbar_expect_tx(bar, (uint32_t)n * bytes);
+    uint32_t to = sm100::smem_u32(s_rows) + (k & 1) * p.batch * stride;
+    auto copy = [&](uint32_t at, const void* from, uint32_t size) {
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + at), "l"(from), "r"(size),
+                   "r"(sm100::smem_u32(bar))
+                   : "memory");
+    };
+    for (int t = first; t < first + n; ++t, to += stride) {
+      copy(0, row_of<const TS>(p.h, b, t), bs);
+      copy(at_d, row_of<const T>(p.d_out, b, t), bt);
+      if (p.y.p) copy(at_y, row_of<const T>(p.y, b, t), bt);
+      if (dh_here) copy(at_dh, row_of<const TS>(p.d_h, b, t), bs);
+    }
+  };
+  if (threadIdx.x == 0) { ask(0); ask(1); }
+  float A[P][8] = {}, D[P][8] = {}, E[P][8] = {}, fm[P][8], fg[P][8];      // (1 + scale) * weight, gate * post weight
   bool mine[P];
 #pragma unroll
-  for (int i = 0; i < P; ++i) mine[i] = 8 * (l + i * tpr) < p.C;
-  const float* gate = p.gate ? p.gate + b * p.gate_s[0] + g * p.gate_s[1] : nullptr;
-  const float* scale = p.scale ? p.scale + b * p.scale_s[0] + g * p.scale_s[1] : nullptr;
-  for (int t = t0; t < t1; ++t) {
-    float h[P][8] = {}, d[P][8] = {}, y[P][8] = {}, dh[P][8] = {};
+  for (int i = 0; i < P; ++i) {
+    const int c = 8 * (l + i * tpr);
+    mine[i] = c < p.C;
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int c = 8 * (l + i * tpr);
-      if (!mine[i]) continue;
-      load_vec<8>(row_of<const TS>(p.h, b, t) + c, h[i]);
-      load_vec<8>(row_of<const T>(p.d_out, b, t) + c, d[i]);
-      if (p.y.p) load_vec<8>(row_of<const T>(p.y, b, t) + c, y[i]);
-      if (p.d_h.p) load_vec<8>(row_of<const TS>(p.d_h, b, t) + c, dh[i]);
+    for (int k = 0; k < 8; ++k) fm[i][k] = fg[i][k] = 1.f;
+    if (!mine[i]) continue;
+    float f[8];
+    if (p.scale) {
+      load_vec<8>(p.scale + b * p.scale_s[0] + g * p.scale_s[1] + c, f);
+      add8(fm[i], fm[i], f);
     }
-    // means, then variances, of both norms
-    float2 s = make_float2(0.f, 0.f);
-    const bool means = p.norm == VMOBA_NORM_LAYER || (p.y.p && p.post == VMOBA_NORM_LAYER);
-    if (means) {
-#pragma unroll
-      for (int i = 0; i < P; ++i)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) { s.x += h[i][k]; s.y += y[i][k]; }
-      s = sum(s.x, s.y, 0);
+    if (p.weight) {
+      load_vec<8>(p.weight + c, f);
+      mul8(fm[i], fm[i], f);
     }
-    const float mean_h = p.norm == VMOBA_NORM_LAYER ? s.x * p.mean : 0.f, mean_y = p.post == VMOBA_NORM_LAYER ? s.y * p.mean : 0.f;
-    s = make_float2(0.f, 0.f);
+    if (p.gate) load_vec<8>(p.gate + b * p.gate_s[0] + g * p.gate_s[1] + c, fg[i]);
+    if (p.post_weight) {
+      load_vec<8>(p.post_weight + c, f);
+      mul8(fg[i], fg[i], f);
+    }
+  }
+  // Channels of thread i, and their number over 8 of this one.
+  auto n_of = [&](int i) {
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < P; ++k) n += i + k * tpr < p.pieces;
+    return 8.f * (float)n;
+  };
+  const float inv_n = 1.f / fmaxf(n_of(l), 1.f);
+  // a thread's channels of a row: their sum and the sum of squares about their mean (about 0: root mean square)
+  auto part_of = [&](bool centred, const float (&v)[P][8]) {
+    float2 s = make_float2(0.f, 0.f), q = s;
+    float mean = 0.f;
+    if (centred) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) sum8(s, v[i]);           // (0 where there are no channels)
+      mean = (s.x + s.y) * inv_n;
+    }
 #pragma unroll
     for (int i = 0; i < P; ++i)
-      if (mine[i])
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          h[i][k] -= mean_h;
-          y[i][k] -= mean_y;
-          s.x = fmaf(h[i][k], h[i][k], s.x);
-          s.y = fmaf(y[i][k], y[i][k], s.y);
-        }
-    s = sum(s.x, s.y, 1);
-    const float rh = 1.f / sqrtf(s.x * p.mean + p.eps), ry = p.post == VMOBA_NORM_NONE ? 1.f : 1.f / sqrtf(s.y * p.mean + p.eps);
-    // the norm's gradient
-    s = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      if (!mine[i]) continue;
-      const int c = 8 * (l + i * tpr);
-      float f[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        h[i][k] *= rh;
-        A[i][k] = fmaf(d[i][k], h[i][k], A[i][k]);
-        D[i][k] += d[i][k];
+      if (P == 1 || mine[i]) {
+        float d[8];
+        add8(d, v[i], Same{-mean});
+        dot8(q, d, d);
       }
-      if (scale) {
-        load_vec<8>(scale + c, f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) d[i][k] = fmaf(d[i][k], f[k], d[i][k]);
-      }
-      if (p.weight) {
-        load_vec<8>(p.weight + c, f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) d[i][k] *= f[k];
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) { s.x = fmaf(d[i][k], h[i][k], s.x); s.y += d[i][k]; }
-    }
-    s = sum(s.x, s.y, 2);
-    const float along = s.x * p.mean, level = p.norm == VMOBA_NORM_LAYER ? s.y * p.mean : 0.f;
-    TS* dx_row = row_of<TS>(p.dx, b, t);
-    s = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      if (!mine[i]) continue;
-      const int c = 8 * (l + i * tpr);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) dh[i][k] = fmaf(rh, d[i][k] - level - h[i][k] * along, dh[i][k]);
-      store_vec<8>(dx_row + c, dh[i]);
-      if (p.y.p) {
-        float f[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          y[i][k] *= ry;
-          E[i][k] = fmaf(dh[i][k], y[i][k], E[i][k]);
-        }
-        if (gate) {
-          load_vec<8>(gate + c, f);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) dh[i][k] *= f[k];
-        }
-        if (p.post_weight) {
-          load_vec<8>(p.post_weight + c, f);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) dh[i][k] *= f[k];
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) { s.x = fmaf(dh[i][k], y[i][k], s.x); s.y += dh[i][k]; }
+    return make_float2(s.x + s.y, q.x + q.y);
+  };
+  // (one warp) mean and 1 / sqrt(variance + eps) of a row from the threads' parts
+  auto stat_of = [&](bool centred, const float2* part, float* mean, float* factor) {
+    float s = 0.f, q = 0.f;
+    for (int i = lane; i < tpr; i += 32) { const float2 a = part[i]; s += a.x; q += a.y; }
+    if (centred) {
+      s = warp_sum(s) * p.mean;
+      for (int i = lane; i < tpr; i += 32) {
+        const float n = n_of(i), d = n > 0.f ? part[i].x * (P == 1 ? 0.125f : __fdividef(1.f, n)) - s : 0.f;
+        q = fmaf(n * d, d, q);
       }
     }
-    if (!p.dy.p) continue;
-    T* dy_row = row_of<T>(p.dy, b, t);
-    if (p.post != VMOBA_NORM_NONE) {
-      s = sum(s.x, s.y, 3);
-      s.x *= p.mean;
-      s.y = p.post == VMOBA_NORM_LAYER ? s.y * p.mean : 0.f;
-    }
+    if (lane == 0) *mean = centred ? s : 0.f;
+    *factor = 1.f / sqrtf(warp_sum(q) * p.mean + p.eps);
+  };
+  auto means_of = [&](const float2* part) {  // (one warp)
+    float2 s = make_float2(0.f, 0.f);
+    for (int i = lane; i < tpr; i += 32) { const float2 a = part[i]; s.x += a.x; s.y += a.y; }
+    s = warp_sum(s);
+    return make_float2(s.x * p.mean, s.y * p.mean);
+  };
+  const int batches = (t1 - t0 + p.batch - 1) / p.batch;
+  for (int k = 0; k < batches; ++k) {
+    const int first = t0 + k * p.batch, n = min(p.batch, t1 - first);
+    const char* half = s_rows + (k & 1) * p.batch * stride;
+    sm100::mbar_wait(&s_full[k & 1], (k >> 1) & 1, &s_abort, p.status);
+    __syncwarp();
+    float h[NB][P][8];
+    // ---- means and variances
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      if (!mine[i]) continue;
-      if (p.post != VMOBA_NORM_NONE)
+    for (int r = 0; r < NB; ++r) {
+      if (r >= n) break;
+      const char* row = half + r * stride;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dh[i][k] = ry * (dh[i][k] - s.y - y[i][k] * s.x);
-      store_vec<8>(dy_row + 8 * (l + i * tpr), dh[i]);
+      for (int i = 0; i < P; ++i) {
+        if (mine[i]) load_vec<8>(reinterpret_cast<const TS*>(row) + 8 * (l + i * tpr), h[r][i]);
+        else
+#pragma unroll
+          for (int q = 0; q < 8; ++q) h[r][i][q] = 0.f;
+      }
+      s_part[r * tpr + l] = part_of(layer, h[r]);
+      if (POST) {
+        float y[P][8];
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          if (mine[i]) load_vec<8>(reinterpret_cast<const T*>(row + at_y) + 8 * (l + i * tpr), y[i]);
+          else
+#pragma unroll
+            for (int q = 0; q < 8; ++q) y[i][q] = 0.f;
+        }
+        s_part_y[r * tpr + l] = part_of(y_layer, y);
+      }
     }
+    __syncthreads();
+    for (int r = warp; r < (POST ? 2 * n : n); r += warps) {
+      RowSums& o = s_sums[r >= n ? r - n : r];
+      float factor;
+      if (r < n) {
+        stat_of(layer, s_part + r * tpr, &o.mean, &factor);
+        if (lane == 0) o.factor = factor;
+      } else {
+        stat_of(y_layer, s_part_y + (r - n) * tpr, &o.y_mean, &factor);
+        if (lane == 0) o.y_factor = factor;
+      }
+    }
+    __syncthreads();
+    // ---- the norm's gradient: how much of it lies along n, and its level
+#pragma unroll
+    for (int r = 0; r < NB; ++r) {
+      if (r >= n) break;
+      const char* row = half + r * stride;
+      const float mean = s_sums[r].mean, factor = s_sums[r].factor;
+      float2 a = make_float2(0.f, 0.f), c = a;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        if (!mine[i]) continue;
+        float d[8];
+        load_vec<8>(reinterpret_cast<const T*>(row + at_d) + 8 * (l + i * tpr), d);
+        fma8(h[r][i], h[r][i], Same{factor}, Same{-mean * factor});
+        fma8(A[i], d, h[r][i], A[i]);
+        add8(D[i], D[i], d);
+        mul8(d, d, fm[i]);
+        dot8(a, d, h[r][i]);
+        if (layer) sum8(c, d);
+      }
+      s_part[r * tpr + l] = make_float2(a.x + a.y, c.x + c.y);
+    }
+    __syncthreads();
+    for (int r = warp; r < n; r += warps) {
+      const float2 s = means_of(s_part + r * tpr);
+      if (lane == 0) { s_sums[r].along = s.x; s_sums[r].level = s.y; }
+    }
+    __syncthreads();
+    // ---- dx, and without a post norm dy
+#pragma unroll
+    for (int r = 0; r < NB; ++r) {
+      if (r >= n) break;
+      const char* row = half + r * stride;
+      const RowSums o = s_sums[r];
+      TS* dx_row = row_of<TS>(p.dx, b, first + r);
+      float2 a = make_float2(0.f, 0.f), c2 = a;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        if (!mine[i]) continue;
+        const int c = 8 * (l + i * tpr);
+        float d[8], dh[8] = {};
+        load_vec<8>(reinterpret_cast<const T*>(row + at_d) + c, d);
+        if (dh_here) load_vec<8>(reinterpret_cast<const TS*>(row + at_dh) + c, dh);
+        else if (p.d_h.p) load_vec<8>(row_of<const TS>(p.d_h, b, first + r) + c, dh);
+        mul8(d, d, fm[i]);
+        if (layer) add8(d, d, Same{-o.level});
+        fma8(d, h[r][i], Same{-o.along}, d);
+        fma8(dh, d, Same{o.factor}, dh);
+        store_vec<8>(dx_row + c, dh);
+        if (p.y.p) {
+          float y[8];
+          load_vec<8>(reinterpret_cast<const T*>(row + at_y) + c, y);
+          if (POST) fma8(y, y, Same{o.y_factor}, Same{-o.y_mean * o.y_factor});
+          fma8(E[i], dh, y, E[i]);
+          mul8(dh, dh, fg[i]);
+          if (POST) {
+            dot8(a, dh, y);
+            if (y_layer) sum8(c2, dh);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) h[r][i][q] = dh[q];       // (n has done its work)
+          } else if (p.dy.p) {
+            store_vec<8>(row_of<T>(p.dy, b, first + r) + c, dh);
+          }
+        }
+      }
+      if (POST) s_part[r * tpr + l] = make_float2(a.x + a.y, c2.x + c2.y);
+    }
+    if (POST && p.dy.p) {
+      __syncthreads();
+      for (int r = warp; r < n; r += warps) {
+        const float2 s = means_of(s_part + r * tpr);
+        if (lane == 0) { s_sums[r].y_along = s.x; s_sums[r].y_level = s.y; }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < NB; ++r) {
+        if (r >= n) break;
+        const RowSums o = s_sums[r];
+        T* dy_row = row_of<T>(p.dy, b, first + r);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          if (!mine[i]) continue;
+          const int c = 8 * (l + i * tpr);
+          float y[8];
+          load_vec<8>(reinterpret_cast<const T*>(half + r * stride + at_y) + c, y);
+          fma8(y, y, Same{o.y_factor}, Same{-o.y_mean * o.y_factor});
+          fma8(y, y, Same{-o.y_along}, h[r][i]);
+          if (y_layer) add8(y, y, Same{-o.y_level});
+          mul8(y, y, Same{o.y_factor});
+          store_vec<8>(dy_row + c, y);
+        }
+      }
+    }
+    __syncthreads();                         // (everybody has read the batch and its sums)
+    if (threadIdx.x == 0) ask(k + 2);
   }
   if (!p.part) return;
   float* part = p.part + (long long)blockIdx.x * 3 * p.C;
@@ -461,15 +654,16 @@ static Params params_of(const vmoba_norm_shape* s, const Dims& D) {
   return p;
 }
 
-// Backward: threads of a row's CTA, and how the rows of a group are cut: as many chunks as run at a time, 20 warps of an SM.
+// Backward: threads of a CTA, two of them on an SM where their warps are few; a group's rows cut into as many chunks as run at a time.
 constexpr int kSms = 148;
-struct Cut { int threads, pieces, cpg, chunk; long long chunks; };
+struct Cut { int threads, pieces, ctas, cpg, chunk; long long chunks; };
 static Cut cut_of(const Dims& D) {
   Cut c;
   const int pieces = D.C / 8;
   c.pieces = pieces <= 256 ? 1 : 2;
   c.threads = ((pieces + c.pieces - 1) / c.pieces + 31) / 32 * 32;
-  const long long run = (long long)kSms * std::max(1, 20 / (c.threads / 32)), groups = (long long)D.B * D.G;
+  c.ctas = std::max(1, 16 / (c.threads / 32));
+  const long long run = (long long)kSms * c.ctas, groups = (long long)D.B * D.G;
   c.cpg = (int)std::max<long long>(1, std::min<long long>(D.gt, run / groups));
   c.chunk = (D.gt + c.cpg - 1) / c.cpg;
   c.cpg = (D.gt + c.chunk - 1) / c.chunk;
@@ -490,21 +684,41 @@ static Scratch scratch_of(const Dims& D, void* ws) {
 template <typename TS, typename T>
 static int go_fwd(const Dims& D, Params& p, cudaStream_t st) {
   p.wpr = 1;
-  while (p.pieces > 32 * p.wpr * kFwdPieces) p.wpr *= 2;
+  while (p.wpr < kFwdWarps && p.pieces > 32 * p.wpr * kFwdPieces) p.wpr *= 2;
   const int per = (p.pieces + 32 * p.wpr - 1) / (32 * p.wpr);
   p.groups = std::min(kFwdWarps / p.wpr, p.rows);
-  const unsigned ctas = (unsigned)std::min<long long>(((long long)p.rows + p.groups - 1) / p.groups, 4ll * sm_count());
-  auto kernel = per <= 1 ? norm_fwd_kernel<TS, T, 1> : per <= 2 ? norm_fwd_kernel<TS, T, 2> : per <= 4 ? norm_fwd_kernel<TS, T, 4> : norm_fwd_kernel<TS, T, 6>;
-  launch_kernel(kernel, ctas, 32 * p.wpr * p.groups, 0, st, p);
+  auto go = [&](auto pieces) {
+    constexpr int P = decltype(pieces)::value;
+    // as many CTAs as run at a time: they share the rows evenly
+    const long long ctas = std::min<long long>(((long long)p.rows + p.groups - 1) / p.groups, (long long)fwd_ctas(P) * sm_count());
+    launch_kernel(norm_fwd_kernel<TS, T, P>, (unsigned)ctas, 32 * p.wpr * p.groups, 0, st, p);
+  };
+  if (per <= 1) go(std::integral_constant<int, 1>{});
+  else if (per == 2) go(std::integral_constant<int, 2>{});
+  else if (per == 3) go(std::integral_constant<int, 3>{});
+  else go(std::integral_constant<int, 4>{});
   VMOBA_LAUNCH_OK(1);
   return VMOBA_OK;
 }
 template <typename TS, typename T>
 static int go_bwd(const Cut& c, Params& p, cudaStream_t st) {
   p.cpg = c.cpg; p.chunk = c.chunk;
-  launch_kernel(c.pieces == 1 ? norm_bwd_kernel<TS, T, 1> : norm_bwd_kernel<TS, T, 2>, (unsigned)c.chunks, c.threads, 0, st, p);
-  VMOBA_LAUNCH_OK(1);
-  return VMOBA_OK;
+  // two rows at least in the ring, d_h not through it where those would not fit (fp32, more than 6,900 channels)
+  auto slot = [&](bool dh) {
+    return align_up((size_t)p.C * ((dh ? 2 : 1) * sizeof(TS) + (p.y.p ? 2 : 1) * sizeof(T)), 128);
+  };
+  p.stage_dh = p.d_h.p && 2 * slot(true) <= (size_t)kSmemMost;
+  const size_t bytes = slot(p.stage_dh != 0), parts = (size_t)c.threads * 2 * sizeof(float2);
+  p.batch = (int)std::min<size_t>(batch_rows(c.pieces), std::max<size_t>(1, kSmemMost / c.ctas / (2 * bytes + parts)));
+  auto go = [&](auto kernel) -> int {
+    VMOBA_CUDA_OK(allow_smem(kernel, kSmemMost));
+    launch_kernel(kernel, (unsigned)c.chunks, c.threads, p.batch * (2 * bytes + parts), st, p);
+    VMOBA_LAUNCH_OK(1);
+    return VMOBA_OK;
+  };
+  const bool post = p.y.p && p.post != VMOBA_NORM_NONE;
+  if (c.pieces == 1) return post ? go(norm_bwd_kernel<TS, T, 1, true>) : go(norm_bwd_kernel<TS, T, 1, false>);
+  return post ? go(norm_bwd_kernel<TS, T, 2, true>) : go(norm_bwd_kernel<TS, T, 2, false>);
 }
 
 }  // namespace norm
@@ -537,7 +751,7 @@ extern "C" int vmoba_block_norm_bwd(const vmoba_norm_shape* shape, const vmoba_n
                                     const int64_t d_out_strides[2], const void* h, const int64_t h_strides[2], const void* d_h,
                                     const int64_t d_h_strides[2], const void* y, const int64_t y_strides[2], void* dx,
                                     const int64_t dx_strides[2], void* dy, const int64_t dy_strides[2], const vmoba_norm_grads* grads,
-                                    void* ws, size_t ws_bytes, void* stream) {
+                                    int32_t* dev_status, void* ws, size_t ws_bytes, void* stream) {
   norm::Dims D;
   if (int rc = norm::make_dims(shape, &D)) return rc;
   if (!params || !grads || !d_out || !h || !dx || !ws || !aligned16(ws) || (dy && !y)) return VMOBA_ERR_ARG;
@@ -561,6 +775,7 @@ extern "C" int vmoba_block_norm_bwd(const vmoba_norm_shape* shape, const vmoba_n
   const bool vectors = grads->weight || grads->bias || grads->post_weight;
   const bool rows = grads->gate || grads->scale || grads->shift;
   p.part = vectors || rows ? s.part : nullptr;
+  p.status = dev_status;
   VMOBA_GUARDS_ARM(s.guards, st);
   int rc;
   if (!D.bf16) rc = norm::go_bwd<float, float>(cut, p, st);
@@ -581,6 +796,6 @@ extern "C" int vmoba_block_norm_bwd(const vmoba_norm_shape* shape, const vmoba_n
       VMOBA_LAUNCH_OK(1);
     }
   }
-  VMOBA_GUARDS_CHECK(s.guards, nullptr, st);
+  VMOBA_GUARDS_CHECK(s.guards, dev_status, st);
   return VMOBA_OK;
 }

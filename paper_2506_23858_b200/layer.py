@@ -360,13 +360,14 @@ class BlockNorm(_Rows):
 
     shape: binding.make_norm_shape().  x, y, h and out are [B, S, channels], x and h of the stream's type; gate, scale and shift fp32
     [B or 1, groups, channels], one row for mod_tokens tokens; weight, bias and post_weight fp32 [channels]; everything but x may be
-    left out.  Holds no tensors, so that any number of streams and captured graphs can use one at the same time."""
+    left out.  Holds no tensors of a call (but a word for the device's status)."""
 
     def __init__(self, shape, device="cuda"):
         self.shape, self.device = shape, _cuda_device(device, "BlockNorm")
         self._ws = vb.block_norm_workspace_bytes(shape)
         if self._ws == 0:
             raise ValueError("BlockNorm: channels are multiples of 8 up to 8192, fp32 branches go with fp32 streams; shape out of range")
+        self.dev_status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.dtype = torch_dtype(shape)
         self.stream_dtype = _BF16 if shape.stream_dtype == vb.BF16 else _F32
 
@@ -410,7 +411,7 @@ class BlockNorm(_Rows):
         there = {"gate": gate, "scale": scale, "shift": shift, "weight": weight, "bias": bias, "post_weight": post_weight}
         grads = {n: self._new((s.B, s.groups, C) if n in ("gate", "scale", "shift") else (C,), _F32) for n, t in there.items() if t is not None}
         with _on(self.device):
-            vb.vmoba_block_norm_bwd(s, params, d_out, dos, h, hs, d_h, dhs, y, ys, dx_out, dxs, dy_out, dys, grads,
+            vb.vmoba_block_norm_bwd(s, params, d_out, dos, h, hs, d_h, dhs, y, ys, dx_out, dxs, dy_out, dys, grads, self.dev_status,
                                     self._new(self._ws, torch.uint8))
         return {"d" + n: grads.get(n) for n in there}
 

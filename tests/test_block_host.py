@@ -137,7 +137,7 @@ def test_norm_refusals():
     def bwd(s, m=None, h=FAKE, d_h=NULL, y=NULL, dx=FAKE, dxs=st, dy=NULL, n=1 << 40, ws=FAKE, **grads):
         m = vb.norm_params() if m is None else m
         return lib.vmoba_block_norm_bwd(ctypes.byref(s), ctypes.byref(m), FAKE, st, h, st, d_h, st, y, st, dx, dxs, dy, st,
-                                        ctypes.byref(vb.NormGrads(**grads)), ws, n, NULL)
+                                        ctypes.byref(vb.NormGrads(**grads)), NULL, ws, n, NULL)
 
     gated = vb.NormParams(0x1000, None, None, pair(256, 64))
     for kw in (dict(h=NULL), dict(dx=NULL), dict(dy=FAKE), dict(dxs=pair(0, 64)), dict(scale=0x1000), dict(gate=0x1000), dict(m=gated, gate=0x1000),
