@@ -514,7 +514,7 @@ typedef struct {
 
 int vmoba_block_norm(const vmoba_norm_shape* shape, const vmoba_norm_params* params, const void* x, const int64_t x_strides[2],
                      const void* y_or_null, const int64_t y_strides[2], void* h_or_null, const int64_t h_strides[2], void* out_or_null,
-                     const int64_t out_strides[2], void* stream);
+                     const int64_t out_strides[2], int32_t* dev_status, void* stream);
 
 /*
  * Its gradients, from h as the forward left it (rounded; without y that is x), y, d_out and what else arrives at h (d_h, NULL: nothing):

@@ -243,7 +243,7 @@ def lib():
     L.vmoba_block_norm_workspace_bytes.restype = sz
     L.vmoba_block_norm_workspace_bytes.argtypes = [ns]
     L.vmoba_block_norm.restype = ctypes.c_int
-    L.vmoba_block_norm.argtypes = [ns, np_] + [vp, p64] * 4 + [vp]
+    L.vmoba_block_norm.argtypes = [ns, np_] + [vp, p64] * 4 + [vp, vp]
     L.vmoba_block_norm_bwd.restype = ctypes.c_int
     L.vmoba_block_norm_bwd.argtypes = [ns, np_] + [vp, p64] * 6 + [ng, vp, vp, sz, vp]
     _lib = L
@@ -535,10 +535,10 @@ def norm_params(gate=None, gate_strides=(0, 0), scale=None, scale_strides=(0, 0)
                       _ptr(bias), _ptr(post_weight))
 
 
-def vmoba_block_norm(shape, params, x, xs, y, ys, h, hs, out, os_, stream=None):
+def vmoba_block_norm(shape, params, x, xs, y, ys, h, hs, out, os_, dev_status, stream=None):
     """params: norm_params(); tensors with their element strides (batch, token)."""
     _check(lib().vmoba_block_norm(ctypes.byref(shape), ctypes.byref(params), _ptr(x), _pair(xs), _ptr(y), _pair(ys), _ptr(h), _pair(hs), _ptr(out),
-                                  _pair(os_), _stream(stream)), "vmoba_block_norm")
+                                  _pair(os_), _ptr(dev_status), _stream(stream)), "vmoba_block_norm")
 
 
 def vmoba_block_norm_bwd(shape, params, d_out, dos, h, hs, d_h, dhs, y, ys, dx, dxs, dy, dys, grads, dev_status, ws, stream=None):

@@ -4,12 +4,10 @@
 //   dh = d_h + r (dm w - n mean(dm w n) [- mean(dm w)]),   dz = gate * dh,   dy = dz, or through the post norm in the same way
 //   with, per group of tokens that share a row of scale, shift and gate,   A = sum d_out n,   D = sum d_out,   E = sum dh post(y):
 //   dscale = w A + b D,  dshift = D,  dgate = wp E,   dw = sum over groups (1 + scale) A,  db = sum (1 + scale) D,  dwp = sum gate E.
-// Bound by HBM: forward x and y in, h and out out; backward d_out, d_h, h and y in, dx and dy out.  So a row stays on the SM between the norms'
-// trips through it.  Forward, a row is taken by as few warps as hold it in three 8-channel pieces per thread, in registers, each group of warps on its
-// own.  Backward, a thread keeps its channels over all rows of its CTA's chunk of a group, so that A, D and E add up in registers and scale and
-// gate are loaded once; the rows come through a ring in shared memory, a bulk copy per tensor, so that the sums over a row (two meetings of the
-// CTA, three with a post norm) wait for no memory.  The chunks' sums are added by a second kernel in a fixed order.
-// Variances are taken about the mean of a warp's channels, and the warps' means and variances put together.
+// Bound by HBM: forward x and y in, h and out out; backward d_out, d_h, h and y in, dx and dy out.  So rows come through a ring in shared
+// memory, a bulk copy per tensor, and stay on the SM between the norms' trips through them; a thread keeps its channels over all rows of its
+// CTA's chunk of a group, so that scale, shift and gate are loaded once and A, D and E add up in registers.  The chunks' sums are added by a second kernel in
+// a fixed order.  Variances are taken about the mean of a thread's channels, and those means and variances put together.
 #include <algorithm>
 
 #include "linear.cuh"
@@ -21,7 +19,10 @@ using linear::load_vec;
 using linear::store_vec;
 
 constexpr int kMostChannels = 8192;
-constexpr int kFwdPieces = 3, kFwdWarps = 8;
+// Threads of a CTA that has a piece of eight channels for each: by the registers that many leave (85 and 102 each).  The backward has 128 with
+// 256 threads at most, for four rows at a time on two CTAs of an SM (1,536 channels, 32,760 rows: 123 us; three CTAs with 102
+// registers and two rows at a time: 157).
+constexpr int kFwdThreads = 768, kBwdThreads = 640, kBwdNarrow = 256;
 
 struct Rows {
   const void* p;
@@ -37,8 +38,7 @@ struct Params {
   const float *gate, *scale, *shift;
   long long gate_s[2], scale_s[2], shift_s[2];
   const float *weight, *bias, *post_weight;
-  int wpr, groups;                           // forward: warps per row, rows that a CTA has under way
-  int cpg, chunk;                            // backward: chunks per group, rows of a chunk
+  int cpg, chunk;                            // chunks per group, rows of a chunk
   int batch, stage_dh;                       // rows of a batch; whether d_h goes through the ring
   float* part;                               // [chunk][3][C]
   int32_t* status;
@@ -62,10 +62,6 @@ __device__ __forceinline__ float2 warp_sum(float2 a) {
   }
   return a;
 }
-__device__ __forceinline__ void meet(int barrier, int warps) {
-  asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
-}
-
 // Eight channels at a time, in pairs: d = a b + c with a number or another piece for b and c.
 struct Same { float v; __device__ __forceinline__ float operator[](int) const { return v; } };
 template <typename B, typename C>
@@ -93,181 +89,239 @@ __device__ __forceinline__ void sum8(float2& s, const float (&a)[8]) {
   for (int k = 0; k < 8; k += 2) sm100::add2(s.x, s.y, s.x, s.y, a[k], a[k + 1]);
 }
 
-// Mean (0 for a root-mean-square norm) and 1 / sqrt(variance + eps) of a row, from those of its warps' channels.
-struct Stat { float mean, factor; };
-// What a warp has to say of its channels: their sum and the sum of squares about their mean (about 0: root mean square); n of them.
-template <int P>
-__device__ __forceinline__ float2 warp_stat(int kind, const float (&v)[P][8], const bool (&mine)[P], float n) {
-  float s = 0.f, q = 0.f;
-  if (kind == VMOBA_NORM_LAYER) {
-#pragma unroll
-    for (int i = 0; i < P; ++i)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) s += v[i][k];            // (0 where there are no channels)
-    s = warp_sum(s);
+__device__ __forceinline__ void bulk_copy(uint32_t to, const void* from, uint32_t size, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(size),
+               "r"(sm100::smem_u32(bar))
+               : "memory");
+}
+
+// What the kernels share.  A CTA takes the rows of one chunk of a group, a few at a time (a batch; the next one is on its way into the other half
+// of the ring), a thread the same channels of all of them, so that scale, shift and gate are loaded once.  What a row's sums need of a
+// thread's channels goes to shared memory, a warp adds up each row, and the threads go on with the sums: no lane adds up with
+// another but in those warps.
+
+// The rows of a CTA.
+struct Chunk {
+  int b, g, t0, t1;
+  __device__ __forceinline__ explicit Chunk(const Params& p) {
+    const int gi = blockIdx.x / p.cpg, j = blockIdx.x - gi * p.cpg;
+    b = gi / p.G;
+    g = gi - b * p.G;
+    t0 = g * p.gt + j * p.chunk;
+    t1 = min(min(t0 + p.chunk, (g + 1) * p.gt), p.S);
   }
-  const float mean = n > 0.f ? __fdividef(s, n) : 0.f;
-#pragma unroll
-  for (int i = 0; i < P; ++i)
-    if (mine[i])
-#pragma unroll
-      for (int k = 0; k < 8; ++k) { const float d = v[i][k] - mean; q = fmaf(d, d, q); }
-  return make_float2(s, warp_sum(q));
-}
-// n_of: the number of channels of a warp.
-template <typename N>
-__device__ __forceinline__ Stat put_together(int kind, const float2* slot, int warps, N n_of, float inv_c, float eps) {
-  float s = 0.f, q = 0.f;
-  for (int w = 0; w < warps; ++w) { const float2 a = slot[w]; s += a.x; q += a.y; }
-  const float mean = s * inv_c;
-  if (kind == VMOBA_NORM_LAYER && warps > 1)
-    for (int w = 0; w < warps; ++w) {
-      const float n = n_of(w);
-      if (n > 0.f) { const float d = __fdividef(slot[w].x, n) - mean; q = fmaf(n * d, d, q); }
-    }
-  return {kind == VMOBA_NORM_LAYER ? mean : 0.f, 1.f / sqrtf(q * inv_c + eps)};
-}
+};
 
-// CTAs of the forward on an SM, by the registers of P pieces per thread.
-__host__ __device__ constexpr int fwd_ctas(int P) { return P == 1 ? 4 : P <= 3 ? 3 : 2; }
-
-// TS: the stream's type, T: the branch's.  P: pieces per thread.
-template <typename TS, typename T, int P>
-__global__ void __launch_bounds__(32 * kFwdWarps, fwd_ctas(P)) norm_fwd_kernel(Params p) {
-  if (!grid_begin()) return;
-  __shared__ float2 s_slots[2][2][kFwdWarps];
-  const int group = (threadIdx.x >> 5) / p.wpr, warp = (threadIdx.x >> 5) - group * p.wpr, tpr = 32 * p.wpr;
-  const int l = threadIdx.x - group * tpr;
-  bool mine[P];
-#pragma unroll
-  for (int i = 0; i < P; ++i) mine[i] = 8 * (l + i * tpr) < p.C;
-  // pieces of warp w: 32 of every run of tpr, as far as there are any
-  auto n_of = [&](int w) {
+// Sums of a row, of parts that the threads' channels give.
+template <int P>
+struct Sums {
+  const Params& p;
+  const int tpr;
+  __device__ __forceinline__ explicit Sums(const Params& p) : p(p), tpr(blockDim.x) {}
+  // channels of thread i
+  __device__ __forceinline__ float n_of(int i) const {
     int n = 0;
 #pragma unroll
-    for (int i = 0; i < P; ++i) n += min(max(p.pieces - 32 * w - i * tpr, 0), 32);
+    for (int k = 0; k < P; ++k) n += i + k * tpr < p.pieces;
     return 8.f * (float)n;
-  };
-  const float n_mine = n_of(warp);
-  int turn = 0;                              // (a row may have a single meeting: the next one's numbers go elsewhere)
-  auto stat = [&](int kind, const float (&v)[P][8], int which) {
-    const float2 a = warp_stat<P>(kind, v, mine, n_mine);
-    if (p.wpr == 1) return put_together(kind, &a, 1, n_of, p.mean, p.eps);
-    float2* slot = &s_slots[turn][which][group * p.wpr];
-    if ((threadIdx.x & 31) == 0) slot[warp] = a;
-    meet(1 + group, p.wpr);
-    return put_together(kind, slot, p.wpr, n_of, p.mean, p.eps);
-  };
-  for (int r = blockIdx.x * p.groups + group; r < p.rows; r += gridDim.x * p.groups, turn ^= 1) {
-    const int b = p.by_S.div(r), t = r - b * p.S, g = p.by_gt.div(t);
-    float h[P][8];
-    const TS* x_row = row_of<const TS>(p.x, b, t);
+  }
+  // a thread's channels of a row (0 where there are none): their sum and the sum of squares about their mean (about 0: root mean square)
+  __device__ __forceinline__ float2 part(bool centred, const float (&v)[P][8], const bool (&mine)[P], float inv_n) const {
+    float2 s = make_float2(0.f, 0.f), q = s;
+    float mean = 0.f;
+    if (centred) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      if (mine[i]) load_vec<8>(x_row + 8 * (l + i * tpr), h[i]);
-      else
-#pragma unroll
-        for (int k = 0; k < 8; ++k) h[i][k] = 0.f;
+      for (int i = 0; i < P; ++i) sum8(s, v[i]);
+      mean = (s.x + s.y) * inv_n;
     }
-    if (p.y.p) {
-      const T* y_row = row_of<const T>(p.y, b, t);
-      float y[P][8];
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        if (mine[i]) load_vec<8>(y_row + 8 * (l + i * tpr), y[i]);
-        else
-#pragma unroll
-          for (int k = 0; k < 8; ++k) y[i][k] = 0.f;
+    for (int i = 0; i < P; ++i)
+      if (P == 1 || mine[i]) {
+        float d[8];
+        add8(d, v[i], Same{-mean});
+        dot8(q, d, d);
       }
-      if (p.post != VMOBA_NORM_NONE) {
-        const Stat s = stat(p.post, y, 0);
+    return make_float2(s.x + s.y, q.x + q.y);
+  }
+  // (one warp) mean and 1 / sqrt(variance + eps) of a row from the threads' parts
+  __device__ __forceinline__ float2 stat(bool centred, const float2* part) const {
+    const int lane = threadIdx.x & 31;
+    float s = 0.f, q = 0.f;
+    for (int i = lane; i < tpr; i += 32) { const float2 a = part[i]; s += a.x; q += a.y; }
+    if (centred) {
+      s = warp_sum(s) * p.mean;
+      for (int i = lane; i < tpr; i += 32) {
+        const float n = n_of(i), d = n > 0.f ? part[i].x * (P == 1 ? 0.125f : __fdividef(1.f, n)) - s : 0.f;
+        q = fmaf(n * d, d, q);
+      }
+    }
+    return make_float2(centred ? s : 0.f, 1.f / sqrtf(warp_sum(q) * p.mean + p.eps));
+  }
+  __device__ __forceinline__ float2 means(const float2* part) const {
+    float2 s = make_float2(0.f, 0.f);
+    for (int i = threadIdx.x & 31; i < tpr; i += 32) { const float2 a = part[i]; s.x += a.x; s.y += a.y; }
+    s = warp_sum(s);
+    return make_float2(s.x * p.mean, s.y * p.mean);
+  }
+};
+
+// TS: the stream's type, T: the branch's.  P: pieces of eight channels per thread.
+template <typename TS, typename T, int P, bool POST>
+__global__ void __launch_bounds__(P == 1 ? kFwdThreads : 512, 1) norm_fwd_kernel(Params p) {
+  if (!grid_begin()) return;
+  constexpr int NB = P == 1 ? 4 : 2;
+  extern __shared__ __align__(128) char s_rows[];
+  __shared__ float2 s_stat[2][NB];
+  __shared__ uint64_t s_full[2];
+  __shared__ int s_abort;
+  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31, l = threadIdx.x, tpr = blockDim.x;
+  const Chunk at(p);
+  const Sums<P> sums(p);
+  const bool layer = p.norm == VMOBA_NORM_LAYER, y_layer = POST && p.post == VMOBA_NORM_LAYER;
+  const uint32_t bs = (uint32_t)p.C * sizeof(TS), bt = p.y.p ? (uint32_t)p.C * sizeof(T) : 0u, stride = (bs + bt + 127u) & ~127u;
+  float2* const s_part = reinterpret_cast<float2*>(s_rows + 2 * p.batch * stride);      // [row][thread]
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) sm100::mbar_init(&s_full[i], 1);
+    s_abort = 0;
+    sm100::fence_barrier_init();
+  }
+  __syncthreads();
+  auto ask = [&](int k) {                    // (one thread) for batch k
+    const int first = at.t0 + k * p.batch, n = min(p.batch, at.t1 - first);
+    if (n <= 0) return;
+    uint64_t* bar = &s_full[k & 1];
+    sm100::mbar_expect_tx(bar, (uint32_t)n * (bs + bt));
+    uint32_t to = sm100::smem_u32(s_rows) + (k & 1) * p.batch * stride;
+    for (int t = first; t < first + n; ++t, to += stride) {
+      bulk_copy(to, row_of<const TS>(p.x, at.b, t), bs, bar);
+      if (bt) bulk_copy(to + bs, row_of<const T>(p.y, at.b, t), bt, bar);
+    }
+  };
+  if (threadIdx.x == 0) { ask(0); ask(1); }
+  float fg[P][8], fm[P][8], fs[P][8];        // gate * post weight; (1 + scale) * weight; (1 + scale) * bias + shift
+  bool mine[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int c = 8 * (l + i * tpr);
+    mine[i] = c < p.C;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) { fm[i][q] = fg[i][q] = 1.f; fs[i][q] = 0.f; }
+    if (!mine[i]) continue;
+    float f[8];
+    if (p.gate) load_vec<8>(p.gate + at.b * p.gate_s[0] + at.g * p.gate_s[1] + c, fg[i]);
+    if (p.post_weight) {
+      load_vec<8>(p.post_weight + c, f);
+      mul8(fg[i], fg[i], f);
+    }
+    if (p.scale) {
+      load_vec<8>(p.scale + at.b * p.scale_s[0] + at.g * p.scale_s[1] + c, f);
+      add8(fm[i], fm[i], f);
+    }
+    if (p.shift) load_vec<8>(p.shift + at.b * p.shift_s[0] + at.g * p.shift_s[1] + c, fs[i]);
+    if (p.bias) {
+      load_vec<8>(p.bias + c, f);
+      fma8(fs[i], f, fm[i], fs[i]);
+    }
+    if (p.weight) {
+      load_vec<8>(p.weight + c, f);
+      mul8(fm[i], fm[i], f);
+    }
+  }
+  const float inv_n = 1.f / fmaxf(sums.n_of(l), 1.f);
+  const int batches = (at.t1 - at.t0 + p.batch - 1) / p.batch;
+  for (int k = 0; k < batches; ++k) {
+    const int first = at.t0 + k * p.batch, n = min(p.batch, at.t1 - first);
+    const char* half = s_rows + (k & 1) * p.batch * stride;
+    sm100::mbar_wait(&s_full[k & 1], (k >> 1) & 1, &s_abort, p.status);
+    __syncwarp();
+    if (POST) {
+#pragma unroll
+      for (int r = 0; r < NB; ++r) {
+        if (r >= n) break;
+        float y[P][8] = {};
 #pragma unroll
         for (int i = 0; i < P; ++i)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) y[i][k] = (y[i][k] - s.mean) * s.factor;
+          if (mine[i]) load_vec<8>(reinterpret_cast<const T*>(half + r * stride + bs) + 8 * (l + i * tpr), y[i]);
+        s_part[r * tpr + l] = sums.part(y_layer, y, mine, inv_n);
       }
-      const float* gate = p.gate ? p.gate + b * p.gate_s[0] + g * p.gate_s[1] : nullptr;
+      __syncthreads();
+      for (int r = warp; r < n; r += warps) {
+        const float2 s = sums.stat(y_layer, s_part + r * tpr);
+        if (lane == 0) s_stat[0][r] = s;
+      }
+      __syncthreads();
+    }
+    float h[NB][P][8];
+#pragma unroll
+    for (int r = 0; r < NB; ++r) {
+      if (r >= n) break;
+      const char* row = half + r * stride;
+      const float2 sy = POST ? s_stat[0][r] : make_float2(0.f, 1.f);
+      TS* h_row = row_of<TS>(p.h, at.b, first + r);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         const int c = 8 * (l + i * tpr);
-        if (!mine[i]) continue;
-        float f[8];
-        if (p.post_weight) {
-          load_vec<8>(p.post_weight + c, f);
+        if (!mine[i]) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) y[i][k] *= f[k];
+          for (int q = 0; q < 8; ++q) h[r][i][q] = 0.f;
+          continue;
         }
-        if (gate) {
-          load_vec<8>(gate + c, f);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) h[i][k] = fmaf(y[i][k], f[k], h[i][k]);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) h[i][k] += y[i][k];
+        load_vec<8>(reinterpret_cast<const TS*>(row) + c, h[r][i]);
+        if (p.y.p) {
+          float y[8];
+          load_vec<8>(reinterpret_cast<const T*>(row + bs) + c, y);
+          if (POST) {
+            add8(y, y, Same{-sy.x});
+            mul8(y, y, Same{sy.y});
+          }
+          fma8(h[r][i], y, fg[i], h[r][i]);
         }
+        if (p.h.p) store_vec<8>(h_row + c, h[r][i]);
       }
+      if (p.out.p) s_part[r * tpr + l] = sums.part(layer, h[r], mine, inv_n);
     }
-    if (p.h.p) {
-      TS* h_row = row_of<TS>(p.h, b, t);
-#pragma unroll
-      for (int i = 0; i < P; ++i)
-        if (mine[i]) store_vec<8>(h_row + 8 * (l + i * tpr), h[i]);
-    }
+    __syncthreads();                         // (everybody has read the batch)
+    if (threadIdx.x == 0) ask(k + 2);
     if (!p.out.p) continue;
-    const Stat s = stat(p.norm, h, 1);
-    const float* scale = p.scale ? p.scale + b * p.scale_s[0] + g * p.scale_s[1] : nullptr;
-    const float* shift = p.shift ? p.shift + b * p.shift_s[0] + g * p.shift_s[1] : nullptr;
-    T* out_row = row_of<T>(p.out, b, t);
+    for (int r = warp; r < n; r += warps) {
+      const float2 s = sums.stat(layer, s_part + r * tpr);
+      if (lane == 0) s_stat[1][r] = s;
+    }
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int c = 8 * (l + i * tpr);
-      if (!mine[i]) continue;
-      float f[8];
+    for (int r = 0; r < NB; ++r) {
+      if (r >= n) break;
+      const float2 s = s_stat[1][r];
+      T* out_row = row_of<T>(p.out, at.b, first + r);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) h[i][k] = (h[i][k] - s.mean) * s.factor;
-      if (p.weight) {
-        load_vec<8>(p.weight + c, f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) h[i][k] *= f[k];
+      for (int i = 0; i < P; ++i) {
+        if (!mine[i]) continue;
+        float o[8];
+        add8(o, h[r][i], Same{-s.x});
+        mul8(o, o, Same{s.y});
+        fma8(o, o, fm[i], fs[i]);
+        store_vec<8>(out_row + 8 * (l + i * tpr), o);
       }
-      if (p.bias) {
-        load_vec<8>(p.bias + c, f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) h[i][k] += f[k];
-      }
-      if (scale) {
-        load_vec<8>(scale + c, f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) h[i][k] = fmaf(h[i][k], f[k], h[i][k]);
-      }
-      if (shift) {
-        load_vec<8>(shift + c, f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) h[i][k] += f[k];
-      }
-      store_vec<8>(out_row + c, h[i]);
     }
   }
 }
 
-// Backward.  A CTA takes the rows of one chunk, a few at a time (a batch; the next one is on its way into the other half of the ring), a thread the
-// same channels of all of them.  What a row's sums need of a thread's channels goes to shared memory, a warp adds up each row, and the
-// threads go on with the sums: no lane adds up with another but in those warps.  (All warps adding up every row across their lanes: 3,400
-// instructions a row of 1,536 channels, 347 us for 32,760 of them; a warp going through a whole row for its sums: 2,290 and 206 us.)
-__host__ __device__ constexpr int batch_rows(int P) { return P == 1 ? 4 : 2; }
+// (The backward with all warps adding up every row across their lanes: 3,400 instructions a row of 1,536 channels, 347 us for 32,760 of them; with
+// a warp going through a whole row for its sums: 2,290 and 206 us; as it is: 1,720 and 123.)
 struct alignas(16) RowSums { float mean, factor, along, level, y_mean, y_factor, y_along, y_level; };
 
-template <typename TS, typename T, int P, bool POST>
-__global__ void __launch_bounds__(P == 1 ? 256 : 512, P == 1 ? 2 : 1) norm_bwd_kernel(Params p) {
+template <typename TS, typename T, int P, bool POST, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_bwd_kernel(Params p) {
   if (!grid_begin()) return;
-  constexpr int NB = batch_rows(P);
+  constexpr int NB = THREADS == 256 ? 4 : 2;
   extern __shared__ __align__(128) char s_rows[];
   __shared__ RowSums s_sums[NB];
   __shared__ uint64_t s_full[2];
   __shared__ int s_abort;
   const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31, l = threadIdx.x, tpr = blockDim.x;
-  const int gi = blockIdx.x / p.cpg, j = blockIdx.x - gi * p.cpg, b = gi / p.G, g = gi - b * p.G;
-  const int t0 = g * p.gt + j * p.chunk, t1 = min(min(t0 + p.chunk, (g + 1) * p.gt), p.S);
+  const Chunk chunk(p);
+  const int b = chunk.b, g = chunk.g, t0 = chunk.t0, t1 = chunk.t1;
+  const Sums<P> sums(p);
   const bool dh_here = p.stage_dh != 0, layer = p.norm == VMOBA_NORM_LAYER, y_layer = POST && p.post == VMOBA_NORM_LAYER;
   // bytes of a row of the stream's and of the branch's type; places in a slot: h, d_out, y, d_h; behind the ring the threads' parts of sums
   const uint32_t bs = (uint32_t)p.C * sizeof(TS), bt = (uint32_t)p.C * sizeof(T);
@@ -287,16 +341,11 @@ __global__ void __launch_bounds__(P == 1 ? 256 : 512, P == 1 ? 2 : 1) norm_bwd_k
     uint64_t* bar = &s_full[k & 1];
     sm100::mbar_expect_tx(bar, (uint32_t)n * bytes);
     uint32_t to = sm100::smem_u32(s_rows) + (k & 1) * p.batch * stride;
-    auto copy = [&](uint32_t at, const void* from, uint32_t size) {
-      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + at), "l"(from), "r"(size),
-                   "r"(sm100::smem_u32(bar))
-                   : "memory");
-    };
     for (int t = first; t < first + n; ++t, to += stride) {
-      copy(0, row_of<const TS>(p.h, b, t), bs);
-      copy(at_d, row_of<const T>(p.d_out, b, t), bt);
-      if (p.y.p) copy(at_y, row_of<const T>(p.y, b, t), bt);
-      if (dh_here) copy(at_dh, row_of<const TS>(p.d_h, b, t), bs);
+      bulk_copy(to, row_of<const TS>(p.h, b, t), bs, bar);
+      bulk_copy(to + at_d, row_of<const T>(p.d_out, b, t), bt, bar);
+      if (p.y.p) bulk_copy(to + at_y, row_of<const T>(p.y, b, t), bt, bar);
+      if (dh_here) bulk_copy(to + at_dh, row_of<const TS>(p.d_h, b, t), bs, bar);
     }
   };
   if (threadIdx.x == 0) { ask(0); ask(1); }
@@ -324,52 +373,7 @@ __global__ void __launch_bounds__(P == 1 ? 256 : 512, P == 1 ? 2 : 1) norm_bwd_k
       mul8(fg[i], fg[i], f);
     }
   }
-  // Channels of thread i, and their number over 8 of this one.
-  auto n_of = [&](int i) {
-    int n = 0;
-#pragma unroll
-    for (int k = 0; k < P; ++k) n += i + k * tpr < p.pieces;
-    return 8.f * (float)n;
-  };
-  const float inv_n = 1.f / fmaxf(n_of(l), 1.f);
-  // a thread's channels of a row: their sum and the sum of squares about their mean (about 0: root mean square)
-  auto part_of = [&](bool centred, const float (&v)[P][8]) {
-    float2 s = make_float2(0.f, 0.f), q = s;
-    float mean = 0.f;
-    if (centred) {
-#pragma unroll
-      for (int i = 0; i < P; ++i) sum8(s, v[i]);           // (0 where there are no channels)
-      mean = (s.x + s.y) * inv_n;
-    }
-#pragma unroll
-    for (int i = 0; i < P; ++i)
-      if (P == 1 || mine[i]) {
-        float d[8];
-        add8(d, v[i], Same{-mean});
-        dot8(q, d, d);
-      }
-    return make_float2(s.x + s.y, q.x + q.y);
-  };
-  // (one warp) mean and 1 / sqrt(variance + eps) of a row from the threads' parts
-  auto stat_of = [&](bool centred, const float2* part, float* mean, float* factor) {
-    float s = 0.f, q = 0.f;
-    for (int i = lane; i < tpr; i += 32) { const float2 a = part[i]; s += a.x; q += a.y; }
-    if (centred) {
-      s = warp_sum(s) * p.mean;
-      for (int i = lane; i < tpr; i += 32) {
-        const float n = n_of(i), d = n > 0.f ? part[i].x * (P == 1 ? 0.125f : __fdividef(1.f, n)) - s : 0.f;
-        q = fmaf(n * d, d, q);
-      }
-    }
-    if (lane == 0) *mean = centred ? s : 0.f;
-    *factor = 1.f / sqrtf(warp_sum(q) * p.mean + p.eps);
-  };
-  auto means_of = [&](const float2* part) {  // (one warp)
-    float2 s = make_float2(0.f, 0.f);
-    for (int i = lane; i < tpr; i += 32) { const float2 a = part[i]; s.x += a.x; s.y += a.y; }
-    s = warp_sum(s);
-    return make_float2(s.x * p.mean, s.y * p.mean);
-  };
+  const float inv_n = 1.f / fmaxf(sums.n_of(l), 1.f);
   const int batches = (t1 - t0 + p.batch - 1) / p.batch;
   for (int k = 0; k < batches; ++k) {
     const int first = t0 + k * p.batch, n = min(p.batch, t1 - first);
@@ -389,7 +393,7 @@ __global__ void __launch_bounds__(P == 1 ? 256 : 512, P == 1 ? 2 : 1) norm_bwd_k
 #pragma unroll
           for (int q = 0; q < 8; ++q) h[r][i][q] = 0.f;
       }
-      s_part[r * tpr + l] = part_of(layer, h[r]);
+      s_part[r * tpr + l] = sums.part(layer, h[r], mine, inv_n);
       if (POST) {
         float y[P][8];
 #pragma unroll
@@ -399,19 +403,18 @@ __global__ void __launch_bounds__(P == 1 ? 256 : 512, P == 1 ? 2 : 1) norm_bwd_k
 #pragma unroll
             for (int q = 0; q < 8; ++q) y[i][q] = 0.f;
         }
-        s_part_y[r * tpr + l] = part_of(y_layer, y);
+        s_part_y[r * tpr + l] = sums.part(y_layer, y, mine, inv_n);
       }
     }
     __syncthreads();
     for (int r = warp; r < (POST ? 2 * n : n); r += warps) {
       RowSums& o = s_sums[r >= n ? r - n : r];
-      float factor;
       if (r < n) {
-        stat_of(layer, s_part + r * tpr, &o.mean, &factor);
-        if (lane == 0) o.factor = factor;
+        const float2 s = sums.stat(layer, s_part + r * tpr);
+        if (lane == 0) { o.mean = s.x; o.factor = s.y; }
       } else {
-        stat_of(y_layer, s_part_y + (r - n) * tpr, &o.y_mean, &factor);
-        if (lane == 0) o.y_factor = factor;
+        const float2 s = sums.stat(y_layer, s_part_y + (r - n) * tpr);
+        if (lane == 0) { o.y_mean = s.x; o.y_factor = s.y; }
       }
     }
     __syncthreads();
@@ -438,7 +441,7 @@ __global__ void __launch_bounds__(P == 1 ? 256 : 512, P == 1 ? 2 : 1) norm_bwd_k
     }
     __syncthreads();
     for (int r = warp; r < n; r += warps) {
-      const float2 s = means_of(s_part + r * tpr);
+      const float2 s = sums.means(s_part + r * tpr);
       if (lane == 0) { s_sums[r].along = s.x; s_sums[r].level = s.y; }
     }
     __syncthreads();
@@ -484,7 +487,7 @@ __global__ void __launch_bounds__(P == 1 ? 256 : 512, P == 1 ? 2 : 1) norm_bwd_k
     if (POST && p.dy.p) {
       __syncthreads();
       for (int r = warp; r < n; r += warps) {
-        const float2 s = means_of(s_part + r * tpr);
+        const float2 s = sums.means(s_part + r * tpr);
         if (lane == 0) { s_sums[r].y_along = s.x; s_sums[r].y_level = s.y; }
       }
       __syncthreads();
@@ -522,7 +525,7 @@ __global__ void __launch_bounds__(P == 1 ? 256 : 512, P == 1 ? 2 : 1) norm_bwd_k
   }
 }
 
-struct Sums {
+struct GroupSums {
   int C, G, cpg, tiles;
   const float* part;
   float* by_group;                           // [group][3][C], for the vectors' gradients
@@ -530,7 +533,7 @@ struct Sums {
   float *dgate, *dscale, *dshift;
 };
 // A CTA has 32 channels of a group, a warp every eighth chunk.
-__global__ void __launch_bounds__(256) group_sums_kernel(Sums p) {
+__global__ void __launch_bounds__(256) group_sums_kernel(GroupSums p) {
   if (!grid_begin()) return;
   __shared__ float s[3][8][33];
   const int g = blockIdx.x / p.tiles, lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = (blockIdx.x - g * p.tiles) * 32 + lane;
@@ -654,18 +657,24 @@ static Params params_of(const vmoba_norm_shape* s, const Dims& D) {
   return p;
 }
 
-// Backward: threads of a CTA, two of them on an SM where their warps are few; a group's rows cut into as many chunks as run at a time.
-constexpr int kSms = 148;
+// Threads of a CTA, how many CTAs there are on an SM (of `warps` in all), and how the rows of a group are cut.
+constexpr int kSms = 148, kFwdWarps = 24, kBwdWarps = 16;
 struct Cut { int threads, pieces, ctas, cpg, chunk; long long chunks; };
-static Cut cut_of(const Dims& D) {
+static Cut cut_of(const Dims& D, int warps, int threads) {
   Cut c;
   const int pieces = D.C / 8;
-  c.pieces = pieces <= 256 ? 1 : 2;
+  c.pieces = pieces <= threads ? 1 : 2;
   c.threads = ((pieces + c.pieces - 1) / c.pieces + 31) / 32 * 32;
-  c.ctas = std::max(1, 16 / (c.threads / 32));
+  c.ctas = std::max(1, warps / (c.threads / 32));
   const long long run = (long long)kSms * c.ctas, groups = (long long)D.B * D.G;
-  c.cpg = (int)std::max<long long>(1, std::min<long long>(D.gt, run / groups));
-  c.chunk = (D.gt + c.cpg - 1) / c.cpg;
+  // chunks per group: the number whose rounds of CTAs take least, in rows (a chunk's beginning and end are worth about eight)
+  long long least = INT64_MAX;
+  c.chunk = D.gt;
+  for (int rounds = 1; rounds <= 4; ++rounds) {
+    const long long n = std::max<long long>(1, std::min<long long>(D.gt, rounds * run / groups)), rows = (D.gt + n - 1) / n;
+    const long long cost = ((groups * ((D.gt + rows - 1) / rows) + run - 1) / run) * (rows + 8);
+    if (cost < least) { least = cost; c.chunk = (int)rows; }
+  }
   c.cpg = (D.gt + c.chunk - 1) / c.chunk;
   c.chunks = groups * c.cpg;
   return c;
@@ -674,7 +683,7 @@ struct Scratch { float *part, *by_group; Guards guards; size_t bytes; };
 static Scratch scratch_of(const Dims& D, void* ws) {
   Carver c(ws);
   Scratch s;
-  s.part = c.take<float>((size_t)cut_of(D).chunks * 3 * D.C);
+  s.part = c.take<float>((size_t)cut_of(D, kBwdWarps, kBwdThreads).chunks * 3 * D.C);
   s.by_group = c.take<float>((size_t)D.B * D.G * 3 * D.C);
   s.guards = c.guards;
   s.bytes = c.total();
@@ -683,22 +692,19 @@ static Scratch scratch_of(const Dims& D, void* ws) {
 
 template <typename TS, typename T>
 static int go_fwd(const Dims& D, Params& p, cudaStream_t st) {
-  p.wpr = 1;
-  while (p.wpr < kFwdWarps && p.pieces > 32 * p.wpr * kFwdPieces) p.wpr *= 2;
-  const int per = (p.pieces + 32 * p.wpr - 1) / (32 * p.wpr);
-  p.groups = std::min(kFwdWarps / p.wpr, p.rows);
-  auto go = [&](auto pieces) {
-    constexpr int P = decltype(pieces)::value;
-    // as many CTAs as run at a time: they share the rows evenly
-    const long long ctas = std::min<long long>(((long long)p.rows + p.groups - 1) / p.groups, (long long)fwd_ctas(P) * sm_count());
-    launch_kernel(norm_fwd_kernel<TS, T, P>, (unsigned)ctas, 32 * p.wpr * p.groups, 0, st, p);
+  const Cut c = cut_of(D, kFwdWarps, kFwdThreads);
+  p.cpg = c.cpg; p.chunk = c.chunk;
+  const size_t bytes = align_up((size_t)p.C * (sizeof(TS) + (p.y.p ? sizeof(T) : 0)), 128), parts = (size_t)c.threads * sizeof(float2);
+  p.batch = (int)std::min<size_t>(c.pieces == 1 ? 4 : 2, std::max<size_t>(1, kSmemMost / c.ctas / (2 * bytes + parts)));
+  auto go = [&](auto kernel) -> int {
+    VMOBA_CUDA_OK(allow_smem(kernel, kSmemMost));
+    launch_kernel(kernel, (unsigned)c.chunks, c.threads, p.batch * (2 * bytes + parts), st, p);
+    VMOBA_LAUNCH_OK(1);
+    return VMOBA_OK;
   };
-  if (per <= 1) go(std::integral_constant<int, 1>{});
-  else if (per == 2) go(std::integral_constant<int, 2>{});
-  else if (per == 3) go(std::integral_constant<int, 3>{});
-  else go(std::integral_constant<int, 4>{});
-  VMOBA_LAUNCH_OK(1);
-  return VMOBA_OK;
+  const bool post = p.y.p && p.post != VMOBA_NORM_NONE;
+  if (c.pieces == 1) return post ? go(norm_fwd_kernel<TS, T, 1, true>) : go(norm_fwd_kernel<TS, T, 1, false>);
+  return post ? go(norm_fwd_kernel<TS, T, 2, true>) : go(norm_fwd_kernel<TS, T, 2, false>);
 }
 template <typename TS, typename T>
 static int go_bwd(const Cut& c, Params& p, cudaStream_t st) {
@@ -709,7 +715,7 @@ static int go_bwd(const Cut& c, Params& p, cudaStream_t st) {
   };
   p.stage_dh = p.d_h.p && 2 * slot(true) <= (size_t)kSmemMost;
   const size_t bytes = slot(p.stage_dh != 0), parts = (size_t)c.threads * 2 * sizeof(float2);
-  p.batch = (int)std::min<size_t>(batch_rows(c.pieces), std::max<size_t>(1, kSmemMost / c.ctas / (2 * bytes + parts)));
+  p.batch = (int)std::min<size_t>(c.threads <= kBwdNarrow && c.pieces == 1 ? 4 : 2, std::max<size_t>(1, kSmemMost / c.ctas / (2 * bytes + parts)));
   auto go = [&](auto kernel) -> int {
     VMOBA_CUDA_OK(allow_smem(kernel, kSmemMost));
     launch_kernel(kernel, (unsigned)c.chunks, c.threads, p.batch * (2 * bytes + parts), st, p);
@@ -717,8 +723,9 @@ static int go_bwd(const Cut& c, Params& p, cudaStream_t st) {
     return VMOBA_OK;
   };
   const bool post = p.y.p && p.post != VMOBA_NORM_NONE;
-  if (c.pieces == 1) return post ? go(norm_bwd_kernel<TS, T, 1, true>) : go(norm_bwd_kernel<TS, T, 1, false>);
-  return post ? go(norm_bwd_kernel<TS, T, 2, true>) : go(norm_bwd_kernel<TS, T, 2, false>);
+  if (c.pieces == 2) return post ? go(norm_bwd_kernel<TS, T, 2, true, 512>) : go(norm_bwd_kernel<TS, T, 2, false, 512>);
+  if (c.threads <= kBwdNarrow) return post ? go(norm_bwd_kernel<TS, T, 1, true, kBwdNarrow>) : go(norm_bwd_kernel<TS, T, 1, false, kBwdNarrow>);
+  return post ? go(norm_bwd_kernel<TS, T, 1, true, kBwdThreads>) : go(norm_bwd_kernel<TS, T, 1, false, kBwdThreads>);
 }
 
 }  // namespace norm
@@ -733,7 +740,7 @@ extern "C" size_t vmoba_block_norm_workspace_bytes(const vmoba_norm_shape* shape
 
 extern "C" int vmoba_block_norm(const vmoba_norm_shape* shape, const vmoba_norm_params* params, const void* x, const int64_t x_strides[2],
                                 const void* y, const int64_t y_strides[2], void* h, const int64_t h_strides[2], void* out,
-                                const int64_t out_strides[2], void* stream) {
+                                const int64_t out_strides[2], int32_t* dev_status, void* stream) {
   norm::Dims D;
   if (int rc = norm::make_dims(shape, &D)) return rc;
   if (!params || !x || (!h && !out)) return VMOBA_ERR_ARG;
@@ -742,6 +749,7 @@ extern "C" int vmoba_block_norm(const vmoba_norm_shape* shape, const vmoba_norm_
       !norm::take(&p.y, y, y_strides, D, D.bf16, false) || !norm::take(&p.h, h, h_strides, D, D.stream_bf16, true) ||
       !norm::take(&p.out, out, out_strides, D, D.bf16, true))
     return VMOBA_ERR_ARG;
+  p.status = dev_status;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (!D.bf16) return norm::go_fwd<float, float>(D, p, st);
   return D.stream_bf16 ? norm::go_fwd<__nv_bfloat16, __nv_bfloat16>(D, p, st) : norm::go_fwd<float, __nv_bfloat16>(D, p, st);
@@ -771,7 +779,7 @@ extern "C" int vmoba_block_norm_bwd(const vmoba_norm_shape* shape, const vmoba_n
   const norm::Scratch s = norm::scratch_of(D, ws);
   if (ws_bytes < s.bytes) return VMOBA_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const norm::Cut cut = norm::cut_of(D);
+  const norm::Cut cut = norm::cut_of(D, norm::kBwdWarps, norm::kBwdThreads);
   const bool vectors = grads->weight || grads->bias || grads->post_weight;
   const bool rows = grads->gate || grads->scale || grads->shift;
   p.part = vectors || rows ? s.part : nullptr;
@@ -785,7 +793,7 @@ extern "C" int vmoba_block_norm_bwd(const vmoba_norm_shape* shape, const vmoba_n
     const int tiles = (D.C + 31) / 32;
     const long long ctas = (long long)D.B * D.G * tiles;
     if (ctas > INT32_MAX) return VMOBA_ERR_SHAPE;
-    const norm::Sums a{D.C, D.G, cut.cpg, tiles, s.part, vectors ? s.by_group : nullptr, p.weight, p.bias, p.post_weight, grads->gate,
+    const norm::GroupSums a{D.C, D.G, cut.cpg, tiles, s.part, vectors ? s.by_group : nullptr, p.weight, p.bias, p.post_weight, grads->gate,
                        grads->scale, grads->shift};
     launch_kernel(norm::group_sums_kernel, (unsigned)ctas, 256, 0, st, a);
     VMOBA_LAUNCH_OK(1);

@@ -98,6 +98,15 @@ __device__ __forceinline__ void load_vec(const float* p, float (&x)[V]) {
 #pragma unroll
   for (int i = 0; i < V; i += 4) { const float4 v = load4(p + i); x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w; }
 }
+// (of what no kernel of the call writes: these may move ahead of stores)
+template <int V>
+__device__ __forceinline__ void load_const(const float* p, float (&x)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; i += 4) {
+    const float4 v = __ldg(reinterpret_cast<const float4*>(p + i));
+    x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
+  }
+}
 template <int V>
 __device__ __forceinline__ void load_vec(const __nv_bfloat16* p, float (&x)[V]) {
   if constexpr (V == 8) {

@@ -404,6 +404,7 @@ int slices(long long tiles, int steps, int pairs) {
   return best;
 }
 
+constexpr int kPairs = 74;                   // of B200's SMs (a workspace's size goes by the shape alone)
 struct Plan { int steps, per, splits; long long tiles; };
 Plan plan_of(const Product& p) {
   const int cols = p.e.kind == kGated ? BN / 2 : BN;
@@ -411,7 +412,7 @@ Plan plan_of(const Product& p) {
   if (p.form == kColsCols) o.steps = p.a.B * ((p.a.S + BK - 1) / BK);
   else o.steps = (p.a.cols + BK - 1) / BK;
   o.tiles = (long long)((p.M + 2 * BM - 1) / (2 * BM)) * ((p.N + cols - 1) / cols);
-  o.splits = slices(o.tiles, o.steps, sm_count() / 2);
+  o.splits = slices(o.tiles, o.steps, kPairs);
   o.per = (o.steps + o.splits - 1) / o.splits;
   return o;
 }

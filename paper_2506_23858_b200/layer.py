@@ -391,7 +391,7 @@ class BlockNorm(_Rows):
         if out is None and h_out is None:
             raise ValueError("BlockNorm: out or h_out required")
         with _on(self.device):
-            vb.vmoba_block_norm(self.shape, params, x, xs, y, ys, h_out, hs, out, os_)
+            vb.vmoba_block_norm(self.shape, params, x, xs, y, ys, h_out, hs, out, os_, self.dev_status)
 
     def backward(self, d_out, h, dx_out, d_h=None, y=None, dy_out=None, gate=None, scale=None, shift=None, weight=None, bias=None,
                  post_weight=None):

@@ -120,7 +120,7 @@ def test_norm_refusals():
 
     def fwd(s, m=None, x=FAKE, xs=st, y=NULL, h=NULL, hs=st, out=FAKE, os_=st):
         m = vb.norm_params() if m is None else m
-        return lib.vmoba_block_norm(ctypes.byref(s), ctypes.byref(m), x, xs, y, st, h, hs, out, os_, NULL)
+        return lib.vmoba_block_norm(ctypes.byref(s), ctypes.byref(m), x, xs, y, st, h, hs, out, os_, NULL, NULL)
 
     rows = lambda at, *strides: vb.NormParams(at, None, None, pair(*strides))
     for kw in (dict(x=NULL), dict(out=NULL), dict(x=ODD), dict(xs=None), dict(xs=pair(16 * 64, 60)), dict(os_=pair(16 * 64, 0)), dict(h=FAKE, hs=pair(0, 64)),
