@@ -18,7 +18,7 @@ namespace tc {
 using namespace sm100;
 
 constexpr int BM = 128, BN = 256, BK = 64;   // per CTA: rows of the accumulator; columns; summed indices of a stage
-constexpr int STAGES = 5;
+constexpr int MOST_STAGES = 5;               // four where results leave by rows, whose residual needs the room (no slower)
 constexpr int HALF = 128 * BK * 2;           // bytes of one operand's half of a stage
 constexpr int PANEL = 64 * 128;              // MN-major: 64 places of the tile x 64 summed indices
 constexpr int THREADS = 384, EPI_WARPS = 8;
@@ -30,7 +30,7 @@ struct Args {
   int N;                                     // columns of out
   int steps, per, splits, items;             // stages of the summed index, of a slice; slices
   int a_inner, b_inner, step_inner;          // columns of a head; (kColsCols) stages per sample
-  FastDiv by_rows_tiles, by_tiles, by_group, by_a_inner, by_b_inner, by_step;
+  FastDiv by_rows_tiles, by_tiles, by_group, by_a_inner, by_b_inner, by_step, by_wide;
   float* part;                               // [slice][row][column of the sums]
   int wide;                                  // columns of the sums
   long long part_rows;
@@ -38,14 +38,20 @@ struct Args {
 };
 
 struct Shared {
-  uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drain;
+  uint64_t full[MOST_STAGES], empty[MOST_STAGES], acc_full[2], acc_empty[2], drain;
   uint32_t tmem;
   int abort;
 };
 constexpr int STAGE_BYTES = 2 * HALF;
 constexpr int TURN_BYTES = 32 * STAGE_W * 4;
-constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * TURN_BYTES + (int)sizeof(Shared);
-static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
+constexpr int AHEAD_BYTES = 32 * STAGE_W * 2; // a warp's residual of the box to come
+// How results leave: boxes written by TMA, or rows of lanes where gate, residual, another order of the rows or parts are in play.
+enum Store { kBoxes = 0, kRows = 1 };
+__host__ __device__ constexpr int stages_of(int store) { return store == kBoxes ? MOST_STAGES : MOST_STAGES - 1; }
+__host__ __device__ constexpr int smem_of(int store) {
+  return 1024 + stages_of(store) * STAGE_BYTES + EPI_WARPS * (TURN_BYTES + (store == kRows ? AHEAD_BYTES : 0)) + (int)sizeof(Shared);
+}
+static_assert(smem_of(kBoxes) <= 227 * 1024 && smem_of(kRows) <= 227 * 1024, "shared memory of a CTA");
 
 __device__ __forceinline__ uint32_t cta_rank() {
   uint32_t r;
@@ -61,8 +67,10 @@ __device__ __forceinline__ uint32_t first_cta(const uint64_t* bar) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(bar)));
   return r;
 }
+// (What it says is that TMEM has been read, which tcgen05.wait::ld has seen to: no wider scope than the CTA's, whose release would wait for the
+// thread's loads and stores under way.)
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 // Into this CTA's shared memory, completion counted by a barrier of either CTA.
 __device__ __forceinline__ void pair_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t cluster_bar, int x, int y, int z, int w) {
@@ -80,11 +88,24 @@ __device__ __forceinline__ void pair_mma(uint32_t d_tmem, uint32_t a_lo, uint32_
       "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(DESC_HI_SW128)
       : "memory");
 }
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap* map, const void* smem_src, int x, int y, int z, int w) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)),
+               "r"(smem_u32(smem_src)), "r"(x), "r"(y), "r"(z), "r"(w)
+               : "memory");
+}
 // Arrives at the barriers of both CTAs when all products issued so far are done.
 __device__ __forceinline__ void pair_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
                "h"((uint16_t)3)
                : "memory");
+}
+
+// u += eight packed bf16
+__device__ __forceinline__ void add_bf16x8(float (&u)[8], const uint4& v) {
+  add_bf16_pair(u[0], u[1], v.x);
+  add_bf16_pair(u[2], u[3], v.y);
+  add_bf16_pair(u[4], u[5], v.z);
+  add_bf16_pair(u[6], u[7], v.w);
 }
 
 struct Item {
@@ -104,15 +125,18 @@ __device__ __forceinline__ Item item_of(const Args& p, int i) {
   return {split, sample, (rt - sample * p.rows_tiles) * 2 * BM, col * COLS};
 }
 
-template <int FORM, int KIND>
+template <int FORM, int KIND, int STORE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
-    pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, Args p) {
+    pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmOut,
+                const __grid_constant__ CUtensorMap tmKept, const __grid_constant__ CUtensorMap tmKept2, Args p) {
   if (!grid_begin()) return;
   constexpr bool A_MN = FORM == kColsCols, B_MN = FORM != kRowsRows;
+  constexpr int STAGES = stages_of(STORE);
   extern __shared__ char smem_raw[];
   char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   char* turn = smem + STAGES * STAGE_BYTES;
-  Shared* sm = reinterpret_cast<Shared*>(turn + EPI_WARPS * TURN_BYTES);
+  char* ahead = turn + EPI_WARPS * TURN_BYTES;
+  Shared* sm = reinterpret_cast<Shared*>(ahead + (STORE == kRows ? EPI_WARPS * AHEAD_BYTES : 0));
   volatile int* abort_flag = &sm->abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cta_rank();
@@ -214,8 +238,102 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
           if (mbar_try_wait(&sm->drain, 0)) break;
       }
     }
-  } else if (warp >= 4) {
-    // ------------------------------------------------------------------ what becomes of the sums
+  } else if (warp >= 4 && STORE == kBoxes) {
+    // ------------------------------------------------------------------ sums to results, box by box: lane = row
+    const int quad = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
+    char* const mine = turn + (warp - 4) * TURN_BYTES;
+    const Epilogue& e = p.e;
+    constexpr int W = KIND == kGated ? 32 : 64, BOXES = 2;             // columns of a box; boxes of out per warp
+    constexpr int COLS = KIND == kGated ? BN / 2 : BN;
+    uint32_t n = 0, turns = 0;
+    for (int i = pair; i < p.items; i += pairs, ++n) {
+      const Item it = item_of<KIND>(p, i);
+      const int row = it.row + (int)rank * BM + quad * 32;             // first row of the warp in the sample
+      mbar_wait_warp(&sm->acc_full[n & 1], (n >> 1) & 1, abort_flag, p.status);
+      tc_fence_after();
+      // W numbers of the lane's row, packed, out through one of two buffers
+      auto emit = [&](const CUtensorMap* map, int inner, const FastDiv& by_inner, const float (&u)[W], int c) {
+        char* const buf = mine + (turns++ & 1) * (32 * 2 * W);
+        if (lane == 0) bulk_wait_group_read<1>();                      // (of the two stores before this one the first has been read)
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < W / 8; ++j) {
+          const int place = W == 64 ? j ^ (lane & 7) : j ^ ((lane >> 1) & 3);
+          *reinterpret_cast<uint4*>(buf + lane * (2 * W) + place * 16) =
+              make_uint4(pack_bf16(u[8 * j], u[8 * j + 1]), pack_bf16(u[8 * j + 2], u[8 * j + 3]), pack_bf16(u[8 * j + 4], u[8 * j + 5]),
+                         pack_bf16(u[8 * j + 6], u[8 * j + 7]));
+        }
+        fence_async_proxy();
+        __syncwarp();
+        if (lane == 0) {
+          if (row < p.Sm) {
+            const int z = by_inner.div(c);
+            tma_store_4d(map, buf, c - z * inner, row, z, it.sample);
+          }
+          bulk_commit_group();
+        }
+      };
+#pragma unroll
+      for (int ch = 0; ch < BOXES; ++ch) {
+        const int at = half * (COLS / 2) + ch * W, c = it.col + at;
+        if (c >= p.N) {                      // (uniform)
+          if (ch == BOXES - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(first_cta(&sm->acc_empty[n & 1]));
+          }
+          continue;
+        }
+        uint32_t v[64];
+        const uint32_t from = lanes + (n & 1) * BN + at;
+        tmem_ld32(from, *reinterpret_cast<uint32_t(*)[32]>(&v[0]));
+        tmem_ld32(KIND == kGated ? from + BN / 2 : from + 32, *reinterpret_cast<uint32_t(*)[32]>(&v[32]));
+        tmem_ld_wait();
+        if (ch == BOXES - 1) {               // the accumulator has been read
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_at(first_cta(&sm->acc_empty[n & 1]));
+        }
+        float u[W], w[W];                    // (w: gated)
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+          u[k] = __uint_as_float(v[k]);
+          if (KIND == kGated) w[k] = __uint_as_float(v[(32 + k) % 64]);
+        }
+        if constexpr (KIND != kPlain) {
+          using T = __nv_bfloat16;
+          auto add_bias = [&](float (&x)[W], const T* b) {             // (the same of all lanes; N is a multiple of 8)
+#pragma unroll
+            for (int j = 0; j < W; j += 8) {
+              if (c + j >= p.N) break;
+              float t[8];
+              load_vec<8>(b + c + j, t);
+#pragma unroll
+              for (int k = 0; k < 8; k += 2) add2(x[j + k], x[j + k + 1], x[j + k], x[j + k + 1], t[k], t[k + 1]);
+            }
+          };
+          if (e.bias) {
+            add_bias(u, static_cast<const T*>(e.bias));
+            if constexpr (KIND == kGated) add_bias(w, static_cast<const T*>(e.bias) + p.N);
+          }
+          if (e.kept) {
+            emit(&tmKept, p.wide, p.by_wide, u, c);
+            if constexpr (KIND == kGated) emit(&tmKept2, p.wide, p.by_wide, w, c);
+          }
+          if (e.act != VMOBA_ACT_NONE)
+#pragma unroll
+            for (int k = 0; k < W; ++k) u[k] = activate<false>(e.act, u[k]);
+          if constexpr (KIND == kGated)
+#pragma unroll
+            for (int k = 0; k < W; k += 2) mul2(u[k], u[k + 1], u[k], u[k + 1], w[k], w[k + 1]);
+        }
+        emit(&tmOut, e.inner, e.by_inner, u, c);
+      }
+    }
+    if (lane == 0) bulk_wait_group<0>();     // (the stores have been read from this CTA's memory and written before it exits)
+  } else if (warp >= 4 && STORE == kRows) {
+    // ------------------------------------------------------------------ sums to results by rows: gate, residual, order of the rows, parts
     using T = __nv_bfloat16;
     const int quad = warp & 3, half = (warp - 4) >> 2;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
@@ -226,63 +344,106 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     const int lr = lane / PER_ROW, lc = (lane % PER_ROW) * 8;
     // four floats at place c4 of a row of the turned tile: rows apart by their number, so that neither rows nor columns meet in a bank
     auto place = [&](int r, int c4) { return reinterpret_cast<float4*>(mine + r * STAGE_W + ((c4 ^ (r & 7)) << 2)); };
-    uint32_t n = 0;
-    for (int i = pair; i < p.items; i += pairs, ++n) {
-      const Item it = item_of<KIND>(p, i);
-      const int local = it.row + (int)rank * BM + quad * 32;       // first row of the warp in the sample
-      const int rows = p.Sm - local;                               // rows that there are
-      const long long first = (long long)it.sample * p.Sm + local;
-      // lane = row: its sample and token of out
-      int ob = 0, ot = -1;
-      if (lane < rows && !p.part) {
-        const int r = (int)first + lane;
-        ob = e.by_S.div(r);
-        ot = r - ob * e.S;
-        if (KIND != kPlain && e.perm) {
-          ot = __ldg(e.perm + ot);
-          if ((unsigned)ot >= (unsigned)e.S) ot = -1;
-        }
+    auto column = [&](int ch) { return KIND == kGated ? half * 64 + ch * 32 : half * 128 + ch * 64; };      // first column in the tile
+    // A tile as a warp sees it; lane = row: its sample, token of out and group; the row of the gate where all rows have the same (nearly always).
+    struct Place { Item it; int rows, b, t, g; long long first; const float* gate; };
+    auto tile_of = [&](int i) {
+      Place o;
+      o.it = item_of<KIND>(p, i);
+      const int local = o.it.row + (int)rank * BM + quad * 32;
+      o.rows = p.Sm - local;
+      o.first = (long long)o.it.sample * p.Sm + local;
+      o.b = o.g = 0;
+      o.t = -1;
+      o.gate = nullptr;
+      if (lane < o.rows && !p.part) {
+        const int r = (int)o.first + lane;
+        o.b = e.by_S.div(r);
+        o.t = r - o.b * e.S;
+        if (KIND != kPlain && e.perm) o.t = __ldg(e.perm + o.t);
       }
-      bool there = false;
-#pragma unroll 1
-      for (int ch = 0; ch < 2; ++ch) {
-        const int at = KIND == kGated ? half * 64 + ch * 32 : half * 128 + ch * 64;      // first column in the tile
-        const int c = it.col + at + lc;
-        const bool col_ok = c < p.N;
-        uint4 res[TURNS];
-        if (KIND != kPlain && e.residual && !p.part) {
+      return o;
+    };
+    auto settle = [&](Place& o) {            // (what hangs on the loaded place)
+      if (KIND == kPlain || p.part) return;
+      if ((unsigned)o.t >= (unsigned)e.S) o.t = -1;
+      if (!e.gate) return;
+      if (o.t >= 0) o.g = e.by_gate.div(o.t);
+      const unsigned some = __ballot_sync(0xffffffffu, o.t >= 0);
+      const int from = some ? __ffs(some) - 1 : 0;
+      const int b0 = __shfl_sync(0xffffffffu, o.b, from), g0 = __shfl_sync(0xffffffffu, o.g, from);
+      if (__all_sync(0xffffffffu, o.t < 0 || (o.b == b0 && o.g == g0))) o.gate = e.gate + b0 * e.gb + g0 * e.gg;
+    };
+    const bool onto = KIND != kPlain && e.residual && !p.part;
+    // What a box of columns needs from memory is asked for a box ahead: beside the operands' loads it takes microseconds, and loads come back
+    // in the order they were asked for.  So bias and gate of the next box and the places of the next tile's rows go ahead of the next box's
+    // residual, a row of which is asked for, into shared memory, when the last one there has been used.
+    uint4 bias_in[2];
+    char* const mine_ahead = ahead + (warp - 4) * AHEAD_BYTES + lane * 16;       // (16 bytes per row and lane)
+    float gate_in[8];
+    auto load_residual = [&](const Place& o, int ch, int q) {
+      const int c = o.it.col + column(ch) + lc;
+      const int b = __shfl_sync(0xffffffffu, o.b, q * ROWS + lr), t = __shfl_sync(0xffffffffu, o.t, q * ROWS + lr);
+      if (c < p.N && t >= 0)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(mine_ahead + q * 512)),
+                     "l"(static_cast<const T*>(e.residual) + b * e.rb + t * e.rt + c)
+                     : "memory");
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto load_columns = [&](const Place& o, int ch) {
+      const int c = o.it.col + column(ch) + lc;
+      if (KIND == kPlain || p.part || c >= p.N) return;
+      if (e.bias) {
+        bias_in[0] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(e.bias) + c));
+        if (KIND == kGated) bias_in[1] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(e.bias) + e.cols + c));
+      }
+      if (o.gate) load_const<8>(o.gate + c, gate_in);
+    };
+    uint32_t n = 0;
+    Place next = tile_of(pair);
+    settle(next);
+    load_columns(next, 0);
+    if (onto)
 #pragma unroll
-          for (int q = 0; q < TURNS; ++q) {
-            const int b = __shfl_sync(0xffffffffu, ob, q * ROWS + lr), t = __shfl_sync(0xffffffffu, ot, q * ROWS + lr);
-            res[q] = make_uint4(0u, 0u, 0u, 0u);
-            if (col_ok && t >= 0) res[q] = *reinterpret_cast<const uint4*>(static_cast<const T*>(e.residual) + b * e.rb + t * e.rt + c);
-          }
-        }
-        float bias[8] = {}, bias2[8] = {};
-        if (KIND != kPlain && e.bias && !p.part && col_ok) {
-          load_vec<8>(static_cast<const T*>(e.bias) + c, bias);
-          if (KIND == kGated) load_vec<8>(static_cast<const T*>(e.bias) + e.cols + c, bias2);
-        }
-        if (!there) {
+      for (int q = 0; q < TURNS; ++q) load_residual(next, 0, q);
+    for (int i = pair; i < p.items; i += pairs, ++n) {
+      const Place now = next;
+      const bool more = i + pairs < p.items;
+#pragma unroll
+      for (int ch = 0; ch < 2; ++ch) {
+        const int at = column(ch), c = now.it.col + at + lc;
+        const bool col_ok = c < p.N;
+        if (ch == 0) {
           mbar_wait_warp(&sm->acc_full[n & 1], (n >> 1) & 1, abort_flag, p.status);
           tc_fence_after();
-          there = true;
         }
-        {
-          uint32_t v[64];
-          const uint32_t from = lanes + (n & 1) * BN + at;
-          tmem_ld32(from, *reinterpret_cast<uint32_t(*)[32]>(&v[0]));
-          tmem_ld32(KIND == kGated ? from + BN / 2 : from + 32, *reinterpret_cast<uint32_t(*)[32]>(&v[32]));
+        const uint32_t from = lanes + (n & 1) * BN + at;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          uint32_t v[32];
+          tmem_ld32(x == 0 ? from : KIND == kGated ? from + BN / 2 : from + 32, v);
           tmem_ld_wait();
-          if (ch == 1) {                     // the accumulator has been read
+          if (x == 0) {
+            __syncwarp();                    // (the tile turned before has been read)
+          } else if (ch == 1) {              // the accumulator has been read
             tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_at(first_cta(&sm->acc_empty[n & 1]));
           }
-          __syncwarp();                      // (the tile turned before has been read)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) *reinterpret_cast<uint4*>(place(lane, j)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-          __syncwarp();
+          for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(place(lane, 8 * x + j)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        }
+        __syncwarp();
+        uint4 bias[2] = {bias_in[0], bias_in[1]};
+        float gate[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) gate[x] = gate_in[x];
+        if (ch == 0) {
+          load_columns(now, 1);
+          if (more) next = tile_of(i + pairs);
+        } else if (more) {
+          settle(next);
+          load_columns(next, 0);
         }
 #pragma unroll
         for (int q = 0; q < TURNS; ++q) {
@@ -300,47 +461,49 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             }
           }
           if (p.part) {
-            if (col_ok && r < rows) {
-              float* to = p.part + ((long long)it.split * p.part_rows + first + r) * p.wide + c;
+            if (col_ok && r < now.rows) {
+              float* to = p.part + ((long long)now.it.split * p.part_rows + now.first + r) * p.wide + c;
               store_vec<8>(to, u);
               if (KIND == kGated) store_vec<8>(to + p.N, w);
             }
             continue;
           }
-          const int b = __shfl_sync(0xffffffffu, ob, r), t = __shfl_sync(0xffffffffu, ot, r);
-          if (!col_ok || r >= rows) continue;
-          if constexpr (KIND != kPlain) {
+          if constexpr (KIND != kPlain) {    // (plain sums come here in parts alone)
+            if (onto) asm volatile("cp.async.wait_group %0;" ::"n"(TURNS - 1) : "memory");      // (the oldest of TURNS rows is here)
+            const int b = __shfl_sync(0xffffffffu, now.b, r), t = __shfl_sync(0xffffffffu, now.t, r), g = __shfl_sync(0xffffffffu, now.g, r);
+            if (col_ok && r < now.rows) {
+              if (e.bias) {
+                add_bf16x8(u, bias[0]);
+                if (KIND == kGated) add_bf16x8(w, bias[1]);
+              }
+              if (e.kept) {
+                T* kept = static_cast<T*>(e.kept) + (now.first + r) * p.wide + c;
+                store_vec<8>(kept, u);
+                if (KIND == kGated) store_vec<8>(kept + p.N, w);
+              }
+              if (e.act != VMOBA_ACT_NONE)
 #pragma unroll
-            for (int x = 0; x < 8; ++x) u[x] += bias[x];
-            if (KIND == kGated) {
+                for (int x = 0; x < 8; ++x) u[x] = activate<false>(e.act, u[x]);
+              if (KIND == kGated)
 #pragma unroll
-              for (int x = 0; x < 8; ++x) w[x] += bias2[x];
+                for (int x = 0; x < 8; x += 2) mul2(u[x], u[x + 1], u[x], u[x + 1], w[x], w[x + 1]);
+              if (t >= 0) {
+                if (e.gate) {
+                  if (!now.gate) load_const<8>(e.gate + b * e.gb + g * e.gg + c, gate);
+#pragma unroll
+                  for (int x = 0; x < 8; x += 2) mul2(u[x], u[x + 1], u[x], u[x + 1], gate[x], gate[x + 1]);
+                }
+                if (e.residual) add_bf16x8(u, *reinterpret_cast<const uint4*>(mine_ahead + q * 512));
+                store_vec<8>(static_cast<T*>(e.out) + b * e.ob + t * e.ot + c, u);
+              }
             }
-            if (e.kept) {
-              T* kept = static_cast<T*>(e.kept) + (first + r) * p.wide + c;
-              store_vec<8>(kept, u);
-              if (KIND == kGated) store_vec<8>(kept + p.N, w);
-            }
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              u[x] = activate<false>(e.act, u[x]);
-              if (KIND == kGated) u[x] *= w[x];
-            }
-            if (t < 0) continue;
-            if (e.gate) {
-              float g[8];
-              load_vec<8>(e.gate + b * e.gb + e.by_gate.div(t) * e.gg + c, g);
-#pragma unroll
-              for (int x = 0; x < 8; ++x) u[x] *= g[x];
-            }
-            if (e.residual) {
-              const uint32_t rw[4] = {res[q].x, res[q].y, res[q].z, res[q].w};
-#pragma unroll
-              for (int x = 0; x < 4; ++x) add_bf16_pair(u[2 * x], u[2 * x + 1], rw[x]);
+            __syncwarp();
+            if (onto) {
+              if (ch == 0) load_residual(now, 1, q);
+              else if (more) load_residual(next, 0, q);
+              else asm volatile("cp.async.commit_group;" ::: "memory");
             }
           }
-          const int h = e.inner == e.cols ? 0 : e.by_inner.div(c);
-          store_vec<8>(static_cast<T*>(e.out) + b * e.ob + t * e.ot + h * e.oh + (c - h * e.inner), u);
         }
       }
     }
@@ -375,13 +538,17 @@ __global__ void __launch_bounds__(256) join_kernel(Args p, FastDiv by_vecs, int 
   }
 }
 
-// [inner, S, heads, B] of a matrix, boxes of 64 columns x `rows` rows.
-bool map_of(CUtensorMap* map, const Matrix& m, int rows) {
-  const uint64_t n[4] = {(uint64_t)m.inner, (uint64_t)m.S, (uint64_t)(m.cols / m.inner), (uint64_t)m.B};
+// [inner, S, heads, B] of a matrix, boxes of `cols` columns (64, 32) x `rows` rows.
+bool map_of(CUtensorMap* map, const Matrix& m, int rows, int cols = 64) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const cuuint64_t n[4] = {(cuuint64_t)m.inner, (cuuint64_t)m.S, (cuuint64_t)(m.cols / m.inner), (cuuint64_t)m.B};
   // (strides of dimensions of one address nothing, but have to be multiples of 16 bytes)
-  const uint64_t stride[4] = {1, m.S > 1 ? (uint64_t)m.st : 8, m.cols > m.inner ? (uint64_t)m.sh : 8, m.B > 1 ? (uint64_t)m.sb : 8};
-  const uint32_t box[4] = {64, (uint32_t)rows, 1, 1};
-  return make_tmap_bf16_strided(map, m.p, 4, n, stride, box);
+  const cuuint64_t stride[3] = {m.S > 1 ? (cuuint64_t)m.st * 2 : 16, m.cols > m.inner ? (cuuint64_t)m.sh * 2 : 16, m.B > 1 ? (cuuint64_t)m.sb * 2 : 16};
+  const cuuint32_t box[4] = {(cuuint32_t)cols, (cuuint32_t)rows, 1, 1}, one[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(m.p), n, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // Samples that follow one another at the tokens' distance are one.
 Matrix folded(Matrix m) {
@@ -417,11 +584,14 @@ Plan plan_of(const Product& p) {
   return o;
 }
 
+struct Maps { CUtensorMap a, b, out, kept, kept2; };
+
 template <int FORM, int KIND>
-int launch(const Args& a, const CUtensorMap& tmA, const CUtensorMap& tmB, cudaStream_t st) {
-  auto kernel = pair_kernel<FORM, KIND>;
-  VMOBA_CUDA_OK(allow_smem(kernel, SMEM_BYTES));
-  launch_kernel(kernel, 2 * (unsigned)std::min(a.items, std::max(1, sm_count() / 2)), THREADS, SMEM_BYTES, st, tmA, tmB, a);
+int launch(const Args& a, const Maps& m, bool boxes, cudaStream_t st) {
+  auto kernel = boxes ? pair_kernel<FORM, KIND, kBoxes> : pair_kernel<FORM, KIND, kRows>;
+  const int smem = smem_of(boxes ? kBoxes : kRows);
+  VMOBA_CUDA_OK(allow_smem(kernel, smem));
+  launch_kernel(kernel, 2 * (unsigned)std::min(a.items, std::max(1, sm_count() / 2)), THREADS, (size_t)smem, st, m.a, m.b, m.out, m.kept, m.kept2, a);
   VMOBA_LAUNCH_OK(1);
   if (a.splits > 1) {
     const long long vecs = a.N / 8, total = a.part_rows * vecs;
@@ -462,11 +632,21 @@ int tc_product(const Product& p, float* scratch, cudaStream_t st) {
       if (a.splits == 1) a.part = nullptr;
     }
     a.step_inner = (ma.S + BK - 1) / BK;
-    a.Sm = p.M;
-  } else {
-    ma = folded(ma);
+  }
+  // how results leave, and (boxes) whether they lie so that all samples' rows can be taken for one's
+  const bool boxes = !a.part && !p.e.gate && !p.e.residual && !p.e.perm;
+  const bool gated = p.e.kind == kGated;
+  Matrix out{p.e.out, p.M / p.e.S, p.e.S, p.e.cols, p.e.inner, p.e.ob, p.e.ot, p.e.oh};
+  Matrix kept{p.e.kept, out.B, out.S, a.wide, a.wide, (long long)out.S * a.wide, a.wide, 0};
+  if (p.form != kColsCols) {
+    if (!boxes || folded(out).B == 1) {
+      ma = folded(ma);
+      if (ma.B == 1) { out = folded(out); kept = folded(kept); }
+    }
     a.step_inner = 1;
     a.Sm = ma.S;
+  } else {
+    a.Sm = p.M;
   }
   a.rows_tiles = (a.Sm + 2 * BM - 1) / (2 * BM);
   a.row_tiles = a.rows_tiles * (p.form == kColsCols ? 1 : ma.B);
@@ -480,11 +660,22 @@ int tc_product(const Product& p, float* scratch, cudaStream_t st) {
   a.by_group = FastDiv((unsigned)(8 * a.col_tiles));
   a.by_a_inner = FastDiv((unsigned)ma.inner); a.by_b_inner = FastDiv((unsigned)mb.inner);
   a.by_step = FastDiv((unsigned)a.step_inner);
-  CUtensorMap tmA, tmB;
-  if (!map_of(&tmA, ma, p.form == kColsCols ? BK : BM) || !map_of(&tmB, mb, p.form == kRowsRows ? 128 : BK)) return VMOBA_ERR_CUDA;
-  if (p.form == kColsCols) return launch<kColsCols, kPlain>(a, tmA, tmB, st);
-  if (p.form == kRowsCols) return launch<kRowsCols, kPlain>(a, tmA, tmB, st);
-  return p.e.kind == kGated ? launch<kRowsRows, kGated>(a, tmA, tmB, st) : launch<kRowsRows, kForward>(a, tmA, tmB, st);
+  a.by_wide = FastDiv((unsigned)a.wide);
+  Maps m{};
+  if (!map_of(&m.a, ma, p.form == kColsCols ? BK : BM) || !map_of(&m.b, mb, p.form == kRowsRows ? 128 : BK)) return VMOBA_ERR_CUDA;
+  if (boxes) {
+    const int box = gated ? 32 : 64;
+    if (!map_of(&m.out, out, 32, box)) return VMOBA_ERR_CUDA;
+    if (kept.p) {                            // (gated: the halves on their own, so that a box of the first ends where it does)
+      Matrix first = kept, second = kept;
+      first.cols = first.inner = second.cols = second.inner = p.N;
+      second.p = static_cast<char*>(p.e.kept) + 2ll * p.N;
+      if (!map_of(&m.kept, first, 32, box) || (gated && !map_of(&m.kept2, second, 32, box))) return VMOBA_ERR_CUDA;
+    }
+  }
+  if (p.form == kColsCols) return launch<kColsCols, kPlain>(a, m, boxes, st);
+  if (p.form == kRowsCols) return launch<kRowsCols, kPlain>(a, m, boxes, st);
+  return gated ? launch<kRowsRows, kGated>(a, m, boxes, st) : launch<kRowsRows, kForward>(a, m, boxes, st);
 }
 
 }  // namespace linear
