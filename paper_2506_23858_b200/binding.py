@@ -6,6 +6,7 @@ missing, or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 
@@ -484,7 +485,9 @@ def vmoba_range_attn_bwd(shape, plan, q, qs, k, ks, v, vs, o, os_, o_resid, lse,
 _I64x2 = ctypes.c_int64 * 2
 
 
+@functools.lru_cache(maxsize=1024)
 def _pair(st):
+    """Strides (a tuple) as an argument; the arrays are only read."""
     return None if st is None else _I64x2(*st)
 
 
@@ -531,7 +534,7 @@ def block_norm_workspace_bytes(shape) -> int:
 
 def norm_params(gate=None, gate_strides=(0, 0), scale=None, scale_strides=(0, 0), shift=None, shift_strides=(0, 0), weight=None, bias=None,
                 post_weight=None) -> NormParams:
-    return NormParams(_ptr(gate), _ptr(scale), _ptr(shift), _I64x2(*gate_strides), _I64x2(*scale_strides), _I64x2(*shift_strides), _ptr(weight),
+    return NormParams(_ptr(gate), _ptr(scale), _ptr(shift), _pair(gate_strides), _pair(scale_strides), _pair(shift_strides), _ptr(weight),
                       _ptr(bias), _ptr(post_weight))
 
 

@@ -220,8 +220,11 @@ int sum_chunks(const float* part, int cols, int groups, int per, void* out, bool
   return VMOBA_OK;
 }
 
-size_t product_scratch(const Product& p) { return p.bf16 ? tc_scratch(p) : 0; }
-int run_product(const Product& p, float* scratch, cudaStream_t st) { return p.bf16 ? tc_product(p, scratch, st) : simt_product(p, st); }
+size_t product_scratch(const Product& p) { return p.bf16 && !few_takes(p) ? tc_scratch(p) : 0; }
+int run_product(const Product& p, float* scratch, cudaStream_t st) {
+  if (!p.bf16) return simt_product(p, st);
+  return few_takes(p) ? few_product(p, st) : tc_product(p, scratch, st);
+}
 
 namespace {
 

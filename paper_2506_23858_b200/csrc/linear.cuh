@@ -61,10 +61,12 @@ struct Product {
 size_t product_scratch(const Product& p);
 int run_product(const Product& p, float* scratch, cudaStream_t st);
 
-// fp32 (linear_simt.cu) and bf16 (linear_tc.cu).
+// fp32 (linear_simt.cu), bf16 (linear_tc.cu), and of those the products of a few tokens with a weight (linear_few.cu).
 int simt_product(const Product& p, cudaStream_t st);
 size_t tc_scratch(const Product& p);
 int tc_product(const Product& p, float* scratch, cudaStream_t st);
+bool few_takes(const Product& p);
+int few_product(const Product& p, cudaStream_t st);
 
 // out[g][c] = sum over the `per` chunks of group g of part[chunk][c], by rows of `cols` floats; of the layer's type (linear.cu).
 int sum_chunks(const float* part, int cols, int groups, int per, void* out, bool bf16, cudaStream_t st);

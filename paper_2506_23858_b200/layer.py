@@ -176,37 +176,39 @@ class _Rows:
 
     def _rows(self, x, channels, dtype, what, written=False):
         """x as the kernels can address it (an input that they cannot is copied) and its strides (batch, token)."""
-        s = self.shape
-        if x.shape != (s.B, s.S, channels) or x.dtype is not dtype or x.device != self.device:
-            raise ValueError(f"{type(self).__name__}: {what} has to be {dtype} [{s.B}, {s.S}, {channels}] on {self.device}")
+        size, dense = self._sizes.get(channels) or self._sizes.setdefault(
+            channels, (torch.Size((self.shape.B, self.shape.S, channels)), (self.shape.S * channels, channels)))
+        if x.shape != size or x.dtype is not dtype or x.device != self.device:
+            raise ValueError(f"{type(self).__name__}: {what} has to be {dtype} {list(size)} on {self.device}")
         if x.is_contiguous() and x.data_ptr() % 16 == 0:
-            return x, (s.S * channels, channels)
+            return x, dense
         st, per = x.stride(), 16 // x.element_size()
-        if x.stride(2) == 1 and x.data_ptr() % 16 == 0 and all(n == 1 or (i % per == 0 and channels <= i < 2 ** 38) for n, i in zip(x.shape[:2], st)):
+        if x.stride(2) == 1 and x.data_ptr() % 16 == 0 and all(n == 1 or (i % per == 0 and channels <= i < 2 ** 38) for n, i in zip(size, st[:2])):
             return x, st[:2]
         if written:
             raise ValueError(f"{type(self).__name__}: {what} needs 16-byte rows on 16-byte boundaries that do not share memory")
-        x = torch.empty(x.shape, dtype=dtype, device=x.device).copy_(x)
-        return x, (s.S * channels, channels)
+        x = torch.empty(size, dtype=dtype, device=x.device).copy_(x)
+        return x, dense
 
     def _groups(self, g, channels, what):
         """Rows of a gate, scale or shift [B (or 1), groups, channels] and their strides (batch, group)."""
         if g is None:
             return None, (0, 0)
-        s = self.shape
-        if g.dim() != 3 or g.shape[0] not in (1, s.B) or g.shape[1:] != (s.groups, channels) or g.dtype is not _F32 or g.device != self.device:
-            raise ValueError(f"{type(self).__name__}: {what} has to be fp32 [{s.B} or 1, {s.groups}, {channels}] on {self.device}")
-        st = [0 if n == 1 else i for n, i in zip(g.shape[:2], g.stride())]
-        if g.stride(2) != 1 or g.data_ptr() % 16 or any(i % 4 or (i != 0 and not channels <= i < 2 ** 38) for i in st):
-            g = torch.empty(g.shape, dtype=_F32, device=g.device).copy_(g)
-            st = [0 if n == 1 else i for n, i in zip(g.shape[:2], g.stride())]
-        return g, st
+        n, s = g.shape, self.shape
+        if len(n) != 3 or (n[0] != s.B and n[0] != 1) or n[1] != self._n_groups or n[2] != channels or g.dtype is not _F32 or g.device != self.device:
+            raise ValueError(f"{type(self).__name__}: {what} has to be fp32 [{s.B} or 1, {self._n_groups}, {channels}] on {self.device}")
+        st = g.stride()
+        sb, sg = 0 if n[0] == 1 else st[0], 0 if n[1] == 1 else st[1]
+        if st[2] != 1 or g.data_ptr() % 16 or sb % 4 or sg % 4 or (sb and not channels <= sb < 2 ** 38) or (sg and not channels <= sg < 2 ** 38):
+            g = torch.empty(n, dtype=_F32, device=g.device).copy_(g)
+            sb, sg = 0 if n[0] == 1 else n[1] * channels, 0 if n[1] == 1 else channels
+        return g, (sb, sg)
 
     def _dense(self, x, shape, dtype, what):
         """A contiguous tensor of this shape; one that begins elsewhere than on 16 bytes is copied."""
         if x is None:
             return None
-        if tuple(x.shape) != tuple(shape) or x.dtype is not dtype or x.device != self.device or not x.is_contiguous():
+        if x.shape != shape or x.dtype is not dtype or x.device != self.device or not x.is_contiguous():
             raise ValueError(f"{type(self).__name__}: {what} has to be {dtype} {list(shape)} on {self.device}, contiguous")
         return x if x.data_ptr() % 16 == 0 else torch.empty_like(x).copy_(x)
 
@@ -217,6 +219,17 @@ class _Rows:
 
     def _new(self, shape, dtype, wanted=True):
         return torch.empty(shape, dtype=dtype, device=self.device) if wanted else None
+
+    def _start(self, shape, device):
+        self.shape, self.device = shape, _cuda_device(device, type(self).__name__)
+        self._n_groups, self._sizes = shape.groups, {}
+        self.dtype = torch_dtype(shape)
+        self.dev_status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._nothing = torch.empty(256, dtype=torch.uint8, device=self.device)      # what calls take that need no scratch
+
+    def _scratch(self, n):
+        """A call's own, so that calls on any streams and in any graphs can be under way at the same time."""
+        return self._nothing if n <= 256 else torch.empty(n, dtype=torch.uint8, device=self.device)
 
     def check_status(self):
         code = int(self.dev_status.item())
@@ -240,13 +253,11 @@ class Linear(_Rows):
     the device's status), so that any number of streams and captured graphs can use it at the same time."""
 
     def __init__(self, shape, device="cuda"):
-        self.shape, self.device = shape, _cuda_device(device, "Linear")
+        self._start(shape, device)
         self._ws = vb.linear_workspace_bytes(shape)
         if self._ws == 0:
             raise ValueError("Linear: channels are multiples of 8, heads of 64 or 128 channels; shape out of range")
         self._ws_bwd = vb.linear_workspace_bytes(shape, True)
-        self.dtype = torch_dtype(shape)
-        self.dev_status = torch.zeros(1, dtype=torch.int32, device=self.device)
 
     def _input(self, x, what, written=False):
         s = self.shape
@@ -273,7 +284,7 @@ class Linear(_Rows):
         kept = self._written(kept, (s.B, s.S, s.wide), dt, "kept")
         with _on(self.device):
             vb.vmoba_linear(s, x, xs, weight, bias, gate, gs, residual, rs, out, os_, kept, self._perm(perm), self.dev_status,
-                            self._new(self._ws, torch.uint8))
+                            self._scratch(self._ws))
 
     def backward(self, d_out, x, weight, dx_out, kept=None, gate=None, perm=None, with_weight=True, with_bias=False):
         """Gradients of forward(), whose residual's is d_out: writes dx_out (the order of x; None: not wanted), returns those of weight, bias
@@ -292,7 +303,7 @@ class Linear(_Rows):
         dg = self._new((s.B, s.groups, s.n_out), _F32, gate is not None)
         with _on(self.device):
             vb.vmoba_linear_bwd(s, d_out, dos, x, xs, weight, kept, gate, gs, dx_out, dxs, dw, db, dg, self._perm(perm), self.dev_status,
-                                self._new(self._ws_bwd, torch.uint8))
+                                self._scratch(self._ws_bwd))
         return dw, db, dg
 
 
@@ -301,13 +312,11 @@ class FeedForward(_Rows):
     h = act(first half of the product) * second half.  Holds no tensors of a call (but a word for the device's status)."""
 
     def __init__(self, B, S, channels, hidden, dtype="bf16", activation="gelu", gated=False, gate_tokens=0, device="cuda"):
-        self.shape, self.device = vb.make_linear_shape(B, S, channels, hidden, dtype, activation, gated, 0, gate_tokens), _cuda_device(device, "FeedForward")
+        self._start(vb.make_linear_shape(B, S, channels, hidden, dtype, activation, gated, 0, gate_tokens), device)
         self._ws = vb.ffn_workspace_bytes(self.shape)
         if self._ws == 0:
             raise ValueError("FeedForward: channels are multiples of 8; shape out of range")
         self._ws_bwd = vb.ffn_workspace_bytes(self.shape, True)
-        self.dtype = torch_dtype(self.shape)
-        self.dev_status = torch.zeros(1, dtype=torch.int32, device=self.device)
 
     def keep(self):
         """Tensors for forward() to leave in what backward() needs: the products ahead of the activation and of the gate."""
@@ -331,7 +340,7 @@ class FeedForward(_Rows):
         up, down = self._written(up, (s.B, s.S, s.wide), dt, "kept"), self._written(down, (s.B, s.S, s.n_in), dt, "kept")
         with _on(self.device):
             vb.vmoba_ffn(s, x, xs, w_up, b_up, w_down, b_down, gate, gs, residual, rs, out, os_, up, down, self.dev_status,
-                         self._new(self._ws, torch.uint8))
+                         self._scratch(self._ws))
 
     def backward(self, d_out, x, w_up, w_down, kept, dx_out, gate=None, with_weights=True, with_bias=False):
         """Gradients of forward(), whose residual's is d_out: writes dx_out (None: not wanted), returns those of w_up, w_down, b_up, b_down and
@@ -351,7 +360,7 @@ class FeedForward(_Rows):
         dg = self._new((s.B, s.groups, s.n_in), _F32, gate is not None)
         with _on(self.device):
             vb.vmoba_ffn_bwd(s, d_out, dos, x, xs, w_up, w_down, up, down, gate, gs, dx_out, dxs, dwu, dbu, dwd, dbd, dg, self.dev_status,
-                             self._new(self._ws_bwd, torch.uint8))
+                             self._scratch(self._ws_bwd))
         return dwu, dwd, dbu, dbd, dg
 
 
@@ -363,20 +372,18 @@ class BlockNorm(_Rows):
     left out.  Holds no tensors of a call (but a word for the device's status)."""
 
     def __init__(self, shape, device="cuda"):
-        self.shape, self.device = shape, _cuda_device(device, "BlockNorm")
+        self._start(shape, device)
         self._ws = vb.block_norm_workspace_bytes(shape)
         if self._ws == 0:
             raise ValueError("BlockNorm: channels are multiples of 8 up to 8192, fp32 branches go with fp32 streams; shape out of range")
-        self.dev_status = torch.zeros(1, dtype=torch.int32, device=self.device)
-        self.dtype = torch_dtype(shape)
         self.stream_dtype = _BF16 if shape.stream_dtype == vb.BF16 else _F32
 
     def _params(self, gate, scale, shift, weight, bias, post_weight):
         C = self.shape.C
         (gate, gs), (scale, ss), (shift, hs) = (self._groups(g, C, n) for g, n in ((gate, "gate"), (scale, "scale"), (shift, "shift")))
         weight, bias, post_weight = (self._dense(v, (C,), _F32, n) for v, n in ((weight, "weight"), (bias, "bias"), (post_weight, "post_weight")))
-        held = (gate, scale, shift, weight, bias, post_weight)      # (copies live until the launch)
-        return vb.norm_params(gate, gs, scale, ss, shift, hs, weight, bias, post_weight), held
+        # (with what the pointers are of: copies live until the launch)
+        return vb.norm_params(gate, gs, scale, ss, shift, hs, weight, bias, post_weight), (gate, scale, shift, weight, bias, post_weight)
 
     def _opt(self, x, dtype, what, written=False):
         return (None, None) if x is None else self._rows(x, self.shape.C, dtype, what, written)
@@ -412,7 +419,7 @@ class BlockNorm(_Rows):
         grads = {n: self._new((s.B, s.groups, C) if n in ("gate", "scale", "shift") else (C,), _F32) for n, t in there.items() if t is not None}
         with _on(self.device):
             vb.vmoba_block_norm_bwd(s, params, d_out, dos, h, hs, d_h, dhs, y, ys, dx_out, dxs, dy_out, dys, grads, self.dev_status,
-                                    self._new(self._ws, torch.uint8))
+                                    self._scratch(self._ws))
         return {"d" + n: grads.get(n) for n in there}
 
 
