@@ -478,8 +478,8 @@ int vmoba_ffn(const vmoba_linear_shape* shape, const void* x, const int64_t x_st
               const void* residual_or_null, const int64_t residual_strides[2], void* out, const int64_t out_strides[2],
               void* kept_up_or_null, void* kept_down_or_null, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
 
-/* Its gradients; what is not wanted may be NULL.  kept_down is read for dgate alone.  The gradient of h is rounded to the block's type
- * once (between the two products it stands between), and db_up is the sum of what follows from it. */
+/* Its gradients; what is not wanted may be NULL.  kept_down is read for dgate alone.  h and the gradient of the first product are rounded to the
+ * block's type, for the products they are in; db_up and dgate are sums of unrounded values.  The results repeat bit for bit. */
 int vmoba_ffn_bwd(const vmoba_linear_shape* shape, const void* d_out, const int64_t d_out_strides[2], const void* x,
                   const int64_t x_strides[2], const void* w_up, const void* w_down, const void* kept_up, const void* kept_down_or_null,
                   const float* gate_or_null, const int64_t gate_strides[2], void* dx_or_null, const int64_t dx_strides[2],

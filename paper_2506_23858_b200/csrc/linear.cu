@@ -80,6 +80,7 @@ struct Prep {
   long long gb, gg;
   const int* inv;                            // place in the order of x of every token of d_out
   void* du;                                  // as kept
+  void* du_low;                              // what du's rounding left (not with kept)
   void* y;                                   // act(kept) again, [rows, cols]
   float* part_b;                             // [chunk][cols or 2 cols]
   float* part_g;                             // [chunk][cols]
@@ -138,6 +139,11 @@ __global__ void __launch_bounds__(256) prep_kernel(Prep p) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) sb[i] += d[i];
       if (p.du) store_vec<8>(static_cast<T*>(p.du) + r * wide + c, d);
+      if (p.du_low) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] -= to_f32<T>(from_f32<T>(d[i]));
+        store_vec<8>(static_cast<T*>(p.du_low) + r * wide + c, d);
+      }
     }
   }
   // the eight warps' sums, one set after another
@@ -233,6 +239,7 @@ Product product(const Dims& D, Form form, const Matrix& a, const Matrix& b, int 
   Product p{};
   p.form = form; p.a = a; p.b = b; p.M = M; p.N = N;
   p.bf16 = D.dtype == VMOBA_BF16;
+  p.planes = 1;
   p.status = status;
   return p;
 }
@@ -252,6 +259,16 @@ Product dx_product(const Dims& D, const Matrix& du, const void* w, const Matrix&
   set_out(&p.e, dx);
   return p;
 }
+// The gradient of the product of the layer ahead (`up`, whose output this layer's input is) from du: through this layer's weight and that
+// layer's activation.
+Product slope_product(const Dims& D, const Dims& up, const Matrix& du, const void* w, const void* kept, const Matrix& d_up, int32_t* status) {
+  Product p = dx_product(D, du, w, d_up, status);
+  p.e.kind = up.gated ? kSlopeGated : kSlope;
+  p.e.act = up.act;
+  p.e.cols = up.out;
+  p.e.kept = const_cast<void*>(kept);
+  return p;
+}
 Product dw_product(const Dims& D, const Matrix& du, const Matrix& x, void* dw, int32_t* status) {
   Product p = product(D, kColsCols, du, x, D.wide, D.in, status);
   set_out(&p.e, dense(dw, D.wide, D.in));
@@ -261,9 +278,15 @@ Product dw_product(const Dims& D, const Matrix& du, const Matrix& x, void* dw, i
 size_t forward_scratch(const Dims& D) {
   return product_scratch(forward_product(D, tokens(nullptr, D, D.in), nullptr, tokens(nullptr, D, D.out), nullptr));
 }
-size_t gradient_scratch(const Dims& D) {
+size_t gradient_scratch(const Dims& D, int planes = 1) {
   const Matrix du = tokens(nullptr, D, D.wide), x = tokens(nullptr, D, D.in);
-  return std::max(product_scratch(dx_product(D, du, nullptr, x, nullptr)), product_scratch(dw_product(D, du, x, nullptr, nullptr)));
+  Product dx = dx_product(D, du, nullptr, x, nullptr), dw = dw_product(D, du, x, nullptr, nullptr);
+  size_t most = std::max(product_scratch(dx), product_scratch(dw));
+  if (planes == 2) {
+    dw.planes = 2;
+    most = std::max(most, product_scratch(dw));
+  }
+  return most;
 }
 
 // The two layers of a feed-forward block.
@@ -339,13 +362,14 @@ Scratch ffn_scratch(const Dims& D, bool backward, void* ws) {
   Scratch s{};
   s.h = c.take<char>((size_t)D.rows * D.out * D.es);
   if (backward) {
-    s.du = c.take<char>((size_t)D.rows * down.out * D.es);
-    s.dh = c.take<char>((size_t)D.rows * D.out * D.es);
-    s.du_up = c.take<char>(D.gated ? (size_t)D.rows * D.wide * D.es : 0);
-    const size_t chunks = chunks_of(D);
-    s.part_b = c.take<float>(chunks * std::max(up.wide, down.out));
+    const bool bf16 = D.dtype == VMOBA_BF16;
+    s.du = c.take<char>((size_t)D.rows * down.out * D.es * (bf16 ? 2 : 1));
+    s.dh = c.take<char>(bf16 ? 0 : (size_t)D.rows * D.out * D.es);
+    s.du_up = c.take<char>(bf16 || D.gated ? (size_t)D.rows * D.wide * D.es : 0);
+    const size_t chunks = chunks_of(D), blocks = (size_t)(D.rows + 31) / 32;
+    s.part_b = c.take<float>(std::max(chunks, bf16 ? blocks : 0) * std::max(up.wide, down.out));
     s.part_g = c.take<float>(chunks * down.out);
-    s.product = c.take<float>(std::max(gradient_scratch(up), gradient_scratch(down)));
+    s.product = c.take<float>(std::max(gradient_scratch(up), gradient_scratch(down, bf16 ? 2 : 1)));
   } else {
     s.product = c.take<float>(std::max(forward_scratch(up), forward_scratch(down)));
   }
@@ -502,25 +526,43 @@ extern "C" int vmoba_ffn_bwd(const vmoba_linear_shape* shape, const void* d_out,
   if (!gate) down = ungrouped(down);
   up = ungrouped(up);
   VMOBA_GUARDS_ARM(s.guards, st);
-  // through the gate
+  // Through the gate.  In bf16 what the rounding of gate * d_out leaves is kept as a second plane, and the products of it have both: rounded
+  // here, at h's gradient and at the product's, the results would be twice as far off as their own rounding leaves them.
+  const bool bf16 = up.dtype == VMOBA_BF16;
   Prep p = prep_of(down, d_out, d_out_strides, gate, gate_strides, dgate ? kept_down : nullptr);
-  const bool apart = gate && (through || dw_down);
+  const long long plane = down.rows * down.out;
+  const bool dense_d = (down.S == 1 || d_out_strides[1] == down.out) && (down.B == 1 || d_out_strides[0] == (int64_t)down.S * down.out);
+  const bool apart = (gate || (bf16 && !dense_d)) && (through || dw_down);
+  const int planes = bf16 && gate && apart ? 2 : 1;
+  if (planes == 2) p.du_low = s.du + plane * up.es;
   if (apart || db_down || dgate)
     if (int rc = prepare(down, p, s, apart ? s.du : nullptr, db_down, dgate, st)) return rc;
   const Matrix d_down = apart ? tokens(s.du, down, down.out) : raster(d_out, d_out_strides, down, down.out);
-  // the gradient of h; from that, the activation's slope, that of the first product (not gated: in its place), and h again
-  void* const d_up = up.gated ? s.du_up : s.dh;
-  if (through)
-    if (int rc = run_product(dx_product(down, d_down, w_down, tokens(s.dh, down, down.in), dev_status), s.product, st)) return rc;
-  if (through || dw_down) {
-    // (for h alone any gradient does)
+  // the gradient of h; from that, the activation's slope, that of the first product, and h again
+  void* const d_up = bf16 || up.gated ? s.du_up : s.dh;
+  if (through && bf16) {
+    Product q = slope_product(down, up, d_down, w_down, kept_up, tokens(d_up, up, up.out), dev_status);
+    q.planes = planes;
+    q.plane = plane;
+    q.e.again = dw_down ? s.h : nullptr;
+    q.e.col_sums = db_up ? s.part_b : nullptr;
+    if (int rc = run_product(q, s.product, st)) return rc;
+    if (db_up)
+      if (int rc = sum_chunks(s.part_b, up.wide, 1, (int)((up.rows + 31) / 32), db_up, true, st)) return rc;
+  } else if (through || dw_down) {           // (fp32: d_up in the place of dh, where it is not gated; for h alone any gradient does)
+    if (through)
+      if (int rc = run_product(dx_product(down, d_down, w_down, tokens(s.dh, down, down.in), dev_status), s.product, st)) return rc;
     const int64_t of_dh[2] = {(int64_t)up.S * up.out, up.out}, of_kept[2] = {(int64_t)up.S * up.wide, up.wide};
     p = prep_of(up, through ? (const void*)s.dh : kept_up, through ? of_dh : of_kept, nullptr, nullptr, kept_up);
     p.y = dw_down ? s.h : nullptr;
     if (int rc = prepare(up, p, s, dx || dw_up ? d_up : nullptr, db_up, nullptr, st)) return rc;
   }
-  if (dw_down)
-    if (int rc = run_product(dw_product(down, d_down, tokens(s.h, down, down.in), dw_down, dev_status), s.product, st)) return rc;
+  if (dw_down) {
+    Product q = dw_product(down, d_down, tokens(s.h, down, down.in), dw_down, dev_status);
+    q.planes = planes;
+    q.plane = plane;
+    if (int rc = run_product(q, s.product, st)) return rc;
+  }
   const Matrix du = tokens(d_up, up, up.wide);
   if (dw_up)
     if (int rc = run_product(dw_product(up, du, input(x, x_strides, up), dw_up, dev_status), s.product, st)) return rc;

@@ -14,7 +14,9 @@ namespace vmoba {
 namespace linear {
 
 enum Form { kRowsRows = 0, kRowsCols = 1, kColsCols = 2 };
-enum Kind { kPlain = 0, kForward = 1, kGated = 2 };
+// What becomes of sums: written; a layer's forward; that of a gated layer; the gradient of a layer's product from that of its output (kSlope,
+// gated: kSlopeGated), together with the output itself.
+enum Kind { kPlain = 0, kForward = 1, kGated = 2, kSlope = 3, kSlopeGated = 4 };
 
 // A matrix in memory whose row r is token s of sample b, r = b * S + s; column c lies at (c / inner) * sh + c % inner of its row (inner: the
 // channels of a head where heads are apart, else all columns).  Element strides.
@@ -40,7 +42,11 @@ struct Epilogue {
   long long rb = 0, rt = 0;
   void* kept = nullptr;                      // sums with bias, ahead of the activation, dense in the order of x
   const int* perm = nullptr;                 // token of out for every token of x
+  // kSlope*: out is dense [rows, cols or 2 cols], kept is read
+  void* again = nullptr;                     // the layer's output, dense [rows, cols]
+  float* col_sums = nullptr;                 // [rows / 32][cols or 2 cols]: sums of out by 32 rows
 };
+inline bool is_gated(int kind) { return kind == kGated || kind == kSlopeGated; }
 inline void set_out(Epilogue* e, const Matrix& m) {
   e->S = m.S; e->by_S = FastDiv((unsigned)m.S);
   e->inner = m.inner; e->by_inner = FastDiv((unsigned)m.inner);
@@ -53,6 +59,8 @@ struct Product {
   Matrix a, b;
   Epilogue e;
   int M, N;                                  // of D; the summed index has a.cols (kRows*) or the rows of a
+  int planes;                                // 2: a is the sum of two matrices, the second `plane` elements behind the first
+  long long plane;
   bool bf16;
   int32_t* status;
 };

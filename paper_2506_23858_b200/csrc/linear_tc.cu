@@ -29,7 +29,8 @@ struct Args {
   int Sm, rows_tiles, row_tiles, col_tiles;  // rows of a sample; tiles of rows per sample and of all; tiles of columns
   int N;                                     // columns of out
   int steps, per, splits, items;             // stages of the summed index, of a slice; slices
-  int a_inner, b_inner, step_inner;          // columns of a head; (kColsCols) stages per sample
+  int a_inner, b_inner, b_samples;           // columns of a head; samples of b (those of a come twice, if it has two planes)
+  int step_inner;                            // stages per sample (kColsCols), per plane
   FastDiv by_rows_tiles, by_tiles, by_group, by_a_inner, by_b_inner, by_step, by_wide;
   float* part;                               // [slice][row][column of the sums]
   int wide;                                  // columns of the sums
@@ -45,11 +46,11 @@ struct Shared {
 constexpr int STAGE_BYTES = 2 * HALF;
 constexpr int TURN_BYTES = 32 * STAGE_W * 4;
 constexpr int AHEAD_BYTES = 32 * STAGE_W * 2; // a warp's residual of the box to come
-// How results leave: boxes written by TMA, or rows of lanes where gate, residual, another order of the rows or parts are in play.
-enum Store { kBoxes = 0, kRows = 1 };
+// How results leave: boxes written by TMA; rows of lanes where gate, residual, another order of the rows or parts are in play; rows again for slopes.
+enum Store { kBoxes = 0, kRows = 1, kSlopes = 2 };
 __host__ __device__ constexpr int stages_of(int store) { return store == kBoxes ? MOST_STAGES : MOST_STAGES - 1; }
 __host__ __device__ constexpr int smem_of(int store) {
-  return 1024 + stages_of(store) * STAGE_BYTES + EPI_WARPS * (TURN_BYTES + (store == kRows ? AHEAD_BYTES : 0)) + (int)sizeof(Shared);
+  return 1024 + stages_of(store) * STAGE_BYTES + EPI_WARPS * (TURN_BYTES + (store != kBoxes ? AHEAD_BYTES : 0)) + (int)sizeof(Shared);
 }
 static_assert(smem_of(kBoxes) <= 227 * 1024 && smem_of(kRows) <= 227 * 1024, "shared memory of a CTA");
 
@@ -136,7 +137,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   char* turn = smem + STAGES * STAGE_BYTES;
   char* ahead = turn + EPI_WARPS * TURN_BYTES;
-  Shared* sm = reinterpret_cast<Shared*>(ahead + (STORE == kRows ? EPI_WARPS * AHEAD_BYTES : 0));
+  Shared* sm = reinterpret_cast<Shared*>(ahead + (STORE != kBoxes ? EPI_WARPS * AHEAD_BYTES : 0));
   volatile int* abort_flag = &sm->abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cta_rank();
@@ -174,24 +175,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
           if (!mbar_wait(&sm->empty[slot], par, abort_flag, p.status)) break;
           const uint32_t a = smem_u32(smem) + slot * STAGE_BYTES, b = a + HALF, bar = first_cta(&sm->full[slot]);
           if (rank == 0) mbar_expect_tx(&sm->full[slot], 2 * STAGE_BYTES);
-          int ks = 0, kb = 0;                // kColsCols: sample and first token of the stage
-          if (A_MN) { kb = p.by_step.div(k); ks = (k - kb * p.step_inner) * BK; }
+          const int kb = p.by_step.div(k), ks = (k - kb * p.step_inner) * BK;      // sample or plane, and first index in it
           if (A_MN) {
             for (int h = 0; h < 2; ++h) {
               const int m = row + 64 * h, z = p.by_a_inner.div(m);
               pair_load_4d(a + h * PANEL, &tmA, bar, m - z * p.a_inner, ks, z, kb);
             }
           } else {
-            const int z = p.by_a_inner.div(k * BK);
-            pair_load_4d(a, &tmA, bar, k * BK - z * p.a_inner, row, z, it.sample);
+            const int z = p.by_a_inner.div(ks);
+            pair_load_4d(a, &tmA, bar, ks - z * p.a_inner, row, z + kb, it.sample);
           }
           if (B_MN) {
             for (int h = 0; h < 2; ++h) {
               const int c = col + 64 * h, z = p.by_b_inner.div(c);
-              pair_load_4d(b + h * PANEL, &tmB, bar, c - z * p.b_inner, A_MN ? ks : k * BK, z, kb);
+              pair_load_4d(b + h * PANEL, &tmB, bar, c - z * p.b_inner, ks, z, A_MN ? (kb < p.b_samples ? kb : kb - p.b_samples) : 0);
             }
           } else {
-            pair_load_4d(b, &tmB, bar, k * BK, col, 0, 0);
+            pair_load_4d(b, &tmB, bar, ks, col, 0, 0);
           }
           ++n;
           if (++slot == STAGES) { slot = 0; par ^= 1; }
@@ -507,6 +507,115 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         }
       }
     }
+  } else if (warp >= 4 && STORE == kSlopes) {
+    // ------------------------------------------------------------------ sums d to d act'(u) and act(u) (gated: d v act'(u), d act(u); act(u) v)
+    using T = __nv_bfloat16;
+    constexpr bool PAIR = KIND == kSlopeGated;
+    constexpr int W = PAIR ? 32 : 64, BOXES = BN / 2 / W;              // columns at a time
+    constexpr int PER_ROW = W / 8, ROWS = 32 / PER_ROW, TURNS = 32 / ROWS;
+    const int quad = warp & 3, half = (warp - 4) >> 2;
+    const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
+    float* const mine = reinterpret_cast<float*>(turn + (warp - 4) * TURN_BYTES);
+    char* const mine_ahead = ahead + (warp - 4) * AHEAD_BYTES + lane * 16;       // u of the box to come, a row per 512 bytes; then v
+    const Epilogue& e = p.e;
+    const int lr = lane / PER_ROW, lc = (lane % PER_ROW) * 8;
+    auto place = [&](int r, int c4) { return reinterpret_cast<float4*>(mine + r * W + ((c4 ^ (r & 7)) << 2)); };
+    auto column = [&](int ch) { return half * (BN / 2) + ch * W; };
+    auto first_row = [&](const Item& it) { return it.row + (int)rank * BM + quad * 32; };
+    auto ask = [&](const Item& it, int ch, int q) {
+      const int c = it.col + column(ch) + lc, r = first_row(it) + q * ROWS + lr;
+      if (c < p.N && r < p.Sm) {
+        const T* from = static_cast<const T*>(e.kept) + (long long)r * p.wide + c;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(mine_ahead + q * 512)), "l"(from) : "memory");
+        if (PAIR) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(mine_ahead + (TURNS + q) * 512)), "l"(from + p.N) : "memory");
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    uint32_t n = 0;
+    Item next = item_of<KIND>(p, pair);
+#pragma unroll
+    for (int q = 0; q < TURNS; ++q) ask(next, 0, q);
+    for (int i = pair; i < p.items; i += pairs, ++n) {
+      const Item now = next;
+      const bool more = i + pairs < p.items;
+      if (more) next = item_of<KIND>(p, i + pairs);
+      const int row = first_row(now);
+#pragma unroll 1
+      for (int ch = 0; ch < BOXES; ++ch) {
+        const int at = column(ch), c = now.col + at + lc;
+        if (ch == 0) {
+          mbar_wait_warp(&sm->acc_full[n & 1], (n >> 1) & 1, abort_flag, p.status);
+          tc_fence_after();
+        }
+#pragma unroll
+        for (int x = 0; x < W / 32; ++x) {
+          uint32_t v[32];
+          tmem_ld32(lanes + (n & 1) * BN + at + 32 * x, v);
+          tmem_ld_wait();
+          if (x == 0) __syncwarp();          // (the tile turned before has been read)
+          if (x == W / 32 - 1 && ch == BOXES - 1) {      // the accumulator has been read
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(first_cta(&sm->acc_empty[n & 1]));
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(place(lane, 8 * x + j)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        }
+        __syncwarp();
+        float su[8] = {}, sv[8] = {};
+#pragma unroll
+        for (int q = 0; q < TURNS; ++q) {
+          const int r = q * ROWS + lr;
+          asm volatile("cp.async.wait_group %0;" ::"n"(TURNS - 1) : "memory");   // (the oldest of TURNS rows is here)
+          if (c < p.N && row + r < p.Sm) {
+            float d[8], u[8], v[8], h[8];
+            const int c4 = lc / 4, swap = PAIR ? 0 : (lane >> 2) & 1;
+            const float4 x = *place(r, c4 + swap), y = *place(r, c4 + (swap ^ 1));
+            const float4 lo = swap ? y : x, hi = swap ? x : y;
+            d[0] = lo.x; d[1] = lo.y; d[2] = lo.z; d[3] = lo.w; d[4] = hi.x; d[5] = hi.y; d[6] = hi.z; d[7] = hi.w;
+            load_vec<8>(reinterpret_cast<const T*>(mine_ahead + q * 512), u);
+            if (PAIR) load_vec<8>(reinterpret_cast<const T*>(mine_ahead + (TURNS + q) * 512), v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float2 a = activate_slope<false>(e.act, u[k]);
+              if (PAIR) {
+                h[k] = a.x * v[k];
+                u[k] = d[k] * v[k] * a.y;
+                v[k] = d[k] * a.x;
+                sv[k] += v[k];
+              } else {
+                h[k] = a.x;
+                u[k] = d[k] * a.y;
+              }
+              su[k] += u[k];
+            }
+            const long long g = row + r;
+            T* out = static_cast<T*>(e.out) + g * p.wide + c;
+            store_vec<8>(out, u);
+            if (PAIR) store_vec<8>(out + p.N, v);
+            if (e.again) store_vec<8>(static_cast<T*>(e.again) + g * p.N + c, h);
+          }
+          __syncwarp();
+          if (ch < BOXES - 1) ask(now, ch + 1, q);
+          else if (more) ask(next, 0, q);
+          else asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        if (e.col_sums && row < p.Sm) {      // of the warp's 32 rows
+#pragma unroll
+          for (int o = PER_ROW; o < 32; o <<= 1)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              su[k] += __shfl_xor_sync(0xffffffffu, su[k], o);
+              if (PAIR) sv[k] += __shfl_xor_sync(0xffffffffu, sv[k], o);
+            }
+          if (lr == 0 && c < p.N) {
+            float* to = e.col_sums + (long long)(row >> 5) * p.wide + c;
+            store_vec<8>(to, su);
+            if (PAIR) store_vec<8>(to + p.N, sv);
+          }
+        }
+      }
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -576,23 +685,27 @@ struct Plan { int steps, per, splits; long long tiles; };
 Plan plan_of(const Product& p) {
   const int cols = p.e.kind == kGated ? BN / 2 : BN;
   Plan o;
-  if (p.form == kColsCols) o.steps = p.a.B * ((p.a.S + BK - 1) / BK);
-  else o.steps = (p.a.cols + BK - 1) / BK;
+  if (p.form == kColsCols) o.steps = p.planes * p.a.B * ((p.a.S + BK - 1) / BK);
+  else o.steps = p.planes * ((p.a.cols + BK - 1) / BK);
   o.tiles = (long long)((p.M + 2 * BM - 1) / (2 * BM)) * ((p.N + cols - 1) / cols);
-  o.splits = slices(o.tiles, o.steps, kPairs);
+  o.splits = p.e.kind >= kSlope ? 1 : slices(o.tiles, o.steps, kPairs);      // (sums of rows' gradients are of whole sums)
   o.per = (o.steps + o.splits - 1) / o.splits;
   return o;
 }
 
 struct Maps { CUtensorMap a, b, out, kept, kept2; };
 
+template <typename K>
+int start(K kernel, int store, const Args& a, const Maps& m, cudaStream_t st) {
+  VMOBA_CUDA_OK(allow_smem(kernel, smem_of(store)));
+  launch_kernel(kernel, 2 * (unsigned)std::min(a.items, std::max(1, sm_count() / 2)), THREADS, (size_t)smem_of(store), st, m.a, m.b, m.out, m.kept,
+                m.kept2, a);
+  VMOBA_LAUNCH_OK(1);
+  return VMOBA_OK;
+}
 template <int FORM, int KIND>
 int launch(const Args& a, const Maps& m, bool boxes, cudaStream_t st) {
-  auto kernel = boxes ? pair_kernel<FORM, KIND, kBoxes> : pair_kernel<FORM, KIND, kRows>;
-  const int smem = smem_of(boxes ? kBoxes : kRows);
-  VMOBA_CUDA_OK(allow_smem(kernel, smem));
-  launch_kernel(kernel, 2 * (unsigned)std::min(a.items, std::max(1, sm_count() / 2)), THREADS, (size_t)smem, st, m.a, m.b, m.out, m.kept, m.kept2, a);
-  VMOBA_LAUNCH_OK(1);
+  if (int rc = boxes ? start(pair_kernel<FORM, KIND, kBoxes>, kBoxes, a, m, st) : start(pair_kernel<FORM, KIND, kRows>, kRows, a, m, st)) return rc;
   if (a.splits > 1) {
     const long long vecs = a.N / 8, total = a.part_rows * vecs;
     launch_kernel(join_kernel<KIND>, (unsigned)std::min<long long>((total + 255) / 256, 16 * sm_count()), 256, 0, st, a, FastDiv((unsigned)vecs),
@@ -617,7 +730,7 @@ int tc_product(const Product& p, float* scratch, cudaStream_t st) {
   const int cols = p.e.kind == kGated ? BN / 2 : BN;
   a.e = p.e;
   a.N = p.N;
-  a.wide = p.e.kind == kGated ? 2 * p.N : p.N;
+  a.wide = is_gated(p.e.kind) ? 2 * p.N : p.N;
   a.part_rows = p.M;
   a.status = p.status;
   a.splits = plan.splits; a.steps = plan.steps; a.per = plan.per;
@@ -626,15 +739,21 @@ int tc_product(const Product& p, float* scratch, cudaStream_t st) {
     if (folded(ma).B == 1 && folded(mb).B == 1) {
       ma = folded(ma);
       mb = folded(mb);
-      a.steps = (ma.S + BK - 1) / BK;        // (no more than before)
+      a.steps = p.planes * ((ma.S + BK - 1) / BK);      // (no more than before)
       a.per = (a.steps + a.splits - 1) / a.splits;
       a.splits = (a.steps + a.per - 1) / a.per;
       if (a.splits == 1) a.part = nullptr;
     }
     a.step_inner = (ma.S + BK - 1) / BK;
+    a.b_samples = mb.B;
+    if (p.planes == 2) {                     // (a plane's samples behind the other's)
+      if (ma.B > 1 && p.plane != ma.B * ma.sb) return VMOBA_ERR_ARG;
+      if (ma.B == 1) ma.sb = p.plane;
+      ma.B *= 2;
+    }
   }
   // how results leave, and (boxes) whether they lie so that all samples' rows can be taken for one's
-  const bool boxes = !a.part && !p.e.gate && !p.e.residual && !p.e.perm;
+  const bool slopes = p.e.kind >= kSlope, boxes = !a.part && !p.e.gate && !p.e.residual && !p.e.perm && !slopes;
   const bool gated = p.e.kind == kGated;
   Matrix out{p.e.out, p.M / p.e.S, p.e.S, p.e.cols, p.e.inner, p.e.ob, p.e.ot, p.e.oh};
   Matrix kept{p.e.kept, out.B, out.S, a.wide, a.wide, (long long)out.S * a.wide, a.wide, 0};
@@ -643,7 +762,11 @@ int tc_product(const Product& p, float* scratch, cudaStream_t st) {
       ma = folded(ma);
       if (ma.B == 1) { out = folded(out); kept = folded(kept); }
     }
-    a.step_inner = 1;
+    a.step_inner = (ma.cols + BK - 1) / BK;
+    if (p.planes == 2) {                     // (as a second head)
+      ma.cols *= 2;
+      ma.sh = p.plane;
+    }
     a.Sm = ma.S;
   } else {
     a.Sm = p.M;
@@ -674,6 +797,8 @@ int tc_product(const Product& p, float* scratch, cudaStream_t st) {
     }
   }
   if (p.form == kColsCols) return launch<kColsCols, kPlain>(a, m, boxes, st);
+  if (p.e.kind == kSlope) return start(pair_kernel<kRowsCols, kSlope, kSlopes>, kSlopes, a, m, st);
+  if (p.e.kind == kSlopeGated) return start(pair_kernel<kRowsCols, kSlopeGated, kSlopes>, kSlopes, a, m, st);
   if (p.form == kRowsCols) return launch<kRowsCols, kPlain>(a, m, boxes, st);
   return gated ? launch<kRowsRows, kGated>(a, m, boxes, st) : launch<kRowsRows, kForward>(a, m, boxes, st);
 }
