@@ -115,21 +115,23 @@ __global__ void __launch_bounds__(256) prep_kernel(Prep p) {
       }
       if (p.kept) {
         float y[8];
+        by_activation(p.act, [&](auto act) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float2 a = activate_slope<EXACT>(p.act, u[i]);
-          y[i] = GATED ? a.x * v[i] : a.x;
-          sg[i] = fmaf(d[i], y[i], sg[i]);
-          if (p.gate) d[i] *= gate[i];
-          if (GATED) {
-            const float dv = d[i] * a.x;
-            d[i] *= a.y * v[i];
-            v[i] = dv;
-            sv[i] += dv;
-          } else {
-            d[i] *= a.y;
+          for (int i = 0; i < 8; ++i) {
+            const float2 a = activate_slope<EXACT, decltype(act)::value>(u[i]);
+            y[i] = GATED ? a.x * v[i] : a.x;
+            sg[i] = fmaf(d[i], y[i], sg[i]);
+            if (p.gate) d[i] *= gate[i];
+            if (GATED) {
+              const float dv = d[i] * a.x;
+              d[i] *= a.y * v[i];
+              v[i] = dv;
+              sv[i] += dv;
+            } else {
+              d[i] *= a.y;
+            }
           }
-        }
+        });
         if (p.y) store_vec<8>(static_cast<T*>(p.y) + r * p.cols + c, y);
         if (GATED && p.du) store_vec<8>(static_cast<T*>(p.du) + r * wide + p.cols + c, v);
       } else if (p.gate) {

@@ -80,27 +80,38 @@ int few_product(const Product& p, cudaStream_t st);
 int sum_chunks(const float* part, int cols, int groups, int per, void* out, bool bf16, cudaStream_t st);
 
 #ifdef __CUDACC__
-// gelu in its tanh form, u s(2 k (u + c u^3)), and silu, u s(u), of the logistic function s.  exp(-x) overflows for very negative x and the
-// quotient is then zero, as it should be.  EXACT: to fp32's last places; else to 2^-20 or so, for results of 8 bits.
+// gelu in its tanh form, u s(2 k (u + c u^3)), and silu, u s(u), of the logistic function s = 1 / (1 + exp(-x)), whose exp overflows for very
+// negative x, where s is zero, as it should be.  EXACT: to fp32's last places; else to 2^-20 or so, for results of 8 bits.
 constexpr float kGeluK = 1.5957691216057308f, kGeluC = 0.044715f;      // 2 sqrt(2 / pi)
 template <bool EXACT>
 __device__ __forceinline__ float logistic(float x) {
-  return EXACT ? 1.f / (1.f + expf(-x)) : __fdividef(1.f, 1.f + __expf(-x));
+  if constexpr (EXACT) {
+    return 1.f / (1.f + expf(-x));
+  } else {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + sm100::ex2(-1.4426950408889634f * x)));
+    return r;
+  }
 }
-template <bool EXACT>
-__device__ __forceinline__ float activate(int act, float u) {
-  if (act == VMOBA_ACT_NONE) return u;
-  return u * logistic<EXACT>(act == VMOBA_ACT_SILU ? u : kGeluK * u * fmaf(kGeluC * u, u, 1.f));
+template <bool EXACT, int ACT>
+__device__ __forceinline__ float activate(float u) {
+  if constexpr (ACT == VMOBA_ACT_NONE) return u;
+  return u * logistic<EXACT>(ACT == VMOBA_ACT_SILU ? u : kGeluK * u * fmaf(kGeluC * u, u, 1.f));
 }
-// The activation and its slope.
-template <bool EXACT>
-__device__ __forceinline__ float2 activate_slope(int act, float u) {
-  if (act == VMOBA_ACT_NONE) return make_float2(u, 1.f);
-  const bool silu = act == VMOBA_ACT_SILU;
-  const float s = logistic<EXACT>(silu ? u : kGeluK * u * fmaf(kGeluC * u, u, 1.f));
-  const float t = s * (1.f - s);             // (zero far out, where what it is multiplied by may be infinite)
-  const float z = silu ? 1.f : kGeluK * fmaf(3.f * kGeluC * u, u, 1.f);
-  return make_float2(u * s, t == 0.f ? s : fmaf(u * t, z, s));
+// The activation and its slope, s + u s (1 - s) z' with z the argument of s.  (Far out s (1 - s) is zero and z' may be infinite: it is held below that.)
+template <bool EXACT, int ACT>
+__device__ __forceinline__ float2 activate_slope(float u) {
+  if constexpr (ACT == VMOBA_ACT_NONE) return make_float2(u, 1.f);
+  const float q = kGeluC * u * u, s = logistic<EXACT>(ACT == VMOBA_ACT_SILU ? u : kGeluK * u * (q + 1.f)), y = u * s, t = y * (1.f - s);
+  if constexpr (ACT == VMOBA_ACT_SILU) return make_float2(y, s + t);
+  return make_float2(y, fmaf(t, fminf(fmaf(3.f * kGeluK, q, kGeluK), 1e30f), s));
+}
+// f(activation), compiled for each.
+template <typename F>
+__device__ __forceinline__ void by_activation(int act, F f) {
+  if (act == VMOBA_ACT_SILU) f(std::integral_constant<int, VMOBA_ACT_SILU>{});
+  else if (act == VMOBA_ACT_GELU) f(std::integral_constant<int, VMOBA_ACT_GELU>{});
+  else f(std::integral_constant<int, VMOBA_ACT_NONE>{});
 }
 
 template <int V>
@@ -187,11 +198,13 @@ __device__ __forceinline__ void finish(const Epilogue& e, const OutRow<T>& row, 
       store_vec<V>(row.kept + c, u);
       if constexpr (KIND == kGated) store_vec<V>(row.kept + e.cols + c, v);
     }
+    by_activation(e.act, [&](auto act) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      u[i] = activate<EXACT>(e.act, u[i]);
-      if constexpr (KIND == kGated) u[i] *= v[i];
-    }
+      for (int i = 0; i < V; ++i) {
+        u[i] = activate<EXACT, decltype(act)::value>(u[i]);
+        if constexpr (KIND == kGated) u[i] *= v[i];
+      }
+    });
     if (row.gate) {
       load_vec<V>(row.gate + c, t);
 #pragma unroll

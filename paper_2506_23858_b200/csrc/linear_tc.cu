@@ -39,7 +39,7 @@ struct Args {
 };
 
 struct Shared {
-  uint64_t full[MOST_STAGES], empty[MOST_STAGES], acc_full[2], acc_empty[2], drain;
+  uint64_t full[MOST_STAGES], empty[MOST_STAGES], acc_full[2], acc_empty[2], ahead[EPI_WARPS], drain;
   uint32_t tmem;
   int abort;
 };
@@ -109,6 +109,21 @@ __device__ __forceinline__ void add_bf16x8(float (&u)[8], const uint4& v) {
   add_bf16_pair(u[6], u[7], v.w);
 }
 
+// Sums over the warp's lanes of 32 numbers each: lane k gets that of x[k].  Half of what is left goes to the other half of the lanes at each step.
+__device__ __forceinline__ float column_sum(float* x) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const bool high = lane & o;
+#pragma unroll
+    for (int k = 0; k < o; ++k) {
+      const float keep = high ? x[k + o] : x[k], give = high ? x[k] : x[k + o];
+      x[k] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+  }
+  return x[0];
+}
+
 struct Item {
   int split, sample, row, col;               // first row of the pair's tile in the sample; first column of out
 };
@@ -129,7 +144,8 @@ __device__ __forceinline__ Item item_of(const Args& p, int i) {
 template <int FORM, int KIND, int STORE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmOut,
-                const __grid_constant__ CUtensorMap tmKept, const __grid_constant__ CUtensorMap tmKept2, Args p) {
+                const __grid_constant__ CUtensorMap tmOut2, const __grid_constant__ CUtensorMap tmKept, const __grid_constant__ CUtensorMap tmKept2,
+                const __grid_constant__ CUtensorMap tmAgain, Args p) {
   if (!grid_begin()) return;
   constexpr bool A_MN = FORM == kColsCols, B_MN = FORM != kRowsRows;
   constexpr int STAGES = stages_of(STORE);
@@ -146,6 +162,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   if (warp == 0 && lane == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(&sm->full[i], 1); mbar_init(&sm->empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sm->acc_full[i], 1); mbar_init(&sm->acc_empty[i], 2 * EPI_WARPS); }
+    for (int i = 0; i < EPI_WARPS; ++i) mbar_init(&sm->ahead[i], 1);
     mbar_init(&sm->drain, 1);
     sm->abort = 0;
     fence_barrier_init();
@@ -321,9 +338,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             emit(&tmKept, p.wide, p.by_wide, u, c);
             if constexpr (KIND == kGated) emit(&tmKept2, p.wide, p.by_wide, w, c);
           }
-          if (e.act != VMOBA_ACT_NONE)
+          by_activation(e.act, [&](auto act) {
 #pragma unroll
-            for (int k = 0; k < W; ++k) u[k] = activate<false>(e.act, u[k]);
+            for (int k = 0; k < W; ++k) u[k] = activate<false, decltype(act)::value>(u[k]);
+          });
           if constexpr (KIND == kGated)
 #pragma unroll
             for (int k = 0; k < W; k += 2) mul2(u[k], u[k + 1], u[k], u[k + 1], w[k], w[k + 1]);
@@ -481,9 +499,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                 store_vec<8>(kept, u);
                 if (KIND == kGated) store_vec<8>(kept + p.N, w);
               }
-              if (e.act != VMOBA_ACT_NONE)
+              by_activation(e.act, [&](auto act) {
 #pragma unroll
-                for (int x = 0; x < 8; ++x) u[x] = activate<false>(e.act, u[x]);
+                for (int x = 0; x < 8; ++x) u[x] = activate<false, decltype(act)::value>(u[x]);
+              });
               if (KIND == kGated)
 #pragma unroll
                 for (int x = 0; x < 8; x += 2) mul2(u[x], u[x + 1], u[x], u[x + 1], w[x], w[x + 1]);
@@ -509,113 +528,127 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     }
   } else if (warp >= 4 && STORE == kSlopes) {
     // ------------------------------------------------------------------ sums d to d act'(u) and act(u) (gated: d v act'(u), d act(u); act(u) v)
-    using T = __nv_bfloat16;
+    // Lane = row; everything comes and goes in boxes by TMA.  (By rows of lanes, 64 or 128 bytes of each: 333 us instead of 277 for 13,440 rows of
+    // 4,104 columns, gated, nearly all of the difference in the stores.)
     constexpr bool PAIR = KIND == kSlopeGated;
-    constexpr int W = PAIR ? 32 : 64, BOXES = BN / 2 / W;              // columns at a time
-    constexpr int PER_ROW = W / 8, ROWS = 32 / PER_ROW, TURNS = 32 / ROWS;
+    constexpr int W = PAIR ? 32 : 64, BOXES = BN / 2 / W, BOX = 32 * 2 * W;      // columns of a box, boxes of a warp, bytes
     const int quad = warp & 3, half = (warp - 4) >> 2;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
-    float* const mine = reinterpret_cast<float*>(turn + (warp - 4) * TURN_BYTES);
-    char* const mine_ahead = ahead + (warp - 4) * AHEAD_BYTES + lane * 16;       // u of the box to come, a row per 512 bytes; then v
+    char* const in = turn + (warp - 4) * (TURN_BYTES + AHEAD_BYTES);             // u (and v), then the results: du (and dv) and h
+    char* const results = in + (PAIR ? 2 : 1) * BOX;
+    uint64_t* const here = &sm->ahead[warp - 4];
     const Epilogue& e = p.e;
-    const int lr = lane / PER_ROW, lc = (lane % PER_ROW) * 8;
-    auto place = [&](int r, int c4) { return reinterpret_cast<float4*>(mine + r * W + ((c4 ^ (r & 7)) << 2)); };
-    auto column = [&](int ch) { return half * (BN / 2) + ch * W; };
-    auto first_row = [&](const Item& it) { return it.row + (int)rank * BM + quad * 32; };
-    auto ask = [&](const Item& it, int ch, int q) {
-      const int c = it.col + column(ch) + lc, r = first_row(it) + q * ROWS + lr;
-      if (c < p.N && r < p.Sm) {
-        const T* from = static_cast<const T*>(e.kept) + (long long)r * p.wide + c;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(mine_ahead + q * 512)), "l"(from) : "memory");
-        if (PAIR) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(mine_ahead + (TURNS + q) * 512)), "l"(from + p.N) : "memory");
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
+    auto ask = [&](const Item& it, int ch) {           // (one lane; places outside read as zeros)
+      const int c = it.col + half * (BN / 2) + ch * W, row = it.row + (int)rank * BM + quad * 32;
+      mbar_expect_tx(here, (PAIR ? 2 : 1) * BOX);
+      tma_load_4d(in, &tmKept, here, c, row, 0, 0);
+      if (PAIR) tma_load_4d(in + BOX, &tmKept2, here, c, row, 0, 0);
     };
-    uint32_t n = 0;
+    // 16-byte piece j of the lane's row of a box
+    auto piece = [&](char* box, int j) {
+      return reinterpret_cast<uint4*>(box + lane * (2 * W) + (W == 64 ? j ^ (lane & 7) : j ^ ((lane >> 1) & 3)) * 16);
+    };
+    uint32_t n = 0, boxes = 0;
     Item next = item_of<KIND>(p, pair);
-#pragma unroll
-    for (int q = 0; q < TURNS; ++q) ask(next, 0, q);
+    if (lane == 0) ask(next, 0);
     for (int i = pair; i < p.items; i += pairs, ++n) {
       const Item now = next;
       const bool more = i + pairs < p.items;
       if (more) next = item_of<KIND>(p, i + pairs);
-      const int row = first_row(now);
+      const int row = now.row + (int)rank * BM + quad * 32;
+      mbar_wait_warp(&sm->acc_full[n & 1], (n >> 1) & 1, abort_flag, p.status);
+      tc_fence_after();
 #pragma unroll 1
-      for (int ch = 0; ch < BOXES; ++ch) {
-        const int at = column(ch), c = now.col + at + lc;
-        if (ch == 0) {
-          mbar_wait_warp(&sm->acc_full[n & 1], (n >> 1) & 1, abort_flag, p.status);
-          tc_fence_after();
-        }
+      for (int ch = 0; ch < BOXES; ++ch, ++boxes) {
+        const int at = half * (BN / 2) + ch * W, c = now.col + at;
+        float d[W];
 #pragma unroll
         for (int x = 0; x < W / 32; ++x) {
           uint32_t v[32];
           tmem_ld32(lanes + (n & 1) * BN + at + 32 * x, v);
           tmem_ld_wait();
-          if (x == 0) __syncwarp();          // (the tile turned before has been read)
-          if (x == W / 32 - 1 && ch == BOXES - 1) {      // the accumulator has been read
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_at(first_cta(&sm->acc_empty[n & 1]));
-          }
 #pragma unroll
-          for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(place(lane, 8 * x + j)) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          for (int k = 0; k < 32; ++k) d[32 * x + k] = __uint_as_float(v[k]);
+        }
+        if (ch == BOXES - 1) {               // the accumulator has been read
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_at(first_cta(&sm->acc_empty[n & 1]));
+        }
+        mbar_wait_warp(here, boxes & 1, abort_flag, p.status);
+        uint4 u4[W / 8], v4[PAIR ? W / 8 : 1];
+#pragma unroll
+        for (int j = 0; j < W / 8; ++j) {
+          u4[j] = *piece(in, j);
+          if (PAIR) v4[j] = *piece(in + BOX, j);
         }
         __syncwarp();
-        float su[8] = {}, sv[8] = {};
-#pragma unroll
-        for (int q = 0; q < TURNS; ++q) {
-          const int r = q * ROWS + lr;
-          asm volatile("cp.async.wait_group %0;" ::"n"(TURNS - 1) : "memory");   // (the oldest of TURNS rows is here)
-          if (c < p.N && row + r < p.Sm) {
-            float d[8], u[8], v[8], h[8];
-            const int c4 = lc / 4, swap = PAIR ? 0 : (lane >> 2) & 1;
-            const float4 x = *place(r, c4 + swap), y = *place(r, c4 + (swap ^ 1));
-            const float4 lo = swap ? y : x, hi = swap ? x : y;
-            d[0] = lo.x; d[1] = lo.y; d[2] = lo.z; d[3] = lo.w; d[4] = hi.x; d[5] = hi.y; d[6] = hi.z; d[7] = hi.w;
-            load_vec<8>(reinterpret_cast<const T*>(mine_ahead + q * 512), u);
-            if (PAIR) load_vec<8>(reinterpret_cast<const T*>(mine_ahead + (TURNS + q) * 512), v);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float2 a = activate_slope<false>(e.act, u[k]);
-              if (PAIR) {
-                h[k] = a.x * v[k];
-                u[k] = d[k] * v[k] * a.y;
-                v[k] = d[k] * a.x;
-                sv[k] += v[k];
-              } else {
-                h[k] = a.x;
-                u[k] = d[k] * a.y;
-              }
-              su[k] += u[k];
-            }
-            const long long g = row + r;
-            T* out = static_cast<T*>(e.out) + g * p.wide + c;
-            store_vec<8>(out, u);
-            if (PAIR) store_vec<8>(out + p.N, v);
-            if (e.again) store_vec<8>(static_cast<T*>(e.again) + g * p.N + c, h);
-          }
-          __syncwarp();
-          if (ch < BOXES - 1) ask(now, ch + 1, q);
-          else if (more) ask(next, 0, q);
-          else asm volatile("cp.async.commit_group;" ::: "memory");
+        if (lane == 0) {                     // the next box, and the last results have left
+          if (ch < BOXES - 1) ask(now, ch + 1);
+          else if (more) ask(next, 0);
+          bulk_wait_group_read<0>();
         }
-        if (e.col_sums && row < p.Sm) {      // of the warp's 32 rows
+        __syncwarp();
+        float dv[PAIR ? W : 1];
+        by_activation(e.act, [&](auto act) {
 #pragma unroll
-          for (int o = PER_ROW; o < 32; o <<= 1)
+          for (int j = 0; j < W / 8; ++j) {
+            float h[8], u[8], v[8];
+            const uint32_t uw[4] = {u4[j].x, u4[j].y, u4[j].z, u4[j].w};
+            const uint4 vq = v4[PAIR ? j : 0];
+            const uint32_t vw[4] = {vq.x, vq.y, vq.z, vq.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              u[2 * k] = __uint_as_float(uw[k] << 16);
+              u[2 * k + 1] = __uint_as_float(uw[k] & 0xffff0000u);
+              if (PAIR) { v[2 * k] = __uint_as_float(vw[k] << 16); v[2 * k + 1] = __uint_as_float(vw[k] & 0xffff0000u); }
+            }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              su[k] += __shfl_xor_sync(0xffffffffu, su[k], o);
-              if (PAIR) sv[k] += __shfl_xor_sync(0xffffffffu, sv[k], o);
+              const float2 s = activate_slope<false, decltype(act)::value>(u[k]);
+              float& x = d[8 * j + k];
+              if (PAIR) {
+                h[k] = s.x * v[k];
+                dv[PAIR ? 8 * j + k : 0] = x * s.x;
+                x *= v[k] * s.y;
+              } else {
+                h[k] = s.x;
+                x *= s.y;
+              }
             }
-          if (lr == 0 && c < p.N) {
-            float* to = e.col_sums + (long long)(row >> 5) * p.wide + c;
-            store_vec<8>(to, su);
-            if (PAIR) store_vec<8>(to + p.N, sv);
+            auto put = [&](char* box, const float* f) {
+              *piece(box, j) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+            };
+            put(results, d + 8 * j);
+            if (PAIR) put(results + BOX, dv + (PAIR ? 8 * j : 0));
+            if (e.again) put(results + (PAIR ? 2 : 1) * BOX, h);
+          }
+        });
+        fence_async_proxy();
+        __syncwarp();
+        if (lane == 0) {
+          if (row < p.Sm && c < p.N) {
+            tma_store_4d(&tmOut, results, c, row, 0, 0);
+            if (PAIR) tma_store_4d(&tmOut2, results + BOX, c, row, 0, 0);
+            if (e.again) tma_store_4d(&tmAgain, results + (PAIR ? 2 : 1) * BOX, c, row, 0, 0);
+          }
+          bulk_commit_group();
+        }
+        if (e.col_sums && row < p.Sm) {      // of the warp's 32 rows (rows outside are zeros)
+          float* to = e.col_sums + (long long)(row >> 5) * p.wide + c + lane;
+#pragma unroll
+          for (int x = 0; x < W / 32; ++x) {
+            const float s = column_sum(d + 32 * x);
+            if (c + 32 * x + lane < p.N) to[32 * x] = s;
+          }
+          if constexpr (PAIR) {
+            const float s = column_sum(dv);
+            if (c + lane < p.N) to[p.N] = s;
           }
         }
       }
     }
+    if (lane == 0) bulk_wait_group<0>();
   }
   tc_fence_before();
   __syncthreads();
@@ -693,13 +726,13 @@ Plan plan_of(const Product& p) {
   return o;
 }
 
-struct Maps { CUtensorMap a, b, out, kept, kept2; };
+struct Maps { CUtensorMap a, b, out, out2, kept, kept2, again; };      // (2: of the second half of the columns)
 
 template <typename K>
 int start(K kernel, int store, const Args& a, const Maps& m, cudaStream_t st) {
   VMOBA_CUDA_OK(allow_smem(kernel, smem_of(store)));
-  launch_kernel(kernel, 2 * (unsigned)std::min(a.items, std::max(1, sm_count() / 2)), THREADS, (size_t)smem_of(store), st, m.a, m.b, m.out, m.kept,
-                m.kept2, a);
+  launch_kernel(kernel, 2 * (unsigned)std::min(a.items, std::max(1, sm_count() / 2)), THREADS, (size_t)smem_of(store), st, m.a, m.b, m.out, m.out2,
+                m.kept, m.kept2, m.again, a);
   VMOBA_LAUNCH_OK(1);
   return VMOBA_OK;
 }
@@ -786,14 +819,23 @@ int tc_product(const Product& p, float* scratch, cudaStream_t st) {
   a.by_wide = FastDiv((unsigned)a.wide);
   Maps m{};
   if (!map_of(&m.a, ma, p.form == kColsCols ? BK : BM) || !map_of(&m.b, mb, p.form == kRowsRows ? 128 : BK)) return VMOBA_ERR_CUDA;
-  if (boxes) {
-    const int box = gated ? 32 : 64;
-    if (!map_of(&m.out, out, 32, box)) return VMOBA_ERR_CUDA;
-    if (kept.p) {                            // (gated: the halves on their own, so that a box of the first ends where it does)
-      Matrix first = kept, second = kept;
-      first.cols = first.inner = second.cols = second.inner = p.N;
-      second.p = static_cast<char*>(p.e.kept) + 2ll * p.N;
-      if (!map_of(&m.kept, first, 32, box) || (gated && !map_of(&m.kept2, second, 32, box))) return VMOBA_ERR_CUDA;
+  if (boxes || slopes) {                     // (gated: the halves on their own, so that a box of the first ends where it does)
+    const bool two = is_gated(p.e.kind);
+    const int box = two ? 32 : 64;
+    auto halves = [&](const Matrix& all, const void* base, CUtensorMap* first, CUtensorMap* second) {
+      Matrix x = all;
+      x.p = base;
+      x.cols = x.inner = p.N;
+      if (!map_of(first, x, 32, box)) return false;
+      x.p = static_cast<const char*>(base) + 2ll * p.N;
+      return !two || map_of(second, x, 32, box);
+    };
+    if (slopes) {
+      if (!halves(kept, p.e.kept, &m.kept, &m.kept2) || !halves(kept, p.e.out, &m.out, &m.out2)) return VMOBA_ERR_CUDA;
+      if (p.e.again && !map_of(&m.again, folded(Matrix{p.e.again, out.B, out.S, p.N, p.N, (long long)out.S * p.N, p.N, 0}), 32, box)) return VMOBA_ERR_CUDA;
+    } else {
+      if (!map_of(&m.out, out, 32, box)) return VMOBA_ERR_CUDA;
+      if (kept.p && !halves(kept, kept.p, &m.kept, &m.kept2)) return VMOBA_ERR_CUDA;
     }
   }
   if (p.form == kColsCols) return launch<kColsCols, kPlain>(a, m, boxes, st);
