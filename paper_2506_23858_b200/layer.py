@@ -565,8 +565,12 @@ class VmobaLayer:
                                  do_bm=self.do_bm if keep_do else None)
 
     # ---- whole layer --------------------------------------------------------------------
-    def forward(self, q, k, v, tau, o_out, fold_o=None, rotary=None, weights=None):
+    def forward(self, q, k, v, tau, o_out, fold_o=None, rotary=None, weights=None, projection=None, projected=None):
         """q, k, v, o_out: [B, S, heads, d] raster-order tensors on the device.
+
+        projection: a Linear of the layer's samples, tokens and heads that o goes through on its way out of block order, instead of an inverse
+        partition pass; o_out is then its output [B, S, n_out].  projected: what its forward() takes besides (weight, and as wanted bias, gate,
+        residual, kept).
 
         rotary: a Rotary of the layer's sizes, whatever its blocks, that q and k go through on their way into block order (its weights:
         of q and of k).
@@ -574,6 +578,10 @@ class VmobaLayer:
         fold_o: let the forward kernels write o in raster order themselves (bf16, head_dim 128) instead of an inverse
         partition pass; off by default (measured on B200: the scattered 256-byte row writes cost the attention kernel
         more than the pass they save, at 12 heads as at 40).  o_out must then stay alive and unchanged until backward()."""
+        if projection is not None:
+            self._projects(projection, projected)
+            if fold_o:
+                raise ValueError("VmobaLayer: a projection takes o in block order (fold_o)")
         # k last: the centroids, computed next, find the end of it in L2
         if rotary is not None:
             rotary.forward((k, q), (self.k_bm, self.q_bm), None if weights is None else (weights[1], weights[0]), block_order=True,
@@ -582,14 +590,30 @@ class VmobaLayer:
             self.partition_many((v, q, k), (self.v_bm, self.q_bm, self.k_bm), perm=self.perm)
         self.block_scores()
         self.select(tau)
+        if projection is not None:
+            self.attn_fwd()
+            projection.forward(self.o_bm, out=o_out, perm=self.perm, **projected)
+            return
         if fold_o:
             self.attn_fwd_raster(o_out)
             return
         self.attn_fwd()
         self.partition(o_out, self.o_bm, inverse=True)
 
-    def backward(self, do, dq_out, dk_out, dv_out, fold_inverse=None, fold_do=False, rotary=None, qk=None, weights=None):
+    def _projects(self, projection, projected):
+        s, p = self.shape, projection.shape
+        if not projected or "weight" not in projected:
+            raise ValueError("VmobaLayer: projected has to have the projection's weight")
+        if (p.B, p.S, p.heads, p.n_in, p.dtype) != (s.B, s.S, s.heads, s.heads * s.head_dim, s.dtype):
+            raise ValueError("VmobaLayer: a projection has to be a Linear of the layer's samples, tokens, heads, channels and type")
+
+    def backward(self, do, dq_out, dk_out, dv_out, fold_inverse=None, fold_do=False, rotary=None, qk=None, weights=None, projection=None,
+                 projected=None):
         """Gradients of the last forward(); do and the outputs are raster-order [B, S, heads, d].
+
+        projection: as given to forward(); do is then the gradient of its output [B, S, n_out], and projected what its backward() takes
+        besides (weight, and as wanted kept, gate, with_weight, with_bias).  What that returns comes back, with a rotary after the
+        weights' gradients of that.
 
         rotary, weights: as given to forward(), with its (q, k) in qk where the Rotary has a norm; dq_out and dk_out are then the
         gradients of those, and the weights' are returned.
@@ -600,6 +624,17 @@ class VmobaLayer:
         for its own purpose, leaves a block-major copy."""
         if fold_inverse is None:
             fold_inverse = self.can_fold_inverse(dq_out, dk_out, dv_out)
+        if projection is not None:               # its input's gradient is block-major: do as the kernels read it
+            self._projects(projection, projected)
+            if fold_do or self.o_raster is not None:
+                raise ValueError("VmobaLayer: a projection takes o and hands do over in block order (fold_o, fold_do)")
+            grads = projection.backward(do, self.o_bm, dx_out=self.do_bm, perm=self.perm, **projected)
+            if fold_inverse:
+                self.attn_bwd_raster(None, dq_out, dk_out, dv_out)
+                return grads if rotary is None else (rotary.backward((dq_out, dk_out), qk, (dq_out, dk_out), weights), grads)
+            self.attn_bwd()
+            dw = self._gradients_out(dq_out, dk_out, dv_out, rotary, qk, weights)
+            return grads if rotary is None else (dw, grads)
         if fold_inverse:
             if fold_do:
                 self.attn_bwd_raster(do, dq_out, dk_out, dv_out)
@@ -610,6 +645,10 @@ class VmobaLayer:
         if self.o_raster is not None:      # the block-major backward reads o_bm, which the raster forward did not write
             self.partition(self.o_raster, self.o_bm)
         self.attn_bwd()
+        return self._gradients_out(dq_out, dk_out, dv_out, rotary, qk, weights)
+
+    def _gradients_out(self, dq_out, dk_out, dv_out, rotary, qk, weights):
+        """The block-major gradients into raster order, through the rotary where there is one."""
         if rotary is not None:
             self.partition(dv_out, self.dv_bm, inverse=True)
             return rotary.backward((self.dq_bm, self.dk_bm), qk, (dq_out, dk_out), weights, block_order=True, shape=self.shape)
@@ -648,8 +687,9 @@ class SteppedAttention:
         self._one_block = vb.Shape.from_buffer_copy(s)
         self._one_block.bT, self._one_block.bH, self._one_block.bW = s.T, s.H, s.W
 
-    def forward(self, step: int, q, k, v, o_out, rotary=None, weights=None) -> str:
-        """Runs step `step`; returns which path ran ("dense" or "sparse").  rotary, weights: as for VmobaLayer.forward()."""
+    def forward(self, step: int, q, k, v, o_out, rotary=None, weights=None, projection=None, projected=None) -> str:
+        """Runs step `step`; returns which path ran ("dense" or "sparse").  rotary, weights, projection, projected: as for
+        VmobaLayer.forward()."""
         if self.schedule[step]:
             # the dense kernels take [B, heads, S, d].  The tokens stay in raster order: the running maximum that a row's
             # weights are rounded against, and with it the last bits of o, depends on the order of the keys.
@@ -664,6 +704,10 @@ class SteppedAttention:
             else:
                 vb.vmoba_partition_many(one, 0, (q, k, v), (qd, kd, vd), [L.raster_strides(x) for x in (q, k, v)])
             vb.vmoba_full_attn(L.shape, qd, kd, vd, od, self._lse, dev_status=L.dev_status)
+            if projection is not None:       # (od has the tokens in raster order)
+                L._projects(projection, projected)
+                projection.forward(od, out=o_out, **projected)
+                return "dense"
             # (an o_out whose elements share memory goes through copy_, which refuses it)
             shared = any(st == 0 and n > 1 for st, n in zip(o_out.stride(), o_out.shape))
             o = o_out if L.partitions(o_out) and not shared else fresh(o_out)
@@ -671,7 +715,7 @@ class SteppedAttention:
             if o is not o_out:
                 o_out.copy_(o)
             return "dense"
-        self.layer.forward(q, k, v, self.tau, o_out, rotary=rotary, weights=weights)
+        self.layer.forward(q, k, v, self.tau, o_out, rotary=rotary, weights=weights, projection=projection, projected=projected)
         return "sparse"
 
 
