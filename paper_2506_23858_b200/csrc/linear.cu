@@ -78,7 +78,8 @@ struct Prep {
   const void* kept;                          // [rows, cols or 2 cols] dense, in the order of x
   const float* gate;
   long long gb, gg;
-  const int* inv;                            // place in the order of x of every token of d_out
+  const int* inv;                            // place in the order of x of every token of d_out, or (by_place: a sample is one group, so that
+  bool by_place;                             // its rows come in any order) token of d_out of every place
   void* du;                                  // as kept
   void* du_low;                              // what du's rounding left (not with kept)
   void* y;                                   // act(kept) again, [rows, cols]
@@ -104,11 +105,11 @@ __global__ void __launch_bounds__(256) prep_kernel(Prep p) {
     const T* d_row = static_cast<const T*>(p.d) + b * p.db + c;
 #pragma unroll 2
     for (int t = t0 + warp; t < t1; t += 8) {
-      const int at = p.inv ? __ldg(p.inv + t) : t;
-      if (at < 0) continue;
+      const int other = p.inv ? __ldg(p.inv + t) : t, at = p.by_place ? t : other, from = p.by_place ? other : t;
+      if ((unsigned)at >= (unsigned)p.S) continue;
       const long long r = (long long)b * p.S + at;
-      float d[8], u[8], v[8];
-      load_vec<8>(d_row + t * p.dt, d);
+      float d[8] = {}, u[8], v[8];
+      if ((unsigned)from < (unsigned)p.S) load_vec<8>(d_row + from * p.dt, d);      // (a place without a token has no gradient)
       if (p.kept) {
         load_vec<8>(static_cast<const T*>(p.kept) + r * wide + c, u);
         if (GATED) load_vec<8>(static_cast<const T*>(p.kept) + r * wide + p.cols + c, v);
@@ -168,18 +169,21 @@ __global__ void __launch_bounds__(256) prep_kernel(Prep p) {
   if (p.part_g) add_up(sg, p.part_g + (long long)blockIdx.x * p.cols);
 }
 
-// place in the order of x of every token (-1: no place), from the token of every place
-__global__ void __launch_bounds__(256) no_place_kernel(int S, int* inv) {
+// Place in the order of x of every token, from the token of every place: the last one where it has several, -1 where it has none.  Places that
+// no token leads to have a gradient of zero.
+__global__ void __launch_bounds__(256) no_place_kernel(int S, int* inv, uint4* du, long long vecs) {
   if (!grid_begin()) return;
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < S) inv[i] = -1;
+  const long long n = (long long)gridDim.x * 256;
+  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < S; i += n) inv[i] = -1;
+  if (du)
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < vecs; i += n) du[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 __global__ void __launch_bounds__(256) place_kernel(int S, const int* perm, int* inv) {
   if (!grid_begin()) return;
   const int i = blockIdx.x * 256 + threadIdx.x;
   if (i < S) {
     const int t = __ldg(perm + i);
-    if ((unsigned)t < (unsigned)S) inv[t] = i;
+    if ((unsigned)t < (unsigned)S) atomicMax(inv + t, i);
   }
 }
 
@@ -199,38 +203,51 @@ int chunks_of(const Dims& D) { return D.B * D.G * ((D.gt + kChunk - 1) / kChunk)
 }  // namespace
 
 // ---------------------------------------------------------------- sums of chunks
-// out[g][c] = sum over the group's chunks of part[chunk][c]: a CTA has 32 columns of a group, a warp every eighth chunk.
-template <typename O>
-__global__ void __launch_bounds__(256) sum_chunks_kernel(const float* part, int cols, int per, int tiles, O* out) {
+// out[g][c] = sum over the `per` chunks of group g of part[chunk][c]: a CTA has 32 columns of a group, a warp every eighth chunk.  Two such sums
+// in one launch.
+struct ChunkSum {
+  const float* part = nullptr;
+  void* out = nullptr;
+  int cols = 0, groups = 0, per = 0, tiles = 0, bf16 = 0;
+};
+__global__ void __launch_bounds__(256) sum_chunks_kernel(ChunkSum a, ChunkSum b) {
   if (!grid_begin()) return;
   __shared__ float s[8][33];
-  const int g = blockIdx.x / tiles, c = (blockIdx.x - g * tiles) * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
-  float a = 0.f;
-  if (c < cols) {
-    const float* from = part + (long long)g * per * cols + c;
+  const int first = a.tiles * a.groups;
+  const bool second = (int)blockIdx.x >= first;
+  const ChunkSum& p = second ? b : a;
+  const int i = second ? blockIdx.x - first : blockIdx.x;
+  const int g = i / p.tiles, c = (i - g * p.tiles) * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+  float sum = 0.f;
+  if (c < p.cols) {
+    const float* from = p.part + (long long)g * p.per * p.cols + c;
 #pragma unroll 8
-    for (int i = w; i < per; i += 8) a += from[(long long)i * cols];
+    for (int k = w; k < p.per; k += 8) sum += from[(long long)k * p.cols];
   }
-  s[w][threadIdx.x & 31] = a;
+  s[w][threadIdx.x & 31] = sum;
   __syncthreads();
-  if (w == 0 && c < cols) {
+  if (w == 0 && c < p.cols) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) a += s[i][threadIdx.x];
-    out[(long long)g * cols + c] = from_f32<O>(a);
+    for (int k = 1; k < 8; ++k) sum += s[k][threadIdx.x];
+    const long long at = (long long)g * p.cols + c;
+    if (p.bf16) static_cast<__nv_bfloat16*>(p.out)[at] = from_f32<__nv_bfloat16>(sum);
+    else static_cast<float*>(p.out)[at] = sum;
   }
 }
-int sum_chunks(const float* part, int cols, int groups, int per, void* out, bool bf16, cudaStream_t st) {
-  const int tiles = (cols + 31) / 32;
-  if ((long long)groups * tiles > INT32_MAX) return VMOBA_ERR_SHAPE;
-  if (bf16) launch_kernel(sum_chunks_kernel<__nv_bfloat16>, (unsigned)(groups * tiles), 256, 0, st, part, cols, per, tiles, (__nv_bfloat16*)out);
-  else launch_kernel(sum_chunks_kernel<float>, (unsigned)(groups * tiles), 256, 0, st, part, cols, per, tiles, (float*)out);
+static int sum_chunks(ChunkSum a, ChunkSum b, cudaStream_t st) {
+  a.tiles = (a.cols + 31) / 32;
+  b.tiles = (b.cols + 31) / 32;
+  const long long ctas = (long long)a.groups * a.tiles + (long long)b.groups * b.tiles;
+  if (ctas > INT32_MAX) return VMOBA_ERR_SHAPE;
+  if (ctas == 0) return VMOBA_OK;
+  launch_kernel(sum_chunks_kernel, (unsigned)ctas, 256, 0, st, a, b);
   VMOBA_LAUNCH_OK(1);
   return VMOBA_OK;
 }
 
-size_t product_scratch(const Product& p) { return p.bf16 && !few_takes(p) ? tc_scratch(p) : 0; }
+size_t product_scratch(const Product& p) { return !p.bf16 ? simt_scratch(p) : few_takes(p) ? 0 : tc_scratch(p); }
 int run_product(const Product& p, float* scratch, cudaStream_t st) {
-  if (!p.bf16) return simt_product(p, st);
+  if (!p.bf16) return simt_product(p, scratch, st);
   return few_takes(p) ? few_product(p, st) : tc_product(p, scratch, st);
 }
 
@@ -393,11 +410,10 @@ int prepare(const Dims& D, Prep p, const Scratch& s, void* du, void* db, float* 
   p.part_g = dgate ? s.part_g : nullptr;
   const int chunks = chunks_of(D);
   if (int rc = run_prep(p, D.dtype == VMOBA_BF16, chunks, st)) return rc;
-  if (db)
-    if (int rc = sum_chunks(s.part_b, D.wide, 1, chunks, db, D.dtype == VMOBA_BF16, st)) return rc;
-  if (dgate)
-    if (int rc = sum_chunks(s.part_g, D.out, D.B * D.G, p.cpg, dgate, false, st)) return rc;
-  return VMOBA_OK;
+  ChunkSum b, g;
+  if (db) b = ChunkSum{s.part_b, db, D.wide, 1, chunks, 0, D.dtype == VMOBA_BF16};
+  if (dgate) g = ChunkSum{s.part_g, dgate, D.out, D.B * D.G, p.cpg, 0, 0};
+  return sum_chunks(b, g, st);
 }
 
 }  // namespace
@@ -455,14 +471,18 @@ extern "C" int vmoba_linear_bwd(const vmoba_linear_shape* shape, const void* d_o
   if (!gate) D = ungrouped(D);
   VMOBA_GUARDS_ARM(s.guards, st);
   Prep p = prep_of(D, d_out, d_out_strides, gate, gate_strides, acts || dgate ? kept : nullptr);
-  if (perm) {
-    launch_kernel(no_place_kernel, (unsigned)((D.S + 255) / 256), 256, 0, st, D.S, s.inv);
+  // (nothing stands between d_out and du in the simplest layer)
+  const bool apart = (acts || gate || perm) && (dx || dweight);
+  if (perm && D.G == 1) {
+    p.inv = perm;
+    p.by_place = true;
+  } else if (perm) {
+    launch_kernel(no_place_kernel, (unsigned)(4 * sm_count()), 256, 0, st, D.S, s.inv, apart ? reinterpret_cast<uint4*>(s.du) : nullptr,
+                  D.rows * D.wide * D.es / 16);
     launch_kernel(place_kernel, (unsigned)((D.S + 255) / 256), 256, 0, st, D.S, perm, s.inv);
     VMOBA_LAUNCH_OK(2);
     p.inv = s.inv;
   }
-  // (nothing stands between d_out and du in the simplest layer)
-  const bool apart = (acts || gate || perm) && (dx || dweight);
   if (apart || dbias || dgate)
     if (int rc = prepare(D, p, s, apart ? s.du : nullptr, dbias, dgate, st)) return rc;
   const Matrix du = apart ? tokens(s.du, D, D.wide) : raster(d_out, d_out_strides, D, D.out);
@@ -550,7 +570,7 @@ extern "C" int vmoba_ffn_bwd(const vmoba_linear_shape* shape, const void* d_out,
     q.e.col_sums = db_up ? s.part_b : nullptr;
     if (int rc = run_product(q, s.product, st)) return rc;
     if (db_up)
-      if (int rc = sum_chunks(s.part_b, up.wide, 1, (int)((up.rows + 31) / 32), db_up, true, st)) return rc;
+      if (int rc = sum_chunks(ChunkSum{s.part_b, db_up, up.wide, 1, (int)((up.rows + 31) / 32), 0, 1}, {}, st)) return rc;
   } else if (through || dw_down) {           // (fp32: d_up in the place of dh, where it is not gated; for h alone any gradient does)
     if (through)
       if (int rc = run_product(dx_product(down, d_down, w_down, tokens(s.dh, down, down.in), dev_status), s.product, st)) return rc;

@@ -70,14 +70,12 @@ size_t product_scratch(const Product& p);
 int run_product(const Product& p, float* scratch, cudaStream_t st);
 
 // fp32 (linear_simt.cu), bf16 (linear_tc.cu), and of those the products of a few tokens with a weight (linear_few.cu).
-int simt_product(const Product& p, cudaStream_t st);
+size_t simt_scratch(const Product& p);
+int simt_product(const Product& p, float* scratch, cudaStream_t st);
 size_t tc_scratch(const Product& p);
 int tc_product(const Product& p, float* scratch, cudaStream_t st);
 bool few_takes(const Product& p);
 int few_product(const Product& p, cudaStream_t st);
-
-// out[g][c] = sum over the `per` chunks of group g of part[chunk][c], by rows of `cols` floats; of the layer's type (linear.cu).
-int sum_chunks(const float* part, int cols, int groups, int per, void* out, bool bf16, cudaStream_t st);
 
 #ifdef __CUDACC__
 // gelu in its tanh form, u s(2 k (u + c u^3)), and silu, u s(u), of the logistic function s = 1 / (1 + exp(-x)), whose exp overflows for very
@@ -219,6 +217,45 @@ __device__ __forceinline__ void finish(const Epilogue& e, const OutRow<T>& row, 
   if (!row.ok) return;
   const int h = e.inner == e.cols ? 0 : e.by_inner.div(c);
   store_vec<V>(row.out + h * e.oh + (c - h * e.inner), u);
+}
+
+// Sums of slices of the summed index: part[slice][row][column of the sums] (N columns, gated: twice as many).
+struct Slices {
+  const float* part;
+  long long rows;
+  int N, wide, count;
+};
+// ... added in order, and what becomes of them.
+template <typename T, int KIND>
+__global__ void __launch_bounds__(256) join_kernel(Slices p, Epilogue e, FastDiv by_vecs, int vecs, int total) {
+  if (!grid_begin()) return;
+  const long long slice = p.rows * p.wide;
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < total; i += gridDim.x * 256) {
+    const int r = by_vecs.div(i), c = (i - r * vecs) * 8;
+    const float* from = p.part + (long long)r * p.wide + c;
+    float u[8] = {}, v[8] = {};
+#pragma unroll 4
+    for (int s = 0; s < p.count; ++s, from += slice) {
+      float t[8];
+      load_vec<8>(from, t);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) u[x] += t[x];
+      if (KIND == kGated) {
+        load_vec<8>(from + p.N, t);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] += t[x];
+      }
+    }
+    finish<T, 8, KIND>(e, OutRow<T>(e, r), c, u, v);
+  }
+}
+template <typename T, int KIND>
+int join(const Slices& p, const Epilogue& e, cudaStream_t st) {
+  const long long vecs = p.N / 8, total = p.rows * vecs;
+  launch_kernel(join_kernel<T, KIND>, (unsigned)((total + 255) / 256 < 16 * sm_count() ? (total + 255) / 256 : 16 * sm_count()), 256, 0, st, p, e,
+                FastDiv((unsigned)vecs), (int)vecs, (int)total);
+  VMOBA_LAUNCH_OK(1);
+  return VMOBA_OK;
 }
 #endif
 

@@ -1,6 +1,9 @@
 // Matrix products on the CUDA cores, in fp32: the operators' fp32 form.
 // D tiles of 128 x 128 or 64 x 64 by CTAs of as many threads as there are 8 x 8 (4 x 4) pieces, 16 summed indices at a time through shared
-// memory, the next 16 on their way in registers.
+// memory, the next 16 on their way in registers.  Where tiles are few the summed index is cut into slices, whose sums a second kernel adds in a
+// fixed order.
+#include <algorithm>
+
 #include "linear.cuh"
 
 namespace vmoba {
@@ -22,6 +25,8 @@ struct Args {
   Matrix a, b;
   FastDiv a_S, a_inner, b_S, b_inner;
   int a_rows, b_rows, M, N, K;
+  int per, slices;                           // summed indices of a slice
+  float* part;                               // [slice][row][column of the sums]
   Epilogue e;
 };
 
@@ -72,8 +77,9 @@ __global__ void __launch_bounds__((TILE / P) * (TILE / P)) product_kernel(Args p
       *reinterpret_cast<float4*>(&s[i / (TILE / 4)][i % (TILE / 4) * 4]) = v;
     }
   };
-  load(0);
-  for (int k0 = 0; k0 < p.K; k0 += BK) {
+  const int k_first = blockIdx.z * p.per, k_end = min(k_first + p.per, p.K);      // (per is a multiple of BK: nobody reads beyond a slice)
+  load(k_first);
+  for (int k0 = k_first; k0 < k_end; k0 += BK) {
     __syncthreads();
 #pragma unroll
     for (int l = 0; l < LOADS; ++l) {
@@ -82,7 +88,7 @@ __global__ void __launch_bounds__((TILE / P) * (TILE / P)) product_kernel(Args p
       for (int w = 0; w < NB; ++w) put(sB[w], B_ROWS, t + l * THREADS, rb[w][l]);
     }
     __syncthreads();
-    if (k0 + BK < p.K) load(k0 + BK);
+    if (k0 + BK < k_end) load(k0 + BK);
 #pragma unroll
     for (int k = 0; k < BK; ++k) {
       float a[P];
@@ -105,6 +111,18 @@ __global__ void __launch_bounds__((TILE / P) * (TILE / P)) product_kernel(Args p
   for (int i = 0; i < P; ++i) {
     const int r = m0 + ty * P + i;
     if (r >= p.M) break;
+    if (p.part) {
+      const int wide = TWO ? 2 * p.N : p.N;
+      float* to = p.part + ((long long)blockIdx.z * p.M + r) * wide;
+#pragma unroll
+      for (int j = 0; j < GROUPS; ++j) {
+        const int c = n0 + tx * 4 + j * (TILE / GROUPS);
+        if (c >= p.N) continue;
+#pragma unroll
+        for (int w = 0; w < NB; ++w) store4(to + w * p.N + c, make_float4(acc[w][i][4 * j], acc[w][i][4 * j + 1], acc[w][i][4 * j + 2], acc[w][i][4 * j + 3]));
+      }
+      continue;
+    }
     const OutRow<T> row(p.e, r);
 #pragma unroll
     for (int j = 0; j < GROUPS; ++j) {
@@ -120,16 +138,28 @@ __global__ void __launch_bounds__((TILE / P) * (TILE / P)) product_kernel(Args p
 
 template <typename T, int FORM, int KIND, int TILE, int P>
 int launch(const Args& a, cudaStream_t st) {
-  launch_kernel(product_kernel<T, FORM, KIND, TILE, P>, dim3((unsigned)((a.M + TILE - 1) / TILE), (unsigned)((a.N + TILE - 1) / TILE)),
+  launch_kernel(product_kernel<T, FORM, KIND, TILE, P>, dim3((unsigned)((a.M + TILE - 1) / TILE), (unsigned)((a.N + TILE - 1) / TILE), (unsigned)a.slices),
                 (TILE / P) * (TILE / P), 0, st, a);
   VMOBA_LAUNCH_OK(1);
-  return VMOBA_OK;
+  return a.part ? join<T, KIND>(Slices{a.part, a.M, a.N, KIND == kGated ? 2 * a.N : a.N, a.slices}, a.e, st) : VMOBA_OK;
 }
 
-template <typename T>
-int by_form(const Product& p, const Args& a, cudaStream_t st) {
-  // the large tile where it gives every SM one
-  const bool large = p.e.kind != kGated && (long long)((a.M + 127) / 128) * ((a.N + 127) / 128) >= sm_count();
+// Whether tiles are 128 x 128 (where that gives every SM one), and slices: up to four CTAs of the small tiles an SM, of 128 summed indices at least.
+struct Cut { bool large; int per, slices; };
+Cut cut_of(const Product& p) {
+  constexpr int kSms = 148;                  // (a workspace's size goes by the shape alone)
+  Cut c;
+  const long long K = p.form == kColsCols ? (long long)p.a.B * p.a.S : p.a.cols;
+  c.large = p.e.kind != kGated && (long long)((p.M + 127) / 128) * ((p.N + 127) / 128) >= kSms;
+  const long long tiles = (long long)((p.M + 63) / 64) * ((p.N + 63) / 64);
+  long long n = c.large ? 1 : std::max<long long>(1, std::min<long long>(4 * kSms / tiles, K / 128));
+  c.per = (int)((K + n - 1) / n + BK - 1) / BK * BK;
+  c.slices = (int)((K + c.per - 1) / c.per);
+  return c;
+}
+
+int by_form(const Product& p, const Args& a, bool large, cudaStream_t st) {
+  using T = float;
   if (p.form == kColsCols) return large ? launch<T, kColsCols, kPlain, 128, 8>(a, st) : launch<T, kColsCols, kPlain, 64, 4>(a, st);
   if (p.form == kRowsCols) return large ? launch<T, kRowsCols, kPlain, 128, 8>(a, st) : launch<T, kRowsCols, kPlain, 64, 4>(a, st);
   if (p.e.kind == kGated) return launch<T, kRowsRows, kGated, 64, 4>(a, st);
@@ -138,14 +168,22 @@ int by_form(const Product& p, const Args& a, cudaStream_t st) {
 
 }  // namespace
 
-int simt_product(const Product& p, cudaStream_t st) {
+size_t simt_scratch(const Product& p) {
+  const Cut c = cut_of(p);
+  return c.slices > 1 ? (size_t)c.slices * p.M * p.N * (p.e.kind == kGated ? 2 : 1) : 0;
+}
+
+int simt_product(const Product& p, float* scratch, cudaStream_t st) {
   Args a;
+  const Cut c = cut_of(p);
+  a.per = c.per; a.slices = c.slices;
+  a.part = c.slices > 1 ? scratch : nullptr;
   a.a = p.a; a.b = p.b; a.e = p.e; a.M = p.M; a.N = p.N;
   a.a_S = FastDiv((unsigned)p.a.S); a.a_inner = FastDiv((unsigned)p.a.inner);
   a.b_S = FastDiv((unsigned)p.b.S); a.b_inner = FastDiv((unsigned)p.b.inner);
   a.a_rows = p.a.B * p.a.S; a.b_rows = p.b.B * p.b.S;
   a.K = p.form == kColsCols ? a.a_rows : p.a.cols;
-  return by_form<float>(p, a, st);
+  return by_form(p, a, c.large, st);
 }
 
 }  // namespace linear

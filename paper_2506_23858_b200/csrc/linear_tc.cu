@@ -141,6 +141,12 @@ __device__ __forceinline__ Item item_of(const Args& p, int i) {
   return {split, sample, (rt - sample * p.rows_tiles) * 2 * BM, col * COLS};
 }
 
+// Columns of the sums that a tile works out: 256, fewer in the last tile of columns, by 64 (4,104 columns: 16 tiles and a quarter, not 17).
+template <int KIND>
+__device__ __forceinline__ int columns_of(const Args& p, const Item& it) {
+  return KIND == kGated ? BN : min(BN, (p.N - it.col + 63) & ~63);
+}
+
 template <int FORM, int KIND, int STORE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmOut,
@@ -187,7 +193,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         const Item it = item_of<KIND>(p, i);
         const int k0 = it.split * p.per, k1 = min(k0 + p.per, p.steps);
         const int row = it.row + (int)rank * BM;
-        const int col = KIND == kGated ? it.col + (int)rank * p.N : it.col + (int)rank * (BN / 2);
+        // (the second CTA has the other half of the tile's columns, of the factor's where gated)
+        const int col = KIND == kGated ? it.col + (int)rank * p.N : it.col + (int)rank * (columns_of<KIND>(p, it) / 2);
         for (int k = k0; k < k1; ++k) {
           if (!mbar_wait(&sm->empty[slot], par, abort_flag, p.status)) break;
           const uint32_t a = smem_u32(smem) + slot * STAGE_BYTES, b = a + HALF, bar = first_cta(&sm->full[slot]);
@@ -226,7 +233,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     // ------------------------------------------------------------------ products of the pair (the whole warp walks the loop, one lane issues)
     if (rank == 0) {
       const bool leader = elect_one();
-      constexpr uint32_t IDESC = make_idesc_bf16(2 * BM, BN, A_MN, B_MN);
       const uint32_t a_lo = desc_lo(smem_u32(smem), A_MN ? PANEL : 16), b_lo = desc_lo(smem_u32(smem) + HALF, B_MN ? PANEL : 16);
       uint32_t slot = 0, par = 0, n = 0;
       const int items = __reduce_max_sync(0xffffffffu, p.items);
@@ -234,6 +240,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         const Item it = item_of<KIND>(p, i);
         const int k0 = it.split * p.per, k1 = __reduce_max_sync(0xffffffffu, min(k0 + p.per, p.steps));
         const uint32_t acc = tmem + (n & 1) * BN;
+        const uint32_t idesc = __reduce_max_sync(0xffffffffu, make_idesc_bf16(2 * BM, columns_of<KIND>(p, it), A_MN, B_MN));
         mbar_wait_warp(&sm->acc_empty[n & 1], ((n >> 1) & 1) ^ 1, abort_flag, p.status);
         tc_fence_after();
         for (int k = k0; k < k1; ++k) {
@@ -242,7 +249,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
           const uint32_t at = slot * (STAGE_BYTES >> 4);
 #pragma unroll
           for (int s = 0; s < BK / 16; ++s)      // sixteen summed indices: 32 bytes of a row, or sixteen rows of 128 bytes
-            if (leader) pair_mma(acc, a_lo + at + s * (A_MN ? 128 : 2), b_lo + at + s * (B_MN ? 128 : 2), IDESC, k > k0 || s > 0 ? 1u : 0u);
+            if (leader) pair_mma(acc, a_lo + at + s * (A_MN ? 128 : 2), b_lo + at + s * (B_MN ? 128 : 2), idesc, k > k0 || s > 0 ? 1u : 0u);
           if (leader) pair_commit(&sm->empty[slot]);
           if (++slot == STAGES) { slot = 0; par ^= 1; }
         }
@@ -656,30 +663,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-// The slices' sums, and what becomes of them.
-template <int KIND>
-__global__ void __launch_bounds__(256) join_kernel(Args p, FastDiv by_vecs, int vecs, int total) {
-  if (!grid_begin()) return;
-  const long long slice = p.part_rows * p.wide;
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < total; i += gridDim.x * 256) {
-    const int r = by_vecs.div(i), c = (i - r * vecs) * 8;
-    const float* from = p.part + (long long)r * p.wide + c;
-    float u[8] = {}, v[8] = {};
-    for (int s = 0; s < p.splits; ++s, from += slice) {
-      float t[8];
-      load_vec<8>(from, t);
-#pragma unroll
-      for (int x = 0; x < 8; ++x) u[x] += t[x];
-      if (KIND == kGated) {
-        load_vec<8>(from + p.N, t);
-#pragma unroll
-        for (int x = 0; x < 8; ++x) v[x] += t[x];
-      }
-    }
-    finish<__nv_bfloat16, 8, KIND>(p.e, OutRow<__nv_bfloat16>(p.e, r), c, u, v);
-  }
-}
-
 // [inner, S, heads, B] of a matrix, boxes of `cols` columns (64, 32) x `rows` rows.
 bool map_of(CUtensorMap* map, const Matrix& m, int rows, int cols = 64) {
   EncodeTiledFn fn = encode_tiled_fn();
@@ -739,13 +722,7 @@ int start(K kernel, int store, const Args& a, const Maps& m, cudaStream_t st) {
 template <int FORM, int KIND>
 int launch(const Args& a, const Maps& m, bool boxes, cudaStream_t st) {
   if (int rc = boxes ? start(pair_kernel<FORM, KIND, kBoxes>, kBoxes, a, m, st) : start(pair_kernel<FORM, KIND, kRows>, kRows, a, m, st)) return rc;
-  if (a.splits > 1) {
-    const long long vecs = a.N / 8, total = a.part_rows * vecs;
-    launch_kernel(join_kernel<KIND>, (unsigned)std::min<long long>((total + 255) / 256, 16 * sm_count()), 256, 0, st, a, FastDiv((unsigned)vecs),
-                  (int)vecs, (int)total);
-    VMOBA_LAUNCH_OK(1);
-  }
-  return VMOBA_OK;
+  return a.splits > 1 ? join<__nv_bfloat16, KIND>(Slices{a.part, a.part_rows, a.N, a.wide, a.splits}, a.e, st) : VMOBA_OK;
 }
 
 }  // namespace tc
