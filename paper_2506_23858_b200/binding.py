@@ -534,7 +534,8 @@ def block_norm_workspace_bytes(shape) -> int:
 
 def norm_params(gate=None, gate_strides=(0, 0), scale=None, scale_strides=(0, 0), shift=None, shift_strides=(0, 0), weight=None, bias=None,
                 post_weight=None) -> NormParams:
-    return NormParams(_ptr(gate), _ptr(scale), _ptr(shift), _pair(gate_strides), _pair(scale_strides), _pair(shift_strides), _ptr(weight),
+    return NormParams(None if gate is None else gate.data_ptr(), None if scale is None else scale.data_ptr(),
+                      None if shift is None else shift.data_ptr(), _pair(gate_strides), _pair(scale_strides), _pair(shift_strides), _ptr(weight),
                       _ptr(bias), _ptr(post_weight))
 
 

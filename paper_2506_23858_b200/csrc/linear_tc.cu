@@ -675,8 +675,9 @@ bool map_of(CUtensorMap* map, const Matrix& m, int rows, int cols = 64) {
             cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// Samples that follow one another at the tokens' distance are one.
+// Samples that follow one another at the tokens' distance are one, and so are samples of one token.
 Matrix folded(Matrix m) {
+  if (m.B > 1 && m.S == 1) { m.S = m.B; m.st = m.sb; m.B = 1; m.sb = 0; }
   if (m.B > 1 && m.sb == (long long)m.S * m.st) { m.S *= m.B; m.B = 1; m.sb = 0; }
   return m;
 }

@@ -176,8 +176,10 @@ class _Rows:
 
     def _rows(self, x, channels, dtype, what, written=False):
         """x as the kernels can address it (an input that they cannot is copied) and its strides (batch, token)."""
-        size, dense = self._sizes.get(channels) or self._sizes.setdefault(
-            channels, (torch.Size((self.shape.B, self.shape.S, channels)), (self.shape.S * channels, channels)))
+        known = self._sizes.get(channels)
+        if known is None:
+            known = self._sizes[channels] = (torch.Size((self.shape.B, self.shape.S, channels)), (self.shape.S * channels, channels))
+        size, dense = known
         if x.shape != size or x.dtype is not dtype or x.device != self.device:
             raise ValueError(f"{type(self).__name__}: {what} has to be {dtype} {list(size)} on {self.device}")
         if x.is_contiguous() and x.data_ptr() % 16 == 0:
@@ -194,9 +196,9 @@ class _Rows:
         """Rows of a gate, scale or shift [B (or 1), groups, channels] and their strides (batch, group)."""
         if g is None:
             return None, (0, 0)
-        n, s = g.shape, self.shape
-        if len(n) != 3 or (n[0] != s.B and n[0] != 1) or n[1] != self._n_groups or n[2] != channels or g.dtype is not _F32 or g.device != self.device:
-            raise ValueError(f"{type(self).__name__}: {what} has to be fp32 [{s.B} or 1, {self._n_groups}, {channels}] on {self.device}")
+        n, B = g.shape, self._B
+        if len(n) != 3 or (n[0] != B and n[0] != 1) or n[1] != self._n_groups or n[2] != channels or g.dtype is not _F32 or g.device != self.device:
+            raise ValueError(f"{type(self).__name__}: {what} has to be fp32 [{B} or 1, {self._n_groups}, {channels}] on {self.device}")
         st = g.stride()
         sb, sg = 0 if n[0] == 1 else st[0], 0 if n[1] == 1 else st[1]
         if st[2] != 1 or g.data_ptr() % 16 or sb % 4 or sg % 4 or (sb and not channels <= sb < 2 ** 38) or (sg and not channels <= sg < 2 ** 38):
@@ -222,7 +224,7 @@ class _Rows:
 
     def _start(self, shape, device):
         self.shape, self.device = shape, _cuda_device(device, type(self).__name__)
-        self._n_groups, self._sizes = shape.groups, {}
+        self._n_groups, self._B, self._sizes = shape.groups, shape.B, {}
         self.dtype = torch_dtype(shape)
         self.dev_status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._nothing = torch.empty(256, dtype=torch.uint8, device=self.device)      # what calls take that need no scratch
@@ -380,8 +382,19 @@ class BlockNorm(_Rows):
 
     def _params(self, gate, scale, shift, weight, bias, post_weight):
         C = self.shape.C
-        (gate, gs), (scale, ss), (shift, hs) = (self._groups(g, C, n) for g, n in ((gate, "gate"), (scale, "scale"), (shift, "shift")))
-        weight, bias, post_weight = (self._dense(v, (C,), _F32, n) for v, n in ((weight, "weight"), (bias, "bias"), (post_weight, "post_weight")))
+        gs = ss = hs = (0, 0)
+        if gate is not None:
+            gate, gs = self._groups(gate, C, "gate")
+        if scale is not None:
+            scale, ss = self._groups(scale, C, "scale")
+        if shift is not None:
+            shift, hs = self._groups(shift, C, "shift")
+        if weight is not None:
+            weight = self._dense(weight, (C,), _F32, "weight")
+        if bias is not None:
+            bias = self._dense(bias, (C,), _F32, "bias")
+        if post_weight is not None:
+            post_weight = self._dense(post_weight, (C,), _F32, "post_weight")
         # (with what the pointers are of: copies live until the launch)
         return vb.norm_params(gate, gs, scale, ss, shift, hs, weight, bias, post_weight), (gate, scale, shift, weight, bias, post_weight)
 

@@ -56,15 +56,15 @@ def through(name, gated, u, ue, f32):
 
 def rows_of(g, S, tokens):
     """[B, groups, C] as [B, S, C]"""
-    at = torch.arange(S) // (tokens if tokens else S)
+    at = torch.arange(S, device=g.device) // (tokens if tokens else S)
     return g[:, at]
 
 
 def group_sums(x, tokens):
     B, S, C = x.shape
     tokens = tokens or S
-    out = torch.zeros(B, -(-S // tokens), C, dtype=x.dtype)
-    return out.index_add_(1, torch.arange(S) // tokens, x)
+    out = torch.zeros(B, -(-S // tokens), C, dtype=x.dtype, device=x.device)
+    return out.index_add_(1, torch.arange(S, device=x.device) // tokens, x)
 
 
 def linear(x, w, b, name="none", gated=False, gate=None, tokens=0, residual=None, f32=False, order=None, xe=None):
