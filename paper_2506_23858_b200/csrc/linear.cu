@@ -66,13 +66,19 @@ bool gate_ok(const float* gate, const int64_t* gs, const Dims& D) {
 }
 
 // ---------------------------------------------------------------- ahead of the backward's products
-constexpr int kChunk = 64;                   // rows of a chunk
 constexpr int kTile = 256;                   // columns of a CTA
+// Rows of a chunk: eight per warp, two of them under way at once; fewer where there would be less than three CTAs for an SM.
+int chunk_of(const Dims& D) {
+  int rows = 64;
+  while (rows > 8 && (long long)D.B * D.G * ((D.gt + rows - 1) / rows) * ((D.out + kTile - 1) / kTile) < 3 * 148) rows /= 2;
+  return rows;
+}
 
 struct Prep {
   int S, G, gt, cpg, cols, act;              // cpg: chunks per group
+  int chunk, tiles;                          // rows of a chunk; tiles of columns
   bool gated;
-  FastDiv by_cpg, by_G;
+  FastDiv by_cpg, by_G, by_tiles;
   const void* d;
   long long db, dt;
   const void* kept;                          // [rows, cols or 2 cols] dense, in the order of x
@@ -87,65 +93,99 @@ struct Prep {
   float* part_g;                             // [chunk][cols]
 };
 
+// Eight numbers as they lie in memory.
+template <typename T>
+struct Packed {
+  uint4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (auto& x : w) x = make_uint4(0u, 0u, 0u, 0u);
+  }
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  __device__ __forceinline__ void unpack(float (&x)[8]) const { load_vec<8>(reinterpret_cast<const T*>(w), x); }
+};
+
 template <typename T, bool GATED>
-__global__ void __launch_bounds__(256) prep_kernel(Prep p) {
+__global__ void __launch_bounds__(256, GATED ? 2 : 3) prep_kernel(Prep p) {
   if (!grid_begin()) return;
   constexpr bool EXACT = sizeof(T) == 4;
   __shared__ float s_sum[8][kTile];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int c = blockIdx.y * kTile + lane * 8;
-  const int gi = p.by_cpg.div(blockIdx.x), j = blockIdx.x - gi * p.cpg;      // group of all samples' and chunk of it
+  // (tiles of columns next to one another in time)
+  const int at_chunk = p.by_tiles.div(blockIdx.x), tile = blockIdx.x - at_chunk * p.tiles, c = tile * kTile + lane * 8;
+  const int gi = p.by_cpg.div(at_chunk), j = at_chunk - gi * p.cpg;          // group of all samples' and chunk of it
   const int b = p.by_G.div(gi), g = gi - b * p.G;
-  const int t0 = g * p.gt + j * kChunk, t1 = min(min(t0 + kChunk, (g + 1) * p.gt), p.S);
+  const int t0 = g * p.gt + j * p.chunk, t1 = min(min(t0 + p.chunk, (g + 1) * p.gt), p.S);
   const int wide = GATED ? 2 * p.cols : p.cols;
   float sb[8] = {}, sv[8] = {}, sg[8] = {};
   if (c < p.cols) {
     float gate[8];
     if (p.gate) load_vec<8>(p.gate + b * p.gb + g * p.gg + c, gate);
     const T* d_row = static_cast<const T*>(p.d) + b * p.db + c;
-#pragma unroll 2
-    for (int t = t0 + warp; t < t1; t += 8) {
-      const int other = p.inv ? __ldg(p.inv + t) : t, at = p.by_place ? t : other, from = p.by_place ? other : t;
-      if ((unsigned)at >= (unsigned)p.S) continue;
-      const long long r = (long long)b * p.S + at;
-      float d[8] = {}, u[8], v[8];
-      if ((unsigned)from < (unsigned)p.S) load_vec<8>(d_row + from * p.dt, d);      // (a place without a token has no gradient)
-      if (p.kept) {
-        load_vec<8>(static_cast<const T*>(p.kept) + r * wide + c, u);
-        if (GATED) load_vec<8>(static_cast<const T*>(p.kept) + r * wide + p.cols + c, v);
-      }
-      if (p.kept) {
-        float y[8];
-        by_activation(p.act, [&](auto act) {
+    constexpr int R = 2;
+#pragma unroll 1
+    for (int first = t0 + warp; first < t1; first += 8 * R) {
+      Packed<T> d_in[R], u_in[R], v_in[R];
+      long long row[R];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float2 a = activate_slope<EXACT, decltype(act)::value>(u[i]);
-            y[i] = GATED ? a.x * v[i] : a.x;
-            sg[i] = fmaf(d[i], y[i], sg[i]);
-            if (p.gate) d[i] *= gate[i];
-            if (GATED) {
-              const float dv = d[i] * a.x;
-              d[i] *= a.y * v[i];
-              v[i] = dv;
-              sv[i] += dv;
-            } else {
-              d[i] *= a.y;
+      for (int k = 0; k < R; ++k) {
+        const int t = first + 8 * k;
+        row[k] = -1;
+        d_in[k].clear();
+        if (t >= t1) continue;
+        const int other = p.inv ? __ldg(p.inv + t) : t, at = p.by_place ? t : other, from = p.by_place ? other : t;
+        if ((unsigned)at >= (unsigned)p.S) continue;
+        row[k] = (long long)b * p.S + at;
+        if ((unsigned)from < (unsigned)p.S) d_in[k].load(d_row + from * p.dt);      // (a place without a token has no gradient)
+        if (p.kept) {
+          u_in[k].load(static_cast<const T*>(p.kept) + row[k] * wide + c);
+          if (GATED) v_in[k].load(static_cast<const T*>(p.kept) + row[k] * wide + p.cols + c);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        const long long r = row[k];
+        if (r < 0) continue;
+        float d[8], u[8], v[8];
+        d_in[k].unpack(d);
+        if (p.kept) {
+          u_in[k].unpack(u);
+          if (GATED) v_in[k].unpack(v);
+          float y[8];
+          by_activation(p.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float2 a = activate_slope<EXACT, decltype(act)::value>(u[i]);
+              y[i] = GATED ? a.x * v[i] : a.x;
+              sg[i] = fmaf(d[i], y[i], sg[i]);
+              if (p.gate) d[i] *= gate[i];
+              if (GATED) {
+                const float dv = d[i] * a.x;
+                d[i] *= a.y * v[i];
+                v[i] = dv;
+                sv[i] += dv;
+              } else {
+                d[i] *= a.y;
+              }
             }
-          }
-        });
-        if (p.y) store_vec<8>(static_cast<T*>(p.y) + r * p.cols + c, y);
-        if (GATED && p.du) store_vec<8>(static_cast<T*>(p.du) + r * wide + p.cols + c, v);
-      } else if (p.gate) {
+          });
+          if (p.y) store_vec<8>(static_cast<T*>(p.y) + r * p.cols + c, y);
+          if (GATED && p.du) store_vec<8>(static_cast<T*>(p.du) + r * wide + p.cols + c, v);
+        } else if (p.gate) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] *= gate[i];
-      }
+          for (int i = 0; i < 8; ++i) d[i] *= gate[i];
+        }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sb[i] += d[i];
-      if (p.du) store_vec<8>(static_cast<T*>(p.du) + r * wide + c, d);
-      if (p.du_low) {
+        for (int i = 0; i < 8; ++i) sb[i] += d[i];
+        if (p.du) store_vec<8>(static_cast<T*>(p.du) + r * wide + c, d);
+        if (p.du_low) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] -= to_f32<T>(from_f32<T>(d[i]));
-        store_vec<8>(static_cast<T*>(p.du_low) + r * wide + c, d);
+          for (int i = 0; i < 8; ++i) d[i] -= to_f32<T>(from_f32<T>(d[i]));
+          store_vec<8>(static_cast<T*>(p.du_low) + r * wide + c, d);
+        }
       }
     }
   }
@@ -154,7 +194,7 @@ __global__ void __launch_bounds__(256) prep_kernel(Prep p) {
     __syncthreads();
     store_vec<8>(&s_sum[warp][lane * 8], s);
     __syncthreads();
-    const int col = blockIdx.y * kTile + threadIdx.x;
+    const int col = tile * kTile + threadIdx.x;
     if (col < p.cols) {
       float a = 0.f;
 #pragma unroll
@@ -163,10 +203,10 @@ __global__ void __launch_bounds__(256) prep_kernel(Prep p) {
     }
   };
   if (p.part_b) {
-    add_up(sb, p.part_b + (long long)blockIdx.x * wide);
-    if (GATED) add_up(sv, p.part_b + (long long)blockIdx.x * wide + p.cols);
+    add_up(sb, p.part_b + (long long)at_chunk * wide);
+    if (GATED) add_up(sv, p.part_b + (long long)at_chunk * wide + p.cols);
   }
-  if (p.part_g) add_up(sg, p.part_g + (long long)blockIdx.x * p.cols);
+  if (p.part_g) add_up(sg, p.part_g + (long long)at_chunk * p.cols);
 }
 
 // Place in the order of x of every token, from the token of every place: the last one where it has several, -1 where it has none.  Places that
@@ -188,8 +228,11 @@ __global__ void __launch_bounds__(256) place_kernel(int S, const int* perm, int*
 }
 
 template <typename T>
-int run_prep(const Prep& p, int chunks, cudaStream_t st) {
-  const dim3 grid((unsigned)chunks, (unsigned)((p.cols + kTile - 1) / kTile));
+int run_prep(Prep p, int chunks, cudaStream_t st) {
+  p.tiles = (p.cols + kTile - 1) / kTile;
+  p.by_tiles = FastDiv((unsigned)p.tiles);
+  if ((long long)chunks * p.tiles > INT32_MAX) return VMOBA_ERR_SHAPE;
+  const unsigned grid = (unsigned)(chunks * p.tiles);
   if (p.gated) launch_kernel(prep_kernel<T, true>, grid, 256, 0, st, p);
   else launch_kernel(prep_kernel<T, false>, grid, 256, 0, st, p);
   VMOBA_LAUNCH_OK(1);
@@ -198,7 +241,7 @@ int run_prep(const Prep& p, int chunks, cudaStream_t st) {
 int run_prep(const Prep& p, bool bf16, int chunks, cudaStream_t st) {
   return bf16 ? run_prep<__nv_bfloat16>(p, chunks, st) : run_prep<float>(p, chunks, st);
 }
-int chunks_of(const Dims& D) { return D.B * D.G * ((D.gt + kChunk - 1) / kChunk); }
+int chunks_of(const Dims& D) { return D.B * D.G * ((D.gt + chunk_of(D) - 1) / chunk_of(D)); }
 
 }  // namespace
 
@@ -338,7 +381,7 @@ struct Ends {
 
 Prep prep_of(const Dims& D, const void* d, const int64_t* ds, const float* gate, const int64_t* gs, const void* kept) {
   Prep p{};
-  p.S = D.S; p.G = D.G; p.gt = D.gt; p.cpg = (D.gt + kChunk - 1) / kChunk; p.cols = D.out; p.act = D.act; p.gated = D.gated;
+  p.S = D.S; p.G = D.G; p.gt = D.gt; p.chunk = chunk_of(D); p.cpg = (D.gt + p.chunk - 1) / p.chunk; p.cols = D.out; p.act = D.act; p.gated = D.gated;
   p.by_cpg = FastDiv((unsigned)p.cpg); p.by_G = FastDiv((unsigned)D.G);
   p.d = d; p.db = D.B > 1 ? ds[0] : 0; p.dt = D.S > 1 ? ds[1] : 0;
   p.kept = kept;
@@ -351,6 +394,9 @@ Dims ungrouped(Dims D) {
   D.gt = D.S; D.G = 1;
   return D;
 }
+
+// Chunks of a layer's rows at most, with its groups or without.
+size_t most_chunks(const Dims& D) { return (size_t)std::max(chunks_of(D), chunks_of(ungrouped(D))); }
 
 struct Scratch {
   int* inv;
@@ -365,8 +411,8 @@ Scratch linear_scratch(const Dims& D, bool backward, void* ws) {
   if (backward) {
     s.inv = c.take<int>(D.heads ? D.S : 0);
     s.du = c.take<char>((size_t)D.rows * D.wide * D.es);
-    s.part_b = c.take<float>((size_t)chunks_of(D) * D.wide);
-    s.part_g = c.take<float>((size_t)chunks_of(D) * D.out);
+    s.part_b = c.take<float>(most_chunks(D) * D.wide);
+    s.part_g = c.take<float>(most_chunks(D) * D.out);
     s.product = c.take<float>(gradient_scratch(D));
   } else {
     s.product = c.take<float>(forward_scratch(D));
@@ -385,9 +431,9 @@ Scratch ffn_scratch(const Dims& D, bool backward, void* ws) {
     s.du = c.take<char>((size_t)D.rows * down.out * D.es * (bf16 ? 2 : 1));
     s.dh = c.take<char>(bf16 ? 0 : (size_t)D.rows * D.out * D.es);
     s.du_up = c.take<char>(bf16 || D.gated ? (size_t)D.rows * D.wide * D.es : 0);
-    const size_t chunks = chunks_of(D), blocks = (size_t)(D.rows + 31) / 32;
-    s.part_b = c.take<float>(std::max(chunks, bf16 ? blocks : 0) * std::max(up.wide, down.out));
-    s.part_g = c.take<float>(chunks * down.out);
+    const size_t of_up = bf16 ? (size_t)(D.rows + 31) / 32 : 0;      // (bf16: sums by 32 rows)
+    s.part_b = c.take<float>(std::max(std::max(most_chunks(up), of_up) * up.wide, most_chunks(down) * down.out));
+    s.part_g = c.take<float>(most_chunks(down) * down.out);
     s.product = c.take<float>(std::max(gradient_scratch(up), gradient_scratch(down, bf16 ? 2 : 1)));
   } else {
     s.product = c.take<float>(std::max(forward_scratch(up), forward_scratch(down)));
