@@ -573,16 +573,18 @@ __global__ void __launch_bounds__(256) vector_sums_kernel(Vectors p) {
   __shared__ float s[3][8][33];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   float a[3] = {};
-  if (c < p.C)
+  if (c < p.C) {
+#pragma unroll 4
     for (int gi = w; gi < p.groups; gi += 8) {
       const int b = gi / p.G, g = gi - b * p.G;
       const float* from = p.by_group + (long long)gi * 3 * p.C + c;
       const float m = p.scale ? 1.f + __ldg(p.scale + b * p.scale_s[0] + g * p.scale_s[1] + c) : 1.f;
       const float f = p.gate ? __ldg(p.gate + b * p.gate_s[0] + g * p.gate_s[1] + c) : 1.f;
-      a[0] = fmaf(from[0], m, a[0]);
-      a[1] = fmaf(from[p.C], m, a[1]);
-      a[2] = fmaf(from[2 * p.C], f, a[2]);
+      a[0] = fmaf(__ldg(from), m, a[0]);
+      a[1] = fmaf(__ldg(from + p.C), m, a[1]);
+      a[2] = fmaf(__ldg(from + 2 * p.C), f, a[2]);
     }
+  }
 #pragma unroll
   for (int k = 0; k < 3; ++k) s[k][w][lane] = a[k];
   __syncthreads();
