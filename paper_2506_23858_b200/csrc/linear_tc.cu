@@ -28,15 +28,16 @@ struct Args {
   Epilogue e;
   int Sm, rows_tiles, row_tiles, col_tiles;  // rows of a sample; tiles of rows per sample and of all; tiles of columns
   int N;                                     // columns of out
-  int steps, per, splits, items;             // stages of the summed index, of a slice; slices
+  int steps, items;                          // stages of the summed index; tiles and slices of tiles
+  int whole, rest, per, splits;              // tiles worked out at once; the other ones, stages of their slices, slices of each
   int a_inner, b_inner, b_samples;           // columns of a head; samples of b (those of a come twice, if it has two planes)
   int step_inner;                            // stages per sample (kColsCols), per plane
-  FastDiv by_rows_tiles, by_tiles, by_group, by_a_inner, by_b_inner, by_step, by_wide;
-  float* part;                               // [slice][row][column of the sums]
+  FastDiv by_rows_tiles, by_rest, by_group, by_a_inner, by_b_inner, by_step, by_wide;
+  float* part;                               // [slice of a tile][256 rows][256 columns]
   int wide;                                  // columns of the sums
-  long long part_rows;
   int32_t* status;
 };
+constexpr long long PART = 2ll * BM * BN;    // floats of a slice of a tile
 
 struct Shared {
   uint64_t full[MOST_STAGES], empty[MOST_STAGES], acc_full[2], acc_empty[2], ahead[EPI_WARPS], drain;
@@ -125,26 +126,45 @@ __device__ __forceinline__ float column_sum(float* x) {
 }
 
 struct Item {
-  int split, sample, row, col;               // first row of the pair's tile in the sample; first column of out
+  int slice, k0, k1;                         // -1: a whole tile; its stages
+  int sample, row, col;                      // first row of the pair's tile in the sample; first column of out
 };
 // Tiles in groups of eight tiles of rows, down the rows first: the tiles that run at a time share rows and columns.
 template <int KIND>
 __device__ __forceinline__ Item item_of(const Args& p, int i) {
   constexpr int G = 8, COLS = KIND == kGated ? BN / 2 : BN;
-  const int split = p.by_tiles.div(i);
-  int t = i - split * p.row_tiles * p.col_tiles;
+  int t = i, slice = -1, k0 = 0, k1 = p.steps;
+  if (i >= p.whole) {                        // slice after slice of the last tiles
+    slice = i - p.whole;
+    const int s = p.by_rest.div(slice);
+    t = i - s * p.rest;
+    k0 = s * p.per;
+    k1 = min(k0 + p.per, p.steps);
+  }
   const int group = p.by_group.div(t);       // (by G * col_tiles)
   t -= group * G * p.col_tiles;
   const int high = min(G, p.row_tiles - group * G);
   const int col = t / high, rt = group * G + t - col * high;
   const int sample = p.by_rows_tiles.div(rt);
-  return {split, sample, (rt - sample * p.rows_tiles) * 2 * BM, col * COLS};
+  return {slice, k0, k1, sample, (rt - sample * p.rows_tiles) * 2 * BM, col * COLS};
 }
 
 // Columns of the sums that a tile works out: 256, fewer in the last tile of columns, by 64 (4,104 columns: 16 tiles and a quarter, not 17).
 template <int KIND>
 __device__ __forceinline__ int columns_of(const Args& p, const Item& it) {
   return KIND == kGated ? BN : min(BN, (p.N - it.col + 63) & ~63);
+}
+
+// A warp's half of the columns of a slice of a tile, as they are; lane = row.
+__device__ __forceinline__ void store_part(uint32_t tmem, float* to) {
+#pragma unroll 1
+  for (int c = 0; c < BN / 2; c += 32) {
+    uint32_t v[32];
+    tmem_ld32(tmem + c, v);
+    tmem_ld_wait();
+#pragma unroll
+    for (int j = 0; j < 32; j += 8) st_global_v8(static_cast<void*>(to + c + j), v[j], v[j + 1], v[j + 2], v[j + 3], v[j + 4], v[j + 5], v[j + 6], v[j + 7]);
+  }
 }
 
 template <int FORM, int KIND, int STORE>
@@ -191,11 +211,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       uint32_t slot = 0, par = 1, n = 0;     // (the first pass through the ring waits for nothing)
       for (int i = pair; i < p.items && !*abort_flag; i += pairs) {
         const Item it = item_of<KIND>(p, i);
-        const int k0 = it.split * p.per, k1 = min(k0 + p.per, p.steps);
         const int row = it.row + (int)rank * BM;
         // (the second CTA has the other half of the tile's columns, of the factor's where gated)
         const int col = KIND == kGated ? it.col + (int)rank * p.N : it.col + (int)rank * (columns_of<KIND>(p, it) / 2);
-        for (int k = k0; k < k1; ++k) {
+        for (int k = it.k0; k < it.k1; ++k) {
           if (!mbar_wait(&sm->empty[slot], par, abort_flag, p.status)) break;
           const uint32_t a = smem_u32(smem) + slot * STAGE_BYTES, b = a + HALF, bar = first_cta(&sm->full[slot]);
           if (rank == 0) mbar_expect_tx(&sm->full[slot], 2 * STAGE_BYTES);
@@ -238,7 +257,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       const int items = __reduce_max_sync(0xffffffffu, p.items);
       for (int i = pair; i < items; i += pairs, ++n) {
         const Item it = item_of<KIND>(p, i);
-        const int k0 = it.split * p.per, k1 = __reduce_max_sync(0xffffffffu, min(k0 + p.per, p.steps));
+        const int k0 = it.k0, k1 = __reduce_max_sync(0xffffffffu, it.k1);
         const uint32_t acc = tmem + (n & 1) * BN;
         const uint32_t idesc = __reduce_max_sync(0xffffffffu, make_idesc_bf16(2 * BM, columns_of<KIND>(p, it), A_MN, B_MN));
         mbar_wait_warp(&sm->acc_empty[n & 1], ((n >> 1) & 1) ^ 1, abort_flag, p.status);
@@ -262,7 +281,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
           if (mbar_try_wait(&sm->drain, 0)) break;
       }
     }
-  } else if (warp >= 4 && STORE == kBoxes) {
+  }
+  // What warps 4 to 11 do with slices of tiles, of which a pair has its last items.
+  auto slices = [&](int i, uint32_t n) {
+    const int quad = warp & 3, half = (warp - 4) >> 2;
+    for (; i < p.items; i += pairs, ++n) {
+      const Item it = item_of<KIND>(p, i);
+      mbar_wait_warp(&sm->acc_full[n & 1], (n >> 1) & 1, abort_flag, p.status);
+      tc_fence_after();
+      store_part(tmem + ((uint32_t)(quad * 32) << 16) + (n & 1) * BN + half * (BN / 2),
+                 p.part + it.slice * PART + ((int)rank * BM + quad * 32 + lane) * BN + half * (BN / 2));
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_at(first_cta(&sm->acc_empty[n & 1]));
+    }
+  };
+  if (warp >= 4 && STORE == kBoxes) {
     // ------------------------------------------------------------------ sums to results, box by box: lane = row
     const int quad = warp & 3, half = (warp - 4) >> 2;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
@@ -271,7 +305,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     constexpr int W = KIND == kGated ? 32 : 64, BOXES = 2;             // columns of a box; boxes of out per warp
     constexpr int COLS = KIND == kGated ? BN / 2 : BN;
     uint32_t n = 0, turns = 0;
-    for (int i = pair; i < p.items; i += pairs, ++n) {
+    int i = pair;
+    for (; i < p.whole; i += pairs, ++n) {
       const Item it = item_of<KIND>(p, i);
       const int row = it.row + (int)rank * BM + quad * 32;             // first row of the warp in the sample
       mbar_wait_warp(&sm->acc_full[n & 1], (n >> 1) & 1, abort_flag, p.status);
@@ -356,9 +391,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         emit(&tmOut, e.inner, e.by_inner, u, c);
       }
     }
+    slices(i, n);
     if (lane == 0) bulk_wait_group<0>();     // (the stores have been read from this CTA's memory and written before it exits)
   } else if (warp >= 4 && STORE == kRows) {
-    // ------------------------------------------------------------------ sums to results by rows: gate, residual, order of the rows, parts
+    // ------------------------------------------------------------------ sums to results by rows: gate, residual, order of the rows
     using T = __nv_bfloat16;
     const int quad = warp & 3, half = (warp - 4) >> 2;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
@@ -381,16 +417,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       o.b = o.g = 0;
       o.t = -1;
       o.gate = nullptr;
-      if (lane < o.rows && !p.part) {
+      if (lane < o.rows) {
         const int r = (int)o.first + lane;
         o.b = e.by_S.div(r);
         o.t = r - o.b * e.S;
-        if (KIND != kPlain && e.perm) o.t = __ldg(e.perm + o.t);
+        if (e.perm) o.t = __ldg(e.perm + o.t);
       }
       return o;
     };
     auto settle = [&](Place& o) {            // (what hangs on the loaded place)
-      if (KIND == kPlain || p.part) return;
       if ((unsigned)o.t >= (unsigned)e.S) o.t = -1;
       if (!e.gate) return;
       if (o.t >= 0) o.g = e.by_gate.div(o.t);
@@ -399,7 +434,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       const int b0 = __shfl_sync(0xffffffffu, o.b, from), g0 = __shfl_sync(0xffffffffu, o.g, from);
       if (__all_sync(0xffffffffu, o.t < 0 || (o.b == b0 && o.g == g0))) o.gate = e.gate + b0 * e.gb + g0 * e.gg;
     };
-    const bool onto = KIND != kPlain && e.residual && !p.part;
+    const bool onto = e.residual != nullptr;
     // What a box of columns needs from memory is asked for a box ahead: beside the operands' loads it takes microseconds, and loads come back
     // in the order they were asked for.  So bias and gate of the next box and the places of the next tile's rows go ahead of the next box's
     // residual, a row of which is asked for, into shared memory, when the last one there has been used.
@@ -417,7 +452,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     };
     auto load_columns = [&](const Place& o, int ch) {
       const int c = o.it.col + column(ch) + lc;
-      if (KIND == kPlain || p.part || c >= p.N) return;
+      if (c >= p.N) return;
       if (e.bias) {
         bias_in[0] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(e.bias) + c));
         if (KIND == kGated) bias_in[1] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(e.bias) + e.cols + c));
@@ -425,15 +460,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       if (o.gate) load_const<8>(o.gate + c, gate_in);
     };
     uint32_t n = 0;
-    Place next = tile_of(pair);
-    settle(next);
-    load_columns(next, 0);
-    if (onto)
+    int i = pair;
+    Place next;
+    if (i < p.whole) {
+      next = tile_of(i);
+      settle(next);
+      load_columns(next, 0);
+      if (onto)
 #pragma unroll
-      for (int q = 0; q < TURNS; ++q) load_residual(next, 0, q);
-    for (int i = pair; i < p.items; i += pairs, ++n) {
+        for (int q = 0; q < TURNS; ++q) load_residual(next, 0, q);
+    }
+    for (; i < p.whole; i += pairs, ++n) {
       const Place now = next;
-      const bool more = i + pairs < p.items;
+      const bool more = i + pairs < p.whole;
 #pragma unroll
       for (int ch = 0; ch < 2; ++ch) {
         const int at = column(ch), c = now.it.col + at + lc;
@@ -485,54 +524,45 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
               w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
             }
           }
-          if (p.part) {
-            if (col_ok && r < now.rows) {
-              float* to = p.part + ((long long)now.it.split * p.part_rows + now.first + r) * p.wide + c;
-              store_vec<8>(to, u);
-              if (KIND == kGated) store_vec<8>(to + p.N, w);
+          if (onto) asm volatile("cp.async.wait_group %0;" ::"n"(TURNS - 1) : "memory");      // (the oldest of TURNS rows is here)
+          const int b = __shfl_sync(0xffffffffu, now.b, r), t = __shfl_sync(0xffffffffu, now.t, r), g = __shfl_sync(0xffffffffu, now.g, r);
+          if (col_ok && r < now.rows) {
+            if (e.bias) {
+              add_bf16x8(u, bias[0]);
+              if (KIND == kGated) add_bf16x8(w, bias[1]);
             }
-            continue;
+            if (e.kept) {
+              T* kept = static_cast<T*>(e.kept) + (now.first + r) * p.wide + c;
+              store_vec<8>(kept, u);
+              if (KIND == kGated) store_vec<8>(kept + p.N, w);
+            }
+            by_activation(e.act, [&](auto act) {
+#pragma unroll
+              for (int x = 0; x < 8; ++x) u[x] = activate<false, decltype(act)::value>(u[x]);
+            });
+            if (KIND == kGated)
+#pragma unroll
+              for (int x = 0; x < 8; x += 2) mul2(u[x], u[x + 1], u[x], u[x + 1], w[x], w[x + 1]);
+            if (t >= 0) {
+              if (e.gate) {
+                if (!now.gate) load_const<8>(e.gate + b * e.gb + g * e.gg + c, gate);
+#pragma unroll
+                for (int x = 0; x < 8; x += 2) mul2(u[x], u[x + 1], u[x], u[x + 1], gate[x], gate[x + 1]);
+              }
+              if (e.residual) add_bf16x8(u, *reinterpret_cast<const uint4*>(mine_ahead + q * 512));
+              store_vec<8>(static_cast<T*>(e.out) + b * e.ob + t * e.ot + c, u);
+            }
           }
-          if constexpr (KIND != kPlain) {    // (plain sums come here in parts alone)
-            if (onto) asm volatile("cp.async.wait_group %0;" ::"n"(TURNS - 1) : "memory");      // (the oldest of TURNS rows is here)
-            const int b = __shfl_sync(0xffffffffu, now.b, r), t = __shfl_sync(0xffffffffu, now.t, r), g = __shfl_sync(0xffffffffu, now.g, r);
-            if (col_ok && r < now.rows) {
-              if (e.bias) {
-                add_bf16x8(u, bias[0]);
-                if (KIND == kGated) add_bf16x8(w, bias[1]);
-              }
-              if (e.kept) {
-                T* kept = static_cast<T*>(e.kept) + (now.first + r) * p.wide + c;
-                store_vec<8>(kept, u);
-                if (KIND == kGated) store_vec<8>(kept + p.N, w);
-              }
-              by_activation(e.act, [&](auto act) {
-#pragma unroll
-                for (int x = 0; x < 8; ++x) u[x] = activate<false, decltype(act)::value>(u[x]);
-              });
-              if (KIND == kGated)
-#pragma unroll
-                for (int x = 0; x < 8; x += 2) mul2(u[x], u[x + 1], u[x], u[x + 1], w[x], w[x + 1]);
-              if (t >= 0) {
-                if (e.gate) {
-                  if (!now.gate) load_const<8>(e.gate + b * e.gb + g * e.gg + c, gate);
-#pragma unroll
-                  for (int x = 0; x < 8; x += 2) mul2(u[x], u[x + 1], u[x], u[x + 1], gate[x], gate[x + 1]);
-                }
-                if (e.residual) add_bf16x8(u, *reinterpret_cast<const uint4*>(mine_ahead + q * 512));
-                store_vec<8>(static_cast<T*>(e.out) + b * e.ob + t * e.ot + c, u);
-              }
-            }
-            __syncwarp();
-            if (onto) {
-              if (ch == 0) load_residual(now, 1, q);
-              else if (more) load_residual(next, 0, q);
-              else asm volatile("cp.async.commit_group;" ::: "memory");
-            }
+          __syncwarp();
+          if (onto) {
+            if (ch == 0) load_residual(now, 1, q);
+            else if (more) load_residual(next, 0, q);
+            else asm volatile("cp.async.commit_group;" ::: "memory");
           }
         }
       }
     }
+    slices(i, n);
   } else if (warp >= 4 && STORE == kSlopes) {
     // ------------------------------------------------------------------ sums d to d act'(u) and act(u) (gated: d v act'(u), d act(u); act(u) v)
     // Lane = row; everything comes and goes in boxes by TMA.  (By rows of lanes, 64 or 128 bytes of each: 333 us instead of 277 for 13,440 rows of
@@ -556,7 +586,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       return reinterpret_cast<uint4*>(box + lane * (2 * W) + (W == 64 ? j ^ (lane & 7) : j ^ ((lane >> 1) & 3)) * 16);
     };
     uint32_t n = 0, boxes = 0;
-    Item next = item_of<KIND>(p, pair);
+    Item next = item_of<KIND>(p, pair);      // (tiles are whole here)
     if (lane == 0) ask(next, 0);
     for (int i = pair; i < p.items; i += pairs, ++n) {
       const Item now = next;
@@ -682,32 +712,64 @@ Matrix folded(Matrix m) {
   return m;
 }
 
-// Slices of the summed index: as many as make the time least, in tiles' times: rounds of the pairs / slices, and what the slices' sums cost
-// in memory (of a tile and slice, 256 KB out and in again at 6.5 TB/s shared by all, against a stage's 0.28 us).
-int slices(long long tiles, int steps, int pairs) {
-  int best = 1;
-  double least = 1e30;
-  for (int s = 1; s <= std::min(steps, 32); ++s) {
-    const int per = (steps + s - 1) / s;
-    if ((steps + per - 1) / per != s) continue;
-    const double rounds = (double)((tiles * s + pairs - 1) / pairs);
-    const double t = rounds * (per * 0.28 + 1.0) + (s > 1 ? 3.0 + tiles * s * 0.08 : 0.0);
-    if (t < least * 0.97) { least = t; best = s; }
+// Tiles worked out as a whole, in rounds of all pairs, and slices of the summed index of those that are left: as many as make the time least.
+// A stage takes 0.28 us, a tile another one at its ends, a slice 1.5 more for its sums in memory; joining them is a launch and the
+// sums' way through the L2.
+constexpr int kPairs = 74;                   // of B200's SMs (a workspace's size goes by the shape alone)
+struct Plan { int whole, rest, per, splits; };
+Plan plan_of(long long tiles, int steps, bool cut) {
+  Plan best{(int)tiles, 0, steps, 1};
+  if (!cut) return best;
+  double least = (double)((tiles + kPairs - 1) / kPairs) * (steps * 0.28 + 1.0);
+  for (long long whole = tiles / kPairs * kPairs; whole >= 0 && whole >= tiles / kPairs * kPairs - kPairs; whole -= kPairs) {
+    const long long rest = tiles - whole;
+    for (int s = 2; s <= std::min(steps, 32) && rest * s <= 8 * kPairs; ++s) {
+      const int per = (steps + s - 1) / s;
+      if ((steps + per - 1) / per != s || rest == 0) continue;
+      const double t = (double)(whole / kPairs) * (steps * 0.28 + 1.0) + (double)((rest * s + kPairs - 1) / kPairs) * (per * 0.28 + 2.5) + 3.0 + rest * s * 0.03;
+      if (t < least * 0.97) {
+        least = t;
+        best = Plan{(int)whole, (int)rest, per, s};
+      }
+    }
   }
   return best;
 }
-
-constexpr int kPairs = 74;                   // of B200's SMs (a workspace's size goes by the shape alone)
-struct Plan { int steps, per, splits; long long tiles; };
-Plan plan_of(const Product& p) {
+// Stages of a product's summed index.
+int steps_of(Form form, const Matrix& a, int planes) {
+  return planes * (form == kColsCols ? a.B * ((a.S + BK - 1) / BK) : (a.cols + BK - 1) / BK);
+}
+// Tiles, of as many samples as do not follow one another.
+long long tiles_of(const Product& p, int samples) {
   const int cols = p.e.kind == kGated ? BN / 2 : BN;
-  Plan o;
-  if (p.form == kColsCols) o.steps = p.planes * p.a.B * ((p.a.S + BK - 1) / BK);
-  else o.steps = p.planes * ((p.a.cols + BK - 1) / BK);
-  o.tiles = (long long)((p.M + 2 * BM - 1) / (2 * BM)) * ((p.N + cols - 1) / cols);
-  o.splits = p.e.kind >= kSlope ? 1 : slices(o.tiles, o.steps, kPairs);      // (sums of rows' gradients are of whole sums)
-  o.per = (o.steps + o.splits - 1) / o.splits;
-  return o;
+  const long long rows = (p.M / samples + 2 * BM - 1) / (2 * BM);
+  return rows * samples * ((p.N + cols - 1) / cols);
+}
+
+// The slices' sums of the last tiles, and what becomes of them: CTAs of 256 pieces of eight columns.
+template <int KIND>
+__global__ void __launch_bounds__(256) join_tiles_kernel(Args p) {
+  if (!grid_begin()) return;
+  constexpr int COLS = KIND == kGated ? BN / 2 : BN, PER_TILE = 2 * BM * COLS / 8 / 256;
+  const int tile = blockIdx.x / PER_TILE, piece = (blockIdx.x - tile * PER_TILE) * 256 + threadIdx.x;
+  const int r = piece / (COLS / 8), c = piece % (COLS / 8) * 8;
+  const Item it = item_of<KIND>(p, p.whole + tile);
+  if (it.row + r >= p.Sm || it.col + c >= p.N) return;
+  const float* from = p.part + tile * PART + r * BN + c;
+  float u[8] = {}, v[8] = {};
+#pragma unroll 2
+  for (int s = 0; s < p.splits; ++s, from += p.rest * PART) {
+    float t[8];
+    load_vec<8>(from, t);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) u[x] += t[x];
+    if (KIND == kGated) {
+      load_vec<8>(from + BN / 2, t);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) v[x] += t[x];
+    }
+  }
+  finish<__nv_bfloat16, 8, KIND>(p.e, OutRow<__nv_bfloat16>(p.e, it.sample * p.Sm + it.row + r), it.col + c, u, v);
 }
 
 struct Maps { CUtensorMap a, b, out, out2, kept, kept2, again; };      // (2: of the second half of the columns)
@@ -722,39 +784,44 @@ int start(K kernel, int store, const Args& a, const Maps& m, cudaStream_t st) {
 }
 template <int FORM, int KIND>
 int launch(const Args& a, const Maps& m, bool boxes, cudaStream_t st) {
-  if (int rc = boxes ? start(pair_kernel<FORM, KIND, kBoxes>, kBoxes, a, m, st) : start(pair_kernel<FORM, KIND, kRows>, kRows, a, m, st)) return rc;
-  return a.splits > 1 ? join<__nv_bfloat16, KIND>(Slices{a.part, a.part_rows, a.N, a.wide, a.splits}, a.e, st) : VMOBA_OK;
+  int rc;
+  if constexpr (KIND == kPlain) rc = start(pair_kernel<FORM, KIND, kBoxes>, kBoxes, a, m, st);
+  else rc = boxes ? start(pair_kernel<FORM, KIND, kBoxes>, kBoxes, a, m, st) : start(pair_kernel<FORM, KIND, kRows>, kRows, a, m, st);
+  if (rc || a.splits == 1) return rc;
+  launch_kernel(join_tiles_kernel<KIND>, (unsigned)a.rest * (2 * BM * (KIND == kGated ? BN / 2 : BN) / 8 / 256), 256, 0, st, a);
+  VMOBA_LAUNCH_OK(1);
+  return VMOBA_OK;
 }
 
 }  // namespace tc
 
+// For the samples' rows in one or not: strides decide that.
 size_t tc_scratch(const Product& p) {
-  const tc::Plan plan = tc::plan_of(p);
-  return plan.splits > 1 ? (size_t)plan.splits * p.M * p.N * (p.e.kind == kGated ? 2 : 1) : 0;
+  size_t most = 0;
+  for (int apart = 0; apart < 2; ++apart) {
+    Matrix a = p.a;
+    if (!apart && a.B > 1) { a.S *= a.B; a.B = 1; }
+    const tc::Plan plan = tc::plan_of(tc::tiles_of(p, p.form == kColsCols ? 1 : a.B), tc::steps_of(p.form, a, p.planes), p.e.kind < kSlope);
+    if (plan.splits > 1) most = std::max(most, (size_t)plan.rest * plan.splits * (size_t)tc::PART);
+  }
+  return most;
 }
 
 int tc_product(const Product& p, float* scratch, cudaStream_t st) {
   using namespace tc;
   Args a{};
-  const Plan plan = plan_of(p);
   Matrix ma = p.a, mb = p.b;
   const int cols = p.e.kind == kGated ? BN / 2 : BN;
   a.e = p.e;
   a.N = p.N;
   a.wide = is_gated(p.e.kind) ? 2 * p.N : p.N;
-  a.part_rows = p.M;
   a.status = p.status;
-  a.splits = plan.splits; a.steps = plan.steps; a.per = plan.per;
-  a.part = plan.splits > 1 ? scratch : nullptr;
   if (p.form == kColsCols) {
     if (folded(ma).B == 1 && folded(mb).B == 1) {
       ma = folded(ma);
       mb = folded(mb);
-      a.steps = p.planes * ((ma.S + BK - 1) / BK);      // (no more than before)
-      a.per = (a.steps + a.splits - 1) / a.splits;
-      a.splits = (a.steps + a.per - 1) / a.per;
-      if (a.splits == 1) a.part = nullptr;
     }
+    a.steps = steps_of(p.form, ma, p.planes);
     a.step_inner = (ma.S + BK - 1) / BK;
     a.b_samples = mb.B;
     if (p.planes == 2) {                     // (a plane's samples behind the other's)
@@ -764,7 +831,7 @@ int tc_product(const Product& p, float* scratch, cudaStream_t st) {
     }
   }
   // how results leave, and (boxes) whether they lie so that all samples' rows can be taken for one's
-  const bool slopes = p.e.kind >= kSlope, boxes = !a.part && !p.e.gate && !p.e.residual && !p.e.perm && !slopes;
+  const bool slopes = p.e.kind >= kSlope, boxes = !p.e.gate && !p.e.residual && !p.e.perm && !slopes;
   const bool gated = p.e.kind == kGated;
   Matrix out{p.e.out, p.M / p.e.S, p.e.S, p.e.cols, p.e.inner, p.e.ob, p.e.ot, p.e.oh};
   Matrix kept{p.e.kept, out.B, out.S, a.wide, a.wide, (long long)out.S * a.wide, a.wide, 0};
@@ -773,6 +840,7 @@ int tc_product(const Product& p, float* scratch, cudaStream_t st) {
       ma = folded(ma);
       if (ma.B == 1) { out = folded(out); kept = folded(kept); }
     }
+    a.steps = steps_of(p.form, ma, p.planes);
     a.step_inner = (ma.cols + BK - 1) / BK;
     if (p.planes == 2) {                     // (as a second head)
       ma.cols *= 2;
@@ -786,11 +854,14 @@ int tc_product(const Product& p, float* scratch, cudaStream_t st) {
   a.row_tiles = a.rows_tiles * (p.form == kColsCols ? 1 : ma.B);
   a.col_tiles = (p.N + cols - 1) / cols;
   const long long tiles = (long long)a.row_tiles * a.col_tiles;
-  if (tiles * a.splits > INT32_MAX - 4096 || (a.splits > 1 && (long long)p.M * (p.N / 8) > INT32_MAX - (1 << 24))) return VMOBA_ERR_SHAPE;
-  a.items = (int)(tiles * a.splits);
+  if (tiles > INT32_MAX - 4096) return VMOBA_ERR_SHAPE;
+  const Plan plan = plan_of(tiles, a.steps, !slopes);      // (slopes' sums of rows are of whole sums)
+  a.whole = plan.whole; a.rest = plan.rest; a.per = plan.per; a.splits = plan.splits;
+  a.items = a.whole + a.rest * a.splits;
+  a.part = scratch;
   a.a_inner = ma.inner; a.b_inner = mb.inner;
   a.by_rows_tiles = FastDiv((unsigned)a.rows_tiles);
-  a.by_tiles = FastDiv((unsigned)tiles);
+  a.by_rest = FastDiv((unsigned)std::max(1, a.rest));
   a.by_group = FastDiv((unsigned)(8 * a.col_tiles));
   a.by_a_inner = FastDiv((unsigned)ma.inner); a.by_b_inner = FastDiv((unsigned)mb.inner);
   a.by_step = FastDiv((unsigned)a.step_inner);
