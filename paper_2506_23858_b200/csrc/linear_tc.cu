@@ -47,7 +47,8 @@ struct Shared {
 constexpr int STAGE_BYTES = 2 * HALF;
 constexpr int TURN_BYTES = 32 * STAGE_W * 4;
 constexpr int AHEAD_BYTES = 32 * STAGE_W * 2; // a warp's residual of the box to come
-// How results leave: boxes written by TMA; rows of lanes where gate, residual, another order of the rows or parts are in play; rows again for slopes.
+// How results leave: boxes written by TMA; rows of lanes where gate, residual or another order of the rows are in play; boxes that
+// came by TMA where they are the slopes of an activation.
 enum Store { kBoxes = 0, kRows = 1, kSlopes = 2 };
 __host__ __device__ constexpr int stages_of(int store) { return store == kBoxes ? MOST_STAGES : MOST_STAGES - 1; }
 __host__ __device__ constexpr int smem_of(int store) {
@@ -565,21 +566,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     slices(i, n);
   } else if (warp >= 4 && STORE == kSlopes) {
     // ------------------------------------------------------------------ sums d to d act'(u) and act(u) (gated: d v act'(u), d act(u); act(u) v)
-    // Lane = row; everything comes and goes in boxes by TMA.  (By rows of lanes, 64 or 128 bytes of each: 333 us instead of 277 for 13,440 rows of
-    // 4,104 columns, gated, nearly all of the difference in the stores.)
+    // Lane = row; everything comes and goes in boxes by TMA (by rows of lanes 77 million instructions instead of 50, in the same time).  Results take
+    // the place of what they are made of, box after box of the columns in turns in one of two places: the next one is asked for into the other,
+    // whose results have left.  (A box asked for into the place of one just read, behind no more than the warp's meeting, came before the last
+    // reads of that: they need not have happened when the lanes meet, only before something is done with their values.)
     constexpr bool PAIR = KIND == kSlopeGated;
     constexpr int W = PAIR ? 32 : 64, BOXES = BN / 2 / W, BOX = 32 * 2 * W;      // columns of a box, boxes of a warp, bytes
+    constexpr int IN = (PAIR ? 2 : 1) * BOX;                                     // u and v, then du and dv
+    static_assert(2 * IN + BOX <= TURN_BYTES + AHEAD_BYTES, "two boxes and h");
     const int quad = warp & 3, half = (warp - 4) >> 2;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
-    char* const in = turn + (warp - 4) * (TURN_BYTES + AHEAD_BYTES);             // u (and v), then the results: du (and dv) and h
-    char* const results = in + (PAIR ? 2 : 1) * BOX;
+    char* const places = turn + (warp - 4) * (TURN_BYTES + AHEAD_BYTES);
+    char* const again = places + 2 * IN;                                         // h
     uint64_t* const here = &sm->ahead[warp - 4];
     const Epilogue& e = p.e;
-    auto ask = [&](const Item& it, int ch) {           // (one lane; places outside read as zeros)
+    auto ask = [&](const Item& it, int ch, char* to) { // (one lane; places outside read as zeros)
       const int c = it.col + half * (BN / 2) + ch * W, row = it.row + (int)rank * BM + quad * 32;
-      mbar_expect_tx(here, (PAIR ? 2 : 1) * BOX);
-      tma_load_4d(in, &tmKept, here, c, row, 0, 0);
-      if (PAIR) tma_load_4d(in + BOX, &tmKept2, here, c, row, 0, 0);
+      mbar_expect_tx(here, IN);
+      tma_load_4d(to, &tmKept, here, c, row, 0, 0);
+      if (PAIR) tma_load_4d(to + BOX, &tmKept2, here, c, row, 0, 0);
     };
     // 16-byte piece j of the lane's row of a box
     auto piece = [&](char* box, int j) {
@@ -587,7 +592,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     };
     uint32_t n = 0, boxes = 0;
     Item next = item_of<KIND>(p, pair);      // (tiles are whole here)
-    if (lane == 0) ask(next, 0);
+    if (lane == 0) ask(next, 0, places);
     for (int i = pair; i < p.items; i += pairs, ++n) {
       const Item now = next;
       const bool more = i + pairs < p.items;
@@ -613,17 +618,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
           if (lane == 0) arrive_at(first_cta(&sm->acc_empty[n & 1]));
         }
         mbar_wait_warp(here, boxes & 1, abort_flag, p.status);
-        uint4 u4[W / 8], v4[PAIR ? W / 8 : 1];
-#pragma unroll
-        for (int j = 0; j < W / 8; ++j) {
-          u4[j] = *piece(in, j);
-          if (PAIR) v4[j] = *piece(in + BOX, j);
-        }
-        __syncwarp();
-        if (lane == 0) {                     // the next box, and the last results have left
-          if (ch < BOXES - 1) ask(now, ch + 1);
-          else if (more) ask(next, 0);
+        char* const box = places + (boxes & 1) * IN;
+        if (lane == 0) {                     // the last results have left
           bulk_wait_group_read<0>();
+          char* const other = places + (~boxes & 1) * IN;
+          if (ch < BOXES - 1) ask(now, ch + 1, other);
+          else if (more) ask(next, 0, other);
         }
         __syncwarp();
         float dv[PAIR ? W : 1];
@@ -631,8 +631,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 #pragma unroll
           for (int j = 0; j < W / 8; ++j) {
             float h[8], u[8], v[8];
-            const uint32_t uw[4] = {u4[j].x, u4[j].y, u4[j].z, u4[j].w};
-            const uint4 vq = v4[PAIR ? j : 0];
+            const uint4 uq = *piece(box, j), vq = PAIR ? *piece(box + BOX, j) : uq;
+            const uint32_t uw[4] = {uq.x, uq.y, uq.z, uq.w};
             const uint32_t vw[4] = {vq.x, vq.y, vq.z, vq.w};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -653,21 +653,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
                 x *= s.y;
               }
             }
-            auto put = [&](char* box, const float* f) {
-              *piece(box, j) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+            auto put = [&](char* to, const float* f) {
+              *piece(to, j) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
             };
-            put(results, d + 8 * j);
-            if (PAIR) put(results + BOX, dv + (PAIR ? 8 * j : 0));
-            if (e.again) put(results + (PAIR ? 2 : 1) * BOX, h);
+            put(box, d + 8 * j);
+            if (PAIR) put(box + BOX, dv + (PAIR ? 8 * j : 0));
+            if (e.again) put(again, h);
           }
         });
         fence_async_proxy();
         __syncwarp();
         if (lane == 0) {
           if (row < p.Sm && c < p.N) {
-            tma_store_4d(&tmOut, results, c, row, 0, 0);
-            if (PAIR) tma_store_4d(&tmOut2, results + BOX, c, row, 0, 0);
-            if (e.again) tma_store_4d(&tmAgain, results + (PAIR ? 2 : 1) * BOX, c, row, 0, 0);
+            tma_store_4d(&tmOut, box, c, row, 0, 0);
+            if (PAIR) tma_store_4d(&tmOut2, box + BOX, c, row, 0, 0);
+            if (e.again) tma_store_4d(&tmAgain, again, c, row, 0, 0);
           }
           bulk_commit_group();
         }
