@@ -87,7 +87,7 @@ struct Prep {
   const int* inv;                            // place in the order of x of every token of d_out, or (by_place: a sample is one group, so that
   bool by_place;                             // its rows come in any order) token of d_out of every place
   void* du;                                  // as kept
-  void* du_low;                              // what du's rounding left (not with kept)
+  void* du_low;                              // what du's rounding left
   void* y;                                   // act(kept) again, [rows, cols]
   float* part_b;                             // [chunk][cols or 2 cols]
   float* part_g;                             // [chunk][cols]
@@ -174,6 +174,11 @@ __global__ void __launch_bounds__(256, GATED ? 2 : 3) prep_kernel(Prep p) {
           });
           if (p.y) store_vec<8>(static_cast<T*>(p.y) + r * p.cols + c, y);
           if (GATED && p.du) store_vec<8>(static_cast<T*>(p.du) + r * wide + p.cols + c, v);
+          if (GATED && sizeof(T) == 2 && p.du_low) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] -= to_f32<T>(from_f32<T>(v[i]));
+            store_vec<8>(static_cast<T*>(p.du_low) + r * wide + p.cols + c, v);
+          }
         } else if (p.gate) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) d[i] *= gate[i];
@@ -181,7 +186,7 @@ __global__ void __launch_bounds__(256, GATED ? 2 : 3) prep_kernel(Prep p) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) sb[i] += d[i];
         if (p.du) store_vec<8>(static_cast<T*>(p.du) + r * wide + c, d);
-        if (p.du_low) {
+        if (sizeof(T) == 2 && p.du_low) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) d[i] -= to_f32<T>(from_f32<T>(d[i]));
           store_vec<8>(static_cast<T*>(p.du_low) + r * wide + c, d);
@@ -345,8 +350,8 @@ size_t gradient_scratch(const Dims& D, int planes = 1) {
   Product dx = dx_product(D, du, nullptr, x, nullptr), dw = dw_product(D, du, x, nullptr, nullptr);
   size_t most = std::max(product_scratch(dx), product_scratch(dw));
   if (planes == 2) {
-    dw.planes = 2;
-    most = std::max(most, product_scratch(dw));
+    dx.planes = dw.planes = 2;
+    most = std::max(most, std::max(product_scratch(dx), product_scratch(dw)));
   }
   return most;
 }
@@ -398,6 +403,11 @@ Dims ungrouped(Dims D) {
 // Chunks of a layer's rows at most, with its groups or without.
 size_t most_chunks(const Dims& D) { return (size_t)std::max(chunks_of(D), chunks_of(ungrouped(D))); }
 
+// Planes of a layer's du in bf16.  What its rounding costs the results, as much as their own rounding, is gone in the sums of many; where there
+// are few, a second plane of what the rounding left keeps it out of them, and the products are of a few microseconds with either (two samples of
+// two tokens, 240 channels to 2 x 56: 22 us).
+int planes_of(const Dims& D) { return D.dtype == VMOBA_BF16 && D.rows * (D.wide + D.in) <= 65536 ? 2 : 1; }
+
 struct Scratch {
   int* inv;
   char *du, *dh, *du_up, *h;
@@ -410,10 +420,10 @@ Scratch linear_scratch(const Dims& D, bool backward, void* ws) {
   Scratch s{};
   if (backward) {
     s.inv = c.take<int>(D.heads ? D.S : 0);
-    s.du = c.take<char>((size_t)D.rows * D.wide * D.es);
+    s.du = c.take<char>((size_t)D.rows * D.wide * D.es * planes_of(D));
     s.part_b = c.take<float>(most_chunks(D) * D.wide);
     s.part_g = c.take<float>(most_chunks(D) * D.out);
-    s.product = c.take<float>(gradient_scratch(D));
+    s.product = c.take<float>(gradient_scratch(D, planes_of(D)));
   } else {
     s.product = c.take<float>(forward_scratch(D));
   }
@@ -519,12 +529,15 @@ extern "C" int vmoba_linear_bwd(const vmoba_linear_shape* shape, const void* d_o
   Prep p = prep_of(D, d_out, d_out_strides, gate, gate_strides, acts || dgate ? kept : nullptr);
   // (nothing stands between d_out and du in the simplest layer)
   const bool apart = (acts || gate || perm) && (dx || dweight);
+  const int planes = apart && (acts || gate) ? planes_of(D) : 1;
+  const long long plane = D.rows * D.wide;
+  if (planes == 2) p.du_low = s.du + plane * D.es;
   if (perm && D.G == 1) {
     p.inv = perm;
     p.by_place = true;
   } else if (perm) {
     launch_kernel(no_place_kernel, (unsigned)(4 * sm_count()), 256, 0, st, D.S, s.inv, apart ? reinterpret_cast<uint4*>(s.du) : nullptr,
-                  D.rows * D.wide * D.es / 16);
+                  planes * plane * D.es / 16);
     launch_kernel(place_kernel, (unsigned)((D.S + 255) / 256), 256, 0, st, D.S, perm, s.inv);
     VMOBA_LAUNCH_OK(2);
     p.inv = s.inv;
@@ -532,10 +545,18 @@ extern "C" int vmoba_linear_bwd(const vmoba_linear_shape* shape, const void* d_o
   if (apart || dbias || dgate)
     if (int rc = prepare(D, p, s, apart ? s.du : nullptr, dbias, dgate, st)) return rc;
   const Matrix du = apart ? tokens(s.du, D, D.wide) : raster(d_out, d_out_strides, D, D.out);
-  if (dx)
-    if (int rc = run_product(dx_product(D, du, weight, input(dx, dx_strides, D), dev_status), s.product, st)) return rc;
-  if (dweight)
-    if (int rc = run_product(dw_product(D, du, input(x, x_strides, D), dweight, dev_status), s.product, st)) return rc;
+  if (dx) {
+    Product q = dx_product(D, du, weight, input(dx, dx_strides, D), dev_status);
+    q.planes = planes;
+    q.plane = plane;
+    if (int rc = run_product(q, s.product, st)) return rc;
+  }
+  if (dweight) {
+    Product q = dw_product(D, du, input(x, x_strides, D), dweight, dev_status);
+    q.planes = planes;
+    q.plane = plane;
+    if (int rc = run_product(q, s.product, st)) return rc;
+  }
   VMOBA_GUARDS_CHECK(s.guards, dev_status, st);
   return VMOBA_OK;
 }

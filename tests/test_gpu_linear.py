@@ -280,3 +280,30 @@ def test_refusals():
     ff = FeedForward(1, 4, 64, 72)
     with pytest.raises(ValueError):
         ff.backward(z(1, 4, 64), z(1, 4, 64), z(72, 64), z(64, 72), (None, None), None)
+
+
+@pytest.mark.parametrize("B,S,K,N,act,gated,heads,gt", [
+    (2, 2, 240, 56, "silu", True, 0, -1), (1, 1, 8, 8, "gelu", False, 0, 0), (3, 17, 128, 72, "none", False, 2, 5),
+    (1, 100, 128, 96, "gelu", True, 1, 0), (2, 40, 128, 264, "silu", False, 0, 7),
+])
+def test_few_results_without_the_roundings_between(B, S, K, N, act, gated, heads, gt):
+    # of du there are two planes: what its rounding left is in the results, to 2^-17 of it
+    g = torch.Generator(device="cuda").manual_seed(S + K)
+    wide, tokens = 2 * N if gated else N, max(gt, 0)
+    dev = lambda *s, by=1.0, dt=torch.bfloat16: (torch.randn(s, generator=g, device="cuda") * by).to(dt)
+    x, w, d, kept = dev(B, S, K), dev(wide, K, by=K ** -0.5), dev(B, S, N), dev(B, S, wide)
+    gate = dev(B, -(-S // gt) if gt else 1, N, dt=torch.float32) if gt >= 0 else None
+    order = torch.randperm(S, device="cuda") if heads else None
+    D = lambda t: None if t is None else t.double()
+    op = Linear(vb.make_linear_shape(B, S, K, N, "bf16", act, gated, heads, tokens))
+    xx = x.view(B, S, heads, K // heads).transpose(1, 2).contiguous() if heads else x
+    dx = torch.empty_like(xx)
+    dw, db, dgate = op.backward(d, xx, w, dx, kept=kept, gate=gate, perm=None if order is None else order.to(torch.int32), with_bias=True)
+    (du, due), dg = P.du_of(D(d), D(kept), act, gated, D(gate), tokens, False, order)
+    rounded = due + 2.0 ** -16 * du.abs()
+    for got, (ref, err), what in ((dx.transpose(1, 2).reshape(B, S, K) if heads else dx, P.input_grad(du, rounded, D(w)), "dx"),
+                                  (dw, P.weight_grad(du, rounded, D(x)), "dweight")):
+        half = torch.finfo(got.dtype).eps / 2
+        off = (got.double() - ref).abs()
+        assert bool((off <= half * ref.abs() + (1 + half) * err + torch.finfo(got.dtype).tiny).all()), what
+    op.check_status()
