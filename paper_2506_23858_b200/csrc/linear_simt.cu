@@ -1,7 +1,7 @@
 // Matrix products on the CUDA cores, in fp32: the operators' fp32 form.
 // D tiles of 128 x 128 (gated: 64 columns of either half), 128 x 32 or 64 x 64 by CTAs of as many threads as there are 8 x 8, 8 x 4 or 4 x 4
-// pieces, 16 summed indices at a time through two places in shared memory, the next 16 on their way in registers.  Where tiles are few the
-// summed index is cut into slices, whose sums a second kernel adds in a fixed order.
+// pieces, 16 summed indices at a time through two places in shared memory, the next 16 on their way.  Where tiles are few the summed index is
+// cut into slices, whose sums a second kernel adds in a fixed order.
 #include <algorithm>
 
 #include "linear.cuh"
@@ -12,15 +12,19 @@ namespace {
 
 constexpr int BK = 16;
 
-// Element (row r, column c) of a matrix, four columns at a time; zeros outside.  ROWS: one sample's rows of no heads (places of rows and columns
-// worked out for any matrix took a sixth of the instructions).
+// Where element (row r, column c) of a matrix lies, the first of four columns; nullptr outside.  ROWS: one sample's rows of no heads (places of
+// rows and columns worked out for any matrix took a sixth of the instructions).
 template <typename T, bool ROWS>
-__device__ __forceinline__ float4 fetch4(const Matrix& m, const FastDiv& by_S, const FastDiv& by_inner, int rows, int r, int c) {
-  if (r >= rows || c >= m.cols) return make_float4(0.f, 0.f, 0.f, 0.f);
-  if (ROWS) return load4(static_cast<const T*>(m.p) + r * m.st + c);
+__device__ __forceinline__ const T* place4(const Matrix& m, const FastDiv& by_S, const FastDiv& by_inner, int rows, int r, int c) {
+  if (r >= rows || c >= m.cols) return nullptr;
+  if (ROWS) return static_cast<const T*>(m.p) + r * m.st + c;
   const int b = m.B == 1 ? 0 : by_S.div(r), s = r - b * m.S;
   const int h = m.inner == m.cols ? 0 : by_inner.div(c);
-  return load4(static_cast<const T*>(m.p) + b * m.sb + s * m.st + h * m.sh + (c - h * m.inner));
+  return static_cast<const T*>(m.p) + b * m.sb + s * m.st + h * m.sh + (c - h * m.inner);
+}
+// 16 bytes straight into shared memory; zeros where there is nothing.
+__device__ __forceinline__ void bring(float* to, const float* from, const void* any) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(sm100::smem_u32(to)), "l"(from ? from : any), "r"(from ? 16 : 0) : "memory");
 }
 
 struct Args {
@@ -32,11 +36,11 @@ struct Args {
   Epilogue e;
 };
 
-// (4,096 tokens, 2,048 channels in and out, forward 760 us; with one CTA an SM and 130 registers instead of two and 128 861, with ROWS 837.
-// Backward 1500; with two CTAs 1571, without ROWS 1703.)
+// Bound by the issue of multiply-adds and what stands between them: 4,096 tokens, 2,048 channels in and out, forward 780 us (44 TFLOP/s), backward
+// 1430 (48).  Two CTAs an SM, at 128 registers; operands that need no turning through registers as well 1500.
 // Tiles of TM x TN (gated: TN columns of either half), a thread's piece PM x PN: rows ty * PM + .., columns tx * 4 + j * (TN / (PN / 4)) + ..
 template <typename T, int FORM, int KIND, bool ROWS, int TM, int TN, int PM, int PN>
-__global__ void __launch_bounds__((TM / PM) * (TN / PN), FORM == kRowsRows && TM == 128 ? 512 / ((TM / PM) * (TN / PN)) : 0) product_kernel(Args p) {
+__global__ void __launch_bounds__((TM / PM) * (TN / PN), TM == 128 ? 512 / ((TM / PM) * (TN / PN)) : 0) product_kernel(Args p) {
   if (!grid_begin()) return;
   constexpr int SIDE = TN / PN, THREADS = (TM / PM) * SIDE, GROUPS = PN / 4;
   constexpr bool TWO = KIND == kGated;
@@ -53,51 +57,55 @@ __global__ void __launch_bounds__((TM / PM) * (TN / PN), FORM == kRowsRows && TM
     for (int i = 0; i < PM; ++i)
 #pragma unroll
       for (int j = 0; j < PN; ++j) acc[w][i][j] = 0.f;
-  float4 ra[LA], rb[NB][LB];
-  // an operand's rows run along the tile (rows: four summed indices of a row) or along the summed index (four places of the tile)
+  // An operand's rows run along the tile (rows: four summed indices of a row, turned on their way through registers) or along the summed index
+  // (four places of the tile, straight into shared memory).
   constexpr bool A_ROWS = FORM != kColsCols, B_ROWS = FORM == kRowsRows;
-  auto load = [&](int k0) {
+  float4 ra[A_ROWS ? LA : 1], rb[NB][B_ROWS ? LB : 1];
+  auto load = [&](int k0, int to) {          // (the place `to` is written at once where the operand goes there directly)
 #pragma unroll
     for (int l = 0; l < LA; ++l) {
       const int i = t + l * THREADS;
-      if (A_ROWS) ra[l] = fetch4<T, ROWS>(p.a, p.a_S, p.a_inner, p.a_rows, m0 + i / (BK / 4), k0 + i % (BK / 4) * 4);
-      else ra[l] = fetch4<T, ROWS>(p.a, p.a_S, p.a_inner, p.a_rows, k0 + i / (TM / 4), m0 + i % (TM / 4) * 4);
+      if constexpr (A_ROWS) {
+        const T* from = place4<T, ROWS>(p.a, p.a_S, p.a_inner, p.a_rows, m0 + i / (BK / 4), k0 + i % (BK / 4) * 4);
+        ra[l] = from ? load4(from) : make_float4(0.f, 0.f, 0.f, 0.f);
+      } else {
+        bring(&sA[to][i / (TM / 4)][i % (TM / 4) * 4], place4<T, ROWS>(p.a, p.a_S, p.a_inner, p.a_rows, k0 + i / (TM / 4), m0 + i % (TM / 4) * 4), p.a.p);
+      }
     }
 #pragma unroll
     for (int l = 0; l < LB; ++l) {
       const int i = t + l * THREADS;
 #pragma unroll
       for (int w = 0; w < NB; ++w) {
-        if (B_ROWS) {
+        if constexpr (B_ROWS) {
           const int n = n0 + i / (BK / 4);      // (the factor's rows of the weight follow the gate's)
-          rb[w][l] = fetch4<T, ROWS>(p.b, p.b_S, p.b_inner, w ? 2 * p.N : p.N, n < p.N ? n + w * p.N : 2 * p.N, k0 + i % (BK / 4) * 4);
+          const T* from = place4<T, ROWS>(p.b, p.b_S, p.b_inner, w ? 2 * p.N : p.N, n < p.N ? n + w * p.N : 2 * p.N, k0 + i % (BK / 4) * 4);
+          rb[w][l] = from ? load4(from) : make_float4(0.f, 0.f, 0.f, 0.f);
         } else {
-          rb[w][l] = fetch4<T, ROWS>(p.b, p.b_S, p.b_inner, p.b_rows, k0 + i / (TN / 4), n0 + i % (TN / 4) * 4);
+          bring(&sB[to][w][i / (TN / 4)][i % (TN / 4) * 4], place4<T, ROWS>(p.b, p.b_S, p.b_inner, p.b_rows, k0 + i / (TN / 4), n0 + i % (TN / 4) * 4), p.b.p);
         }
       }
     }
   };
-  auto put = [&](auto& s, bool rows, int i, float4 v) {
-    constexpr int WIDTH = sizeof(s[0]) / 4 - 4;
-    if (rows) {
-      const int r = i / (BK / 4), k = i % (BK / 4) * 4;
-      s[k][r] = v.x; s[k + 1][r] = v.y; s[k + 2][r] = v.z; s[k + 3][r] = v.w;
-    } else {
-      *reinterpret_cast<float4*>(&s[i / (WIDTH / 4)][i % (WIDTH / 4) * 4]) = v;
-    }
+  auto turn = [&](auto& s, int i, float4 v) {
+    const int r = i / (BK / 4), k = i % (BK / 4) * 4;
+    s[k][r] = v.x; s[k + 1][r] = v.y; s[k + 2][r] = v.z; s[k + 3][r] = v.w;
   };
   const int k_first = blockIdx.z * p.per, k_end = min(k_first + p.per, p.K);      // (per is a multiple of BK: nobody reads beyond a slice)
-  load(k_first);
   int at = 0;
+  load(k_first, 0);
   for (int k0 = k_first; k0 < k_end; k0 += BK, at ^= 1) {
+    if constexpr (A_ROWS)
 #pragma unroll
-    for (int l = 0; l < LA; ++l) put(sA[at], A_ROWS, t + l * THREADS, ra[l]);
+      for (int l = 0; l < LA; ++l) turn(sA[at], t + l * THREADS, ra[l]);
+    if constexpr (B_ROWS)
 #pragma unroll
-    for (int l = 0; l < LB; ++l)
+      for (int l = 0; l < LB; ++l)
 #pragma unroll
-      for (int w = 0; w < NB; ++w) put(sB[at][w], B_ROWS, t + l * THREADS, rb[w][l]);
-    __syncthreads();                         // (the place written next was read ahead of this)
-    if (k0 + BK < k_end) load(k0 + BK);
+        for (int w = 0; w < NB; ++w) turn(sB[at][w], t + l * THREADS, rb[w][l]);
+    if constexpr (!A_ROWS || !B_ROWS) asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();                         // (and the place written next was read ahead of this)
+    if (k0 + BK < k_end) load(k0 + BK, at ^ 1);
 #pragma unroll
     for (int k = 0; k < BK; ++k) {
       float a[PM];
@@ -157,8 +165,9 @@ int launch(const Args& a, cudaStream_t st) {
   return a.part ? join<float, KIND>(Slices{a.part, a.M, a.N, KIND == kGated ? 2 * a.N : a.N, a.slices}, a.e, st) : VMOBA_OK;
 }
 
-// Tiles: wide ones where that gives every SM one; of few columns for products that have no more; and slices otherwise, up to four CTAs
-// of the tiles an SM, of 128 summed indices at least.
+// Tiles: of few columns for products that have no more; wide ones where those, cut into slices of 256 summed indices at least for two CTAs an
+// SM, give every SM one and leave little of a tile empty (232 tokens, 3,248 -> 6,960 channels, the product of the input's gradient); small ones otherwise, in slices of 128
+// for up to four CTAs an SM.
 enum Tile { kWide, kNarrow, kSmall };
 struct Cut { Tile tile; int per, slices; };
 Cut cut_of(const Product& p) {
@@ -167,9 +176,11 @@ Cut cut_of(const Product& p) {
   const bool two = p.e.kind == kGated;
   const long long K = p.form == kColsCols ? (long long)p.a.B * p.a.S : p.a.cols;
   auto tiles = [&](int rows, int cols) { return (long long)((p.M + rows - 1) / rows) * ((p.N + cols - 1) / cols); };
-  c.tile = p.N <= 32 && !two && p.M >= 128 ? kNarrow : tiles(128, two ? 64 : 128) >= kSms ? kWide : kSmall;
-  const long long of = c.tile == kNarrow ? tiles(128, 32) : tiles(64, 64);
-  const long long n = c.tile == kWide ? 1 : std::max<long long>(1, std::min<long long>(4 * kSms / of, K / 128));
+  const int cols = two ? 64 : 128;
+  const long long wide = tiles(128, cols), small = tiles(64, 64), cuts = std::max<long long>(1, std::min<long long>(2 * kSms / wide, K / 256));
+  c.tile = p.N <= 32 && !two && p.M >= 128 ? kNarrow : wide * cuts >= kSms && wide * 2 * (cols / 64) * 4 <= small * 5 ? kWide : kSmall;
+  const long long of = c.tile == kNarrow ? tiles(128, 32) : small;
+  const long long n = c.tile == kWide ? cuts : std::max<long long>(1, std::min<long long>(4 * kSms / of, K / 128));
   c.per = (int)((K + n - 1) / n + BK - 1) / BK * BK;
   c.slices = (int)((K + c.per - 1) / c.per);
   return c;
