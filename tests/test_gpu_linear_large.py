@@ -190,3 +190,25 @@ def test_permutations_that_are_none():
             sound[[3, 9, 20]] = False
             assert torch.equal(dx[:, :, sound], ref[:, :, sound]) and not bool(dx[:, :, ~sound].any())
             assert bool(dw.isfinite().all()) and bool(dg.isfinite().all())
+
+
+@pytest.mark.parametrize("B,S,K,N,heads,gt", [(1, 5000, 256, 1544, 2, 700), (2, 1700, 1536, 1536, 0, 0), (3, 3, 136, 1032, 0, -1)])
+def test_residual_that_is_the_output(B, S, K, N, heads, gt):
+    g = torch.Generator(device="cuda").manual_seed(N)
+    x, w, b, res = rnd(g, B, S, K), rnd(g, N, K, by=K ** -0.5), rnd(g, N, by=0.2), rnd(g, B, S, N)
+    gate = rnd(g, B, -(-S // gt) if gt else 1, N, dt=torch.float32) if gt >= 0 else None
+    perm = torch.randperm(S, device="cuda").to(torch.int32) if heads else None
+    op = Linear(vb.make_linear_shape(B, S, K, N, "bf16", "none", False, heads, max(gt, 0)))
+    xx = x.view(B, S, heads, K // heads).transpose(1, 2).contiguous() if heads else x
+    apart, stream = torch.empty_like(res), res.clone()
+    op.forward(xx, w, apart, bias=b, gate=gate, residual=res, perm=perm)
+    op.forward(xx, w, stream, bias=b, gate=gate, residual=stream, perm=perm)
+    assert torch.equal(apart, stream)
+    block = FeedForward(B, S, K, 264, "bf16", "gelu", False, 0)
+    w1, w2 = rnd(g, 264, K, by=K ** -0.5), rnd(g, K, 264, by=264 ** -0.5)
+    apart, stream = torch.empty_like(x), x.clone()
+    block.forward(x, w1, w2, apart, residual=x)
+    block.forward(x, w1, w2, stream, residual=stream)
+    assert torch.equal(apart, stream)
+    op.check_status()
+    block.check_status()
