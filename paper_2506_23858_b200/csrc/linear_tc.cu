@@ -153,9 +153,13 @@ __device__ __forceinline__ Item item_of(const Args& p, int i) {
 }
 
 // Columns of the sums that a tile works out: 256, fewer in the last tile of columns, by 64 (4,104 columns: 16 tiles and a quarter, not 17).
-template <int KIND>
+// Where columns are channels of heads (kColsCols), a box of 64 ends with the head that it begins in, and half of 192 columns begins in the middle
+// of a head: all 256 there.  (Half of 64 begins there too, but needs no more than the box has.)
+template <int FORM, int KIND>
 __device__ __forceinline__ int columns_of(const Args& p, const Item& it) {
-  return KIND == kGated ? BN : min(BN, (p.N - it.col + 63) & ~63);
+  if (KIND == kGated) return BN;
+  const int cols = min(BN, (p.N - it.col + 63) & ~63);
+  return FORM == kColsCols && cols == 192 && p.b_inner < p.N ? BN : cols;
 }
 
 // A warp's half of the columns of a slice of a tile, as they are; lane = row.
@@ -216,7 +220,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         const Item it = item_of<KIND>(p, i);
         const int row = it.row + (int)rank * BM;
         // (the second CTA has the other half of the tile's columns, of the factor's where gated)
-        const int col = KIND == kGated ? it.col + (int)rank * p.N : it.col + (int)rank * (columns_of<KIND>(p, it) / 2);
+        const int col = KIND == kGated ? it.col + (int)rank * p.N : it.col + (int)rank * (columns_of<FORM, KIND>(p, it) / 2);
         for (int k = it.k0; k < it.k1; ++k) {
           if (!mbar_wait(&sm->empty[slot], par, abort_flag, p.status)) break;
           const uint32_t a = smem_u32(smem) + slot * STAGE_BYTES, b = a + HALF, bar = first_cta(&sm->full[slot]);
@@ -262,7 +266,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         const Item it = item_of<KIND>(p, i);
         const int k0 = it.k0, k1 = __reduce_max_sync(0xffffffffu, it.k1);
         const uint32_t acc = tmem + (n & 1) * BN;
-        const uint32_t idesc = __reduce_max_sync(0xffffffffu, make_idesc_bf16(2 * BM, columns_of<KIND>(p, it), A_MN, B_MN));
+        const uint32_t idesc = __reduce_max_sync(0xffffffffu, make_idesc_bf16(2 * BM, columns_of<FORM, KIND>(p, it), A_MN, B_MN));
         mbar_wait_warp(&sm->acc_empty[n & 1], ((n >> 1) & 1) ^ 1, abort_flag, p.status);
         tc_fence_after();
         for (int k = k0; k < k1; ++k) {
