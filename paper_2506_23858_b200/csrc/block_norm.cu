@@ -711,12 +711,14 @@ static int go_fwd(const Dims& D, Params& p, cudaStream_t st) {
 template <typename TS, typename T>
 static int go_bwd(const Cut& c, Params& p, cudaStream_t st) {
   p.cpg = c.cpg; p.chunk = c.chunk;
-  // two rows at least in the ring, d_h not through it where those would not fit (fp32, more than 6,900 channels)
+  // two rows at least in the ring and their parts behind it, d_h not through it where those would not fit (fp32, more than 6,880 channels)
   auto slot = [&](bool dh) {
     return align_up((size_t)p.C * ((dh ? 2 : 1) * sizeof(TS) + (p.y.p ? 2 : 1) * sizeof(T)), 128);
   };
-  p.stage_dh = p.d_h.p && 2 * slot(true) <= (size_t)kSmemMost;
-  const size_t bytes = slot(p.stage_dh != 0), parts = (size_t)c.threads * 2 * sizeof(float2);
+  const size_t parts = (size_t)c.threads * 2 * sizeof(float2);
+  static_assert(2 * kMostChannels * (sizeof(TS) + 2 * sizeof(T)) + 512 * 2 * sizeof(float2) <= kSmemMost, "rows without d_h always fit");
+  p.stage_dh = p.d_h.p && 2 * slot(true) + parts <= (size_t)kSmemMost;
+  const size_t bytes = slot(p.stage_dh != 0);
   p.batch = (int)std::min<size_t>(c.threads <= kBwdNarrow && c.pieces == 1 ? 4 : 2, std::max<size_t>(1, kSmemMost / c.ctas / (2 * bytes + parts)));
   auto go = [&](auto kernel) -> int {
     VMOBA_CUDA_OK(allow_smem(kernel, kSmemMost));
