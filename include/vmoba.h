@@ -448,7 +448,8 @@ typedef struct {
   int32_t gate_tokens;  /* tokens that share a row of the gate; 0: all of a sample                         */
 } vmoba_linear_shape;
 
-/* Scratch of a forward (backward = 0) or backward call, one buffer per call under way; 0 bytes: invalid shape. */
+/* Scratch of a forward (backward = 0) or backward call, one buffer per call under way; 0 bytes: invalid shape.  Exactly 256: the call uses none
+ * of it, so that calls under way at the same time may be given the same; this holds for vmoba_ffn_workspace_bytes too. */
 size_t vmoba_linear_workspace_bytes(const vmoba_linear_shape* shape, int backward);
 int vmoba_linear(const vmoba_linear_shape* shape, const void* x, const int64_t x_strides[2], const void* weight, const void* bias_or_null,
                  const float* gate_or_null, const int64_t gate_strides[2], const void* residual_or_null, const int64_t residual_strides[2],

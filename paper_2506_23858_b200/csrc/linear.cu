@@ -416,6 +416,8 @@ struct Scratch {
   Guards guards;
   size_t bytes;
 };
+// The size that a call states: 256 says that it uses none of them, so that several calls can be given the same; more wherever it uses some.
+size_t stated(const Carver& c) { return c.total() ? std::max<size_t>(c.total(), 512) : 256; }
 Scratch linear_scratch(const Dims& D, bool backward, void* ws) {
   Carver c(ws);
   Scratch s{};
@@ -429,7 +431,7 @@ Scratch linear_scratch(const Dims& D, bool backward, void* ws) {
     s.product = c.take<float>(forward_scratch(D));
   }
   s.guards = c.guards;
-  s.bytes = std::max<size_t>(c.total(), 256);
+  s.bytes = stated(c);
   return s;
 }
 Scratch ffn_scratch(const Dims& D, bool backward, void* ws) {
@@ -450,7 +452,7 @@ Scratch ffn_scratch(const Dims& D, bool backward, void* ws) {
     s.product = c.take<float>(std::max(forward_scratch(up), forward_scratch(down)));
   }
   s.guards = c.guards;
-  s.bytes = std::max<size_t>(c.total(), 256);
+  s.bytes = stated(c);
   return s;
 }
 

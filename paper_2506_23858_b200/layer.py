@@ -230,8 +230,8 @@ class _Rows:
         self._nothing = torch.empty(256, dtype=torch.uint8, device=self.device)      # what calls take that need no scratch
 
     def _scratch(self, n):
-        """A call's own, so that calls on any streams and in any graphs can be under way at the same time."""
-        return self._nothing if n <= 256 else torch.empty(n, dtype=torch.uint8, device=self.device)
+        """A call's own, so that calls on any streams and in any graphs can be under way at the same time (256 bytes: it uses none)."""
+        return self._nothing if n == 256 else torch.empty(n, dtype=torch.uint8, device=self.device)
 
     def check_status(self):
         code = int(self.dev_status.item())
