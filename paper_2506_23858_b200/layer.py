@@ -707,6 +707,8 @@ class SteppedAttention:
             # the dense kernels take [B, heads, S, d].  The tokens stay in raster order: the running maximum that a row's
             # weights are rounded against, and with it the last bits of o, depends on the order of the keys.
             L, one = self.layer, self._one_block
+            if projection is not None:
+                L._projects(projection, projected)
             # (a fresh tensor, not contiguous(): that returns a contiguous tensor as it is, whatever its address, the strides
             # of its dimensions of size one and its type)
             fresh = lambda x: torch.empty(x.shape, dtype=L.q_bm.dtype, device=L.device)
@@ -718,7 +720,6 @@ class SteppedAttention:
                 vb.vmoba_partition_many(one, 0, (q, k, v), (qd, kd, vd), [L.raster_strides(x) for x in (q, k, v)])
             vb.vmoba_full_attn(L.shape, qd, kd, vd, od, self._lse, dev_status=L.dev_status)
             if projection is not None:       # (od has the tokens in raster order)
-                L._projects(projection, projected)
                 projection.forward(od, out=o_out, **projected)
                 return "dense"
             # (an o_out whose elements share memory goes through copy_, which refuses it)
