@@ -40,6 +40,7 @@ struct Args {
   int32_t* status;
 };
 constexpr long long PART = 2ll * BM * BN;    // floats of a slice of a tile
+constexpr int TO_PART = 4;                   // floats at most from a 16-byte boundary, on which scratch begins, to a 32-byte one, as store_part has to have
 
 struct Shared {
   uint64_t full[MOST_STAGES], empty[MOST_STAGES], acc_full[2], acc_empty[2], ahead[EPI_WARPS], drain;
@@ -808,7 +809,7 @@ size_t tc_scratch(const Product& p) {
     Matrix a = p.a;
     if (!apart && a.B > 1) { a.S *= a.B; a.B = 1; }
     const tc::Plan plan = tc::plan_of(tc::tiles_of(p, p.form == kColsCols ? 1 : a.B), tc::steps_of(p.form, a, p.planes), p.e.kind < kSlope);
-    if (plan.splits > 1) most = std::max(most, (size_t)plan.rest * plan.splits * (size_t)tc::PART);
+    if (plan.splits > 1) most = std::max(most, (size_t)plan.rest * plan.splits * (size_t)tc::PART + tc::TO_PART);
   }
   return most;
 }
@@ -864,7 +865,7 @@ int tc_product(const Product& p, float* scratch, cudaStream_t st) {
   const Plan plan = plan_of(tiles, a.steps, !slopes);      // (slopes' sums of rows are of whole sums)
   a.whole = plan.whole; a.rest = plan.rest; a.per = plan.per; a.splits = plan.splits;
   a.items = a.whole + a.rest * a.splits;
-  a.part = scratch;
+  a.part = scratch + reinterpret_cast<uintptr_t>(scratch) % 32 / sizeof(float);      // (0 or TO_PART)
   a.a_inner = ma.inner; a.b_inner = mb.inner;
   a.by_rows_tiles = FastDiv((unsigned)a.rows_tiles);
   a.by_rest = FastDiv((unsigned)std::max(1, a.rest));
