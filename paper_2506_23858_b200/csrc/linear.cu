@@ -136,11 +136,14 @@ __global__ void __launch_bounds__(256, GATED ? 2 : 3) prep_kernel(Prep p) {
         const int t = first + 8 * k;
         row[k] = -1;
         d_in[k].clear();
+        u_in[k].clear();
+        v_in[k].clear();
         if (t >= t1) continue;
         const int other = p.inv ? __ldg(p.inv + t) : t, at = p.by_place ? t : other, from = p.by_place ? other : t;
         if ((unsigned)at >= (unsigned)p.S) continue;
         row[k] = (long long)b * p.S + at;
-        if ((unsigned)from < (unsigned)p.S) d_in[k].load(d_row + from * p.dt);      // (a place without a token has no gradient)
+        if ((unsigned)from >= (unsigned)p.S) continue;      // (a place without a token has no gradient, whatever was kept there)
+        d_in[k].load(d_row + from * p.dt);
         if (p.kept) {
           u_in[k].load(static_cast<const T*>(p.kept) + row[k] * wide + c);
           if (GATED) v_in[k].load(static_cast<const T*>(p.kept) + row[k] * wide + p.cols + c);
