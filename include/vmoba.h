@@ -461,7 +461,7 @@ int vmoba_linear(const vmoba_linear_shape* shape, const void* x, const int64_t x
  * [B, groups, out], contiguous; NULL where one is not wanted.  kept as the forward left it: needed with an activation, gated, and for dgate.
  * du, the gradient of the product, is rounded to the layer's type ahead of dx and dweight; dbias and dgate are sums of unrounded
  * values.  The results repeat bit for bit.
- * Places of x outside [0, S) have a dx of zeros and no part in the sums, whatever kept has there; x has to be finite there, since dweight
+ * Places of x that perm sends outside [0, S) have a dx of zeros and no part in the sums, whatever kept has there; x has to be finite there, since dweight
  * adds up its products with zeros.
  */
 int vmoba_linear_bwd(const vmoba_linear_shape* shape, const void* d_out, const int64_t d_out_strides[2], const void* x,

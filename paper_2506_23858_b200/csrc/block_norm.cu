@@ -280,7 +280,8 @@ __global__ void __launch_bounds__(P == 1 ? kFwdThreads : 512, 1) norm_fwd_kernel
       }
       if (p.out.p) s_part[r * tpr + l] = sums.part(layer, h[r], mine, inv_n);
     }
-    __syncthreads();                         // (everybody has read the batch)
+    sm100::fence_async_proxy();              // (the thread's reads of the batch come ahead of the copy that takes its place, ..
+    __syncthreads();                         //  .. all of them)
     if (threadIdx.x == 0) ask(k + 2);
     if (!p.out.p) continue;
     for (int r = warp; r < n; r += warps) {
@@ -510,7 +511,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_bwd_kern
         }
       }
     }
-    __syncthreads();                         // (everybody has read the batch and its sums)
+    sm100::fence_async_proxy();              // (as in the forward)
+    __syncthreads();
     if (threadIdx.x == 0) ask(k + 2);
   }
   if (!p.part) return;
