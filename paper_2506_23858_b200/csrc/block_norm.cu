@@ -29,9 +29,8 @@ struct Rows {
   long long sb, st;
 };
 struct Params {
-  int B, S, G, gt, C, pieces, rows;
+  int S, G, gt, C, pieces;
   int norm, post;
-  FastDiv by_S, by_gt;
   float eps, mean;                           // mean: 1 / C
   Rows x, y, h, out;                         // forward; backward: h, y
   Rows d_out, d_h, dx, dy;
@@ -655,9 +654,8 @@ static bool take_params(Params* p, const vmoba_norm_params* m, const Dims& D) {
 }
 static Params params_of(const vmoba_norm_shape* s, const Dims& D) {
   Params p = {};
-  p.B = D.B; p.S = D.S; p.G = D.G; p.gt = D.gt; p.C = D.C; p.pieces = D.C / 8; p.rows = D.B * D.S;
+  p.S = D.S; p.G = D.G; p.gt = D.gt; p.C = D.C; p.pieces = D.C / 8;
   p.norm = s->norm; p.post = s->post_norm; p.eps = s->eps; p.mean = 1.f / (float)D.C;
-  p.by_S = FastDiv((unsigned)D.S); p.by_gt = FastDiv((unsigned)D.gt);
   return p;
 }
 
