@@ -460,7 +460,8 @@ int vmoba_linear(const vmoba_linear_shape* shape, const void* x, const int64_t x
  * Its gradients (the residual's is d_out itself): dx in the order of x, dweight and dbias of the layer's type, dgate fp32
  * [B, groups, out], contiguous; NULL where one is not wanted.  kept as the forward left it: needed with an activation, gated, and for dgate.
  * du, the gradient of the product, is rounded to the layer's type ahead of dx and dweight; dbias and dgate are sums of unrounded
- * values.  The results repeat bit for bit.
+ * values.  The results repeat bit for bit.  Small bf16 calls go on with what that rounding leaves too, so that du is held to 2^-16 of it: those with
+ * B * S * (in + rows of the weight) <= 2^16, in * rows of the weight <= 2^22 and rows of the weight <= 2^13.
  * Places of x that perm sends outside [0, S) have a dx of zeros and no part in the sums, whatever kept has there; x has to be finite there, since dweight
  * adds up its products with zeros.
  */

@@ -407,10 +407,15 @@ Dims ungrouped(Dims D) {
 // Chunks of a layer's rows at most, with its groups or without.
 size_t most_chunks(const Dims& D) { return (size_t)std::max(chunks_of(D), chunks_of(ungrouped(D))); }
 
-// Planes of a layer's du in bf16.  What its rounding costs the results, as much as their own rounding, is gone in the sums of many; where there
-// are few, a second plane of what the rounding left keeps it out of them, and the products are of a few microseconds with either (two samples of
-// two tokens, 240 channels to 2 x 56: 22 us).
-int planes_of(const Dims& D) { return D.dtype == VMOBA_BF16 && D.rows * (D.wide + D.in) <= 65536 ? 2 : 1; }
+// Planes of a layer's du in bf16.  Its rounding adds as much to the error of dx and dweight as their own has, however many terms their sums are of: root
+// mean square against 64 bits 2.35e-3 at 128 tokens as at 32,760, and 1.66e-3, their own alone, with a second plane of what the rounding left.
+// That doubles the products (13,440 tokens, 1,536 channels in and out: 122 us and 208), so it is there where it costs nothing: the host takes
+// 28 to 31 us for a call and the device 11 to 28 with both planes (0.4 to 7 less with one, which is what a graph of such calls would gain).
+// Beyond it shows: one token, 8,192 channels in and out 84 us a call and 103, 8 to 65,528 channels 36 and 46.
+int planes_of(const Dims& D) {
+  const bool few = D.rows * (D.wide + D.in) <= 1 << 16 && (long long)D.wide * D.in <= 1 << 22 && D.wide <= 1 << 13;
+  return D.dtype == VMOBA_BF16 && few ? 2 : 1;
+}
 
 struct Scratch {
   int* inv;
@@ -622,7 +627,7 @@ extern "C" int vmoba_ffn_bwd(const vmoba_linear_shape* shape, const void* d_out,
   up = ungrouped(up);
   VMOBA_GUARDS_ARM(s.guards, st);
   // Through the gate.  In bf16 what the rounding of gate * d_out leaves is kept as a second plane, and the products of it have both: rounded
-  // here, at h's gradient and at the product's, the results would be twice as far off as their own rounding leaves them.
+  // here and again at the first product's gradient, dx and dw_up would be 1.7 times as far off as their own rounding leaves them, not 1.4.
   const bool bf16 = up.dtype == VMOBA_BF16;
   Prep p = prep_of(down, d_out, d_out_strides, gate, gate_strides, dgate ? kept_down : nullptr);
   const long long plane = down.rows * down.out;
