@@ -21,7 +21,8 @@ using linear::store_vec;
 constexpr int kMostChannels = 8192;
 // Threads of a CTA that has a piece of eight channels for each: by the registers that many leave (85 and 102 each).  The backward has 128 with
 // 256 threads at most, for four rows at a time on two CTAs of an SM (1,536 channels, 32,760 rows: 123 us; three CTAs with 102
-// registers and two rows at a time: 157).
+// registers and two rows at a time: 157).  More channels than either has threads for are two pieces a thread, 512 threads at most: there the backward's 128
+// registers leave 140 to 252 bytes of spills (8,192 channels, 4,000 rows: 196 us, 2.0 TB/s; 5,120 and 13,440: 184 us, 4.5).
 constexpr int kFwdThreads = 768, kBwdThreads = 640, kBwdNarrow = 256;
 
 struct Rows {

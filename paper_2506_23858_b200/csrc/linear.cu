@@ -409,7 +409,7 @@ size_t most_chunks(const Dims& D) { return (size_t)std::max(chunks_of(D), chunks
 
 // Planes of a layer's du in bf16.  Its rounding adds as much to the error of dx and dweight as their own has, however many terms their sums are of: root
 // mean square against 64 bits 2.35e-3 at 128 tokens as at 32,760, and 1.66e-3, their own alone, with a second plane of what the rounding left.
-// That doubles the products (13,440 tokens, 1,536 channels in and out: 122 us and 208), so it is there where it costs nothing: the host takes
+// That doubles the products (a call of 13,440 tokens, 1,536 channels in and out: 122 us and 208), so it is there where it costs nothing: the host takes
 // 28 to 31 us for a call and the device 11 to 28 with both planes (0.4 to 7 less with one, which is what a graph of such calls would gain).
 // Beyond it shows: one token, 8,192 channels in and out 84 us a call and 103, 8 to 65,528 channels 36 and 46.
 int planes_of(const Dims& D) {

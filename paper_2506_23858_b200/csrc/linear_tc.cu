@@ -7,8 +7,8 @@
 // is summed.  An operand whose summed index runs along its rows is read as it lies (MN-major tiles), so that no gradient needs a transpose.
 // gated: the pair's columns are 128 of the gate (first CTA's half) and 128 of the factor.
 // Where tiles would leave SMs idle, the summed index is cut into slices, whose sums a second kernel adds in a fixed order.
-// Bound by the tensor pipe and, in long calls, the power limit: 32,760 tokens, 1,536 -> 4,608 channels 352 us (1.32 PFLOP/s, the pipe 94 % busy in
-// a launch on its own); 5,120 -> 20,480 -> 5,120 10.25 ms (1.34); gradients of 13,440 tokens' weights of 8,208 x 1,536 232 us (1.46).
+// Bound by the tensor pipe and, in long calls, the power limit: 32,760 tokens, 1,536 -> 4,608 channels 361 us (1.29 PFLOP/s; a launch on its own 291,
+// the pipe 94 % busy); 5,120 -> 20,480 -> 5,120 10.5 ms (1.31); gradient of a weight of 8,208 x 1,536 over 13,440 tokens, on its own, 232 us (1.46).
 #include <algorithm>
 
 #include "linear.cuh"

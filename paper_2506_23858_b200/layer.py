@@ -291,7 +291,8 @@ class Linear(_Rows):
     def backward(self, d_out, x, weight, dx_out, kept=None, gate=None, perm=None, with_weight=True, with_bias=False):
         """Gradients of forward(), whose residual's is d_out: writes dx_out (the order of x; None: not wanted), returns those of weight, bias
         and gate (fp32 [B, groups, n_out]), None for what is not wanted or not there.  kept as forward() left it; without an activation, gated product
-        or gate it may be None."""
+        or gate it may be None.  In bf16 the gradient of the product is rounded once ahead of dx_out and the weight's (small calls hold it to
+        2^-16).  Places that perm sends outside the sample have gradients of zero; x has to be finite there."""
         s, dt = self.shape, self.dtype
         d_out, dos = self._rows(d_out, s.n_out, dt, "d_out")
         x, xs = self._input(x, "x")
